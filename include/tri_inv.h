@@ -81,7 +81,8 @@ enum {
 };
 
 /* ---- storage type of K, V, W, U ------------------------------------------ */
-enum { TRI_INV_F32 = 0, TRI_INV_BF16 = 1 };
+enum { TRI_INV_F32 = 0, TRI_INV_BF16 = 1,
+       TRI_INV_E4M3 = 2 /* 8-bit codes with separate scales: outputs of tri_inv_rms_norm only */ };
 
 /* ---- inversion scheme ("method" argument) -------------------------------- */
 enum {
@@ -308,6 +309,76 @@ int tri_inv_selftest_kda_scan_wait_timeout(const void* Q, const void* K, const v
                                            const tri_inv_desc* desc, uint64_t wait_limit_ns, void* cuda_stream);
 
 /*
+ * Linear attention with a decay for each head: the layer without the delta rule's correction (no inverse is needed), and what serving and
+ * training it take.  Per sequence and head, with lambda = exp(log_decay[h]) and S_0 = S0 or zero:
+ *     S_t = lambda S_{t-1} + k_t v_t^T,       o_t = scale S_t^T q_t
+ * computed in the chunk form, tiles of 64 tokens: O = scale (diag(lambda^{i+1}) Q S + ((Q K^T) * D) V) with D_ij = lambda^{i-j} for j <= i,
+ * S <- lambda^n S + (diag(lambda^{n-1-j}) K)^T V.
+ *   Q, K [B,T,H,d_k], V, O [B,T,H,d_v]: device, desc->kv_dtype;  log_decay [H] fp32 device: at most 0 in any model (-inf: the state forgets at
+ *   once), but positive values are computed as given;  S0, S_out [n_sequences,H,d_k,d_v] fp32 device, each may be NULL; S_out may be S0 itself.
+ *   O may not overlap Q, K or V.  All pointers 16-byte aligned.
+ * Dense and packed sequences as in tri_inv_build (lengths from 0 up); desc->C is not used.  d_k <= 256, d_v <= 65536, multiples of 8, else TRI_INV_ERR_UNSUPPORTED
+ * (INVALID_ARG for other multiples).  bf16 with d_k and d_v of 64 or 128 runs on the tensor cores (the state is kept in fp32; its bf16 copy and P are
+ * operands; the increment of a state that is asked for or passed on takes lambda^{n-1-j} v_j as a sum of two bf16 numbers, so that S_out is good to
+ * about 1e-5); every other shape and fp32 storage on the CUDA cores in fp32.  A key or value that is not finite reaches its whole tile's tokens
+ * of its sequence, earlier ones too; nothing reaches another sequence.
+ * Where few heads and long sequences would leave SMs idle, a sequence is cut into segments: their own states first, then joined in order, then all segments at once.
+ * workspace: device memory of at least tri_inv_linear_attention_workspace() bytes (which may be 0: then it may be NULL), 16-byte aligned, contents
+ * arbitrary; nothing else may use it until the call has run.  Nothing is allocated.  Launches on cuda_stream, up to 1 + (n_sequences + 319) / 320 + 2.
+ */
+int tri_inv_linear_attention_workspace(const tri_inv_desc* desc, size_t* bytes);
+int tri_inv_linear_attention(const void* Q, const void* K, const void* V, const float* log_decay, const float* S0, void* O, float* S_out,
+                             float scale, void* workspace, size_t workspace_bytes, const tri_inv_desc* desc, void* cuda_stream);
+
+/*
+ * Its gradient: from dO [B,T,H,d_v] (and dS, the gradient of the final state, or NULL: zero) those of Q, K, V and, where dS0 is not NULL, of S0.
+ * log_decay is a constant of the model and has none.  S0 as in the forward call (NULL: zero).  With weights w_ij = lambda^{i-j}, j <= i:
+ *     dQ_i = scale (sum_j w_ij (dO_i . v_j) k_j + lambda^{i+1} S0 dO_i),      dK_j = scale sum_i w_ij (dO_i . v_j) q_i + lambda^{T-1-j} dS v_j,
+ *     dV_j = scale sum_i w_ij (q_i . k_j) dO_i + lambda^{T-1-j} dS^T k_j,      dS0 = lambda^T dS + scale sum_i lambda^{i+1} q_i dO_i^T
+ * Nothing of the forward call is kept: its states are not needed, dQ has its own.  Types, layouts, sequences, routes and the workspace as there; d_v <= 256
+ * too.  No two outputs may overlap each other or an input (dS0 == dS: INVALID_ARG).
+ */
+int tri_inv_linear_attention_backward_workspace(const tri_inv_desc* desc, size_t* bytes);
+int tri_inv_linear_attention_backward(const void* dO, const void* Q, const void* K, const void* V, const float* log_decay, const float* S0,
+                                      const float* dS, void* dQ, void* dK, void* dV, float* dS0, float scale, void* workspace,
+                                      size_t workspace_bytes, const tri_inv_desc* desc, void* cuda_stream);
+
+/*
+ * One token for each of B rows (desc->T == 1, dense), on states in the slots of a cache, updated in place:
+ *     S <- lambda S + k v^T,      o = scale S^T q        with S = S[slots[b]]
+ *   Q, K [B,H,d_k], V, O [B,H,d_v], desc->kv_dtype;  S [n_slots,H,d_k,d_v] fp32;  slots [B] int32 device, or NULL: row b has slot b (n_slots >= B).
+ * A negative slot is a padded row: its output is zero and no state is touched.  The slots of the other rows have to differ from each other and lie below
+ * n_slots: a row that has an earlier row's slot, or one past the cache, is treated as padding and raises TRI_INV_ERR_INVALID_ARG in the status
+ * word (tri_inv_last_device_status).  fp32 arithmetic; one launch, nothing is allocated.  desc->C is not used.
+ */
+int tri_inv_linear_attention_step(const void* Q, const void* K, const void* V, const float* log_decay, float* S, const int32_t* slots, int32_t n_slots,
+                                  void* O, float scale, const tri_inv_desc* desc, void* cuda_stream);
+
+/*
+ * Root-mean-square norm of rows, as it stands in front of a layer's projections (with the residual's addition) and on each head's output:
+ *     h = x + r,      y = h w / sqrt(mean h^2 + eps)
+ *   X, R (may be NULL: h = x), H (may be NULL; h rounded to the storage type) [rows, n];  w [n];  all of `dtype` (TRI_INV_F32 or TRI_INV_BF16).
+ *   Y [rows, n] of out_dtype: `dtype`, or TRI_INV_E4M3 with scales: group = 128: scales [rows, ceil(n / 128)], one for each 128 columns (the last group may be
+ *   short), group = 0: scales [rows].  scale = max |y| / 448 over the group, 1 where that is 0; the code is y / scale rounded to nearest even.  A
+ *   group with an infinity or a NaN has codes without meaning.  Other groups: TRI_INV_ERR_UNSUPPORTED.  scales is not used with out_dtype == dtype.
+ * y is formed from h as it is in fp32, before it is rounded.  H may be X or R itself; otherwise outputs overlap nothing.  Pointers aligned to their type; rows
+ * of whole 16-byte vectors at 16-byte aligned pointers take the faster kernels.  One launch, nothing is allocated.
+ */
+int tri_inv_rms_norm(const void* X, const void* R, const void* w, void* Y, void* H, float* scales, int64_t rows, int32_t n, int32_t group, float eps,
+                     int dtype, int out_dtype, void* cuda_stream);
+
+/*
+ * Its gradient, from dY, X (the h of the forward call) and w: with rstd = 1 / sqrt(mean x^2 + eps) and u = dy w
+ *     dx = rstd (u - x rstd^2 mean(u x)) + dh,        dw = sum over rows of dy x rstd
+ * dH [rows, n] (may be NULL) is the gradient that reaches h past the norm, along the residual stream.  dX [rows, n] may be dY, X or dH itself; it is the
+ * gradient of both summands of h.  dw [n], summed in fp32 in an order that depends on the sizes alone.  All of `dtype`.  workspace: at least
+ * tri_inv_rms_norm_backward_workspace() bytes of device memory, 16-byte aligned.  Two launches, nothing is allocated.
+ */
+int tri_inv_rms_norm_backward_workspace(int64_t rows, int32_t n, size_t* bytes);
+int tri_inv_rms_norm_backward(const void* dY, const void* X, const void* w, const void* dH, void* dX, void* dw, int64_t rows, int32_t n, float eps,
+                              int dtype, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Fused call with the layer's front end folded in: the kernel takes what the projections produce and
  * does the three producers that otherwise run as separate passes over memory before the inversion
  * (the gating recipe of a Gated-DeltaNet layer; in the paper these are among the kernels its fused
@@ -417,7 +488,8 @@ int tri_inv_count_matrices(const tri_inv_desc* desc, int64_t* out);
  * After the caller has synchronised the stream: reads and clears the device
  * status word of the current device.  *out is TRI_INV_OK, or
  * TRI_INV_ERR_DEVICE_TIMEOUT if a kernel gave up on a bounded wait (the
- * kernel then returned early and its outputs are incomplete).  This call
+ * kernel then returned early and its outputs are incomplete), or
+ * TRI_INV_ERR_INVALID_ARG if tri_inv_linear_attention_step met a slot that it refuses.  This call
  * copies 4 bytes from the device and so synchronises with it.
  */
 int tri_inv_last_device_status(int* out);

@@ -27,7 +27,7 @@ LIB_PATH = os.environ.get("TRI_INV_LIB") or os.path.join(_PKG, "libtri_inv.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CUDA, ERR_DEVICE_TIMEOUT, ERR_TOO_LARGE, ERR_DEBUG_CHECK = 0, 1, 2, 3, 4, 5, 6
 STATIC_MAX_CHUNKS = 16384
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 BLOCK_RECURSIVE, PRODUCT_SERIES, NEWTON_SCHULZ = 0, 1, 2
 LEAF_SERIES = 0x100
 REFINE = 0x200
@@ -43,7 +43,10 @@ def ns_iters(m: int) -> int:
 FORCE_SIMT = 0x10000
 W_DECAY = 0x20000
 
-EXPORTS = ("tri_inv_build", "tri_inv_build_kda", "tri_inv_fused_kda", "tri_inv_chunk_scan_kda", "tri_inv_chunk_scan", "tri_inv_gdn_forward", "tri_inv_gdn_forward_workspace", "tri_inv_wy", "tri_inv_fused", "tri_inv_fused_raw", "tri_inv_fused_packed_static", "tri_inv_count_matrices",
+EXPORTS = ("tri_inv_build", "tri_inv_build_kda", "tri_inv_fused_kda", "tri_inv_chunk_scan_kda", "tri_inv_chunk_scan", "tri_inv_gdn_forward", "tri_inv_gdn_forward_workspace",
+           "tri_inv_linear_attention", "tri_inv_linear_attention_workspace", "tri_inv_linear_attention_backward", "tri_inv_linear_attention_backward_workspace",
+           "tri_inv_linear_attention_step", "tri_inv_rms_norm", "tri_inv_rms_norm_backward", "tri_inv_rms_norm_backward_workspace",
+           "tri_inv_wy", "tri_inv_fused", "tri_inv_fused_raw", "tri_inv_fused_packed_static", "tri_inv_count_matrices",
            "tri_inv_fused_host", "tri_inv_fused_host_workspace", "tri_inv_selftest_wait_timeout", "tri_inv_selftest_scan_wait_timeout", "tri_inv_selftest_kda_wait_timeout", "tri_inv_selftest_bounds_check", "tri_inv_last_device_status", "tri_inv_launch_count", "tri_inv_status_string")
 
 
@@ -116,6 +119,19 @@ def load():
         if hasattr(lib, "tri_inv_selftest_kda_scan_wait_timeout"):
             lib.tri_inv_selftest_kda_scan_wait_timeout.argtypes = [vp, vp, vp, vp, vp, vp, dp, ctypes.c_uint64, vp]
             lib.tri_inv_selftest_kda_scan_wait_timeout.restype = i32
+        if hasattr(lib, "tri_inv_linear_attention"):
+            sz, f32, i64, n32 = ctypes.c_size_t, ctypes.c_float, ctypes.c_int64, ctypes.c_int32
+            szp = ctypes.POINTER(sz)
+            lib.tri_inv_linear_attention_workspace.argtypes = lib.tri_inv_linear_attention_backward_workspace.argtypes = [dp, szp]
+            lib.tri_inv_linear_attention.argtypes = [vp] * 7 + [f32, vp, sz, dp, vp]
+            lib.tri_inv_linear_attention_backward.argtypes = [vp] * 11 + [f32, vp, sz, dp, vp]
+            lib.tri_inv_linear_attention_step.argtypes = [vp] * 6 + [n32, vp, f32, dp, vp]
+            lib.tri_inv_rms_norm.argtypes = [vp] * 6 + [i64, n32, n32, f32, i32, i32, vp]
+            lib.tri_inv_rms_norm_backward_workspace.argtypes = [i64, n32, szp]
+            lib.tri_inv_rms_norm_backward.argtypes = [vp] * 6 + [i64, n32, f32, i32, vp, sz, vp]
+            for f in EXPORTS:
+                if "linear_attention" in f or "rms_norm" in f:
+                    getattr(lib, f).restype = i32
         lib.tri_inv_count_matrices.argtypes = [dp, ctypes.POINTER(ctypes.c_int64)]
         lib.tri_inv_last_device_status.argtypes = [ctypes.POINTER(ctypes.c_int)]
         for f in ("tri_inv_build", "tri_inv_wy", "tri_inv_fused", "tri_inv_count_matrices", "tri_inv_last_device_status"):
@@ -300,6 +316,146 @@ def gdn_forward(Q, K, V, beta, g, C, scale=1.0, S0=None, method=BLOCK_RECURSIVE,
     if rc != OK:
         raise TriInvError("tri_inv_gdn_forward", rc)
     return O, S
+
+
+def _operand(name, t, shape, dtype):
+    """A contiguous tensor of the current CUDA device with this shape and type, or an error that names it."""
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if not t.is_cuda or not t.is_contiguous() or t.device.index != torch.cuda.current_device():
+        raise ValueError("%s must be a contiguous tensor on the current CUDA device" % name)
+    return t.data_ptr()
+
+
+def _optional(name, t, shape, dtype):
+    return None if t is None else _operand(name, t, shape, dtype)
+
+
+def _made_for(t, stream):
+    """A tensor made here, on the current stream's memory, for a call on ``stream``."""
+    if t is not None and stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def _workspace(fn, device, stream, *args):
+    """(tensor or None, bytes) of what the entry point's workspace query asks for."""
+    need = ctypes.c_size_t(0)
+    rc = getattr(load(), fn)(*args, need)
+    if rc != OK:
+        raise TriInvError(fn, rc)
+    if not need.value:
+        return None, 0
+    return _made_for(torch.empty(need.value, dtype=torch.uint8, device=device), stream), need.value
+
+
+def _attention_shapes(Q, V, cu_seqlens):
+    if Q.dim() != 4 or V.dim() != 4:
+        raise ValueError("Q and V must be [B, T, H, d], got %s and %s" % (tuple(Q.shape), tuple(V.shape)))
+    B, T, H, d_k = Q.shape
+    d_v = V.shape[3]
+    desc, keep = make_desc(B, T, H, d_k, d_v, 64, _dtype_code(Q), cu_seqlens)
+    n_seqs = B if keep is None else len(keep) - 1
+    return desc, keep, (B, T, H, d_k), (B, T, H, d_v), (n_seqs, H, d_k, d_v)
+
+
+def linear_attention(Q, K, V, log_decay, scale=1.0, S0=None, cu_seqlens=None, out=None, want_state=True, state_out=None, stream=None):
+    """Linear attention with a decay for each head -> (O, S_final or None): S_t = exp(log_decay) S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t.
+    Q, K [B,T,H,d_k], V [B,T,H,d_v]; log_decay [H] fp32; S0, S_final [sequences,H,d_k,d_v] fp32 (``state_out`` may be S0 itself)."""
+    desc, keep, qk, vo, st = _attention_shapes(Q, V, cu_seqlens)
+    dt, f32 = Q.dtype, torch.float32
+    args = [_operand("Q", Q, qk, dt), _operand("K", K, qk, dt), _operand("V", V, vo, dt), _operand("log_decay", log_decay, (qk[2],), f32), _optional("S0", S0, st, f32)]
+    O = _made_for(torch.empty_like(V), stream) if out is None else out
+    S = state_out
+    if S is None and want_state:
+        S = _made_for(torch.empty(st, dtype=f32, device=V.device), stream)
+    args += [_operand("out", O, vo, dt), _optional("state_out", S, st, f32)]
+    work, need = _workspace("tri_inv_linear_attention_workspace", V.device, stream, desc)
+    rc = load().tri_inv_linear_attention(*args, float(scale), _p(work), need, desc, _stream(stream))
+    if rc != OK:
+        raise TriInvError("tri_inv_linear_attention", rc)
+    return O, S
+
+
+def linear_attention_backward(dO, Q, K, V, log_decay, scale=1.0, S0=None, dS=None, cu_seqlens=None, want_dS0=None, stream=None):
+    """The gradient of ``linear_attention`` -> (dQ, dK, dV, dS0 or None), from dO and, where the final state has one, dS.  ``want_dS0``: by
+    default where S0 is given."""
+    desc, keep, qk, vo, st = _attention_shapes(Q, V, cu_seqlens)
+    dt, f32 = Q.dtype, torch.float32
+    args = [_operand("dO", dO, vo, dt), _operand("Q", Q, qk, dt), _operand("K", K, qk, dt), _operand("V", V, vo, dt),
+            _operand("log_decay", log_decay, (qk[2],), f32), _optional("S0", S0, st, f32), _optional("dS", dS, st, f32)]
+    dQ, dK, dV = (_made_for(torch.empty_like(x), stream) for x in (Q, K, V))
+    dS0 = None
+    if S0 is not None if want_dS0 is None else want_dS0:
+        dS0 = _made_for(torch.empty(st, dtype=f32, device=V.device), stream)
+    work, need = _workspace("tri_inv_linear_attention_backward_workspace", V.device, stream, desc)
+    rc = load().tri_inv_linear_attention_backward(*args, _p(dQ), _p(dK), _p(dV), _p(dS0), float(scale), _p(work), need, desc, _stream(stream))
+    if rc != OK:
+        raise TriInvError("tri_inv_linear_attention_backward", rc)
+    return dQ, dK, dV, dS0
+
+
+def linear_attention_step(Q, K, V, log_decay, S, scale=1.0, slots=None, out=None, stream=None):
+    """One token for each row, on states that lie in the slots of a cache and are updated in place -> O [B,H,d_v].  Q, K [B,H,d_k], V [B,H,d_v],
+    S [n_slots,H,d_k,d_v] fp32, slots [B] int32 (negative: a padded row, output zero) or None: row b has slot b.  Slots that do not differ, or lie past the
+    cache, are left out and show in ``last_device_status``."""
+    if Q.dim() != 3 or V.dim() != 3 or S.dim() != 4:
+        raise ValueError("Q and V must be [B, H, d] and S [slots, H, d_k, d_v], got %s, %s and %s" % (tuple(Q.shape), tuple(V.shape), tuple(S.shape)))
+    B, H, d_k = Q.shape
+    d_v, dt, f32 = V.shape[2], Q.dtype, torch.float32
+    O = _made_for(torch.empty_like(V), stream) if out is None else out
+    if B == 0:
+        return O
+    desc, _ = make_desc(B, 1, H, d_k, d_v, 64, _dtype_code(Q))
+    rc = load().tri_inv_linear_attention_step(
+        _operand("Q", Q, (B, H, d_k), dt), _operand("K", K, (B, H, d_k), dt), _operand("V", V, (B, H, d_v), dt), _operand("log_decay", log_decay, (H,), f32),
+        _operand("S", S, (S.shape[0], H, d_k, d_v), f32), _optional("slots", slots, (B,), torch.int32), S.shape[0], _operand("out", O, (B, H, d_v), dt),
+        float(scale), desc, _stream(stream))
+    if rc != OK:
+        raise TriInvError("tri_inv_linear_attention_step", rc)
+    return O
+
+
+def rms_norm(X, w, eps=1e-6, residual=None, out_dtype=None, group=128, out=None, residual_out=None, stream=None):
+    """Root-mean-square norm over the last dimension -> (Y, H, scales): H = X + residual (None without a residual), Y = H w / sqrt(mean H^2 + eps) in the type of
+    X, or, with ``out_dtype=torch.float8_e4m3fn``, in 8 bits with fp32 scales: one for each ``group`` = 128 columns, or one a row (``group=0``); else scales is None.
+    ``residual_out`` may be X or residual itself."""
+    n, dt = X.shape[-1], X.dtype
+    code = _dtype_code(X)
+    coded = out_dtype is not None and out_dtype != dt
+    if coded and out_dtype != torch.float8_e4m3fn:
+        raise TypeError("out_dtype must be the type of X or torch.float8_e4m3fn, got %s" % out_dtype)
+    rows = X.numel() // n if n else 0
+    Y = _made_for(torch.empty_like(X, dtype=out_dtype), stream) if out is None else out
+    H = residual_out
+    if H is None and residual is not None:
+        H = _made_for(torch.empty_like(X), stream)
+    scales = None
+    if coded:
+        scales = _made_for(torch.empty(X.shape[:-1] + ((-(-n // 128),) if group else (1,)), dtype=torch.float32, device=X.device), stream)
+    rc = load().tri_inv_rms_norm(_operand("X", X, X.shape, dt), _optional("residual", residual, X.shape, dt), _operand("w", w, (n,), dt),
+                                 _operand("out", Y, X.shape, out_dtype if coded else dt), _optional("residual_out", H, X.shape, dt), _p(scales),
+                                 rows, n, int(group), float(eps), code, E4M3 if coded else code, _stream(stream))
+    if rc != OK:
+        raise TriInvError("tri_inv_rms_norm", rc)
+    return Y, H, scales
+
+
+def rms_norm_backward(dY, X, w, eps=1e-6, dH=None, stream=None):
+    """The gradient of ``rms_norm`` -> (dX, dw): X is the H of the forward call (X where there was no residual), dH what reaches it past the norm; dX is the
+    gradient of both summands."""
+    n, dt = X.shape[-1], X.dtype
+    code = _dtype_code(X)
+    rows = X.numel() // n if n else 0
+    dX, dw = _made_for(torch.empty_like(X), stream), _made_for(torch.empty_like(w), stream)
+    work, need = _workspace("tri_inv_rms_norm_backward_workspace", X.device, stream, rows, n)
+    rc = load().tri_inv_rms_norm_backward(_operand("dY", dY, X.shape, dt), _operand("X", X, X.shape, dt), _operand("w", w, (n,), dt), _optional("dH", dH, X.shape, dt),
+                                          _p(dX), _p(dw), rows, n, float(eps), code, _p(work), need, _stream(stream))
+    if rc != OK:
+        raise TriInvError("tri_inv_rms_norm_backward", rc)
+    return dX, dw
 
 
 def wy(A, K, V, beta, cu_seqlens=None, out=None, stream=None):

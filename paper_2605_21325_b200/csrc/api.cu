@@ -36,6 +36,25 @@ int* status_word_for_current_device(cudaError_t* err) {
 
 void count_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
 
+int check_desc(const tri_inv_desc* d, bool need_dv) {
+  if (!d) return TRI_INV_ERR_INVALID_ARG;
+  if (d->B < 1 || d->T < 0 || d->H < 1) return TRI_INV_ERR_INVALID_ARG;
+  if (d->d_k < 8 || (d->d_k & 7)) return TRI_INV_ERR_INVALID_ARG;
+  if (need_dv && (d->d_v < 8 || (d->d_v & 7))) return TRI_INV_ERR_INVALID_ARG;
+  if (d->C != 16 && d->C != 32 && d->C != 64 && d->C != 128) return TRI_INV_ERR_INVALID_ARG;
+  if (d->kv_dtype != TRI_INV_F32 && d->kv_dtype != TRI_INV_BF16) return TRI_INV_ERR_INVALID_ARG;
+  if ((long long)d->B * d->T > 0x7fffffffLL) return TRI_INV_ERR_INVALID_ARG;
+  if (d->cu_seqlens) {
+    if (d->B != 1 || d->n_seqs < 0) return TRI_INV_ERR_INVALID_ARG;
+    if (d->cu_seqlens[0] != 0 || d->cu_seqlens[d->n_seqs] != d->T) return TRI_INV_ERR_INVALID_ARG;
+    for (int s = 0; s < d->n_seqs; ++s)
+      if (d->cu_seqlens[s + 1] < d->cu_seqlens[s]) return TRI_INV_ERR_INVALID_ARG;
+  } else if (d->n_seqs != 0) {
+    return TRI_INV_ERR_INVALID_ARG;
+  }
+  return TRI_INV_OK;
+}
+
 namespace {
 
 // Stream-ordered pool for the packed path's chunk tables.  It keeps what it has allocated (release
@@ -69,25 +88,6 @@ bool log_enabled() {
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-int check_desc(const tri_inv_desc* d, bool need_dv) {
-  if (!d) return TRI_INV_ERR_INVALID_ARG;
-  if (d->B < 1 || d->T < 0 || d->H < 1) return TRI_INV_ERR_INVALID_ARG;
-  if (d->d_k < 8 || (d->d_k & 7)) return TRI_INV_ERR_INVALID_ARG;
-  if (need_dv && (d->d_v < 8 || (d->d_v & 7))) return TRI_INV_ERR_INVALID_ARG;
-  if (d->C != 16 && d->C != 32 && d->C != 64 && d->C != 128) return TRI_INV_ERR_INVALID_ARG;
-  if (d->kv_dtype != TRI_INV_F32 && d->kv_dtype != TRI_INV_BF16) return TRI_INV_ERR_INVALID_ARG;
-  if ((long long)d->B * d->T > 0x7fffffffLL) return TRI_INV_ERR_INVALID_ARG;
-  if (d->cu_seqlens) {
-    if (d->B != 1 || d->n_seqs < 0) return TRI_INV_ERR_INVALID_ARG;
-    if (d->cu_seqlens[0] != 0 || d->cu_seqlens[d->n_seqs] != d->T) return TRI_INV_ERR_INVALID_ARG;
-    for (int s = 0; s < d->n_seqs; ++s)
-      if (d->cu_seqlens[s + 1] < d->cu_seqlens[s]) return TRI_INV_ERR_INVALID_ARG;
-  } else if (d->n_seqs != 0) {
-    return TRI_INV_ERR_INVALID_ARG;
-  }
-  return TRI_INV_OK;
-}
 
 int check_method(int method, bool w_decay_ok = false, bool shift_ok = true) {
   int m = method & TRI_INV_METHOD_MASK;

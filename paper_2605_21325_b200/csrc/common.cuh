@@ -204,6 +204,9 @@ cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t sm
   return e;
 }
 
+// TRI_INV_OK, or what is wrong with a descriptor (api.cu).
+int check_desc(const tri_inv_desc* d, bool need_dv);
+
 // Address of the device status word (0 = ok) of the current device; nullptr and *err on failure.
 int* status_word_for_current_device(cudaError_t* err);
 

@@ -1,0 +1,217 @@
+// extern "C" boundary of linear attention and of the RMS norm: argument checks, the cut into segments, dispatch.
+#include <algorithm>
+#include <cmath>
+
+#include "linear_attention.cuh"
+#include "rms_norm.cuh"
+
+namespace tri_inv {
+namespace {
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+template <class... P>
+bool all_aligned(P... p) { return (aligned16(p) && ...); }
+long long tokens_of(const tri_inv_desc* d) { return d->cu_seqlens ? (long long)d->T : (long long)d->T * d->B; }
+// whether the tensor-core kernel takes the call (without a token there is nothing for it to map)
+bool on_tensor_cores(const tri_inv_desc* d) { return tokens_of(d) > 0 && linear_tc_fits(d->d_k, d->d_v, d->kv_dtype); }
+size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// desc->C plays no part: the tiles are the kernels' own.
+int check_linear(const tri_inv_desc* d) {
+  if (!d) return TRI_INV_ERR_INVALID_ARG;
+  tri_inv_desc x = *d;
+  x.C = 64;
+  const int rc = check_desc(&x, true);
+  if (rc) return rc;
+  return d->d_k > 256 || d->d_v > 65536 ? TRI_INV_ERR_UNSUPPORTED : TRI_INV_OK;
+}
+
+// How a call of `walks` walks is cut.  A cut sequence is read twice where it is not the last segment (k and v, for the states), and joining takes two
+// launches more, so it pays only where the walk of the longest sequence is long beside what the chip could do with every SM at work.
+int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return TRI_INV_ERR_CUDA;
+  const int n_seqs = d->cu_seqlens ? d->n_seqs : d->B;
+  auto len = [&](int s) { return d->cu_seqlens ? d->cu_seqlens[s + 1] - d->cu_seqlens[s] : d->T; };
+  long long tiles = 0, longest = 0;
+  if (d->cu_seqlens) {
+    for (int s = 0; s < n_seqs; ++s) {
+      const long long t = (len(s) + kLinTile - 1) / kLinTile;
+      tiles += t;
+      longest = std::max(longest, t);
+    }
+  } else {
+    longest = (d->T + kLinTile - 1) / kLinTile;
+    tiles = longest * n_seqs;
+  }
+  // blocks that one tile of tokens keeps busy, and blocks that the chip has room for
+  const long long per_tile = (long long)d->H * walks * (tc ? 1 : (std::max(d->d_k, d->d_v) + 63) / 64);
+  const long long room = tc ? sms : 2 * (long long)sms;
+  long long seg = std::max<long long>((tiles * per_tile + room - 1) / room, tc ? 8 : 4);
+  const long long launches = tc ? 10 : 4;   // the two launches more, in tiles
+  if (2 * seg + launches >= longest) seg = std::max<long long>(longest, 1);
+  p->seg_tokens = (int)std::min<long long>(seg * kLinTile, 0x40000000);
+  long long n = 0;
+  if (d->cu_seqlens) {
+    for (int s = 0; s < n_seqs; ++s) n += std::max<long long>(1, ((long long)len(s) + p->seg_tokens - 1) / p->seg_tokens);
+    p->segs_per_seq = 0;
+  } else {
+    p->segs_per_seq = (int)std::max<long long>(1, ((long long)d->T + p->seg_tokens - 1) / p->seg_tokens);
+    n = (long long)p->segs_per_seq * n_seqs;
+  }
+  if (n * d->H * walks * ((std::max(d->d_k, d->d_v) + 63) / 64) > 0x7fffffffLL) return TRI_INV_ERR_INVALID_ARG;   // blocks are counted in 32 bits
+  p->n_segs = (int)n;
+  p->cut = longest * kLinTile > p->seg_tokens;
+  p->table_bytes = d->cu_seqlens ? round_up((size_t)n * sizeof(LinSeg)) : 0;
+  p->state_bytes = p->cut ? round_up((size_t)walks * n * d->H * d->d_k * d->d_v * sizeof(float)) : 0;
+  return TRI_INV_OK;
+}
+
+int run_walks(LinArgs& a, const LinPlan& p, const tri_inv_desc* d, bool tc, void* workspace, cudaStream_t stream) {
+  cudaError_t err;
+  a.status = status_word_for_current_device(&err);
+  if (!a.status) return TRI_INV_ERR_CUDA;
+  a.H = d->H; a.T = d->T;
+  a.seg_tokens = p.seg_tokens; a.segs_per_seq = p.segs_per_seq; a.n_segs = p.n_segs;
+  if (p.n_segs == 0) return TRI_INV_OK;
+  if (d->cu_seqlens) {
+    a.table = (const LinSeg*)workspace;
+    if (launch_linear_table((LinSeg*)workspace, p.seg_tokens, d, stream) != cudaSuccess) return TRI_INV_ERR_CUDA;
+  }
+  auto walk = [&]() { return tc ? launch_linear_tc(a, tokens_of(d), stream) : launch_linear_simt(a, d->kv_dtype, stream); };
+  if (p.cut) {
+    a.seg_state = (float*)((char*)workspace + p.table_bytes);
+    a.state_only = 1;
+    if (walk() != cudaSuccess || launch_linear_join(a, stream) != cudaSuccess) return TRI_INV_ERR_CUDA;
+    a.state_only = 0;
+  }
+  return walk() == cudaSuccess ? TRI_INV_OK : TRI_INV_ERR_CUDA;
+}
+
+int workspace_of(const tri_inv_desc* d, int walks, size_t* bytes) {
+  const int rc = check_linear(d);
+  if (rc) return rc;
+  if (!bytes) return TRI_INV_ERR_INVALID_ARG;
+  LinPlan p;
+  const int e = plan(d, walks, on_tensor_cores(d), &p);
+  if (e) return e;
+  *bytes = p.table_bytes + p.state_bytes;
+  return TRI_INV_OK;
+}
+
+LinWalk make_walk(const void* q, const void* k, const void* v, void* out, const float* s_in, float* s_out, int d_k, int d_v, int back, int turned, float scale) {
+  return LinWalk{q, k, v, out, s_in, s_out, d_k, d_v, back, turned, back ? scale : 1.f, back ? 1.f : scale};
+}
+
+int check_norm(int64_t rows, int32_t n, float eps, int dtype) {
+  if (rows < 0 || rows > 0x7fffffffLL || n < 1 || !(eps >= 0.f) || std::isinf(eps)) return TRI_INV_ERR_INVALID_ARG;
+  return dtype == TRI_INV_F32 || dtype == TRI_INV_BF16 ? TRI_INV_OK : TRI_INV_ERR_INVALID_ARG;
+}
+// whether pointers to values of the storage type are aligned to that type
+template <class... P>
+bool on_type(int dtype, P... p) { return (((reinterpret_cast<uintptr_t>(p) & (dtype == TRI_INV_F32 ? 3u : 1u)) == 0) && ...); }
+
+}  // namespace
+}  // namespace tri_inv
+
+using namespace tri_inv;
+
+extern "C" {
+
+int tri_inv_linear_attention_workspace(const tri_inv_desc* desc, size_t* bytes) { return workspace_of(desc, 1, bytes); }
+
+int tri_inv_linear_attention(const void* Q, const void* K, const void* V, const float* log_decay, const float* S0, void* O, float* S_out,
+                             float scale, void* workspace, size_t workspace_bytes, const tri_inv_desc* desc, void* cuda_stream) {
+  const int rc = check_linear(desc);
+  if (rc) return rc;
+  if (!log_decay || (tokens_of(desc) > 0 && (!Q || !K || !V || !O)) || !all_aligned(Q, K, V, log_decay, S0, O, S_out, workspace)) return TRI_INV_ERR_INVALID_ARG;
+  const bool tc = on_tensor_cores(desc);
+  LinPlan p;
+  const int e = plan(desc, 1, tc, &p);
+  if (e) return e;
+  if (workspace_bytes < p.table_bytes + p.state_bytes || (p.table_bytes + p.state_bytes > 0 && !workspace)) return TRI_INV_ERR_INVALID_ARG;
+  LinArgs a{};
+  a.log_decay = log_decay;
+  a.n_walks = 1;
+  a.walk[0] = make_walk(Q, K, V, O, S0, S_out, desc->d_k, desc->d_v, 0, 0, scale);
+  return run_walks(a, p, desc, tc, workspace, (cudaStream_t)cuda_stream);
+}
+
+int tri_inv_linear_attention_backward_workspace(const tri_inv_desc* desc, size_t* bytes) {
+  if (desc && desc->d_v > 256) return TRI_INV_ERR_UNSUPPORTED;
+  return workspace_of(desc, 3, bytes);
+}
+
+int tri_inv_linear_attention_backward(const void* dO, const void* Q, const void* K, const void* V, const float* log_decay, const float* S0, const float* dS,
+                                      void* dQ, void* dK, void* dV, float* dS0, float scale, void* workspace, size_t workspace_bytes,
+                                      const tri_inv_desc* desc, void* cuda_stream) {
+  const int rc = check_linear(desc);
+  if (rc) return rc;
+  if (desc->d_v > 256) return TRI_INV_ERR_UNSUPPORTED;   // two of the three walks have the value dimension as their key dimension
+  if (!log_decay || (tokens_of(desc) > 0 && (!dO || !Q || !K || !V || !dQ || !dK || !dV)) ||
+      !all_aligned(dO, Q, K, V, log_decay, S0, dS, dQ, dK, dV, dS0, workspace))
+    return TRI_INV_ERR_INVALID_ARG;
+  if (dS0 && dS0 == dS) return TRI_INV_ERR_INVALID_ARG;   // another walk may still have to read dS
+  const bool tc = on_tensor_cores(desc);
+  LinPlan p;
+  const int e = plan(desc, 3, tc, &p);
+  if (e) return e;
+  if (workspace_bytes < p.table_bytes + p.state_bytes || (p.table_bytes + p.state_bytes > 0 && !workspace)) return TRI_INV_ERR_INVALID_ARG;
+  LinArgs a{};
+  a.log_decay = log_decay;
+  a.n_walks = 3;
+  a.walk[0] = make_walk(dO, V, K, dQ, S0, nullptr, desc->d_v, desc->d_k, 0, 1, scale);
+  a.walk[1] = make_walk(V, dO, Q, dK, dS, nullptr, desc->d_v, desc->d_k, 1, 1, scale);
+  a.walk[2] = make_walk(K, Q, dO, dV, dS, dS0, desc->d_k, desc->d_v, 1, 0, scale);
+  return run_walks(a, p, desc, tc, workspace, (cudaStream_t)cuda_stream);
+}
+
+int tri_inv_linear_attention_step(const void* Q, const void* K, const void* V, const float* log_decay, float* S, const int32_t* slots, int32_t n_slots,
+                                  void* O, float scale, const tri_inv_desc* desc, void* cuda_stream) {
+  const int rc = check_linear(desc);
+  if (rc) return rc;
+  if (desc->cu_seqlens || desc->T != 1 || n_slots < 0) return TRI_INV_ERR_INVALID_ARG;
+  if (!slots && n_slots < desc->B) return TRI_INV_ERR_INVALID_ARG;
+  if (!Q || !K || !V || !log_decay || !S || !O || !all_aligned(Q, K, V, log_decay, S, O) || (reinterpret_cast<uintptr_t>(slots) & 3u)) return TRI_INV_ERR_INVALID_ARG;
+  if ((long long)desc->B * desc->H * ((desc->d_v + 31) / 32) > 0x7fffffffLL) return TRI_INV_ERR_INVALID_ARG;
+  LinStepArgs a{Q, K, V, log_decay, S, slots, O, desc->B, desc->H, desc->d_k, desc->d_v, n_slots, desc->kv_dtype == TRI_INV_BF16, scale, nullptr};
+  cudaError_t err;
+  a.status = status_word_for_current_device(&err);
+  if (!a.status) return TRI_INV_ERR_CUDA;
+  return launch_linear_step(a, (cudaStream_t)cuda_stream) == cudaSuccess ? TRI_INV_OK : TRI_INV_ERR_CUDA;
+}
+
+int tri_inv_rms_norm(const void* X, const void* R, const void* w, void* Y, void* H, float* scales, int64_t rows, int32_t n, int32_t group, float eps,
+                     int dtype, int out_dtype, void* cuda_stream) {
+  const int rc = check_norm(rows, n, eps, dtype);
+  if (rc) return rc;
+  if (out_dtype != dtype && out_dtype != TRI_INV_E4M3) return TRI_INV_ERR_INVALID_ARG;
+  const bool coded = out_dtype == TRI_INV_E4M3;
+  if (coded && group != 0 && group != 128) return TRI_INV_ERR_UNSUPPORTED;
+  if (rows == 0) return TRI_INV_OK;
+  if (!X || !w || !Y || (coded && !scales) || !on_type(dtype, X, R, w, H) || (!coded && !on_type(dtype, Y)) || (reinterpret_cast<uintptr_t>(scales) & 3u))
+    return TRI_INV_ERR_INVALID_ARG;
+  RmsNormArgs a{X, R, w, Y, H, scales, rows, n, eps};
+  return launch_rms_norm(a, dtype, !coded ? 0 : group == 128 ? 1 : 2, (cudaStream_t)cuda_stream) == cudaSuccess ? TRI_INV_OK : TRI_INV_ERR_CUDA;
+}
+
+int tri_inv_rms_norm_backward_workspace(int64_t rows, int32_t n, size_t* bytes) {
+  const int rc = check_norm(rows, n, 0.f, TRI_INV_F32);
+  if (rc) return rc;
+  if (!bytes) return TRI_INV_ERR_INVALID_ARG;
+  *bytes = (size_t)kRmsNormPartials * n * sizeof(float);
+  return TRI_INV_OK;
+}
+
+int tri_inv_rms_norm_backward(const void* dY, const void* X, const void* w, const void* dH, void* dX, void* dw, int64_t rows, int32_t n, float eps, int dtype,
+                              void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  const int rc = check_norm(rows, n, eps, dtype);
+  if (rc) return rc;
+  if (!w || !dw || !workspace || !aligned16(workspace) || workspace_bytes < (size_t)kRmsNormPartials * n * sizeof(float)) return TRI_INV_ERR_INVALID_ARG;
+  if (rows > 0 && (!dY || !X || !dX)) return TRI_INV_ERR_INVALID_ARG;
+  if (!on_type(dtype, dY, X, w, dH, dX, dw)) return TRI_INV_ERR_INVALID_ARG;
+  RmsNormBackwardArgs a{dY, X, w, dH, dX, dw, (float*)workspace, rows, n, eps};
+  return launch_rms_norm_backward(a, dtype, (cudaStream_t)cuda_stream) == cudaSuccess ? TRI_INV_OK : TRI_INV_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,286 @@
+// Linear attention with a decay for each head, on the CUDA cores: every shape and storage type, fp32 arithmetic throughout.
+//
+// One CTA walks one (segment, head, slice of 64 value columns) tile after tile of 64 tokens (the walk's formulas: linear_attention.cuh); value
+// columns of the state never mix.  q, k, v, P and the state's slice lie in shared memory; each of the four products is made of
+// thread tiles of 4 x 4 (the state: 4 x 4 for every 64 features), rows read as float4 along the summed index, so that a thread reads 8 x 16 bytes for 64 FMAs.
+// What bounds it: the FMAs (per token 2 d_k + 128 of them for a value column, and as many again for every further slice's P).
+#include <algorithm>
+
+#include "linear_attention.cuh"
+
+namespace tri_inv {
+namespace {
+
+constexpr int L = kLinTile, SL = 64, LDV = SL + 4, kThreadsLin = 256;
+
+struct alignas(8) Half4 { __nv_bfloat162 a, b; };
+template <class T>
+__device__ __forceinline__ float4 load4(const T* p) {
+  if constexpr (sizeof(T) == 4) {
+    return *reinterpret_cast<const float4*>(p);
+  } else {
+    const Half4 x = *reinterpret_cast<const Half4*>(p);
+    const float2 a = __bfloat1622float2(x.a), b = __bfloat1622float2(x.b);
+    return make_float4(a.x, a.y, b.x, b.y);
+  }
+}
+template <class T>
+__device__ __forceinline__ void store4(T* p, float4 x) {
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = x;
+  else *reinterpret_cast<Half4*>(p) = Half4{__floats2bfloat162_rn(x.x, x.y), __floats2bfloat162_rn(x.z, x.w)};
+}
+__device__ __forceinline__ float4 lds4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ void fma4(float (&d)[4], float a, float4 b) {
+  d[0] = fmaf(a, b.x, d[0]); d[1] = fmaf(a, b.y, d[1]); d[2] = fmaf(a, b.z, d[2]); d[3] = fmaf(a, b.w, d[3]);
+}
+
+template <class T, int MK>   // MK: groups of 64 features
+__global__ void __launch_bounds__(kThreadsLin) linear_simt_kernel(const __grid_constant__ LinArgs a, int max_slices) {
+  extern __shared__ __align__(16) float sm[];
+  int x = blockIdx.x;
+  const int slice = x % max_slices; x /= max_slices;
+  const int h = x % a.H; x /= a.H;
+  const int s = x % a.n_segs, wi = x / a.n_segs;
+  const LinWalk w = a.walk[wi];
+  const int c0 = slice * SL;
+  if (c0 >= w.d_v) return;
+  const int dk = w.d_k, ldk = dk + 4;
+  float *sq = sm, *sk = sq + L * ldk, *sv = sk + L * max(ldk, LDV), *sS = sv + L * LDV, *pw = sS + dk * LDV;   // pw: lambda^0 .. lambda^64
+  float* sp = sk;   // P lies where k was: k's other reader, the state's increment, comes first
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  const LinSeg g = lin_segment(a, s);
+  if (a.state_only && !lin_exit_state(a, w, wi, s, g, h)) return;
+  const float l2 = lin_log2_decay(a, h);
+  for (int n = tid; n <= L; n += kThreadsLin) pw[n] = exp2f(l2 * n);
+  bool turned;
+  const float* s_in = lin_entry_state(a, w, wi, s, g, h, &turned);
+  for (int e = tid; e < dk * SL; e += kThreadsLin) {
+    const int d = turned ? e % dk : e / SL, c = turned ? e / dk : e % SL;
+    sS[d * LDV + c] = s_in && c0 + c < w.d_v ? (turned ? s_in[(size_t)(c0 + c) * dk + d] : s_in[(size_t)d * w.d_v + c0 + c]) : 0.f;
+  }
+  const T *Q = (const T*)w.q, *K = (const T*)w.k, *V = (const T*)w.v;
+  T* O = (T*)w.out;
+  const int n_tiles = (g.n + L - 1) / L, b = w.back;
+  for (int it = 0; it < n_tiles; ++it) {
+    const int tile = b ? n_tiles - 1 - it : it, tok0 = g.tok0 + tile * L, rows = min(L, g.n - tile * L);
+    __syncthreads();   // the last tile's readers are through
+    for (int e = tid; e < L * (dk / 4); e += kThreadsLin) {
+      const int i = e / (dk / 4), d = 4 * (e % (dk / 4));
+      const size_t at = ((size_t)(tok0 + i) * a.H + h) * dk + d;
+      const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+      *reinterpret_cast<float4*>(sk + i * ldk + d) = i < rows ? load4(K + at) : zero;
+      if (!a.state_only) *reinterpret_cast<float4*>(sq + i * ldk + d) = i < rows ? load4(Q + at) : zero;
+    }
+    {
+      const int c = 4 * tx;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = ty + 16 * r;
+        const bool in = i < rows && c0 + c < w.d_v;
+        *reinterpret_cast<float4*>(sv + i * LDV + c) = in ? load4(V + ((size_t)(tok0 + i) * a.H + h) * w.d_v + c0 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+    }
+    __syncthreads();
+    // the state's increment, features 64 m + 4 ty .. and columns 4 tx ..
+    float ds[MK][4][4] = {};
+    for (int j = 0; j < rows; ++j) {
+      const float wj = w.k_factor * pw[b ? j + 1 : rows - 1 - j];
+      float4 vv = lds4(sv + j * LDV + 4 * tx);
+      vv.x *= wj; vv.y *= wj; vv.z *= wj; vv.w *= wj;
+#pragma unroll
+      for (int m = 0; m < MK; ++m) {
+        const int d = 64 * m + 4 * ty;
+        if (d < dk) {
+          const float4 kk = lds4(sk + j * ldk + d);
+          fma4(ds[m][0], kk.x, vv); fma4(ds[m][1], kk.y, vv); fma4(ds[m][2], kk.z, vv); fma4(ds[m][3], kk.w, vv);
+        }
+      }
+    }
+    if (!a.state_only) {
+      {   // P, rows ty + 16 r, columns tx + 16 m
+        float acc[4][4] = {};
+        for (int d = 0; d < dk; d += 4) {
+          float4 kk[4];
+#pragma unroll
+          for (int m = 0; m < 4; ++m) kk[m] = lds4(sk + (tx + 16 * m) * ldk + d);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float4 qq = lds4(sq + (ty + 16 * r) * ldk + d);
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+              acc[r][m] = fmaf(qq.x, kk[m].x, fmaf(qq.y, kk[m].y, fmaf(qq.z, kk[m].z, fmaf(qq.w, kk[m].w, acc[r][m]))));
+          }
+        }
+        __syncthreads();   // k has been read
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            const int i = ty + 16 * r, j = tx + 16 * m, gap = b ? j - i : i - j;
+            sp[i * LDV + j] = gap >= 0 ? acc[r][m] * (w.k_factor * pw[gap]) : 0.f;
+          }
+      }
+      __syncthreads();
+      float acc[4][4] = {};   // rows ty + 16 r, columns 4 tx ..
+      for (int d = 0; d < dk; d += 4) {
+        float4 ss[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) ss[m] = lds4(sS + (d + m) * LDV + 4 * tx);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float4 qq = lds4(sq + (ty + 16 * r) * ldk + d);
+          fma4(acc[r], qq.x, ss[0]); fma4(acc[r], qq.y, ss[1]); fma4(acc[r], qq.z, ss[2]); fma4(acc[r], qq.w, ss[3]);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = ty + 16 * r, p = b ? rows - 1 - i : i;
+        const float f = i < rows ? pw[p + 1 - b] : 0.f;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) acc[r][m] *= f;
+      }
+      for (int j = 0; j < L; j += 4) {
+        float4 vv[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) vv[m] = lds4(sv + (j + m) * LDV + 4 * tx);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float4 pp = lds4(sp + (ty + 16 * r) * LDV + j);
+          fma4(acc[r], pp.x, vv[0]); fma4(acc[r], pp.y, vv[1]); fma4(acc[r], pp.z, vv[2]); fma4(acc[r], pp.w, vv[3]);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = ty + 16 * r, c = c0 + 4 * tx;
+        if (i < rows && c < w.d_v)
+          store4(O + ((size_t)(tok0 + i) * a.H + h) * w.d_v + c,
+                 make_float4(w.out_factor * acc[r][0], w.out_factor * acc[r][1], w.out_factor * acc[r][2], w.out_factor * acc[r][3]));
+      }
+      __syncthreads();   // every reader of the entering state is through
+    }
+    // S <- lambda^rows S + the increment; lambda^rows - 1 by expm1f: a factor near 1 that is off by a rounding
+    // would be off by it in every tile, always to the same side
+    const float less = expm1f(l2 * rows * 0.6931471805599453f);
+#pragma unroll
+    for (int m = 0; m < MK; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int d = 64 * m + 4 * ty + r;
+        if (d < dk) {
+          float4 y = lds4(sS + d * LDV + 4 * tx);
+          y.x = fmaf(y.x, less, y.x) + ds[m][r][0]; y.y = fmaf(y.y, less, y.y) + ds[m][r][1];
+          y.z = fmaf(y.z, less, y.z) + ds[m][r][2]; y.w = fmaf(y.w, less, y.w) + ds[m][r][3];
+          *reinterpret_cast<float4*>(sS + d * LDV + 4 * tx) = y;
+        }
+      }
+  }
+  float* s_out = lin_exit_state(a, w, wi, s, g, h);
+  if (s_out) {
+    __syncthreads();
+    for (int e = tid; e < dk * SL; e += kThreadsLin)
+      if (c0 + e % SL < w.d_v) s_out[(size_t)(e / SL) * w.d_v + c0 + e % SL] = sS[(e / SL) * LDV + e % SL];
+  }
+}
+
+template <class T, int MK>
+cudaError_t launch_one(const LinArgs& a, int max_dk, int max_dv, cudaStream_t stream) {
+  const size_t smem = ((size_t)L * (max_dk + 4) + (size_t)L * std::max(max_dk + 4, LDV) + (size_t)(L + max_dk) * LDV + L + 1) * sizeof(float);
+  const cudaError_t e = cudaFuncSetAttribute(linear_simt_kernel<T, MK>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) { (void)cudaGetLastError(); return e; }
+  const int slices = (max_dv + SL - 1) / SL;
+  const long long grid = (long long)slices * a.H * a.n_segs * a.n_walks;
+  if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
+  linear_simt_kernel<T, MK><<<(unsigned)grid, kThreadsLin, smem, stream>>>(a, slices);
+  return launched();
+}
+
+// One block for 256 elements of the states of one (walk, first segment, head): element by element along the sequence's segments.
+__global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant__ LinArgs a, int parts) {
+  int x = blockIdx.x;
+  const int part = x % parts; x /= parts;
+  const int h = x % a.H; x /= a.H;
+  const int s0 = x % a.n_segs, wi = x / a.n_segs;
+  const LinWalk& w = a.walk[wi];
+  LinSeg g = lin_segment(a, s0);
+  if (!(g.ends & 1) || (g.ends & 2)) return;            // one block a sequence, and nothing to join in one of one segment
+  const int size = w.d_k * w.d_v, e = part * 256 + threadIdx.x;
+  if (e >= size) return;
+  int n = 1;
+  while (!(lin_segment(a, s0 + n - 1).ends & 2)) ++n;   // the sequence's segments follow one another
+  const float l2 = lin_log2_decay(a, h);
+  const float* s_in = w.s_in ? w.s_in + ((size_t)g.seq * a.H + h) * size : nullptr;
+  float S = s_in ? s_in[w.s_turned ? (e % w.d_v) * w.d_k + e / w.d_v : e] : 0.f;
+  float* at = a.seg_state + ((size_t)wi * a.n_segs * a.H + h) * size + e;
+  for (int i = 0; i < n; ++i) {
+    const int s = s0 + (w.back ? n - 1 - i : i);
+    const LinSeg gs = lin_segment(a, s);
+    float* p = at + (size_t)s * a.H * size;
+    const float own = i + 1 < n ? *p : 0.f;
+    *p = S;
+    S = fmaf(S, exp2f(l2 * gs.n), own);
+  }
+}
+
+constexpr int kSeqsPerTable = 320;
+struct SeqRange { int32_t tok0, n, seq; };
+struct TableBatch {
+  SeqRange seq[kSeqsPerTable];
+  int32_t n_seqs, first_seg, seg_tokens;
+};
+// A warp per sequence, as in the chunk table (chunk_table.cu): its lanes sum the segments of the sequences before it.
+__global__ void __launch_bounds__(256) linear_table_kernel(LinSeg* tab, const __grid_constant__ TableBatch b) {
+  __shared__ SeqRange seq[kSeqsPerTable];
+  const int lane = threadIdx.x & 31, s = blockIdx.x * 8 + (threadIdx.x >> 5);
+  for (int q = threadIdx.x; q < b.n_seqs; q += 256) seq[q] = b.seq[q];
+  __syncthreads();
+  let_successor_start();
+  wait_for_predecessor();
+  if (s >= b.n_seqs) return;
+  auto segs = [&](int q) { return max(1, (seq[q].n + b.seg_tokens - 1) / b.seg_tokens); };
+  int before = 0;
+  for (int q = lane; q < s; q += 32) before += segs(q);
+#pragma unroll
+  for (int m = 16; m >= 1; m >>= 1) before += __shfl_xor_sync(0xffffffffu, before, m);
+  const int n = segs(s);
+  for (int i = lane; i < n; i += 32) {
+    const int at = i * b.seg_tokens;
+    tab[b.first_seg + before + i] = LinSeg{seq[s].tok0 + at, min(b.seg_tokens, seq[s].n - at), seq[s].seq, (i == 0 ? 1 : 0) | (i == n - 1 ? 2 : 0)};
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_linear_simt(const LinArgs& a, int kv_dtype, cudaStream_t stream) {
+  int dk = 0, dv = 0;
+  for (int i = 0; i < a.n_walks; ++i) { dk = std::max(dk, a.walk[i].d_k); dv = std::max(dv, a.walk[i].d_v); }
+  const bool f32 = kv_dtype == TRI_INV_F32;
+  if (dk <= 64) return f32 ? launch_one<float, 1>(a, dk, dv, stream) : launch_one<__nv_bfloat16, 1>(a, dk, dv, stream);
+  if (dk <= 128) return f32 ? launch_one<float, 2>(a, dk, dv, stream) : launch_one<__nv_bfloat16, 2>(a, dk, dv, stream);
+  return f32 ? launch_one<float, 4>(a, dk, dv, stream) : launch_one<__nv_bfloat16, 4>(a, dk, dv, stream);
+}
+
+cudaError_t launch_linear_join(const LinArgs& a, cudaStream_t stream) {
+  const int parts = (a.walk[0].d_k * a.walk[0].d_v + 255) / 256;
+  const long long grid = (long long)parts * a.H * a.n_segs * a.n_walks;
+  if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
+  linear_join_kernel<<<(unsigned)grid, 256, 0, stream>>>(a, parts);
+  return launched();
+}
+
+cudaError_t launch_linear_table(LinSeg* dev_tab, int seg_tokens, const tri_inv_desc* d, cudaStream_t stream) {
+  TableBatch b;
+  b.seg_tokens = seg_tokens;
+  b.first_seg = 0;
+  for (int s0 = 0; s0 < d->n_seqs; s0 += kSeqsPerTable) {
+    b.n_seqs = std::min(kSeqsPerTable, d->n_seqs - s0);
+    for (int q = 0; q < b.n_seqs; ++q) b.seq[q] = SeqRange{d->cu_seqlens[s0 + q], d->cu_seqlens[s0 + q + 1] - d->cu_seqlens[s0 + q], s0 + q};
+    // the longest first, so that blocks, and the items of a persistent block, end about together
+    std::sort(b.seq, b.seq + b.n_seqs, [](const SeqRange& x, const SeqRange& y) { return x.n != y.n ? x.n > y.n : x.seq < y.seq; });
+    const cudaError_t e = launch_early(linear_table_kernel, dim3((b.n_seqs + 7) / 8), 256, 0, stream, dev_tab, b);
+    if (e != cudaSuccess) return e;
+    for (int q = 0; q < b.n_seqs; ++q) b.first_seg += std::max(1, (b.seq[q].n + seg_tokens - 1) / seg_tokens);
+  }
+  return cudaSuccess;
+}
+
+}  // namespace tri_inv
