@@ -1,5 +1,568 @@
+// Linear attention with a decay for each head, on the tensor cores: bf16, d_k and d_v of 64 or 128 (the walk's formulas: linear_attention.cuh).
+//
+// A persistent CTA per SM walks (walk, segment, head) items tile after tile of 64 tokens.  As in the delta rule's scan (scan_kernel.cu) everything that carries the state
+// lies transposed, value columns as tensor-memory lanes, so that its operands go from registers straight into tensor memory:
+//   QK [64 x 64]    = Q . K^T                 both K-major tiles
+//   DS [d_v x d_k]  = (V~hi + V~lo)^T . K     V~ = lambda^(n-1-j) v_j as two bf16 numbers; the K tile is read MN-major
+//   QS [d_v x 64]   = S^T . Q^T               S^T in bf16
+//   PV [d_v x 64]   = V^T . P^T               P = QK * D in bf16, in shared memory
+// Unlike there nothing but S <- lambda^n S + DS hangs on the tile before: no product is on a dependent chain, and the tensor cores take one after the other.
+// lambda is a constant of the head, so the factors of P, V~ and QS are formed once an item, in the registers of the threads that use them: a thread has
+// the same places of every tile.
+//
+// Warps 0..7 ("state"): lanes 32 (w & 3) .. + 31, half (w >> 2) of the features; S^T in fp32 registers for the whole item.  Warps 8..11 ("value"): V out of its
+// tile into tensor memory, transposed by ldmatrix, plain and scaled.  Warps 12..15 ("output"): P, and O one tile behind.  Then one warp each that issues
+// every product (control), requests the tile copies, and stores O by the copy engine.  Hand-offs are mbarriers with one phase a tile: a commit for a
+// product that is done, an arrival of each warp for an operand that is written or an accumulator that is read.
+//
+// The low half of V~ (256 of a tile's 1,152 cycles of products at d_k = d_v = 128) is left out where the item's last state is not wanted: O takes S in bf16 anyway.
+// Every mbarrier wait is bounded; on expiry the CTA raises the status word, waits for its own products and copies, frees its tensor memory and returns.
 #include "linear_attention.cuh"
+#include "tc_warps.cuh"
+
 namespace tri_inv {
-bool linear_tc_fits(int, int, int) { return false; }
-cudaError_t launch_linear_tc(const LinArgs&, long long, cudaStream_t) { return cudaErrorNotSupported; }
+namespace {
+
+constexpr int L = kLinTile;
+constexpr int kStateWarps = 8, kValue = 8, kOutput = 12, kControlL = 16, kCopyL = 17, kStoreL = 18, kThreadsL = 19 * 32;
+
+struct LinMaps { CUtensorMap q[kLinMaxWalks], k[kLinMaxWalks], v[kLinMaxWalks], o[kLinMaxWalks]; };
+struct LinTcArgs {
+  LinArgs a;
+  int first_walk, n_walks;   // the walks of this launch: those of its head dimensions
+};
+
+template <int DK, int DV>
+struct LinCfg {
+  static constexpr int LG = DV == 128 ? 2 : 1;            // groups of 16 tensor-memory lanes per quadrant in use
+  static constexpr int M = 64 * LG, RPQ = DV / 4;         // value columns (rows here) per quadrant
+  static constexpr int KB = DK / 64, VB = DV / 64;        // boxes of 64 features
+  static constexpr int SH = DK / 2;                       // features of a state warp's half
+  static constexpr int BOX = L * 128;
+  static constexpr int OFF_K = KB * BOX, OFF_V = 2 * KB * BOX, STAGE = (2 * KB + VB) * BOX;
+  static constexpr int STAGES = 4;
+  static constexpr int OFF_P = STAGES * STAGE, OFF_O = OFF_P + L * 128, OFF_BAR = OFF_O + L * DV * 2, SMEM = OFF_BAR + 256;
+  static constexpr int TM_S = 0, TM_V = TM_S + DK / 2, TM_VH = TM_V + 32, TM_VL = TM_VH + 32, TM_DS = TM_VL + 32, TM_QS = TM_DS + DK, TM_PV = TM_QS + 64, TM_QK = TM_PV + 64;
+  static_assert(TM_QK + 64 <= 512 && SMEM <= 232448, "one CTA per SM");
+};
+
+// 32 lanes x 32 columns: a lane's row
+__device__ __forceinline__ void tmem_ld_row32(float (&r)[32], uint32_t taddr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]),
+        "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]),
+        "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st_row16(const uint32_t (&r)[16], uint32_t taddr) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                 "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+}
+
+template <int DK, int DV>
+__global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_constant__ LinMaps maps, const __grid_constant__ LinTcArgs args) {
+  using cfg = LinCfg<DK, DV>;
+  constexpr int LG = cfg::LG;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const LinArgs& a = args.a;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + cfg::OFF_BAR + 192);
+  const uint32_t s0 = smem_u32(smem), sP = s0 + cfg::OFF_P, bars = s0 + cfg::OFF_BAR;
+  // copies: bar_full + 8 stage; stage free again: bar_empty + 8 stage (its products' commit, value warps)
+  // products done (commit): ds, qs, qk, pv.  Operands written: vs (V~, value warps), vr (V), sr (S^T, state warps), pr (P, output warps).
+  // Accumulators read: dsf (DS), qkf (QK), acc (QS and PV).  O's tile: o full, os read.
+  const uint32_t bar_full = bars, bar_empty = bars + 32, b_ds = bars + 64, b_qs = bars + 72, b_qk = bars + 80, b_pv = bars + 88, b_exit = bars + 96,
+                 b_vs = bars + 104, b_vr = bars + 112, b_sr = bars + 120, b_pr = bars + 128, b_dsf = bars + 136, b_qkf = bars + 144, b_acc = bars + 152,
+                 b_o = bars + 160, b_os = bars + 168;
+  const unsigned long long lim = a.wait_limit_ns ? a.wait_limit_ns : kWaitLimitNs;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;   // warp: uniform for the compiler
+  const int quad = warp & 3, half = (warp >> 2) & 1;
+  const int gq = lane >> 2, t2 = 2 * (lane & 3), mi = lane >> 3, mr = lane & 7;
+  const bool misaligned = (s0 & 1023u) != 0;     // never expected; the swizzle pattern would not match the copies
+  wait_for_predecessor();
+  if (warp == kControlL) {
+    if (lane == 0) {
+      for (int b = 0; b < cfg::STAGES; ++b) { mbar_init(bar_full + 8 * b, 1); mbar_init(bar_empty + 8 * b, 5); }
+      for (uint32_t b = b_ds; b <= b_exit; b += 8) mbar_init(b, 1);
+      mbar_init(b_vs, 4); mbar_init(b_vr, 4); mbar_init(b_sr, kStateWarps); mbar_init(b_pr, 4);
+      mbar_init(b_dsf, kStateWarps); mbar_init(b_qkf, 4); mbar_init(b_acc, 4);
+      mbar_init(b_o, 4); mbar_init(b_os, 1);
+      fence_mbar_init();
+    }
+    __syncwarp();
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+  const uint32_t tmem_w = tmem + ((uint32_t)(32 * quad) << 16);   // this warp's lanes, column 0
+  bool failed = misaligned;
+  auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return __all_sync(0xffffffffu, wait_by_warp(bar, parity, lim));
+  };
+  const bool whole = !a.state_only;
+  const int per_seg = a.H * args.n_walks, n_items = a.n_segs * per_seg;
+
+  // Every role walks the same items: the longest first, dealt to the CTAs back and forth.  f(walk, segment, head, n_tiles) returns false to give up.
+  auto for_items = [&](auto&& f) {
+    for (int round = 0; round * (int)gridDim.x < n_items && !failed; ++round) {
+      const int item = round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+      if (item >= n_items) continue;
+      const int s = item / per_seg, wh = item - s * per_seg, wi = args.first_walk + wh / a.H, h = wh % a.H;
+      LinSeg g = lin_segment(a, s);
+      g.tok0 = __shfl_sync(0xffffffffu, g.tok0, 0);   // uniform for the compiler
+      g.n = __shfl_sync(0xffffffffu, g.n, 0);
+      const LinWalk& w = a.walk[wi];
+      float* s_out = lin_exit_state(a, w, wi, s, g, h);
+      if (a.state_only && !s_out) continue;
+      if (!f(w, wi, s, g, h, (g.n + L - 1) / L, s_out)) failed = true;
+    }
+  };
+  auto tile_of = [](const LinWalk& w, int i, int n_tiles) { return w.back ? n_tiles - 1 - i : i; };
+  auto rows_of = [](const LinSeg& g, int tile) { return g.n - tile * L < L ? g.n - tile * L : L; };
+  uint32_t t = 0;   // tiles of this CTA so far, the same in every role: tile t's barriers are in phase t
+  auto stage = [](uint32_t t) { return t % cfg::STAGES; };
+  auto lap = [](uint32_t t) { return (t / cfg::STAGES) & 1u; };
+
+  if (misaligned) {
+  } else if (warp == kControlL) {
+    // ---------------------------------------------------------------- control warp: every tcgen05.mma of the CTA
+    constexpr uint32_t idesc_qk = umma_idesc(64, 64, 0), idesc_ds = umma_idesc(cfg::M, 64, 1), idesc_s = umma_idesc(cfg::M, 64, 0);
+    const uint64_t dQ = umma_desc(s0, 16, 1024), dK = umma_desc(s0 + cfg::OFF_K, 16, 1024), dKm = umma_desc(s0 + cfg::OFF_K, cfg::BOX, 1024), dP = umma_desc(sP, 16, 1024);
+    auto issue_qk = [&](uint32_t t) {
+      const uint32_t st = (stage(t) * cfg::STAGE) >> 4;
+#pragma unroll
+      for (int ks = 0; ks < DK / 16; ++ks) {
+        const uint32_t off = st + (((ks >> 2) * cfg::BOX + (ks & 3) * 32) >> 4);
+        umma_bf16(tmem + cfg::TM_QK, dQ + off, dK + off, idesc_qk, ks > 0);
+      }
+      umma_commit(b_qk);
+    };
+    auto seen = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, mbar_test_wait(bar, parity)); };
+    for_items([&](const LinWalk& w, int, int, const LinSeg&, int, int n_tiles, float* s_out) -> bool {
+      for (int i = 0; i < n_tiles; ++i, ++t) {
+        const uint32_t ph = t & 1, st = (stage(t) * cfg::STAGE) >> 4;
+        if (i == 0) {
+          if (!wait(bar_full + 8 * stage(t), lap(t))) return false;
+          if (whole) {
+            if (t > 0 && !wait(b_qkf, ph ^ 1)) return false;
+            tc_fence_after();
+            issue_qk(t);
+          }
+        }
+        if (!wait(b_vs, ph) || (t > 0 && !wait(b_dsf, ph ^ 1))) return false;
+        tc_fence_after();
+        // self-test (LinArgs::test_stall): the first CTA leaves out this product of its second tile, so that its waits run out
+        const bool stall = a.test_stall && blockIdx.x == 0 && t == 1;
+#pragma unroll
+        for (int fh = 0; fh < cfg::KB; ++fh) {
+#pragma unroll
+          for (int ks = 0; ks < 4; ++ks)
+            if (!stall) umma_bf16_ta(tmem + cfg::TM_DS + 64 * fh, tmem + cfg::TM_VH + 8 * ks, dKm + st + ((fh * cfg::BOX + ks * 2048) >> 4), idesc_ds, ks > 0);
+        }
+        if (s_out && !stall) {
+#pragma unroll
+          for (int fh = 0; fh < cfg::KB; ++fh) {
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              umma_bf16_ta(tmem + cfg::TM_DS + 64 * fh, tmem + cfg::TM_VL + 8 * ks, dKm + st + ((fh * cfg::BOX + ks * 2048) >> 4), idesc_ds, 1u);
+          }
+        }
+        if (!stall) umma_commit(b_ds);
+        if (!whole) {
+          umma_commit(bar_empty + 8 * stage(t));
+          if (i + 1 < n_tiles && !wait(bar_full + 8 * stage(t + 1), lap(t + 1))) return false;
+          continue;
+        }
+        if (!wait(b_sr, ph) || (t > 0 && !wait(b_acc, ph ^ 1))) return false;
+        tc_fence_after();
+#pragma unroll
+        for (int ks = 0; ks < DK / 16; ++ks)
+          umma_bf16_ta(tmem + cfg::TM_QS, tmem + cfg::TM_S + 8 * ks, dQ + st + (((ks >> 2) * cfg::BOX + (ks & 3) * 32) >> 4), idesc_s, ks > 0);
+        umma_commit(b_qs);
+        umma_commit(bar_empty + 8 * stage(t));
+        // the next tile's QK, if its tiles have landed and this tile's QK has been read; otherwise behind PV
+        const bool more = i + 1 < n_tiles;
+        const bool early = more && seen(bar_full + 8 * stage(t + 1), lap(t + 1)) && seen(b_qkf, ph);
+        if (early) { tc_fence_after(); issue_qk(t + 1); }
+        if (!wait(b_pr, ph) || !wait(b_vr, ph)) return false;
+        fence_proxy_async();   // P was written by ordinary stores
+        tc_fence_after();
+#pragma unroll
+        for (int ks = 0; ks < L / 16; ++ks)
+          umma_bf16_ta(tmem + cfg::TM_PV, tmem + cfg::TM_V + 8 * ks, dP + ((ks * 32) >> 4), idesc_s, ks > 0);
+        umma_commit(b_pv);
+        if (more && !early) {
+          if (!wait(bar_full + 8 * stage(t + 1), lap(t + 1)) || !wait(b_qkf, ph)) return false;
+          tc_fence_after();
+          issue_qk(t + 1);
+        }
+      }
+      return true;
+    });
+    if (failed) {   // every product issued so far is waited for, with a limit, before the CTA gives up its memory
+      umma_commit(b_exit);
+      mbar_wait_bounded(b_exit, 0u, lim);
+    }
+  } else if (warp == kCopyL) {
+    // ---------------------------------------------------------------- copy warp
+    for_items([&](const LinWalk& w, int wi, int, const LinSeg& g, int h, int n_tiles, float*) -> bool {
+      for (int i = 0; i < n_tiles; ++i, ++t) {
+        if (t >= cfg::STAGES && !wait(bar_empty + 8 * stage(t), lap(t) ^ 1)) return false;
+        if (lane == 0) {
+          const uint32_t base = s0 + stage(t) * cfg::STAGE, bar = bar_full + 8 * stage(t);
+          const int tok = g.tok0 + tile_of(w, i, n_tiles) * L;
+          mbar_expect_tx(bar, whole ? cfg::STAGE : cfg::STAGE - cfg::KB * cfg::BOX);
+#pragma unroll
+          for (int b = 0; b < cfg::KB; ++b) tma_load_2d(base + cfg::OFF_K + b * cfg::BOX, &maps.k[wi], bar, h * DK + 64 * b, tok);
+#pragma unroll
+          for (int b = 0; b < cfg::VB; ++b) tma_load_2d(base + cfg::OFF_V + b * cfg::BOX, &maps.v[wi], bar, h * DV + 64 * b, tok);
+          if (whole)
+#pragma unroll
+            for (int b = 0; b < cfg::KB; ++b) tma_load_2d(base + b * cfg::BOX, &maps.q[wi], bar, h * DK + 64 * b, tok);
+        }
+        __syncwarp();
+      }
+      return true;
+    });
+    if (failed && lane == 0)   // the copies still on their way into this CTA's shared memory
+      for (uint32_t c = t >= cfg::STAGES ? t - cfg::STAGES : 0; c < t; ++c) mbar_wait_bounded(bar_full + 8 * stage(c), lap(c), lim);
+  } else if (warp < kStateWarps) {
+    // ---------------------------------------------------------------- state warps
+    const int dv = DV == 128 ? 32 * quad + lane : 16 * quad + (lane & 15);
+    const bool mine = DV == 128 || lane < 16;
+    float S[cfg::SH];   // feature SH half + c of value column dv
+    for_items([&](const LinWalk& w, int wi, int s, const LinSeg& g, int h, int n_tiles, float* s_out) -> bool {
+      bool turned;
+      const float* s_in = lin_entry_state(a, w, wi, s, g, h, &turned);
+      if (!s_in) {
+#pragma unroll
+        for (int c = 0; c < cfg::SH; ++c) S[c] = 0.f;
+      } else if (turned) {
+        const float4* p = reinterpret_cast<const float4*>(s_in + (size_t)dv * DK + cfg::SH * half);
+#pragma unroll
+        for (int c = 0; c < cfg::SH; c += 4) {
+          const float4 x = p[c / 4];
+          S[c] = x.x; S[c + 1] = x.y; S[c + 2] = x.z; S[c + 3] = x.w;
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < cfg::SH; ++c) S[c] = s_in[(size_t)(cfg::SH * half + c) * DV + dv];
+      }
+      const float l = lin_log2_decay(a, h) * 0.6931471805599453f;
+      for (int i = 0; i < n_tiles; ++i, ++t) {
+        const uint32_t ph = t & 1;
+        if (whole) {
+          if (t > 0 && !wait(b_qs, ph ^ 1)) return false;   // the operand's last reader
+          tc_fence_after();
+#pragma unroll
+          for (int c = 0; c < cfg::SH; c += 32) {
+            uint32_t r[16];
+#pragma unroll
+            for (int q = 0; q < 16; ++q) r[q] = pack_bf16(S[c + 2 * q], S[c + 2 * q + 1]);
+            tmem_st_row16(r, tmem_w + cfg::TM_S + (cfg::SH * half + c) / 2);
+          }
+          tmem_wait_st();
+          tc_fence_before();
+          warp_arrive(b_sr, lane);
+        }
+        // lambda^rows - 1: a factor near 1 that is off by a rounding would be off by it in every tile, always to the same side
+        const float less = expm1f(l * rows_of(g, tile_of(w, i, n_tiles)));
+        if (!wait(b_ds, ph)) return false;
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < cfg::SH; c += 32) {
+          float ds[32];
+          tmem_ld_row32(ds, tmem_w + cfg::TM_DS + cfg::SH * half + c);
+          tmem_wait_ld();
+          if (c + 32 == cfg::SH) { tc_fence_before(); warp_arrive(b_dsf, lane); }
+#pragma unroll
+          for (int q = 0; q < 32; ++q) S[c + q] = fmaf(S[c + q], less, S[c + q]) + ds[q];
+        }
+      }
+      if (s_out && mine) {
+#pragma unroll
+        for (int c = 0; c < cfg::SH; ++c) s_out[(size_t)(cfg::SH * half + c) * DV + dv] = S[c];
+      }
+      return true;
+    });
+  } else if (warp < kOutput) {
+    // ---------------------------------------------------------------- value warps
+    const int row0 = quad * cfg::RPQ;
+    for_items([&](const LinWalk& w, int, int, const LinSeg& g, int h, int n_tiles, float* s_out) -> bool {
+      const float l2 = lin_log2_decay(a, h);
+      float f[2][4][2];   // lambda^.. of the tokens 32 th + 8 nt + t2, + 1
+      auto factors = [&](int rows) {
+#pragma unroll
+        for (int th = 0; th < 2; ++th)
+#pragma unroll
+          for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              const int j = 32 * th + 8 * nt + t2 + q, n = w.back ? j + 1 : rows - 1 - j;
+              f[th][nt][q] = j < rows ? w.k_factor * exp2f(l2 * n) : 0.f;
+            }
+      };
+      int made_for = 0;
+      for (int i = 0; i < n_tiles; ++i, ++t) {
+        const uint32_t ph = t & 1, base = s0 + stage(t) * cfg::STAGE, sV = base + cfg::OFF_V;
+        const int rows = rows_of(g, tile_of(w, i, n_tiles));
+        if (rows != made_for) { factors(rows); made_for = rows; }
+        if (!wait(bar_full + 8 * stage(t), lap(t))) return false;
+        uint32_t x[LG][2][8];   // V, pairs of tokens
+#pragma unroll
+        for (int lg = 0; lg < LG; ++lg)
+#pragma unroll
+          for (int th = 0; th < 2; ++th)
+#pragma unroll
+            for (int nt = 0; nt < 4; nt += 2) {
+              const int tok = 32 * th + 8 * (nt + (mi >> 1)) + mr, n = row0 + 16 * lg + 8 * (mi & 1);
+              ldmatrix_x4_trans(sV + (n >> 6) * cfg::BOX + tok * 128 + ((((n & 63) >> 3) ^ (tok & 7)) << 4), x[lg][th][2 * nt], x[lg][th][2 * nt + 1], x[lg][th][2 * nt + 2],
+                                x[lg][th][2 * nt + 3]);
+            }
+        if (rows < L) {
+          // Behind the sequence's end lie a neighbour's rows.  V counts as zero there, and zero times a key that is not finite is not zero: the key tile's
+          // rows are cleared too (QK may be reading them: those columns of P are left out by selection)
+#pragma unroll
+          for (int lg = 0; lg < LG; ++lg)
+#pragma unroll
+            for (int th = 0; th < 2; ++th)
+#pragma unroll
+              for (int nt = 0; nt < 4; ++nt) {
+                const int j = 32 * th + 8 * nt + t2;
+                const uint32_t keep = (j < rows ? 0xffffu : 0u) | (j + 1 < rows ? 0xffff0000u : 0u);
+                x[lg][th][2 * nt] &= keep;
+                x[lg][th][2 * nt + 1] &= keep;
+              }
+          for (int e = tid - 32 * kValue; e < (L - rows) * 8 * cfg::KB; e += 128)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + cfg::OFF_K + (e / ((L - rows) * 8)) * cfg::BOX + (rows + (e / 8) % (L - rows)) * 128 + (e & 7) * 16), "r"(0) : "memory");
+          fence_proxy_async();
+        }
+        warp_arrive(bar_empty + 8 * stage(t), lane);
+        if (t > 0 && !wait(b_ds, ph ^ 1)) return false;
+        tc_fence_after();
+#pragma unroll
+        for (int lg = 0; lg < LG; ++lg)
+#pragma unroll
+          for (int th = 0; th < 2; ++th) {
+            uint32_t hi[8], lo[8];
+#pragma unroll
+            for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const uint32_t v = x[lg][th][2 * nt + e];
+                const float y0 = __uint_as_float(v << 16) * f[th][nt][0], y1 = __uint_as_float(v & 0xffff0000u) * f[th][nt][1];
+                const uint32_t p = pack_bf16(y0, y1);
+                hi[2 * nt + e] = p;
+                lo[2 * nt + e] = pack_bf16(y0 - __uint_as_float(p << 16), y1 - __uint_as_float(p & 0xffff0000u));
+              }
+            const uint32_t at = tmem_w + ((uint32_t)(16 * lg) << 16) + 16 * th;
+            tmem_st_packed16(hi, at + cfg::TM_VH);
+            if (s_out) tmem_st_packed16(lo, at + cfg::TM_VL);
+          }
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive(b_vs, lane);
+        if (whole) {
+          if (t > 0 && !wait(b_pv, ph ^ 1)) return false;
+          tc_fence_after();
+#pragma unroll
+          for (int lg = 0; lg < LG; ++lg)
+#pragma unroll
+            for (int th = 0; th < 2; ++th) tmem_st_packed16(x[lg][th], tmem_w + ((uint32_t)(16 * lg) << 16) + 16 * th + cfg::TM_V);
+          tmem_wait_st();
+          tc_fence_before();
+          warp_arrive(b_vr, lane);
+        }
+      }
+      return true;
+    });
+  } else if (warp < kControlL && whole) {
+    // ---------------------------------------------------------------- output warps
+    const int row0 = quad * cfg::RPQ, ia = 16 * quad + gq, ib = ia + 8;
+    for_items([&](const LinWalk& w, int, int, const LinSeg& g, int h, int n_tiles, float*) -> bool {
+      const float l2 = lin_log2_decay(a, h), pv_factor = w.k_factor * w.out_factor;
+      float f[8][4], y[8][2];   // P's factors (negative: masked); QS's of the tokens 8 nt + t2, + 1
+#pragma unroll
+      for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int d = (q < 2 ? ia : ib) - (8 * nt + t2 + (q & 1)), gap = w.back ? -d : d;
+          f[nt][q] = gap >= 0 ? exp2f(l2 * gap) : -1.f;
+        }
+      auto out_factors = [&](int rows) {
+#pragma unroll
+        for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const int i = 8 * nt + t2 + q, p = w.back ? rows - 1 - i : i + 1;
+            y[nt][q] = i < rows ? w.out_factor * exp2f(l2 * p) : 0.f;
+          }
+      };
+      int made_for = 0;
+      // O of tile t (its position in the item: i) out of tensor memory into its tile, [token][column]; behind the wait for its PV
+      auto put_output = [&](uint32_t t, int rows) -> bool {
+        if (rows != made_for) { out_factors(rows); made_for = rows; }
+        if (t > 0 && !wait(b_os, (t - 1) & 1)) return false;   // the last tile's store has read it
+#pragma unroll
+        for (int lg = 0; lg < LG; ++lg) {
+#pragma unroll
+          for (int n0 = 0; n0 < 8; n0 += 4) {
+            const uint32_t at = tmem_w + ((uint32_t)(16 * lg) << 16) + 8 * n0;
+            float pv[4][4], qs[4][4];
+            tmem_ld_16x32(pv, at + cfg::TM_PV);
+            tmem_ld_16x32(qs, at + cfg::TM_QS);
+            tmem_wait_ld();
+#pragma unroll
+            for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) pv[nt][q] = fmaf(pv[nt][q], pv_factor, y[n0 + nt][q & 1] * qs[nt][q]);
+#pragma unroll
+            for (int nt = 0; nt < 4; nt += 2) {
+              const int tok = 8 * (n0 + nt + (mi >> 1)) + mr, col = row0 + 16 * lg + 8 * (mi & 1);
+              stmatrix_x4_trans(s0 + cfg::OFF_O + (col >> 6) * cfg::BOX + tok * 128 + ((((col >> 3) ^ tok) & 7) << 4), pack_bf16(pv[nt][0], pv[nt][1]), pack_bf16(pv[nt][2], pv[nt][3]),
+                                pack_bf16(pv[nt + 1][0], pv[nt + 1][1]), pack_bf16(pv[nt + 1][2], pv[nt + 1][3]));
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) { mbar_arrive(b_acc); mbar_arrive(b_o); }
+        return true;
+      };
+      int last_rows = 0;
+      for (int i = 0; i <= n_tiles && n_tiles > 0; ++i, ++t) {
+        const uint32_t ph = t & 1;
+        const bool more = i < n_tiles;
+        uint32_t wa[8], wb[8];
+        int rows = 0;
+        if (more) {
+          rows = rows_of(g, tile_of(w, i, n_tiles));
+          if (!wait(b_qk, ph)) return false;
+          tc_fence_after();
+          float qk[8][4];
+          tmem_ld_16x64(qk, tmem_w + cfg::TM_QK);
+          tmem_wait_ld();
+          tc_fence_before();
+          warp_arrive(b_qkf, lane);
+#pragma unroll
+          for (int nt = 0; nt < 8; ++nt) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) qk[nt][q] = f[nt][q] < 0.f ? 0.f : qk[nt][q] * f[nt][q];
+            if (rows < L) {   // backwards, a row meets the columns behind the sequence's end
+              const int j = 8 * nt + t2;
+              if (j >= rows) qk[nt][0] = qk[nt][2] = 0.f;
+              if (j + 1 >= rows) qk[nt][1] = qk[nt][3] = 0.f;
+            }
+            wa[nt] = pack_bf16(qk[nt][0], qk[nt][1]);
+            wb[nt] = pack_bf16(qk[nt][2], qk[nt][3]);
+          }
+        }
+        if (t > 0 && !wait(b_pv, ph ^ 1)) return false;   // PV of the tile before is done: its O can be read, and P's tile is free
+        tc_fence_after();
+        if (more) {
+          const int row = 16 * quad + 8 * (mi & 1) + mr;
+#pragma unroll
+          for (int nt = 0; nt < 8; nt += 2) stmatrix_x4(sP + row * 128 + (((nt + (mi >> 1)) ^ (row & 7)) << 4), wa[nt], wb[nt], wa[nt + 1], wb[nt + 1]);
+          warp_arrive(b_pr, lane);   // (the fence for the asynchronous proxy is the control warp's)
+        }
+        if (i > 0 && !put_output(t - 1, last_rows)) return false;
+        last_rows = rows;
+        if (!more) break;   // t stays at the next item's first tile
+      }
+      return true;
+    });
+  } else if (warp == kStoreL && whole) {
+    // ---------------------------------------------------------------- store warp: O's tile to memory
+    for_items([&](const LinWalk& w, int wi, int, const LinSeg& g, int h, int n_tiles, float*) -> bool {
+      for (int i = 0; i < n_tiles; ++i, ++t) {
+        if (!wait(b_o, t & 1)) return false;
+        const int tile = tile_of(w, i, n_tiles), tok0 = g.tok0 + tile * L, rows = rows_of(g, tile);
+        if (rows == L) {
+          if (lane == 0) {
+            fence_proxy_async();   // the tile was written by ordinary stores
+#pragma unroll
+            for (int b = 0; b < cfg::VB; ++b) tma_store_2d(&maps.o[wi], s0 + cfg::OFF_O + b * cfg::BOX, h * DV + 64 * b, tok0);
+            bulk_commit();
+            bulk_wait_read();
+          }
+        } else {
+          __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(w.out) + ((size_t)tok0 * a.H + h) * DV;
+          for (int e = lane; e < rows * (DV / 8); e += 32) {
+            const int tok = e / (DV / 8), pc = e % (DV / 8);
+            *reinterpret_cast<uint4*>(out + (size_t)tok * a.H * DV + 8 * pc) =
+                *reinterpret_cast<const uint4*>(smem + cfg::OFF_O + (pc >> 3) * cfg::BOX + tok * 128 + (((pc ^ tok) & 7) << 4));
+          }
+        }
+        warp_arrive(b_os, lane);
+      }
+      return true;
+    });
+  }
+  if (failed) atomicMax(a.status, (int)TRI_INV_ERR_DEVICE_TIMEOUT);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+template <int DK, int DV>
+cudaError_t launch_one(const LinMaps& maps, const LinTcArgs& args, int sms, cudaStream_t stream) {
+  using cfg = LinCfg<DK, DV>;
+  static std::mutex mu;
+  static bool ready[64] = {false};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  {
+    std::lock_guard<std::mutex> lock(mu);
+    if (!ready[dev]) {
+      if ((e = cudaFuncSetAttribute(linear_tc_kernel<DK, DV>, cudaFuncAttributeMaxDynamicSharedMemorySize, cfg::SMEM)) != cudaSuccess) { (void)cudaGetLastError(); return e; }
+      ready[dev] = true;
+    }
+  }
+  const long long items = (long long)args.a.n_segs * args.a.H * args.n_walks;
+  e = launch_early(linear_tc_kernel<DK, DV>, dim3((unsigned)(items < sms ? items : sms)), kThreadsL, cfg::SMEM, stream, maps, args);
+  return e == cudaSuccess ? launched() : e;
+}
+
+}  // namespace
+
+bool linear_tc_fits(int d_k, int d_v, int kv_dtype) {
+  return kv_dtype == TRI_INV_BF16 && (d_k == 64 || d_k == 128) && (d_v == 64 || d_v == 128);
+}
+
+cudaError_t launch_linear_tc(const LinArgs& a, long long tokens, cudaStream_t stream) {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return cudaErrorUnknown;
+  LinMaps maps;
+  for (int i = 0; i < a.n_walks; ++i) {
+    const LinWalk& w = a.walk[i];
+    if (!make_tmap(&maps.q[i], w.q, tokens, a.H, w.d_k, L) || !make_tmap(&maps.k[i], w.k, tokens, a.H, w.d_k, L) || !make_tmap(&maps.v[i], w.v, tokens, a.H, w.d_v, L) ||
+        !make_tmap(&maps.o[i], w.out, tokens, a.H, w.d_v, L))
+      return cudaErrorUnknown;
+  }
+  // the walks of one launch have the same dimensions: all of them where d_k = d_v, else the last apart
+  LinTcArgs args{a, 0, 0};
+  for (int first = 0; first < a.n_walks; first += args.n_walks) {
+    const LinWalk& w = a.walk[first];
+    args.first_walk = first;
+    args.n_walks = 1;
+    while (first + args.n_walks < a.n_walks && a.walk[first + args.n_walks].d_k == w.d_k && a.walk[first + args.n_walks].d_v == w.d_v) ++args.n_walks;
+    const cudaError_t e = w.d_k == 128 ? (w.d_v == 128 ? launch_one<128, 128>(maps, args, sms, stream) : launch_one<128, 64>(maps, args, sms, stream))
+                                       : (w.d_v == 128 ? launch_one<64, 128>(maps, args, sms, stream) : launch_one<64, 64>(maps, args, sms, stream));
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
 }  // namespace tri_inv
