@@ -45,7 +45,7 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
     tiles = longest * n_seqs;
   }
   // blocks that one tile of tokens keeps busy, and blocks that the chip has room for
-  const long long per_tile = (long long)d->H * walks * (tc ? 1 : (std::max(d->d_k, d->d_v) + 63) / 64);
+  const long long per_tile = (long long)d->H * walks * ((std::max(d->d_k, d->d_v) + 63) / 64);
   const long long room = tc ? sms : 2 * (long long)sms;
   long long seg = std::max<long long>((tiles * per_tile + room - 1) / room, tc ? 8 : 4);
   const long long launches = tc ? 10 : 4;   // the two launches more, in tiles

@@ -30,6 +30,7 @@ struct LinMaps { CUtensorMap q[kLinMaxWalks], k[kLinMaxWalks], v[kLinMaxWalks], 
 struct LinTcArgs {
   LinArgs a;
   int first_walk, n_walks;   // the walks of this launch: those of its head dimensions
+  int slices;                // slices of DV value columns
 };
 
 template <int DK, int DV>
@@ -41,8 +42,9 @@ struct LinCfg {
   static constexpr int BOX = L * 128;
   static constexpr int OFF_K = KB * BOX, OFF_V = 2 * KB * BOX, STAGE = (2 * KB + VB) * BOX;
   static constexpr int STAGES = 4;
-  static constexpr int OFF_P = STAGES * STAGE, OFF_O = OFF_P + L * 128, OFF_BAR = OFF_O + L * DV * 2, SMEM = OFF_BAR + 256;
-  static constexpr int TM_S = 0, TM_V = TM_S + DK / 2, TM_VH = TM_V + 32, TM_VL = TM_VH + 32, TM_DS = TM_VL + 32, TM_QS = TM_DS + DK, TM_PV = TM_QS + 64, TM_QK = TM_PV + 64;
+  static constexpr int OFF_P = STAGES * STAGE, OFF_O = OFF_P + L * 128, OFF_BAR = OFF_O + L * DV * 2,
+                       OFF_F = OFF_BAR + 256, SMEM = OFF_F + 8 * L * 4;   // F: the value and output warps' factors, a table of each warp
+  static constexpr int TM_S = 0, TM_V = TM_S + DK / 2, TM_VH = TM_V + 64, TM_VL = TM_VH + 32, TM_DS = TM_VL + 32, TM_QS = TM_DS + DK, TM_PV = TM_QS + 64, TM_QK = TM_PV + 64;
   static_assert(TM_QK + 64 <= 512 && SMEM <= 232448, "one CTA per SM");
 };
 
@@ -62,6 +64,16 @@ __device__ __forceinline__ void tmem_st_row16(const uint32_t (&r)[16], uint32_t 
                  "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
 }
 
+// Two elements in one instruction, each rounded as by the scalar one: what the loops below issue is what bounds them
+struct Pair { unsigned long long v; };
+__device__ __forceinline__ Pair pair(float x, float y) { Pair p; asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(x), "f"(y)); return p; }
+__device__ __forceinline__ float2 parts(Pair p) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p.v)); return r; }
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) { Pair d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v)); return d; }
+__device__ __forceinline__ Pair add2(Pair a, Pair b) { Pair d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v)); return d; }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return d; }
+__device__ __forceinline__ uint32_t pack_bf16(Pair p) { const float2 x = parts(p); return pack_bf16(x.x, x.y); }
+__device__ __forceinline__ Pair unpack_bf16(uint32_t x) { return pair(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
+
 template <int DK, int DV>
 __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_constant__ LinMaps maps, const __grid_constant__ LinTcArgs args) {
   using cfg = LinCfg<DK, DV>;
@@ -71,10 +83,10 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + cfg::OFF_BAR + 192);
   const uint32_t s0 = smem_u32(smem), sP = s0 + cfg::OFF_P, bars = s0 + cfg::OFF_BAR;
   // copies: bar_full + 8 stage; stage free again: bar_empty + 8 stage (its products' commit, value warps)
-  // products done (commit): ds, qs, qk, pv.  Operands written: vs (V~, value warps), vr (V), sr (S^T, state warps), pr (P, output warps).
+  // products done (commit): ds, qs, qk, pv.  Operands written: vs (V and V~, value warps), sr (S^T, state warps), pr (P, output warps).
   // Accumulators read: dsf (DS), qkf (QK), acc (QS and PV).  O's tile: o full, os read.
   const uint32_t bar_full = bars, bar_empty = bars + 32, b_ds = bars + 64, b_qs = bars + 72, b_qk = bars + 80, b_pv = bars + 88, b_exit = bars + 96,
-                 b_vs = bars + 104, b_vr = bars + 112, b_sr = bars + 120, b_pr = bars + 128, b_dsf = bars + 136, b_qkf = bars + 144, b_acc = bars + 152,
+                 b_vs = bars + 104, b_sr = bars + 120, b_pr = bars + 128, b_dsf = bars + 136, b_qkf = bars + 144, b_acc = bars + 152,
                  b_o = bars + 160, b_os = bars + 168;
   const unsigned long long lim = a.wait_limit_ns ? a.wait_limit_ns : kWaitLimitNs;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;   // warp: uniform for the compiler
@@ -86,7 +98,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
     if (lane == 0) {
       for (int b = 0; b < cfg::STAGES; ++b) { mbar_init(bar_full + 8 * b, 1); mbar_init(bar_empty + 8 * b, 5); }
       for (uint32_t b = b_ds; b <= b_exit; b += 8) mbar_init(b, 1);
-      mbar_init(b_vs, 4); mbar_init(b_vr, 4); mbar_init(b_sr, kStateWarps); mbar_init(b_pr, 4);
+      mbar_init(b_vs, 4); mbar_init(b_sr, kStateWarps); mbar_init(b_pr, 4);
       mbar_init(b_dsf, kStateWarps); mbar_init(b_qkf, 4); mbar_init(b_acc, 4);
       mbar_init(b_o, 4); mbar_init(b_os, 1);
       fence_mbar_init();
@@ -104,27 +116,29 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
   const uint32_t tmem_w = tmem + ((uint32_t)(32 * quad) << 16);   // this warp's lanes, column 0
   bool failed = misaligned;
   auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
-#pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-      if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
     return __all_sync(0xffffffffu, wait_by_warp(bar, parity, lim));
   };
   const bool whole = !a.state_only;
-  const int per_seg = a.H * args.n_walks, n_items = a.n_segs * per_seg;
+  const int per_walk = a.H * args.slices, per_seg = per_walk * args.n_walks, n_items = a.n_segs * per_seg;
 
-  // Every role walks the same items: the longest first, dealt to the CTAs back and forth.  f(walk, segment, head, n_tiles) returns false to give up.
+  // Every role walks the same items: the longest first, dealt to the CTAs back and forth.  f(walk, segment, head, first column, ..) returns false to give up.
   auto for_items = [&](auto&& f) {
     for (int round = 0; round * (int)gridDim.x < n_items && !failed; ++round) {
       const int item = round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
       if (item >= n_items) continue;
-      const int s = item / per_seg, wh = item - s * per_seg, wi = args.first_walk + wh / a.H, h = wh % a.H;
+      const int s = item / per_seg, wh = item - s * per_seg, wi = args.first_walk + wh / per_walk, hs = wh % per_walk, h = hs / args.slices, col0 = (hs - h * args.slices) * DV;
       LinSeg g = lin_segment(a, s);
-      g.tok0 = __shfl_sync(0xffffffffu, g.tok0, 0);   // uniform for the compiler
+      // All of it uniform for the compiler.  tcgen05.mma takes uniform registers; where the control warp's loop, and so the stage's address, hung on
+      // a value that could differ between lanes, each of a tile's 36 instructions cost about 55 cycles of moves into them, 2,000 of 4,400
+      g.tok0 = __shfl_sync(0xffffffffu, g.tok0, 0);
       g.n = __shfl_sync(0xffffffffu, g.n, 0);
+      g.seq = __shfl_sync(0xffffffffu, g.seq, 0);
+      g.ends = __shfl_sync(0xffffffffu, g.ends, 0);
       const LinWalk& w = a.walk[wi];
       float* s_out = lin_exit_state(a, w, wi, s, g, h);
       if (a.state_only && !s_out) continue;
-      if (!f(w, wi, s, g, h, (g.n + L - 1) / L, s_out)) failed = true;
+      if (!f(w, wi, s, g, h, col0, (g.n + L - 1) / L, s_out)) failed = true;
     }
   };
   auto tile_of = [](const LinWalk& w, int i, int n_tiles) { return w.back ? n_tiles - 1 - i : i; };
@@ -148,7 +162,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
       umma_commit(b_qk);
     };
     auto seen = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, mbar_test_wait(bar, parity)); };
-    for_items([&](const LinWalk& w, int, int, const LinSeg&, int, int n_tiles, float* s_out) -> bool {
+    for_items([&](const LinWalk& w, int, int, const LinSeg&, int, int, int n_tiles, float* s_out) -> bool {
       for (int i = 0; i < n_tiles; ++i, ++t) {
         const uint32_t ph = t & 1, st = (stage(t) * cfg::STAGE) >> 4;
         if (i == 0) {
@@ -183,6 +197,10 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
           if (i + 1 < n_tiles && !wait(bar_full + 8 * stage(t + 1), lap(t + 1))) return false;
           continue;
         }
+        // the next tile's QK, if its tiles have landed and this tile's QK has been read; otherwise behind PV
+        const bool more = i + 1 < n_tiles;
+        const bool early = more && seen(bar_full + 8 * stage(t + 1), lap(t + 1)) && seen(b_qkf, ph);
+        if (early) { tc_fence_after(); issue_qk(t + 1); }
         if (!wait(b_sr, ph) || (t > 0 && !wait(b_acc, ph ^ 1))) return false;
         tc_fence_after();
 #pragma unroll
@@ -190,16 +208,12 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
           umma_bf16_ta(tmem + cfg::TM_QS, tmem + cfg::TM_S + 8 * ks, dQ + st + (((ks >> 2) * cfg::BOX + (ks & 3) * 32) >> 4), idesc_s, ks > 0);
         umma_commit(b_qs);
         umma_commit(bar_empty + 8 * stage(t));
-        // the next tile's QK, if its tiles have landed and this tile's QK has been read; otherwise behind PV
-        const bool more = i + 1 < n_tiles;
-        const bool early = more && seen(bar_full + 8 * stage(t + 1), lap(t + 1)) && seen(b_qkf, ph);
-        if (early) { tc_fence_after(); issue_qk(t + 1); }
-        if (!wait(b_pr, ph) || !wait(b_vr, ph)) return false;
+        if (!wait(b_pr, ph)) return false;   // (V came with V~)
         fence_proxy_async();   // P was written by ordinary stores
         tc_fence_after();
 #pragma unroll
         for (int ks = 0; ks < L / 16; ++ks)
-          umma_bf16_ta(tmem + cfg::TM_PV, tmem + cfg::TM_V + 8 * ks, dP + ((ks * 32) >> 4), idesc_s, ks > 0);
+          umma_bf16_ta(tmem + cfg::TM_PV, tmem + cfg::TM_V + 32 * ph + 8 * ks, dP + ((ks * 32) >> 4), idesc_s, ks > 0);
         umma_commit(b_pv);
         if (more && !early) {
           if (!wait(bar_full + 8 * stage(t + 1), lap(t + 1)) || !wait(b_qkf, ph)) return false;
@@ -215,7 +229,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
     }
   } else if (warp == kCopyL) {
     // ---------------------------------------------------------------- copy warp
-    for_items([&](const LinWalk& w, int wi, int, const LinSeg& g, int h, int n_tiles, float*) -> bool {
+    for_items([&](const LinWalk& w, int wi, int, const LinSeg& g, int h, int col0, int n_tiles, float*) -> bool {
       for (int i = 0; i < n_tiles; ++i, ++t) {
         if (t >= cfg::STAGES && !wait(bar_empty + 8 * stage(t), lap(t) ^ 1)) return false;
         if (lane == 0) {
@@ -225,7 +239,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
 #pragma unroll
           for (int b = 0; b < cfg::KB; ++b) tma_load_2d(base + cfg::OFF_K + b * cfg::BOX, &maps.k[wi], bar, h * DK + 64 * b, tok);
 #pragma unroll
-          for (int b = 0; b < cfg::VB; ++b) tma_load_2d(base + cfg::OFF_V + b * cfg::BOX, &maps.v[wi], bar, h * DV + 64 * b, tok);
+          for (int b = 0; b < cfg::VB; ++b) tma_load_2d(base + cfg::OFF_V + b * cfg::BOX, &maps.v[wi], bar, h * w.d_v + col0 + 64 * b, tok);
           if (whole)
 #pragma unroll
             for (int b = 0; b < cfg::KB; ++b) tma_load_2d(base + b * cfg::BOX, &maps.q[wi], bar, h * DK + 64 * b, tok);
@@ -238,87 +252,95 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
       for (uint32_t c = t >= cfg::STAGES ? t - cfg::STAGES : 0; c < t; ++c) mbar_wait_bounded(bar_full + 8 * stage(c), lap(c), lim);
   } else if (warp < kStateWarps) {
     // ---------------------------------------------------------------- state warps
-    const int dv = DV == 128 ? 32 * quad + lane : 16 * quad + (lane & 15);
-    const bool mine = DV == 128 || lane < 16;
-    float S[cfg::SH];   // feature SH half + c of value column dv
-    for_items([&](const LinWalk& w, int wi, int s, const LinSeg& g, int h, int n_tiles, float* s_out) -> bool {
+    // S^T as pairs of features.  128 value columns: lane's row 32 quad + lane, features SH half + 2 c, + 1 (S[c]).  64: rows 16 quad + gq and + 8 in
+    // lanes 0 .. 15, in accumulator fragments: S[2 nt + e] = row + 8 e, features SH half + 8 nt + t2, + 1.
+    constexpr int NP = cfg::SH / 2 * LG / 2, STEP = NP < 16 ? NP : 16;
+    Pair S[NP];
+    auto for_state = [&](auto&& f) {   // f(pair, value column, its first feature)
+#pragma unroll
+      for (int c = 0; c < NP; ++c) {
+        if constexpr (DV == 128) f(S[c], 32 * quad + lane, cfg::SH * half + 2 * c);
+        else f(S[c], 16 * quad + 8 * (c & 1) + gq, cfg::SH * half + 8 * (c >> 1) + t2);
+      }
+    };
+    for_items([&](const LinWalk& w, int wi, int s, const LinSeg& g, int h, int col0, int n_tiles, float* s_out) -> bool {
       bool turned;
       const float* s_in = lin_entry_state(a, w, wi, s, g, h, &turned);
-      if (!s_in) {
-#pragma unroll
-        for (int c = 0; c < cfg::SH; ++c) S[c] = 0.f;
-      } else if (turned) {
-        const float4* p = reinterpret_cast<const float4*>(s_in + (size_t)dv * DK + cfg::SH * half);
-#pragma unroll
-        for (int c = 0; c < cfg::SH; c += 4) {
-          const float4 x = p[c / 4];
-          S[c] = x.x; S[c + 1] = x.y; S[c + 2] = x.z; S[c + 3] = x.w;
-        }
-      } else {
-#pragma unroll
-        for (int c = 0; c < cfg::SH; ++c) S[c] = s_in[(size_t)(cfg::SH * half + c) * DV + dv];
-      }
-      const float l = lin_log2_decay(a, h) * 0.6931471805599453f;
+      if (!s_in) for_state([&](Pair& x, int, int) { x = pair(0.f, 0.f); });
+      else if (turned) for_state([&](Pair& x, int v, int k) { const float2 y = *reinterpret_cast<const float2*>(s_in + (size_t)(col0 + v) * DK + k); x = pair(y.x, y.y); });
+      else for_state([&](Pair& x, int v, int k) { x = pair(s_in[(size_t)k * w.d_v + col0 + v], s_in[(size_t)(k + 1) * w.d_v + col0 + v]); });
+      // lambda^n - 1 for S <- (S + (lambda^n - 1) S) + DS: a factor near 1 that is off by a rounding would be off by it in every tile, always to the same side
+      const float l = lin_log2_decay(a, h) * 0.6931471805599453f, less_full = expm1f(l * L), less_last = expm1f(l * (g.n - (n_tiles - 1) * L));
       for (int i = 0; i < n_tiles; ++i, ++t) {
         const uint32_t ph = t & 1;
         if (whole) {
           if (t > 0 && !wait(b_qs, ph ^ 1)) return false;   // the operand's last reader
           tc_fence_after();
 #pragma unroll
-          for (int c = 0; c < cfg::SH; c += 32) {
-            uint32_t r[16];
+          for (int c = 0; c < NP; c += STEP) {
+            uint32_t r[STEP];
 #pragma unroll
-            for (int q = 0; q < 16; ++q) r[q] = pack_bf16(S[c + 2 * q], S[c + 2 * q + 1]);
-            tmem_st_row16(r, tmem_w + cfg::TM_S + (cfg::SH * half + c) / 2);
+            for (int q = 0; q < STEP; ++q) r[q] = pack_bf16(S[c + q]);
+            const uint32_t at = tmem_w + cfg::TM_S + cfg::SH / 2 * half + c;
+            if constexpr (DV == 128) tmem_st_row16(r, at);
+            else if constexpr (STEP == 16) tmem_st_packed32(r, at);
+            else tmem_st_packed16(r, at);
           }
           tmem_wait_st();
           tc_fence_before();
           warp_arrive(b_sr, lane);
         }
-        // lambda^rows - 1: a factor near 1 that is off by a rounding would be off by it in every tile, always to the same side
-        const float less = expm1f(l * rows_of(g, tile_of(w, i, n_tiles)));
+        const float less1 = tile_of(w, i, n_tiles) == n_tiles - 1 ? less_last : less_full;
+        const Pair less = pair(less1, less1);
         if (!wait(b_ds, ph)) return false;
         tc_fence_after();
 #pragma unroll
-        for (int c = 0; c < cfg::SH; c += 32) {
-          float ds[32];
-          tmem_ld_row32(ds, tmem_w + cfg::TM_DS + cfg::SH * half + c);
+        for (int c = 0; c < NP; c += STEP) {
+          float ds[2 * STEP];
+          const uint32_t at = tmem_w + cfg::TM_DS + cfg::SH * half + 2 * c;
+          if constexpr (DV == 128) tmem_ld_row32(ds, at);
+          else if constexpr (STEP == 16) tmem_ld_16x64(reinterpret_cast<float (&)[8][4]>(ds), at);
+          else tmem_ld_16x32(reinterpret_cast<float (&)[4][4]>(ds), at);
           tmem_wait_ld();
-          if (c + 32 == cfg::SH) { tc_fence_before(); warp_arrive(b_dsf, lane); }
+          if (c + STEP == NP) { tc_fence_before(); warp_arrive(b_dsf, lane); }
 #pragma unroll
-          for (int q = 0; q < 32; ++q) S[c + q] = fmaf(S[c + q], less, S[c + q]) + ds[q];
+          for (int q = 0; q < STEP; ++q) S[c + q] = add2(fma2(S[c + q], less, S[c + q]), pair(ds[2 * q], ds[2 * q + 1]));
         }
       }
-      if (s_out && mine) {
-#pragma unroll
-        for (int c = 0; c < cfg::SH; ++c) s_out[(size_t)(cfg::SH * half + c) * DV + dv] = S[c];
-      }
+      if (s_out)
+        for_state([&](Pair& x, int v, int k) {
+          const float2 y = parts(x);
+          s_out[(size_t)k * w.d_v + col0 + v] = y.x;
+          s_out[(size_t)(k + 1) * w.d_v + col0 + v] = y.y;
+        });
       return true;
     });
   } else if (warp < kOutput) {
     // ---------------------------------------------------------------- value warps
     const int row0 = quad * cfg::RPQ;
-    for_items([&](const LinWalk& w, int, int, const LinSeg& g, int h, int n_tiles, float* s_out) -> bool {
+    float* f = reinterpret_cast<float*>(smem + cfg::OFF_F) + quad * L;   // this warp's table of the tokens' factors
+    for_items([&](const LinWalk& w, int, int, const LinSeg& g, int h, int col0, int n_tiles, float* s_out) -> bool {
       const float l2 = lin_log2_decay(a, h);
-      float f[2][4][2];   // lambda^.. of the tokens 32 th + 8 nt + t2, + 1
-      auto factors = [&](int rows) {
-#pragma unroll
-        for (int th = 0; th < 2; ++th)
-#pragma unroll
-          for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              const int j = 32 * th + 8 * nt + t2 + q, n = w.back ? j + 1 : rows - 1 - j;
-              f[th][nt][q] = j < rows ? w.k_factor * exp2f(l2 * n) : 0.f;
-            }
-      };
       int made_for = 0;
       for (int i = 0; i < n_tiles; ++i, ++t) {
         const uint32_t ph = t & 1, base = s0 + stage(t) * cfg::STAGE, sV = base + cfg::OFF_V;
         const int rows = rows_of(g, tile_of(w, i, n_tiles));
-        if (rows != made_for) { factors(rows); made_for = rows; }
+        if (rows != made_for) {
+          made_for = rows;
+          __syncwarp();
+#pragma unroll 1
+          for (int j = lane; j < L; j += 32) f[j] = j < rows ? w.k_factor * exp2f(l2 * (w.back ? j + 1 : rows - 1 - j)) : 0.f;
+          __syncwarp();
+        }
         if (!wait(bar_full + 8 * stage(t), lap(t))) return false;
-        uint32_t x[LG][2][8];   // V, pairs of tokens
+        if (rows < L) {
+          // Behind the sequence's end lie a neighbour's rows.  V counts as zero there (below), and zero times a key that is not finite is not zero: the key
+          // tile's rows are cleared too (QK may be reading them: those columns of P are left out by selection)
+          for (int e = tid - 32 * kValue; e < (L - rows) * 8 * cfg::KB; e += 128)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + cfg::OFF_K + (e / ((L - rows) * 8)) * cfg::BOX + (rows + (e / 8) % (L - rows)) * 128 + (e & 7) * 16), "r"(0) : "memory");
+          fence_proxy_async();
+        }
+        uint32_t x[LG][2][8];   // V: pairs of tokens 32 th + 8 nt + t2, + 1 of value columns row0 + 16 lg + gq (2 nt) and + 8 (2 nt + 1)
 #pragma unroll
         for (int lg = 0; lg < LG; ++lg)
 #pragma unroll
@@ -330,113 +352,104 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
                                 x[lg][th][2 * nt + 3]);
             }
         if (rows < L) {
-          // Behind the sequence's end lie a neighbour's rows.  V counts as zero there, and zero times a key that is not finite is not zero: the key tile's
-          // rows are cleared too (QK may be reading them: those columns of P are left out by selection)
 #pragma unroll
-          for (int lg = 0; lg < LG; ++lg)
+          for (int th = 0; th < 2; ++th)
 #pragma unroll
-            for (int th = 0; th < 2; ++th)
+            for (int nt = 0; nt < 4; ++nt) {
+              const int j = 32 * th + 8 * nt + t2;
+              const uint32_t keep = (j < rows ? 0xffffu : 0u) | (j + 1 < rows ? 0xffff0000u : 0u);
 #pragma unroll
-              for (int nt = 0; nt < 4; ++nt) {
-                const int j = 32 * th + 8 * nt + t2;
-                const uint32_t keep = (j < rows ? 0xffffu : 0u) | (j + 1 < rows ? 0xffff0000u : 0u);
-                x[lg][th][2 * nt] &= keep;
-                x[lg][th][2 * nt + 1] &= keep;
-              }
-          for (int e = tid - 32 * kValue; e < (L - rows) * 8 * cfg::KB; e += 128)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + cfg::OFF_K + (e / ((L - rows) * 8)) * cfg::BOX + (rows + (e / 8) % (L - rows)) * 128 + (e & 7) * 16), "r"(0) : "memory");
-          fence_proxy_async();
+              for (int lg = 0; lg < LG; ++lg) { x[lg][th][2 * nt] &= keep; x[lg][th][2 * nt + 1] &= keep; }
+            }
         }
-        warp_arrive(bar_empty + 8 * stage(t), lane);
+        // DS of the tile before is done: V~ may be overwritten; and with it, since products are done in order, PV of the one before that: V is kept for two tiles in turn
         if (t > 0 && !wait(b_ds, ph ^ 1)) return false;
         tc_fence_after();
 #pragma unroll
-        for (int lg = 0; lg < LG; ++lg)
+        for (int th = 0; th < 2; ++th) {
+          Pair fj[4];
 #pragma unroll
-          for (int th = 0; th < 2; ++th) {
+          for (int nt = 0; nt < 4; ++nt) { const float2 y = *reinterpret_cast<const float2*>(f + 32 * th + 8 * nt + t2); fj[nt] = pair(y.x, y.y); }
+#pragma unroll
+          for (int lg = 0; lg < LG; ++lg) {
             uint32_t hi[8], lo[8];
 #pragma unroll
             for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                const uint32_t v = x[lg][th][2 * nt + e];
-                const float y0 = __uint_as_float(v << 16) * f[th][nt][0], y1 = __uint_as_float(v & 0xffff0000u) * f[th][nt][1];
-                const uint32_t p = pack_bf16(y0, y1);
-                hi[2 * nt + e] = p;
-                lo[2 * nt + e] = pack_bf16(y0 - __uint_as_float(p << 16), y1 - __uint_as_float(p & 0xffff0000u));
+                const Pair y = mul2(unpack_bf16(x[lg][th][2 * nt + e]), fj[nt]);
+                hi[2 * nt + e] = pack_bf16(y);
+                if (s_out) lo[2 * nt + e] = pack_bf16(fma2(unpack_bf16(hi[2 * nt + e]), pair(-1.f, -1.f), y));
               }
             const uint32_t at = tmem_w + ((uint32_t)(16 * lg) << 16) + 16 * th;
             tmem_st_packed16(hi, at + cfg::TM_VH);
             if (s_out) tmem_st_packed16(lo, at + cfg::TM_VL);
+            if (whole) tmem_st_packed16(x[lg][th], at + cfg::TM_V + 32 * ph);
           }
+        }
         tmem_wait_st();
         tc_fence_before();
-        warp_arrive(b_vs, lane);
-        if (whole) {
-          if (t > 0 && !wait(b_pv, ph ^ 1)) return false;
-          tc_fence_after();
-#pragma unroll
-          for (int lg = 0; lg < LG; ++lg)
-#pragma unroll
-            for (int th = 0; th < 2; ++th) tmem_st_packed16(x[lg][th], tmem_w + ((uint32_t)(16 * lg) << 16) + 16 * th + cfg::TM_V);
-          tmem_wait_st();
-          tc_fence_before();
-          warp_arrive(b_vr, lane);
-        }
+        __syncwarp();
+        if (lane == 0) { mbar_arrive(b_vs); mbar_arrive(bar_empty + 8 * stage(t)); }
       }
       return true;
     });
   } else if (warp < kControlL && whole) {
     // ---------------------------------------------------------------- output warps
     const int row0 = quad * cfg::RPQ, ia = 16 * quad + gq, ib = ia + 8;
-    for_items([&](const LinWalk& w, int, int, const LinSeg& g, int h, int n_tiles, float*) -> bool {
+    float* y = reinterpret_cast<float*>(smem + cfg::OFF_F) + (4 + quad) * L;   // this warp's table of the tokens' factors of QS
+    for_items([&](const LinWalk& w, int, int, const LinSeg& g, int h, int col0, int n_tiles, float*) -> bool {
       const float l2 = lin_log2_decay(a, h), pv_factor = w.k_factor * w.out_factor;
-      float f[8][4], y[8][2];   // P's factors (negative: masked); QS's of the tokens 8 nt + t2, + 1
+      Pair f[8][2];   // P's factors, zero where it is masked: columns 8 nt + t2, + 1 of rows ia and ib
 #pragma unroll
       for (int nt = 0; nt < 8; ++nt)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int d = (q < 2 ? ia : ib) - (8 * nt + t2 + (q & 1)), gap = w.back ? -d : d;
-          f[nt][q] = gap >= 0 ? exp2f(l2 * gap) : -1.f;
+        for (int e = 0; e < 2; ++e) {
+          const int d = (e ? ib : ia) - (8 * nt + t2), g0 = w.back ? -d : d, g1 = w.back ? 1 - d : d - 1;
+          f[nt][e] = pair(g0 >= 0 ? exp2f(l2 * g0) : 0.f, g1 >= 0 ? exp2f(l2 * g1) : 0.f);
         }
-      auto out_factors = [&](int rows) {
-#pragma unroll
-        for (int nt = 0; nt < 8; ++nt)
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const int i = 8 * nt + t2 + q, p = w.back ? rows - 1 - i : i + 1;
-            y[nt][q] = i < rows ? w.out_factor * exp2f(l2 * p) : 0.f;
-          }
-      };
       int made_for = 0;
       // O of tile t (its position in the item: i) out of tensor memory into its tile, [token][column]; behind the wait for its PV
       auto put_output = [&](uint32_t t, int rows) -> bool {
-        if (rows != made_for) { out_factors(rows); made_for = rows; }
+        if (rows != made_for) {
+          made_for = rows;
+          __syncwarp();
+#pragma unroll 1
+          for (int i = lane; i < L; i += 32) y[i] = i < rows ? w.out_factor * exp2f(l2 * (w.back ? rows - 1 - i : i + 1)) : 0.f;
+          __syncwarp();
+        }
         if (t > 0 && !wait(b_os, (t - 1) & 1)) return false;   // the last tile's store has read it
 #pragma unroll
         for (int lg = 0; lg < LG; ++lg) {
+          // 64 tokens x 16 value columns: two halves' loads in flight
+          float pv[2][4][4], qs[2][4][4];
 #pragma unroll
-          for (int n0 = 0; n0 < 8; n0 += 4) {
-            const uint32_t at = tmem_w + ((uint32_t)(16 * lg) << 16) + 8 * n0;
-            float pv[4][4], qs[4][4];
-            tmem_ld_16x32(pv, at + cfg::TM_PV);
-            tmem_ld_16x32(qs, at + cfg::TM_QS);
-            tmem_wait_ld();
+          for (int hf = 0; hf < 2; ++hf) {
+            const uint32_t at = tmem_w + ((uint32_t)(16 * lg) << 16) + 32 * hf;
+            tmem_ld_16x32(pv[hf], at + cfg::TM_PV);
+            tmem_ld_16x32(qs[hf], at + cfg::TM_QS);
+          }
+          tmem_wait_ld();
+          if (lg == LG - 1) { tc_fence_before(); warp_arrive(b_acc, lane); }
 #pragma unroll
-            for (int nt = 0; nt < 4; ++nt)
+          for (int hf = 0; hf < 2; ++hf) {
+            uint32_t o[4][2];
 #pragma unroll
-              for (int q = 0; q < 4; ++q) pv[nt][q] = fmaf(pv[nt][q], pv_factor, y[n0 + nt][q & 1] * qs[nt][q]);
+            for (int nt = 0; nt < 4; ++nt) {
+              const float2 yt = *reinterpret_cast<const float2*>(y + 32 * hf + 8 * nt + t2);
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                o[nt][e] = pack_bf16(fma2(pair(pv[hf][nt][2 * e], pv[hf][nt][2 * e + 1]), pair(pv_factor, pv_factor),
+                                          mul2(pair(yt.x, yt.y), pair(qs[hf][nt][2 * e], qs[hf][nt][2 * e + 1]))));
+            }
 #pragma unroll
             for (int nt = 0; nt < 4; nt += 2) {
-              const int tok = 8 * (n0 + nt + (mi >> 1)) + mr, col = row0 + 16 * lg + 8 * (mi & 1);
-              stmatrix_x4_trans(s0 + cfg::OFF_O + (col >> 6) * cfg::BOX + tok * 128 + ((((col >> 3) ^ tok) & 7) << 4), pack_bf16(pv[nt][0], pv[nt][1]), pack_bf16(pv[nt][2], pv[nt][3]),
-                                pack_bf16(pv[nt + 1][0], pv[nt + 1][1]), pack_bf16(pv[nt + 1][2], pv[nt + 1][3]));
+              const int tok = 32 * hf + 8 * (nt + (mi >> 1)) + mr, col = row0 + 16 * lg + 8 * (mi & 1);
+              stmatrix_x4_trans(s0 + cfg::OFF_O + (col >> 6) * cfg::BOX + tok * 128 + ((((col >> 3) ^ tok) & 7) << 4), o[nt][0], o[nt][1], o[nt + 1][0], o[nt + 1][1]);
             }
           }
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) { mbar_arrive(b_acc); mbar_arrive(b_o); }
+        warp_arrive(b_o, lane);
         return true;
       };
       int last_rows = 0;
@@ -454,17 +467,18 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
           tmem_wait_ld();
           tc_fence_before();
           warp_arrive(b_qkf, lane);
+          if (rows < L) {   // columns behind the sequence's end: a neighbour's keys, which need not be finite
 #pragma unroll
-          for (int nt = 0; nt < 8; ++nt) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) qk[nt][q] = f[nt][q] < 0.f ? 0.f : qk[nt][q] * f[nt][q];
-            if (rows < L) {   // backwards, a row meets the columns behind the sequence's end
+            for (int nt = 0; nt < 8; ++nt) {
               const int j = 8 * nt + t2;
               if (j >= rows) qk[nt][0] = qk[nt][2] = 0.f;
               if (j + 1 >= rows) qk[nt][1] = qk[nt][3] = 0.f;
             }
-            wa[nt] = pack_bf16(qk[nt][0], qk[nt][1]);
-            wb[nt] = pack_bf16(qk[nt][2], qk[nt][3]);
+          }
+#pragma unroll
+          for (int nt = 0; nt < 8; ++nt) {
+            wa[nt] = pack_bf16(mul2(pair(qk[nt][0], qk[nt][1]), f[nt][0]));
+            wb[nt] = pack_bf16(mul2(pair(qk[nt][2], qk[nt][3]), f[nt][1]));
           }
         }
         if (t > 0 && !wait(b_pv, ph ^ 1)) return false;   // PV of the tile before is done: its O can be read, and P's tile is free
@@ -483,7 +497,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
     });
   } else if (warp == kStoreL && whole) {
     // ---------------------------------------------------------------- store warp: O's tile to memory
-    for_items([&](const LinWalk& w, int wi, int, const LinSeg& g, int h, int n_tiles, float*) -> bool {
+    for_items([&](const LinWalk& w, int wi, int, const LinSeg& g, int h, int col0, int n_tiles, float*) -> bool {
       for (int i = 0; i < n_tiles; ++i, ++t) {
         if (!wait(b_o, t & 1)) return false;
         const int tile = tile_of(w, i, n_tiles), tok0 = g.tok0 + tile * L, rows = rows_of(g, tile);
@@ -491,15 +505,15 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
           if (lane == 0) {
             fence_proxy_async();   // the tile was written by ordinary stores
 #pragma unroll
-            for (int b = 0; b < cfg::VB; ++b) tma_store_2d(&maps.o[wi], s0 + cfg::OFF_O + b * cfg::BOX, h * DV + 64 * b, tok0);
+            for (int b = 0; b < cfg::VB; ++b) tma_store_2d(&maps.o[wi], s0 + cfg::OFF_O + b * cfg::BOX, h * w.d_v + col0 + 64 * b, tok0);
             bulk_commit();
             bulk_wait_read();
           }
         } else {
-          __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(w.out) + ((size_t)tok0 * a.H + h) * DV;
+          __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(w.out) + ((size_t)tok0 * a.H + h) * w.d_v + col0;
           for (int e = lane; e < rows * (DV / 8); e += 32) {
             const int tok = e / (DV / 8), pc = e % (DV / 8);
-            *reinterpret_cast<uint4*>(out + (size_t)tok * a.H * DV + 8 * pc) =
+            *reinterpret_cast<uint4*>(out + (size_t)tok * a.H * w.d_v + 8 * pc) =
                 *reinterpret_cast<const uint4*>(smem + cfg::OFF_O + (pc >> 3) * cfg::BOX + tok * 128 + (((pc ^ tok) & 7) << 4));
           }
         }
@@ -530,10 +544,13 @@ cudaError_t launch_one(const LinMaps& maps, const LinTcArgs& args, int sms, cuda
       ready[dev] = true;
     }
   }
-  const long long items = (long long)args.a.n_segs * args.a.H * args.n_walks;
+  const long long items = (long long)args.a.n_segs * args.a.H * args.n_walks * args.slices;
   e = launch_early(linear_tc_kernel<DK, DV>, dim3((unsigned)(items < sms ? items : sms)), kThreadsL, cfg::SMEM, stream, maps, args);
   return e == cudaSuccess ? launched() : e;
 }
+
+// Slices of a walk's 128 value columns: two of 64 while each gets an SM of its own.
+int lin_tc_slices(const LinArgs& a, int sms) { return (long long)a.n_segs * a.H * a.n_walks * 2 <= sms ? 2 : 1; }
 
 }  // namespace
 
@@ -552,14 +569,16 @@ cudaError_t launch_linear_tc(const LinArgs& a, long long tokens, cudaStream_t st
       return cudaErrorUnknown;
   }
   // the walks of one launch have the same dimensions: all of them where d_k = d_v, else the last apart
-  LinTcArgs args{a, 0, 0};
+  LinTcArgs args{a, 0, 0, 1};
   for (int first = 0; first < a.n_walks; first += args.n_walks) {
     const LinWalk& w = a.walk[first];
     args.first_walk = first;
     args.n_walks = 1;
     while (first + args.n_walks < a.n_walks && a.walk[first + args.n_walks].d_k == w.d_k && a.walk[first + args.n_walks].d_v == w.d_v) ++args.n_walks;
-    const cudaError_t e = w.d_k == 128 ? (w.d_v == 128 ? launch_one<128, 128>(maps, args, sms, stream) : launch_one<128, 64>(maps, args, sms, stream))
-                                       : (w.d_v == 128 ? launch_one<64, 128>(maps, args, sms, stream) : launch_one<64, 64>(maps, args, sms, stream));
+    const bool narrow = w.d_v == 64 || lin_tc_slices(a, sms) == 2;
+    args.slices = narrow ? w.d_v / 64 : 1;
+    const cudaError_t e = w.d_k == 128 ? (narrow ? launch_one<128, 64>(maps, args, sms, stream) : launch_one<128, 128>(maps, args, sms, stream))
+                                       : (narrow ? launch_one<64, 64>(maps, args, sms, stream) : launch_one<64, 128>(maps, args, sms, stream));
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
