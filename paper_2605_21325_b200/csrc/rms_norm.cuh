@@ -4,7 +4,7 @@
 
 namespace tri_inv {
 
-constexpr int kRmsNormPartials = 592;   // rows of partial sums of dw, at most: the blocks of the gradient's kernel times the rows that one takes side by side
+constexpr int kRmsNormPartials = 592;   // rows of partial sums of dw, at most: the blocks of the gradient's kernel, four for each of 148 SMs
 
 struct RmsNormArgs {
   const void *X, *R, *w;   // R: residual or null

@@ -27,16 +27,14 @@ __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bf
 template <class T> struct Vec;
 template <> struct Vec<float> {
   static constexpr int N = 4;
-  static __device__ __forceinline__ void load(float (&v)[4], const float* p) {
-    const float4 x = *reinterpret_cast<const float4*>(p);
-    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+  static __device__ __forceinline__ void widen(float (&v)[4], const uint4& x) {
+    v[0] = __uint_as_float(x.x); v[1] = __uint_as_float(x.y); v[2] = __uint_as_float(x.z); v[3] = __uint_as_float(x.w);
   }
   static __device__ __forceinline__ void store(float* p, const float (&v)[4]) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
 };
 template <> struct Vec<__nv_bfloat16> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ void load(float (&v)[8], const __nv_bfloat16* p) {
-    const uint4 x = *reinterpret_cast<const uint4*>(p);
+  static __device__ __forceinline__ void widen(float (&v)[8], const uint4& x) {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
@@ -51,6 +49,8 @@ template <> struct Vec<__nv_bfloat16> {
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 };
+template <class T>
+__device__ __forceinline__ uint4 load_raw(const T* p) { return *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {   // two codes, rounded to nearest even
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
@@ -96,42 +96,45 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) rms_norm_kernel(const _
   const size_t base = (size_t)(real ? row : 0) * a.n;
   const T *X = (const T*)a.X, *R = (const T*)a.R, *Wt = (const T*)a.w;
   wait_for_predecessor();
-  float h[NV][N], w[NV][N], sum[1] = {0.f};
+  uint4 raw[NV], res[NV], wr[NV];   // everything is requested before anything is used
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (t + i * TPR) * N;
-#pragma unroll
-    for (int j = 0; j < N; ++j) h[i][j] = w[i][j] = 0.f;
-    if (real && c < a.n) Vec<T>::load(h[i], X + base + c);
-  }
-  if (R) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (t + i * TPR) * N;
-      float r[N];
-      if (real && c < a.n) {
-        Vec<T>::load(r, R + base + c);
-#pragma unroll
-        for (int j = 0; j < N; ++j) h[i][j] += r[j];
-      }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (t + i * TPR) * N;
+    raw[i] = res[i] = wr[i] = make_uint4(0u, 0u, 0u, 0u);
     if (real && c < a.n) {
-      Vec<T>::load(w[i], Wt + c);
-      if (a.H) Vec<T>::store((T*)a.H + base + c, h[i]);
+      raw[i] = load_raw(X + base + c);
+      if (R) res[i] = load_raw(R + base + c);
     }
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (t + i * TPR) * N;
+    if (real && c < a.n) wr[i] = load_raw(Wt + c);
+  }
+  float h[NV][N], sum[1] = {0.f};
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (t + i * TPR) * N;
+    Vec<T>::widen(h[i], raw[i]);
+    if (R) {
+      float r[N];
+      Vec<T>::widen(r, res[i]);
+#pragma unroll
+      for (int j = 0; j < N; ++j) h[i][j] += r[j];
+    }
+    if (a.H && real && c < a.n) Vec<T>::store((T*)a.H + base + c, h[i]);
 #pragma unroll
     for (int j = 0; j < N; ++j) sum[0] = fmaf(h[i][j], h[i][j], sum[0]);
   }
   row_reduce<TPR>(sum, words, tid);
   const float rstd = rsqrtf(sum[0] / (float)a.n + a.eps);
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+  for (int i = 0; i < NV; ++i) {
+    float w[N];
+    Vec<T>::widen(w, wr[i]);
 #pragma unroll
-    for (int j = 0; j < N; ++j) h[i][j] *= rstd * w[i][j];
+    for (int j = 0; j < N; ++j) h[i][j] *= rstd * w[j];
+  }
   if constexpr (OUT == 0) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -167,10 +170,11 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) rms_norm_kernel(const _
     for (int i = 0; i < NV; ++i) {
       const int c = (t + i * TPR) * N;
       if (real && c < a.n) {
+        const float up = 1.f / scale[i];   // (a division for every value took as long as all the rest)
         uint32_t code[N / 4];
 #pragma unroll
         for (int j = 0; j < N; j += 4)
-          code[j / 4] = pack_e4m3(h[i][j] / scale[i], h[i][j + 1] / scale[i]) | pack_e4m3(h[i][j + 2] / scale[i], h[i][j + 3] / scale[i]) << 16;
+          code[j / 4] = pack_e4m3(h[i][j] * up, h[i][j + 1] * up) | pack_e4m3(h[i][j + 2] * up, h[i][j + 3] * up) << 16;
         uint8_t* y = (uint8_t*)a.Y + base + c;
         if constexpr (N == 8) *reinterpret_cast<uint2*>(y) = make_uint2(code[0], code[1]);
         else *reinterpret_cast<uint32_t*>(y) = code[0];
@@ -223,73 +227,110 @@ __global__ void __launch_bounds__(256) rms_norm_any_kernel(const __grid_constant
       const int c = gr * kGroup + 32 * i + (tid & 31);
       if (c < a.n) {
         if constexpr (OUT == 0) put((T*)a.Y + base + c, y[i]);
-        else ((uint8_t*)a.Y)[base + c] = (uint8_t)pack_e4m3(y[i] / scale, 0.f);
+        else ((uint8_t*)a.Y)[base + c] = (uint8_t)pack_e4m3(y[i] * (1.f / scale), 0.f);
         if (a.H) put((T*)a.H + base + c, h[i]);
       }
     }
   }
 }
 
-// The gradient: a block takes every gridDim.x-th group of rows; a thread has the same columns in all of them and sums their dw in registers.
+// The gradient: a block takes every gridDim.x-th group of rows; a thread has the same columns in all of them and sums their dw in registers.  The
+// next rows are requested before these are worked on; rows side by side join their sums in shared memory, so that a block leaves one row of them.
 template <class T, int TPR, int NV>
-__global__ void __launch_bounds__(TPR > 256 ? TPR : 256) rms_norm_backward_kernel(const __grid_constant__ RmsNormBackwardArgs a) {
+__global__ void __launch_bounds__(TPR > 256 ? TPR : 256, NV == 1 ? (TPR > 256 ? 2 : 4) : 1) rms_norm_backward_kernel(const __grid_constant__ RmsNormBackwardArgs a) {
   constexpr int N = Vec<T>::N, THREADS = TPR > 256 ? TPR : 256, ROWS = THREADS / TPR;
   __shared__ float words[2][32];
+  __shared__ __align__(16) float joined[ROWS > 1 ? (ROWS - 1) * TPR * NV * N : 4];
   const int tid = threadIdx.x, t = tid % TPR, sub = tid / TPR;
   const T *X = (const T*)a.X, *DY = (const T*)a.dY, *DH = (const T*)a.dH, *Wt = (const T*)a.w;
   wait_for_predecessor();
-  float w[NV][N], dw[NV][N];
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  uint4 wr[NV];
+  float dw[NV][N];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (t + i * TPR) * N;
+    wr[i] = c < a.n ? load_raw(Wt + c) : zero;
 #pragma unroll
-    for (int j = 0; j < N; ++j) w[i][j] = dw[i][j] = 0.f;
-    if (c < a.n) Vec<T>::load(w[i], Wt + c);
+    for (int j = 0; j < N; ++j) dw[i][j] = 0.f;
   }
   const long long steps = (a.rows + ROWS - 1) / ROWS;
-  for (long long step = blockIdx.x; step < steps; step += gridDim.x) {   // the block's threads stay together: the reductions meet all of them
+  uint4 xn[NV], dn[NV], pn[NV];
+  auto request = [&](long long step) {
     const long long row = step * ROWS + sub;
-    const bool real = row < a.rows;
-    const size_t base = (size_t)(real ? row : 0) * a.n;
-    float h[NV][N], u[NV][N], sum[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (t + i * TPR) * N;
-#pragma unroll
-      for (int j = 0; j < N; ++j) h[i][j] = u[i][j] = 0.f;
-      if (real && c < a.n) { Vec<T>::load(h[i], X + base + c); Vec<T>::load(u[i], DY + base + c); }
+      const bool in = row < a.rows && c < a.n;
+      const size_t at = (size_t)(in ? row : 0) * a.n + c;
+      xn[i] = in ? load_raw(X + at) : zero;
+      dn[i] = in ? load_raw(DY + at) : zero;
+      pn[i] = in && DH ? load_raw(DH + at) : zero;
     }
+  };
+  request(blockIdx.x);
+  for (long long step = blockIdx.x; step < steps; step += gridDim.x) {   // the block's threads stay together: the reductions meet all of them
+    const long long row = step * ROWS + sub;
+    uint4 xr[NV], dr[NV], pr[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) { xr[i] = xn[i]; dr[i] = dn[i]; pr[i] = pn[i]; }
+    // (dX may be dY, X or dH: the next rows are not this block's present ones, and no other block's)
+    if (step + gridDim.x < steps) request(step + gridDim.x);
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float h[N], u[N], w[N];
+      Vec<T>::widen(h, xr[i]);
+      Vec<T>::widen(u, dr[i]);
+      Vec<T>::widen(w, wr[i]);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        sum[0] = fmaf(h[i][j], h[i][j], sum[0]);
-        sum[1] = fmaf(u[i][j] * w[i][j], h[i][j], sum[1]);
+        sum[0] = fmaf(h[j], h[j], sum[0]);
+        sum[1] = fmaf(u[j] * w[j], h[j], sum[1]);
       }
+    }
     row_reduce<TPR>(sum, words, tid);
     const float rstd = rsqrtf(sum[0] / (float)a.n + a.eps), back = rstd * rstd * (sum[1] / (float)a.n);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (t + i * TPR) * N;
-      if (real && c < a.n) {
-        float dx[N];
-        if (DH) Vec<T>::load(dx, DH + base + c);
+      float h[N], u[N], w[N], dx[N];
+      Vec<T>::widen(h, xr[i]);
+      Vec<T>::widen(u, dr[i]);
+      Vec<T>::widen(w, wr[i]);
+      Vec<T>::widen(dx, pr[i]);   // zero without dH
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          dw[i][j] = fmaf(u[i][j], h[i][j] * rstd, dw[i][j]);
-          const float g = rstd * (u[i][j] * w[i][j] - h[i][j] * back);
-          dx[j] = DH ? dx[j] + g : g;
-        }
-        Vec<T>::store((T*)a.dX + base + c, dx);
+      for (int j = 0; j < N; ++j) {
+        dw[i][j] = fmaf(u[j], h[j] * rstd, dw[i][j]);
+        dx[j] += rstd * (u[j] * w[j] - h[j] * back);
       }
+      if (row < a.rows && c < a.n) Vec<T>::store((T*)a.dX + (size_t)row * a.n + c, dx);
     }
   }
-  // one row of partial sums for each of the block's rows side by side: ROWS * gridDim.x in all
+  if constexpr (ROWS > 1) {
+    if (sub > 0)
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < N; j += 4)
+          *reinterpret_cast<float4*>(joined + ((sub - 1) * NV * N + i * N + j) * TPR + 4 * t) = make_float4(dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]);
+    __syncthreads();
+    if (sub > 0) return;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < N; j += 4)
+#pragma unroll
+        for (int s = 0; s < ROWS - 1; ++s) {
+          const float4 x = *reinterpret_cast<const float4*>(joined + (s * NV * N + i * N + j) * TPR + 4 * t);
+          dw[i][j] += x.x; dw[i][j + 1] += x.y; dw[i][j + 2] += x.z; dw[i][j + 3] += x.w;
+        }
+  }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (t + i * TPR) * N;
     if (c < a.n) {
-      float* p = a.partial + ((size_t)blockIdx.x * ROWS + sub) * a.n + c;
+      float* p = a.partial + (size_t)blockIdx.x * a.n + c;
 #pragma unroll
       for (int j = 0; j < N; j += 4) *reinterpret_cast<float4*>(p + j) = make_float4(dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]);
     }
@@ -321,28 +362,26 @@ __global__ void __launch_bounds__(256) rms_norm_backward_any_kernel(const __grid
     }
   }
 }
-// dw = the sum of the partial rows, in their order: 32 columns and 8 runs of rows a block
+// dw = the sum of the partial rows, in an order that the sizes alone fix: 32 columns and 32 runs of rows a block
 template <class T>
-__global__ void __launch_bounds__(256) rms_norm_dw_kernel(const float* partial, T* dw, int n, int rows) {
-  __shared__ float part[8][33];
+__global__ void __launch_bounds__(1024) rms_norm_dw_kernel(const float* partial, T* dw, int n, int rows) {
+  __shared__ float part[32][33];
   const int lane = threadIdx.x & 31, run = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   wait_for_predecessor();
   float s[4] = {0.f, 0.f, 0.f, 0.f};
   if (c < n) {
     int r = run;
-    for (; r + 24 < rows; r += 32)
+    for (; r + 96 < rows; r += 128)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) s[q] += partial[(size_t)(r + 8 * q) * n + c];
-    for (; r < rows; r += 8) s[0] += partial[(size_t)r * n + c];
+      for (int q = 0; q < 4; ++q) s[q] += partial[(size_t)(r + 32 * q) * n + c];
+    for (; r < rows; r += 32) s[0] += partial[(size_t)r * n + c];
   }
   part[run][lane] = (s[0] + s[1]) + (s[2] + s[3]);
   __syncthreads();
-  if (run == 0 && c < n) {
-    float y = 0.f;
+  float y = part[lane][run];   // a warp a column
 #pragma unroll
-    for (int q = 0; q < 8; ++q) y += part[q][lane];
-    put(dw + c, y);
-  }
+  for (int m = 16; m >= 1; m >>= 1) y += __shfl_xor_sync(0xffffffffu, y, m);
+  if (lane == 0 && blockIdx.x * 32 + run < n) put(dw + blockIdx.x * 32 + run, y);
 }
 
 // Threads a row and vectors a thread for rows of `vecs` vectors: 0 threads where the register kernels do not take the row.
@@ -358,6 +397,16 @@ RowShape row_shape(int vecs, long long rows, int sms) {
   if (vecs <= 512) return few ? RowShape{256, 2} : RowShape{128, 4};
   if (vecs <= 1024) return {256, 4};
   return {512, 4};
+}
+// The gradient holds three rows twice and a row of sums: one vector a thread while the row allows it.
+RowShape backward_shape(int vecs) {
+  if (vecs <= 32) return {32, 1};
+  if (vecs <= 64) return {64, 1};
+  if (vecs <= 128) return {128, 1};
+  if (vecs <= 256) return {256, 1};
+  if (vecs <= 512) return {512, 1};
+  if (vecs <= 1024) return {512, 2};
+  return vecs <= 2048 ? RowShape{512, 4} : RowShape{0, 0};
 }
 bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -387,27 +436,28 @@ cudaError_t launch_forward(const RmsNormArgs& a, int sms, cudaStream_t stream) {
 template <class T>
 cudaError_t launch_backward(const RmsNormBackwardArgs& a, int sms, cudaStream_t stream) {
   const bool whole = a.n % Vec<T>::N == 0 && aligned(a.X) && aligned(a.dY) && aligned(a.w) && aligned(a.dH) && aligned(a.dX);
-  const RowShape f = whole ? row_shape(a.n / Vec<T>::N, a.rows, sms) : RowShape{0, 0};
+  const RowShape f = whole ? backward_shape(a.n / Vec<T>::N) : RowShape{0, 0};
   int partial_rows = 0;
   auto go = [&](auto kernel, int tpr) {
     const int threads = std::max(tpr, 256), rows = threads / tpr;
-    const int grid = (int)std::min<long long>((a.rows + rows - 1) / rows, (long long)kRmsNormPartials / rows);
-    partial_rows = grid * rows;
+    const int grid = (int)std::min<long long>((a.rows + rows - 1) / rows, kRmsNormPartials);
+    partial_rows = grid;
     return launch_early(kernel, dim3(grid), threads, 0, stream, a);
   };
   cudaError_t e = cudaSuccess;
   if (a.rows == 0) ;   // the sum of no rows
-  else if (f.tpr == 32) e = f.nv == 1 ? go(rms_norm_backward_kernel<T, 32, 1>, 32) : f.nv == 2 ? go(rms_norm_backward_kernel<T, 32, 2>, 32) : go(rms_norm_backward_kernel<T, 32, 4>, 32);
-  else if (f.tpr == 128) e = f.nv == 1 ? go(rms_norm_backward_kernel<T, 128, 1>, 128) : f.nv == 2 ? go(rms_norm_backward_kernel<T, 128, 2>, 128) : go(rms_norm_backward_kernel<T, 128, 4>, 128);
-  else if (f.tpr == 256) e = f.nv == 1 ? go(rms_norm_backward_kernel<T, 256, 1>, 256) : f.nv == 2 ? go(rms_norm_backward_kernel<T, 256, 2>, 256) : go(rms_norm_backward_kernel<T, 256, 4>, 256);
-  else if (f.tpr == 512) e = go(rms_norm_backward_kernel<T, 512, 4>, 512);
+  else if (f.tpr == 32) e = go(rms_norm_backward_kernel<T, 32, 1>, 32);
+  else if (f.tpr == 64) e = go(rms_norm_backward_kernel<T, 64, 1>, 64);
+  else if (f.tpr == 128) e = go(rms_norm_backward_kernel<T, 128, 1>, 128);
+  else if (f.tpr == 256) e = go(rms_norm_backward_kernel<T, 256, 1>, 256);
+  else if (f.tpr == 512) e = f.nv == 1 ? go(rms_norm_backward_kernel<T, 512, 1>, 512) : f.nv == 2 ? go(rms_norm_backward_kernel<T, 512, 2>, 512) : go(rms_norm_backward_kernel<T, 512, 4>, 512);
   else {
     partial_rows = (int)std::min<long long>(a.rows, kRmsNormPartials);
     rms_norm_backward_any_kernel<T><<<partial_rows, 256, 0, stream>>>(a);
     e = cudaGetLastError();
   }
   if (e != cudaSuccess || (a.rows > 0 && (e = launched()) != cudaSuccess)) return e;
-  e = launch_early(rms_norm_dw_kernel<T>, dim3((a.n + 31) / 32), 256, 0, stream, (const float*)a.partial, (T*)a.dw, a.n, partial_rows);
+  e = launch_early(rms_norm_dw_kernel<T>, dim3((a.n + 31) / 32), 1024, 0, stream, (const float*)a.partial, (T*)a.dw, a.n, partial_rows);
   return e == cudaSuccess ? launched() : e;
 }
 
