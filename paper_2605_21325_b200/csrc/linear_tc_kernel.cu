@@ -10,8 +10,8 @@
 // lambda is a constant of the head, so the factors of P, V~ and QS are formed once an item, in the registers of the threads that use them: a thread has
 // the same places of every tile.
 //
-// Warps 0..7 ("state"): lanes 32 (w & 3) .. + 31, half (w >> 2) of the features; S^T in fp32 registers for the whole item.  Warps 8..11 ("value"): V out of its
-// tile into tensor memory, transposed by ldmatrix, plain and scaled.  Warps 12..15 ("output"): P, and O one tile behind.  Then one warp each that issues
+// Warps 0..7 ("state"): lanes 32 (w & 3) .. + 31, half (w >> 2) of the features; S^T in fp32 registers for the whole item.  Warps 8..15 ("value"): V out of its
+// tile into tensor memory, transposed by ldmatrix, plain and scaled.  Warps 16..23 ("output"): P, and O one tile behind.  Then one warp each that issues
 // every product (control), requests the tile copies, and stores O by the copy engine.  Hand-offs are mbarriers with one phase a tile: a commit for a
 // product that is done, an arrival of each warp for an operand that is written or an accumulator that is read.
 //
@@ -24,7 +24,10 @@ namespace tri_inv {
 namespace {
 
 constexpr int L = kLinTile;
-constexpr int kStateWarps = 8, kValue = 8, kOutput = 12, kControlL = 16, kCopyL = 17, kStoreL = 18, kThreadsL = 19 * 32;
+constexpr int kStateWarps = 8, kValue = 8, kOutput = 16, kControlL = 24, kCopyL = 25, kStoreL = 26, kThreadsL = 28 * 32;
+// Registers of a thread of each role's warpgroups: 72 at launch (7 warpgroups), 2 x 104 + 2 x 64 + 2 x 64 + 40 = 7 x 72
+template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 struct LinMaps { CUtensorMap q[kLinMaxWalks], k[kLinMaxWalks], v[kLinMaxWalks], o[kLinMaxWalks]; };
 struct LinTcArgs {
@@ -43,25 +46,21 @@ struct LinCfg {
   static constexpr int OFF_K = KB * BOX, OFF_V = 2 * KB * BOX, STAGE = (2 * KB + VB) * BOX;
   static constexpr int STAGES = 4;
   static constexpr int OFF_P = STAGES * STAGE, OFF_O = OFF_P + L * 128, OFF_BAR = OFF_O + L * DV * 2,
-                       OFF_F = OFF_BAR + 256, SMEM = OFF_F + 8 * L * 4;   // F: the value and output warps' factors, a table of each warp
+                       OFF_F = OFF_BAR + 256, SMEM = OFF_F + 16 * L * 4;   // F: the value and output warps' factors, a table of each warp
   static constexpr int TM_S = 0, TM_V = TM_S + DK / 2, TM_VH = TM_V + 64, TM_VL = TM_VH + 32, TM_DS = TM_VL + 32, TM_QS = TM_DS + DK, TM_PV = TM_QS + 64, TM_QK = TM_PV + 64;
   static_assert(TM_QK + 64 <= 512 && SMEM <= 232448, "one CTA per SM");
 };
 
-// 32 lanes x 32 columns: a lane's row
-__device__ __forceinline__ void tmem_ld_row32(float (&r)[32], uint32_t taddr) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]),
-        "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]),
-        "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
-      : "r"(taddr));
+// 32 lanes x 16 columns: a lane's row
+__device__ __forceinline__ void tmem_ld_row16(float (&r)[16], uint32_t taddr) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+                 "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+               : "r"(taddr));
 }
-__device__ __forceinline__ void tmem_st_row16(const uint32_t (&r)[16], uint32_t taddr) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
-               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                 "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+__device__ __forceinline__ void tmem_st_row8(const uint32_t (&r)[8], uint32_t taddr) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
+               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr) : "memory");
 }
 
 // Two elements in one instruction, each rounded as by the scalar one: what the loops below issue is what bounds them
@@ -96,11 +95,11 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
   wait_for_predecessor();
   if (warp == kControlL) {
     if (lane == 0) {
-      for (int b = 0; b < cfg::STAGES; ++b) { mbar_init(bar_full + 8 * b, 1); mbar_init(bar_empty + 8 * b, 5); }
+      for (int b = 0; b < cfg::STAGES; ++b) { mbar_init(bar_full + 8 * b, 1); mbar_init(bar_empty + 8 * b, 9); }
       for (uint32_t b = b_ds; b <= b_exit; b += 8) mbar_init(b, 1);
-      mbar_init(b_vs, 4); mbar_init(b_sr, kStateWarps); mbar_init(b_pr, 4);
-      mbar_init(b_dsf, kStateWarps); mbar_init(b_qkf, 4); mbar_init(b_acc, 4);
-      mbar_init(b_o, 4); mbar_init(b_os, 1);
+      mbar_init(b_vs, 8); mbar_init(b_sr, kStateWarps); mbar_init(b_pr, 8);
+      mbar_init(b_dsf, kStateWarps); mbar_init(b_qkf, 8); mbar_init(b_acc, 8);
+      mbar_init(b_o, 8); mbar_init(b_os, 1);
       fence_mbar_init();
     }
     __syncwarp();
@@ -116,8 +115,15 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
   const uint32_t tmem_w = tmem + ((uint32_t)(32 * quad) << 16);   // this warp's lanes, column 0
   bool failed = misaligned;
   auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+    // (inline: a call would keep to the launch's registers)
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    return __all_sync(0xffffffffu, wait_by_warp(bar, parity, lim));
+    const unsigned long long t0 = global_timer_ns();
+#pragma unroll 1
+    for (uint32_t i = 1; i < kSpinLimit; ++i) {
+      if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+      if ((i & 63u) == 0 && __any_sync(0xffffffffu, global_timer_ns() - t0 > lim)) return false;
+    }
+    return false;
   };
   const bool whole = !a.state_only;
   const int per_walk = a.H * args.slices, per_seg = per_walk * args.n_walks, n_items = a.n_segs * per_seg;
@@ -147,114 +153,13 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
   auto stage = [](uint32_t t) { return t % cfg::STAGES; };
   auto lap = [](uint32_t t) { return (t / cfg::STAGES) & 1u; };
 
-  if (misaligned) {
-  } else if (warp == kControlL) {
-    // ---------------------------------------------------------------- control warp: every tcgen05.mma of the CTA
-    constexpr uint32_t idesc_qk = umma_idesc(64, 64, 0), idesc_ds = umma_idesc(cfg::M, 64, 1), idesc_s = umma_idesc(cfg::M, 64, 0);
-    const uint64_t dQ = umma_desc(s0, 16, 1024), dK = umma_desc(s0 + cfg::OFF_K, 16, 1024), dKm = umma_desc(s0 + cfg::OFF_K, cfg::BOX, 1024), dP = umma_desc(sP, 16, 1024);
-    auto issue_qk = [&](uint32_t t) {
-      const uint32_t st = (stage(t) * cfg::STAGE) >> 4;
-#pragma unroll
-      for (int ks = 0; ks < DK / 16; ++ks) {
-        const uint32_t off = st + (((ks >> 2) * cfg::BOX + (ks & 3) * 32) >> 4);
-        umma_bf16(tmem + cfg::TM_QK, dQ + off, dK + off, idesc_qk, ks > 0);
-      }
-      umma_commit(b_qk);
-    };
-    auto seen = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, mbar_test_wait(bar, parity)); };
-    for_items([&](const LinWalk& w, int, int, const LinSeg&, int, int, int n_tiles, float* s_out) -> bool {
-      for (int i = 0; i < n_tiles; ++i, ++t) {
-        const uint32_t ph = t & 1, st = (stage(t) * cfg::STAGE) >> 4;
-        if (i == 0) {
-          if (!wait(bar_full + 8 * stage(t), lap(t))) return false;
-          if (whole) {
-            if (t > 0 && !wait(b_qkf, ph ^ 1)) return false;
-            tc_fence_after();
-            issue_qk(t);
-          }
-        }
-        if (!wait(b_vs, ph) || (t > 0 && !wait(b_dsf, ph ^ 1))) return false;
-        tc_fence_after();
-        // self-test (LinArgs::test_stall): the first CTA leaves out this product of its second tile, so that its waits run out
-        const bool stall = a.test_stall && blockIdx.x == 0 && t == 1;
-#pragma unroll
-        for (int fh = 0; fh < cfg::KB; ++fh) {
-#pragma unroll
-          for (int ks = 0; ks < 4; ++ks)
-            if (!stall) umma_bf16_ta(tmem + cfg::TM_DS + 64 * fh, tmem + cfg::TM_VH + 8 * ks, dKm + st + ((fh * cfg::BOX + ks * 2048) >> 4), idesc_ds, ks > 0);
-        }
-        if (s_out && !stall) {
-#pragma unroll
-          for (int fh = 0; fh < cfg::KB; ++fh) {
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-              umma_bf16_ta(tmem + cfg::TM_DS + 64 * fh, tmem + cfg::TM_VL + 8 * ks, dKm + st + ((fh * cfg::BOX + ks * 2048) >> 4), idesc_ds, 1u);
-          }
-        }
-        if (!stall) umma_commit(b_ds);
-        if (!whole) {
-          umma_commit(bar_empty + 8 * stage(t));
-          if (i + 1 < n_tiles && !wait(bar_full + 8 * stage(t + 1), lap(t + 1))) return false;
-          continue;
-        }
-        // the next tile's QK, if its tiles have landed and this tile's QK has been read; otherwise behind PV
-        const bool more = i + 1 < n_tiles;
-        const bool early = more && seen(bar_full + 8 * stage(t + 1), lap(t + 1)) && seen(b_qkf, ph);
-        if (early) { tc_fence_after(); issue_qk(t + 1); }
-        if (!wait(b_sr, ph) || (t > 0 && !wait(b_acc, ph ^ 1))) return false;
-        tc_fence_after();
-#pragma unroll
-        for (int ks = 0; ks < DK / 16; ++ks)
-          umma_bf16_ta(tmem + cfg::TM_QS, tmem + cfg::TM_S + 8 * ks, dQ + st + (((ks >> 2) * cfg::BOX + (ks & 3) * 32) >> 4), idesc_s, ks > 0);
-        umma_commit(b_qs);
-        umma_commit(bar_empty + 8 * stage(t));
-        if (!wait(b_pr, ph)) return false;   // (V came with V~)
-        fence_proxy_async();   // P was written by ordinary stores
-        tc_fence_after();
-#pragma unroll
-        for (int ks = 0; ks < L / 16; ++ks)
-          umma_bf16_ta(tmem + cfg::TM_PV, tmem + cfg::TM_V + 32 * ph + 8 * ks, dP + ((ks * 32) >> 4), idesc_s, ks > 0);
-        umma_commit(b_pv);
-        if (more && !early) {
-          if (!wait(bar_full + 8 * stage(t + 1), lap(t + 1)) || !wait(b_qkf, ph)) return false;
-          tc_fence_after();
-          issue_qk(t + 1);
-        }
-      }
-      return true;
-    });
-    if (failed) {   // every product issued so far is waited for, with a limit, before the CTA gives up its memory
-      umma_commit(b_exit);
-      mbar_wait_bounded(b_exit, 0u, lim);
-    }
-  } else if (warp == kCopyL) {
-    // ---------------------------------------------------------------- copy warp
-    for_items([&](const LinWalk& w, int wi, int, const LinSeg& g, int h, int col0, int n_tiles, float*) -> bool {
-      for (int i = 0; i < n_tiles; ++i, ++t) {
-        if (t >= cfg::STAGES && !wait(bar_empty + 8 * stage(t), lap(t) ^ 1)) return false;
-        if (lane == 0) {
-          const uint32_t base = s0 + stage(t) * cfg::STAGE, bar = bar_full + 8 * stage(t);
-          const int tok = g.tok0 + tile_of(w, i, n_tiles) * L;
-          mbar_expect_tx(bar, whole ? cfg::STAGE : cfg::STAGE - cfg::KB * cfg::BOX);
-#pragma unroll
-          for (int b = 0; b < cfg::KB; ++b) tma_load_2d(base + cfg::OFF_K + b * cfg::BOX, &maps.k[wi], bar, h * DK + 64 * b, tok);
-#pragma unroll
-          for (int b = 0; b < cfg::VB; ++b) tma_load_2d(base + cfg::OFF_V + b * cfg::BOX, &maps.v[wi], bar, h * w.d_v + col0 + 64 * b, tok);
-          if (whole)
-#pragma unroll
-            for (int b = 0; b < cfg::KB; ++b) tma_load_2d(base + b * cfg::BOX, &maps.q[wi], bar, h * DK + 64 * b, tok);
-        }
-        __syncwarp();
-      }
-      return true;
-    });
-    if (failed && lane == 0)   // the copies still on their way into this CTA's shared memory
-      for (uint32_t c = t >= cfg::STAGES ? t - cfg::STAGES : 0; c < t; ++c) mbar_wait_bounded(bar_full + 8 * stage(c), lap(c), lim);
-  } else if (warp < kStateWarps) {
+  // (each role changes its registers first of all: nobody waits for a share that another still holds behind a wait)
+  if (warp < kStateWarps) {
     // ---------------------------------------------------------------- state warps
+    more_registers<104>();
     // S^T as pairs of features.  128 value columns: lane's row 32 quad + lane, features SH half + 2 c, + 1 (S[c]).  64: rows 16 quad + gq and + 8 in
     // lanes 0 .. 15, in accumulator fragments: S[2 nt + e] = row + 8 e, features SH half + 8 nt + t2, + 1.
-    constexpr int NP = cfg::SH / 2 * LG / 2, STEP = NP < 16 ? NP : 16;
+    constexpr int NP = cfg::SH / 2 * LG / 2, STEP = DV == 128 || NP < 16 ? 8 : 16;
     Pair S[NP];
     auto for_state = [&](auto&& f) {   // f(pair, value column, its first feature)
 #pragma unroll
@@ -282,7 +187,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
 #pragma unroll
             for (int q = 0; q < STEP; ++q) r[q] = pack_bf16(S[c + q]);
             const uint32_t at = tmem_w + cfg::TM_S + cfg::SH / 2 * half + c;
-            if constexpr (DV == 128) tmem_st_row16(r, at);
+            if constexpr (DV == 128) tmem_st_row8(r, at);
             else if constexpr (STEP == 16) tmem_st_packed32(r, at);
             else tmem_st_packed16(r, at);
           }
@@ -298,7 +203,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
         for (int c = 0; c < NP; c += STEP) {
           float ds[2 * STEP];
           const uint32_t at = tmem_w + cfg::TM_DS + cfg::SH * half + 2 * c;
-          if constexpr (DV == 128) tmem_ld_row32(ds, at);
+          if constexpr (DV == 128) tmem_ld_row16(ds, at);
           else if constexpr (STEP == 16) tmem_ld_16x64(reinterpret_cast<float (&)[8][4]>(ds), at);
           else tmem_ld_16x32(reinterpret_cast<float (&)[4][4]>(ds), at);
           tmem_wait_ld();
@@ -317,8 +222,9 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
     });
   } else if (warp < kOutput) {
     // ---------------------------------------------------------------- value warps
+    fewer_registers<64>();
     const int row0 = quad * cfg::RPQ;
-    float* f = reinterpret_cast<float*>(smem + cfg::OFF_F) + quad * L;   // this warp's table of the tokens' factors
+    float* f = reinterpret_cast<float*>(smem + cfg::OFF_F) + (warp - kValue) * L;   // this warp's table of the tokens' factors
     for_items([&](const LinWalk& w, int, int, const LinSeg& g, int h, int col0, int n_tiles, float* s_out) -> bool {
       const float l2 = lin_log2_decay(a, h);
       int made_for = 0;
@@ -336,56 +242,52 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
         if (rows < L) {
           // Behind the sequence's end lie a neighbour's rows.  V counts as zero there (below), and zero times a key that is not finite is not zero: the key
           // tile's rows are cleared too (QK may be reading them: those columns of P are left out by selection)
-          for (int e = tid - 32 * kValue; e < (L - rows) * 8 * cfg::KB; e += 128)
+          for (int e = tid - 32 * kValue; e < (L - rows) * 8 * cfg::KB; e += 256)
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + cfg::OFF_K + (e / ((L - rows) * 8)) * cfg::BOX + (rows + (e / 8) % (L - rows)) * 128 + (e & 7) * 16), "r"(0) : "memory");
           fence_proxy_async();
         }
-        uint32_t x[LG][2][8];   // V: pairs of tokens 32 th + 8 nt + t2, + 1 of value columns row0 + 16 lg + gq (2 nt) and + 8 (2 nt + 1)
+        // A warp's part: with 128 value columns 16 of its quadrant's (half) and all tokens, with 64 the quadrant's 16 and 32 tokens (half)
+        constexpr int TH = LG;   // blocks of 32 tokens
+        const int lg = LG == 2 ? half : 0, th0 = LG == 2 ? 0 : half;
+        uint32_t x[TH][8];   // V: pairs of tokens 32 (th0 + th) + 8 nt + t2, + 1 of value columns row0 + 16 lg + gq (2 nt) and + 8 (2 nt + 1)
 #pragma unroll
-        for (int lg = 0; lg < LG; ++lg)
+        for (int th = 0; th < TH; ++th)
 #pragma unroll
-          for (int th = 0; th < 2; ++th)
-#pragma unroll
-            for (int nt = 0; nt < 4; nt += 2) {
-              const int tok = 32 * th + 8 * (nt + (mi >> 1)) + mr, n = row0 + 16 * lg + 8 * (mi & 1);
-              ldmatrix_x4_trans(sV + (n >> 6) * cfg::BOX + tok * 128 + ((((n & 63) >> 3) ^ (tok & 7)) << 4), x[lg][th][2 * nt], x[lg][th][2 * nt + 1], x[lg][th][2 * nt + 2],
-                                x[lg][th][2 * nt + 3]);
-            }
+          for (int nt = 0; nt < 4; nt += 2) {
+            const int tok = 32 * (th0 + th) + 8 * (nt + (mi >> 1)) + mr, n = row0 + 16 * lg + 8 * (mi & 1);
+            ldmatrix_x4_trans(sV + (n >> 6) * cfg::BOX + tok * 128 + ((((n & 63) >> 3) ^ (tok & 7)) << 4), x[th][2 * nt], x[th][2 * nt + 1], x[th][2 * nt + 2], x[th][2 * nt + 3]);
+          }
         if (rows < L) {
 #pragma unroll
-          for (int th = 0; th < 2; ++th)
+          for (int th = 0; th < TH; ++th)
 #pragma unroll
             for (int nt = 0; nt < 4; ++nt) {
-              const int j = 32 * th + 8 * nt + t2;
+              const int j = 32 * (th0 + th) + 8 * nt + t2;
               const uint32_t keep = (j < rows ? 0xffffu : 0u) | (j + 1 < rows ? 0xffff0000u : 0u);
-#pragma unroll
-              for (int lg = 0; lg < LG; ++lg) { x[lg][th][2 * nt] &= keep; x[lg][th][2 * nt + 1] &= keep; }
+              x[th][2 * nt] &= keep;
+              x[th][2 * nt + 1] &= keep;
             }
         }
         // DS of the tile before is done: V~ may be overwritten; and with it, since products are done in order, PV of the one before that: V is kept for two tiles in turn
         if (t > 0 && !wait(b_ds, ph ^ 1)) return false;
         tc_fence_after();
 #pragma unroll
-        for (int th = 0; th < 2; ++th) {
-          Pair fj[4];
+        for (int th = 0; th < TH; ++th) {
+          uint32_t hi[8], lo[8];
 #pragma unroll
-          for (int nt = 0; nt < 4; ++nt) { const float2 y = *reinterpret_cast<const float2*>(f + 32 * th + 8 * nt + t2); fj[nt] = pair(y.x, y.y); }
+          for (int nt = 0; nt < 4; ++nt) {
+            const float2 fj = *reinterpret_cast<const float2*>(f + 32 * (th0 + th) + 8 * nt + t2);
 #pragma unroll
-          for (int lg = 0; lg < LG; ++lg) {
-            uint32_t hi[8], lo[8];
-#pragma unroll
-            for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const Pair y = mul2(unpack_bf16(x[lg][th][2 * nt + e]), fj[nt]);
-                hi[2 * nt + e] = pack_bf16(y);
-                if (s_out) lo[2 * nt + e] = pack_bf16(fma2(unpack_bf16(hi[2 * nt + e]), pair(-1.f, -1.f), y));
-              }
-            const uint32_t at = tmem_w + ((uint32_t)(16 * lg) << 16) + 16 * th;
-            tmem_st_packed16(hi, at + cfg::TM_VH);
-            if (s_out) tmem_st_packed16(lo, at + cfg::TM_VL);
-            if (whole) tmem_st_packed16(x[lg][th], at + cfg::TM_V + 32 * ph);
+            for (int e = 0; e < 2; ++e) {
+              const Pair y = mul2(unpack_bf16(x[th][2 * nt + e]), pair(fj.x, fj.y));
+              hi[2 * nt + e] = pack_bf16(y);
+              if (s_out) lo[2 * nt + e] = pack_bf16(fma2(unpack_bf16(hi[2 * nt + e]), pair(-1.f, -1.f), y));
+            }
           }
+          const uint32_t at = tmem_w + ((uint32_t)(16 * lg) << 16) + 16 * (th0 + th);
+          tmem_st_packed16(hi, at + cfg::TM_VH);
+          if (s_out) tmem_st_packed16(lo, at + cfg::TM_VL);
+          if (whole) tmem_st_packed16(x[th], at + cfg::TM_V + 32 * ph);
         }
         tmem_wait_st();
         tc_fence_before();
@@ -394,18 +296,20 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
       }
       return true;
     });
-  } else if (warp < kControlL && whole) {
+  } else if (warp < kControlL) {
     // ---------------------------------------------------------------- output warps
+    fewer_registers<64>();
+    if (whole) {
     const int row0 = quad * cfg::RPQ, ia = 16 * quad + gq, ib = ia + 8;
-    float* y = reinterpret_cast<float*>(smem + cfg::OFF_F) + (4 + quad) * L;   // this warp's table of the tokens' factors of QS
+    float* y = reinterpret_cast<float*>(smem + cfg::OFF_F) + (warp - kValue) * L;   // this warp's table of the tokens' factors of QS
     for_items([&](const LinWalk& w, int, int, const LinSeg& g, int h, int col0, int n_tiles, float*) -> bool {
       const float l2 = lin_log2_decay(a, h), pv_factor = w.k_factor * w.out_factor;
-      Pair f[8][2];   // P's factors, zero where it is masked: columns 8 nt + t2, + 1 of rows ia and ib
+      Pair f[4][2];   // P's factors, zero where it is masked: columns 32 half + 8 nt + t2, + 1 of rows ia and ib
 #pragma unroll
-      for (int nt = 0; nt < 8; ++nt)
+      for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int d = (e ? ib : ia) - (8 * nt + t2), g0 = w.back ? -d : d, g1 = w.back ? 1 - d : d - 1;
+          const int d = (e ? ib : ia) - (32 * half + 8 * nt + t2), g0 = w.back ? -d : d, g1 = w.back ? 1 - d : d - 1;
           f[nt][e] = pair(g0 >= 0 ? exp2f(l2 * g0) : 0.f, g1 >= 0 ? exp2f(l2 * g1) : 0.f);
         }
       int made_for = 0;
@@ -419,34 +323,29 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
           __syncwarp();
         }
         if (t > 0 && !wait(b_os, (t - 1) & 1)) return false;   // the last tile's store has read it
+        // a warp's part as the value warps': 16 value columns and all tokens, or 32 of them
+        constexpr int HF = LG;
+        const int lg = LG == 2 ? half : 0, hf0 = LG == 2 ? 0 : half;
 #pragma unroll
-        for (int lg = 0; lg < LG; ++lg) {
-          // 64 tokens x 16 value columns: two halves' loads in flight
-          float pv[2][4][4], qs[2][4][4];
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            const uint32_t at = tmem_w + ((uint32_t)(16 * lg) << 16) + 32 * hf;
-            tmem_ld_16x32(pv[hf], at + cfg::TM_PV);
-            tmem_ld_16x32(qs[hf], at + cfg::TM_QS);
-          }
+        for (int hf = 0; hf < HF; ++hf) {
+          float pv[4][4], qs[4][4];
+          const uint32_t at = tmem_w + ((uint32_t)(16 * lg) << 16) + 32 * (hf0 + hf);
+          tmem_ld_16x32(pv, at + cfg::TM_PV);
+          tmem_ld_16x32(qs, at + cfg::TM_QS);
           tmem_wait_ld();
-          if (lg == LG - 1) { tc_fence_before(); warp_arrive(b_acc, lane); }
+          if (hf == HF - 1) { tc_fence_before(); warp_arrive(b_acc, lane); }
+          uint32_t o[4][2];
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            uint32_t o[4][2];
+          for (int nt = 0; nt < 4; ++nt) {
+            const float2 yt = *reinterpret_cast<const float2*>(y + 32 * (hf0 + hf) + 8 * nt + t2);
 #pragma unroll
-            for (int nt = 0; nt < 4; ++nt) {
-              const float2 yt = *reinterpret_cast<const float2*>(y + 32 * hf + 8 * nt + t2);
+            for (int e = 0; e < 2; ++e)
+              o[nt][e] = pack_bf16(fma2(pair(pv[nt][2 * e], pv[nt][2 * e + 1]), pair(pv_factor, pv_factor), mul2(pair(yt.x, yt.y), pair(qs[nt][2 * e], qs[nt][2 * e + 1]))));
+          }
 #pragma unroll
-              for (int e = 0; e < 2; ++e)
-                o[nt][e] = pack_bf16(fma2(pair(pv[hf][nt][2 * e], pv[hf][nt][2 * e + 1]), pair(pv_factor, pv_factor),
-                                          mul2(pair(yt.x, yt.y), pair(qs[hf][nt][2 * e], qs[hf][nt][2 * e + 1]))));
-            }
-#pragma unroll
-            for (int nt = 0; nt < 4; nt += 2) {
-              const int tok = 32 * hf + 8 * (nt + (mi >> 1)) + mr, col = row0 + 16 * lg + 8 * (mi & 1);
-              stmatrix_x4_trans(s0 + cfg::OFF_O + (col >> 6) * cfg::BOX + tok * 128 + ((((col >> 3) ^ tok) & 7) << 4), o[nt][0], o[nt][1], o[nt + 1][0], o[nt + 1][1]);
-            }
+          for (int nt = 0; nt < 4; nt += 2) {
+            const int tok = 32 * (hf0 + hf) + 8 * (nt + (mi >> 1)) + mr, col = row0 + 16 * lg + 8 * (mi & 1);
+            stmatrix_x4_trans(s0 + cfg::OFF_O + (col >> 6) * cfg::BOX + tok * 128 + ((((col >> 3) ^ tok) & 7) << 4), o[nt][0], o[nt][1], o[nt + 1][0], o[nt + 1][1]);
           }
         }
         warp_arrive(b_o, lane);
@@ -456,27 +355,27 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
       for (int i = 0; i <= n_tiles && n_tiles > 0; ++i, ++t) {
         const uint32_t ph = t & 1;
         const bool more = i < n_tiles;
-        uint32_t wa[8], wb[8];
+        uint32_t wa[4], wb[4];
         int rows = 0;
         if (more) {
           rows = rows_of(g, tile_of(w, i, n_tiles));
           if (!wait(b_qk, ph)) return false;
           tc_fence_after();
-          float qk[8][4];
-          tmem_ld_16x64(qk, tmem_w + cfg::TM_QK);
+          float qk[4][4];
+          tmem_ld_16x32(qk, tmem_w + cfg::TM_QK + 32 * half);
           tmem_wait_ld();
           tc_fence_before();
           warp_arrive(b_qkf, lane);
           if (rows < L) {   // columns behind the sequence's end: a neighbour's keys, which need not be finite
 #pragma unroll
-            for (int nt = 0; nt < 8; ++nt) {
-              const int j = 8 * nt + t2;
+            for (int nt = 0; nt < 4; ++nt) {
+              const int j = 32 * half + 8 * nt + t2;
               if (j >= rows) qk[nt][0] = qk[nt][2] = 0.f;
               if (j + 1 >= rows) qk[nt][1] = qk[nt][3] = 0.f;
             }
           }
 #pragma unroll
-          for (int nt = 0; nt < 8; ++nt) {
+          for (int nt = 0; nt < 4; ++nt) {
             wa[nt] = pack_bf16(mul2(pair(qk[nt][0], qk[nt][1]), f[nt][0]));
             wb[nt] = pack_bf16(mul2(pair(qk[nt][2], qk[nt][3]), f[nt][1]));
           }
@@ -486,7 +385,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
         if (more) {
           const int row = 16 * quad + 8 * (mi & 1) + mr;
 #pragma unroll
-          for (int nt = 0; nt < 8; nt += 2) stmatrix_x4(sP + row * 128 + (((nt + (mi >> 1)) ^ (row & 7)) << 4), wa[nt], wb[nt], wa[nt + 1], wb[nt + 1]);
+          for (int nt = 0; nt < 4; nt += 2) stmatrix_x4(sP + row * 128 + (((4 * half + nt + (mi >> 1)) ^ (row & 7)) << 4), wa[nt], wb[nt], wa[nt + 1], wb[nt + 1]);
           warp_arrive(b_pr, lane);   // (the fence for the asynchronous proxy is the control warp's)
         }
         if (i > 0 && !put_output(t - 1, last_rows)) return false;
@@ -495,32 +394,139 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
       }
       return true;
     });
-  } else if (warp == kStoreL && whole) {
-    // ---------------------------------------------------------------- store warp: O's tile to memory
-    for_items([&](const LinWalk& w, int wi, int, const LinSeg& g, int h, int col0, int n_tiles, float*) -> bool {
-      for (int i = 0; i < n_tiles; ++i, ++t) {
-        if (!wait(b_o, t & 1)) return false;
-        const int tile = tile_of(w, i, n_tiles), tok0 = g.tok0 + tile * L, rows = rows_of(g, tile);
-        if (rows == L) {
-          if (lane == 0) {
-            fence_proxy_async();   // the tile was written by ordinary stores
+    }
+  } else {
+    // the last warpgroup: one of its warps has no role.  (setmaxnreg is one instruction for a whole warpgroup)
+    fewer_registers<40>();
+    if (warp == kControlL) {
+      // ---------------------------------------------------------------- control warp: every tcgen05.mma of the CTA
+      constexpr uint32_t idesc_qk = umma_idesc(64, 64, 0), idesc_ds = umma_idesc(cfg::M, 64, 1), idesc_s = umma_idesc(cfg::M, 64, 0);
+      const uint64_t dQ = umma_desc(s0, 16, 1024), dK = umma_desc(s0 + cfg::OFF_K, 16, 1024), dKm = umma_desc(s0 + cfg::OFF_K, cfg::BOX, 1024), dP = umma_desc(sP, 16, 1024);
+      auto issue_qk = [&](uint32_t t) {
+        const uint32_t st = (stage(t) * cfg::STAGE) >> 4;
 #pragma unroll
-            for (int b = 0; b < cfg::VB; ++b) tma_store_2d(&maps.o[wi], s0 + cfg::OFF_O + b * cfg::BOX, h * w.d_v + col0 + 64 * b, tok0);
-            bulk_commit();
-            bulk_wait_read();
+        for (int ks = 0; ks < DK / 16; ++ks) {
+          const uint32_t off = st + (((ks >> 2) * cfg::BOX + (ks & 3) * 32) >> 4);
+          umma_bf16(tmem + cfg::TM_QK, dQ + off, dK + off, idesc_qk, ks > 0);
+        }
+        umma_commit(b_qk);
+      };
+      auto seen = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, mbar_test_wait(bar, parity)); };
+      for_items([&](const LinWalk& w, int, int, const LinSeg&, int, int, int n_tiles, float* s_out) -> bool {
+        for (int i = 0; i < n_tiles; ++i, ++t) {
+          const uint32_t ph = t & 1, st = (stage(t) * cfg::STAGE) >> 4;
+          if (i == 0) {
+            if (!wait(bar_full + 8 * stage(t), lap(t))) return false;
+            if (whole) {
+              if (t > 0 && !wait(b_qkf, ph ^ 1)) return false;
+              tc_fence_after();
+              issue_qk(t);
+            }
           }
-        } else {
-          __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(w.out) + ((size_t)tok0 * a.H + h) * w.d_v + col0;
-          for (int e = lane; e < rows * (DV / 8); e += 32) {
-            const int tok = e / (DV / 8), pc = e % (DV / 8);
-            *reinterpret_cast<uint4*>(out + (size_t)tok * a.H * w.d_v + 8 * pc) =
-                *reinterpret_cast<const uint4*>(smem + cfg::OFF_O + (pc >> 3) * cfg::BOX + tok * 128 + (((pc ^ tok) & 7) << 4));
+          if (!wait(b_vs, ph) || (t > 0 && !wait(b_dsf, ph ^ 1))) return false;
+          tc_fence_after();
+          // self-test (LinArgs::test_stall): the first CTA leaves out this product of its second tile, so that its waits run out
+          const bool stall = a.test_stall && blockIdx.x == 0 && t == 1;
+#pragma unroll
+          for (int fh = 0; fh < cfg::KB; ++fh) {
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              if (!stall) umma_bf16_ta(tmem + cfg::TM_DS + 64 * fh, tmem + cfg::TM_VH + 8 * ks, dKm + st + ((fh * cfg::BOX + ks * 2048) >> 4), idesc_ds, ks > 0);
+          }
+          if (s_out && !stall) {
+#pragma unroll
+            for (int fh = 0; fh < cfg::KB; ++fh) {
+#pragma unroll
+              for (int ks = 0; ks < 4; ++ks)
+                umma_bf16_ta(tmem + cfg::TM_DS + 64 * fh, tmem + cfg::TM_VL + 8 * ks, dKm + st + ((fh * cfg::BOX + ks * 2048) >> 4), idesc_ds, 1u);
+            }
+          }
+          if (!stall) umma_commit(b_ds);
+          if (!whole) {
+            umma_commit(bar_empty + 8 * stage(t));
+            if (i + 1 < n_tiles && !wait(bar_full + 8 * stage(t + 1), lap(t + 1))) return false;
+            continue;
+          }
+          // the next tile's QK, if its tiles have landed and this tile's QK has been read; otherwise behind PV
+          const bool more = i + 1 < n_tiles;
+          const bool early = more && seen(bar_full + 8 * stage(t + 1), lap(t + 1)) && seen(b_qkf, ph);
+          if (early) { tc_fence_after(); issue_qk(t + 1); }
+          if (!wait(b_sr, ph) || (t > 0 && !wait(b_acc, ph ^ 1))) return false;
+          tc_fence_after();
+#pragma unroll
+          for (int ks = 0; ks < DK / 16; ++ks)
+            umma_bf16_ta(tmem + cfg::TM_QS, tmem + cfg::TM_S + 8 * ks, dQ + st + (((ks >> 2) * cfg::BOX + (ks & 3) * 32) >> 4), idesc_s, ks > 0);
+          umma_commit(b_qs);
+          umma_commit(bar_empty + 8 * stage(t));
+          if (!wait(b_pr, ph)) return false;   // (V came with V~)
+          fence_proxy_async();   // P was written by ordinary stores
+          tc_fence_after();
+#pragma unroll
+          for (int ks = 0; ks < L / 16; ++ks)
+            umma_bf16_ta(tmem + cfg::TM_PV, tmem + cfg::TM_V + 32 * ph + 8 * ks, dP + ((ks * 32) >> 4), idesc_s, ks > 0);
+          umma_commit(b_pv);
+          if (more && !early) {
+            if (!wait(bar_full + 8 * stage(t + 1), lap(t + 1)) || !wait(b_qkf, ph)) return false;
+            tc_fence_after();
+            issue_qk(t + 1);
           }
         }
-        warp_arrive(b_os, lane);
+        return true;
+      });
+      if (failed) {   // every product issued so far is waited for, with a limit, before the CTA gives up its memory
+        umma_commit(b_exit);
+        mbar_wait_bounded(b_exit, 0u, lim);
       }
-      return true;
-    });
+    } else if (warp == kCopyL) {
+      // ---------------------------------------------------------------- copy warp
+      for_items([&](const LinWalk& w, int wi, int, const LinSeg& g, int h, int col0, int n_tiles, float*) -> bool {
+        for (int i = 0; i < n_tiles; ++i, ++t) {
+          if (t >= cfg::STAGES && !wait(bar_empty + 8 * stage(t), lap(t) ^ 1)) return false;
+          if (lane == 0) {
+            const uint32_t base = s0 + stage(t) * cfg::STAGE, bar = bar_full + 8 * stage(t);
+            const int tok = g.tok0 + tile_of(w, i, n_tiles) * L;
+            mbar_expect_tx(bar, whole ? cfg::STAGE : cfg::STAGE - cfg::KB * cfg::BOX);
+#pragma unroll
+            for (int b = 0; b < cfg::KB; ++b) tma_load_2d(base + cfg::OFF_K + b * cfg::BOX, &maps.k[wi], bar, h * DK + 64 * b, tok);
+#pragma unroll
+            for (int b = 0; b < cfg::VB; ++b) tma_load_2d(base + cfg::OFF_V + b * cfg::BOX, &maps.v[wi], bar, h * w.d_v + col0 + 64 * b, tok);
+            if (whole)
+#pragma unroll
+              for (int b = 0; b < cfg::KB; ++b) tma_load_2d(base + b * cfg::BOX, &maps.q[wi], bar, h * DK + 64 * b, tok);
+          }
+          __syncwarp();
+        }
+        return true;
+      });
+      if (failed && lane == 0)   // the copies still on their way into this CTA's shared memory
+        for (uint32_t c = t >= cfg::STAGES ? t - cfg::STAGES : 0; c < t; ++c) mbar_wait_bounded(bar_full + 8 * stage(c), lap(c), lim);
+    } else if (warp == kStoreL && whole) {
+      // ---------------------------------------------------------------- store warp: O's tile to memory
+      for_items([&](const LinWalk& w, int wi, int, const LinSeg& g, int h, int col0, int n_tiles, float*) -> bool {
+        for (int i = 0; i < n_tiles; ++i, ++t) {
+          if (!wait(b_o, t & 1)) return false;
+          const int tile = tile_of(w, i, n_tiles), tok0 = g.tok0 + tile * L, rows = rows_of(g, tile);
+          if (rows == L) {
+            if (lane == 0) {
+              fence_proxy_async();   // the tile was written by ordinary stores
+#pragma unroll
+              for (int b = 0; b < cfg::VB; ++b) tma_store_2d(&maps.o[wi], s0 + cfg::OFF_O + b * cfg::BOX, h * w.d_v + col0 + 64 * b, tok0);
+              bulk_commit();
+              bulk_wait_read();
+            }
+          } else {
+            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(w.out) + ((size_t)tok0 * a.H + h) * w.d_v + col0;
+            for (int e = lane; e < rows * (DV / 8); e += 32) {
+              const int tok = e / (DV / 8), pc = e % (DV / 8);
+              *reinterpret_cast<uint4*>(out + (size_t)tok * a.H * w.d_v + 8 * pc) =
+                  *reinterpret_cast<const uint4*>(smem + cfg::OFF_O + (pc >> 3) * cfg::BOX + tok * 128 + (((pc ^ tok) & 7) << 4));
+            }
+          }
+          warp_arrive(b_os, lane);
+        }
+        return true;
+      });
+    }
   }
   if (failed) atomicMax(a.status, (int)TRI_INV_ERR_DEVICE_TIMEOUT);
   tc_fence_before();
