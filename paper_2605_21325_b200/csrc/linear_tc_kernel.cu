@@ -24,7 +24,7 @@ namespace tri_inv {
 namespace {
 
 constexpr int L = kLinTile;
-constexpr int kStateWarps = 8, kValue = 8, kOutput = 16, kControlL = 24, kCopyL = 25, kStoreL = 26, kThreadsL = 28 * 32;
+constexpr int kStateWarps = 8, kValue = 8, kOutput = 16, kControlA = 24, kControlB = 25, kCopyL = 26, kStoreL = 27, kThreadsL = 28 * 32;
 // Registers of a thread of each role's warpgroups: 72 at launch (7 warpgroups), 2 x 104 + 2 x 64 + 2 x 64 + 40 = 7 x 72
 template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -79,24 +79,25 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
   constexpr int LG = cfg::LG;
   extern __shared__ __align__(1024) uint8_t smem[];
   const LinArgs& a = args.a;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + cfg::OFF_BAR + 192);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + cfg::OFF_BAR + 224);
   const uint32_t s0 = smem_u32(smem), sP = s0 + cfg::OFF_P, bars = s0 + cfg::OFF_BAR;
-  // copies: bar_full + 8 stage; stage free again: bar_empty + 8 stage (its products' commit, value warps)
-  // products done (commit): ds, qs, qk, pv.  Operands written: vs (V and V~, value warps), sr (S^T, state warps), pr (P, output warps).
+  // copies: bar_full + 8 stage; stage free again: bar_empty + 8 stage (both control warps' commits, value warps)
+  // products done (commit): ds, qs, qk, pv.  Operands written: vs (V~, value warps), vr (V), sr (S^T, state warps), pr (P, output warps).
   // Accumulators read: dsf (DS), qkf (QK), acc (QS and PV).  O's tile: o full, os read.
-  const uint32_t bar_full = bars, bar_empty = bars + 32, b_ds = bars + 64, b_qs = bars + 72, b_qk = bars + 80, b_pv = bars + 88, b_exit = bars + 96,
-                 b_vs = bars + 104, b_sr = bars + 120, b_pr = bars + 128, b_dsf = bars + 136, b_qkf = bars + 144, b_acc = bars + 152,
-                 b_o = bars + 160, b_os = bars + 168;
+  const uint32_t bar_full = bars, bar_empty = bars + 32, b_ds = bars + 64, b_qs = bars + 72, b_qk = bars + 80, b_exit = bars + 88, b_exitb = bars + 96,
+                 b_vs = bars + 104, b_vr = bars + 192, b_pv = bars + 112 /* two of each, in turn: V is kept for two tiles, and the value warps may be two ahead */, b_sr = bars + 128, b_pr = bars + 136, b_dsf = bars + 144, b_qkf = bars + 152, b_acc = bars + 160,
+                 b_o = bars + 168, b_os = bars + 176;
   const unsigned long long lim = a.wait_limit_ns ? a.wait_limit_ns : kWaitLimitNs;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;   // warp: uniform for the compiler
   const int quad = warp & 3, half = (warp >> 2) & 1;
   const int gq = lane >> 2, t2 = 2 * (lane & 3), mi = lane >> 3, mr = lane & 7;
   const bool misaligned = (s0 & 1023u) != 0;     // never expected; the swizzle pattern would not match the copies
   wait_for_predecessor();
-  if (warp == kControlL) {
+  if (warp == kControlA) {
     if (lane == 0) {
-      for (int b = 0; b < cfg::STAGES; ++b) { mbar_init(bar_full + 8 * b, 1); mbar_init(bar_empty + 8 * b, 9); }
-      for (uint32_t b = b_ds; b <= b_exit; b += 8) mbar_init(b, 1);
+      for (int b = 0; b < cfg::STAGES; ++b) { mbar_init(bar_full + 8 * b, 1); mbar_init(bar_empty + 8 * b, a.state_only ? 9 : 10); }
+      for (uint32_t b = b_ds; b <= b_exitb; b += 8) mbar_init(b, 1);
+      mbar_init(b_pv, 1); mbar_init(b_pv + 8, 1); mbar_init(b_vr, 8); mbar_init(b_vr + 8, 8);
       mbar_init(b_vs, 8); mbar_init(b_sr, kStateWarps); mbar_init(b_pr, 8);
       mbar_init(b_dsf, kStateWarps); mbar_init(b_qkf, 8); mbar_init(b_acc, 8);
       mbar_init(b_o, 8); mbar_init(b_os, 1);
@@ -268,7 +269,6 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
               x[th][2 * nt + 1] &= keep;
             }
         }
-        // DS of the tile before is done: V~ may be overwritten; and with it, since products are done in order, PV of the one before that: V is kept for two tiles in turn
         if (t > 0 && !wait(b_ds, ph ^ 1)) return false;
         tc_fence_after();
 #pragma unroll
@@ -287,16 +287,24 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
           const uint32_t at = tmem_w + ((uint32_t)(16 * lg) << 16) + 16 * (th0 + th);
           tmem_st_packed16(hi, at + cfg::TM_VH);
           if (s_out) tmem_st_packed16(lo, at + cfg::TM_VL);
-          if (whole) tmem_st_packed16(x[th], at + cfg::TM_V + 32 * ph);
         }
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) { mbar_arrive(b_vs); mbar_arrive(bar_empty + 8 * stage(t)); }
+        if (whole) {   // V itself, kept for two tiles in turn
+          if (t > 1 && !wait(b_pv + 8 * ph, ((t >> 1) & 1) ^ 1)) return false;
+          tc_fence_after();
+#pragma unroll
+          for (int th = 0; th < TH; ++th) tmem_st_packed16(x[th], tmem_w + ((uint32_t)(16 * lg) << 16) + 16 * (th0 + th) + cfg::TM_V + 32 * ph);
+          tmem_wait_st();
+          tc_fence_before();
+          warp_arrive(b_vr + 8 * ph, lane);
+        }
       }
       return true;
     });
-  } else if (warp < kControlL) {
+  } else if (warp < kControlA) {
     // ---------------------------------------------------------------- output warps
     fewer_registers<64>();
     if (whole) {
@@ -380,7 +388,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
             wb[nt] = pack_bf16(mul2(pair(qk[nt][2], qk[nt][3]), f[nt][1]));
           }
         }
-        if (t > 0 && !wait(b_pv, ph ^ 1)) return false;   // PV of the tile before is done: its O can be read, and P's tile is free
+        if (t > 0 && !wait(b_pv + 8 * (ph ^ 1), ((t - 1) >> 1) & 1)) return false;   // PV of the tile before is done: its O can be read, and P's tile is free
         tc_fence_after();
         if (more) {
           const int row = 16 * quad + 8 * (mi & 1) + mr;
@@ -396,12 +404,14 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
     });
     }
   } else {
-    // the last warpgroup: one of its warps has no role.  (setmaxnreg is one instruction for a whole warpgroup)
+    // the last warpgroup, a role a warp (setmaxnreg is one instruction for all of it)
     fewer_registers<40>();
-    if (warp == kControlL) {
-      // ---------------------------------------------------------------- control warp: every tcgen05.mma of the CTA
-      constexpr uint32_t idesc_qk = umma_idesc(64, 64, 0), idesc_ds = umma_idesc(cfg::M, 64, 1), idesc_s = umma_idesc(cfg::M, 64, 0);
-      const uint64_t dQ = umma_desc(s0, 16, 1024), dK = umma_desc(s0 + cfg::OFF_K, 16, 1024), dKm = umma_desc(s0 + cfg::OFF_K, cfg::BOX, 1024), dP = umma_desc(sP, 16, 1024);
+    // The descriptors below differ from their bases only in the address field (bits 0 .. 13, units of 16 bytes).
+    const uint64_t dQ = umma_desc(s0, 16, 1024), dK = umma_desc(s0 + cfg::OFF_K, 16, 1024), dKm = umma_desc(s0 + cfg::OFF_K, cfg::BOX, 1024), dP = umma_desc(sP, 16, 1024);
+    if (warp == kControlA) {
+      // ---------------------------------------------------------------- control warp A: DS and QK, which need no state.  (One warp for all the products was what bounded a
+      // tile: 36 instructions and seven waits, 2,200 cycles)
+      constexpr uint32_t idesc_qk = umma_idesc(64, 64, 0), idesc_ds = umma_idesc(cfg::M, DK, 1);
       auto issue_qk = [&](uint32_t t) {
         const uint32_t st = (stage(t) * cfg::STAGE) >> 4;
 #pragma unroll
@@ -411,7 +421,6 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
         }
         umma_commit(b_qk);
       };
-      auto seen = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, mbar_test_wait(bar, parity)); };
       for_items([&](const LinWalk& w, int, int, const LinSeg&, int, int, int n_tiles, float* s_out) -> bool {
         for (int i = 0; i < n_tiles; ++i, ++t) {
           const uint32_t ph = t & 1, st = (stage(t) * cfg::STAGE) >> 4;
@@ -427,48 +436,23 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
           tc_fence_after();
           // self-test (LinArgs::test_stall): the first CTA leaves out this product of its second tile, so that its waits run out
           const bool stall = a.test_stall && blockIdx.x == 0 && t == 1;
+          if (!stall) {
 #pragma unroll
-          for (int fh = 0; fh < cfg::KB; ++fh) {
+            for (int ks = 0; ks < 4; ++ks) umma_bf16_ta(tmem + cfg::TM_DS, tmem + cfg::TM_VH + 8 * ks, dKm + st + ((ks * 2048) >> 4), idesc_ds, ks > 0);
+            if (s_out) {
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-              if (!stall) umma_bf16_ta(tmem + cfg::TM_DS + 64 * fh, tmem + cfg::TM_VH + 8 * ks, dKm + st + ((fh * cfg::BOX + ks * 2048) >> 4), idesc_ds, ks > 0);
-          }
-          if (s_out && !stall) {
-#pragma unroll
-            for (int fh = 0; fh < cfg::KB; ++fh) {
-#pragma unroll
-              for (int ks = 0; ks < 4; ++ks)
-                umma_bf16_ta(tmem + cfg::TM_DS + 64 * fh, tmem + cfg::TM_VL + 8 * ks, dKm + st + ((fh * cfg::BOX + ks * 2048) >> 4), idesc_ds, 1u);
+              for (int ks = 0; ks < 4; ++ks) umma_bf16_ta(tmem + cfg::TM_DS, tmem + cfg::TM_VL + 8 * ks, dKm + st + ((ks * 2048) >> 4), idesc_ds, 1u);
             }
+            umma_commit(b_ds);
           }
-          if (!stall) umma_commit(b_ds);
-          if (!whole) {
-            umma_commit(bar_empty + 8 * stage(t));
-            if (i + 1 < n_tiles && !wait(bar_full + 8 * stage(t + 1), lap(t + 1))) return false;
-            continue;
-          }
-          // the next tile's QK, if its tiles have landed and this tile's QK has been read; otherwise behind PV
-          const bool more = i + 1 < n_tiles;
-          const bool early = more && seen(bar_full + 8 * stage(t + 1), lap(t + 1)) && seen(b_qkf, ph);
-          if (early) { tc_fence_after(); issue_qk(t + 1); }
-          if (!wait(b_sr, ph) || (t > 0 && !wait(b_acc, ph ^ 1))) return false;
-          tc_fence_after();
-#pragma unroll
-          for (int ks = 0; ks < DK / 16; ++ks)
-            umma_bf16_ta(tmem + cfg::TM_QS, tmem + cfg::TM_S + 8 * ks, dQ + st + (((ks >> 2) * cfg::BOX + (ks & 3) * 32) >> 4), idesc_s, ks > 0);
-          umma_commit(b_qs);
           umma_commit(bar_empty + 8 * stage(t));
-          if (!wait(b_pr, ph)) return false;   // (V came with V~)
-          fence_proxy_async();   // P was written by ordinary stores
-          tc_fence_after();
-#pragma unroll
-          for (int ks = 0; ks < L / 16; ++ks)
-            umma_bf16_ta(tmem + cfg::TM_PV, tmem + cfg::TM_V + 32 * ph + 8 * ks, dP + ((ks * 32) >> 4), idesc_s, ks > 0);
-          umma_commit(b_pv);
-          if (more && !early) {
-            if (!wait(bar_full + 8 * stage(t + 1), lap(t + 1)) || !wait(b_qkf, ph)) return false;
-            tc_fence_after();
-            issue_qk(t + 1);
+          if (i + 1 < n_tiles) {
+            if (!wait(bar_full + 8 * stage(t + 1), lap(t + 1))) return false;
+            if (whole) {
+              if (!wait(b_qkf, ph)) return false;
+              tc_fence_after();
+              issue_qk(t + 1);
+            }
           }
         }
         return true;
@@ -476,6 +460,33 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
       if (failed) {   // every product issued so far is waited for, with a limit, before the CTA gives up its memory
         umma_commit(b_exit);
         mbar_wait_bounded(b_exit, 0u, lim);
+      }
+    } else if (warp == kControlB && whole) {
+      // ---------------------------------------------------------------- control warp B: QS and PV
+      constexpr uint32_t idesc_s = umma_idesc(cfg::M, 64, 0);
+      for_items([&](const LinWalk& w, int, int, const LinSeg&, int, int, int n_tiles, float*) -> bool {
+        for (int i = 0; i < n_tiles; ++i, ++t) {
+          const uint32_t ph = t & 1, st = (stage(t) * cfg::STAGE) >> 4;
+          if (!wait(bar_full + 8 * stage(t), lap(t)) || !wait(b_sr, ph) || (t > 0 && !wait(b_acc, ph ^ 1))) return false;
+          tc_fence_after();
+#pragma unroll
+          for (int ks = 0; ks < DK / 16; ++ks)
+            umma_bf16_ta(tmem + cfg::TM_QS, tmem + cfg::TM_S + 8 * ks, dQ + st + (((ks >> 2) * cfg::BOX + (ks & 3) * 32) >> 4), idesc_s, ks > 0);
+          umma_commit(b_qs);
+          umma_commit(bar_empty + 8 * stage(t));
+          if (!wait(b_pr, ph) || !wait(b_vr + 8 * ph, (t >> 1) & 1)) return false;
+          fence_proxy_async();   // P was written by ordinary stores
+          tc_fence_after();
+#pragma unroll
+          for (int ks = 0; ks < L / 16; ++ks)
+            umma_bf16_ta(tmem + cfg::TM_PV, tmem + cfg::TM_V + 32 * ph + 8 * ks, dP + ((ks * 32) >> 4), idesc_s, ks > 0);
+          umma_commit(b_pv + 8 * ph);
+        }
+        return true;
+      });
+      if (failed) {
+        umma_commit(b_exitb);
+        mbar_wait_bounded(b_exitb, 0u, lim);
       }
     } else if (warp == kCopyL) {
       // ---------------------------------------------------------------- copy warp
