@@ -26,6 +26,22 @@ int check_linear(const tri_inv_desc* d) {
   return d->d_k > 256 || d->d_v > 65536 ? TRI_INV_ERR_UNSUPPORTED : TRI_INV_OK;
 }
 
+// Times of the tensor-core kernel, in tiles of 1.25 us (64 tokens, d_k = d_v = 128, one CTA): a tile of all 128 value columns, of 64; the same of the pass that
+// only wants states; what a CTA's share of the memory traffic takes when every SM is at work; a kernel's launch, start and end; a cut's second launch and join.
+// Measured as calls of 1 .. 24 segments of either width (us, estimate / measured): 1 x 4096 tokens x 16 heads uncut 86 / 86, in halves of the columns 67 / 67, also in
+// four segments 49 / 50; 1 x 32768 x 8: uncut 646 / 634, 18 segments 102 / 102; 1 x 32768 x 32: uncut 646 / 638, in halves 492 / 490, four segments 279 / 286;
+// 4 x 4096 x 16: 86 / 87, in halves 67 / 70, two segments 110 / 103, its gradient 166 / 159.
+constexpr double kTileAll = 1.0, kTileHalf = 0.76, kStateAll = 0.56, kStateHalf = 0.45, kBusyTile = 1.3, kBusyState = 0.65, kLaunch = 5.0, kCut = 14.0;
+
+// Cost of a walk over `tiles` tiles in all, cut into segments of `seg` of at most `longest`, `units` blocks a tile, each of which takes `alone` by itself and `busy` of all SMs
+// at work.  Equal segments run in whole rounds; packed ones, the longest first, end about together.
+double passes(double tiles, double seg, double units, bool equal, int sms, double alone, double busy) {
+  const double blocks = tiles / seg * units;
+  const double rounds = equal ? std::ceil(blocks / sms) : std::max(1.0, blocks / sms + 0.3);
+  const double used = std::min(1.0, blocks / sms);
+  return rounds * seg * std::max(alone, busy * used);
+}
+
 // How a call of `walks` walks is cut.  A cut sequence is read twice where it is not the last segment (k and v, for the states), and joining takes two
 // launches more, so it pays only where the walk of the longest sequence is long beside what the chip could do with every SM at work.
 int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
@@ -44,12 +60,29 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
     longest = (d->T + kLinTile - 1) / kLinTile;
     tiles = longest * n_seqs;
   }
-  // blocks that one tile of tokens keeps busy, and blocks that the chip has room for
-  const long long per_tile = (long long)d->H * walks * ((std::max(d->d_k, d->d_v) + 63) / 64);
-  const long long room = tc ? sms : 2 * (long long)sms;
-  long long seg = std::max<long long>((tiles * per_tile + room - 1) / room, tc ? 8 : 4);
-  const long long launches = tc ? 10 : 4;   // the two launches more, in tiles
-  if (2 * seg + launches >= longest) seg = std::max<long long>(longest, 1);
+  long long seg = std::max<long long>(longest, 1);
+  p->slices = 1;
+  if (tc) {
+    const bool wide = std::max(d->d_k, d->d_v) == 128;
+    double best = 1e300;
+    for (int slices = wide ? 2 : 1; slices >= 1; --slices) {
+      const bool half = !wide || slices == 2;
+      const double units = (double)d->H * walks * slices;
+      for (int n = 1; n <= 64 && (n == 1 || longest >= 4 * n); ++n) {
+        const long long s = std::max<long long>(1, (longest + n - 1) / n);
+        const bool equal = !d->cu_seqlens;
+        // (halves of the columns read q and k twice, from the L2 cache the second time)
+        double cost = kLaunch + passes((double)tiles, (double)s, units, equal, sms, half ? kTileHalf : kTileAll, kBusyTile / slices);
+        if (n > 1) cost += kCut + passes((double)tiles * (n - 1) / n, (double)s, units, equal, sms, half ? kStateHalf : kStateAll, kBusyState / slices);
+        if (cost < best) { best = cost; seg = s; p->slices = slices; }
+      }
+    }
+  } else {
+    // blocks that one tile of tokens keeps busy, and blocks that the chip has room for
+    const long long per_tile = (long long)d->H * walks * ((std::max(d->d_k, d->d_v) + 63) / 64), room = 2 * (long long)sms;
+    const long long s = std::max<long long>((tiles * per_tile + room - 1) / room, 4);
+    if (2 * s + 4 < longest) seg = s;
+  }
   p->seg_tokens = (int)std::min<long long>(seg * kLinTile, 0x40000000);
   long long n = 0;
   if (d->cu_seqlens) {
@@ -72,7 +105,7 @@ int run_walks(LinArgs& a, const LinPlan& p, const tri_inv_desc* d, bool tc, void
   a.status = status_word_for_current_device(&err);
   if (!a.status) return TRI_INV_ERR_CUDA;
   a.H = d->H; a.T = d->T;
-  a.seg_tokens = p.seg_tokens; a.segs_per_seq = p.segs_per_seq; a.n_segs = p.n_segs;
+  a.seg_tokens = p.seg_tokens; a.segs_per_seq = p.segs_per_seq; a.n_segs = p.n_segs; a.slices = p.slices;
   if (p.n_segs == 0) return TRI_INV_OK;
   if (d->cu_seqlens) {
     a.table = (const LinSeg*)workspace;

@@ -47,6 +47,7 @@ struct LinArgs {
   int H, T;                   // T: dense tokens a sequence
   int seg_tokens, segs_per_seq;   // dense: segments of a sequence
   int n_segs;                 // in all
+  int slices;                 // tensor cores: 2 where a walk's 128 value columns go as two blocks
   float* seg_state;           // [n_walks][n_segs][H][d_k d_v]: the states that enter the segments; null: no sequence is cut
   int state_only;             // write to seg_state what each segment alone leaves
   int* status;
@@ -56,7 +57,7 @@ struct LinArgs {
 
 // How a call is cut.
 struct LinPlan {
-  int seg_tokens, segs_per_seq, n_segs;
+  int seg_tokens, segs_per_seq, n_segs, slices;
   bool cut;                   // some sequence has more than one segment
   size_t table_bytes, state_bytes;
 };

@@ -196,6 +196,7 @@ cudaError_t launch_one(const LinArgs& a, int max_dk, int max_dv, cudaStream_t st
 
 // One block for 256 elements of the states of one (walk, first segment, head): element by element along the sequence's segments.
 __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant__ LinArgs a, int parts) {
+  wait_for_predecessor();
   int x = blockIdx.x;
   const int part = x % parts; x /= parts;
   const int h = x % a.H; x /= a.H;
@@ -263,8 +264,8 @@ cudaError_t launch_linear_join(const LinArgs& a, cudaStream_t stream) {
   const int parts = (a.walk[0].d_k * a.walk[0].d_v + 255) / 256;
   const long long grid = (long long)parts * a.H * a.n_segs * a.n_walks;
   if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
-  linear_join_kernel<<<(unsigned)grid, 256, 0, stream>>>(a, parts);
-  return launched();
+  const cudaError_t e = launch_early(linear_join_kernel, dim3((unsigned)grid), 256, 0, stream, a, parts);
+  return e == cudaSuccess ? launched() : e;
 }
 
 cudaError_t launch_linear_table(LinSeg* dev_tab, int seg_tokens, const tri_inv_desc* d, cudaStream_t stream) {

@@ -73,7 +73,8 @@ __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair d; asm("fma.
 __device__ __forceinline__ uint32_t pack_bf16(Pair p) { const float2 x = parts(p); return pack_bf16(x.x, x.y); }
 __device__ __forceinline__ Pair unpack_bf16(uint32_t x) { return pair(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
 
-template <int DK, int DV>
+// WHOLE: outputs; otherwise the pass that only wants the states (LinArgs::state_only)
+template <int DK, int DV, bool WHOLE>
 __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_constant__ LinMaps maps, const __grid_constant__ LinTcArgs args) {
   using cfg = LinCfg<DK, DV>;
   constexpr int LG = cfg::LG;
@@ -83,10 +84,11 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
   const uint32_t s0 = smem_u32(smem), sP = s0 + cfg::OFF_P, bars = s0 + cfg::OFF_BAR;
   // copies: bar_full + 8 stage; stage free again: bar_empty + 8 stage (both control warps' commits, value warps)
   // products done (commit): ds, qs, qk, pv.  Operands written: vs (V~, value warps), vr (V), sr (S^T, state warps), pr (P, output warps).
-  // Accumulators read: dsf (DS), qkf (QK), acc (QS and PV).  O's tile: o full, os read.
-  const uint32_t bar_full = bars, bar_empty = bars + 32, b_ds = bars + 64, b_qs = bars + 72, b_qk = bars + 80, b_exit = bars + 88, b_exitb = bars + 96,
-                 b_vs = bars + 104, b_vr = bars + 192, b_pv = bars + 112 /* two of each, in turn: V is kept for two tiles, and the value warps may be two ahead */, b_sr = bars + 128, b_pr = bars + 136, b_dsf = bars + 144, b_qkf = bars + 152, b_acc = bars + 160,
-                 b_o = bars + 168, b_os = bars + 176;
+  // Accumulators read: dsf (DS), qkf (QK), acc (QS and PV).  O's tile: o full, os read.  ds, pv, vs, vr and dsf are two barriers each, in turn: V is kept for two
+  // tiles, in the pass that only wants states V~ and DS too, so that who writes them may be two tiles ahead of who waits.
+  const uint32_t bar_full = bars, bar_empty = bars + 32, b_ds = bars + 64, b_pv = bars + 80, b_qs = bars + 96, b_qk = bars + 104, b_exit = bars + 112, b_exitb = bars + 120,
+                 b_vs = bars + 128, b_vr = bars + 144, b_dsf = bars + 160, b_sr = bars + 176, b_pr = bars + 184, b_qkf = bars + 192, b_acc = bars + 200, b_o = bars + 208,
+                 b_os = bars + 216;
   const unsigned long long lim = a.wait_limit_ns ? a.wait_limit_ns : kWaitLimitNs;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;   // warp: uniform for the compiler
   const int quad = warp & 3, half = (warp >> 2) & 1;
@@ -95,12 +97,10 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
   wait_for_predecessor();
   if (warp == kControlA) {
     if (lane == 0) {
-      for (int b = 0; b < cfg::STAGES; ++b) { mbar_init(bar_full + 8 * b, 1); mbar_init(bar_empty + 8 * b, a.state_only ? 9 : 10); }
+      for (int b = 0; b < cfg::STAGES; ++b) { mbar_init(bar_full + 8 * b, 1); mbar_init(bar_empty + 8 * b, WHOLE ? 10 : 9); }
       for (uint32_t b = b_ds; b <= b_exitb; b += 8) mbar_init(b, 1);
-      mbar_init(b_pv, 1); mbar_init(b_pv + 8, 1); mbar_init(b_vr, 8); mbar_init(b_vr + 8, 8);
-      mbar_init(b_vs, 8); mbar_init(b_sr, kStateWarps); mbar_init(b_pr, 8);
-      mbar_init(b_dsf, kStateWarps); mbar_init(b_qkf, 8); mbar_init(b_acc, 8);
-      mbar_init(b_o, 8); mbar_init(b_os, 1);
+      for (uint32_t b = b_vs; b <= b_o; b += 8) mbar_init(b, 8);   // eight warps each
+      mbar_init(b_os, 1);
       fence_mbar_init();
     }
     __syncwarp();
@@ -122,11 +122,10 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
 #pragma unroll 1
     for (uint32_t i = 1; i < kSpinLimit; ++i) {
       if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-      if ((i & 63u) == 0 && __any_sync(0xffffffffu, global_timer_ns() - t0 > lim)) return false;
+      if (__shfl_sync(0xffffffffu, (uint32_t)(global_timer_ns() - t0 > lim), 0)) return false;
     }
     return false;
   };
-  const bool whole = !a.state_only;
   const int per_walk = a.H * args.slices, per_seg = per_walk * args.n_walks, n_items = a.n_segs * per_seg;
 
   // Every role walks the same items: the longest first, dealt to the CTAs back and forth.  f(walk, segment, head, first column, ..) returns false to give up.
@@ -144,7 +143,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
       g.ends = __shfl_sync(0xffffffffu, g.ends, 0);
       const LinWalk& w = a.walk[wi];
       float* s_out = lin_exit_state(a, w, wi, s, g, h);
-      if (a.state_only && !s_out) continue;
+      if (!WHOLE && !s_out) continue;
       if (!f(w, wi, s, g, h, col0, (g.n + L - 1) / L, s_out)) failed = true;
     }
   };
@@ -153,6 +152,14 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
   uint32_t t = 0;   // tiles of this CTA so far, the same in every role: tile t's barriers are in phase t
   auto stage = [](uint32_t t) { return t % cfg::STAGES; };
   auto lap = [](uint32_t t) { return (t / cfg::STAGES) & 1u; };
+  // Barriers in turn: that of tile t, and its phase.  Two of pv and vr always; two of ds, vs and dsf in the pass that only wants states, which keeps V~ and DS for
+  // two tiles, the odd ones' where V and QS, PV would be (the control warps' addresses are on a tile's longest path: no turns where none are needed)
+  constexpr uint32_t kTurn = WHOLE ? 0 : 1;
+  auto turn2 = [](uint32_t bar, uint32_t t) { return bar + 8 * (t & 1); };
+  auto wait_turn2 = [&](uint32_t bar, uint32_t t) { return wait(turn2(bar, t), (t >> 1) & 1); };
+  auto turn = [](uint32_t bar, uint32_t t) { return bar + 8 * (t & kTurn); };
+  auto wait_turn = [&](uint32_t bar, uint32_t t) { return wait(turn(bar, t), (t >> kTurn) & 1); };
+  constexpr uint32_t vs_turn = WHOLE ? 0 : (uint32_t)(cfg::TM_V - cfg::TM_VH), ds_turn = WHOLE ? 0 : (uint32_t)(cfg::TM_QS - cfg::TM_DS);
 
   // (each role changes its registers first of all: nobody waits for a share that another still holds behind a wait)
   if (warp < kStateWarps) {
@@ -179,7 +186,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
       const float l = lin_log2_decay(a, h) * 0.6931471805599453f, less_full = expm1f(l * L), less_last = expm1f(l * (g.n - (n_tiles - 1) * L));
       for (int i = 0; i < n_tiles; ++i, ++t) {
         const uint32_t ph = t & 1;
-        if (whole) {
+        if constexpr (WHOLE) {
           if (t > 0 && !wait(b_qs, ph ^ 1)) return false;   // the operand's last reader
           tc_fence_after();
 #pragma unroll
@@ -198,17 +205,17 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
         }
         const float less1 = tile_of(w, i, n_tiles) == n_tiles - 1 ? less_last : less_full;
         const Pair less = pair(less1, less1);
-        if (!wait(b_ds, ph)) return false;
+        if (!wait_turn(b_ds, t)) return false;
         tc_fence_after();
 #pragma unroll
         for (int c = 0; c < NP; c += STEP) {
           float ds[2 * STEP];
-          const uint32_t at = tmem_w + cfg::TM_DS + cfg::SH * half + 2 * c;
+          const uint32_t at = tmem_w + cfg::TM_DS + ph * ds_turn + cfg::SH * half + 2 * c;
           if constexpr (DV == 128) tmem_ld_row16(ds, at);
           else if constexpr (STEP == 16) tmem_ld_16x64(reinterpret_cast<float (&)[8][4]>(ds), at);
           else tmem_ld_16x32(reinterpret_cast<float (&)[4][4]>(ds), at);
           tmem_wait_ld();
-          if (c + STEP == NP) { tc_fence_before(); warp_arrive(b_dsf, lane); }
+          if (c + STEP == NP) { tc_fence_before(); warp_arrive(turn(b_dsf, t), lane); }
 #pragma unroll
           for (int q = 0; q < STEP; ++q) S[c + q] = add2(fma2(S[c + q], less, S[c + q]), pair(ds[2 * q], ds[2 * q + 1]));
         }
@@ -221,8 +228,8 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
         });
       return true;
     });
-  } else if (warp < kOutput) {
-    // ---------------------------------------------------------------- value warps
+  } else if (WHOLE ? warp < kOutput : warp < kControlA) {
+    // ---------------------------------------------------------------- value warps (in the pass that only wants states the output warps too: every second tile each)
     fewer_registers<64>();
     const int row0 = quad * cfg::RPQ;
     float* f = reinterpret_cast<float*>(smem + cfg::OFF_F) + (warp - kValue) * L;   // this warp's table of the tokens' factors
@@ -230,6 +237,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
       const float l2 = lin_log2_decay(a, h);
       int made_for = 0;
       for (int i = 0; i < n_tiles; ++i, ++t) {
+        if (!WHOLE && (t & 1) != (uint32_t)(warp >= kOutput)) continue;
         const uint32_t ph = t & 1, base = s0 + stage(t) * cfg::STAGE, sV = base + cfg::OFF_V;
         const int rows = rows_of(g, tile_of(w, i, n_tiles));
         if (rows != made_for) {
@@ -243,7 +251,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
         if (rows < L) {
           // Behind the sequence's end lie a neighbour's rows.  V counts as zero there (below), and zero times a key that is not finite is not zero: the key
           // tile's rows are cleared too (QK may be reading them: those columns of P are left out by selection)
-          for (int e = tid - 32 * kValue; e < (L - rows) * 8 * cfg::KB; e += 256)
+          for (int e = (tid - 32 * kValue) & 255; e < (L - rows) * 8 * cfg::KB; e += 256)
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + cfg::OFF_K + (e / ((L - rows) * 8)) * cfg::BOX + (rows + (e / 8) % (L - rows)) * 128 + (e & 7) * 16), "r"(0) : "memory");
           fence_proxy_async();
         }
@@ -269,7 +277,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
               x[th][2 * nt + 1] &= keep;
             }
         }
-        if (t > 0 && !wait(b_ds, ph ^ 1)) return false;
+        if (WHOLE ? t > 0 && !wait_turn(b_ds, t - 1) : t > 1 && !wait_turn(b_ds, t - 2)) return false;   // V~'s place is free
         tc_fence_after();
 #pragma unroll
         for (int th = 0; th < TH; ++th) {
@@ -284,41 +292,41 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
               if (s_out) lo[2 * nt + e] = pack_bf16(fma2(unpack_bf16(hi[2 * nt + e]), pair(-1.f, -1.f), y));
             }
           }
-          const uint32_t at = tmem_w + ((uint32_t)(16 * lg) << 16) + 16 * (th0 + th);
+          const uint32_t at = tmem_w + ((uint32_t)(16 * lg) << 16) + 16 * (th0 + th) + ph * vs_turn;
           tmem_st_packed16(hi, at + cfg::TM_VH);
           if (s_out) tmem_st_packed16(lo, at + cfg::TM_VL);
         }
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) { mbar_arrive(b_vs); mbar_arrive(bar_empty + 8 * stage(t)); }
-        if (whole) {   // V itself, kept for two tiles in turn
-          if (t > 1 && !wait(b_pv + 8 * ph, ((t >> 1) & 1) ^ 1)) return false;
+        if (lane == 0) { mbar_arrive(turn(b_vs, t)); mbar_arrive(bar_empty + 8 * stage(t)); }
+        if constexpr (WHOLE) {   // V itself, kept for two tiles in turn
+          if (t > 1 && !wait_turn2(b_pv, t - 2)) return false;
           tc_fence_after();
 #pragma unroll
           for (int th = 0; th < TH; ++th) tmem_st_packed16(x[th], tmem_w + ((uint32_t)(16 * lg) << 16) + 16 * (th0 + th) + cfg::TM_V + 32 * ph);
           tmem_wait_st();
           tc_fence_before();
-          warp_arrive(b_vr + 8 * ph, lane);
+          warp_arrive(turn2(b_vr, t), lane);
         }
       }
       return true;
     });
-  } else if (warp < kControlA) {
+  } else if (WHOLE && warp < kControlA) {
     // ---------------------------------------------------------------- output warps
     fewer_registers<64>();
-    if (whole) {
+    if constexpr (WHOLE) {
     const int row0 = quad * cfg::RPQ, ia = 16 * quad + gq, ib = ia + 8;
     float* y = reinterpret_cast<float*>(smem + cfg::OFF_F) + (warp - kValue) * L;   // this warp's table of the tokens' factors of QS
     for_items([&](const LinWalk& w, int, int, const LinSeg& g, int h, int col0, int n_tiles, float*) -> bool {
-      const float l2 = lin_log2_decay(a, h), pv_factor = w.k_factor * w.out_factor;
+      const float l2 = lin_log2_decay(a, h), scale = w.k_factor * w.out_factor;
       Pair f[4][2];   // P's factors, zero where it is masked: columns 32 half + 8 nt + t2, + 1 of rows ia and ib
 #pragma unroll
       for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int d = (e ? ib : ia) - (32 * half + 8 * nt + t2), g0 = w.back ? -d : d, g1 = w.back ? 1 - d : d - 1;
-          f[nt][e] = pair(g0 >= 0 ? exp2f(l2 * g0) : 0.f, g1 >= 0 ? exp2f(l2 * g1) : 0.f);
+          f[nt][e] = pair(g0 >= 0 ? scale * exp2f(l2 * g0) : 0.f, g1 >= 0 ? scale * exp2f(l2 * g1) : 0.f);
         }
       int made_for = 0;
       // O of tile t (its position in the item: i) out of tensor memory into its tile, [token][column]; behind the wait for its PV
@@ -348,7 +356,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
             const float2 yt = *reinterpret_cast<const float2*>(y + 32 * (hf0 + hf) + 8 * nt + t2);
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-              o[nt][e] = pack_bf16(fma2(pair(pv[nt][2 * e], pv[nt][2 * e + 1]), pair(pv_factor, pv_factor), mul2(pair(yt.x, yt.y), pair(qs[nt][2 * e], qs[nt][2 * e + 1]))));
+              o[nt][e] = pack_bf16(fma2(pair(yt.x, yt.y), pair(qs[nt][2 * e], qs[nt][2 * e + 1]), pair(pv[nt][2 * e], pv[nt][2 * e + 1])));
           }
 #pragma unroll
           for (int nt = 0; nt < 4; nt += 2) {
@@ -388,7 +396,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
             wb[nt] = pack_bf16(mul2(pair(qk[nt][2], qk[nt][3]), f[nt][1]));
           }
         }
-        if (t > 0 && !wait(b_pv + 8 * (ph ^ 1), ((t - 1) >> 1) & 1)) return false;   // PV of the tile before is done: its O can be read, and P's tile is free
+        if (t > 0 && !wait_turn2(b_pv, t - 1)) return false;   // PV of the tile before is done: its O can be read, and P's tile is free
         tc_fence_after();
         if (more) {
           const int row = 16 * quad + 8 * (mi & 1) + mr;
@@ -426,29 +434,30 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
           const uint32_t ph = t & 1, st = (stage(t) * cfg::STAGE) >> 4;
           if (i == 0) {
             if (!wait(bar_full + 8 * stage(t), lap(t))) return false;
-            if (whole) {
+            if constexpr (WHOLE) {
               if (t > 0 && !wait(b_qkf, ph ^ 1)) return false;
               tc_fence_after();
               issue_qk(t);
             }
           }
-          if (!wait(b_vs, ph) || (t > 0 && !wait(b_dsf, ph ^ 1))) return false;
+          if (!wait_turn(b_vs, t) || (WHOLE ? t > 0 && !wait_turn(b_dsf, t - 1) : t > 1 && !wait_turn(b_dsf, t - 2))) return false;
           tc_fence_after();
           // self-test (LinArgs::test_stall): the first CTA leaves out this product of its second tile, so that its waits run out
           const bool stall = a.test_stall && blockIdx.x == 0 && t == 1;
           if (!stall) {
+            const uint32_t d = tmem + cfg::TM_DS + ph * ds_turn, v = tmem + ph * vs_turn;
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) umma_bf16_ta(tmem + cfg::TM_DS, tmem + cfg::TM_VH + 8 * ks, dKm + st + ((ks * 2048) >> 4), idesc_ds, ks > 0);
+            for (int ks = 0; ks < 4; ++ks) umma_bf16_ta(d, v + cfg::TM_VH + 8 * ks, dKm + st + ((ks * 2048) >> 4), idesc_ds, ks > 0);
             if (s_out) {
 #pragma unroll
-              for (int ks = 0; ks < 4; ++ks) umma_bf16_ta(tmem + cfg::TM_DS, tmem + cfg::TM_VL + 8 * ks, dKm + st + ((ks * 2048) >> 4), idesc_ds, 1u);
+              for (int ks = 0; ks < 4; ++ks) umma_bf16_ta(d, v + cfg::TM_VL + 8 * ks, dKm + st + ((ks * 2048) >> 4), idesc_ds, 1u);
             }
-            umma_commit(b_ds);
+            umma_commit(turn(b_ds, t));
           }
           umma_commit(bar_empty + 8 * stage(t));
           if (i + 1 < n_tiles) {
             if (!wait(bar_full + 8 * stage(t + 1), lap(t + 1))) return false;
-            if (whole) {
+            if constexpr (WHOLE) {
               if (!wait(b_qkf, ph)) return false;
               tc_fence_after();
               issue_qk(t + 1);
@@ -461,7 +470,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
         umma_commit(b_exit);
         mbar_wait_bounded(b_exit, 0u, lim);
       }
-    } else if (warp == kControlB && whole) {
+    } else if (warp == kControlB && WHOLE) {
       // ---------------------------------------------------------------- control warp B: QS and PV
       constexpr uint32_t idesc_s = umma_idesc(cfg::M, 64, 0);
       for_items([&](const LinWalk& w, int, int, const LinSeg&, int, int, int n_tiles, float*) -> bool {
@@ -474,13 +483,13 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
             umma_bf16_ta(tmem + cfg::TM_QS, tmem + cfg::TM_S + 8 * ks, dQ + st + (((ks >> 2) * cfg::BOX + (ks & 3) * 32) >> 4), idesc_s, ks > 0);
           umma_commit(b_qs);
           umma_commit(bar_empty + 8 * stage(t));
-          if (!wait(b_pr, ph) || !wait(b_vr + 8 * ph, (t >> 1) & 1)) return false;
+          if (!wait(b_pr, ph) || !wait_turn2(b_vr, t)) return false;
           fence_proxy_async();   // P was written by ordinary stores
           tc_fence_after();
 #pragma unroll
           for (int ks = 0; ks < L / 16; ++ks)
             umma_bf16_ta(tmem + cfg::TM_PV, tmem + cfg::TM_V + 32 * ph + 8 * ks, dP + ((ks * 32) >> 4), idesc_s, ks > 0);
-          umma_commit(b_pv + 8 * ph);
+          umma_commit(turn2(b_pv, t));
         }
         return true;
       });
@@ -496,12 +505,12 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
           if (lane == 0) {
             const uint32_t base = s0 + stage(t) * cfg::STAGE, bar = bar_full + 8 * stage(t);
             const int tok = g.tok0 + tile_of(w, i, n_tiles) * L;
-            mbar_expect_tx(bar, whole ? cfg::STAGE : cfg::STAGE - cfg::KB * cfg::BOX);
+            mbar_expect_tx(bar, WHOLE ? cfg::STAGE : cfg::STAGE - cfg::KB * cfg::BOX);
 #pragma unroll
             for (int b = 0; b < cfg::KB; ++b) tma_load_2d(base + cfg::OFF_K + b * cfg::BOX, &maps.k[wi], bar, h * DK + 64 * b, tok);
 #pragma unroll
             for (int b = 0; b < cfg::VB; ++b) tma_load_2d(base + cfg::OFF_V + b * cfg::BOX, &maps.v[wi], bar, h * w.d_v + col0 + 64 * b, tok);
-            if (whole)
+            if constexpr (WHOLE)
 #pragma unroll
               for (int b = 0; b < cfg::KB; ++b) tma_load_2d(base + b * cfg::BOX, &maps.q[wi], bar, h * DK + 64 * b, tok);
           }
@@ -511,7 +520,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
       });
       if (failed && lane == 0)   // the copies still on their way into this CTA's shared memory
         for (uint32_t c = t >= cfg::STAGES ? t - cfg::STAGES : 0; c < t; ++c) mbar_wait_bounded(bar_full + 8 * stage(c), lap(c), lim);
-    } else if (warp == kStoreL && whole) {
+    } else if (warp == kStoreL && WHOLE) {
       // ---------------------------------------------------------------- store warp: O's tile to memory
       for_items([&](const LinWalk& w, int wi, int, const LinSeg& g, int h, int col0, int n_tiles, float*) -> bool {
         for (int i = 0; i < n_tiles; ++i, ++t) {
@@ -545,8 +554,8 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
-template <int DK, int DV>
-cudaError_t launch_one(const LinMaps& maps, const LinTcArgs& args, int sms, cudaStream_t stream) {
+template <int DK, int DV, bool WHOLE>
+cudaError_t launch_form(const LinMaps& maps, const LinTcArgs& args, int sms, cudaStream_t stream) {
   using cfg = LinCfg<DK, DV>;
   static std::mutex mu;
   static bool ready[64] = {false};
@@ -557,17 +566,19 @@ cudaError_t launch_one(const LinMaps& maps, const LinTcArgs& args, int sms, cuda
   {
     std::lock_guard<std::mutex> lock(mu);
     if (!ready[dev]) {
-      if ((e = cudaFuncSetAttribute(linear_tc_kernel<DK, DV>, cudaFuncAttributeMaxDynamicSharedMemorySize, cfg::SMEM)) != cudaSuccess) { (void)cudaGetLastError(); return e; }
+      if ((e = cudaFuncSetAttribute(linear_tc_kernel<DK, DV, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize, cfg::SMEM)) != cudaSuccess) { (void)cudaGetLastError(); return e; }
       ready[dev] = true;
     }
   }
   const long long items = (long long)args.a.n_segs * args.a.H * args.n_walks * args.slices;
-  e = launch_early(linear_tc_kernel<DK, DV>, dim3((unsigned)(items < sms ? items : sms)), kThreadsL, cfg::SMEM, stream, maps, args);
+  e = launch_early(linear_tc_kernel<DK, DV, WHOLE>, dim3((unsigned)(items < sms ? items : sms)), kThreadsL, cfg::SMEM, stream, maps, args);
   return e == cudaSuccess ? launched() : e;
 }
 
-// Slices of a walk's 128 value columns: two of 64 while each gets an SM of its own.
-int lin_tc_slices(const LinArgs& a, int sms) { return (long long)a.n_segs * a.H * a.n_walks * 2 <= sms ? 2 : 1; }
+template <int DK, int DV>
+cudaError_t launch_one(const LinMaps& maps, const LinTcArgs& args, int sms, cudaStream_t stream) {
+  return args.a.state_only ? launch_form<DK, DV, false>(maps, args, sms, stream) : launch_form<DK, DV, true>(maps, args, sms, stream);
+}
 
 }  // namespace
 
@@ -592,7 +603,7 @@ cudaError_t launch_linear_tc(const LinArgs& a, long long tokens, cudaStream_t st
     args.first_walk = first;
     args.n_walks = 1;
     while (first + args.n_walks < a.n_walks && a.walk[first + args.n_walks].d_k == w.d_k && a.walk[first + args.n_walks].d_v == w.d_v) ++args.n_walks;
-    const bool narrow = w.d_v == 64 || lin_tc_slices(a, sms) == 2;
+    const bool narrow = w.d_v == 64 || a.slices == 2;
     args.slices = narrow ? w.d_v / 64 : 1;
     const cudaError_t e = w.d_k == 128 ? (narrow ? launch_one<128, 64>(maps, args, sms, stream) : launch_one<128, 128>(maps, args, sms, stream))
                                        : (narrow ? launch_one<64, 64>(maps, args, sms, stream) : launch_one<64, 128>(maps, args, sms, stream));
