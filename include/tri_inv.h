@@ -331,6 +331,15 @@ int tri_inv_linear_attention(const void* Q, const void* K, const void* V, const 
                              float scale, void* workspace, size_t workspace_bytes, const tri_inv_desc* desc, void* cuda_stream);
 
 /*
+ * Self-test of the tensor-core kernel's give-up path: the call (dense, zero initial state, scale 1) with every wait limited to wait_limit_ns, and the first thread block
+ * leaving out one product of its second tile of 64 tokens.  Its waits run out one after the other, it raises TRI_INV_ERR_DEVICE_TIMEOUT in the status word, waits, with a
+ * limit, for what it has in flight and returns: what follows in sequence 0, head 0 (its first value columns) is undefined, with more heads and sequences than SMs also that
+ * block's later ones.  All other output is as usual.  Synchronises the stream.  TRI_INV_ERR_UNSUPPORTED for shapes that run elsewhere.
+ */
+int tri_inv_selftest_linear_wait_timeout(const void* Q, const void* K, const void* V, const float* log_decay, void* O, const tri_inv_desc* desc,
+                                         uint64_t wait_limit_ns, void* cuda_stream);
+
+/*
  * Its gradient: from dO [B,T,H,d_v] (and dS, the gradient of the final state, or NULL: zero) those of Q, K, V and, where dS0 is not NULL, of S0.
  * log_decay is a constant of the model and has none.  S0 as in the forward call (NULL: zero).  With weights w_ij = lambda^{i-j}, j <= i:
  *     dQ_i = scale (sum_j w_ij (dO_i . v_j) k_j + lambda^{i+1} S0 dO_i),      dK_j = scale sum_i w_ij (dO_i . v_j) q_i + lambda^{T-1-j} dS v_j,

@@ -45,7 +45,7 @@ W_DECAY = 0x20000
 
 EXPORTS = ("tri_inv_build", "tri_inv_build_kda", "tri_inv_fused_kda", "tri_inv_chunk_scan_kda", "tri_inv_chunk_scan", "tri_inv_gdn_forward", "tri_inv_gdn_forward_workspace",
            "tri_inv_linear_attention", "tri_inv_linear_attention_workspace", "tri_inv_linear_attention_backward", "tri_inv_linear_attention_backward_workspace",
-           "tri_inv_linear_attention_step", "tri_inv_rms_norm", "tri_inv_rms_norm_backward", "tri_inv_rms_norm_backward_workspace",
+           "tri_inv_linear_attention_step", "tri_inv_selftest_linear_wait_timeout", "tri_inv_rms_norm", "tri_inv_rms_norm_backward", "tri_inv_rms_norm_backward_workspace",
            "tri_inv_wy", "tri_inv_fused", "tri_inv_fused_raw", "tri_inv_fused_packed_static", "tri_inv_count_matrices",
            "tri_inv_fused_host", "tri_inv_fused_host_workspace", "tri_inv_selftest_wait_timeout", "tri_inv_selftest_scan_wait_timeout", "tri_inv_selftest_kda_wait_timeout", "tri_inv_selftest_bounds_check", "tri_inv_last_device_status", "tri_inv_launch_count", "tri_inv_status_string")
 
@@ -125,12 +125,13 @@ def load():
             lib.tri_inv_linear_attention_workspace.argtypes = lib.tri_inv_linear_attention_backward_workspace.argtypes = [dp, szp]
             lib.tri_inv_linear_attention.argtypes = [vp] * 7 + [f32, vp, sz, dp, vp]
             lib.tri_inv_linear_attention_backward.argtypes = [vp] * 11 + [f32, vp, sz, dp, vp]
+            lib.tri_inv_selftest_linear_wait_timeout.argtypes = [vp] * 5 + [dp, ctypes.c_uint64, vp]
             lib.tri_inv_linear_attention_step.argtypes = [vp] * 6 + [n32, vp, f32, dp, vp]
             lib.tri_inv_rms_norm.argtypes = [vp] * 6 + [i64, n32, n32, f32, i32, i32, vp]
             lib.tri_inv_rms_norm_backward_workspace.argtypes = [i64, n32, szp]
             lib.tri_inv_rms_norm_backward.argtypes = [vp] * 6 + [i64, n32, f32, i32, vp, sz, vp]
             for f in EXPORTS:
-                if "linear_attention" in f or "rms_norm" in f:
+                if "linear" in f or "rms_norm" in f:
                     getattr(lib, f).restype = i32
         lib.tri_inv_count_matrices.argtypes = [dp, ctypes.POINTER(ctypes.c_int64)]
         lib.tri_inv_last_device_status.argtypes = [ctypes.POINTER(ctypes.c_int)]
@@ -162,6 +163,39 @@ def load_native():
             warnings.warn("%s: gdn_forward is marshalled in Python (build it with `python -m paper_2605_21325_b200.build`)" % e)
             _native_layer = lambda *args: None   # noqa: E731
     return _native_layer
+
+
+_native_ops = None
+
+
+class _NoNative:
+    """In place of the extension where it has not been built: every call goes through the Python body."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
+def _operators():
+    """The extension's functions for linear attention and the RMS norm, bound to the loaded library (once)."""
+    global _native_ops
+    if _native_ops is None:
+        load_native()   # its warning where the extension is missing
+        try:
+            from . import _native
+            addr = lambda f: ctypes.cast(getattr(load(), "tri_inv_" + f), ctypes.c_void_p).value   # noqa: E731
+            _native.bind_operators(*(addr(f) for f in ("linear_attention_workspace", "linear_attention", "linear_attention_backward_workspace", "linear_attention_backward",
+                                                       "linear_attention_step", "rms_norm", "rms_norm_backward_workspace", "rms_norm_backward")))
+            _native_ops = _native
+        except (ImportError, AttributeError):
+            _native_ops = _NoNative()
+    return _native_ops
+
+
+def _marshalled(out, name):
+    """What the extension made of a call: its result, or the error that its status means."""
+    if out.__class__ is int:
+        raise TriInvError(name if out < 256 else name + "_workspace", out & 255)
+    return out
 
 
 def status_string(status: int) -> str:
@@ -364,6 +398,10 @@ def _attention_shapes(Q, V, cu_seqlens):
 def linear_attention(Q, K, V, log_decay, scale=1.0, S0=None, cu_seqlens=None, out=None, want_state=True, state_out=None, stream=None):
     """Linear attention with a decay for each head -> (O, S_final or None): S_t = exp(log_decay) S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t.
     Q, K [B,T,H,d_k], V [B,T,H,d_v]; log_decay [H] fp32; S0, S_final [sequences,H,d_k,d_v] fp32 (``state_out`` may be S0 itself)."""
+    if out is None and state_out is None and stream is None:
+        made = (_native_ops or _operators()).linear_attention(Q, K, V, log_decay, scale, S0, cu_seqlens, bool(want_state))
+        if made is not None:
+            return _marshalled(made, "tri_inv_linear_attention")
     desc, keep, qk, vo, st = _attention_shapes(Q, V, cu_seqlens)
     dt, f32 = Q.dtype, torch.float32
     args = [_operand("Q", Q, qk, dt), _operand("K", K, qk, dt), _operand("V", V, vo, dt), _operand("log_decay", log_decay, (qk[2],), f32), _optional("S0", S0, st, f32)]
@@ -379,16 +417,32 @@ def linear_attention(Q, K, V, log_decay, scale=1.0, S0=None, cu_seqlens=None, ou
     return O, S
 
 
+def selftest_linear_wait_timeout(Q, K, V, log_decay, wait_limit_ns, out, stream=None):
+    """tri_inv_selftest_linear_wait_timeout: the tensor-core linear attention with short wait limits and one product of the first thread block left out.
+    ``out`` = O."""
+    desc, keep, _, _, _ = _attention_shapes(Q, V, None)
+    rc = load().tri_inv_selftest_linear_wait_timeout(_p(Q), _p(K), _p(V), _p(log_decay), _p(out), desc, ctypes.c_uint64(int(wait_limit_ns)), _stream(stream))
+    if rc != OK:
+        raise TriInvError("tri_inv_selftest_linear_wait_timeout", rc)
+    return out
+
+
 def linear_attention_backward(dO, Q, K, V, log_decay, scale=1.0, S0=None, dS=None, cu_seqlens=None, want_dS0=None, stream=None):
     """The gradient of ``linear_attention`` -> (dQ, dK, dV, dS0 or None), from dO and, where the final state has one, dS.  ``want_dS0``: by
     default where S0 is given."""
+    if want_dS0 is None:
+        want_dS0 = S0 is not None
+    if stream is None:
+        made = (_native_ops or _operators()).linear_attention_backward(dO, Q, K, V, log_decay, scale, S0, dS, cu_seqlens, bool(want_dS0))
+        if made is not None:
+            return _marshalled(made, "tri_inv_linear_attention_backward")
     desc, keep, qk, vo, st = _attention_shapes(Q, V, cu_seqlens)
     dt, f32 = Q.dtype, torch.float32
     args = [_operand("dO", dO, vo, dt), _operand("Q", Q, qk, dt), _operand("K", K, qk, dt), _operand("V", V, vo, dt),
             _operand("log_decay", log_decay, (qk[2],), f32), _optional("S0", S0, st, f32), _optional("dS", dS, st, f32)]
     dQ, dK, dV = (_made_for(torch.empty_like(x), stream) for x in (Q, K, V))
     dS0 = None
-    if S0 is not None if want_dS0 is None else want_dS0:
+    if want_dS0:
         dS0 = _made_for(torch.empty(st, dtype=f32, device=V.device), stream)
     work, need = _workspace("tri_inv_linear_attention_backward_workspace", V.device, stream, desc)
     rc = load().tri_inv_linear_attention_backward(*args, _p(dQ), _p(dK), _p(dV), _p(dS0), float(scale), _p(work), need, desc, _stream(stream))
@@ -401,6 +455,10 @@ def linear_attention_step(Q, K, V, log_decay, S, scale=1.0, slots=None, out=None
     """One token for each row, on states that lie in the slots of a cache and are updated in place -> O [B,H,d_v].  Q, K [B,H,d_k], V [B,H,d_v],
     S [n_slots,H,d_k,d_v] fp32, slots [B] int32 (negative: a padded row, output zero) or None: row b has slot b.  Slots that do not differ, or lie past the
     cache, are left out and show in ``last_device_status``."""
+    if out is None and stream is None:
+        made = (_native_ops or _operators()).linear_attention_step(Q, K, V, log_decay, S, scale, slots)
+        if made is not None:
+            return _marshalled(made, "tri_inv_linear_attention_step")
     if Q.dim() != 3 or V.dim() != 3 or S.dim() != 4:
         raise ValueError("Q and V must be [B, H, d] and S [slots, H, d_k, d_v], got %s, %s and %s" % (tuple(Q.shape), tuple(V.shape), tuple(S.shape)))
     B, H, d_k = Q.shape
@@ -422,6 +480,10 @@ def rms_norm(X, w, eps=1e-6, residual=None, out_dtype=None, group=128, out=None,
     """Root-mean-square norm over the last dimension -> (Y, H, scales): H = X + residual (None without a residual), Y = H w / sqrt(mean H^2 + eps) in the type of
     X, or, with ``out_dtype=torch.float8_e4m3fn``, in 8 bits with fp32 scales: one for each ``group`` = 128 columns, or one a row (``group=0``); else scales is None.
     ``residual_out`` may be X or residual itself."""
+    if out is None and residual_out is None and stream is None and (out_dtype is None or out_dtype is torch.float8_e4m3fn):
+        made = (_native_ops or _operators()).rms_norm(X, w, eps, residual, out_dtype is not None, group)
+        if made is not None:
+            return _marshalled(made, "tri_inv_rms_norm")
     n, dt = X.shape[-1], X.dtype
     code = _dtype_code(X)
     coded = out_dtype is not None and out_dtype != dt
@@ -446,6 +508,10 @@ def rms_norm(X, w, eps=1e-6, residual=None, out_dtype=None, group=128, out=None,
 def rms_norm_backward(dY, X, w, eps=1e-6, dH=None, stream=None):
     """The gradient of ``rms_norm`` -> (dX, dw): X is the H of the forward call (X where there was no residual), dH what reaches it past the norm; dX is the
     gradient of both summands."""
+    if stream is None:
+        made = (_native_ops or _operators()).rms_norm_backward(dY, X, w, eps, dH)
+        if made is not None:
+            return _marshalled(made, "tri_inv_rms_norm_backward")
     n, dt = X.shape[-1], X.dtype
     code = _dtype_code(X)
     rows = X.numel() // n if n else 0

@@ -170,6 +170,24 @@ int tri_inv_linear_attention(const void* Q, const void* K, const void* V, const 
   return run_walks(a, p, desc, tc, workspace, (cudaStream_t)cuda_stream);
 }
 
+int tri_inv_selftest_linear_wait_timeout(const void* Q, const void* K, const void* V, const float* log_decay, void* O, const tri_inv_desc* desc,
+                                         uint64_t wait_limit_ns, void* cuda_stream) {
+  const int rc = check_linear(desc);
+  if (rc) return rc;
+  if (!on_tensor_cores(desc) || desc->cu_seqlens) return TRI_INV_ERR_UNSUPPORTED;
+  if (!Q || !K || !V || !log_decay || !O || !wait_limit_ns || !all_aligned(Q, K, V, log_decay, O)) return TRI_INV_ERR_INVALID_ARG;
+  const LinPlan p{(desc->T + kLinTile - 1) / kLinTile * kLinTile, 1, desc->B, 1, false, 0, 0};
+  LinArgs a{};
+  a.log_decay = log_decay;
+  a.n_walks = 1;
+  a.walk[0] = make_walk(Q, K, V, O, nullptr, nullptr, desc->d_k, desc->d_v, 0, 0, 1.f);
+  a.wait_limit_ns = wait_limit_ns;
+  a.test_stall = 1;
+  const int e = run_walks(a, p, desc, true, nullptr, (cudaStream_t)cuda_stream);
+  if (e) return e;
+  return cudaStreamSynchronize((cudaStream_t)cuda_stream) == cudaSuccess ? TRI_INV_OK : TRI_INV_ERR_CUDA;
+}
+
 int tri_inv_linear_attention_backward_workspace(const tri_inv_desc* desc, size_t* bytes) {
   if (desc && desc->d_v > 256) return TRI_INV_ERR_UNSUPPORTED;
   return workspace_of(desc, 3, bytes);
