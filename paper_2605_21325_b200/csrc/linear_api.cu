@@ -26,20 +26,20 @@ int check_linear(const tri_inv_desc* d) {
   return d->d_k > 256 || d->d_v > 65536 ? TRI_INV_ERR_UNSUPPORTED : TRI_INV_OK;
 }
 
-// Times of the tensor-core kernel, in tiles of 1.25 us (64 tokens, d_k = d_v = 128, one CTA): a tile of all 128 value columns, of 64; the same of the pass that
-// only wants states; what a CTA's share of the memory traffic takes when every SM is at work; a kernel's launch, start and end; a cut's second launch and join.
-// Measured as calls of 1 .. 24 segments of either width (us, estimate / measured): 1 x 4096 tokens x 16 heads uncut 86 / 86, in halves of the columns 67 / 67, also in
-// four segments 49 / 50; 1 x 32768 x 8: uncut 646 / 634, 18 segments 102 / 102; 1 x 32768 x 32: uncut 646 / 638, in halves 492 / 490, four segments 279 / 286;
-// 4 x 4096 x 16: 86 / 87, in halves 67 / 70, two segments 110 / 103, its gradient 166 / 159.
-constexpr double kTileAll = 1.0, kTileHalf = 0.76, kStateAll = 0.56, kStateHalf = 0.45, kBusyTile = 1.3, kBusyState = 0.65, kLaunch = 5.0, kCut = 14.0;
+// Times of the tensor-core kernel in units of 1.25 us: a tile (64 tokens, d_k = d_v = 128) of all value columns and of 64, the same of the pass that only wants states, what the
+// memory traffic takes for a tile with a block on every SM (less for a gradient's three walks, which read the same tensors), a block's start and end in tiles, a kernel's launch, a
+// cut's second launch and join, and a segment's state written, joined and read.  Measured, us, estimate / calls in a row: 1 x 4096 tokens x 16 heads uncut 86 / 86, in halves of the
+// columns 69 / 67, also in four segments 53 / 49, eight of all columns 59 / 54; 1 x 32768 x 8 uncut 649 / 634, 18 segments 99 / 102; 1 x 32768 x 32 in halves 495 / 490, four
+// segments 305 / 295, nine 322 / 349; 4 x 4096 x 16 in halves 70 / 70, two segments 125 / 103, its gradient 174 / 160.
+constexpr double kTileAll = 1.0, kTileHalf = 0.76, kStateAll = 0.56, kStateHalf = 0.45, kBusyTile = 1.3, kBusyState = 0.65, kShared = 0.75, kBlock = 3.0, kLaunch = 4.0,
+                 kCut = 11.0, kSegment = 0.06;
 
-// Cost of a walk over `tiles` tiles in all, cut into segments of `seg` of at most `longest`, `units` blocks a tile, each of which takes `alone` by itself and `busy` of all SMs
-// at work.  Equal segments run in whole rounds; packed ones, the longest first, end about together.
-double passes(double tiles, double seg, double units, bool equal, int sms, double alone, double busy) {
-  const double blocks = tiles / seg * units;
-  const double rounds = equal ? std::ceil(blocks / sms) : std::max(1.0, blocks / sms + 0.3);
-  const double used = std::min(1.0, blocks / sms);
-  return rounds * seg * std::max(alone, busy * used);
+// Cost of a pass over `tiles` tiles in all, in segments of `seg` with `units` blocks a tile: whole rounds of blocks on all SMs and one on what is left, a tile taking `alone`
+// where its SM bounds it and `busy` times the share of SMs at work where the memory does.  (Packed segments, the longest first, end about together.)
+double pass_cost(double tiles, double seg, double units, bool equal, int sms, double alone, double busy) {
+  const double rounds = tiles / seg * units / sms, full = std::floor(rounds), rest = rounds - full;
+  const double last = rest <= 0 ? 0 : equal || full == 0 ? std::max(alone, busy * rest) : std::max(alone, busy) * rest;
+  return (seg + kBlock) * (full * std::max(alone, busy) + last);
 }
 
 // How a call of `walks` walks is cut.  A cut sequence is read twice where it is not the last segment (k and v, for the states), and joining takes two
@@ -64,6 +64,7 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
   p->slices = 1;
   if (tc) {
     const bool wide = std::max(d->d_k, d->d_v) == 128;
+    const double shared = walks == 3 ? kShared : 1.0;
     double best = 1e300;
     for (int slices = wide ? 2 : 1; slices >= 1; --slices) {
       const bool half = !wide || slices == 2;
@@ -72,8 +73,10 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
         const long long s = std::max<long long>(1, (longest + n - 1) / n);
         const bool equal = !d->cu_seqlens;
         // (halves of the columns read q and k twice, from the L2 cache the second time)
-        double cost = kLaunch + passes((double)tiles, (double)s, units, equal, sms, half ? kTileHalf : kTileAll, kBusyTile / slices);
-        if (n > 1) cost += kCut + passes((double)tiles * (n - 1) / n, (double)s, units, equal, sms, half ? kStateHalf : kStateAll, kBusyState / slices);
+        double cost = kLaunch + pass_cost((double)tiles, (double)s, units, equal, sms, half ? kTileHalf : kTileAll, shared * kBusyTile / slices);
+        if (n > 1)
+          cost += kCut + kSegment * tiles / s * d->H * walks +
+                  pass_cost((double)tiles * (n - 1) / n, (double)s, units, equal, sms, half ? kStateHalf : kStateAll, shared * kBusyState / slices);
         if (cost < best) { best = cost; seg = s; p->slices = slices; }
       }
     }
