@@ -63,7 +63,7 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
   long long seg = std::max<long long>(longest, 1);
   p->slices = 1;
   if (tc) {
-    const bool wide = std::max(d->d_k, d->d_v) == 128;
+    const bool wide = std::max(d->d_k, d->d_v) > 64;
     const double shared = walks == 3 ? kShared : 1.0;
     double best = 1e300;
     for (int slices = wide ? 2 : 1; slices >= 1; --slices) {

@@ -95,7 +95,7 @@ __device__ __forceinline__ float* lin_exit_state(const LinArgs& a, const LinWalk
 
 // Every shape and both storage types, in fp32 on the CUDA cores (d_k and d_v multiples of 8, d_k <= 256).
 cudaError_t launch_linear_simt(const LinArgs& a, int kv_dtype, cudaStream_t stream);
-// bf16 with head dimensions of 64 and 128, on the tensor cores.
+// bf16 with head dimensions up to 128, on the tensor cores.
 bool linear_tc_fits(int d_k, int d_v, int kv_dtype);
 cudaError_t launch_linear_tc(const LinArgs& a, long long tokens, cudaStream_t stream);
 // Between the two passes of a call with cut sequences: seg_state[s] from what segment s alone leaves to what enters it.

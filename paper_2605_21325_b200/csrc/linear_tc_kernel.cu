@@ -1,4 +1,5 @@
-// Linear attention with a decay for each head, on the tensor cores: bf16, d_k and d_v of 64 or 128 (the walk's formulas: linear_attention.cuh).
+// Linear attention with a decay for each head, on the tensor cores: bf16, d_k and d_v up to 128 (the walk's formulas: linear_attention.cuh), in tiles
+// of 64 or 128 features, padded with zeros by the copy engine.
 //
 // A persistent CTA per SM walks (walk, segment, head) items tile after tile of 64 tokens.  As in the delta rule's scan (scan_kernel.cu) everything that carries the state
 // lies transposed, value columns as tensor-memory lanes, so that its operands go from registers straight into tensor memory:
@@ -179,9 +180,19 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
     for_items([&](const LinWalk& w, int wi, int s, const LinSeg& g, int h, int col0, int n_tiles, float* s_out) -> bool {
       bool turned;
       const float* s_in = lin_entry_state(a, w, wi, s, g, h, &turned);
+      auto inside = [&](int v, int k) { return k < w.d_k && col0 + v < w.d_v; };   // (d_k is even)
       if (!s_in) for_state([&](Pair& x, int, int) { x = pair(0.f, 0.f); });
-      else if (turned) for_state([&](Pair& x, int v, int k) { const float2 y = *reinterpret_cast<const float2*>(s_in + (size_t)(col0 + v) * DK + k); x = pair(y.x, y.y); });
-      else for_state([&](Pair& x, int v, int k) { x = pair(s_in[(size_t)k * w.d_v + col0 + v], s_in[(size_t)(k + 1) * w.d_v + col0 + v]); });
+      else if (turned)
+        for_state([&](Pair& x, int v, int k) {
+          const float2 y = inside(v, k) ? *reinterpret_cast<const float2*>(s_in + (size_t)(col0 + v) * w.d_k + k) : make_float2(0.f, 0.f);
+          x = pair(y.x, y.y);
+        });
+      else
+        for_state([&](Pair& x, int v, int k) {
+          const float* at = s_in + (size_t)k * w.d_v + col0 + v;
+          const bool in = inside(v, k);
+          x = pair(in ? at[0] : 0.f, in ? at[w.d_v] : 0.f);
+        });
       // lambda^n - 1 for S <- (S + (lambda^n - 1) S) + DS: a factor near 1 that is off by a rounding would be off by it in every tile, always to the same side
       const float l = lin_log2_decay(a, h) * 0.6931471805599453f, less_full = expm1f(l * L), less_last = expm1f(l * (g.n - (n_tiles - 1) * L));
       for (int i = 0; i < n_tiles; ++i, ++t) {
@@ -223,8 +234,10 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
       if (s_out)
         for_state([&](Pair& x, int v, int k) {
           const float2 y = parts(x);
-          s_out[(size_t)k * w.d_v + col0 + v] = y.x;
-          s_out[(size_t)(k + 1) * w.d_v + col0 + v] = y.y;
+          if (inside(v, k)) {
+            s_out[(size_t)k * w.d_v + col0 + v] = y.x;
+            s_out[(size_t)(k + 1) * w.d_v + col0 + v] = y.y;
+          }
         });
       return true;
     });
@@ -507,12 +520,12 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
             const int tok = g.tok0 + tile_of(w, i, n_tiles) * L;
             mbar_expect_tx(bar, WHOLE ? cfg::STAGE : cfg::STAGE - cfg::KB * cfg::BOX);
 #pragma unroll
-            for (int b = 0; b < cfg::KB; ++b) tma_load_2d(base + cfg::OFF_K + b * cfg::BOX, &maps.k[wi], bar, h * DK + 64 * b, tok);
+            for (int b = 0; b < cfg::KB; ++b) tma_load_3d(base + cfg::OFF_K + b * cfg::BOX, &maps.k[wi], bar, 64 * b, h, tok);
 #pragma unroll
-            for (int b = 0; b < cfg::VB; ++b) tma_load_2d(base + cfg::OFF_V + b * cfg::BOX, &maps.v[wi], bar, h * w.d_v + col0 + 64 * b, tok);
+            for (int b = 0; b < cfg::VB; ++b) tma_load_3d(base + cfg::OFF_V + b * cfg::BOX, &maps.v[wi], bar, col0 + 64 * b, h, tok);
             if constexpr (WHOLE)
 #pragma unroll
-              for (int b = 0; b < cfg::KB; ++b) tma_load_2d(base + b * cfg::BOX, &maps.q[wi], bar, h * DK + 64 * b, tok);
+              for (int b = 0; b < cfg::KB; ++b) tma_load_3d(base + b * cfg::BOX, &maps.q[wi], bar, 64 * b, h, tok);
           }
           __syncwarp();
         }
@@ -530,7 +543,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
             if (lane == 0) {
               fence_proxy_async();   // the tile was written by ordinary stores
 #pragma unroll
-              for (int b = 0; b < cfg::VB; ++b) tma_store_2d(&maps.o[wi], s0 + cfg::OFF_O + b * cfg::BOX, h * w.d_v + col0 + 64 * b, tok0);
+              for (int b = 0; b < cfg::VB; ++b) tma_store_3d(&maps.o[wi], s0 + cfg::OFF_O + b * cfg::BOX, col0 + 64 * b, h, tok0);
               bulk_commit();
               bulk_wait_read();
             }
@@ -538,7 +551,8 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
             __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(w.out) + ((size_t)tok0 * a.H + h) * w.d_v + col0;
             for (int e = lane; e < rows * (DV / 8); e += 32) {
               const int tok = e / (DV / 8), pc = e % (DV / 8);
-              *reinterpret_cast<uint4*>(out + (size_t)tok * a.H * w.d_v + 8 * pc) =
+              if (col0 + 8 * pc < w.d_v)
+                *reinterpret_cast<uint4*>(out + (size_t)tok * a.H * w.d_v + 8 * pc) =
                   *reinterpret_cast<const uint4*>(smem + cfg::OFF_O + (pc >> 3) * cfg::BOX + tok * 128 + (((pc ^ tok) & 7) << 4));
             }
           }
@@ -552,6 +566,18 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
   tc_fence_before();
   __syncthreads();
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+// 3-D view [tokens, H, d] of bf16: a box is 64 features of one head (zeros behind the head's last, which a store leaves out) x 64 tokens, in rows of 128 bytes, swizzled
+bool make_head_map(CUtensorMap* tm, const void* base, long long tokens, int H, int d) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)H, (cuuint64_t)tokens};
+  cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)H * d * 2};
+  cuuint32_t box[3] = {64, 1, (cuuint32_t)L};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int DK, int DV, bool WHOLE>
@@ -583,7 +609,7 @@ cudaError_t launch_one(const LinMaps& maps, const LinTcArgs& args, int sms, cuda
 }  // namespace
 
 bool linear_tc_fits(int d_k, int d_v, int kv_dtype) {
-  return kv_dtype == TRI_INV_BF16 && (d_k == 64 || d_k == 128) && (d_v == 64 || d_v == 128);
+  return kv_dtype == TRI_INV_BF16 && d_k <= 128 && d_v <= 128;
 }
 
 cudaError_t launch_linear_tc(const LinArgs& a, long long tokens, cudaStream_t stream) {
@@ -592,21 +618,22 @@ cudaError_t launch_linear_tc(const LinArgs& a, long long tokens, cudaStream_t st
   LinMaps maps;
   for (int i = 0; i < a.n_walks; ++i) {
     const LinWalk& w = a.walk[i];
-    if (!make_tmap(&maps.q[i], w.q, tokens, a.H, w.d_k, L) || !make_tmap(&maps.k[i], w.k, tokens, a.H, w.d_k, L) || !make_tmap(&maps.v[i], w.v, tokens, a.H, w.d_v, L) ||
-        !make_tmap(&maps.o[i], w.out, tokens, a.H, w.d_v, L))
+    if (!make_head_map(&maps.q[i], w.q, tokens, a.H, w.d_k) || !make_head_map(&maps.k[i], w.k, tokens, a.H, w.d_k) || !make_head_map(&maps.v[i], w.v, tokens, a.H, w.d_v) ||
+        !make_head_map(&maps.o[i], w.out, tokens, a.H, w.d_v))
       return cudaErrorUnknown;
   }
-  // the walks of one launch have the same dimensions: all of them where d_k = d_v, else the last apart
+  // the walks of one launch take the same form of the kernel: head dimensions up to 64 or up to 128 (the tiles' rest is zeros)
+  auto wide_k = [&](int i) { return a.walk[i].d_k > 64; };
+  auto wide_v = [&](int i) { return a.walk[i].d_v > 64; };
   LinTcArgs args{a, 0, 0, 1};
   for (int first = 0; first < a.n_walks; first += args.n_walks) {
-    const LinWalk& w = a.walk[first];
     args.first_walk = first;
     args.n_walks = 1;
-    while (first + args.n_walks < a.n_walks && a.walk[first + args.n_walks].d_k == w.d_k && a.walk[first + args.n_walks].d_v == w.d_v) ++args.n_walks;
-    const bool narrow = w.d_v == 64 || a.slices == 2;
-    args.slices = narrow ? w.d_v / 64 : 1;
-    const cudaError_t e = w.d_k == 128 ? (narrow ? launch_one<128, 64>(maps, args, sms, stream) : launch_one<128, 128>(maps, args, sms, stream))
-                                       : (narrow ? launch_one<64, 64>(maps, args, sms, stream) : launch_one<64, 128>(maps, args, sms, stream));
+    while (first + args.n_walks < a.n_walks && wide_k(first + args.n_walks) == wide_k(first) && wide_v(first + args.n_walks) == wide_v(first)) ++args.n_walks;
+    args.slices = wide_v(first) ? a.slices : 1;
+    const bool narrow = !wide_v(first) || args.slices == 2;
+    const cudaError_t e = wide_k(first) ? (narrow ? launch_one<128, 64>(maps, args, sms, stream) : launch_one<128, 128>(maps, args, sms, stream))
+                                        : (narrow ? launch_one<64, 64>(maps, args, sms, stream) : launch_one<64, 128>(maps, args, sms, stream));
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
