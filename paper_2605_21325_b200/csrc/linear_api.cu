@@ -81,10 +81,17 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
       }
     }
   } else {
-    // blocks that one tile of tokens keeps busy, and blocks that the chip has room for
-    const long long per_tile = (long long)d->H * walks * ((std::max(d->d_k, d->d_v) + 63) / 64), room = 2 * (long long)sms;
-    const long long s = std::max<long long>((tiles * per_tile + room - 1) / room, 4);
-    if (2 * s + 4 < longest) seg = s;
+    // The CUDA-core kernel, in us: a tile of one block by itself and its share of an SM at work, the same of the pass that only wants states (one product of four), and the two
+    // launches more
+    const double alone = 3.0 + 0.18 * std::max(d->d_k, d->d_v), shared = 0.75 * alone, cut = 14.0;
+    const double units = (double)d->H * walks * ((std::max(d->d_k, d->d_v) + 63) / 64);
+    double best = 1e300;
+    for (int n = 1; n <= 256 && n <= std::max<long long>(longest, 1); ++n) {
+      const long long s = std::max<long long>(1, (longest + n - 1) / n);
+      const double rounds = std::max(1.0, std::ceil((double)tiles / s * units / (2.0 * sms) - 0.05)), all = std::max(rounds * s * alone, tiles * units / sms * shared);
+      const double cost = all + (n > 1 ? cut + 0.4 * all : 0);
+      if (cost < best) { best = cost; seg = s; }
+    }
   }
   p->seg_tokens = (int)std::min<long long>(seg * kLinTile, 0x40000000);
   long long n = 0;

@@ -3,7 +3,8 @@
 // One CTA walks one (segment, head, slice of 64 value columns) tile after tile of 64 tokens (the walk's formulas: linear_attention.cuh); value
 // columns of the state never mix.  q, k, v, P and the state's slice lie in shared memory; each of the four products is made of
 // thread tiles of 4 x 4 (the state: 4 x 4 for every 64 features), rows read as float4 along the summed index, so that a thread reads 8 x 16 bytes for 64 FMAs.
-// What bounds it: the FMAs (per token 2 d_k + 128 of them for a value column, and as many again for every further slice's P).
+// What bounds it: the FMAs (per token 2 d_k + 128 of them for a value column, and as many again for every further slice's P) and, with few blocks, the
+// latency of a tile's steps.  (512 threads with tiles of 4 x 2: 16 x 64 tokens x 8 heads of 128 in 52 us, 45 so.)
 #include <algorithm>
 
 #include "linear_attention.cuh"
@@ -11,7 +12,7 @@
 namespace tri_inv {
 namespace {
 
-constexpr int L = kLinTile, SL = 64, LDV = SL + 4, kThreadsLin = 256;
+constexpr int L = kLinTile, SL = 64, kThreadsLin = 256;
 
 struct alignas(8) Half4 { __nv_bfloat162 a, b; };
 template <class T>
@@ -35,7 +36,7 @@ __device__ __forceinline__ void fma4(float (&d)[4], float a, float4 b) {
 }
 
 template <class T, int MK>   // MK: groups of 64 features
-__global__ void __launch_bounds__(kThreadsLin) linear_simt_kernel(const __grid_constant__ LinArgs a, int max_slices) {
+__global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : 2) linear_simt_kernel(const __grid_constant__ LinArgs a, int max_slices) {
   extern __shared__ __align__(16) float sm[];
   int x = blockIdx.x;
   const int slice = x % max_slices; x /= max_slices;
@@ -44,54 +45,68 @@ __global__ void __launch_bounds__(kThreadsLin) linear_simt_kernel(const __grid_c
   const LinWalk w = a.walk[wi];
   const int c0 = slice * SL;
   if (c0 >= w.d_v) return;
-  const int dk = w.d_k, ldk = dk + 4;
-  float *sq = sm, *sk = sq + L * ldk, *sv = sk + L * max(ldk, LDV), *sS = sv + L * LDV, *pw = sS + dk * LDV;   // pw: lambda^0 .. lambda^64
+  // Rows without padding, so that two blocks of d_k = 128 fit an SM.  Only k is read by rows that differ between lanes: its pieces of 16 bytes change places within 128 bytes by the
+  // row (piece ^ row & 7), or, where rows are not whole 128 bytes, rows are padded by one.
+  const int dk = w.d_k, ldk = dk % 32 ? dk + 4 : dk, swz = dk % 32 ? 0 : 7;
+  float *sq = sm, *sk = sq + L * dk, *sv = sk + L * max(ldk, SL), *sS = sv + L * SL, *pw = sS + dk * SL;   // pw: lambda^0 .. lambda^64
   float* sp = sk;   // P lies where k was: k's other reader, the state's increment, comes first
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, warp = tid >> 5, lane = tid & 31;
   const LinSeg g = lin_segment(a, s);
-  if (a.state_only && !lin_exit_state(a, w, wi, s, g, h)) return;
+  float* s_out = lin_exit_state(a, w, wi, s, g, h);
+  if (a.state_only && !s_out) return;
   const float l2 = lin_log2_decay(a, h);
-  for (int n = tid; n <= L; n += kThreadsLin) pw[n] = exp2f(l2 * n);
+  if (tid <= L) pw[tid] = exp2f(l2 * tid);
   bool turned;
   const float* s_in = lin_entry_state(a, w, wi, s, g, h, &turned);
-  for (int e = tid; e < dk * SL; e += kThreadsLin) {
-    const int d = turned ? e % dk : e / SL, c = turned ? e / dk : e % SL;
-    sS[d * LDV + c] = s_in && c0 + c < w.d_v ? (turned ? s_in[(size_t)(c0 + c) * dk + d] : s_in[(size_t)d * w.d_v + c0 + c]) : 0.f;
+  if (!s_in || !turned) {
+#pragma unroll 4
+    for (int e = tid; e < dk * (SL / 4); e += kThreadsLin) {
+      const int d = e / (SL / 4), c = 4 * (e % (SL / 4));
+      *reinterpret_cast<float4*>(sS + d * SL + c) = s_in && c0 + c < w.d_v ? lds4(s_in + (size_t)d * w.d_v + c0 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  } else {
+    for (int c = warp; c < SL; c += kThreadsLin / 32)
+      for (int d = lane; d < dk; d += 32) sS[d * SL + c] = c0 + c < w.d_v ? s_in[(size_t)(c0 + c) * dk + d] : 0.f;
   }
   const T *Q = (const T*)w.q, *K = (const T*)w.k, *V = (const T*)w.v;
   T* O = (T*)w.out;
   const int n_tiles = (g.n + L - 1) / L, b = w.back;
+  const size_t row_k = (size_t)a.H * dk, row_v = (size_t)a.H * w.d_v;
   for (int it = 0; it < n_tiles; ++it) {
     const int tile = b ? n_tiles - 1 - it : it, tok0 = g.tok0 + tile * L, rows = min(L, g.n - tile * L);
     __syncthreads();   // the last tile's readers are through
-    for (int e = tid; e < L * (dk / 4); e += kThreadsLin) {
-      const int i = e / (dk / 4), d = 4 * (e % (dk / 4));
-      const size_t at = ((size_t)(tok0 + i) * a.H + h) * dk + d;
-      const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-      *reinterpret_cast<float4*>(sk + i * ldk + d) = i < rows ? load4(K + at) : zero;
-      if (!a.state_only) *reinterpret_cast<float4*>(sq + i * ldk + d) = i < rows ? load4(Q + at) : zero;
-    }
-    {
-      const int c = 4 * tx;
+    const T *Kt = K + ((size_t)tok0 * a.H + h) * dk, *Qt = Q + ((size_t)tok0 * a.H + h) * dk, *Vt = V + ((size_t)tok0 * a.H + h) * w.d_v + c0;
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    // a warp per row, 4 features a lane
+#pragma unroll 4
+    for (int i = warp; i < L; i += kThreadsLin / 32) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = ty + 16 * r;
-        const bool in = i < rows && c0 + c < w.d_v;
-        *reinterpret_cast<float4*>(sv + i * LDV + c) = in ? load4(V + ((size_t)(tok0 + i) * a.H + h) * w.d_v + c0 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int m = 0; m < (MK + 1) / 2; ++m) {
+        const int d = 4 * (lane + 32 * m);
+        if (d < dk) {
+          *reinterpret_cast<float4*>(sk + i * ldk + (d ^ (i & swz) << 2)) = i < rows ? load4(Kt + i * row_k + d) : zero;
+          if (!a.state_only) *reinterpret_cast<float4*>(sq + i * dk + d) = i < rows ? load4(Qt + i * row_k + d) : zero;
+        }
       }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int i = ty + 16 * r, c = 4 * tx;
+      *reinterpret_cast<float4*>(sv + i * SL + c) = i < rows && c0 + c < w.d_v ? load4(Vt + i * row_v + c) : zero;
     }
     __syncthreads();
     // the state's increment, features 64 m + 4 ty .. and columns 4 tx ..
     float ds[MK][4][4] = {};
+#pragma unroll 2
     for (int j = 0; j < rows; ++j) {
       const float wj = w.k_factor * pw[b ? j + 1 : rows - 1 - j];
-      float4 vv = lds4(sv + j * LDV + 4 * tx);
+      float4 vv = lds4(sv + j * SL + 4 * tx);
       vv.x *= wj; vv.y *= wj; vv.z *= wj; vv.w *= wj;
 #pragma unroll
       for (int m = 0; m < MK; ++m) {
         const int d = 64 * m + 4 * ty;
         if (d < dk) {
-          const float4 kk = lds4(sk + j * ldk + d);
+          const float4 kk = lds4(sk + j * ldk + (d ^ (j & swz) << 2));
           fma4(ds[m][0], kk.x, vv); fma4(ds[m][1], kk.y, vv); fma4(ds[m][2], kk.z, vv); fma4(ds[m][3], kk.w, vv);
         }
       }
@@ -99,16 +114,22 @@ __global__ void __launch_bounds__(kThreadsLin) linear_simt_kernel(const __grid_c
     if (!a.state_only) {
       {   // P, rows ty + 16 r, columns tx + 16 m
         float acc[4][4] = {};
+        const int turn = (tx & swz) << 2;
         for (int d = 0; d < dk; d += 4) {
           float4 kk[4];
 #pragma unroll
-          for (int m = 0; m < 4; ++m) kk[m] = lds4(sk + (tx + 16 * m) * ldk + d);
+          for (int m = 0; m < 4; ++m) kk[m] = lds4(sk + (tx + 16 * m) * ldk + (d ^ turn));
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float4 qq = lds4(sq + (ty + 16 * r) * ldk + d);
+            const float4 qq = lds4(sq + (ty + 16 * r) * dk + d);
 #pragma unroll
-            for (int m = 0; m < 4; ++m)
-              acc[r][m] = fmaf(qq.x, kk[m].x, fmaf(qq.y, kk[m].y, fmaf(qq.z, kk[m].z, fmaf(qq.w, kk[m].w, acc[r][m]))));
+            for (int m = 0; m < 4; ++m) acc[r][m] = fmaf(qq.x, kk[m].x, acc[r][m]);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) acc[r][m] = fmaf(qq.y, kk[m].y, acc[r][m]);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) acc[r][m] = fmaf(qq.z, kk[m].z, acc[r][m]);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) acc[r][m] = fmaf(qq.w, kk[m].w, acc[r][m]);
           }
         }
         __syncthreads();   // k has been read
@@ -117,7 +138,7 @@ __global__ void __launch_bounds__(kThreadsLin) linear_simt_kernel(const __grid_c
 #pragma unroll
           for (int m = 0; m < 4; ++m) {
             const int i = ty + 16 * r, j = tx + 16 * m, gap = b ? j - i : i - j;
-            sp[i * LDV + j] = gap >= 0 ? acc[r][m] * (w.k_factor * pw[gap]) : 0.f;
+            sp[i * SL + j] = gap >= 0 ? acc[r][m] * (w.k_factor * pw[gap]) : 0.f;
           }
       }
       __syncthreads();
@@ -125,10 +146,10 @@ __global__ void __launch_bounds__(kThreadsLin) linear_simt_kernel(const __grid_c
       for (int d = 0; d < dk; d += 4) {
         float4 ss[4];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) ss[m] = lds4(sS + (d + m) * LDV + 4 * tx);
+        for (int m = 0; m < 4; ++m) ss[m] = lds4(sS + (d + m) * SL + 4 * tx);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float4 qq = lds4(sq + (ty + 16 * r) * ldk + d);
+          const float4 qq = lds4(sq + (ty + 16 * r) * dk + d);
           fma4(acc[r], qq.x, ss[0]); fma4(acc[r], qq.y, ss[1]); fma4(acc[r], qq.z, ss[2]); fma4(acc[r], qq.w, ss[3]);
         }
       }
@@ -142,19 +163,19 @@ __global__ void __launch_bounds__(kThreadsLin) linear_simt_kernel(const __grid_c
       for (int j = 0; j < L; j += 4) {
         float4 vv[4];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) vv[m] = lds4(sv + (j + m) * LDV + 4 * tx);
+        for (int m = 0; m < 4; ++m) vv[m] = lds4(sv + (j + m) * SL + 4 * tx);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float4 pp = lds4(sp + (ty + 16 * r) * LDV + j);
+          const float4 pp = lds4(sp + (ty + 16 * r) * SL + j);
           fma4(acc[r], pp.x, vv[0]); fma4(acc[r], pp.y, vv[1]); fma4(acc[r], pp.z, vv[2]); fma4(acc[r], pp.w, vv[3]);
         }
       }
+      T* Ot = O + ((size_t)tok0 * a.H + h) * w.d_v + c0 + 4 * tx;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int i = ty + 16 * r, c = c0 + 4 * tx;
-        if (i < rows && c < w.d_v)
-          store4(O + ((size_t)(tok0 + i) * a.H + h) * w.d_v + c,
-                 make_float4(w.out_factor * acc[r][0], w.out_factor * acc[r][1], w.out_factor * acc[r][2], w.out_factor * acc[r][3]));
+        const int i = ty + 16 * r;
+        if (i < rows && c0 + 4 * tx < w.d_v)
+          store4(Ot + i * row_v, make_float4(w.out_factor * acc[r][0], w.out_factor * acc[r][1], w.out_factor * acc[r][2], w.out_factor * acc[r][3]));
       }
       __syncthreads();   // every reader of the entering state is through
     }
@@ -167,24 +188,28 @@ __global__ void __launch_bounds__(kThreadsLin) linear_simt_kernel(const __grid_c
       for (int r = 0; r < 4; ++r) {
         const int d = 64 * m + 4 * ty + r;
         if (d < dk) {
-          float4 y = lds4(sS + d * LDV + 4 * tx);
+          float4 y = lds4(sS + d * SL + 4 * tx);
           y.x = fmaf(y.x, less, y.x) + ds[m][r][0]; y.y = fmaf(y.y, less, y.y) + ds[m][r][1];
           y.z = fmaf(y.z, less, y.z) + ds[m][r][2]; y.w = fmaf(y.w, less, y.w) + ds[m][r][3];
-          *reinterpret_cast<float4*>(sS + d * LDV + 4 * tx) = y;
+          *reinterpret_cast<float4*>(sS + d * SL + 4 * tx) = y;
         }
       }
   }
-  float* s_out = lin_exit_state(a, w, wi, s, g, h);
   if (s_out) {
     __syncthreads();
-    for (int e = tid; e < dk * SL; e += kThreadsLin)
-      if (c0 + e % SL < w.d_v) s_out[(size_t)(e / SL) * w.d_v + c0 + e % SL] = sS[(e / SL) * LDV + e % SL];
+#pragma unroll 4
+    for (int e = tid; e < dk * (SL / 4); e += kThreadsLin) {
+      const int d = e / (SL / 4), c = 4 * (e % (SL / 4));
+      if (c0 + c < w.d_v) *reinterpret_cast<float4*>(s_out + (size_t)d * w.d_v + c0 + c) = lds4(sS + d * SL + c);
+    }
   }
 }
 
 template <class T, int MK>
 cudaError_t launch_one(const LinArgs& a, int max_dk, int max_dv, cudaStream_t stream) {
-  const size_t smem = ((size_t)L * (max_dk + 4) + (size_t)L * std::max(max_dk + 4, LDV) + (size_t)(L + max_dk) * LDV + L + 1) * sizeof(float);
+  int max_ldk = 0;
+  for (int i = 0; i < a.n_walks; ++i) max_ldk = std::max(max_ldk, a.walk[i].d_k % 32 ? a.walk[i].d_k + 4 : a.walk[i].d_k);
+  const size_t smem = ((size_t)L * max_dk + (size_t)L * std::max(max_ldk, SL) + (size_t)(L + max_dk) * SL + L + 1) * sizeof(float);
   const cudaError_t e = cudaFuncSetAttribute(linear_simt_kernel<T, MK>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) { (void)cudaGetLastError(); return e; }
   const int slices = (max_dv + SL - 1) / SL;
@@ -212,13 +237,20 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
   const float* s_in = w.s_in ? w.s_in + ((size_t)g.seq * a.H + h) * size : nullptr;
   float S = s_in ? s_in[w.s_turned ? (e % w.d_v) * w.d_k + e / w.d_v : e] : 0.f;
   float* at = a.seg_state + ((size_t)wi * a.n_segs * a.H + h) * size + e;
-  for (int i = 0; i < n; ++i) {
-    const int s = s0 + (w.back ? n - 1 - i : i);
-    const LinSeg gs = lin_segment(a, s);
-    float* p = at + (size_t)s * a.H * size;
-    const float own = i + 1 < n ? *p : 0.f;
-    *p = S;
-    S = fmaf(S, exp2f(l2 * gs.n), own);
+  for (int i0 = 0; i0 < n; i0 += 8) {   // eight segments' states and lengths on their way at once
+    float own[8], keep[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int i = i0 + q, s = s0 + (w.back ? n - 1 - i : i);
+      own[q] = i + 1 < n ? at[(size_t)s * a.H * size] : 0.f;
+      keep[q] = i < n ? exp2f(l2 * lin_segment(a, s).n) : 0.f;
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int i = i0 + q, s = s0 + (w.back ? n - 1 - i : i);
+      if (i < n) at[(size_t)s * a.H * size] = S;
+      S = fmaf(S, keep[q], own[q]);
+    }
   }
 }
 
