@@ -368,7 +368,7 @@ int tri_inv_linear_attention_step(const void* Q, const void* K, const void* V, c
  *     h = x + r,      y = h w / sqrt(mean h^2 + eps)
  *   X, R (may be NULL: h = x), H (may be NULL; h rounded to the storage type) [rows, n];  w [n];  all of `dtype` (TRI_INV_F32 or TRI_INV_BF16).
  *   Y [rows, n] of out_dtype: `dtype`, or TRI_INV_E4M3 with scales: group = 128: scales [rows, ceil(n / 128)], one for each 128 columns (the last group may be
- *   short), group = 0: scales [rows].  scale = max |y| / 448 over the group, 1 where that is 0; the code is y / scale rounded to nearest even.  A
+ *   short), group = 0: scales [rows].  scale = max |y| / 448 over the group (2^-126 at least), 1 where the maximum is 0; the code is y (1 / scale) rounded to nearest even.  A
  *   group with an infinity or a NaN has codes without meaning.  Other groups: TRI_INV_ERR_UNSUPPORTED.  scales is not used with out_dtype == dtype.
  * y is formed from h as it is in fp32, before it is rounded.  H may be X or R itself; otherwise outputs overlap nothing.  Pointers aligned to their type; rows
  * of whole 16-byte vectors at 16-byte aligned pointers take the faster kernels.  One launch, nothing is allocated.

@@ -1,6 +1,6 @@
 // Root-mean-square norm over rows of n values, with the residual's addition in front and an output in 8 bits behind, and its gradient.
 //     h = x + r,    y = h w / sqrt(mean h^2 + eps)
-//     y in the storage type, or per group of columns: scale = max |y| / 448 (1 where that is 0), y / scale rounded to e4m3
+//     y in the storage type, or per group of columns: scale = max |y| / 448 (1 where that is 0), y (1 / scale) rounded to e4m3
 //     u = dy w,     dx = rstd (u - h rstd^2 mean(u h)) + dh,     dw = sum over rows of dy h rstd                rstd = 1 / sqrt(mean h^2 + eps)
 // Sums, h (before it is stored), y (before it is rounded) and dw's sums over rows are fp32.
 //
@@ -17,6 +17,8 @@ namespace {
 
 constexpr int kGroup = 128;         // columns that share a scale
 constexpr float kMaxE4m3 = 448.f;
+// The scale of a group whose largest value is m: a normal number, so that its reciprocal is finite
+__device__ __forceinline__ float scale_of(float m) { return m > 0.f ? fmaxf(m / kMaxE4m3, 1.17549435e-38f) : 1.f; }
 
 __device__ __forceinline__ float up(float x) { return x; }
 __device__ __forceinline__ float up(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -152,7 +154,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) rms_norm_kernel(const _
       if constexpr (OUT == 1) {   // N columns a lane: 128 / N neighbouring lanes hold a group
 #pragma unroll
         for (int x = kGroup / N / 2; x >= 1; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-        scale[i] = m > 0.f ? m / kMaxE4m3 : 1.f;
+        scale[i] = scale_of(m);
         const int c = (t + i * TPR) * N;
         if (real && c < a.n && c % kGroup == 0) a.scales[(size_t)row * ((a.n + kGroup - 1) / kGroup) + c / kGroup] = scale[i];
       } else {
@@ -161,7 +163,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) rms_norm_kernel(const _
     }
     if constexpr (OUT == 2) {
       row_reduce<TPR, 1, true>(top, words, tid);
-      const float s = top[0] > 0.f ? top[0] / kMaxE4m3 : 1.f;
+      const float s = scale_of(top[0]);
 #pragma unroll
       for (int i = 0; i < NV; ++i) scale[i] = s;
       if (real && t == 0) a.scales[row] = s;
@@ -202,7 +204,7 @@ __global__ void __launch_bounds__(256) rms_norm_any_kernel(const __grid_constant
     float top[1] = {0.f};
     for (int c = tid; c < a.n; c += 256) top[0] = fmaxf(top[0], fabsf(y_at(h_at(c), c)));
     row_reduce<256, 1, true>(top, words, tid);
-    row_scale = top[0] > 0.f ? top[0] / kMaxE4m3 : 1.f;
+    row_scale = scale_of(top[0]);
     if (tid == 0) a.scales[blockIdx.x] = row_scale;
   }
   const int n_groups = (a.n + kGroup - 1) / kGroup;
@@ -219,7 +221,7 @@ __global__ void __launch_bounds__(256) rms_norm_any_kernel(const __grid_constant
     if constexpr (OUT == 1) {
 #pragma unroll
       for (int x = 16; x >= 1; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-      scale = m > 0.f ? m / kMaxE4m3 : 1.f;
+      scale = scale_of(m);
       if ((tid & 31) == 0) a.scales[(size_t)blockIdx.x * n_groups + gr] = scale;
     }
 #pragma unroll

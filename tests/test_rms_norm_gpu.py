@@ -140,6 +140,12 @@ def test_in_place_unaligned_and_leading_dimensions(bnd, n, dtype):
     assert not bool(y5[2].any()) and not bool(torch.isnan(y5).any())
     c, _, s = bnd.rms_norm(x["X"], torch.zeros_like(x["w"]), out_dtype=torch.float8_e4m3fn)
     assert bool((s == 1).all()) and not bool(c.float().any())
+    if dtype == torch.float32:   # values so small that their scale's reciprocal would overflow: the scale stays a normal number, zeros stay zeros
+        tiny = torch.full_like(x["w"], 1e-40)
+        tiny[:5] = 0
+        for group in (128, 0):
+            c, _, s = bnd.rms_norm(x["X"], tiny, out_dtype=torch.float8_e4m3fn, group=group)
+            assert bool((s >= 2.0 ** -126).all()) and bool(torch.isfinite(c.float()).all()) and not bool(c.float()[:, :5].any())
 
 
 def test_a_row_that_is_not_finite_stays_alone(bnd):
