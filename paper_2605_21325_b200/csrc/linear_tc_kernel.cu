@@ -479,10 +479,9 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
         }
         return true;
       });
-      if (failed) {   // every product issued so far is waited for, with a limit, before the CTA gives up its memory
-        umma_commit(b_exit);
-        mbar_wait_bounded(b_exit, 0u, lim);
-      }
+      // every product issued is waited for, with a limit, before the CTA gives up its memory: who reads them may have given up
+      umma_commit(b_exit);
+      mbar_wait_bounded(b_exit, 0u, lim);
     } else if (warp == kControlB && WHOLE) {
       // ---------------------------------------------------------------- control warp B: QS and PV
       constexpr uint32_t idesc_s = umma_idesc(cfg::M, 64, 0);
@@ -506,10 +505,8 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
         }
         return true;
       });
-      if (failed) {
-        umma_commit(b_exitb);
-        mbar_wait_bounded(b_exitb, 0u, lim);
-      }
+      umma_commit(b_exitb);
+      mbar_wait_bounded(b_exitb, 0u, lim);
     } else if (warp == kCopyL) {
       // ---------------------------------------------------------------- copy warp
       for_items([&](const LinWalk& w, int wi, int, const LinSeg& g, int h, int col0, int n_tiles, float*) -> bool {
@@ -531,7 +528,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
         }
         return true;
       });
-      if (failed && lane == 0)   // the copies still on their way into this CTA's shared memory
+      if (lane == 0)   // and every copy into this CTA's shared memory
         for (uint32_t c = t >= cfg::STAGES ? t - cfg::STAGES : 0; c < t; ++c) mbar_wait_bounded(bar_full + 8 * stage(c), lap(c), lim);
     } else if (warp == kStoreL && WHOLE) {
       // ---------------------------------------------------------------- store warp: O's tile to memory

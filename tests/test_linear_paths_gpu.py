@@ -29,9 +29,10 @@ def check(x, ld, O, S, cu=None, scale=1.0, S0=None):
     ref = lo.forward(x["Q"], x["K"], x["V"], ld, scale, S0, cu)
     mag = lo.forward(x["Q"].abs(), x["K"].abs(), x["V"].abs(), ld, scale, None if S0 is None else S0.abs(), cu)
     depth = 2 * (x["Q"].shape[3] + 64) + 4 * (x["Q"].shape[1] // 64 + 1) + 128      # as in test_linear_attention_gpu.py
-    lo.within(O, ref[0], mag[0], 1, True, depth)
+    bf = x["Q"].dtype == torch.bfloat16
+    lo.within(O, ref[0], mag[0], int(bf), bf, depth)
     if S is not None:
-        lo.within(S, ref[1], mag[1], 2.0 ** -8, False, depth)
+        lo.within(S, ref[1], mag[1], 2.0 ** -8 * bf, False, depth)
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -85,20 +86,29 @@ def test_native_marshalling_gives_the_python_bodys_bits(bnd):
         bnd.linear_attention(X, X[:, :5].contiguous(), X, ld)
 
 
-@pytest.mark.parametrize("shape", [(40, 70, 4, 128, 128), (1, 0, 7, 128, 128), (200, 3, 2, 64, 64), (1, 640, 75, 128, 128)], ids=["short", "packed", "tiny", "heads"])
-def test_more_items_than_blocks(bnd, shape):
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("shape", [(40, 70, 4, 128, 128), (1, 0, 7, 128, 128), (1, -1, 2, 64, 64), (200, 3, 2, 64, 64), (1, 640, 75, 128, 128)],
+                         ids=["short", "packed", "packed_many", "tiny", "heads"])
+def test_more_items_than_blocks(bnd, shape, dtype):
     """Blocks that walk several heads and sequences one after the other, of lengths that differ, empty ones among them."""
     B, T, H, dk, dv = shape
     cu, n = None, None
-    if T == 0:
-        lens = [(37 * i) % 151 for i in range(60)]
+    if T <= 0:
+        lens = [(37 * i) % 151 for i in range(60)] if T == 0 else [(5 * i) % 9 for i in range(700)]   # (more than one launch's worth of the table)
         cu = np.cumsum([0] + lens).astype(np.int32)
         B, T, n = 1, int(cu[-1]), len(lens)
-    x, ld = make(B, T, H, dk, dv, seed=3, n=n)
+    x, ld = make(B, T, H, dk, dv, dtype, seed=3, n=n)
     O, S = bnd.linear_attention(x["Q"], x["K"], x["V"], ld, scale=0.3, S0=x["S0"], cu_seqlens=cu)
     torch.cuda.synchronize()
     assert bnd.last_device_status() == 0
     check(x, ld, O, S, cu, 0.3, x["S0"])
+    g = bnd.linear_attention_backward(x["dO"], x["Q"], x["K"], x["V"], ld, scale=0.3, S0=x["S0"], dS=x["dS"], cu_seqlens=cu)
+    ref = lo.backward(x["dO"], x["Q"], x["K"], x["V"], ld, 0.3, x["S0"], x["dS"], cu)
+    a = {k: v.abs() for k, v in x.items()}
+    mag = lo.backward(a["dO"], a["Q"], a["K"], a["V"], ld, 0.3, a["S0"], a["dS"], cu)
+    bf = dtype == torch.bfloat16
+    for i in range(4):
+        lo.within(g[i], ref[i], mag[i], (int(bf) if i < 3 else 2.0 ** -8 * bf), bf and i < 3, 2 * (128 + 64) + 4 * (T // 64 + 1) + 128)
 
 
 def test_offsets_past_two_to_the_31st(bnd):
