@@ -188,7 +188,7 @@ inline cudaError_t launched() {
 // on one stream 5.4, 5.3 and 6.2), fused calls of 148 13.1 and 10.2 (9.5), decode steps of 4 x 8 heads 4.5 and 3.6 (4.4), fp32 layers of 2 x 512 x 4 heads 38.7 and 31.9 (33.9).
 // The tables and the layer's preparation, a few blocks each, signal at once.  What it saves is the launch and
 // the blocks' start, 0.5 to 3 us a kernel; calls in a row, us, ordinary -> this: layer on 8 x 1 tokens x 16 heads 5.6 -> 4.7 (in a graph), 333 tokens 20.5 -> 17.9, fp32
-// 2 x 2048 x 8 heads 104.7 -> 99.7, build of 8 fp32 matrices 7.5 -> 6.9.  The general CUDA-core kernels do not use it.
+// 2 x 2048 x 8 heads 104.7 -> 99.7, build of 8 fp32 matrices 7.5 -> 6.9.  The delta rule's general CUDA-core kernels do not use it.
 __device__ __forceinline__ void wait_for_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_successor_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 template <class... P, class... A>

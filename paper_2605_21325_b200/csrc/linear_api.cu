@@ -81,15 +81,24 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
       }
     }
   } else {
-    // The CUDA-core kernel, in us: a tile of one block by itself and its share of an SM at work, the same of the pass that only wants states (one product of four), and the two
-    // launches more
-    const double alone = 3.0 + 0.18 * std::max(d->d_k, d->d_v), shared = 0.75 * alone, cut = 14.0;
-    const double units = (double)d->H * walks * ((std::max(d->d_k, d->d_v) + 63) / 64);
+    // The CUDA-core kernel, in us, by the key dimension: a tile of a block that has its SM to itself, of one of two that share it, the same of the pass that only wants states (one
+    // product of four; a cut sequence's last tiles need no increment, which is another), a block's start, and what a cut costs: two launches, and each state written, joined and read.
+    // Measured, fp32, estimate / calls in a row: 16 x 64 tokens x 8 heads of 128 uncut 43 / 41; 8 x 512 x 8 of 128 uncut 206 / 201, in tiles 211 / 203, its gradient uncut 468 / 457, in
+    // pairs of tiles 532 / 524; 1 x 4096 x 8 of 128 in tiles 211 / 198, in fours 232 / 215; 2 x 2048 x 8 of 64 in tiles 75 / 68, its gradient 182 / 166; five sequences of up to 1000 x 4
+    // heads of 64 in tiles, gradient, 67 / 57.
+    const int slices_v = (d->d_v + 63) / 64, d_most = walks == 3 ? std::max(d->d_k, d->d_v) : d->d_k;
+    const double per_tile = (double)d->H * (walks == 3 ? 2 * ((d->d_k + 63) / 64) + slices_v : slices_v), slots = (d_most > 128 ? 1.0 : 2.0) * sms;
+    const double alone = 2.5 + 0.175 * d_most, state_alone = std::max(3.0, 0.11 * d_most - 2.0), start = 3.0;
+    const double both = d_most > 128 ? 1.0 : 1.45, many = d_most > 128 ? 1.0 : 1.3;   // two at a time, once and in full rounds
+    auto pass = [&](double tiles_in_all, double s, double a_tile) {
+      const double blocks = std::max(1.0, tiles_in_all / s * per_tile), full = std::floor(blocks / slots), rest = blocks - full * slots;
+      return s * a_tile * (full * many + (rest > sms ? both : rest > 0 ? 1.0 : 0.0)) + start * (full + 1);
+    };
     double best = 1e300;
     for (int n = 1; n <= 256 && n <= std::max<long long>(longest, 1); ++n) {
       const long long s = std::max<long long>(1, (longest + n - 1) / n);
-      const double rounds = std::max(1.0, std::ceil((double)tiles / s * units / (2.0 * sms) - 0.05)), all = std::max(rounds * s * alone, tiles * units / sms * shared);
-      const double cost = all + (n > 1 ? cut + 0.4 * all : 0);
+      double cost = kLaunch + pass((double)tiles, (double)s, alone * (n > 1 ? 1.0 - 0.25 / s : 1.0));
+      if (n > 1) cost += 12.0 + pass((double)tiles * (n - 1) / n, (double)s, state_alone) + 2.4e-6 * tiles / s * d->H * walks * d->d_k * d->d_v;
       if (cost < best) { best = cost; seg = s; }
     }
   }
@@ -105,7 +114,7 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
   if (n * d->H * walks * ((std::max(d->d_k, d->d_v) + 63) / 64) > 0x40000000LL) return TRI_INV_ERR_INVALID_ARG;   // blocks are counted in 32 bits, and by whole rounds of them
   p->n_segs = (int)n;
   p->cut = longest * kLinTile > p->seg_tokens;
-  p->table_bytes = d->cu_seqlens ? round_up((size_t)n * sizeof(LinSeg)) : 0;
+  p->table_bytes = d->cu_seqlens ? round_up((size_t)n * sizeof(LinSeg) + (size_t)n_seqs * sizeof(int32_t)) : 0;
   p->state_bytes = p->cut ? round_up((size_t)walks * n * d->H * d->d_k * d->d_v * sizeof(float)) : 0;
   return TRI_INV_OK;
 }
@@ -114,12 +123,13 @@ int run_walks(LinArgs& a, const LinPlan& p, const tri_inv_desc* d, bool tc, void
   cudaError_t err;
   a.status = status_word_for_current_device(&err);
   if (!a.status) return TRI_INV_ERR_CUDA;
-  a.H = d->H; a.T = d->T;
+  a.H = d->H; a.T = d->T; a.n_seqs = d->cu_seqlens ? d->n_seqs : d->B;
   a.seg_tokens = p.seg_tokens; a.segs_per_seq = p.segs_per_seq; a.n_segs = p.n_segs; a.slices = p.slices;
   if (p.n_segs == 0) return TRI_INV_OK;
   if (d->cu_seqlens) {
     a.table = (const LinSeg*)workspace;
-    if (launch_linear_table((LinSeg*)workspace, p.seg_tokens, d, stream) != cudaSuccess) return TRI_INV_ERR_CUDA;
+    a.first = (const int32_t*)(a.table + p.n_segs);
+    if (launch_linear_table((LinSeg*)workspace, (int32_t*)((LinSeg*)workspace + p.n_segs), p.seg_tokens, d, stream) != cudaSuccess) return TRI_INV_ERR_CUDA;
   }
   auto walk = [&]() { return tc ? launch_linear_tc(a, tokens_of(d), stream) : launch_linear_simt(a, d->kv_dtype, stream); };
   if (p.cut) {

@@ -44,6 +44,8 @@ struct LinArgs {
   int n_walks;
   const float* log_decay;     // [H] device
   const LinSeg* table;        // packed sequences; null: dense
+  const int32_t* first;       // with it: each sequence's first segment, in the table's order
+  int n_seqs;
   int H, T;                   // T: dense tokens a sequence
   int seg_tokens, segs_per_seq;   // dense: segments of a sequence
   int n_segs;                 // in all
@@ -101,7 +103,7 @@ cudaError_t launch_linear_tc(const LinArgs& a, long long tokens, cudaStream_t st
 // Between the two passes of a call with cut sequences: seg_state[s] from what segment s alone leaves to what enters it.
 cudaError_t launch_linear_join(const LinArgs& a, cudaStream_t stream);
 // The table of packed sequences, the longest first, from the host offsets of d.
-cudaError_t launch_linear_table(LinSeg* dev_tab, int seg_tokens, const tri_inv_desc* d, cudaStream_t stream);
+cudaError_t launch_linear_table(LinSeg* dev_tab, int32_t* dev_first, int seg_tokens, const tri_inv_desc* d, cudaStream_t stream);
 // One step on states in slots (linear_step_kernel.cu).
 struct LinStepArgs {
   const void *q, *k, *v;
