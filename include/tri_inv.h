@@ -373,7 +373,7 @@ int tri_inv_linear_attention_step(const void* Q, const void* K, const void* V, c
  *   short), group = 0: scales [rows].  scale = max |y| / 448 over the group (2^-126 at least), 1 where the maximum is 0; the code is y (1 / scale) rounded to nearest even.  A
  *   group with an infinity or a NaN has codes without meaning.  Other groups: TRI_INV_ERR_UNSUPPORTED.  scales is not used with out_dtype == dtype.
  * y is formed from h as it is in fp32, before it is rounded.  H may be X or R itself; otherwise outputs overlap nothing.  Pointers aligned to their type; rows
- * of whole 16-byte vectors at 16-byte aligned pointers take the faster kernels.  One launch, nothing is allocated.
+ * of whole 16-byte vectors at 16-byte aligned pointers are the fastest.  One launch, nothing is allocated.
  */
 int tri_inv_rms_norm(const void* X, const void* R, const void* w, void* Y, void* H, float* scales, int64_t rows, int32_t n, int32_t group, float eps,
                      int dtype, int out_dtype, void* cuda_stream);

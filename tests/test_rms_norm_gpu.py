@@ -13,7 +13,8 @@ EPS = 1e-6
 STEP = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
 DTYPES = [torch.float32, torch.bfloat16]
 SHAPES = [(1, 1), (3, 7), (2, 64), (5, 128), (1000, 128), (4, 130), (700, 200), (8, 2048), (2000, 512), (700, 1024), (700, 2048), (2, 2056), (400, 4096), (9, 5120),
-          (9, 8191), (5, 8192), (400, 8192), (3, 16384), (2, 20000)]
+          (9, 8191), (5, 8192), (400, 8192), (3, 16384), (2, 20000),
+          (5000, 127), (700, 333), (700, 801), (700, 2047), (700, 4001), (100, 7001)]   # not whole vectors: more rows than blocks, each width of the rows held value by value
 
 
 @pytest.fixture(scope="module")
