@@ -9,6 +9,7 @@
 // Measured, calls in a row: 16 x 64 tokens x 8 heads of 128 41 us, 0.27 of the FMAs' rate; 1 x 4096 x 8 of 128 198 (loads through registers and always all four products: 252), gradient of five
 // sequences of up to 1000 tokens x 4 heads of 64 57 (87).  (512 threads with tiles of 4 x 2: 16 x 64 x 8 of 128 in 52 us, 45 with these before the copies.)
 #include <algorithm>
+#include <type_traits>
 
 #include "linear_attention.cuh"
 
@@ -16,6 +17,7 @@ namespace tri_inv {
 namespace {
 
 constexpr int L = kLinTile, SL = 64, kThreadsLin = 256;
+constexpr int kFew = 16;   // a tile of at most this many tokens: a sixteenth of P, a quarter of the other rows
 
 struct alignas(8) Half4 { __nv_bfloat162 a, b; };
 template <class T>
@@ -74,7 +76,7 @@ __global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : 2) linear_simt_kern
   // A tile's rows of n features to shared memory, a warp a row, 4 features a lane (fp32: asynchronously)
   auto fetch_rows = [&](const T* src, size_t row, float* dst, int ld, int turn, int rows) {
 #pragma unroll 4
-    for (int i = warp; i < L; i += kThreadsLin / 32) {
+    for (int i = warp; i < (rows <= kFew ? kFew : L); i += kThreadsLin / 32) {
 #pragma unroll
       for (int m = 0; m < (MK + 1) / 2; ++m) {
         const int d = 4 * (lane + 32 * m);
@@ -105,18 +107,27 @@ __global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : 2) linear_simt_kern
   const float l2 = lin_log2_decay(a, h);
   if (tid <= L) pw[tid] = exp2f(l2 * tid);
   float state[WHOLE ? 1 : MK][4][4] = {};   // in the pass that only wants it: from zero, in registers
+  bool fresh = false;   // the state is still zero: not in shared memory yet, and no part of the first tile's outputs
   if constexpr (WHOLE) {
     bool turned;
     const float* s_in = lin_entry_state(a, w, wi, s, g, h, &turned);
-    if (!s_in || !turned) {
+    fresh = !s_in;
+    if (fresh) {
+    } else if (!turned) {
 #pragma unroll 4
       for (int e = tid; e < dk * (SL / 4); e += kThreadsLin) {
         const int d = e / (SL / 4), c = 4 * (e % (SL / 4));
-        *reinterpret_cast<float4*>(sS + d * SL + c) = s_in && c0 + c < w.d_v ? lds4(s_in + (size_t)d * w.d_v + c0 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+        *reinterpret_cast<float4*>(sS + d * SL + c) = c0 + c < w.d_v ? lds4(s_in + (size_t)d * w.d_v + c0 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
       }
     } else {
-      for (int c = warp; c < SL; c += kThreadsLin / 32)
-        for (int d = lane; d < dk; d += 32) sS[d * SL + c] = c0 + c < w.d_v ? s_in[(size_t)(c0 + c) * dk + d] : 0.f;
+      // a warp: 8 columns x 16 features, so that its stores meet in fours on a bank (a column x 32 features: all 32)
+      for (int e = warp; e < SL / 8 * ((dk + 15) / 16); e += kThreadsLin / 32) {
+        const int c = 8 * (e % (SL / 8)) + (lane & 7), d = 16 * (e / (SL / 8)) + 4 * (lane >> 3);
+        if (d < dk) {
+          const float4 y = c0 + c < w.d_v ? lds4(s_in + (size_t)(c0 + c) * dk + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+          sS[d * SL + c] = y.x; sS[(d + 1) * SL + c] = y.y; sS[(d + 2) * SL + c] = y.z; sS[(d + 3) * SL + c] = y.w;
+        }
+      }
     }
   }
   for (int it = 0; it < n_tiles; ++it) {
@@ -146,76 +157,84 @@ __global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : 2) linear_simt_kern
     // would be off by it in every tile, always to the same side
     const float less = expm1f(l2 * rows * 0.6931471805599453f);
     if constexpr (WHOLE) {
-      {   // P, rows ty + 16 r, columns tx + 16 m
-        float acc[4][4] = {};
-        const int turn = (tx & swz) << 2;
+      // R: 16 R of the tile's rows are in use
+      auto outputs = [&](auto rows_in_use) {
+        constexpr int R = decltype(rows_in_use)::value;
+        {   // P, rows ty + 16 r, columns tx + 16 m
+          float acc[R][R] = {};
+          const int turn = (tx & swz) << 2;
 #pragma unroll 2
-        for (int d = 0; d < dk; d += 4) {
-          float4 kk[4];
+          for (int d = 0; d < dk; d += 4) {
+            float4 kk[R];
 #pragma unroll
-          for (int m = 0; m < 4; ++m) kk[m] = lds4(sk + (tx + 16 * m) * ldk + (d ^ turn));
+            for (int m = 0; m < R; ++m) kk[m] = lds4(sk + (tx + 16 * m) * ldk + (d ^ turn));
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float4 qq = lds4(sq + (ty + 16 * r) * dk + d);
+            for (int r = 0; r < R; ++r) {
+              const float4 qq = lds4(sq + (ty + 16 * r) * dk + d);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) acc[r][m] = fmaf(qq.x, kk[m].x, acc[r][m]);
+              for (int m = 0; m < R; ++m) acc[r][m] = fmaf(qq.x, kk[m].x, acc[r][m]);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) acc[r][m] = fmaf(qq.y, kk[m].y, acc[r][m]);
+              for (int m = 0; m < R; ++m) acc[r][m] = fmaf(qq.y, kk[m].y, acc[r][m]);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) acc[r][m] = fmaf(qq.z, kk[m].z, acc[r][m]);
+              for (int m = 0; m < R; ++m) acc[r][m] = fmaf(qq.z, kk[m].z, acc[r][m]);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) acc[r][m] = fmaf(qq.w, kk[m].w, acc[r][m]);
+              for (int m = 0; m < R; ++m) acc[r][m] = fmaf(qq.w, kk[m].w, acc[r][m]);
+            }
+          }
+          __syncthreads();   // k has been read
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int m = 0; m < R; ++m) {
+              const int i = ty + 16 * r, j = tx + 16 * m, gap = b ? j - i : i - j;
+              sp[i * SL + j] = gap >= 0 ? acc[r][m] * (w.k_factor * pw[gap]) : 0.f;
+            }
+        }
+        __syncthreads();
+        float acc[R][4] = {};   // rows ty + 16 r, columns 4 tx ..
+        if (!fresh) {
+#pragma unroll 2
+          for (int d = 0; d < dk; d += 4) {
+            float4 ss[4];
+#pragma unroll
+            for (int m = 0; m < 4; ++m) ss[m] = lds4(sS + (d + m) * SL + 4 * tx);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              const float4 qq = lds4(sq + (ty + 16 * r) * dk + d);
+              fma4(acc[r], qq.x, ss[0]); fma4(acc[r], qq.y, ss[1]); fma4(acc[r], qq.z, ss[2]); fma4(acc[r], qq.w, ss[3]);
+            }
+          }
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const int i = ty + 16 * r, p = b ? rows - 1 - i : i;
+            const float f = i < rows ? pw[p + 1 - b] : 0.f;
+#pragma unroll
+            for (int m = 0; m < 4; ++m) acc[r][m] *= f;
           }
         }
-        __syncthreads();   // k has been read
+#pragma unroll 2
+        for (int j = 0; j < 16 * R; j += 4) {
+          float4 vv[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+          for (int m = 0; m < 4; ++m) vv[m] = lds4(sv + (j + m) * SL + 4 * tx);
 #pragma unroll
-          for (int m = 0; m < 4; ++m) {
-            const int i = ty + 16 * r, j = tx + 16 * m, gap = b ? j - i : i - j;
-            sp[i * SL + j] = gap >= 0 ? acc[r][m] * (w.k_factor * pw[gap]) : 0.f;
+          for (int r = 0; r < R; ++r) {
+            const float4 pp = lds4(sp + (ty + 16 * r) * SL + j);
+            fma4(acc[r], pp.x, vv[0]); fma4(acc[r], pp.y, vv[1]); fma4(acc[r], pp.z, vv[2]); fma4(acc[r], pp.w, vv[3]);
           }
-      }
-      __syncthreads();
-      float acc[4][4] = {};   // rows ty + 16 r, columns 4 tx ..
-#pragma unroll 2
-      for (int d = 0; d < dk; d += 4) {
-        float4 ss[4];
-#pragma unroll
-        for (int m = 0; m < 4; ++m) ss[m] = lds4(sS + (d + m) * SL + 4 * tx);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float4 qq = lds4(sq + (ty + 16 * r) * dk + d);
-          fma4(acc[r], qq.x, ss[0]); fma4(acc[r], qq.y, ss[1]); fma4(acc[r], qq.z, ss[2]); fma4(acc[r], qq.w, ss[3]);
         }
-      }
+        __syncthreads();   // every reader of the tile and of the entering state is through
+        if (it + 1 < n_tiles) request(it + 1);
+        T* Ot = O + ((size_t)tok0 * a.H + h) * w.d_v + c0 + 4 * tx;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = ty + 16 * r, p = b ? rows - 1 - i : i;
-        const float f = i < rows ? pw[p + 1 - b] : 0.f;
-#pragma unroll
-        for (int m = 0; m < 4; ++m) acc[r][m] *= f;
-      }
-#pragma unroll 2
-      for (int j = 0; j < L; j += 4) {
-        float4 vv[4];
-#pragma unroll
-        for (int m = 0; m < 4; ++m) vv[m] = lds4(sv + (j + m) * SL + 4 * tx);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float4 pp = lds4(sp + (ty + 16 * r) * SL + j);
-          fma4(acc[r], pp.x, vv[0]); fma4(acc[r], pp.y, vv[1]); fma4(acc[r], pp.z, vv[2]); fma4(acc[r], pp.w, vv[3]);
+        for (int r = 0; r < R; ++r) {
+          const int i = ty + 16 * r;
+          if (i < rows && c0 + 4 * tx < w.d_v)
+            store4(Ot + i * row_v, make_float4(w.out_factor * acc[r][0], w.out_factor * acc[r][1], w.out_factor * acc[r][2], w.out_factor * acc[r][3]));
         }
-      }
-      __syncthreads();   // every reader of the tile and of the entering state is through
-      if (it + 1 < n_tiles) request(it + 1);
-      T* Ot = O + ((size_t)tok0 * a.H + h) * w.d_v + c0 + 4 * tx;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = ty + 16 * r;
-        if (i < rows && c0 + 4 * tx < w.d_v)
-          store4(Ot + i * row_v, make_float4(w.out_factor * acc[r][0], w.out_factor * acc[r][1], w.out_factor * acc[r][2], w.out_factor * acc[r][3]));
-      }
+      };
+      if (rows <= kFew) outputs(std::integral_constant<int, 1>{});
+      else outputs(std::integral_constant<int, L / 16>{});
       if (passes) {
 #pragma unroll
         for (int m = 0; m < MK; ++m)
@@ -223,12 +242,13 @@ __global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : 2) linear_simt_kern
           for (int r = 0; r < 4; ++r) {
             const int d = 64 * m + 4 * ty + r;
             if (d < dk) {
-              float4 y = lds4(sS + d * SL + 4 * tx);
+              float4 y = fresh ? make_float4(0.f, 0.f, 0.f, 0.f) : lds4(sS + d * SL + 4 * tx);
               y.x = fmaf(y.x, less, y.x) + ds[m][r][0]; y.y = fmaf(y.y, less, y.y) + ds[m][r][1];
               y.z = fmaf(y.z, less, y.z) + ds[m][r][2]; y.w = fmaf(y.w, less, y.w) + ds[m][r][3];
               *reinterpret_cast<float4*>(sS + d * SL + 4 * tx) = y;
             }
           }
+        fresh = false;
       }
     } else {
       __syncthreads();   // the tile has been read
@@ -247,7 +267,7 @@ __global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : 2) linear_simt_kern
 #pragma unroll 4
       for (int e = tid; e < dk * (SL / 4); e += kThreadsLin) {
         const int d = e / (SL / 4), c = 4 * (e % (SL / 4));
-        if (c0 + c < w.d_v) *reinterpret_cast<float4*>(s_out + (size_t)d * w.d_v + c0 + c) = lds4(sS + d * SL + c);
+        if (c0 + c < w.d_v) *reinterpret_cast<float4*>(s_out + (size_t)d * w.d_v + c0 + c) = fresh ? make_float4(0.f, 0.f, 0.f, 0.f) : lds4(sS + d * SL + c);
       }
     } else if (c0 + 4 * tx < w.d_v) {
 #pragma unroll
