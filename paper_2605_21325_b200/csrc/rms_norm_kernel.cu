@@ -201,21 +201,30 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256, N == 1 && NV == 16 ? 2 
       for (int i = 0; i < NV; ++i) scale[i] = s;
       if (real && t == 0) a.scales[row] = s;
     }
+    uint8_t* Y = (uint8_t*)a.Y + base;
+    if constexpr (N == 1) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = column<N, TPR>(t, i);
-      if (real && c < a.n) {
-        const float up = 1.f / scale[i];   // (a division for every value took as long as all the rest)
-        uint8_t* y = (uint8_t*)a.Y + base + c;
-        if constexpr (N == 1) {
-          *y = (uint8_t)pack_e4m3(h[i][0] * up, 0.f);
-        } else {
+      for (int i = 0; i < NV; i += 4) {   // a group's
+        const float up = 1.f / scale[i];
+        const uint32_t code = pack_e4m3(h[i][0] * up, h[i + 1][0] * up) | pack_e4m3(h[i + 2][0] * up, h[i + 3][0] * up) << 16;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int c = column<N, TPR>(t, i + q);
+          if (real && c < a.n) Y[c] = (uint8_t)(code >> 8 * q);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = column<N, TPR>(t, i);
+        if (real && c < a.n) {
+          const float up = 1.f / scale[i];   // (a division for every value took as long as all the rest)
           uint32_t code[N / 4];
 #pragma unroll
           for (int j = 0; j < N; j += 4)
             code[j / 4] = pack_e4m3(h[i][j] * up, h[i][j + 1] * up) | pack_e4m3(h[i][j + 2] * up, h[i][j + 3] * up) << 16;
-          if constexpr (N == 8) *reinterpret_cast<uint2*>(y) = make_uint2(code[0], code[1]);
-          else *reinterpret_cast<uint32_t*>(y) = code[0];
+          if constexpr (N == 8) *reinterpret_cast<uint2*>(Y + c) = make_uint2(code[0], code[1]);
+          else *reinterpret_cast<uint32_t*>(Y + c) = code[0];
         }
       }
     }
@@ -464,8 +473,9 @@ RowShape backward_shape(int vecs) {
 template <class T>
 RowShape narrow_shape(int n) {
   if (n <= 128) return {32, 4};
-  if (n <= 512) return {128, 4};
-  if (n <= 1024) return {256, 4};
+  if (n <= 256) return {32, 8};
+  if (n <= 512) return {64, 8};
+  if (n <= 1024) return {128, 8};
   if (n <= 2048) return {256, 8};
   if (n <= 4096) return {512, 8};
   return n <= 8192 && sizeof(T) == 4 ? RowShape{512, 16} : RowShape{0, 0};
@@ -485,9 +495,10 @@ cudaError_t launch_forward(const RmsNormArgs& a, int sms, cudaStream_t stream) {
   };
   cudaError_t e;
   if (!whole && f.tpr) {
-    if (f.tpr == 32) e = go(rms_norm_kernel<T, 1, 32, 4, OUT>, 32);
-    else if (f.tpr == 128) e = go(rms_norm_kernel<T, 1, 128, 4, OUT>, 128);
-    else if (f.tpr == 256) e = f.nv == 4 ? go(rms_norm_kernel<T, 1, 256, 4, OUT>, 256) : go(rms_norm_kernel<T, 1, 256, 8, OUT>, 256);
+    if (f.tpr == 32) e = f.nv == 4 ? go(rms_norm_kernel<T, 1, 32, 4, OUT>, 32) : go(rms_norm_kernel<T, 1, 32, 8, OUT>, 32);
+    else if (f.tpr == 64) e = go(rms_norm_kernel<T, 1, 64, 8, OUT>, 64);
+    else if (f.tpr == 128) e = go(rms_norm_kernel<T, 1, 128, 8, OUT>, 128);
+    else if (f.tpr == 256) e = go(rms_norm_kernel<T, 1, 256, 8, OUT>, 256);
     else if (f.nv == 8) e = go(rms_norm_kernel<T, 1, 512, 8, OUT>, 512);
     else e = go(rms_norm_kernel<float, 1, 512, 16, OUT>, 512);
   }
@@ -518,9 +529,10 @@ cudaError_t launch_backward(const RmsNormBackwardArgs& a, int sms, cudaStream_t 
   cudaError_t e = cudaSuccess;
   if (a.rows == 0) ;   // the sum of no rows
   else if (!whole && f.tpr) {
-    if (f.tpr == 32) e = go(rms_norm_backward_kernel<T, 1, 32, 4>, 32);
-    else if (f.tpr == 128) e = go(rms_norm_backward_kernel<T, 1, 128, 4>, 128);
-    else if (f.tpr == 256) e = f.nv == 4 ? go(rms_norm_backward_kernel<T, 1, 256, 4>, 256) : go(rms_norm_backward_kernel<T, 1, 256, 8>, 256);
+    if (f.tpr == 32) e = f.nv == 4 ? go(rms_norm_backward_kernel<T, 1, 32, 4>, 32) : go(rms_norm_backward_kernel<T, 1, 32, 8>, 32);
+    else if (f.tpr == 64) e = go(rms_norm_backward_kernel<T, 1, 64, 8>, 64);
+    else if (f.tpr == 128) e = go(rms_norm_backward_kernel<T, 1, 128, 8>, 128);
+    else if (f.tpr == 256) e = go(rms_norm_backward_kernel<T, 1, 256, 8>, 256);
     else if (f.nv == 8) e = go(rms_norm_backward_kernel<T, 1, 512, 8>, 512);
     else e = go(rms_norm_backward_kernel<float, 1, 512, 16>, 512);
   }
