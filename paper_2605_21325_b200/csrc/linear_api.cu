@@ -81,18 +81,21 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
       }
     }
   } else {
-    // The CUDA-core kernel, in us, by the key dimension: a tile of a block that has its SM to itself, of one of two that share it, the same of the pass that only wants states (one
+    // The CUDA-core kernel, in us, by the key dimension: a tile of a block that has its SM to itself, of one of two or three that share it, the same of the pass that only wants states (one
     // product of four; a cut sequence's last tiles need no increment, which is another), a block's start, and what a cut costs: two launches, and each state written, joined and read.
-    // Measured, fp32, estimate / calls in a row: 16 x 64 tokens x 8 heads of 128 uncut 43 / 41; 8 x 512 x 8 of 128 uncut 206 / 201, in tiles 211 / 203, its gradient uncut 468 / 457, in
-    // pairs of tiles 532 / 524; 1 x 4096 x 8 of 128 in tiles 211 / 198, in fours 232 / 215; 2 x 2048 x 8 of 64 in tiles 75 / 68, its gradient 182 / 166; five sequences of up to 1000 x 4
-    // heads of 64 in tiles, gradient, 67 / 57.
+    // Measured, fp32, estimate / calls in a row: 16 x 64 tokens x 8 heads of 128 uncut 43 / 30; 8 x 512 x 8 of 128 uncut 206 / 167, in tiles 211 / 198, its gradient uncut 468 / 398, in
+    // pairs of tiles 532 / 495; 1 x 4096 x 8 of 128 in tiles 211 / 189, in fours 232 / 202; 2 x 2048 x 8 of 64 in tiles 77 / 65, its gradient 162 / 146; gradients of packed sequences: five of up
+    // to 1000 x 4 heads of 64 in tiles 55 / 46, twelve of up to 600 x 8 of 128 uncut 388 / 415, in tiles 620 / 520.
     const int slices_v = (d->d_v + 63) / 64, d_most = walks == 3 ? std::max(d->d_k, d->d_v) : d->d_k;
-    const double per_tile = (double)d->H * (walks == 3 ? 2 * ((d->d_k + 63) / 64) + slices_v : slices_v), slots = (d_most > 128 ? 1.0 : 2.0) * sms;
+    const double per_tile = (double)d->H * (walks == 3 ? 2 * ((d->d_k + 63) / 64) + slices_v : slices_v), slots = (d_most > 128 ? 1.0 : d_most > 64 ? 2.0 : 3.0) * sms;
     const double alone = 2.5 + 0.175 * d_most, state_alone = std::max(3.0, 0.11 * d_most - 2.0), start = 3.0;
-    const double both = d_most > 128 ? 1.0 : 1.45, many = d_most > 128 ? 1.0 : 1.3;   // two at a time, once and in full rounds
+    const double many = d_most > 128 ? 1.0 : d_most > 64 ? 1.3 : 1.85;   // a tile in full rounds of two or three blocks an SM; in a last round by the number there
     auto pass = [&](double tiles_in_all, double s, double a_tile) {
       const double blocks = std::max(1.0, tiles_in_all / s * per_tile), full = std::floor(blocks / slots), rest = blocks - full * slots;
-      return s * a_tile * (full * many + (rest > sms ? both : rest > 0 ? 1.0 : 0.0)) + start * (full + 1);
+      auto shared = [&](double n) { return n > 2.0 * sms ? 1.9 : n > sms ? 1.45 : n > 0 ? 1.0 : 0.0; };
+      // (packed: the longest first, so that the short ones fill what the last round would leave)
+      const double rounds = d->cu_seqlens ? std::max(shared(std::min(blocks, slots)), blocks / slots * many) : full * many + shared(rest);
+      return s * a_tile * rounds + start * (full + 1);
     };
     double best = 1e300;
     for (int n = 1; n <= 256 && n <= std::max<long long>(longest, 1); ++n) {

@@ -5,9 +5,10 @@
 // thread tiles of 4 x 4 (the state: 4 x 4 for every 64 features), rows read as float4 along the summed index, so that a thread reads 8 x 16 bytes for 64 FMAs.
 // What bounds it: shared memory's data path (a thread's 8 reads take about as long as its 64 FMAs) and, with few blocks, the latency of a tile's steps.  fp32 tiles arrive by
 // asynchronous copies, q, k and v at once, the next tile's while this one's output is stored.  The state's increment is formed only where another tile or the caller takes the state, so that a sequence cut into
-// single tiles costs no more products than an uncut one: one in the pass for the states, which keeps them in registers, three in the other.
-// Measured, calls in a row: 16 x 64 tokens x 8 heads of 128 41 us, 0.27 of the FMAs' rate; 1 x 4096 x 8 of 128 198 (loads through registers and always all four products: 252), gradient of five
-// sequences of up to 1000 tokens x 4 heads of 64 57 (87).  (512 threads with tiles of 4 x 2: 16 x 64 x 8 of 128 in 52 us, 45 with these before the copies.)
+// single tiles costs no more products than an uncut one: one in the pass for the states, which keeps them in registers, three in the other.  Three blocks an SM at d_k <= 64 (80 registers a thread and a
+// few spills; with two, fp32 2 x 2048 x 8 heads of 64 64 us forward and 162 backward, 66 and 154 so, five packed sequences 57 and 47), two at 128.
+// Measured, calls in a row: 16 x 64 tokens x 8 heads of 128 30 us, 0.37 of the FMAs' rate (the work with a state); 1 x 4096 x 8 of 128 189 (loads through registers and always all four products: 252), gradient
+// of five sequences of up to 1000 tokens x 4 heads of 64 46 (87).  (512 threads with tiles of 4 x 2: 16 x 64 x 8 of 128 in 52 us, 45 with these before the copies.)
 #include <algorithm>
 #include <type_traits>
 
@@ -47,7 +48,7 @@ __device__ __forceinline__ void fetch16(float* dst, const float* src, bool valid
 
 // MK: groups of 64 features.  WHOLE: outputs; otherwise the pass that only wants states (LinArgs::state_only).
 template <class T, int MK, bool WHOLE>
-__global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : 2) linear_simt_kernel(const __grid_constant__ LinArgs a, int max_slices) {
+__global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : MK == 2 ? 2 : 3) linear_simt_kernel(const __grid_constant__ LinArgs a, int max_slices) {
   extern __shared__ __align__(16) float sm[];
   constexpr bool F32 = sizeof(T) == 4;
   int x = blockIdx.x;
@@ -61,7 +62,7 @@ __global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : 2) linear_simt_kern
   // Rows without padding, so that two blocks of d_k = 128 fit an SM.  Only k is read by rows that differ between lanes: its pieces of 16 bytes change places within 128 bytes by the
   // row (piece ^ row & 7), or, where rows are not whole 128 bytes, rows are padded by one.
   const int dk = w.d_k, ldk = dk % 32 ? dk + 4 : dk, swz = dk % 32 ? 0 : 7;
-  float *sk = sm, *sv = sk + L * max(ldk, SL), *pw = sv + L * SL, *sq = pw + L + 4, *sS = sq + L * dk;   // pw: lambda^0 .. lambda^64
+  float *sk = sm, *sv = sk + L * max(ldk, SL), *pw = sv + L * SL, *wt = pw + L + 4, *sq = wt + L, *sS = sq + L * dk;   // pw: lambda^0 .. lambda^64; wt: the factors of a tile's tokens in the increment
   float* sp = sk;   // P lies where k was: k's other reader, the state's increment, comes first
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, warp = tid >> 5, lane = tid & 31;
   const LinSeg g = lin_segment(a, s);
@@ -106,6 +107,7 @@ __global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : 2) linear_simt_kern
   if (n_tiles > 0) request(0);
   const float l2 = lin_log2_decay(a, h);
   if (tid <= L) pw[tid] = exp2f(l2 * tid);
+  __syncthreads();
   float state[WHOLE ? 1 : MK][4][4] = {};   // in the pass that only wants it: from zero, in registers
   bool fresh = false;   // the state is still zero: not in shared memory yet, and no part of the first tile's outputs
   if constexpr (WHOLE) {
@@ -132,23 +134,28 @@ __global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : 2) linear_simt_kern
   }
   for (int it = 0; it < n_tiles; ++it) {
     const int tok0 = g.tok0 + tile_at(it) * L, rows = rows_at(it);
+    if (tid < L) wt[tid] = tid < rows ? w.k_factor * pw[b ? tid + 1 : rows - 1 - tid] : 0.f;
     if constexpr (F32) asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
     // the state's increment, features 64 m + 4 ty .. and columns 4 tx ..: where another tile or the caller takes the state
     const bool passes = it + 1 < n_tiles || s_out;
     float ds[MK][4][4] = {};
     if (passes) {
-#pragma unroll 4
-      for (int j = 0; j < rows; ++j) {
-        const float wj = w.k_factor * pw[b ? j + 1 : rows - 1 - j];
-        float4 vv = lds4(sv + j * SL + 4 * tx);
-        vv.x *= wj; vv.y *= wj; vv.z *= wj; vv.w *= wj;
+      for (int j0 = 0; j0 < rows; j0 += 4) {   // (rows of k and v behind the last are zeros, and so are their factors)
+        const float4 w4 = lds4(wt + j0);
+        const float wj[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
-        for (int m = 0; m < MK; ++m) {
-          const int d = 64 * m + 4 * ty;
-          if (d < dk) {
-            const float4 kk = lds4(sk + j * ldk + (d ^ (j & swz) << 2));
-            fma4(ds[m][0], kk.x, vv); fma4(ds[m][1], kk.y, vv); fma4(ds[m][2], kk.z, vv); fma4(ds[m][3], kk.w, vv);
+        for (int i = 0; i < 4; ++i) {
+          const int j = j0 + i;
+          float4 vv = lds4(sv + j * SL + 4 * tx);
+          vv.x *= wj[i]; vv.y *= wj[i]; vv.z *= wj[i]; vv.w *= wj[i];
+#pragma unroll
+          for (int m = 0; m < MK; ++m) {
+            const int d = 64 * m + 4 * ty;
+            if (d < dk) {
+              const float4 kk = lds4(sk + j * ldk + (d ^ (j & swz) << 2));
+              fma4(ds[m][0], kk.x, vv); fma4(ds[m][1], kk.y, vv); fma4(ds[m][2], kk.z, vv); fma4(ds[m][3], kk.w, vv);
+            }
           }
         }
       }
@@ -284,7 +291,7 @@ template <class T, int MK, bool WHOLE>
 cudaError_t launch_form(const LinArgs& a, int max_dk, int max_dv, cudaStream_t stream) {
   int max_ldk = SL;
   for (int i = 0; i < a.n_walks; ++i) max_ldk = std::max(max_ldk, a.walk[i].d_k % 32 ? a.walk[i].d_k + 4 : a.walk[i].d_k);
-  size_t words = (size_t)L * max_ldk + (size_t)L * SL + L + 4;
+  size_t words = (size_t)L * max_ldk + (size_t)L * SL + 2 * L + 4;
   if (WHOLE) words += (size_t)(L + SL) * max_dk;
   const size_t smem = words * sizeof(float);
   const cudaError_t e = cudaFuncSetAttribute(linear_simt_kernel<T, MK, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);

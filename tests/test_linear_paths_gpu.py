@@ -1,5 +1,8 @@
 """GPU tests of linear attention's routes: the give-up path of its waits, the two ways of marshalling, both widths of the value columns, many items a block."""
+import ctypes
+
 import numpy as np
+import pytest
 import pytest
 import torch
 
@@ -109,6 +112,31 @@ def test_more_items_than_blocks(bnd, shape, dtype):
     bf = dtype == torch.bfloat16
     for i in range(4):
         lo.within(g[i], ref[i], mag[i], (int(bf) if i < 3 else 2.0 ** -8 * bf), bf and i < 3, 2 * (128 + 64) + 4 * (T // 64 + 1) + 128)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+def test_cut_sequences_among_many(bnd, dtype):
+    """More sequences than one launch of the table takes, two of them long enough to be cut, one in each launch's part; forward and gradient."""
+    lens = [(7 * i) % 11 for i in range(400)]
+    lens[5], lens[390] = 5000, 3001
+    cu = [0]
+    for n in lens:
+        cu.append(cu[-1] + n)
+    B, T, H, dk, dv, n = 1, cu[-1], 1, 64, 64, len(lens)
+    x, ld = make(B, T, H, dk, dv, dtype, seed=4, n=n)
+    need = ctypes.c_size_t(0)
+    desc, _ = bnd.make_desc(B, T, H, dk, dv, 64, bnd._dtype_code(x["Q"]), cu)
+    assert bnd.load().tri_inv_linear_attention_workspace(ctypes.byref(desc), ctypes.byref(need)) == 0
+    assert need.value > 400 * 20 + 2 * dk * dv * 4   # states of segments beside the table
+    O, S = bnd.linear_attention(x["Q"], x["K"], x["V"], ld, scale=0.3, S0=x["S0"], cu_seqlens=cu)
+    check(x, ld, O, S, cu, 0.3, x["S0"])
+    g = bnd.linear_attention_backward(x["dO"], x["Q"], x["K"], x["V"], ld, scale=0.3, S0=x["S0"], dS=x["dS"], cu_seqlens=cu)
+    ref = lo.backward(x["dO"], x["Q"], x["K"], x["V"], ld, 0.3, x["S0"], x["dS"], cu)
+    a = {k: v.abs() for k, v in x.items()}
+    mag = lo.backward(a["dO"], a["Q"], a["K"], a["V"], ld, 0.3, a["S0"], a["dS"], cu)
+    bf = dtype == torch.bfloat16
+    for i in range(4):
+        lo.within(g[i], ref[i], mag[i], (int(bf) if i < 3 else 2.0 ** -8 * bf), bf and i < 3, 2 * (128 + 64) + 4 * (5000 // 64 + 1) + 128)
 
 
 def test_offsets_past_two_to_the_31st(bnd):
