@@ -344,7 +344,8 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256, backward_blocks(N, TPR,
       }
     }
     row_reduce<TPR>(sum, words, tid);
-    const float rstd = rsqrtf(sum[0] / (float)a.n + a.eps), back = rstd * rstd * (sum[1] / (float)a.n);
+    // (a row behind the last one adds nothing to dw: without eps its zeros would meet 1 / sqrt(0))
+    const float rstd = row < a.rows ? rsqrtf(sum[0] / (float)a.n + a.eps) : 0.f, back = rstd * rstd * (sum[1] / (float)a.n);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = column<N, TPR>(t, i);
