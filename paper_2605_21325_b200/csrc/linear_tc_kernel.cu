@@ -17,8 +17,9 @@
 // Hand-offs are mbarriers with one phase a tile: a commit for a product that is done, an arrival of each warp for an operand that is written or an accumulator that is read.
 //
 // Roundings: P, the copy of S that QS reads and O are bf16, as any operand of these products has to be (each 2^-8 relative at most, over sums in fp32; S itself
-// stays fp32 from tile to tile).  V~ = V~hi + V~lo keeps 16 bits, so that a state that is handed on is good to about 1e-5; the low half (256 of a tile's 1,152 cycles of products at
-// d_k = d_v = 128) is left out where the item's last state is not wanted: O takes S in bf16 anyway (O against 64 bits 2.6e-3 of its norm without, 2.3e-3 with, 1.7e-3 is bf16's own).
+// stays fp32 from tile to tile).  V~ = V~hi + V~lo keeps 16 bits, so that S is good to about 1e-5 wherever it goes, to the next tile, the next segment or the caller, and O's bits
+// depend neither on whether the last state is wanted nor on a segment's place.  (The low half is 256 of a tile's 1,152 cycles of products at d_k = d_v = 128; with it O is 2.3e-3 of its norm
+// from 64 bits, without it 2.6e-3, where bf16's own rounding is 1.7e-3.)
 //
 // What bounds it: a tile's chain of hand-offs while the chip has room, 1.25 us with all 128 value columns and 0.95 with 64 (the same hand-offs without arithmetic and products: three
 // quarters of that); from about as many walks as SMs on the memory.  Two slices of 64 columns double the walks and read Q and K twice, the second time mostly from L2.  bf16,
@@ -253,7 +254,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
     fewer_registers<64>();
     const int row0 = quad * cfg::RPQ;
     float* f = reinterpret_cast<float*>(smem + cfg::OFF_F) + (warp - kValue) * L;   // this warp's table of the tokens' factors
-    for_items([&](const LinWalk& w, int, int, const LinSeg& g, int h, int col0, int n_tiles, float* s_out) -> bool {
+    for_items([&](const LinWalk& w, int, int, const LinSeg& g, int h, int col0, int n_tiles, float*) -> bool {
       const float l2 = lin_log2_decay(a, h);
       int made_for = 0;
       for (int i = 0; i < n_tiles; ++i, ++t) {
@@ -309,12 +310,12 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
             for (int e = 0; e < 2; ++e) {
               const Pair y = mul2(unpack_bf16(x[th][2 * nt + e]), pair(fj.x, fj.y));
               hi[2 * nt + e] = pack_bf16(y);
-              if (s_out) lo[2 * nt + e] = pack_bf16(fma2(unpack_bf16(hi[2 * nt + e]), pair(-1.f, -1.f), y));
+              lo[2 * nt + e] = pack_bf16(fma2(unpack_bf16(hi[2 * nt + e]), pair(-1.f, -1.f), y));
             }
           }
           const uint32_t at = tmem_w + ((uint32_t)(16 * lg) << 16) + 16 * (th0 + th) + ph * vs_turn;
           tmem_st_packed16(hi, at + cfg::TM_VH);
-          if (s_out) tmem_st_packed16(lo, at + cfg::TM_VL);
+          tmem_st_packed16(lo, at + cfg::TM_VL);
         }
         tmem_wait_st();
         tc_fence_before();
@@ -449,7 +450,7 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
         }
         umma_commit(b_qk);
       };
-      for_items([&](const LinWalk& w, int, int, const LinSeg&, int, int, int n_tiles, float* s_out) -> bool {
+      for_items([&](const LinWalk& w, int, int, const LinSeg&, int, int, int n_tiles, float*) -> bool {
         for (int i = 0; i < n_tiles; ++i, ++t) {
           const uint32_t ph = t & 1, st = (stage(t) * cfg::STAGE) >> 4;
           if (i == 0) {
@@ -468,10 +469,8 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
             const uint32_t d = tmem + cfg::TM_DS + ph * ds_turn, v = tmem + ph * vs_turn;
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) umma_bf16_ta(d, v + cfg::TM_VH + 8 * ks, dKm + st + ((ks * 2048) >> 4), idesc_ds, ks > 0);
-            if (s_out) {
 #pragma unroll
-              for (int ks = 0; ks < 4; ++ks) umma_bf16_ta(d, v + cfg::TM_VL + 8 * ks, dKm + st + ((ks * 2048) >> 4), idesc_ds, 1u);
-            }
+            for (int ks = 0; ks < 4; ++ks) umma_bf16_ta(d, v + cfg::TM_VL + 8 * ks, dKm + st + ((ks * 2048) >> 4), idesc_ds, 1u);
             umma_commit(turn(b_ds, t));
           }
           umma_commit(bar_empty + 8 * stage(t));
