@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <mutex>
+
 #include "tri_inv.h"
 
 namespace tri_inv {
@@ -201,6 +203,24 @@ cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t sm
   cfg.attrs = &attr; cfg.numAttrs = 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
   if (e != cudaSuccess) (void)cudaGetLastError();   // it is returned here
+  return e;
+}
+
+// Lets `kernel` be launched with `bytes` of dynamic shared memory on the current device, where its launches differ in size.  The limit is the kernel's, not the launch's: it is only ever
+// raised, so that no other thread's smaller call lowers it between a call's own request and its launch.
+template <auto kernel>
+cudaError_t allow_shared(size_t bytes) {
+  static std::mutex mu;
+  static size_t most[64] = {0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(mu);
+  if (bytes <= most[dev]) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e != cudaSuccess) (void)cudaGetLastError();   // it is returned here
+  else most[dev] = bytes;
   return e;
 }
 

@@ -294,8 +294,8 @@ cudaError_t launch_form(const LinArgs& a, int max_dk, int max_dv, cudaStream_t s
   size_t words = (size_t)L * max_ldk + (size_t)L * SL + 2 * L + 4;
   if (WHOLE) words += (size_t)(L + SL) * max_dk;
   const size_t smem = words * sizeof(float);
-  const cudaError_t e = cudaFuncSetAttribute(linear_simt_kernel<T, MK, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) { (void)cudaGetLastError(); return e; }
+  const cudaError_t e = allow_shared<linear_simt_kernel<T, MK, WHOLE>>(smem);
+  if (e != cudaSuccess) return e;
   const int slices = (max_dv + SL - 1) / SL;
   const long long grid = (long long)slices * a.H * a.n_segs * a.n_walks;
   if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;

@@ -148,7 +148,7 @@ cudaError_t launch_chunk_scan_simt(const ScanParams& p, const void* Q, const voi
   SimtScanArgs a{Q, K, W, d_k, d_v, C, kv_dtype};
   const size_t bytes = sizeof(float) * ((size_t)d_k * kNS + (size_t)C * kNS + (size_t)C * (C + 1) + C + 3 * (size_t)C * (kSlice + 1));
   if (bytes > 220 * 1024) return cudaErrorInvalidValue;
-  cudaError_t e = cudaFuncSetAttribute(scan_simt_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  const cudaError_t e = allow_shared<scan_simt_kernel>(bytes);
   if (e != cudaSuccess) return e;
   const long long grid = (long long)p.n_seqs * p.H * ((d_v + kNS - 1) / kNS);
   if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;

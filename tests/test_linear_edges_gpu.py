@@ -26,3 +26,41 @@ def test_outputs_do_not_depend_on_the_state_being_wanted(bnd, shape, dtype):   #
     g = bnd.linear_attention_backward(x["dO"], x["Q"], x["K"], x["V"], ld, scale=0.3, S0=x["S0"], dS=x["dS"], cu_seqlens=cu)
     g2 = bnd.linear_attention_backward(x["dO"], x["Q"], x["K"], x["V"], ld, scale=0.3, S0=x["S0"], dS=x["dS"], cu_seqlens=cu, want_dS0=False)
     assert g2[3] is None and all(torch.equal(a, b) for a, b in zip(g[:3], g2[:3]))
+
+
+def two_threads(calls, rounds=1500):
+    """The last results of each call, made again and again by a thread of its own on a stream of its own."""
+    errors, results, start = [], {}, threading.Barrier(len(calls))
+
+    def work(i):
+        try:
+            torch.cuda.set_device(0)
+            with torch.cuda.stream(torch.cuda.Stream()):
+                start.wait()
+                for _ in range(rounds):
+                    results[i] = calls[i]()
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:   # reported by the test
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(calls))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors, errors
+    return [results[i] for i in range(len(calls))]
+
+
+def test_two_host_threads(bnd):   # noqa: F811
+    """Calls of different sizes from two threads: neither takes away the shared memory that the other's launch of the same kernel needs."""
+    ld = slopes(2)
+    xs = [make(1, 200, 2, d, d, torch.float32, seed=d) for d in (64, 8)]
+    g = torch.Generator(device="cuda").manual_seed(45)
+    scans = [[torch.randn(1, 256, 2, d, device="cuda", generator=g) * d ** -0.5 for _ in range(4)] + [-torch.rand(1, 256, 2, device="cuda", generator=g), C] for d, C in ((256, 64), (16, 16))]
+    for calls in ([lambda x=x: bnd.linear_attention(x["Q"], x["K"], x["V"], ld) for x in xs], [lambda s=s: bnd.chunk_scan(*s) for s in scans]):
+        want = [c() for c in calls]
+        torch.cuda.synchronize()
+        for a, b in zip(want, two_threads(calls)):
+            assert all(torch.equal(p, q) for p, q in zip(a, b))
