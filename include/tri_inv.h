@@ -346,7 +346,7 @@ int tri_inv_selftest_linear_wait_timeout(const void* Q, const void* K, const voi
  *     dQ_i = scale (sum_j w_ij (dO_i . v_j) k_j + lambda^{i+1} S0 dO_i),      dK_j = scale sum_i w_ij (dO_i . v_j) q_i + lambda^{T-1-j} dS v_j,
  *     dV_j = scale sum_i w_ij (q_i . k_j) dO_i + lambda^{T-1-j} dS^T k_j,      dS0 = lambda^T dS + scale sum_i lambda^{i+1} q_i dO_i^T
  * Nothing of the forward call is kept: its states are not needed, dQ has its own.  Types, layouts, sequences, routes and the workspace as there; d_v <= 256
- * too.  No two outputs may overlap each other or an input (dS0 == dS: INVALID_ARG).  Launches as there, on the tensor cores twice the walks where one of d_k and d_v is above 64 and
+ * too.  No output may overlap another or an input, dS0 neither dS nor S0: TRI_INV_ERR_INVALID_ARG.  Launches as there, on the tensor cores twice the walks where one of d_k and d_v is above 64 and
  * the other is not.
  */
 int tri_inv_linear_attention_backward_workspace(const tri_inv_desc* desc, size_t* bytes);

@@ -11,9 +11,20 @@ namespace {
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 template <class... P>
 bool all_aligned(P... p) { return (aligned16(p) && ...); }
+// A buffer of a call, and whether one that is written meets another (one that is absent or empty meets nothing)
+struct Span { const void* p; __int128 bytes; };   // (a descriptor's products may pass 64 bits)
+bool meets(Span a, Span b) {
+  const __int128 x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && a.bytes > 0 && b.bytes > 0 && x < y + b.bytes && y < x + a.bytes;
+}
+template <class... S>
+bool meets_any(Span a, S... b) { return (meets(a, b) || ...); }
 long long tokens_of(const tri_inv_desc* d) { return d->cu_seqlens ? (long long)d->T : (long long)d->T * d->B; }
 // whether the tensor-core kernel takes the call (without a token there is nothing for it to map)
 bool on_tensor_cores(const tri_inv_desc* d) { return tokens_of(d) > 0 && linear_tc_fits(d->d_k, d->d_v, d->kv_dtype); }
+// the bytes of a tensor of `d` features for each token and head, and of the states
+__int128 token_bytes(const tri_inv_desc* d, int features) { return (__int128)tokens_of(d) * d->H * features * (d->kv_dtype == TRI_INV_F32 ? 4 : 2); }
+__int128 state_bytes(const tri_inv_desc* d) { return (__int128)(d->cu_seqlens ? d->n_seqs : d->B) * d->H * d->d_k * d->d_v * 4; }
 size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // desc->C plays no part: the tiles are the kernels' own.
@@ -225,7 +236,14 @@ int tri_inv_linear_attention_backward(const void* dO, const void* Q, const void*
   if (!log_decay || (tokens_of(desc) > 0 && (!dO || !Q || !K || !V || !dQ || !dK || !dV)) ||
       !all_aligned(dO, Q, K, V, log_decay, S0, dS, dQ, dK, dV, dS0, workspace))
     return TRI_INV_ERR_INVALID_ARG;
-  if (dS0 && dS0 == dS) return TRI_INV_ERR_INVALID_ARG;   // another walk may still have to read dS
+  // the walks run side by side: what one writes another may still have to read
+  const __int128 qk = token_bytes(desc, desc->d_k), vo = token_bytes(desc, desc->d_v), state = state_bytes(desc);
+  const Span out[4] = {{dQ, qk}, {dK, qk}, {dV, vo}, {dS0, state}};
+  for (int i = 0; i < 4; ++i) {
+    if (meets_any(out[i], Span{dO, vo}, Span{Q, qk}, Span{K, qk}, Span{V, vo}, Span{log_decay, 4ll * desc->H}, Span{S0, state}, Span{dS, state})) return TRI_INV_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (meets(out[i], out[j])) return TRI_INV_ERR_INVALID_ARG;
+  }
   const bool tc = on_tensor_cores(desc);
   LinPlan p;
   const int e = plan(desc, 3, tc, &p);

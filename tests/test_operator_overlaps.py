@@ -1,0 +1,51 @@
+"""Buffers that may not overlap are refused on the host, before any device work: no GPU is needed.  (Only refusals are called here: the pointers are never followed.)"""
+import pytest
+
+import __graft_entry__ as entry
+
+
+@pytest.fixture(scope="module")
+def lib():
+    entry.build()
+    from paper_2605_21325_b200 import binding
+    return binding.load(), binding
+
+
+MB = 1 << 20
+TOKENS, STATE = 2 * 64 * 3 * 64 * 4, 2 * 3 * 64 * 64 * 4      # bytes of a tensor of tokens and of the states below
+
+
+def desc(b, **kw):
+    k = dict(B=2, T=64, H=3, d_k=64, d_v=64, C=64, kv_dtype=b.F32)
+    k.update(kw)
+    return b.make_desc(**k)
+
+
+def apart(n):
+    return [MB * (1 + i) for i in range(n)]
+
+
+def over(size, other):
+    """Where a buffer of ``size`` bytes meets one of ``other`` bytes at 0: at its start, its last 16 bytes, and with its own last 16."""
+    return 0, other - 16, 16 - size
+
+
+def test_a_gradient_in_an_input_state(lib):
+    L, b = lib
+    p = apart(11)                                    # dO Q K V log_decay S0 dS | dQ dK dV dS0
+    call = lambda q: L.tri_inv_linear_attention_backward(*q, 1.0, MB * 64, 1 << 30, desc(b)[0], None)   # noqa: E731
+    for other in (5, 6):
+        for at in over(STATE, STATE):
+            assert call(p[:10] + [p[other] + at]) == b.ERR_INVALID_ARG
+
+
+def test_linear_attention_backward(lib):
+    L, b = lib
+    p = apart(11)
+    call = lambda q: L.tri_inv_linear_attention_backward(*q, 1.0, MB * 64, 1 << 30, desc(b)[0], None)   # noqa: E731
+    sizes = [TOKENS] * 4 + [16] + [STATE] * 2 + [TOKENS] * 3 + [STATE]
+    for out in (7, 8, 9, 10):
+        for i in range(11):
+            if i != out:
+                for at in over(sizes[out], sizes[i]):
+                    assert call([p[i] + at if j == out else x for j, x in enumerate(p)]) == b.ERR_INVALID_ARG, (out, i, at)
