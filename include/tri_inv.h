@@ -316,7 +316,7 @@ int tri_inv_selftest_kda_scan_wait_timeout(const void* Q, const void* K, const v
  * S <- lambda^n S + (diag(lambda^{n-1-j}) K)^T V.
  *   Q, K [B,T,H,d_k], V, O [B,T,H,d_v]: device, desc->kv_dtype;  log_decay [H] fp32 device: at most 0 in any model (-inf: the state forgets at
  *   once), but positive values are computed as given;  S0, S_out [n_sequences,H,d_k,d_v] fp32 device, each may be NULL; S_out may be S0 itself.
- *   O may not overlap Q, K or V.  All pointers 16-byte aligned.
+ *   Otherwise no output may overlap an input or the other: TRI_INV_ERR_INVALID_ARG.  All pointers 16-byte aligned.
  * Dense and packed sequences as in tri_inv_build (lengths from 0 up); desc->C is not used.  d_k <= 256, d_v <= 65536, multiples of 8, else TRI_INV_ERR_UNSUPPORTED
  * (INVALID_ARG for other multiples).  bf16 with d_k and d_v up to 128 runs on the tensor cores (the state is kept in fp32; its bf16 copy and P are
  * operands; the state's increment takes lambda^{n-1-j} v_j as a sum of two bf16 numbers, so that S_out is good to about 1e-5, and O is the same with and

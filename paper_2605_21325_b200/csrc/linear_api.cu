@@ -192,6 +192,9 @@ int tri_inv_linear_attention(const void* Q, const void* K, const void* V, const 
   const int rc = check_linear(desc);
   if (rc) return rc;
   if (!log_decay || (tokens_of(desc) > 0 && (!Q || !K || !V || !O)) || !all_aligned(Q, K, V, log_decay, S0, O, S_out, workspace)) return TRI_INV_ERR_INVALID_ARG;
+  const __int128 qk = token_bytes(desc, desc->d_k), vo = token_bytes(desc, desc->d_v), state = state_bytes(desc);
+  const Span q{Q, qk}, k{K, qk}, v{V, vo}, decay{log_decay, 4ll * desc->H}, s0{S0, state}, o{O, vo}, s_out{S_out, state};
+  if (meets_any(o, q, k, v, decay, s0, s_out) || meets_any(s_out, q, k, v, decay) || (S_out != S0 && meets(s_out, s0))) return TRI_INV_ERR_INVALID_ARG;
   const bool tc = on_tensor_cores(desc);
   LinPlan p;
   const int e = plan(desc, 1, tc, &p);

@@ -49,3 +49,17 @@ def test_linear_attention_backward(lib):
             if i != out:
                 for at in over(sizes[out], sizes[i]):
                     assert call([p[i] + at if j == out else x for j, x in enumerate(p)]) == b.ERR_INVALID_ARG, (out, i, at)
+
+
+def test_linear_attention(lib):
+    L, b = lib
+    p = apart(7)                                     # Q K V log_decay S0 | O S_out
+    call = lambda q: L.tri_inv_linear_attention(*q, 1.0, MB * 64, 1 << 30, desc(b)[0], None)   # noqa: E731
+    sizes = [TOKENS, TOKENS, TOKENS, 12, STATE, TOKENS, STATE]
+    for i in (0, 1, 2, 3, 4, 6):
+        for at in over(TOKENS, max(sizes[i], 16)):
+            assert call(p[:5] + [p[i] + at] + p[6:]) == b.ERR_INVALID_ARG
+    for i in (0, 1, 2, 3, 4):
+        for at in over(STATE, max(sizes[i], 16)):
+            if i != 4 or at:                         # S_out may be S0 itself
+                assert call(p[:6] + [p[i] + at]) == b.ERR_INVALID_ARG
