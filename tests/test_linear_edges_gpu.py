@@ -64,3 +64,16 @@ def test_two_host_threads(bnd):   # noqa: F811
         torch.cuda.synchronize()
         for a, b in zip(want, two_threads(calls)):
             assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["fp32", "bf16"])
+def test_a_step_in_its_values(bnd, dtype):   # noqa: F811
+    """O in V's place gives the bits of an O of its own, in blocks of few and of many rows."""
+    for B, H, d in ((3, 2, 128), (300, 2, 128), (300, 2, 64)):
+        g = torch.Generator(device="cuda").manual_seed(46)
+        r = lambda *s: torch.randn(*s, device="cuda", generator=g)   # noqa: E731
+        Q, K, V, S, ld = r(B, H, d).to(dtype), r(B, H, d).to(dtype), r(B, H, d).to(dtype), r(B, H, d, d), slopes(H)
+        S2 = S.clone()
+        O = bnd.linear_attention_step(Q, K, V, ld, S)
+        bnd.linear_attention_step(Q, K, V, ld, S2, out=V)
+        assert torch.equal(O, V) and torch.equal(S, S2)

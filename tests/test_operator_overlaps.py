@@ -63,3 +63,14 @@ def test_linear_attention(lib):
         for at in over(STATE, max(sizes[i], 16)):
             if i != 4 or at:                         # S_out may be S0 itself
                 assert call(p[:6] + [p[i] + at]) == b.ERR_INVALID_ARG
+
+
+def test_step(lib):
+    L, b = lib
+    p = apart(6)                                     # Q K V log_decay S slots
+    row, slots = 8 * 3 * 64 * 4, 8 * 4
+    call = lambda o: L.tri_inv_linear_attention_step(*p, 8, o, 1.0, desc(b, B=8, T=1)[0], None)   # noqa: E731
+    for i, size in ((0, row), (1, row), (2, row), (3, 16), (4, 8 * 3 * 64 * 64 * 4), (5, slots)):
+        for at in over(row, size):
+            if i != 2 or at:                         # O may be V itself
+                assert call(p[i] + at) == b.ERR_INVALID_ARG, (i, at)
