@@ -320,8 +320,9 @@ int tri_inv_selftest_kda_scan_wait_timeout(const void* Q, const void* K, const v
  * Dense and packed sequences as in tri_inv_build (lengths from 0 up); desc->C is not used.  d_k <= 256, d_v <= 65536, multiples of 8, else TRI_INV_ERR_UNSUPPORTED
  * (INVALID_ARG for other multiples).  bf16 with d_k and d_v up to 128 runs on the tensor cores (the state is kept in fp32; its bf16 copy and P are
  * operands; the state's increment takes lambda^{n-1-j} v_j as a sum of two bf16 numbers, so that S_out is good to about 1e-5, and O is the same with and
- * without S_out); larger d_k or d_v and fp32 storage on the CUDA cores in fp32.  A key or value that is not finite reaches its whole tile's tokens
- * of its sequence, earlier ones too; nothing reaches another sequence.
+ * without S_out); larger d_k or d_v and fp32 storage on the CUDA cores in fp32.  A token's operands reach no earlier
+ * output, with one exception: a value that is not finite (for dQ, dK and dV what stands in its place, k, q and dO) reaches its whole tile's tokens of its sequence.  Nothing reaches another
+ * sequence.
  * Where few heads and long sequences would leave SMs idle, a sequence is cut into segments: their own states first, then joined in order, then all segments at once.
  * workspace: device memory of at least tri_inv_linear_attention_workspace() bytes (which may be 0: then it may be NULL), 16-byte aligned, contents
  * arbitrary; nothing else may use it until the call has run.  Nothing is allocated.  Launches on cuda_stream: one, two more where

@@ -341,7 +341,11 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
     float* y = reinterpret_cast<float*>(smem + cfg::OFF_F) + (warp - kValue) * L;   // this warp's table of the tokens' factors of QS
     for_items([&](const LinWalk& w, int, int, const LinSeg& g, int h, int col0, int n_tiles, float*) -> bool {
       const float l2 = lin_log2_decay(a, h), scale = w.k_factor * w.out_factor;
-      Pair f[4][2];   // P's factors, zero where it is masked: columns 32 half + 8 nt + t2, + 1 of rows ia and ib
+      Pair f[4][2];   // P's factors: columns 32 half + 8 nt + t2, + 1 of rows ia and ib
+      // The bits of such a pair that are kept, d rows below its first column.  (Zero factors are not enough where P is masked: a product there may have passed the largest number, or be
+      // NaN, and belongs to a token that has not come yet.  Formed at each use: kept in registers they cost a short call 0.2 us more)
+      const int da = ia - (32 * half + t2);
+      auto kept = [&](int d) { return w.back ? (d <= 1 ? 0xffff0000u : 0u) | (d <= 0 ? 0xffffu : 0u) : (d >= 0 ? 0xffffu : 0u) | (d >= 1 ? 0xffff0000u : 0u); };
 #pragma unroll
       for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
@@ -413,8 +417,8 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
           }
 #pragma unroll
           for (int nt = 0; nt < 4; ++nt) {
-            wa[nt] = pack_bf16(mul2(pair(qk[nt][0], qk[nt][1]), f[nt][0]));
-            wb[nt] = pack_bf16(mul2(pair(qk[nt][2], qk[nt][3]), f[nt][1]));
+            wa[nt] = pack_bf16(mul2(pair(qk[nt][0], qk[nt][1]), f[nt][0])) & kept(da - 8 * nt);
+            wb[nt] = pack_bf16(mul2(pair(qk[nt][2], qk[nt][3]), f[nt][1])) & kept(da + 8 - 8 * nt);
           }
         }
         if (t > 0 && !wait_turn2(b_pv, t - 1)) return false;   // PV of the tile before is done: its O can be read, and P's tile is free

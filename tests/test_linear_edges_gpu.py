@@ -77,3 +77,24 @@ def test_a_step_in_its_values(bnd, dtype):   # noqa: F811
         O = bnd.linear_attention_step(Q, K, V, ld, S)
         bnd.linear_attention_step(Q, K, V, ld, S2, out=V)
         assert torch.equal(O, V) and torch.equal(S, S2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["fp32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("at", [0, 40, 63, 70])
+def test_finite_values_whose_products_overflow(bnd, dtype, d, at):   # noqa: F811
+    """A query, key, value or gradient of the type's lowest value at one token: what does not follow from that token is what it is without it."""
+    x = make(1, 100, 2, d, d, dtype, seed=42)
+    ld = slopes(2)
+    O, _ = bnd.linear_attention(x["Q"], x["K"], x["V"], ld, S0=x["S0"])
+    g = bnd.linear_attention_backward(x["dO"], x["Q"], x["K"], x["V"], ld, S0=x["S0"], dS=x["dS"])
+    before, behind, all_but = slice(0, at), slice(at + 1, 100), [i for i in range(100) if i != at]
+    # the tokens of O, dQ, dK, dV that do not see the operand's token (None: all of them, [] : it is the operand's own affair)
+    clean = {"Q": (all_but, all_but, behind, behind), "K": (before, before, None, all_but), "V": (before, before, all_but, None), "dO": (None, all_but, behind, behind)}
+    for name, rows in clean.items():
+        y = dict(x, **{name: x[name].clone()})
+        y[name][:, at] = torch.finfo(dtype).min
+        O2, _ = bnd.linear_attention(y["Q"], y["K"], y["V"], ld, S0=y["S0"])
+        g2 = bnd.linear_attention_backward(y["dO"], y["Q"], y["K"], y["V"], ld, S0=y["S0"], dS=y["dS"])
+        for a, b, keep in zip((O, *g[:3]), (O2, *g2[:3]), rows):
+            assert torch.equal(a, b) if keep is None else torch.equal(a[:, keep], b[:, keep]), name
