@@ -77,6 +77,14 @@ __device__ __forceinline__ float lin_log2_decay(const LinArgs& a, int h) {
   return 1.4426950408889634f * (x < -1e4f ? -1e4f : x);
 }
 
+// lambda^n = keep + less for S <- (keep S + less S) + the increment.  Near 1 as 1 + (lambda^n - 1): a factor that is off by a rounding would be off by it in every tile, always to the same side.
+// Where it is at most a half, by itself: lambda^n - 1 rounded is off by up to 2^-25, which against a small lambda^n is not small.
+struct LinFade { float keep, less; };
+__device__ __forceinline__ LinFade lin_fade(float log2_decay, int n) {
+  const float x = log2_decay * n;
+  return x > -1.f ? LinFade{1.f, expm1f(x * 0.6931471805599453f)} : LinFade{0.f, exp2f(x)};
+}
+
 // The state that enters a segment: null stands for zero; *turned: it lies [d_v][d_k].  In a cut sequence the first segment's comes from seg_state
 // as well: s_in is then read before any s_out is written, and the two may be one buffer.
 __device__ __forceinline__ const float* lin_entry_state(const LinArgs& a, const LinWalk& w, int walk, int s, const LinSeg& g, int h, bool* turned) {

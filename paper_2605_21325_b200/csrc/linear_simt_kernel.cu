@@ -160,9 +160,7 @@ __global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : MK == 2 ? 2 : 3) li
         }
       }
     }
-    // S <- lambda^rows S + the increment; lambda^rows - 1 by expm1f: a factor near 1 that is off by a rounding
-    // would be off by it in every tile, always to the same side
-    const float less = expm1f(l2 * rows * 0.6931471805599453f);
+    const LinFade fade = lin_fade(l2, rows);   // S <- lambda^rows S + the increment
     if constexpr (WHOLE) {
       // R: 16 R of the tile's rows are in use
       auto outputs = [&](auto rows_in_use) {
@@ -250,8 +248,8 @@ __global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : MK == 2 ? 2 : 3) li
             const int d = 64 * m + 4 * ty + r;
             if (d < dk) {
               float4 y = fresh ? make_float4(0.f, 0.f, 0.f, 0.f) : lds4(sS + d * SL + 4 * tx);
-              y.x = fmaf(y.x, less, y.x) + ds[m][r][0]; y.y = fmaf(y.y, less, y.y) + ds[m][r][1];
-              y.z = fmaf(y.z, less, y.z) + ds[m][r][2]; y.w = fmaf(y.w, less, y.w) + ds[m][r][3];
+              y.x = fmaf(y.x, fade.less, fade.keep * y.x) + ds[m][r][0]; y.y = fmaf(y.y, fade.less, fade.keep * y.y) + ds[m][r][1];
+              y.z = fmaf(y.z, fade.less, fade.keep * y.z) + ds[m][r][2]; y.w = fmaf(y.w, fade.less, fade.keep * y.w) + ds[m][r][3];
               *reinterpret_cast<float4*>(sS + d * SL + 4 * tx) = y;
             }
           }
@@ -265,7 +263,7 @@ __global__ void __launch_bounds__(kThreadsLin, MK == 4 ? 1 : MK == 2 ? 2 : 3) li
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) state[m][r][c] = fmaf(state[m][r][c], less, state[m][r][c]) + ds[m][r][c];
+          for (int c = 0; c < 4; ++c) state[m][r][c] = fmaf(state[m][r][c], fade.less, fade.keep * state[m][r][c]) + ds[m][r][c];
     }
   }
   if (s_out) {

@@ -201,8 +201,8 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
           const bool in = inside(v, k);
           x = pair(in ? at[0] : 0.f, in ? at[w.d_v] : 0.f);
         });
-      // lambda^n - 1 for S <- (S + (lambda^n - 1) S) + DS: a factor near 1 that is off by a rounding would be off by it in every tile, always to the same side
-      const float l = lin_log2_decay(a, h) * 0.6931471805599453f, less_full = expm1f(l * L), less_last = expm1f(l * (g.n - (n_tiles - 1) * L));
+      const float l2 = lin_log2_decay(a, h);
+      const LinFade full = lin_fade(l2, L), last = lin_fade(l2, g.n - (n_tiles - 1) * L);
       for (int i = 0; i < n_tiles; ++i, ++t) {
         const uint32_t ph = t & 1;
         if constexpr (WHOLE) {
@@ -222,8 +222,8 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
           tc_fence_before();
           warp_arrive(b_sr, lane);
         }
-        const float less1 = tile_of(w, i, n_tiles) == n_tiles - 1 ? less_last : less_full;
-        const Pair less = pair(less1, less1);
+        const LinFade fade = tile_of(w, i, n_tiles) == n_tiles - 1 ? last : full;
+        const Pair less = pair(fade.less, fade.less);
         if (!wait_turn(b_ds, t)) return false;
         tc_fence_after();
 #pragma unroll
@@ -235,8 +235,13 @@ __global__ void __launch_bounds__(kThreadsL, 1) linear_tc_kernel(const __grid_co
           else tmem_ld_16x32(reinterpret_cast<float (&)[4][4]>(ds), at);
           tmem_wait_ld();
           if (c + STEP == NP) { tc_fence_before(); warp_arrive(turn(b_dsf, t), lane); }
+          if (fade.keep != 0.f) {
 #pragma unroll
-          for (int q = 0; q < STEP; ++q) S[c + q] = add2(fma2(S[c + q], less, S[c + q]), pair(ds[2 * q], ds[2 * q + 1]));
+            for (int q = 0; q < STEP; ++q) S[c + q] = add2(fma2(S[c + q], less, S[c + q]), pair(ds[2 * q], ds[2 * q + 1]));
+          } else {
+#pragma unroll
+            for (int q = 0; q < STEP; ++q) S[c + q] = fma2(S[c + q], less, pair(ds[2 * q], ds[2 * q + 1]));
+          }
         }
       }
       if (s_out)

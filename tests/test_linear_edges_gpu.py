@@ -98,3 +98,24 @@ def test_finite_values_whose_products_overflow(bnd, dtype, d, at):   # noqa: F81
         g2 = bnd.linear_attention_backward(y["dO"], y["Q"], y["K"], y["V"], ld, S0=y["S0"], dS=y["dS"])
         for a, b, keep in zip((O, *g[:3]), (O2, *g2[:3]), rows):
             assert torch.equal(a, b) if keep is None else torch.equal(a[:, keep], b[:, keep]), name
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["fp32", "bf16"])
+@pytest.mark.parametrize("T", [64, 100, 128])
+@pytest.mark.parametrize("ld", [-0.01, -0.1, -0.2, -0.25, -0.5])
+def test_a_large_state_that_fades(bnd, dtype, ld, T):   # noqa: F811
+    """States carried in that are a million times what the tokens add, under decays that leave from 0.5 to 1e-14 of them after a tile: what is left is good to its own last bits,
+    not to those of what it was."""
+    x = make(2, T, 2, 128, 128, dtype, seed=43)
+    x["S0"] *= 1e6
+    x["dS"] *= 1e6
+    d = torch.full((2,), ld, device="cuda")
+    O, S = bnd.linear_attention(x["Q"], x["K"], x["V"], d, scale=0.3, S0=x["S0"])
+    check_forward(bnd, x, d, None, 0.3, O, S)
+    got = bnd.linear_attention_backward(x["dO"], x["Q"], x["K"], x["V"], d, scale=0.3, S0=x["S0"], dS=x["dS"])
+    ref = lo.backward(x["dO"], x["Q"], x["K"], x["V"], d, 0.3, x["S0"], x["dS"], None)
+    a = {k: v.abs() for k, v in x.items()}
+    mag = lo.backward(a["dO"], a["Q"], a["K"], a["V"], d, 0.3, a["S0"], a["dS"], None)
+    bf = dtype == torch.bfloat16
+    for i in range(4):
+        lo.within(got[i], ref[i], mag[i], (int(bf) if i < 3 else 2.0 ** -8 * bf), bf and i < 3, depth(T, 128))
