@@ -367,10 +367,16 @@ def _optional(name, t, shape, dtype):
     return None if t is None else _operand(name, t, shape, dtype)
 
 
-def _made_for(t, stream):
-    """A tensor made here, on the current stream's memory, for a call on ``stream``."""
-    if t is not None and stream is not None:
-        t.record_stream(stream)
+def _made_for(stream, make, *args, **kw):
+    """``make(...)``, a tensor for a call on ``stream`` (None: the current one), out of that stream's memory: the current stream's may be blocks that work still queued there is going to
+    write.  The result is the caller's to use and to drop on the current stream, which the allocator is told."""
+    if stream is None:
+        return make(*args, **kw)
+    current = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        t = make(*args, **kw)
+    if t.is_cuda:
+        t.record_stream(current)
     return t
 
 
@@ -382,7 +388,8 @@ def _workspace(fn, device, stream, *args):
         raise TriInvError(fn, rc)
     if not need.value:
         return None, 0
-    return _made_for(torch.empty(need.value, dtype=torch.uint8, device=device), stream), need.value
+    with torch.cuda.stream(stream):   # (None: as it is)  Nothing but the call uses it
+        return torch.empty(need.value, dtype=torch.uint8, device=device), need.value
 
 
 def _attention_shapes(Q, V, cu_seqlens):
@@ -405,10 +412,10 @@ def linear_attention(Q, K, V, log_decay, scale=1.0, S0=None, cu_seqlens=None, ou
     desc, keep, qk, vo, st = _attention_shapes(Q, V, cu_seqlens)
     dt, f32 = Q.dtype, torch.float32
     args = [_operand("Q", Q, qk, dt), _operand("K", K, qk, dt), _operand("V", V, vo, dt), _operand("log_decay", log_decay, (qk[2],), f32), _optional("S0", S0, st, f32)]
-    O = _made_for(torch.empty_like(V), stream) if out is None else out
+    O = _made_for(stream, torch.empty_like, V) if out is None else out
     S = state_out
     if S is None and want_state:
-        S = _made_for(torch.empty(st, dtype=f32, device=V.device), stream)
+        S = _made_for(stream, torch.empty, st, dtype=f32, device=V.device)
     args += [_operand("out", O, vo, dt), _optional("state_out", S, st, f32)]
     work, need = _workspace("tri_inv_linear_attention_workspace", V.device, stream, desc)
     rc = load().tri_inv_linear_attention(*args, float(scale), _p(work), need, desc, _stream(stream))
@@ -440,10 +447,10 @@ def linear_attention_backward(dO, Q, K, V, log_decay, scale=1.0, S0=None, dS=Non
     dt, f32 = Q.dtype, torch.float32
     args = [_operand("dO", dO, vo, dt), _operand("Q", Q, qk, dt), _operand("K", K, qk, dt), _operand("V", V, vo, dt),
             _operand("log_decay", log_decay, (qk[2],), f32), _optional("S0", S0, st, f32), _optional("dS", dS, st, f32)]
-    dQ, dK, dV = (_made_for(torch.empty_like(x), stream) for x in (Q, K, V))
+    dQ, dK, dV = (_made_for(stream, torch.empty_like, x) for x in (Q, K, V))
     dS0 = None
     if want_dS0:
-        dS0 = _made_for(torch.empty(st, dtype=f32, device=V.device), stream)
+        dS0 = _made_for(stream, torch.empty, st, dtype=f32, device=V.device)
     work, need = _workspace("tri_inv_linear_attention_backward_workspace", V.device, stream, desc)
     rc = load().tri_inv_linear_attention_backward(*args, _p(dQ), _p(dK), _p(dV), _p(dS0), float(scale), _p(work), need, desc, _stream(stream))
     if rc != OK:
@@ -463,7 +470,7 @@ def linear_attention_step(Q, K, V, log_decay, S, scale=1.0, slots=None, out=None
         raise ValueError("Q and V must be [B, H, d] and S [slots, H, d_k, d_v], got %s, %s and %s" % (tuple(Q.shape), tuple(V.shape), tuple(S.shape)))
     B, H, d_k = Q.shape
     d_v, dt, f32 = V.shape[2], Q.dtype, torch.float32
-    O = _made_for(torch.empty_like(V), stream) if out is None else out
+    O = _made_for(stream, torch.empty_like, V) if out is None else out
     if B == 0:
         return O
     desc, _ = make_desc(B, 1, H, d_k, d_v, 64, _dtype_code(Q))
@@ -490,13 +497,13 @@ def rms_norm(X, w, eps=1e-6, residual=None, out_dtype=None, group=128, out=None,
     if coded and out_dtype != torch.float8_e4m3fn:
         raise TypeError("out_dtype must be the type of X or torch.float8_e4m3fn, got %s" % out_dtype)
     rows = X.numel() // n if n else 0
-    Y = _made_for(torch.empty_like(X, dtype=out_dtype), stream) if out is None else out
+    Y = _made_for(stream, torch.empty_like, X, dtype=out_dtype) if out is None else out
     H = residual_out
     if H is None and residual is not None:
-        H = _made_for(torch.empty_like(X), stream)
+        H = _made_for(stream, torch.empty_like, X)
     scales = None
     if coded:
-        scales = _made_for(torch.empty(X.shape[:-1] + ((-(-n // 128),) if group else (1,)), dtype=torch.float32, device=X.device), stream)
+        scales = _made_for(stream, torch.empty, X.shape[:-1] + ((-(-n // 128),) if group else (1,)), dtype=torch.float32, device=X.device)
     rc = load().tri_inv_rms_norm(_operand("X", X, X.shape, dt), _optional("residual", residual, X.shape, dt), _operand("w", w, (n,), dt),
                                  _operand("out", Y, X.shape, out_dtype if coded else dt), _optional("residual_out", H, X.shape, dt), _p(scales),
                                  rows, n, int(group), float(eps), code, E4M3 if coded else code, _stream(stream))
@@ -515,7 +522,7 @@ def rms_norm_backward(dY, X, w, eps=1e-6, dH=None, stream=None):
     n, dt = X.shape[-1], X.dtype
     code = _dtype_code(X)
     rows = X.numel() // n if n else 0
-    dX, dw = _made_for(torch.empty_like(X), stream), _made_for(torch.empty_like(w), stream)
+    dX, dw = _made_for(stream, torch.empty_like, X), _made_for(stream, torch.empty_like, w)
     work, need = _workspace("tri_inv_rms_norm_backward_workspace", X.device, stream, rows, n)
     rc = load().tri_inv_rms_norm_backward(_operand("dY", dY, X.shape, dt), _operand("X", X, X.shape, dt), _operand("w", w, (n,), dt), _optional("dH", dH, X.shape, dt),
                                           _p(dX), _p(dw), rows, n, float(eps), code, _p(work), need, _stream(stream))

@@ -119,3 +119,37 @@ def test_a_large_state_that_fades(bnd, dtype, ld, T):   # noqa: F811
     bf = dtype == torch.bfloat16
     for i in range(4):
         lo.within(got[i], ref[i], mag[i], (int(bf) if i < 3 else 2.0 ** -8 * bf), bf and i < 3, depth(T, 128))
+
+
+def test_memory_made_for_a_named_stream(bnd):   # noqa: F811
+    """Outputs and workspaces of a call on another stream are not memory that work still queued on the current one is going to write: blocks of the outputs' and the workspace's sizes are
+    filled there behind a delay, and given back before the call."""
+    x = make(1, 3000, 2, 128, 128, torch.bfloat16, seed=44)
+    ld, w = slopes(2), torch.ones(128, device="cuda", dtype=torch.bfloat16)
+    q, k, v = (x[n][0, :2].contiguous() for n in ("Q", "K", "V"))
+    S = torch.randn(2, 2, 128, 128, device="cuda")
+    calls = [lambda **s: bnd.linear_attention(x["Q"], x["K"], x["V"], ld, S0=x["S0"], **s),
+             lambda **s: bnd.linear_attention_backward(x["dO"], x["Q"], x["K"], x["V"], ld, S0=x["S0"], dS=x["dS"], **s),
+             lambda **s: (bnd.linear_attention_step(q, k, v, ld, S.clone() if not s else states, **s),),
+             lambda **s: bnd.rms_norm(x["Q"], w, residual=x["K"], **s)[:2],
+             lambda **s: bnd.rms_norm(x["Q"], w, residual=x["K"], out_dtype=torch.float8_e4m3fn, **s),
+             lambda **s: bnd.rms_norm_backward(x["dO"], x["Q"], w, **s)]
+    desc, _ = bnd.make_desc(1, 3000, 2, 128, 128, 64, bnd.BF16)
+    need = []
+    for f in ("tri_inv_linear_attention_workspace", "tri_inv_linear_attention_backward_workspace"):
+        n = ctypes.c_size_t(0)
+        assert getattr(bnd.load(), f)(ctypes.byref(desc), ctypes.byref(n)) == 0 and n.value > 0
+        need.append(n.value)
+    other = torch.cuda.Stream()
+    for call in calls:
+        want = call()
+        states = S.clone()
+        torch.cuda.synchronize()
+        blocks = [torch.empty(n, dtype=torch.uint8, device="cuda") for t in want for n in [t.numel() * t.element_size()] * 2] + [torch.empty(n, dtype=torch.uint8, device="cuda") for n in need]
+        torch.cuda._sleep(100_000_000)   # some 50 ms
+        for b in blocks:
+            b.fill_(0x7f)
+        del blocks, b
+        got = call(stream=other)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a.float(), b.float()) for a, b in zip(want, got))
