@@ -59,7 +59,7 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return TRI_INV_ERR_CUDA;
   const int n_seqs = d->cu_seqlens ? d->n_seqs : d->B;
-  auto len = [&](int s) { return d->cu_seqlens ? d->cu_seqlens[s + 1] - d->cu_seqlens[s] : d->T; };
+  auto len = [&](int s) -> long long { return d->cu_seqlens ? d->cu_seqlens[s + 1] - d->cu_seqlens[s] : d->T; };   // rounded up to tiles it may pass 2^31 - 1
   long long tiles = 0, longest = 0;
   if (d->cu_seqlens) {
     for (int s = 0; s < n_seqs; ++s) {
@@ -68,7 +68,7 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
       longest = std::max(longest, t);
     }
   } else {
-    longest = (d->T + kLinTile - 1) / kLinTile;
+    longest = ((long long)d->T + kLinTile - 1) / kLinTile;
     tiles = longest * n_seqs;
   }
   long long seg = std::max<long long>(longest, 1);
@@ -119,7 +119,7 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
   p->seg_tokens = (int)std::min<long long>(seg * kLinTile, 0x40000000);
   long long n = 0;
   if (d->cu_seqlens) {
-    for (int s = 0; s < n_seqs; ++s) n += std::max<long long>(1, ((long long)len(s) + p->seg_tokens - 1) / p->seg_tokens);
+    for (int s = 0; s < n_seqs; ++s) n += std::max<long long>(1, (len(s) + p->seg_tokens - 1) / p->seg_tokens);
     p->segs_per_seq = 0;
   } else {
     p->segs_per_seq = (int)std::max<long long>(1, ((long long)d->T + p->seg_tokens - 1) / p->seg_tokens);
@@ -211,7 +211,7 @@ int tri_inv_selftest_linear_wait_timeout(const void* Q, const void* K, const voi
                                          uint64_t wait_limit_ns, void* cuda_stream) {
   const int rc = check_linear(desc);
   if (rc) return rc;
-  if (!on_tensor_cores(desc) || desc->cu_seqlens) return TRI_INV_ERR_UNSUPPORTED;
+  if (!on_tensor_cores(desc) || desc->cu_seqlens || desc->T > 0x40000000) return TRI_INV_ERR_UNSUPPORTED;   // (longer sequences are always cut)
   if (!Q || !K || !V || !log_decay || !O || !wait_limit_ns || !all_aligned(Q, K, V, log_decay, O)) return TRI_INV_ERR_INVALID_ARG;
   const LinPlan p{(desc->T + kLinTile - 1) / kLinTile * kLinTile, 1, desc->B, 1, false, 0, 0};
   LinArgs a{};

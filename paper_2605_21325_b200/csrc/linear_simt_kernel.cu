@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(256) linear_table_kernel(LinSeg* tab, int32_t*
   let_successor_start();
   wait_for_predecessor();
   if (s >= b.n_seqs) return;
-  auto segs = [&](int q) { return max(1, (seq[q].n + b.seg_tokens - 1) / b.seg_tokens); };
+  auto segs = [&](int q) { return max(1, (int)(((unsigned)seq[q].n + (unsigned)b.seg_tokens - 1u) / (unsigned)b.seg_tokens)); };   // (the sum may pass 2^31 - 1)
   int before = 0;
   for (int q = lane; q < s; q += 32) before += segs(q);
 #pragma unroll
@@ -398,7 +398,7 @@ cudaError_t launch_linear_table(LinSeg* dev_tab, int32_t* dev_first, int seg_tok
     std::sort(b.seq, b.seq + b.n_seqs, [](const SeqRange& x, const SeqRange& y) { return x.n != y.n ? x.n > y.n : x.seq < y.seq; });
     const cudaError_t e = launch_early(linear_table_kernel, dim3((b.n_seqs + 7) / 8), 256, 0, stream, dev_tab, dev_first, b);
     if (e != cudaSuccess) return e;
-    for (int q = 0; q < b.n_seqs; ++q) b.first_seg += std::max(1, (b.seq[q].n + seg_tokens - 1) / seg_tokens);
+    for (int q = 0; q < b.n_seqs; ++q) b.first_seg += (int)std::max(1ll, ((long long)b.seq[q].n + seg_tokens - 1) / seg_tokens);
   }
   return cudaSuccess;
 }

@@ -153,3 +153,14 @@ def test_memory_made_for_a_named_stream(bnd):   # noqa: F811
         got = call(stream=other)
         torch.cuda.synchronize()
         assert all(torch.equal(a.float(), b.float()) for a, b in zip(want, got))
+
+
+@pytest.mark.parametrize("packed", [False, True], ids=["dense", "packed"])
+def test_the_largest_counts_of_tokens(bnd, packed):   # noqa: F811
+    """The cut of a sequence whose tokens, rounded up to tiles, pass 2^31 - 1: the workspace is that of the sequence a few tokens shorter."""
+    def size(T):
+        desc, keep = bnd.make_desc(1, T, 1, 8, 8, 64, bnd.BF16, [0, T] if packed else None)   # noqa: F841
+        n = ctypes.c_size_t(0)
+        assert bnd.load().tri_inv_linear_attention_workspace(ctypes.byref(desc), ctypes.byref(n)) == 0
+        return n.value
+    assert size(2 ** 31 - 1) == size(2 ** 31 - 64) > 0
