@@ -370,7 +370,7 @@ int tri_inv_linear_attention_step(const void* Q, const void* K, const void* V, c
 /*
  * Root-mean-square norm of rows, as it stands in front of a layer's projections (with the residual's addition) and on each head's output:
  *     h = x + r,      y = h w / sqrt(mean h^2 + eps)
- *   X, R (may be NULL: h = x), H (may be NULL; h rounded to the storage type) [rows, n];  w [n];  all of `dtype` (TRI_INV_F32 or TRI_INV_BF16).
+ *   X, R (may be NULL: h = x), H (may be NULL; h rounded to the storage type) [rows, n], rows < 2^31, n <= 2^31 - 256 (longer: TRI_INV_ERR_UNSUPPORTED);  w [n];  all of `dtype` (TRI_INV_F32 or TRI_INV_BF16).
  *   Y [rows, n] of out_dtype: `dtype`, or TRI_INV_E4M3 with scales: group = 128: scales [rows, ceil(n / 128)], one for each 128 columns (the last group may be
  *   short), group = 0: scales [rows].  scale = max |y| / 448 over the group (2^-126 at least), 1 where the maximum is 0; the code is y (1 / scale) rounded to nearest even.  A
  *   group with an infinity or a NaN has codes without meaning.  Other groups: TRI_INV_ERR_UNSUPPORTED.  scales is not used with out_dtype == dtype.

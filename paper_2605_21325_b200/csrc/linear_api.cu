@@ -172,7 +172,8 @@ LinWalk make_walk(const void* q, const void* k, const void* v, void* out, const 
 
 int check_norm(int64_t rows, int32_t n, float eps, int dtype) {
   if (rows < 0 || rows > 0x7fffffffLL || n < 1 || !(eps >= 0.f) || std::isinf(eps)) return TRI_INV_ERR_INVALID_ARG;
-  return dtype == TRI_INV_F32 || dtype == TRI_INV_BF16 ? TRI_INV_OK : TRI_INV_ERR_INVALID_ARG;
+  if (dtype != TRI_INV_F32 && dtype != TRI_INV_BF16) return TRI_INV_ERR_INVALID_ARG;
+  return n > 0x7fffff00 ? TRI_INV_ERR_UNSUPPORTED : TRI_INV_OK;   // columns are counted in 32 bits, and by 256 past the last
 }
 // whether pointers to values of the storage type are aligned to that type
 template <class... P>

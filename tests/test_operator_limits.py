@@ -1,4 +1,4 @@
-"""Buffers that may not overlap are refused on the host, before any device work: no GPU is needed.  (Only refusals are called here: the pointers are never followed.)"""
+"""Buffers that may not overlap and sizes that cannot be counted are refused on the host, before any device work: no GPU is needed.  (Only refusals are called here: the pointers are never followed.)"""
 import pytest
 
 import __graft_entry__ as entry
@@ -74,3 +74,10 @@ def test_step(lib):
         for at in over(row, size):
             if i != 2 or at:                         # O may be V itself
                 assert call(p[i] + at) == b.ERR_INVALID_ARG, (i, at)
+
+
+def test_rows_too_long_to_count(lib):
+    L, b = lib
+    for n in (2 ** 31 - 1, 2 ** 31 - 255):
+        assert L.tri_inv_rms_norm(4096, None, 4096, 4096, None, None, 1, n, 128, 1e-6, b.F32, b.F32, None) == b.ERR_UNSUPPORTED
+        assert L.tri_inv_rms_norm_backward(4096, 4096, 4096, None, 4096, 4096, 1, n, 1e-6, b.F32, 4096, 1 << 60, None) == b.ERR_UNSUPPORTED
