@@ -9,8 +9,9 @@ The marshalling of one call is native too: ``csrc/py_layer.cpp``, a CPython exte
 (``paper_2605_21325_b200/_native.so``, ``build_native``).
 
 ``build(debug=True)`` makes a second library, ``libtri_inv_debug.so``, from the same sources with
-``-DTRI_INV_DEBUG``: every shared-memory offset and global store of the kernels is bounds-checked and
-mbarrier parities are tracked; a violation raises the device status word (never a trap).
+``-DTRI_INV_DEBUG``: the swizzled shared-memory offsets, the global stores and the table reads of the factor kernels (build, WY, fused) are
+bounds-checked and mbarrier parities are tracked; a violation raises the device status word (never a trap).  The scans, the layer in one kernel,
+linear attention and the RMS norm have no such checks.
 """
 from __future__ import annotations
 

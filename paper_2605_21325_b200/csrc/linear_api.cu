@@ -39,9 +39,10 @@ int check_linear(const tri_inv_desc* d) {
 
 // Times of the tensor-core kernel in units of 1.25 us: a tile (64 tokens, d_k = d_v = 128) of all value columns and of 64, the same of the pass that only wants states, what the
 // memory traffic takes for a tile with a block on every SM (less for a gradient's three walks, which read the same tensors), a block's start and end in tiles, a kernel's launch, a
-// cut's second launch and join, and a segment's state written, joined and read.  Measured, us, estimate / calls in a row: 1 x 4096 tokens x 16 heads uncut 86 / 86, in halves of the
-// columns 69 / 67, also in four segments 53 / 49, eight of all columns 59 / 54; 1 x 32768 x 8 uncut 649 / 634, 18 segments 99 / 102; 1 x 32768 x 32 in halves 495 / 490, four
-// segments 305 / 295, nine 322 / 349; 4 x 4096 x 16 in halves 70 / 70, two segments 125 / 103, its gradient 174 / 160.
+// cut's second launch and join, and a segment's state written, joined and read.  Measured, us, estimate / calls in a captured graph on a rested GPU: 1 x 4096 tokens x 16 heads uncut
+// 89 / 85, in halves of the columns 69 / 70, also in four segments 52 / 47, eight of all columns 52 / 45; 1 x 32768 x 8 uncut 649 / 632, 18 segments 102 / 97; 1 x 32768 x 32 in
+// halves 494 / 511, four segments 304 / 289, nine 320 / 301; 4 x 4096 x 16 in halves 69 / 76, all columns 89 / 88, two segments 102 / 101; its gradient 173 / 179, in halves 196 / 223;
+// the gradient of 1 x 4096 x 16 in halves 69 / 73, uncut 89 / 87, three segments 78 / 78.
 constexpr double kTileAll = 1.0, kTileHalf = 0.76, kStateAll = 0.56, kStateHalf = 0.45, kBusyTile = 1.3, kBusyState = 0.65, kShared = 0.75, kBlock = 3.0, kLaunch = 4.0,
                  kCut = 11.0, kSegment = 0.06;
 
@@ -94,9 +95,9 @@ int plan(const tri_inv_desc* d, int walks, bool tc, LinPlan* p) {
   } else {
     // The CUDA-core kernel, in us, by the key dimension: a tile of a block that has its SM to itself, of one of two or three that share it, the same of the pass that only wants states (one
     // product of four; a cut sequence's last tiles need no increment, which is another), a block's start, and what a cut costs: two launches, and each state written, joined and read.
-    // Measured, fp32, estimate / calls in a row: 16 x 64 tokens x 8 heads of 128 uncut 43 / 30; 8 x 512 x 8 of 128 uncut 206 / 167, in tiles 211 / 198, its gradient uncut 468 / 398, in
-    // pairs of tiles 532 / 495; 1 x 4096 x 8 of 128 in tiles 211 / 189, in fours 232 / 202; 2 x 2048 x 8 of 64 in tiles 77 / 65, its gradient 162 / 146; gradients of packed sequences: five of up
-    // to 1000 x 4 heads of 64 in tiles 55 / 46, twelve of up to 600 x 8 of 128 uncut 388 / 415, in tiles 620 / 520.
+    // Measured, fp32, estimate / calls in a captured graph: 16 x 64 tokens x 8 heads of 128 uncut 43 / 30; 8 x 512 x 8 of 128 uncut 206 / 167, in tiles 211 / 198, its gradient uncut 468 / 394, in
+    // pairs of tiles 532 / 495; 1 x 4096 x 8 of 128 in tiles 211 / 186, in fours 232 / 202; 2 x 2048 x 8 of 64 in tiles 77 / 66, its gradient 162 / 154; gradients of packed sequences: five of up
+    // to 1000 x 4 heads of 64 in tiles 55 / 50, twelve of up to 600 x 8 of 128 uncut 388 / 412, in tiles 620 / 520.
     const int slices_v = (d->d_v + 63) / 64, d_most = walks == 3 ? std::max(d->d_k, d->d_v) : d->d_k;
     const double per_tile = (double)d->H * (walks == 3 ? 2 * ((d->d_k + 63) / 64) + slices_v : slices_v), slots = (d_most > 128 ? 1.0 : d_most > 64 ? 2.0 : 3.0) * sms;
     const double alone = 2.5 + 0.175 * d_most, state_alone = std::max(3.0, 0.11 * d_most - 2.0), start = 3.0;

@@ -7,8 +7,8 @@
 // asynchronous copies, q, k and v at once, the next tile's while this one's output is stored.  The state's increment is formed only where another tile or the caller takes the state, so that a sequence cut into
 // single tiles costs no more products than an uncut one: one in the pass for the states, which keeps them in registers, three in the other.  Three blocks an SM at d_k <= 64 (80 registers a thread and a
 // few spills; with two, fp32 2 x 2048 x 8 heads of 64 64 us forward and 162 backward, 66 and 154 so, five packed sequences 57 and 47), two at 128.
-// Measured, calls in a row: 16 x 64 tokens x 8 heads of 128 30 us, 0.37 of the FMAs' rate (the work with a state); 1 x 4096 x 8 of 128 189 (loads through registers and always all four products: 252), gradient
-// of five sequences of up to 1000 tokens x 4 heads of 64 46 (87).  (512 threads with tiles of 4 x 2: 16 x 64 x 8 of 128 in 52 us, 45 with these before the copies.)
+// Measured, fp32, calls in a captured graph: 16 x 64 tokens x 8 heads of 128 30 us, 0.37 of the FMAs' rate (the work with a state); 1 x 4096 x 8 of 128 186 (loads through registers and always all four
+// products: 252); 4 x 4096 x 16 of 128 1322, 0.22 of that rate; the gradient of five sequences of up to 1000 tokens x 4 heads of 64 50 (87).  bf16, 4 x 4096 x 16 of 256: 6451 us, 12 TFLOP/s.  (512 threads with tiles of 4 x 2: 16 x 64 x 8 of 128 in 52 us, 45 with these before the copies.)
 #include <algorithm>
 #include <type_traits>
 

@@ -4,7 +4,7 @@
 // One CTA per (row, head, 4 LANES value columns): a lane has four columns, a group of LANES lanes a run of features, so that the state streams
 // through registers once, in rows of 16 LANES bytes, all of a thread's loads in flight before the first is used.  What bounds it: the bytes of
 // the state, read once and written once; with few rows the latency of one load, one exchange and one store.  256 rows x 32 heads of 128 x 128 (9 of them padding): 163 us, 6.4 TB/s, 0.98 of a copy's rate; 8 rows x 16
-// heads 4.1 us on the device.
+// heads 4.2 us on the device.
 // A slot that an earlier row of the call has, or one past the cache, is an error of the caller's that only the device can see: the row's output is zero,
 // its state is left alone and the status word says TRI_INV_ERR_INVALID_ARG.
 #include "linear_attention.cuh"

@@ -21,10 +21,11 @@
 // depend neither on whether the last state is wanted nor on a segment's place.  (The low half is 256 of a tile's 1,152 cycles of products at d_k = d_v = 128; with it O is 2.3e-3 of its norm
 // from 64 bits, without it 2.6e-3, where bf16's own rounding is 1.7e-3.)
 //
-// What bounds it: a tile's chain of hand-offs while the chip has room, 1.25 us with all 128 value columns and 0.95 with 64 (the same hand-offs without arithmetic and products: three
-// quarters of that); from about as many walks as SMs on the memory.  Two slices of 64 columns double the walks and read Q and K twice, the second time mostly from L2.  bf16,
-// d = 128, calls in a row: 4 x 4096 x 16 heads (128 slices) 70 us, 3.8 TB/s; 4 x 4096 x 37 heads (148 walks of all columns) 107 us, 5.8 TB/s; the same layer's
-// gradient of 4 x 4096 x 16 (192 walks) 159 us; 1 x 32768 x 32 in segments 280 us.  A long run draws 985 W and the SM clock goes down to 1.3 to 1.8 GHz: 5 to 20 % more.
+// What bounds it: a tile's chain of hand-offs while the chip has room, 1.3 us with all 128 value columns and 1.0 with 64 (the same hand-offs without arithmetic and products: three
+// quarters of that); from about as many walks as SMs on the memory.  Two slices of 64 columns double the walks and read Q and K twice, the second time mostly from L2.  bf16, d = 128,
+// calls in a captured graph, three input sets in turn, on a rested GPU and after 0.3 s of them (the power cap then holds the SM clock at 1.7 to 1.9 GHz): 4 x 4096 x 16 heads (128
+// slices) 76 and 80 us, 3.4 TB/s; 4 x 4096 x 37 heads (148 walks of all columns) 114 and 136, 4.6 TB/s; the gradient of 4 x 4096 x 16 (192 walks) 179 and 190; 1 x 32768 x 32 in
+// segments 289 and 340.
 // Every mbarrier wait is bounded; on expiry the CTA raises the status word, waits for its own products and copies, frees its tensor memory and returns.
 #include "linear_attention.cuh"
 #include "tc_warps.cuh"

@@ -6,9 +6,10 @@
 //
 // A row is held in the registers of TPR threads, NV vectors of 16 bytes each: every value is read once and written once, which bounds the large calls; a
 // call of a few rows is the latency of one load, one exchange and one store, and takes more threads a row.  Rows that are not whole vectors, or not aligned to them, are held value by
-// value (16384 x 2047 bf16 56 us, 41 with 2048; their gradient 75 and 51); long ones take a kernel that reads them twice.
-// Measured, calls in a row: 16384 x 4096 bf16 with residual to e4m3 76 us, 6.2 TB/s, 0.94 of a copy's rate; 8 x 2048 1.5 us on the device (6 with the call); the gradient of 16384 x
-// 2048 bf16 with dH 51.5 us, 5.2 TB/s (its blocks pause at two barriers a row and end with 592 partial rows of dw, which the second launch sums), of 40000 x 128 fp32 10.7 us.
+// value (16384 x 2047 bf16 with residual 58 us, 41 with 2048; their gradient 75 and 54); long ones take a kernel that reads them twice.
+// Measured, calls in a captured graph, three input sets in turn: 16384 x 4096 bf16 with residual to e4m3 77 us rested, 80 after 0.3 s of them, 0.90 of a copy's rate; 8 x 2048 2.1 us (6 with the call);
+// the gradient of 16384 x 2048 bf16 with dH 54 us, 4.9 TB/s (its blocks pause at two barriers a row and end with 592 partial rows of dw, which the second launch sums), of 40000 x 128 fp32 13 us (11 on one input
+// set, which the L2 cache holds).
 #include <algorithm>
 
 #include "common.cuh"
