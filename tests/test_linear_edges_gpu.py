@@ -164,3 +164,23 @@ def test_the_largest_counts_of_tokens(bnd, packed):   # noqa: F811
         assert bnd.load().tri_inv_linear_attention_workspace(ctypes.byref(desc), ctypes.byref(n)) == 0
         return n.value
     assert size(2 ** 31 - 1) == size(2 ** 31 - 64) > 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["fp32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("at", [0, 40, 63, 70])
+def test_what_is_not_finite_and_not_a_value(bnd, dtype, d, at):   # noqa: F811
+    """A query or key (in the gradient what stands in its place) that is not finite at one token: what does not follow from that token is what it is without it."""
+    x = make(1, 100, 2, d, d, dtype, seed=47)
+    ld = slopes(2)
+    O, _ = bnd.linear_attention(x["Q"], x["K"], x["V"], ld, S0=x["S0"])
+    g = bnd.linear_attention_backward(x["dO"], x["Q"], x["K"], x["V"], ld, S0=x["S0"], dS=x["dS"])
+    before, behind, all_but = slice(0, at), slice(at + 1, 100), [i for i in range(100) if i != at]
+    clean = {"Q": {0: all_but, 3: behind}, "K": {0: before, 3: all_but}, "V": {1: before, 2: all_but}, "dO": {1: all_but, 2: behind}}   # of O, dQ, dK, dV
+    for bad in (float("nan"), float("inf")):
+        for name, rows in clean.items():
+            y = dict(x, **{name: x[name].clone()})
+            y[name][:, at] = bad
+            got = (bnd.linear_attention(y["Q"], y["K"], y["V"], ld, S0=y["S0"])[0],) + bnd.linear_attention_backward(y["dO"], y["Q"], y["K"], y["V"], ld, S0=y["S0"], dS=y["dS"])[:3]
+            for i, keep in rows.items():
+                assert torch.equal((O, *g)[i][:, keep], got[i][:, keep]), (name, i)
