@@ -367,29 +367,30 @@ def _optional(name, t, shape, dtype):
     return None if t is None else _operand(name, t, shape, dtype)
 
 
-def _made_for(stream, make, *args, **kw):
-    """``make(...)``, a tensor for a call on ``stream`` (None: the current one), out of that stream's memory: the current stream's may be blocks that work still queued there is going to
-    write.  The result is the caller's to use and to drop on the current stream, which the allocator is told."""
-    if stream is None:
-        return make(*args, **kw)
-    current = torch.cuda.current_stream()
-    with torch.cuda.stream(stream):
-        t = make(*args, **kw)
-    if t.is_cuda:
-        t.record_stream(current)
-    return t
+def _made_for(stream, make, work_bytes=0):
+    """(the tensors of ``make()``, ``work_bytes`` of workspace or None) for a call on ``stream`` (None: the current one), out of that stream's memory: the current stream's may be blocks
+    that work still queued there is going to write.  The tensors are the caller's to use and to drop on the current stream, which the allocator is told."""
+    current = None if stream is None else torch.cuda.current_stream()
+    if stream == current:
+        return make(), torch.empty(work_bytes, dtype=torch.uint8, device="cuda") if work_bytes else None
+    torch.cuda.set_stream(stream)   # (the context manager takes 12 us)
+    try:
+        made, work = make(), torch.empty(work_bytes, dtype=torch.uint8, device="cuda") if work_bytes else None
+    finally:
+        torch.cuda.set_stream(current)
+    for t in made:
+        if t is not None and t.is_cuda:
+            t.record_stream(current)
+    return made, work
 
 
-def _workspace(fn, device, stream, *args):
-    """(tensor or None, bytes) of what the entry point's workspace query asks for."""
+def _workspace(fn, *args):
+    """Bytes of what the entry point's workspace query asks for."""
     need = ctypes.c_size_t(0)
     rc = getattr(load(), fn)(*args, need)
     if rc != OK:
         raise TriInvError(fn, rc)
-    if not need.value:
-        return None, 0
-    with torch.cuda.stream(stream):   # (None: as it is)  Nothing but the call uses it
-        return torch.empty(need.value, dtype=torch.uint8, device=device), need.value
+    return need.value
 
 
 def _attention_shapes(Q, V, cu_seqlens):
@@ -412,12 +413,10 @@ def linear_attention(Q, K, V, log_decay, scale=1.0, S0=None, cu_seqlens=None, ou
     desc, keep, qk, vo, st = _attention_shapes(Q, V, cu_seqlens)
     dt, f32 = Q.dtype, torch.float32
     args = [_operand("Q", Q, qk, dt), _operand("K", K, qk, dt), _operand("V", V, vo, dt), _operand("log_decay", log_decay, (qk[2],), f32), _optional("S0", S0, st, f32)]
-    O = _made_for(stream, torch.empty_like, V) if out is None else out
-    S = state_out
-    if S is None and want_state:
-        S = _made_for(stream, torch.empty, st, dtype=f32, device=V.device)
+    need = _workspace("tri_inv_linear_attention_workspace", desc)
+    (O, S), work = _made_for(stream, lambda: (torch.empty_like(V) if out is None else None, torch.empty(st, dtype=f32, device=V.device) if state_out is None and want_state else None), need)
+    O, S = O if out is None else out, S if state_out is None else state_out
     args += [_operand("out", O, vo, dt), _optional("state_out", S, st, f32)]
-    work, need = _workspace("tri_inv_linear_attention_workspace", V.device, stream, desc)
     rc = load().tri_inv_linear_attention(*args, float(scale), _p(work), need, desc, _stream(stream))
     if rc != OK:
         raise TriInvError("tri_inv_linear_attention", rc)
@@ -447,11 +446,8 @@ def linear_attention_backward(dO, Q, K, V, log_decay, scale=1.0, S0=None, dS=Non
     dt, f32 = Q.dtype, torch.float32
     args = [_operand("dO", dO, vo, dt), _operand("Q", Q, qk, dt), _operand("K", K, qk, dt), _operand("V", V, vo, dt),
             _operand("log_decay", log_decay, (qk[2],), f32), _optional("S0", S0, st, f32), _optional("dS", dS, st, f32)]
-    dQ, dK, dV = (_made_for(stream, torch.empty_like, x) for x in (Q, K, V))
-    dS0 = None
-    if want_dS0:
-        dS0 = _made_for(stream, torch.empty, st, dtype=f32, device=V.device)
-    work, need = _workspace("tri_inv_linear_attention_backward_workspace", V.device, stream, desc)
+    need = _workspace("tri_inv_linear_attention_backward_workspace", desc)
+    (dQ, dK, dV, dS0), work = _made_for(stream, lambda: (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V), torch.empty(st, dtype=f32, device=V.device) if want_dS0 else None), need)
     rc = load().tri_inv_linear_attention_backward(*args, _p(dQ), _p(dK), _p(dV), _p(dS0), float(scale), _p(work), need, desc, _stream(stream))
     if rc != OK:
         raise TriInvError("tri_inv_linear_attention_backward", rc)
@@ -470,7 +466,7 @@ def linear_attention_step(Q, K, V, log_decay, S, scale=1.0, slots=None, out=None
         raise ValueError("Q and V must be [B, H, d] and S [slots, H, d_k, d_v], got %s, %s and %s" % (tuple(Q.shape), tuple(V.shape), tuple(S.shape)))
     B, H, d_k = Q.shape
     d_v, dt, f32 = V.shape[2], Q.dtype, torch.float32
-    O = _made_for(stream, torch.empty_like, V) if out is None else out
+    O = _made_for(stream, lambda: (torch.empty_like(V),))[0][0] if out is None else out
     if B == 0:
         return O
     desc, _ = make_desc(B, 1, H, d_k, d_v, 64, _dtype_code(Q))
@@ -497,13 +493,9 @@ def rms_norm(X, w, eps=1e-6, residual=None, out_dtype=None, group=128, out=None,
     if coded and out_dtype != torch.float8_e4m3fn:
         raise TypeError("out_dtype must be the type of X or torch.float8_e4m3fn, got %s" % out_dtype)
     rows = X.numel() // n if n else 0
-    Y = _made_for(stream, torch.empty_like, X, dtype=out_dtype) if out is None else out
-    H = residual_out
-    if H is None and residual is not None:
-        H = _made_for(stream, torch.empty_like, X)
-    scales = None
-    if coded:
-        scales = _made_for(stream, torch.empty, X.shape[:-1] + ((-(-n // 128),) if group else (1,)), dtype=torch.float32, device=X.device)
+    (Y, H, scales), _ = _made_for(stream, lambda: (torch.empty_like(X, dtype=out_dtype) if out is None else None, torch.empty_like(X) if residual_out is None and residual is not None else None,
+                                                   torch.empty(X.shape[:-1] + ((-(-n // 128),) if group else (1,)), dtype=torch.float32, device=X.device) if coded else None))
+    Y, H = Y if out is None else out, H if residual_out is None else residual_out
     rc = load().tri_inv_rms_norm(_operand("X", X, X.shape, dt), _optional("residual", residual, X.shape, dt), _operand("w", w, (n,), dt),
                                  _operand("out", Y, X.shape, out_dtype if coded else dt), _optional("residual_out", H, X.shape, dt), _p(scales),
                                  rows, n, int(group), float(eps), code, E4M3 if coded else code, _stream(stream))
@@ -522,8 +514,8 @@ def rms_norm_backward(dY, X, w, eps=1e-6, dH=None, stream=None):
     n, dt = X.shape[-1], X.dtype
     code = _dtype_code(X)
     rows = X.numel() // n if n else 0
-    dX, dw = _made_for(stream, torch.empty_like, X), _made_for(stream, torch.empty_like, w)
-    work, need = _workspace("tri_inv_rms_norm_backward_workspace", X.device, stream, rows, n)
+    need = _workspace("tri_inv_rms_norm_backward_workspace", rows, n)
+    (dX, dw), work = _made_for(stream, lambda: (torch.empty_like(X), torch.empty_like(w)), need)
     rc = load().tri_inv_rms_norm_backward(_operand("dY", dY, X.shape, dt), _operand("X", X, X.shape, dt), _operand("w", w, (n,), dt), _optional("dH", dH, X.shape, dt),
                                           _p(dX), _p(dw), rows, n, float(eps), code, _p(work), need, _stream(stream))
     if rc != OK:
