@@ -361,7 +361,7 @@ int tri_inv_linear_attention_backward(const void* dO, const void* Q, const void*
  *   Q, K [B,H,d_k], V, O [B,H,d_v], desc->kv_dtype;  S [n_slots,H,d_k,d_v] fp32;  slots [B] int32 device, or NULL: row b has slot b (n_slots >= B).
  * A negative slot is a padded row: its output is zero and no state is touched.  The slots of the other rows have to differ from each other and lie below
  * n_slots: a row that has an earlier row's slot, or one past the cache, is treated as padding and raises TRI_INV_ERR_INVALID_ARG in the status
- * word (tri_inv_last_device_status).  O may be V itself; otherwise it may not overlap anything: TRI_INV_ERR_INVALID_ARG.  fp32 arithmetic; one launch, nothing is
+ * word (tri_inv_last_device_status).  O may be V itself; otherwise neither O nor S may overlap anything: TRI_INV_ERR_INVALID_ARG.  fp32 arithmetic; one launch, nothing is
  * allocated.  desc->C is not used.
  */
 int tri_inv_linear_attention_step(const void* Q, const void* K, const void* V, const float* log_decay, float* S, const int32_t* slots, int32_t n_slots,

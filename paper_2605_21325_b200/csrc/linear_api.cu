@@ -271,10 +271,10 @@ int tri_inv_linear_attention_step(const void* Q, const void* K, const void* V, c
   if (!slots && n_slots < desc->B) return TRI_INV_ERR_INVALID_ARG;
   if (!Q || !K || !V || !log_decay || !S || !O || !all_aligned(Q, K, V, log_decay, S, O) || (reinterpret_cast<uintptr_t>(slots) & 3u)) return TRI_INV_ERR_INVALID_ARG;
   if ((long long)desc->B * desc->H * ((desc->d_v + 31) / 32) > 0x7fffffffLL) return TRI_INV_ERR_INVALID_ARG;
-  // blocks of one row and head read all of q and k; v and o only where they write
+  // blocks of one row and head read all of q and k while others write their part of the state and of o; of v a block reads what its o takes
   const __int128 qk = token_bytes(desc, desc->d_k), vo = token_bytes(desc, desc->d_v);
-  const Span o{O, vo}, v{V, vo}, states{S, (__int128)n_slots * desc->H * desc->d_k * desc->d_v * 4};
-  if (meets_any(o, Span{Q, qk}, Span{K, qk}, Span{log_decay, 4ll * desc->H}, states, Span{slots, 4ll * desc->B}) || (O != V && meets(o, v))) return TRI_INV_ERR_INVALID_ARG;
+  const Span q{Q, qk}, k{K, qk}, v{V, vo}, decay{log_decay, 4ll * desc->H}, states{S, (__int128)n_slots * desc->H * desc->d_k * desc->d_v * 4}, rows{slots, 4ll * desc->B}, o{O, vo};
+  if (meets_any(states, q, k, v, decay, rows, o) || meets_any(o, q, k, decay, rows) || (O != V && meets(o, v))) return TRI_INV_ERR_INVALID_ARG;
   LinStepArgs a{Q, K, V, log_decay, S, slots, O, desc->B, desc->H, desc->d_k, desc->d_v, n_slots, desc->kv_dtype == TRI_INV_BF16, scale, nullptr};
   cudaError_t err;
   a.status = status_word_for_current_device(&err);

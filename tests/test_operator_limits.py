@@ -76,6 +76,16 @@ def test_step(lib):
                 assert call(p[i] + at) == b.ERR_INVALID_ARG, (i, at)
 
 
+def test_states_of_a_step_over_its_operands(lib):
+    L, b = lib
+    p = apart(6)                                     # Q K V log_decay S slots
+    row, state = 8 * 3 * 64 * 4, 8 * 3 * 64 * 64 * 4
+    call = lambda s: L.tri_inv_linear_attention_step(*p[:4], s, p[5], 8, MB * 32, 1.0, desc(b, B=8, T=1)[0], None)   # noqa: E731
+    for i, size in ((0, row), (1, row), (2, row), (3, 16), (5, 32)):
+        for at in over(state, size):
+            assert call(p[i] + at) == b.ERR_INVALID_ARG, (i, at)
+
+
 def test_rows_too_long_to_count(lib):
     L, b = lib
     for n in (2 ** 31 - 1, 2 ** 31 - 255):
