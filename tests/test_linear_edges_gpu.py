@@ -184,3 +184,23 @@ def test_what_is_not_finite_and_not_a_value(bnd, dtype, d, at):   # noqa: F811
             got = (bnd.linear_attention(y["Q"], y["K"], y["V"], ld, S0=y["S0"])[0],) + bnd.linear_attention_backward(y["dO"], y["Q"], y["K"], y["V"], ld, S0=y["S0"], dS=y["dS"])[:3]
             for i, keep in rows.items():
                 assert torch.equal((O, *g)[i][:, keep], got[i][:, keep]), (name, i)
+
+
+WIDE = [(1, 200, 2, 256, 256, None), (1, 2500, 1, 136, 200, None), (1, 0, 2, 160, 72, PACKED), (1, 0, 2, 72, 160, PACKED), (2, 20, 3, 8, 256, None)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["fp32", "bf16"])
+@pytest.mark.parametrize("shape", WIDE, ids=["x".join(map(str, s[:5])) for s in WIDE])
+def test_heads_wider_than_the_tensor_cores_tiles(bnd, shape, dtype):   # noqa: F811
+    """Key or value dimensions above 128, cut, packed and short: prompt and gradient, inside the bounds of test_linear_attention_gpu.py."""
+    B, T, H, dk, dv, cu = shape
+    x = make(B, T, H, dk, dv, dtype, cu, seed=48)
+    ld, scale, bf = slopes(H), 0.3, dtype == torch.bfloat16
+    O, S = bnd.linear_attention(x["Q"], x["K"], x["V"], ld, scale=scale, S0=x["S0"], cu_seqlens=cu)
+    check_forward(bnd, x, ld, cu, scale, O, S)
+    got = bnd.linear_attention_backward(x["dO"], x["Q"], x["K"], x["V"], ld, scale=scale, S0=x["S0"], dS=x["dS"], cu_seqlens=cu)
+    ref = lo.backward(x["dO"], x["Q"], x["K"], x["V"], ld, scale, x["S0"], x["dS"], cu)
+    a = {k: v.abs() for k, v in x.items()}
+    mag = lo.backward(a["dO"], a["Q"], a["K"], a["V"], ld, scale, a["S0"], a["dS"], cu)
+    for i in range(4):
+        lo.within(got[i], ref[i], mag[i], (int(bf) if i < 3 else 2.0 ** -8 * bf), bf and i < 3, depth(x["Q"].shape[1], max(dk, dv)))
