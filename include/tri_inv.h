@@ -392,6 +392,111 @@ int tri_inv_rms_norm_backward(const void* dY, const void* X, const void* w, cons
                               int dtype, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * Gated linear recurrence: the layer whose state is one value for each channel.  Per sequence and channel, with h_0 = h0 or zero:
+ *     h_t = a_t h_{t-1} + u_t,      y_t = h_t
+ * where the decay a and the input u come from what the projections give, x and g, by the mode:
+ *     TRI_INV_REC_DECAY    a = exp(g),             u = x
+ *     TRI_INV_REC_NORMED   a = exp(g),             u = sqrt(1 - a^2) x        (0 where g >= 0)
+ *     TRI_INV_REC_GATE     a = 1 / (1 + exp(-g)),  u = (1 - a) x
+ * g is at most 0 in any model of the first two (-inf: the state forgets at once), but positive values are computed as given, as long as the decays' product over 64 tokens is finite.  Where a is zero
+ * the state is u, whatever came before it, also where that is not finite; a state that is not finite may also be forgotten where the decays' product since is below 2^-149.
+ */
+enum { TRI_INV_REC_DECAY = 0, TRI_INV_REC_NORMED = 1, TRI_INV_REC_GATE = 2 };
+#define TRI_INV_REC_TILE 64   /* tokens from one carried state to the next */
+typedef struct tri_inv_rec_desc {
+  int32_t B;        /* sequences in dense mode; must be 1 in packed mode */
+  int32_t T;        /* tokens per sequence (dense) or total tokens (packed); B * T < 2^31 */
+  int32_t D;        /* channels, at least 1 */
+  int32_t dtype;    /* storage of X, G, Y and of the gradients' tensors: TRI_INV_F32 or TRI_INV_BF16 */
+  int32_t mode;     /* TRI_INV_REC_* */
+  int32_t n_seqs;   /* packed: number of sequences; dense: 0 */
+  const int32_t* cu_seqlens;   /* packed: HOST array of n_seqs + 1 offsets, 0 first, T last, none below the one before; dense: NULL */
+} tri_inv_rec_desc;
+/*
+ *   X, G, Y: one row of D values for each token, ldx, ldg, ldy values from one token's row to the next (at least D; dense: a sequence's first row follows the last one's last), so that
+ *   halves of one projection's output need no copy.  Pointers aligned to their type; pointers and rows that are 16-byte aligned are the fastest.  h0, h_out [n_sequences, D] fp32, each may be NULL.
+ *   carries [tri_inv_gated_recurrence_carries() rows, D] fp32 or NULL: the state behind every 64th token of a sequence, for the gradient; rows that no token stands for are left as they are.
+ * Y may be X or G itself, h_out may be h0 itself; otherwise no output may overlap an input or another output: TRI_INV_ERR_INVALID_ARG.  Y NULL: only the states are wanted.
+ * Everything between loads and stores is fp32.  The sums' order, and so every bit of the result, depends on the call's sizes alone, save where tiles of a long sequence meet: which
+ * of the maps that join them were already joined depends on timing (a rounding of the carried state, 2^-24).
+ * workspace: at least tri_inv_gated_recurrence_workspace() bytes of device memory (which may be 0: then it may be NULL), 16-byte aligned, contents arbitrary; nothing else
+ * may use it until the call has run.  Nothing is allocated.  Launches: one, one more where sequences are cut, and with packed sequences one for every 320 of them.
+ */
+int tri_inv_gated_recurrence_carries(const tri_inv_rec_desc* desc, int64_t* rows);
+int tri_inv_gated_recurrence_workspace(const tri_inv_rec_desc* desc, size_t* bytes);
+int tri_inv_gated_recurrence(const void* X, int64_t ldx, const void* G, int64_t ldg, const float* h0, void* Y, int64_t ldy, float* h_out, float* carries,
+                             void* workspace, size_t workspace_bytes, const tri_inv_rec_desc* desc, void* cuda_stream);
+
+/*
+ * Self-test of the give-up path: the call (dense, sequences cut, zero initial state) with every wait limited to wait_limit_ns, and the first tile of the first channels of sequence 0 never
+ * announced.  The tile behind it raises TRI_INV_ERR_DEVICE_TIMEOUT in the status word and goes on with NaN: what follows the first 64 tokens there is undefined, all other output as usual.
+ * Synchronises the stream.  TRI_INV_ERR_UNSUPPORTED where the call cuts no sequence.
+ */
+int tri_inv_selftest_recurrence_wait_timeout(const void* X, const void* G, void* Y, void* workspace, size_t workspace_bytes, const tri_inv_rec_desc* desc,
+                                             uint64_t wait_limit_ns, void* cuda_stream);
+
+/*
+ * Its gradient: from dY (and dh, the gradient of the final state, or NULL: zero) those of X, G and, where dh0 is not NULL, of h0.  With c_t what token t passes on to the one before it
+ * (c behind the last token: dh) and m the factor of x in u:
+ *     e_t = dy_t + c_{t+1},    c_t = a_t e_t,    dx_t = m_t e_t,    dh0 = c_1,
+ *     dg_t = e_t a_t h_{t-1}  |  e_t (a_t h_{t-1} - a_t^2 / m_t x_t)  |  e_t (h_{t-1} - x_t) a_t (1 - a_t)
+ * (normed: the second term counts as 0 where m = 0; where a = 0 all of dg is 0 and nothing reaches what came before).  The states are formed again in fp32, from h0 and from `carries` as the forward call with the same X, G, h0 and sequences left
+ * them, or, where carries is NULL, from a walk of this call's own.  dX may be X or dY itself, dG may be G or dY itself, dh0 may be dh itself (dX and dG not both dY); otherwise no output may overlap anything.
+ * Types, layouts, sequences and launches as there (one walk more without carries); workspace: by the query with the same desc and whether carries are given.
+ */
+int tri_inv_gated_recurrence_backward_workspace(const tri_inv_rec_desc* desc, int with_carries, size_t* bytes);
+int tri_inv_gated_recurrence_backward(const void* dY, int64_t lddy, const void* X, int64_t ldx, const void* G, int64_t ldg, const float* h0, const float* dh,
+                                      const float* carries, void* dX, int64_t lddx, void* dG, int64_t lddg, float* dh0, void* workspace,
+                                      size_t workspace_bytes, const tri_inv_rec_desc* desc, void* cuda_stream);
+
+/*
+ * One token for each of B rows (desc->T == 1, dense), on states in the slots of a cache, updated in place: h <- a h + u, y = h with h = h[slots[b]].
+ *   X, G, Y as above;  h [n_slots, D] fp32;  slots [B] int32 device, or NULL: row b has slot b (n_slots >= B).
+ * A negative slot is a padded row: its output is zero and no state is touched.  The slots of the other rows have to differ from each other and lie below n_slots: a row that has an earlier row's slot,
+ * or one past the cache, is treated as padding and raises TRI_INV_ERR_INVALID_ARG in the status word (tri_inv_last_device_status).  Y may be X or G itself; otherwise neither Y nor h may
+ * overlap anything: TRI_INV_ERR_INVALID_ARG.  One launch, nothing is allocated.
+ */
+int tri_inv_gated_recurrence_step(const void* X, int64_t ldx, const void* G, int64_t ldg, float* h, const int32_t* slots, int32_t n_slots, void* Y, int64_t ldy,
+                                  const tri_inv_rec_desc* desc, void* cuda_stream);
+
+/*
+ * Norm of each query and key head with the position rotation in the same pass, as it stands between a layer's projections and its linear attention.  Per token and head:
+ *     y = R(p) (x w / sqrt(mean x^2 + eps))
+ * where R(p) turns pair i of the head's first 2 r features by the angle p inv_freq[i]: (u, v) -> (u cos - v sin, v cos + u sin).
+ */
+typedef struct tri_inv_heads_desc {
+  int64_t tokens;       /* below 2^31 */
+  int32_t T;            /* without positions a token's position is its index modulo T (T >= 1); else not used */
+  int32_t H_q, H_k;     /* heads, each at least 0 */
+  int32_t d;            /* features of a head, 1 .. 256 (more: TRI_INV_ERR_UNSUPPORTED) */
+  int32_t r;            /* pairs that are turned, 0 .. d / 2 */
+  int32_t interleaved;  /* 0: pair i is features (i, i + r);  1: (2 i, 2 i + 1) */
+  int32_t dtype;        /* storage of every tensor but inv_freq: TRI_INV_F32 or TRI_INV_BF16 */
+  float eps;            /* >= 0 */
+} tri_inv_heads_desc;
+/*
+ *   Q, Yq: a row of H_q heads of d values for each token, ldq, ldyq values from one row to the next (at least H_q d); K, Yk the same with H_k (0: K, wk and Yk are not used).  wq, wk [d], each may be NULL (ones);
+ *   inv_freq [r] fp32 device, finite;  positions [tokens] int32 device or NULL.  A negative position is a padded token: its outputs are zero.
+ * Angles are exact to 2^-25 of a turn at any position: p inv_freq / 2 pi is taken modulo 1 in 64 bits.  The rest is fp32.  Yq may be Q itself and Yk may be K itself; otherwise outputs overlap nothing
+ * (rows of one buffer may lie beside each other): TRI_INV_ERR_INVALID_ARG.  Pointers aligned to their type; d, r (where pairs are not interleaved), rows and pointers in
+ * whole 16-byte vectors are the fastest.  One launch, nothing is allocated.
+ */
+int tri_inv_qk_norm_rope(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* wq, const void* wk, const float* inv_freq, const int32_t* positions,
+                         void* Yq, int64_t ldyq, void* Yk, int64_t ldyk, const tri_inv_heads_desc* desc, void* cuda_stream);
+
+/*
+ * Its gradient, from dYq, dYk and the forward call's Q, K and weights: with v = R(-p) dy, rstd = 1 / sqrt(mean x^2 + eps) and u = v w
+ *     dx = rstd (u - x rstd^2 mean(u x)),        dw = sum over tokens and heads of v x rstd
+ * A padded token's dQ and dK are zero and it adds nothing to dw.  dwq, dwk [d], each may be NULL; summed in fp32 in an order that depends on the sizes and layouts alone.  dQ may be Q or dYq itself, dK may be K or dYk itself; otherwise outputs
+ * overlap nothing.  workspace: at least tri_inv_qk_norm_rope_backward_workspace() bytes of device memory, 16-byte aligned.  Two launches (one without dwq and dwk), nothing is allocated.
+ */
+int tri_inv_qk_norm_rope_backward_workspace(const tri_inv_heads_desc* desc, size_t* bytes);
+int tri_inv_qk_norm_rope_backward(const void* dYq, int64_t lddyq, const void* dYk, int64_t lddyk, const void* Q, int64_t ldq, const void* K, int64_t ldk,
+                                  const void* wq, const void* wk, const float* inv_freq, const int32_t* positions, void* dQ, int64_t lddq, void* dK,
+                                  int64_t lddk, void* dwq, void* dwk, void* workspace, size_t workspace_bytes, const tri_inv_heads_desc* desc,
+                                  void* cuda_stream);
+
+/*
  * Fused call with the layer's front end folded in: the kernel takes what the projections produce and
  * does the three producers that otherwise run as separate passes over memory before the inversion
  * (the gating recipe of a Gated-DeltaNet layer; in the paper these are among the kernels its fused

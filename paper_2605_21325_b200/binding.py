@@ -40,12 +40,17 @@ def ns_iters(m: int) -> int:
     return (int(m) & 0xF) << 12
 
 
+REC_DECAY, REC_NORMED, REC_GATE = 0, 1, 2
+REC_TILE = 64
+
 FORCE_SIMT = 0x10000
 W_DECAY = 0x20000
 
 EXPORTS = ("tri_inv_build", "tri_inv_build_kda", "tri_inv_fused_kda", "tri_inv_chunk_scan_kda", "tri_inv_chunk_scan", "tri_inv_gdn_forward", "tri_inv_gdn_forward_workspace",
            "tri_inv_linear_attention", "tri_inv_linear_attention_workspace", "tri_inv_linear_attention_backward", "tri_inv_linear_attention_backward_workspace",
            "tri_inv_linear_attention_step", "tri_inv_selftest_linear_wait_timeout", "tri_inv_rms_norm", "tri_inv_rms_norm_backward", "tri_inv_rms_norm_backward_workspace",
+           "tri_inv_gated_recurrence", "tri_inv_gated_recurrence_carries", "tri_inv_gated_recurrence_workspace", "tri_inv_gated_recurrence_backward", "tri_inv_gated_recurrence_backward_workspace",
+           "tri_inv_gated_recurrence_step", "tri_inv_selftest_recurrence_wait_timeout", "tri_inv_qk_norm_rope", "tri_inv_qk_norm_rope_backward", "tri_inv_qk_norm_rope_backward_workspace",
            "tri_inv_wy", "tri_inv_fused", "tri_inv_fused_raw", "tri_inv_fused_packed_static", "tri_inv_count_matrices",
            "tri_inv_fused_host", "tri_inv_fused_host_workspace", "tri_inv_selftest_wait_timeout", "tri_inv_selftest_scan_wait_timeout", "tri_inv_selftest_kda_wait_timeout", "tri_inv_selftest_bounds_check", "tri_inv_last_device_status", "tri_inv_launch_count", "tri_inv_status_string")
 
@@ -55,6 +60,16 @@ class Desc(ctypes.Structure):
                 ("d_k", ctypes.c_int32), ("d_v", ctypes.c_int32), ("C", ctypes.c_int32),
                 ("kv_dtype", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
                 ("cu_seqlens", ctypes.c_void_p)]
+
+
+class RecDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32), ("mode", ctypes.c_int32),
+                ("n_seqs", ctypes.c_int32), ("cu_seqlens", ctypes.c_void_p)]
+
+
+class HeadsDesc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("T", ctypes.c_int32), ("H_q", ctypes.c_int32), ("H_k", ctypes.c_int32), ("d", ctypes.c_int32), ("r", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
 class TriInvError(RuntimeError):
@@ -130,8 +145,19 @@ def load():
             lib.tri_inv_rms_norm.argtypes = [vp] * 6 + [i64, n32, n32, f32, i32, i32, vp]
             lib.tri_inv_rms_norm_backward_workspace.argtypes = [i64, n32, szp]
             lib.tri_inv_rms_norm_backward.argtypes = [vp] * 6 + [i64, n32, f32, i32, vp, sz, vp]
+            rp, hp = ctypes.POINTER(RecDesc), ctypes.POINTER(HeadsDesc)
+            lib.tri_inv_gated_recurrence_carries.argtypes = [rp, ctypes.POINTER(i64)]
+            lib.tri_inv_gated_recurrence_workspace.argtypes = [rp, szp]
+            lib.tri_inv_gated_recurrence.argtypes = [vp, i64, vp, i64, vp, vp, i64, vp, vp, vp, sz, rp, vp]
+            lib.tri_inv_gated_recurrence_backward_workspace.argtypes = [rp, i32, szp]
+            lib.tri_inv_gated_recurrence_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, sz, rp, vp]
+            lib.tri_inv_gated_recurrence_step.argtypes = [vp, i64, vp, i64, vp, vp, n32, vp, i64, rp, vp]
+            lib.tri_inv_selftest_recurrence_wait_timeout.argtypes = [vp, vp, vp, vp, sz, rp, ctypes.c_uint64, vp]
+            lib.tri_inv_qk_norm_rope.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, hp, vp]
+            lib.tri_inv_qk_norm_rope_backward_workspace.argtypes = [hp, szp]
+            lib.tri_inv_qk_norm_rope_backward.argtypes = [vp, i64] * 4 + [vp] * 4 + [vp, i64] * 2 + [vp, vp, vp, sz, hp, vp]
             for f in EXPORTS:
-                if "linear" in f or "rms_norm" in f:
+                if "linear" in f or "rms_norm" in f or "recurrence" in f or "rope" in f:
                     getattr(lib, f).restype = i32
         lib.tri_inv_count_matrices.argtypes = [dp, ctypes.POINTER(ctypes.c_int64)]
         lib.tri_inv_last_device_status.argtypes = [ctypes.POINTER(ctypes.c_int)]
@@ -521,6 +547,163 @@ def rms_norm_backward(dY, X, w, eps=1e-6, dH=None, stream=None):
     if rc != OK:
         raise TriInvError("tri_inv_rms_norm_backward", rc)
     return dX, dw
+
+
+def _rows(name, t, shape, dtype, inner=1):
+    """(address, values from one token's row to the next) of a tensor of this shape and type on the current CUDA device, whose last ``inner`` dimensions are contiguous and whose tokens, the
+    dimensions before them, lie at one distance: a slice of a projection's output, for instance."""
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError("%s must be on the current CUDA device" % name)
+    width = 1
+    for n, st in zip(reversed(t.shape[-inner:]), reversed(t.stride()[-inner:])):
+        if n != 1 and st != width and t.numel():
+            raise ValueError("%s must be contiguous within a token" % name)
+        width *= n
+    ld, tokens = None, 1
+    for n, st in zip(reversed(t.shape[:-inner]), reversed(t.stride()[:-inner])):
+        if n != 1 and t.numel():
+            if ld is None:
+                ld = st
+            elif st != ld * tokens:
+                raise ValueError("%s must have its tokens at one distance from each other" % name)
+            tokens *= n
+    return t.data_ptr(), max(width, 1) if ld is None else ld
+
+
+def _rec_desc(X, mode, cu_seqlens):
+    if X.dim() != 3:
+        raise ValueError("X must be [B, T, D], got %s" % (tuple(X.shape),))
+    keep, ptr, n_seqs = None, None, 0
+    if cu_seqlens is not None:
+        keep = np.ascontiguousarray(np.asarray(cu_seqlens), dtype=np.int32)
+        ptr, n_seqs = keep.ctypes.data, len(keep) - 1
+    B, T, D = X.shape
+    return RecDesc(B, T, D, _dtype_code(X), int(mode), n_seqs, ptr), keep, (B if keep is None else n_seqs, D)
+
+
+def gated_recurrence_carries(X, cu_seqlens=None) -> int:
+    """Rows of the carried states that ``gated_recurrence`` keeps for its gradient."""
+    desc, keep, _ = _rec_desc(X, REC_DECAY, cu_seqlens)
+    rows = ctypes.c_int64(0)
+    rc = load().tri_inv_gated_recurrence_carries(desc, rows)
+    if rc != OK:
+        raise TriInvError("tri_inv_gated_recurrence_carries", rc)
+    return rows.value
+
+
+def gated_recurrence(X, G, mode=REC_DECAY, h0=None, cu_seqlens=None, out=None, want_state=True, state_out=None, want_carries=False, stream=None):
+    """The gated linear recurrence h_t = a_t h_{t-1} + u_t of every channel -> (Y, h_final or None, carries or None).  X, G, Y [B,T,D] (slices of one projection's output need no
+    copy); h0, h_final [sequences,D] fp32 (``state_out`` may be h0 itself).  ``mode``: REC_DECAY a = exp(G), u = X; REC_NORMED a = exp(G), u = sqrt(1 - a^2) X;
+    REC_GATE a = sigmoid(G), u = (1 - a) X.  ``want_carries``: the states that ``gated_recurrence_backward`` takes to save a walk.  ``out`` may be X or G itself."""
+    desc, keep, st = _rec_desc(X, mode, cu_seqlens)
+    dt, f32 = X.dtype, torch.float32
+    x, g, s0 = _rows("X", X, X.shape, dt), _rows("G", G, X.shape, dt), _optional("h0", h0, st, f32)
+    rows = gated_recurrence_carries(X, cu_seqlens) if want_carries else 0
+    need = _workspace("tri_inv_gated_recurrence_workspace", desc)
+    (Y, S, carries), work = _made_for(stream, lambda: (torch.empty(X.shape, dtype=dt, device=X.device) if out is None else None,
+                                                       torch.empty(st, dtype=f32, device=X.device) if state_out is None and want_state else None,
+                                                       torch.empty((rows, st[1]), dtype=f32, device=X.device) if want_carries else None), need)
+    Y, S = Y if out is None else out, S if state_out is None else state_out
+    rc = load().tri_inv_gated_recurrence(*x, *g, s0, *_rows("out", Y, X.shape, dt), _optional("state_out", S, st, f32), _p(carries), _p(work), need, desc, _stream(stream))
+    if rc != OK:
+        raise TriInvError("tri_inv_gated_recurrence", rc)
+    return Y, S, carries
+
+
+def selftest_recurrence_wait_timeout(X, G, wait_limit_ns, out, mode=REC_DECAY):
+    """tri_inv_selftest_recurrence_wait_timeout: the recurrence with short wait limits and the first tile of the first channels never announced.  ``out`` = Y."""
+    desc, keep, _ = _rec_desc(X, mode, None)
+    need = _workspace("tri_inv_gated_recurrence_workspace", desc)
+    work = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    rc = load().tri_inv_selftest_recurrence_wait_timeout(_p(X), _p(G), _p(out), _p(work), need, desc, ctypes.c_uint64(int(wait_limit_ns)), _stream(None))
+    if rc != OK:
+        raise TriInvError("tri_inv_selftest_recurrence_wait_timeout", rc)
+    return out
+
+
+def gated_recurrence_backward(dY, X, G, mode=REC_DECAY, h0=None, dh=None, carries=None, cu_seqlens=None, want_dh0=None, out=None, stream=None):
+    """The gradient of ``gated_recurrence`` -> (dX, dG, dh0 or None), from dY and, where the final state has one, dh.  ``carries``: of the forward call with the same X, G, h0 and sequences, or None: the
+    states are walked again.  ``want_dh0``: by default where h0 is given.  ``out`` = (dX, dG), which may be slices of one projection's gradient."""
+    if want_dh0 is None:
+        want_dh0 = h0 is not None
+    desc, keep, st = _rec_desc(X, mode, cu_seqlens)
+    dt, f32 = X.dtype, torch.float32
+    args = [*_rows("dY", dY, X.shape, dt), *_rows("X", X, X.shape, dt), *_rows("G", G, X.shape, dt), _optional("h0", h0, st, f32), _optional("dh", dh, st, f32),
+            None if carries is None else _operand("carries", carries, (gated_recurrence_carries(X, cu_seqlens), st[1]), f32)]
+    need = _workspace("tri_inv_gated_recurrence_backward_workspace", desc, int(carries is not None))
+    made = lambda: torch.empty(X.shape, dtype=dt, device=X.device) if out is None else None   # noqa: E731
+    (dX, dG, dh0), work = _made_for(stream, lambda: (made(), made(), torch.empty(st, dtype=f32, device=X.device) if want_dh0 else None), need)
+    dX, dG = (dX, dG) if out is None else out
+    rc = load().tri_inv_gated_recurrence_backward(*args, *_rows("dX", dX, X.shape, dt), *_rows("dG", dG, X.shape, dt), _p(dh0), _p(work), need, desc, _stream(stream))
+    if rc != OK:
+        raise TriInvError("tri_inv_gated_recurrence_backward", rc)
+    return dX, dG, dh0
+
+
+def gated_recurrence_step(X, G, h, mode=REC_DECAY, slots=None, out=None, stream=None):
+    """One token for each row, on states that lie in the slots of a cache and are updated in place -> Y [B,D].  X, G [B,D], h [n_slots,D] fp32, slots [B] int32 (negative: a padded
+    row, output zero) or None: row b has slot b.  Slots that do not differ, or lie past the cache, are left out and show in ``last_device_status``.  ``out`` may be X or G itself."""
+    if X.dim() != 2 or h.dim() != 2:
+        raise ValueError("X must be [B, D] and h [slots, D], got %s and %s" % (tuple(X.shape), tuple(h.shape)))
+    B, D = X.shape
+    dt = X.dtype
+    Y = _made_for(stream, lambda: (torch.empty((B, D), dtype=dt, device=X.device),))[0][0] if out is None else out
+    if B == 0:
+        return Y
+    rc = load().tri_inv_gated_recurrence_step(*_rows("X", X, (B, D), dt), *_rows("G", G, (B, D), dt), _operand("h", h, (h.shape[0], D), torch.float32),
+                                              _optional("slots", slots, (B,), torch.int32), h.shape[0], *_rows("out", Y, (B, D), dt),
+                                              RecDesc(B, 1, D, _dtype_code(X), int(mode), 0, None), _stream(stream))
+    if rc != OK:
+        raise TriInvError("tri_inv_gated_recurrence_step", rc)
+    return Y
+
+
+def _heads_call(Q, K, inv_freq, positions, eps, interleaved, wq, wk):
+    if Q.dim() < 3 or (K is not None and (K.dim() != Q.dim() or K.shape[:-2] != Q.shape[:-2] or K.shape[-1] != Q.shape[-1])):
+        raise ValueError("Q and K must be [..., heads, d] of the same tokens and d, got %s and %s" % (tuple(Q.shape), None if K is None else tuple(K.shape)))
+    tokens, d = Q.shape[:-2], Q.shape[-1]
+    n = tokens.numel()
+    r = 0 if inv_freq is None else inv_freq.numel()
+    desc = HeadsDesc(n, max(1, tokens[-1]), Q.shape[-2], 0 if K is None else K.shape[-2], d, r, int(bool(interleaved)), _dtype_code(Q), float(eps))
+    return desc, [_optional("wq", wq, (d,), Q.dtype), None if K is None else _optional("wk", wk, (d,), Q.dtype), _optional("inv_freq", inv_freq, (r,), torch.float32),
+                  _optional("positions", positions, tokens, torch.int32)]
+
+
+def _heads_rows(name, t, like):
+    return (None, 0) if like is None else _rows(name, t, like.shape, like.dtype, 2)
+
+
+def qk_norm_rope(Q, K, wq, wk, inv_freq, positions=None, eps=1e-6, interleaved=False, out=None, stream=None):
+    """The RMS norm of each query and key head, then the rotation of the pairs of its first 2 len(inv_freq) features by the angles position x inv_freq -> (Yq, Yk).  Q [...,heads,d], K [...,key
+    heads,d] or None (slices of one projection's output need no copy), wq, wk [d] or None (ones), inv_freq [r] fp32 or None (no rotation), positions int32, one for each token (negative: a padded
+    token, outputs zero) or None: a token's index along the dimension in front of the heads.  Pairs are (i, i + r), or (2 i, 2 i + 1) if ``interleaved``.  ``out`` = (Yq, Yk), which may be Q and K."""
+    desc, small = _heads_call(Q, K, inv_freq, positions, eps, interleaved, wq, wk)
+    q, k = _heads_rows("Q", Q, Q), _heads_rows("K", K, K)
+    (Yq, Yk), _ = _made_for(stream, lambda: (torch.empty(Q.shape, dtype=Q.dtype, device=Q.device), None if K is None else torch.empty(K.shape, dtype=K.dtype, device=K.device))) if out is None else (out, None)
+    rc = load().tri_inv_qk_norm_rope(*q, *k, *small, *_heads_rows("out[0]", Yq, Q), *_heads_rows("out[1]", Yk, K), desc, _stream(stream))
+    if rc != OK:
+        raise TriInvError("tri_inv_qk_norm_rope", rc)
+    return Yq, Yk
+
+
+def qk_norm_rope_backward(dYq, dYk, Q, K, wq, wk, inv_freq, positions=None, eps=1e-6, interleaved=False, out=None, stream=None):
+    """The gradient of ``qk_norm_rope`` -> (dQ, dK, dwq, dwk), from those of its outputs and its other arguments as they were; None for what was None.  ``out`` = (dQ, dK), which
+    may be slices of one projection's gradient, or dYq and dYk, or Q and K."""
+    desc, small = _heads_call(Q, K, inv_freq, positions, eps, interleaved, wq, wk)
+    rows = [*_heads_rows("dYq", dYq, Q), *_heads_rows("dYk", dYk, K), *_heads_rows("Q", Q, Q), *_heads_rows("K", K, K)]
+    need = _workspace("tri_inv_qk_norm_rope_backward_workspace", desc)
+    (dwq, dwk, dQ, dK), work = _made_for(stream, lambda: (None if wq is None else torch.empty_like(wq), None if wk is None or K is None else torch.empty_like(wk),
+                                                          torch.empty(Q.shape, dtype=Q.dtype, device=Q.device) if out is None else None,
+                                                          torch.empty(K.shape, dtype=K.dtype, device=K.device) if out is None and K is not None else None), need)
+    dQ, dK = (dQ, dK) if out is None else out
+    rc = load().tri_inv_qk_norm_rope_backward(*rows, *small, *_heads_rows("dQ", dQ, Q), *_heads_rows("dK", dK, K), _p(dwq), _p(dwk), _p(work), need, desc, _stream(stream))
+    if rc != OK:
+        raise TriInvError("tri_inv_qk_norm_rope_backward", rc)
+    return dQ, dK, dwq, dwk
 
 
 def wy(A, K, V, beta, cu_seqlens=None, out=None, stream=None):

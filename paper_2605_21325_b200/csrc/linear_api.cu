@@ -2,23 +2,13 @@
 #include <algorithm>
 #include <cmath>
 
+#include "call_checks.cuh"
 #include "linear_attention.cuh"
 #include "rms_norm.cuh"
 
 namespace tri_inv {
 namespace {
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-template <class... P>
-bool all_aligned(P... p) { return (aligned16(p) && ...); }
-// A buffer of a call, and whether one that is written meets another (one that is absent or empty meets nothing)
-struct Span { const void* p; __int128 bytes; };   // (a descriptor's products may pass 64 bits)
-bool meets(Span a, Span b) {
-  const __int128 x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-  return a.p && b.p && a.bytes > 0 && b.bytes > 0 && x < y + b.bytes && y < x + a.bytes;
-}
-template <class... S>
-bool meets_any(Span a, S... b) { return (meets(a, b) || ...); }
 long long tokens_of(const tri_inv_desc* d) { return d->cu_seqlens ? (long long)d->T : (long long)d->T * d->B; }
 // whether the tensor-core kernel takes the call (without a token there is nothing for it to map)
 bool on_tensor_cores(const tri_inv_desc* d) { return tokens_of(d) > 0 && linear_tc_fits(d->d_k, d->d_v, d->kv_dtype); }
@@ -176,10 +166,6 @@ int check_norm(int64_t rows, int32_t n, float eps, int dtype) {
   if (dtype != TRI_INV_F32 && dtype != TRI_INV_BF16) return TRI_INV_ERR_INVALID_ARG;
   return n > 0x7fffff00 ? TRI_INV_ERR_UNSUPPORTED : TRI_INV_OK;   // columns are counted in 32 bits, and by 256 past the last
 }
-// whether pointers to values of the storage type are aligned to that type
-template <class... P>
-bool on_type(int dtype, P... p) { return (((reinterpret_cast<uintptr_t>(p) & (dtype == TRI_INV_F32 ? 3u : 1u)) == 0) && ...); }
-
 }  // namespace
 }  // namespace tri_inv
 
