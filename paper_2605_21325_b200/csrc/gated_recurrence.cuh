@@ -8,7 +8,7 @@
 //     e_t = dy_t + c_{t+1},   c_t = a_t e_t,   dx_t = m_t e_t (m: what multiplies x in u),   dh0 = c_0,
 //     dg_t = e_t w_t,   w_t = a_t h_{t-1} (decay),   a_t h_{t-1} - a_t^2 / m_t x_t (normed),   (h_{t-1} - x_t) a_t (1 - a_t) (gate)
 //
-// Both are walks over tiles of kRecTile tokens of kRecRow bytes of channels.  A tile is an affine map of what enters it, (P, H): h -> P h + H,
+// Both are walks over tiles of kRecTile tokens of kRecChannels channels.  A tile is an affine map of what enters it, (P, H): h -> P h + H,
 // and so is a run of tiles; the tokens of a warp, the warps of a tile and the tiles of a sequence join by the same rule.
 #pragma once
 #include "common.cuh"
@@ -16,7 +16,7 @@
 namespace tri_inv {
 
 constexpr int kRecTile = 64;      // tokens of a tile
-constexpr int kRecRow = 128;      // bytes of its channels: 64 in bf16, 32 in fp32
+constexpr int kRecChannels = 64;  // and its channels
 
 // An entry of the table of packed sequences: a tile, or a whole sequence (index 0)
 struct RecTile {
@@ -69,87 +69,124 @@ cudaError_t launch_gated_recurrence_step(const RecStepArgs& a, int dtype, cudaSt
 
 enum : int { kRecDecay = TRI_INV_REC_DECAY, kRecNormed = TRI_INV_REC_NORMED, kRecGate = TRI_INV_REC_GATE };
 
-// A channel pair (bf16) or a channel (fp32) of a lane
+// Two fp32 numbers, a lane's two channels, that the arithmetic takes at a time
+struct Pair { unsigned long long v; };
+__device__ __forceinline__ Pair pair(float x, float y) { Pair d; asm("mov.b64 %0, {%1, %2};" : "=l"(d.v) : "f"(x), "f"(y)); return d; }
+__device__ __forceinline__ float2 both(Pair a) { float2 d; asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(a.v)); return d; }
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) { Pair d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v)); return d; }
+__device__ __forceinline__ Pair add2(Pair a, Pair b) { Pair d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v)); return d; }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return d; }
+__device__ __forceinline__ Pair twice(float x) { return pair(x, x); }
+
+// A lane's two channels as they lie in a row
 template <class T> struct RecLane;
 template <> struct RecLane<__nv_bfloat16> {
-  static constexpr int N = 2;
-  static __device__ __forceinline__ void widen(float (&v)[2], uint32_t raw) { v[0] = __uint_as_float(raw << 16); v[1] = __uint_as_float(raw & 0xffff0000u); }
-  static __device__ __forceinline__ uint32_t pack(const float (&v)[2]) {
-    const __nv_bfloat162 p = __floats2bfloat162_rn(v[0], v[1]);
+  using Raw = uint32_t;
+  static __device__ __forceinline__ Pair widen(Raw r) { return pair(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u)); }
+  static __device__ __forceinline__ Raw pack(Pair v) {
+    const float2 f = both(v);
+    const __nv_bfloat162 p = __floats2bfloat162_rn(f.x, f.y);
     return reinterpret_cast<const uint32_t&>(p);
   }
 };
 template <> struct RecLane<float> {
-  static constexpr int N = 1;
-  static __device__ __forceinline__ void widen(float (&v)[1], uint32_t raw) { v[0] = __uint_as_float(raw); }
-  static __device__ __forceinline__ uint32_t pack(const float (&v)[1]) { return __float_as_uint(v[0]); }
+  using Raw = uint2;
+  static __device__ __forceinline__ Pair widen(Raw r) { return pair(__uint_as_float(r.x), __uint_as_float(r.y)); }
+  static __device__ __forceinline__ Raw pack(Pair v) {
+    const float2 f = both(v);
+    return make_uint2(__float_as_uint(f.x), __float_as_uint(f.y));
+  }
 };
 
-// 1 - e^g for g in [-1/4, 0], from the series of (e^g - 1) / g to the seventh power: the first term left out is 1/8! g^7 < 2^-29 of the sum
-__device__ __forceinline__ float rec_fall(float g) {
-  float s = 1.f / 5040.f;
-  s = fmaf(s, g, 1.f / 720.f);
-  s = fmaf(s, g, 1.f / 120.f);
-  s = fmaf(s, g, 1.f / 24.f);
-  s = fmaf(s, g, 1.f / 6.f);
-  s = fmaf(s, g, 0.5f);
-  s = fmaf(s, g, 1.f);
-  return -g * s;
+// (1 - e^g) / -g from its series up to the seventh power: for |g| <= 1/4 the first term left out is g^7 / 8! < 2^-29
+__device__ __forceinline__ Pair rec_slope(Pair g) {
+  Pair s = twice(1.f / 5040.f);
+  s = fma2(s, g, twice(1.f / 720.f));
+  s = fma2(s, g, twice(1.f / 120.f));
+  s = fma2(s, g, twice(1.f / 24.f));
+  s = fma2(s, g, twice(1.f / 6.f));
+  s = fma2(s, g, twice(0.5f));
+  return fma2(s, g, twice(1.f));
+}
+__device__ __forceinline__ float rec_reciprocal(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float rec_over_root(float x) { float y; asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// a and m (what multiplies x).  Near 1, a is formed as 1 minus what it lacks, so that its error is a rounding's and has no preferred side: a state sums a's errors over as many tokens as
+// it remembers.
+template <int MODE>
+__device__ __forceinline__ void rec_factors(Pair gp, Pair& a, Pair& m) {
+  const float2 g = both(gp);
+  if constexpr (MODE == kRecDecay) {
+    a = pair(expf(g.x), expf(g.y));
+    m = twice(1.f);
+  } else if constexpr (MODE == kRecNormed) {
+    const float2 e = make_float2(expf(g.x), expf(g.y));
+    const bool nx = fabsf(g.x) <= 0.25f, ny = fabsf(g.y) <= 0.25f;
+    const Pair minus = twice(-1.f), one = twice(1.f);
+    const Pair qn = mul2(mul2(gp, minus), rec_slope(gp)), qf = fma2(pair(e.x, e.y), minus, one);   // 1 - a
+    const float2 n = both(qn), f = both(qf), an = both(fma2(qn, minus, one));
+    a = pair(nx ? an.x : e.x, ny ? an.y : e.y);
+    const Pair q = pair(nx ? n.x : f.x, ny ? n.y : f.y), sp = mul2(q, add2(a, one));   // 1 - a^2
+    const float2 s = both(sp);
+    m = mul2(sp, pair(s.x >= 1.17549435e-38f ? rec_over_root(s.x) : 0.f, s.y >= 1.17549435e-38f ? rec_over_root(s.y) : 0.f));
+  } else {
+    const float2 e = make_float2(expf(-fabsf(g.x)), expf(-fabsf(g.y)));
+    const Pair ep = pair(e.x, e.y), one = twice(1.f);
+    const float2 d = both(add2(ep, one));
+    const Pair rp = pair(rec_reciprocal(d.x), rec_reciprocal(d.y)), sp = mul2(ep, rp), bp = fma2(sp, twice(-1.f), one);   // s: the smaller of a and 1 - a
+    const float2 r = both(rp), s = both(sp), b = both(bp);
+    a = pair(g.x >= 0.f ? b.x : s.x, g.y >= 0.f ? b.y : s.y);
+    m = pair(g.x >= 0.f ? s.x : r.x, g.y >= 0.f ? s.y : r.y);
+  }
 }
 
-// a, m (what multiplies x) and, for the gradient of the normed form, 1 / m.  Near 1, a is formed as 1 minus what it lacks, so that its error is a rounding's and has no
-// preferred side: a state sums a's errors over as many tokens as it remembers.
 template <int MODE>
-__device__ __forceinline__ void rec_factors(float g, float& a, float& m, float& over_m) {
-  if constexpr (MODE == kRecDecay) {
-    a = expf(g);
-    m = 1.f;
-    over_m = 1.f;
-  } else if constexpr (MODE == kRecNormed) {
-    const float e = expf(g);
-    const bool near = g > -0.25f && g <= 0.f;
-    const float q = near ? rec_fall(g) : 1.f - e;
-    a = near ? 1.f - q : e;
-    const float s = q * (1.f + a);
-    over_m = s > 0.f ? rsqrtf(s) : s <= 0.f ? 0.f : s;   // (a NaN stays one)
-    m = s * over_m;
-  } else {
-    const float e = expf(-fabsf(g)), r = __fdividef(1.f, 1.f + e), s = e * r;   // s: the smaller of a and 1 - a
-    a = g >= 0.f ? 1.f - s : s;
-    m = g >= 0.f ? s : r;
-    if (g != g) a = m = g;
-    over_m = 1.f;
-  }
+__device__ __forceinline__ Pair rec_input(Pair m, Pair x) {   // u
+  if constexpr (MODE == kRecDecay) return x;
+  else return mul2(m, x);
 }
 
 // One token, or one map behind another.  Where a is zero nothing of what came before is left, not even what is not finite.
 __device__ __forceinline__ float rec_step(float a, float h, float u) { return a == 0.f ? u : fmaf(a, h, u); }
+__device__ __forceinline__ Pair rec_step(Pair a, Pair h, Pair u) {
+  const float2 x = both(a), y = both(h), z = both(u);
+  return pair(rec_step(x.x, y.x, z.x), rec_step(x.y, y.y, z.y));
+}
+__device__ __forceinline__ bool any_zero(Pair a) { const float2 x = both(a); return x.x == 0.f || x.y == 0.f; }
 
-// 4 bytes of a row at channel c: what lies past `width` channels reads as zero.  pairs: 4-byte accesses are aligned.
+// How a tensor's rows are moved: 16 bytes (everything aligned to them), 4 bytes, or value by value (bf16 at odd places)
+enum : int { kRecWide = 0, kRecFours = 1, kRecSingle = 2 };
 template <class T>
-__device__ __forceinline__ uint32_t rec_load(const T* row, int c, int width, bool pairs) {
+__device__ __forceinline__ int rec_access(const void* p, long long ld) {
+  const unsigned long long at = reinterpret_cast<unsigned long long>(p) | (unsigned long long)ld * sizeof(T);
+  return (at & 15) == 0 ? kRecWide : (at & 3) == 0 ? kRecFours : kRecSingle;
+}
+
+// A lane's channels c, c + 1 of a row of `width`: those past the last read as zero and are not written.
+template <class T>
+__device__ __forceinline__ typename RecLane<T>::Raw rec_load(const T* row, int c, int width, int access) {
   if constexpr (sizeof(T) == 4) {
-    return c < width ? __float_as_uint(row[c]) : 0u;
+    if (access == kRecWide && c + 1 < width) return *reinterpret_cast<const uint2*>(row + c);
+    return make_uint2(c < width ? __float_as_uint(row[c]) : 0u, c + 1 < width ? __float_as_uint(row[c + 1]) : 0u);
   } else {
-    if (pairs && c + 1 < width) return *reinterpret_cast<const uint32_t*>(row + c);
+    if (access != kRecSingle && c + 1 < width) return *reinterpret_cast<const uint32_t*>(row + c);
     const uint16_t* p = reinterpret_cast<const uint16_t*>(row);
     const uint32_t lo = c < width ? p[c] : 0u, hi = c + 1 < width ? p[c + 1] : 0u;
     return lo | hi << 16;
   }
 }
 template <class T>
-__device__ __forceinline__ void rec_store(T* row, int c, int width, bool pairs, const float (&v)[RecLane<T>::N]) {
+__device__ __forceinline__ void rec_store(T* row, int c, int width, int access, Pair v) {
+  const typename RecLane<T>::Raw raw = RecLane<T>::pack(v);
   if constexpr (sizeof(T) == 4) {
-    if (c < width) row[c] = v[0];
+    if (access == kRecWide && c + 1 < width) { *reinterpret_cast<uint2*>(row + c) = raw; return; }
+    if (c < width) row[c] = __uint_as_float(raw.x);
+    if (c + 1 < width) row[c + 1] = __uint_as_float(raw.y);
   } else {
-    const uint32_t raw = RecLane<T>::pack(v);
-    if (pairs && c + 1 < width) {
-      *reinterpret_cast<uint32_t*>(row + c) = raw;
-    } else {
-      uint16_t* p = reinterpret_cast<uint16_t*>(row);
-      if (c < width) p[c] = (uint16_t)raw;
-      if (c + 1 < width) p[c + 1] = (uint16_t)(raw >> 16);
-    }
+    if (access != kRecSingle && c + 1 < width) { *reinterpret_cast<uint32_t*>(row + c) = raw; return; }
+    uint16_t* p = reinterpret_cast<uint16_t*>(row);
+    if (c < width) p[c] = (uint16_t)raw;
+    if (c + 1 < width) p[c + 1] = (uint16_t)(raw >> 16);
   }
 }
 
@@ -163,41 +200,43 @@ __device__ __forceinline__ void rec_commit() { asm volatile("cp.async.commit_gro
 template <int N>
 __device__ __forceinline__ void rec_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// How a tensor's rows are moved: 16 bytes (everything aligned to them), 4 bytes, or value by value (bf16 at odd places)
-enum : int { kRecWide = 0, kRecPairs = 1, kRecSingle = 2 };
-template <class T>
-__device__ __forceinline__ int rec_access(const void* p, long long ld) {
-  const unsigned long long at = reinterpret_cast<unsigned long long>(p) | (unsigned long long)ld * sizeof(T);
-  return (at & 15) == 0 ? kRecWide : (at & 3) == 0 ? kRecPairs : kRecSingle;
-}
-
-// Asks for a warp's ROWS rows of a tile: rows row0 .. of which `rows` exist, columns c0 .. of `width`; smem: the warp's rows of kRecRow bytes.
+// Asks for a warp's ROWS rows of a tile: rows row0 .. of which `rows` exist, channels c0 .. of `width`; what does not exist reads as zero.
 template <class T, int ROWS>
 __device__ __forceinline__ void rec_request(unsigned char* smem, const T* base, long long ld, long long row0, int rows, int c0, int width, int access) {
+  constexpr int BYTES = kRecChannels * (int)sizeof(T), LANES = BYTES / 16, AT_ONCE = 32 / LANES;   // of a row; lanes of 16 bytes; rows
+  static_assert(ROWS % AT_ONCE == 0, "");
   const int lane = threadIdx.x & 31;
-  const int left = (width - c0) * (int)sizeof(T);   // bytes of a row from the tile's first column on
+  const int left = (width - c0) * (int)sizeof(T);   // bytes of a row from the tile's first channel on
   const uint32_t to = (uint32_t)__cvta_generic_to_shared(smem);
   if (access == kRecWide) {
+    const int r0 = lane / LANES, at = 16 * (lane % LANES), bytes = min(16, left - at);
+    const T* from = base + (row0 + r0) * ld + c0 + at / (int)sizeof(T);
+    const uint32_t there = to + r0 * BYTES + at;
+    if (rows >= ROWS && left >= BYTES) {
 #pragma unroll
-    for (int i = 0; i < (ROWS + 3) / 4; ++i) {
-      const int r = 4 * i + (lane >> 3), at = 16 * (lane & 7);
-      const int bytes = r < rows && r < ROWS ? min(16, max(0, left - at)) : 0;
-      const T* from = bytes ? base + (row0 + r) * ld + c0 + at / (int)sizeof(T) : base;
-      if (ROWS % 4 == 0 || r < ROWS) rec_copy(to + r * kRecRow + at, from, bytes);
-    }
-  } else if (access == kRecPairs && (sizeof(T) == 4 || (left & 3) == 0 || left >= kRecRow)) {
+      for (int i = 0; i < ROWS / AT_ONCE; ++i) rec_copy(there + i * AT_ONCE * BYTES, from + i * AT_ONCE * ld, 16);
+    } else {
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      const int bytes = r < rows && 4 * lane < left ? 4 : 0;
-      const T* from = bytes ? base + (row0 + r) * ld + c0 + 4 * lane / (int)sizeof(T) : base;
-      rec_copy4(to + r * kRecRow + 4 * lane, from, bytes);
+      for (int i = 0; i < ROWS / AT_ONCE; ++i) {
+        const bool in = r0 + i * AT_ONCE < rows && bytes > 0;
+        rec_copy(there + i * AT_ONCE * BYTES, in ? from + i * AT_ONCE * ld : base, in ? bytes : 0);
+      }
     }
+  } else if (access == kRecFours && (left % 4 == 0 || left >= BYTES)) {
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+      for (int i = 0; i < BYTES / 128; ++i) {
+        const int at = 128 * i + 4 * lane;
+        const bool in = r < rows && at < left;
+        rec_copy4(to + r * BYTES + at, in ? base + (row0 + r) * ld + c0 + at / (int)sizeof(T) : base, in ? 4 : 0);
+      }
   } else {
-    uint32_t raw[ROWS];
+    typename RecLane<T>::Raw raw[ROWS];
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) raw[r] = r < rows ? rec_load(base + (row0 + r) * ld, c0 + 4 * lane / (int)sizeof(T), width, access != kRecSingle) : 0u;
+    for (int r = 0; r < ROWS; ++r) raw[r] = r < rows ? rec_load(base + (row0 + r) * ld, c0 + 2 * lane, width, access) : typename RecLane<T>::Raw{};
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) *reinterpret_cast<uint32_t*>(smem + r * kRecRow + 4 * lane) = raw[r];
+    for (int r = 0; r < ROWS; ++r) *reinterpret_cast<typename RecLane<T>::Raw*>(smem + r * BYTES + 2 * lane * (int)sizeof(T)) = raw[r];
   }
 }
 
@@ -219,15 +258,14 @@ __device__ __forceinline__ unsigned long long rec_now() {
 }
 
 // What enters a tile, from the words of the `count` tiles in front of it in its sequence (words of one channel, `step` from one to the one before): their maps join
-// from the nearest on until one forgets what came before (P = 0; a tile that knows what leaves it says so with P = 0, the first one always does).  A word
-// that is missing for the time limit raises the status word, and the NaN that is returned then goes on with this tile's own word, so that no later tile waits as long.
+// from the nearest on until one forgets what came before (P = 0; a tile that knows what leaves it says so with P = 0, the first one always does).
+// A word that is missing for the time limit raises the status word, and the NaN that is returned then goes on with this tile's own word, so that no later tile waits as long.
 __device__ __forceinline__ float rec_look_back(const unsigned long long* word, long long step, int count, unsigned long long limit, int* status) {
-  constexpr int AT_ONCE = 4;
+  constexpr int AT_ONCE = 8;   // words that are asked for together
   constexpr unsigned long long NONE = ~0ull;
   float P = 1.f, H = 0.f;
   unsigned long long begin = 0;
-  unsigned int polls = 0;
-  while (count > 0) {
+  for (unsigned int polls = 1;; ++polls) {
     unsigned long long v[AT_ONCE];
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) v[i] = i < count ? rec_peek(word - i * step) : NONE;
@@ -245,7 +283,8 @@ __device__ __forceinline__ float rec_look_back(const unsigned long long* word, l
     }
     word -= got * step;
     count -= got;
-    if (got == 0 && (++polls & 127) == 0) {
+    if (count <= 0) return H;
+    if (got == 0 && (polls & 127) == 0) {
       const unsigned long long now = rec_now();
       if (begin == 0) begin = now;
       else if (now - begin > limit) {
@@ -254,8 +293,12 @@ __device__ __forceinline__ float rec_look_back(const unsigned long long* word, l
       }
     }
   }
-  return H;
 }
+
+// Where the warps of tokens and the threads of channels meet: the maps of a tile's warps are there, a tile's entry is there; tiles take two of each in turn
+enum : int { kRecMaps = 1, kRecEntry = 3 };
+__device__ __forceinline__ void rec_meet(int which, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(which), "r"(threads) : "memory"); }
+__device__ __forceinline__ void rec_arrive(int which, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(which), "r"(threads) : "memory"); }
 
 // Where a block stands: a tile of an item, which is a tile (with words) or a whole sequence
 struct RecAt {
@@ -266,37 +309,69 @@ struct RecAt {
   __device__ __forceinline__ long long tok0() const { return (long long)begin + (long long)index * kRecTile; }
   __device__ __forceinline__ int n() const { return min(kRecTile, len - index * kRecTile); }
 };
+// The tile of an item, its entry of the table at hand (packed sequences)
 template <bool WORDS>
-__device__ __forceinline__ RecAt rec_decode(const RecArgs& a, int item, bool back) {
+__device__ __forceinline__ RecAt rec_decode(const RecArgs& a, int item, const RecTile& entry, bool back) {
   RecAt t{};
   t.item = item;
   if (item >= a.n_segs * a.cols) return t;
-  const int r0 = item / a.cols, r = back && WORDS ? a.n_segs - 1 - r0 : r0;
-  t.col = item - r0 * a.cols;
+  const int r = item / a.cols;
+  t.col = item - r * a.cols;
   if (a.table) {
-    const RecTile s = a.table[r];
-    t.begin = s.tok0; t.len = s.n; t.seq = s.seq; t.index = s.index; t.tiles = s.tiles;
+    t.begin = entry.tok0; t.len = entry.n; t.seq = entry.seq; t.index = entry.index; t.tiles = entry.tiles;
   } else {
-    t.index = WORDS ? r / a.n_seqs : 0;   // the sequences' tiles in turn: the one in front of a tile is n_seqs (times the columns) items ahead of it
+    const int rank = back && WORDS ? a.n_segs - 1 - r : r;
+    t.index = WORDS ? rank / a.n_seqs : 0;   // the sequences' tiles in turn: the one in front of a tile is n_seqs (times the columns) items ahead of it
     t.tiles = max(1, (int)(((unsigned)a.T + kRecTile - 1) / kRecTile));
-    t.seq = WORDS ? r - t.index * a.n_seqs : r;
+    t.seq = WORDS ? rank - t.index * a.n_seqs : rank;
     t.begin = t.seq * a.T;
     t.len = a.T;
   }
   if (!WORDS && back) t.index = t.tiles - 1;
   return t;
 }
-// The tile after `t` in its sequence's walk (backwards: in front of it), or the first of the next item
-template <bool WORDS>
-__device__ __forceinline__ RecAt rec_next(const RecArgs& a, const RecAt& t, int drawn, bool back) {
-  if (WORDS) return rec_decode<true>(a, drawn, back);
-  if (back ? t.index > 0 : t.index + 1 < t.tiles) {
-    RecAt s = t;
-    s.index += back ? -1 : 1;
-    return s;
-  }
-  return rec_decode<false>(a, t.item + gridDim.x, back);
+__device__ __forceinline__ RecTile rec_entry(const RecArgs& a, int item, bool back) {   // of the table, for an item that may be past the last
+  if (!a.table || item >= a.n_segs * a.cols) return RecTile{};
+  const int r = item / a.cols;
+  return a.table[back ? a.n_segs - 1 - r : r];
 }
+
+// A block's tiles in order: the one that it works on, the one before (whose entry is awaited) and those that are on their way lie in a ring in shared memory, which one thread keeps ahead.
+// With words the items are drawn from the ticket, so that the tiles in front of a tile are done or in the hands of blocks that run; else they go by a fixed stride.
+constexpr int kRecRing = 8;
+template <bool WORDS>
+struct RecFeed {
+  int drawn;         // the item whose entry is asked for next
+  RecAt last;        // without words: the tile that was given last
+  RecTile entry;
+  // Ahead of the first tile: `n` tiles into the ring
+  __device__ __forceinline__ void begin(const RecArgs& a, RecAt* ring, int n, bool back) {
+    const int stride = gridDim.x;
+    int item = blockIdx.x;
+    for (int i = 0; i < n; ++i) {
+      if (WORDS) item = (int)atomicAdd(a.ticket, 1u);
+      if (!WORDS && i > 0 && more(last, back)) { ring[i] = last = after(last, back); continue; }
+      ring[i] = last = rec_decode<WORDS>(a, item, rec_entry(a, item, back), back);
+      item += stride;
+    }
+    drawn = WORDS ? (int)atomicAdd(a.ticket, 1u) : item;
+  }
+  static __device__ __forceinline__ bool more(const RecAt& t, bool back) { return back ? t.index > 0 : t.index + 1 < t.tiles; }
+  static __device__ __forceinline__ RecAt after(RecAt t, bool back) { t.index += back ? -1 : 1; return t; }
+  // Early in a round: asks for what `give` needs
+  int next_drawn, given;
+  __device__ __forceinline__ void ask(const RecArgs& a, bool back) {
+    given = drawn;
+    entry = rec_entry(a, drawn, back);
+    if (WORDS) next_drawn = (int)atomicAdd(a.ticket, 1u);
+  }
+  __device__ __forceinline__ RecAt give(const RecArgs& a, bool back) {
+    if (!WORDS && last.item < a.n_segs * a.cols && more(last, back)) return last = after(last, back);
+    last = rec_decode<WORDS>(a, given, entry, back);
+    drawn = WORDS ? next_drawn : given + (int)gridDim.x;
+    return last;
+  }
+};
 #endif
 
 }  // namespace tri_inv

@@ -6,173 +6,229 @@
 namespace tri_inv {
 namespace {
 
-constexpr int kWarps = 8, kTok = kRecTile / kWarps, kThreads = 32 * kWarps;
-constexpr int kStageBytes = 3 * kRecTile * kRecRow;
-constexpr size_t kSmem = 2 * (size_t)kStageBytes;
+constexpr int kWarps = 8, kTok = kRecTile / kWarps, kStages = 3;
+constexpr int kThreads = 32 * kWarps + kRecChannels;   // warps of tokens, and a thread for each channel that joins them
+template <class T> constexpr int kTensor = kRecTile * kRecChannels * (int)sizeof(T);   // bytes of a tile of one tensor
+
+// What a warp's tokens of a tile make of x, from what the first pass over them left: a, m
+template <int MODE> struct Held { Pair a[kTok], m[kTok]; };
+template <> struct Held<kRecDecay> { Pair a[kTok]; };
+
+// w: what multiplies e in dg, from the state in front of the token
+template <int MODE>
+__device__ __forceinline__ Pair weight(Pair a, Pair m, Pair h, Pair x) {
+  const Pair minus = twice(-1.f);
+  if constexpr (MODE == kRecDecay) {
+    return mul2(a, h);
+  } else if constexpr (MODE == kRecNormed) {
+    const float2 f = both(m);
+    const Pair over = pair(f.x > 0.f ? rec_reciprocal(f.x) : 0.f, f.y > 0.f ? rec_reciprocal(f.y) : 0.f);
+    return mul2(a, fma2(mul2(mul2(a, over), x), minus, h));
+  } else {
+    return mul2(fma2(x, minus, h), mul2(a, m));
+  }
+}
+__device__ __forceinline__ Pair none_where_zero(Pair a, Pair v) {
+  const float2 x = both(a), y = both(v);
+  return pair(x.x == 0.f ? 0.f : y.x, x.y == 0.f ? 0.f : y.y);
+}
 
 template <class T, int MODE, bool WORDS>
-__global__ void __launch_bounds__(kThreads, 3) gated_recurrence_backward_kernel(const __grid_constant__ RecArgs a) {
-  constexpr int N = RecLane<T>::N, CH = kRecRow / (int)sizeof(T);
+__global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(const __grid_constant__ RecArgs a) {
   extern __shared__ __align__(128) unsigned char stages[];
-  __shared__ __align__(16) float2 part[kWarps][CH];   // (P, H) of each warp's tokens
-  __shared__ __align__(8) float back[kWarps][CH];     // what reaches the token in front of them, where nothing reaches them from behind
-  __shared__ __align__(8) float entry[CH];            // what reaches the tile from behind
-  __shared__ int drawn;
+  __shared__ __align__(16) float2 part[2][kWarps][kRecChannels];   // (P, H) of each warp's tokens; then (P, C) of all tokens of the tile behind them
+  __shared__ __align__(8) float side[2][kWarps][kRecChannels];     // C: what each warp's tokens pass on, where nothing reaches them from behind; then the state in front of them
+  __shared__ __align__(8) float entry[2][kRecChannels];            // what reaches a tile from behind
+  __shared__ RecAt ring[kRecRing];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const T *X = (const T*)a.x, *G = (const T*)a.g, *DY = (const T*)a.dy;
   const int items = a.n_segs * a.cols;
-  const int x_access = rec_access<T>(X, a.ld_x), g_access = rec_access<T>(G, a.ld_g), dy_access = rec_access<T>(DY, a.ld_dy);
-  const bool dx_pairs = rec_access<T>(a.dx, a.ld_dx) != kRecSingle, dg_pairs = rec_access<T>(a.dg, a.ld_dg) != kRecSingle;
-  const unsigned long long limit = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
+  RecFeed<WORDS> feed;
   wait_for_predecessor();
+  if (tid == 32 * kWarps) feed.begin(a, ring, 4, true);
+  __syncthreads();
 
+  if (warp >= kWarps) {   // a channel
+    const int ch = tid - 32 * kWarps;
+    const unsigned long long limit = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
+    float carried = 0.f;
+    for (int i = 0;; ++i) {
+      const RecAt t = ring[i & (kRecRing - 1)];
+      if (t.item >= items) break;
+      if (ch == 0) feed.ask(a, true);
+      const int c = t.col * kRecChannels + ch;
+      const bool in = c < a.D, first = t.index == 0, last = t.index + 1 == t.tiles;
+      const long long at = (rec_slot(t.begin, t.seq) + t.index) * a.D + c, state = (long long)t.seq * a.D + c;
+      float h = !in ? 0.f : !first ? a.carries[at - a.D] : a.h0 ? a.h0[state] : 0.f;   // the state in front of the tile
+      float e = last && in && a.dh ? a.dh[state] : 0.f;
+      rec_meet(kRecMaps + (i & 1), kThreads);
+      float P = 1.f, C = 0.f, kept[kWarps];
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float2 q = part[i & 1][w][ch];
+        kept[w] = h;
+        h = rec_step(q.x, h, q.y);
+      }
+#pragma unroll
+      for (int w = kWarps - 1; w >= 0; --w) {
+        const float p = part[i & 1][w][ch].x, c_own = side[i & 1][w][ch];
+        part[i & 1][w][ch] = make_float2(P, C);
+        side[i & 1][w][ch] = kept[w];
+        P *= p;
+        C = rec_step(p, C, c_own);
+      }
+      if (in) {
+        if (WORDS && !last) {
+          if (!first) rec_post(a.words + at, P, C);
+          e = rec_look_back(a.words + at + a.D, -(long long)a.D, t.tiles - 1 - t.index, limit, a.status);
+        } else if (!last) {
+          e = carried;
+        }
+        carried = rec_step(P, e, C);
+        if (first) {
+          if (a.dh0) a.dh0[state] = carried;
+        } else if (WORDS) {
+          rec_post(a.words + at, 0.f, carried);
+        }
+      }
+      entry[i & 1][ch] = e;
+      if (ch == 0) ring[(i + 4) & (kRecRing - 1)] = feed.give(a, true);
+      rec_arrive(kRecEntry + (i & 1), kThreads);
+    }
+    return;
+  }
+
+  using Lane = RecLane<T>;
+  using Raw = typename Lane::Raw;
+  constexpr int ROW = kRecChannels * (int)sizeof(T);
+  const T *X = (const T*)a.x, *G = (const T*)a.g, *DY = (const T*)a.dy;
+  const int x_access = rec_access<T>(X, a.ld_x), g_access = rec_access<T>(G, a.ld_g), dy_access = rec_access<T>(DY, a.ld_dy);
+  const int dx_access = rec_access<T>(a.dx, a.ld_dx), dg_access = rec_access<T>(a.dg, a.ld_dg), plain = sizeof(T) == 4 ? kRecWide : kRecFours;   // whole lanes can be written
   auto request = [&](const RecAt& t, int stage) {
     if (t.item < items) {
-      const int first = warp * kTok, rows = t.n() - first;
-      unsigned char* at = stages + stage * kStageBytes + first * kRecRow;
-      rec_request<T, kTok>(at, X, a.ld_x, t.tok0() + first, rows, t.col * CH, a.D, x_access);
-      rec_request<T, kTok>(at + kRecTile * kRecRow, G, a.ld_g, t.tok0() + first, rows, t.col * CH, a.D, g_access);
-      rec_request<T, kTok>(at + 2 * kRecTile * kRecRow, DY, a.ld_dy, t.tok0() + first, rows, t.col * CH, a.D, dy_access);
+      const int first = warp * kTok, rows = t.n() - first, c0 = t.col * kRecChannels;
+      unsigned char* at = stages + stage * 3 * kTensor<T> + first * ROW;
+      rec_request<T, kTok>(at, X, a.ld_x, t.tok0() + first, rows, c0, a.D, x_access);
+      rec_request<T, kTok>(at + kTensor<T>, G, a.ld_g, t.tok0() + first, rows, c0, a.D, g_access);
+      rec_request<T, kTok>(at + 2 * kTensor<T>, DY, a.ld_dy, t.tok0() + first, rows, c0, a.D, dy_access);
     }
     rec_commit();
   };
-  int ahead = 0;
-  if (WORDS) {
-    if (tid == 0) drawn = (int)atomicAdd(a.ticket, 2u);
-    __syncthreads();
-    ahead = drawn + 1;
-  }
-  RecAt now = rec_decode<WORDS>(a, WORDS ? ahead - 1 : (int)blockIdx.x, true);
-  request(now, 0);
-  float carried = 0.f;
-  for (int stage = 0; now.item < items; stage ^= 1) {
-    const RecAt next = rec_next<WORDS>(a, now, ahead, true);
-    request(next, stage ^ 1);
-    int ticket = 0;
-    if (WORDS && tid == 0) ticket = (int)atomicAdd(a.ticket, 1u);
-    const int n = now.n(), c0 = now.col * CH, left = n - warp * kTok;
-    const long long slot = rec_slot(now.begin, now.seq) + now.index;
-    float h[N];   // the state in front of the tile
-    {
-      const float* from = now.index > 0 ? a.carries + (slot - 1) * a.D : a.h0 ? a.h0 + (long long)now.seq * a.D : nullptr;
+  request(ring[0], 0);
+  // Round i: the maps of tile i, and the output of tile i - 1, whose entry the channels' threads have found out meanwhile.  A tile's rows stay for both.
+  Held<MODE> even, odd;
+  bool resets = false;
+  int stage = 0, stage_before = 2;
+  auto round = [&](int i, Held<MODE>& now, const Held<MODE>& before) -> bool {
+    const int stage_next = 3 - stage - stage_before;
+    request(ring[(i + 1) & (kRecRing - 1)], stage_next);
+    const bool has_now = ring[i & (kRecRing - 1)].item < items;
+    const int place = warp * kTok * ROW + 2 * lane * (int)sizeof(T);
+    bool now_resets = false;
+    if (has_now) {
+      rec_wait<1>();
+      __syncwarp();
+      const unsigned char* sx = stages + stage * 3 * kTensor<T> + place;
+      auto read = [&](int tensor, int k) { return Lane::widen(*reinterpret_cast<const Raw*>(sx + tensor * kTensor<T> + k * ROW)); };
+      const int left = ring[i & (kRecRing - 1)].n() - warp * kTok;
+      Pair P = twice(1.f), H = twice(0.f), C = twice(0.f);
 #pragma unroll
-      for (int j = 0; j < N; ++j) h[j] = from && c0 + lane * N + j < a.D ? from[c0 + lane * N + j] : 0.f;
-    }
-    rec_wait<1>();
-    __syncwarp();
-    const unsigned char* sx = stages + stage * kStageBytes + warp * kTok * kRecRow + 4 * lane;
-    auto read = [&](float (&v)[N], int tensor, int t) { RecLane<T>::widen(v, *reinterpret_cast<const uint32_t*>(sx + (tensor * kRecTile + t) * kRecRow)); };
-    float av[kTok][N], mv[kTok][N], wv[kTok][N], P[N], H[N], C[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) { P[j] = 1.f; H[j] = 0.f; C[j] = 0.f; }
-#pragma unroll
-    for (int t = 0; t < kTok; ++t) {
-      float x[N], g[N], over;
-      read(x, 0, t);
-      read(g, 1, t);
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        rec_factors<MODE>(g[j], av[t][j], mv[t][j], over);
-        if (t >= left) { av[t][j] = 1.f; mv[t][j] = 0.f; }
-        wv[t][j] = MODE == kRecNormed ? av[t][j] * over * x[j] : x[j];   // beside the state: what w takes from it
-        P[j] *= av[t][j];
-        H[j] = rec_step(av[t][j], H[j], mv[t][j] * x[j]);
+      for (int k = 0; k < kTok; ++k) {
+        Pair m;
+        rec_factors<MODE>(read(1, k), now.a[k], m);
+        if constexpr (MODE != kRecDecay) now.m[k] = m;
       }
-    }
+      if (left < kTok) {
 #pragma unroll
-    for (int t = kTok - 1; t >= 0; --t) {
-      float dy[N];
-      read(dy, 2, t);
-#pragma unroll
-      for (int j = 0; j < N; ++j) C[j] = av[t][j] == 0.f ? 0.f : av[t][j] * (C[j] + dy[j]);
-    }
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      part[warp][lane * N + j] = make_float2(P[j], H[j]);
-      back[warp][lane * N + j] = C[j];
-    }
-    __syncthreads();
-    float q_back = 0.f;
-    if (tid < CH) {   // a channel of the tile: its word goes out first
-      float TP = 1.f, TC = 0.f;
-#pragma unroll
-      for (int w = kWarps - 1; w >= 0; --w) {
-        const float p = part[w][tid].x;
-        TP *= p;
-        TC = rec_step(p, TC, back[w][tid]);
+        for (int k = 0; k < kTok; ++k)
+          if (k >= left) {
+            now.a[k] = twice(1.f);
+            if constexpr (MODE != kRecDecay) now.m[k] = twice(0.f);
+          }
       }
-      const int c = c0 + tid;
-      const bool first = now.index == 0, last = now.index + 1 == now.tiles;
-      unsigned long long* word = WORDS ? a.words + slot * a.D + c : nullptr;
-      if (c < a.D) {
-        if (last) q_back = a.dh ? a.dh[(long long)now.seq * a.D + c] : 0.f;
-        else if (!WORDS) q_back = carried;
-        else {
-          if (!first) rec_post(word, TP, TC);
-          q_back = rec_look_back(word + a.D, -(long long)a.D, now.tiles - 1 - now.index, limit, a.status);
+      auto input = [&](int k) {
+        if constexpr (MODE == kRecDecay) return read(0, k);
+        else return mul2(now.m[k], read(0, k));
+      };
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) {
+        P = mul2(P, now.a[k]);
+        H = fma2(now.a[k], H, input(k));
+        C = mul2(now.a[kTok - 1 - k], add2(C, read(2, kTok - 1 - k)));
+      }
+      now_resets = __any_sync(0xffffffffu, any_zero(P));
+      if (now_resets) {
+        H = C = twice(0.f);
+#pragma unroll
+        for (int k = 0; k < kTok; ++k) {
+          H = rec_step(now.a[k], H, input(k));
+          C = none_where_zero(now.a[kTok - 1 - k], mul2(now.a[kTok - 1 - k], add2(C, read(2, kTok - 1 - k))));
         }
-        carried = rec_step(TP, q_back, TC);
-        if (first) { if (a.dh0) a.dh0[(long long)now.seq * a.D + c] = carried; }
-        else if (WORDS) rec_post(word, 0.f, carried);
       }
-      entry[tid] = q_back;
+      const float2 pp = both(P), hh = both(H), cc = both(C);
+      *reinterpret_cast<float4*>(&part[i & 1][warp][2 * lane]) = make_float4(pp.x, hh.x, pp.y, hh.y);
+      *reinterpret_cast<float2*>(&side[i & 1][warp][2 * lane]) = cc;
+      rec_arrive(kRecMaps + (i & 1), kThreads);
     }
-    // the state in front of the warp's tokens, and what reaches it from the warps behind it
+    if (i > 0) {
+      const unsigned char* sx = stages + stage_before * 3 * kTensor<T> + place;
+      auto read = [&](int tensor, int k) { return Lane::widen(*reinterpret_cast<const Raw*>(sx + tensor * kTensor<T> + k * ROW)); };
+      rec_meet(kRecEntry + ((i - 1) & 1), kThreads);
+      const RecAt& p = ring[(i - 1) & (kRecRing - 1)];
+      const float4 q = *reinterpret_cast<const float4*>(&part[(i - 1) & 1][warp][2 * lane]);
+      const float2 s = *reinterpret_cast<const float2*>(&side[(i - 1) & 1][warp][2 * lane]), e0 = *reinterpret_cast<const float2*>(&entry[(i - 1) & 1][2 * lane]);
+      Pair h = pair(s.x, s.y), C = rec_step(pair(q.x, q.z), pair(e0.x, e0.y), pair(q.y, q.w)), w[kTok];
+      const int left = p.n() - warp * kTok, c = p.col * kRecChannels + 2 * lane;
+      T* dx_row = (T*)a.dx + (p.tok0() + warp * kTok) * a.ld_dx;
+      T* dg_row = (T*)a.dg + (p.tok0() + warp * kTok) * a.ld_dg;
+      auto m_of = [&](int k) {
+        if constexpr (MODE == kRecDecay) return twice(1.f);
+        else return before.m[k];
+      };
+      if (left >= kTok && (p.col + 1) * kRecChannels <= a.D && dx_access <= plain && dg_access <= plain && !resets) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) { P[j] = 1.f; C[j] = 0.f; }
-    for (int w = 0; w < warp; ++w)
+        for (int k = 0; k < kTok; ++k) {
+          const Pair x = read(0, k);
+          w[k] = weight<MODE>(before.a[k], m_of(k), h, x);
+          h = fma2(before.a[k], h, rec_input<MODE>(m_of(k), x));
+        }
+        dx_row += (kTok - 1) * a.ld_dx + c;
+        dg_row += (kTok - 1) * a.ld_dg + c;
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float2 q = part[w][lane * N + j];
-        h[j] = rec_step(q.x, h[j], q.y);
-      }
-    for (int w = kWarps - 1; w > warp; --w)
+        for (int k = kTok - 1; k >= 0; --k) {
+          const Pair e = add2(C, read(2, k));
+          *reinterpret_cast<Raw*>(dx_row) = Lane::pack(rec_input<MODE>(m_of(k), e));
+          *reinterpret_cast<Raw*>(dg_row) = Lane::pack(mul2(w[k], e));
+          C = mul2(before.a[k], e);
+          dx_row -= a.ld_dx;
+          dg_row -= a.ld_dg;
+        }
+      } else {
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float p = part[w][lane * N + j].x;
-        P[j] *= p;
-        C[j] = rec_step(p, C[j], back[w][lane * N + j]);
-      }
+        for (int k = 0; k < kTok; ++k) {
+          const Pair x = read(0, k);
+          w[k] = none_where_zero(before.a[k], weight<MODE>(before.a[k], m_of(k), h, x));
+          h = rec_step(before.a[k], h, rec_input<MODE>(m_of(k), x));
+        }
 #pragma unroll
-    for (int t = 0; t < kTok; ++t) {
-      float x[N];
-      read(x, 0, t);
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float av_ = av[t][j];
-        float w;
-        if constexpr (MODE == kRecDecay) w = av_ * h[j];
-        else if constexpr (MODE == kRecNormed) w = av_ * (h[j] - wv[t][j]);
-        else w = (h[j] - x[j]) * (av_ * mv[t][j]);
-        wv[t][j] = av_ == 0.f ? 0.f : w;
-        h[j] = rec_step(av_, h[j], mv[t][j] * x[j]);
-      }
-    }
-    if (WORDS && tid == 0) drawn = ticket;
-    __syncthreads();
-    if (WORDS) ahead = drawn;
-#pragma unroll
-    for (int j = 0; j < N; ++j) C[j] = rec_step(P[j], entry[lane * N + j], C[j]);
-    T* dx_row = (T*)a.dx + (now.tok0() + warp * kTok) * a.ld_dx;
-    T* dg_row = (T*)a.dg + (now.tok0() + warp * kTok) * a.ld_dg;
-#pragma unroll
-    for (int t = kTok - 1; t >= 0; --t) {
-      float dy[N], dx[N], dg[N];
-      read(dy, 2, t);
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float e = C[j] + dy[j];
-        dx[j] = mv[t][j] * e;
-        dg[j] = wv[t][j] * e;
-        C[j] = av[t][j] == 0.f ? 0.f : av[t][j] * e;
-      }
-      if (t < left) {
-        rec_store(dx_row + t * a.ld_dx, c0 + lane * N, a.D, dx_pairs, dx);
-        rec_store(dg_row + t * a.ld_dg, c0 + lane * N, a.D, dg_pairs, dg);
+        for (int k = kTok - 1; k >= 0; --k) {
+          const Pair e = add2(C, read(2, k));
+          if (k < left) {
+            rec_store(dx_row + k * a.ld_dx, c, a.D, dx_access, rec_input<MODE>(m_of(k), e));
+            rec_store(dg_row + k * a.ld_dg, c, a.D, dg_access, mul2(w[k], e));
+          }
+          C = none_where_zero(before.a[k], mul2(before.a[k], e));
+        }
       }
     }
-    now = next;
+    resets = now_resets;
+    stage_before = stage;
+    stage = stage_next;
     __syncwarp();
+    return has_now;
+  };
+  for (int i = 0;; i += 2) {
+    if (!round(i, even, odd)) break;
+    if (!round(i + 1, odd, even)) break;
   }
   rec_wait<0>();
 }
@@ -182,9 +238,10 @@ cudaError_t launch_one(const RecArgs& a, cudaStream_t stream) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess || (e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-  if ((e = allow_shared<gated_recurrence_backward_kernel<T, MODE, WORDS>>(kSmem)) != cudaSuccess) return e;
+  constexpr size_t smem = (size_t)kStages * 3 * kTensor<T>;
+  if ((e = allow_shared<gated_recurrence_backward_kernel<T, MODE, WORDS>>(smem)) != cudaSuccess) return e;
   const long long items = (long long)a.n_segs * a.cols;
-  if ((e = launch_early(gated_recurrence_backward_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, 3ll * sms)), kThreads, kSmem, stream, a)) != cudaSuccess) return e;
+  if ((e = launch_early(gated_recurrence_backward_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, 2ll * sms)), kThreads, smem, stream, a)) != cudaSuccess) return e;
   return launched();
 }
 template <class T>

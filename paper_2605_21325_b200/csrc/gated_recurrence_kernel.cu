@@ -6,133 +6,159 @@
 namespace tri_inv {
 namespace {
 
-constexpr int kWarps = 8, kTok = kRecTile / kWarps, kThreads = 32 * kWarps;
-constexpr int kStageBytes = 2 * kRecTile * kRecRow;
-constexpr size_t kSmem = 2 * (size_t)kStageBytes;
+constexpr int kWarps = 8, kTok = kRecTile / kWarps, kStages = 3;
+constexpr int kThreads = 32 * kWarps + kRecChannels;   // warps of tokens, and a thread for each channel that joins them
+template <class T> constexpr int kTensor = kRecTile * kRecChannels * (int)sizeof(T);   // bytes of a tile of one tensor
 
 template <class T, int MODE, bool WORDS>
-__global__ void __launch_bounds__(kThreads, 4) gated_recurrence_kernel(const __grid_constant__ RecArgs a) {
-  constexpr int N = RecLane<T>::N, CH = kRecRow / (int)sizeof(T);
+__global__ void __launch_bounds__(kThreads, 2) gated_recurrence_kernel(const __grid_constant__ RecArgs a) {
   extern __shared__ __align__(128) unsigned char stages[];
-  __shared__ __align__(16) float2 part[kWarps][CH];   // (P, H) of each warp's tokens
-  __shared__ __align__(8) float entry[CH];            // what enters the tile
-  __shared__ int drawn;
+  __shared__ __align__(16) float2 part[2][kWarps][kRecChannels];   // (P, H) of each warp's tokens, then of all tokens of the tile before them
+  __shared__ __align__(8) float entry[2][kRecChannels];            // what enters a tile
+  __shared__ RecAt ring[kRecRing];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int items = a.n_segs * a.cols;
+  RecFeed<WORDS> feed;
+  wait_for_predecessor();
+  if (tid == 32 * kWarps) feed.begin(a, ring, 4, false);
+  __syncthreads();
+
+  if (warp >= kWarps) {   // a channel
+    const int ch = tid - 32 * kWarps;
+    const unsigned long long limit = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
+    float carried = 0.f;   // without words: what leaves the tile before
+    for (int i = 0;; ++i) {
+      const RecAt t = ring[i & (kRecRing - 1)];
+      if (t.item >= items) break;
+      if (ch == 0) feed.ask(a, false);
+      const int c = t.col * kRecChannels + ch;
+      const bool in = c < a.D, first = t.index == 0, last = t.index + 1 == t.tiles;
+      float h = first && in && a.h0 ? a.h0[(long long)t.seq * a.D + c] : 0.f;
+      rec_meet(kRecMaps + (i & 1), kThreads);
+      float P = 1.f, H = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float2 q = part[i & 1][w][ch];
+        part[i & 1][w][ch] = make_float2(P, H);
+        P *= q.x;
+        H = rec_step(q.x, H, q.y);
+      }
+      if (in) {
+        const long long at = (rec_slot(t.begin, t.seq) + t.index) * a.D + c;
+        if (WORDS && !first) {
+          if (!last) rec_post(a.words + at, P, H);
+          h = rec_look_back(a.words + at - a.D, a.D, t.index, limit, a.status);
+        } else if (!first) {
+          h = carried;
+        }
+        carried = rec_step(P, h, H);
+        if (last) {
+          if (a.h_out) a.h_out[(long long)t.seq * a.D + c] = carried;
+        } else {
+          if (WORDS && !(a.test_stall && t.item == 0)) rec_post(a.words + at, 0.f, carried);
+          if (a.carries) a.carries[at] = carried;
+        }
+      }
+      entry[i & 1][ch] = h;
+      if (ch == 0) ring[(i + 4) & (kRecRing - 1)] = feed.give(a, false);
+      rec_arrive(kRecEntry + (i & 1), kThreads);
+    }
+    return;
+  }
+
+  using Lane = RecLane<T>;
+  constexpr int ROW = kRecChannels * (int)sizeof(T);
   const T *X = (const T*)a.x, *G = (const T*)a.g;
   T* Y = (T*)a.y;
-  const int items = a.n_segs * a.cols;
-  const int x_access = rec_access<T>(X, a.ld_x), g_access = rec_access<T>(G, a.ld_g);
-  const bool y_pairs = rec_access<T>(Y, a.ld_y) != kRecSingle;
-  const unsigned long long limit = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
-  wait_for_predecessor();
-
+  const int x_access = rec_access<T>(X, a.ld_x), g_access = rec_access<T>(G, a.ld_g), y_access = rec_access<T>(Y, a.ld_y);
   // A warp asks for the rows that it alone reads, so that no barrier stands between a copy and its use.
   auto request = [&](const RecAt& t, int stage) {
     if (t.item < items) {
       const int first = warp * kTok, rows = t.n() - first;
-      unsigned char* at = stages + stage * kStageBytes + first * kRecRow;
-      rec_request<T, kTok>(at, X, a.ld_x, t.tok0() + first, rows, t.col * CH, a.D, x_access);
-      rec_request<T, kTok>(at + kRecTile * kRecRow, G, a.ld_g, t.tok0() + first, rows, t.col * CH, a.D, g_access);
+      unsigned char* at = stages + stage * 2 * kTensor<T> + first * ROW;
+      rec_request<T, kTok>(at, X, a.ld_x, t.tok0() + first, rows, t.col * kRecChannels, a.D, x_access);
+      rec_request<T, kTok>(at + kTensor<T>, G, a.ld_g, t.tok0() + first, rows, t.col * kRecChannels, a.D, g_access);
     }
     rec_commit();
   };
-  // Items: with words drawn from the ticket, one ahead, so that the tiles in front of a tile are done or in the hands of blocks that run; else by a fixed stride.
-  int ahead = 0;
-  if (WORDS) {
-    if (tid == 0) drawn = (int)atomicAdd(a.ticket, 2u);
-    __syncthreads();
-    ahead = drawn + 1;
-  }
-  RecAt now = rec_decode<WORDS>(a, WORDS ? ahead - 1 : (int)blockIdx.x, false);
-  request(now, 0);
-  float carried = 0.f;   // without words: what leaves the last tile, channel tid
-  for (int stage = 0; now.item < items; stage ^= 1) {
-    const RecAt next = rec_next<WORDS>(a, now, ahead, false);
-    request(next, stage ^ 1);
-    int ticket = 0;
-    if (WORDS && tid == 0) ticket = (int)atomicAdd(a.ticket, 1u);
-    rec_wait<1>();
-    __syncwarp();
-    const int n = now.n(), c0 = now.col * CH, left = n - warp * kTok;
-    const unsigned char* sx = stages + stage * kStageBytes + warp * kTok * kRecRow + 4 * lane;
-    float av[kTok][N], uv[kTok][N], P[N], H[N];
+  request(ring[0], 0);
+  request(ring[1], 1);
+  // Round i: the maps of tile i, and the output of tile i - 1, whose entry the channels' threads have found out meanwhile.
+  struct Held { Pair a[kTok], u[kTok]; };
+  Held even, odd;
+  bool resets = false;   // whether some decay of the warp's tokens of tile i - 1 is zero
+  int stage = 0;
+  auto round = [&](int i, Held& now, const Held& before) -> bool {
+    request(ring[(i + 2) & (kRecRing - 1)], stage == 0 ? 2 : stage - 1);
+    const bool has_now = ring[i & (kRecRing - 1)].item < items;
+    bool now_resets = false;
+    if (has_now) {
+      rec_wait<2>();
+      __syncwarp();
+      const unsigned char* sx = stages + stage * 2 * kTensor<T> + warp * kTok * ROW + 2 * lane * (int)sizeof(T);
 #pragma unroll
-    for (int j = 0; j < N; ++j) { P[j] = 1.f; H[j] = 0.f; }
-#pragma unroll
-    for (int t = 0; t < kTok; ++t) {
-      float x[N], g[N];
-      RecLane<T>::widen(x, *reinterpret_cast<const uint32_t*>(sx + t * kRecRow));
-      RecLane<T>::widen(g, *reinterpret_cast<const uint32_t*>(sx + (kRecTile + t) * kRecRow));
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        float m, over;
-        rec_factors<MODE>(g[j], av[t][j], m, over);
-        uv[t][j] = m * x[j];
-        if (t >= left) { av[t][j] = 1.f; uv[t][j] = 0.f; }
-        P[j] *= av[t][j];
-        H[j] = rec_step(av[t][j], H[j], uv[t][j]);
+      for (int k = 0; k < kTok; ++k) {
+        const Pair x = Lane::widen(*reinterpret_cast<const typename Lane::Raw*>(sx + k * ROW)), g = Lane::widen(*reinterpret_cast<const typename Lane::Raw*>(sx + kTensor<T> + k * ROW));
+        Pair m;
+        rec_factors<MODE>(g, now.a[k], m);
+        now.u[k] = rec_input<MODE>(m, x);
       }
+      const int left = ring[i & (kRecRing - 1)].n() - warp * kTok;
+      if (left < kTok) {
+#pragma unroll
+        for (int k = 0; k < kTok; ++k)
+          if (k >= left) { now.a[k] = twice(1.f); now.u[k] = twice(0.f); }
+      }
+      Pair P = now.a[0], H = now.u[0];
+#pragma unroll
+      for (int k = 1; k < kTok; ++k) {
+        P = mul2(P, now.a[k]);
+        H = fma2(now.a[k], H, now.u[k]);
+      }
+      now_resets = __any_sync(0xffffffffu, any_zero(P));
+      if (now_resets) {
+        H = twice(0.f);
+#pragma unroll
+        for (int k = 0; k < kTok; ++k) H = rec_step(now.a[k], H, now.u[k]);
+      }
+      const float2 pp = both(P), hh = both(H);
+      *reinterpret_cast<float4*>(&part[i & 1][warp][2 * lane]) = make_float4(pp.x, hh.x, pp.y, hh.y);
+      rec_arrive(kRecMaps + (i & 1), kThreads);
     }
+    if (i > 0) {
+      rec_meet(kRecEntry + ((i - 1) & 1), kThreads);
+      if (Y) {
+        const RecAt& p = ring[(i - 1) & (kRecRing - 1)];
+        const float4 q = *reinterpret_cast<const float4*>(&part[(i - 1) & 1][warp][2 * lane]);
+        const float2 e = *reinterpret_cast<const float2*>(&entry[(i - 1) & 1][2 * lane]);
+        Pair h = rec_step(pair(q.x, q.z), pair(e.x, e.y), pair(q.y, q.w));
+        const int left = p.n() - warp * kTok, c = p.col * kRecChannels + 2 * lane;
+        T* row = Y + (p.tok0() + warp * kTok) * a.ld_y;
+        if (left >= kTok && (p.col + 1) * kRecChannels <= a.D && (sizeof(T) == 4 ? y_access == kRecWide : y_access != kRecSingle) && !resets) {
+          row += c;
 #pragma unroll
-    for (int j = 0; j < N; ++j) part[warp][lane * N + j] = make_float2(P[j], H[j]);
-    __syncthreads();
-    // what the warps before this one make of the tile's entry
+          for (int k = 0; k < kTok; ++k) {
+            h = fma2(before.a[k], h, before.u[k]);
+            *reinterpret_cast<typename Lane::Raw*>(row) = Lane::pack(h);
+            row += a.ld_y;
+          }
+        } else {
 #pragma unroll
-    for (int j = 0; j < N; ++j) { P[j] = 1.f; H[j] = 0.f; }
-    for (int w = 0; w < warp; ++w)
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float2 q = part[w][lane * N + j];
-        P[j] *= q.x;
-        H[j] = rec_step(q.x, H[j], q.y);
-      }
-    if (tid < CH) {   // a channel of the tile
-      float TP = 1.f, TH = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float2 q = part[w][tid];
-        TP *= q.x;
-        TH = rec_step(q.x, TH, q.y);
-      }
-      const int c = c0 + tid;
-      const bool in = c < a.D, first = now.index == 0, last = now.index + 1 == now.tiles;
-      const long long slot = rec_slot(now.begin, now.seq) + now.index;
-      unsigned long long* word = WORDS ? a.words + slot * a.D + c : nullptr;
-      const bool stalled = a.test_stall && now.item == 0;
-      float h = 0.f;
-      if (in) {
-        if (first) h = a.h0 ? a.h0[(long long)now.seq * a.D + c] : 0.f;
-        else if (!WORDS) h = carried;
-        else {
-          if (!last) rec_post(word, TP, TH);
-          h = rec_look_back(word - a.D, a.D, now.index, limit, a.status);
-        }
-        carried = rec_step(TP, h, TH);
-        if (last) { if (a.h_out) a.h_out[(long long)now.seq * a.D + c] = carried; }
-        else {
-          if (WORDS && !stalled) rec_post(word, 0.f, carried);
-          if (a.carries) a.carries[slot * a.D + c] = carried;
+          for (int k = 0; k < kTok; ++k) {
+            h = rec_step(before.a[k], h, before.u[k]);
+            if (k < left) rec_store(row + k * a.ld_y, c, a.D, y_access, h);
+          }
         }
       }
-      entry[tid] = h;
     }
-    if (WORDS && tid == 0) drawn = ticket;
-    __syncthreads();
-    if (WORDS) ahead = drawn;
-    if (Y) {
-      float h[N];
-#pragma unroll
-      for (int j = 0; j < N; ++j) h[j] = rec_step(P[j], entry[lane * N + j], H[j]);
-      T* row = Y + (now.tok0() + warp * kTok) * a.ld_y;
-#pragma unroll
-      for (int t = 0; t < kTok; ++t) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) h[j] = rec_step(av[t][j], h[j], uv[t][j]);
-        if (t < left) rec_store(row + t * a.ld_y, c0 + lane * N, a.D, y_pairs, h);
-      }
-    }
-    now = next;
+    resets = now_resets;
+    stage = stage == 2 ? 0 : stage + 1;
     __syncwarp();
+    return has_now;
+  };
+  for (int i = 0;; i += 2) {
+    if (!round(i, even, odd)) break;
+    if (!round(i + 1, odd, even)) break;
   }
   rec_wait<0>();
 }
@@ -198,9 +224,10 @@ cudaError_t launch_one(const RecArgs& a, cudaStream_t stream) {
     if ((e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
     sms[dev] = n;
   }
-  if ((e = allow_shared<gated_recurrence_kernel<T, MODE, WORDS>>(kSmem)) != cudaSuccess) return e;
+  constexpr size_t smem = (size_t)kStages * 2 * kTensor<T>;
+  if ((e = allow_shared<gated_recurrence_kernel<T, MODE, WORDS>>(smem)) != cudaSuccess) return e;
   const long long items = (long long)a.n_segs * a.cols;
-  if ((e = launch_early(gated_recurrence_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, 4ll * n)), kThreads, kSmem, stream, a)) != cudaSuccess) return e;
+  if ((e = launch_early(gated_recurrence_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, 2ll * n)), kThreads, smem, stream, a)) != cudaSuccess) return e;
   return launched();
 }
 template <class T>

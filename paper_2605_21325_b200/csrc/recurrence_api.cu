@@ -43,7 +43,7 @@ struct RecPlan {
   size_t bytes() const { return table_bytes + word_bytes; }
 };
 int plan(const tri_inv_rec_desc* d, RecPlan* p) {
-  const int n_seqs = seqs_of(d), channels = kRecRow / (d->dtype == TRI_INV_F32 ? 4 : 2);
+  const int n_seqs = seqs_of(d);
   auto tiles_of = [](long long n) { return std::max(1ll, (n + kRecTile - 1) / kRecTile); };
   long long tiles = 0, longest = 1;
   if (d->cu_seqlens) {
@@ -56,7 +56,7 @@ int plan(const tri_inv_rec_desc* d, RecPlan* p) {
     longest = tiles_of(d->T);
     tiles = longest * n_seqs;
   }
-  p->cols = (int)(((long long)d->D + channels - 1) / channels);
+  p->cols = (int)(((long long)d->D + kRecChannels - 1) / kRecChannels);
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return TRI_INV_ERR_CUDA;
   p->words = longest > 1;
