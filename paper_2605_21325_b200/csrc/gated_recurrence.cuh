@@ -8,15 +8,16 @@
 //     e_t = dy_t + c_{t+1},   c_t = a_t e_t,   dx_t = m_t e_t (m: what multiplies x in u),   dh0 = c_0,
 //     dg_t = e_t w_t,   w_t = a_t h_{t-1} (decay),   a_t h_{t-1} - a_t^2 / m_t x_t (normed),   (h_{t-1} - x_t) a_t (1 - a_t) (gate)
 //
-// Both are walks over tiles of kRecTile tokens of kRecChannels channels.  A tile is an affine map of what enters it, (P, H): h -> P h + H,
+// Both are walks over tiles of kRecTile (kRecCarry) tokens of kRecChannels channels.  A tile is an affine map of what enters it, (P, H): h -> P h + H,
 // and so is a run of tiles; the tokens of a warp, the warps of a tile and the tiles of a sequence join by the same rule.
 #pragma once
 #include "common.cuh"
 
 namespace tri_inv {
 
-constexpr int kRecTile = 64;      // tokens of a tile
-constexpr int kRecChannels = 64;  // and its channels
+constexpr int kRecCarry = TRI_INV_REC_TILE;   // tokens from one carried state to the next
+constexpr int kRecTile = 128;                 // tokens of a tile of the forward walk; the gradient's have kRecCarry
+constexpr int kRecChannels = 64;              // channels of a tile
 
 // An entry of the table of packed sequences: a tile, or a whole sequence (index 0)
 struct RecTile {
@@ -24,8 +25,8 @@ struct RecTile {
   int32_t index, tiles;     // the tile, of how many
 };
 
-// Where a tile's words and carried state lie: sequences of any length leave no two tiles at one place.
-__host__ __device__ __forceinline__ long long rec_slot(long long tok0, int seq) { return tok0 / kRecTile + seq; }
+// Where the words of a sequence's tiles, and its carried states, begin: sequences of any length leave no two tiles at one place.
+__host__ __device__ __forceinline__ long long rec_slot(long long tok0, int seq, int tile) { return tok0 / tile + seq; }
 
 struct RecArgs {
   const void *x, *g, *dy;          // dy: gradient only
@@ -33,7 +34,7 @@ struct RecArgs {
   long long ld_x, ld_g, ld_dy, ld_y, ld_dx, ld_dg;   // values from one token to the next
   const float* h0;                 // [n_seqs, D] or null
   float* h_out;                    // [n_seqs, D] or null
-  float* carries;                  // [slots, D]: the state behind each tile; written by the forward walk (or null), read by the gradient
+  float* carries;                  // [slots of kRecCarry, D]: the states carried on; written by the forward walk (or null), read by the gradient
   const float* dh;                 // gradient: [n_seqs, D] or null
   float* dh0;                      // [n_seqs, D] or null
   unsigned long long* words;       // [slots, D] (P, H) of each tile, or (0, what leaves it); all ones: not there yet.  Null: whole sequences are walked
@@ -51,7 +52,7 @@ cudaError_t launch_gated_recurrence(const RecArgs& a, int dtype, cudaStream_t st
 cudaError_t launch_gated_recurrence_backward(const RecArgs& a, int dtype, cudaStream_t stream);
 // What the walks find in their workspace: the ticket (zero), the words (all ones; null: none, the table then holds whole sequences) and the table of packed sequences
 // from the host offsets `cu` (null: dense, no table).
-cudaError_t launch_rec_setup(unsigned int* ticket, unsigned long long* words, long long n_words, RecTile* table, const int32_t* cu, int n_seqs, cudaStream_t stream);
+cudaError_t launch_rec_setup(unsigned int* ticket, unsigned long long* words, long long n_words, RecTile* table, int tile, const int32_t* cu, int n_seqs, cudaStream_t stream);
 
 struct RecStepArgs {
   const void *x, *g;
@@ -108,6 +109,16 @@ __device__ __forceinline__ Pair rec_slope(Pair g) {
   s = fma2(s, g, twice(0.5f));
   return fma2(s, g, twice(1.f));
 }
+// e^g for g in -inf .. 88 as 2^(g log2 e), the product in two parts t + r (the second changes the power by its factor 1 + r ln 2): off by the power's own error, 2^-22.5.  Results below 2^-126 are 0.
+__device__ __forceinline__ float rec_above(float g) { float y; asm("max.NaN.f32 %0, %1, 0fC3480000;" : "=f"(y) : "f"(g)); return y; }   // -200: so that t and r are finite
+__device__ __forceinline__ float rec_power(float t) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(t)); return y; }
+__device__ __forceinline__ Pair rec_exp(float gx, float gy) {
+  const Pair g = pair(rec_above(gx), rec_above(gy)), log2e = twice(1.44269504088896341f);
+  const Pair t = mul2(g, log2e), r = fma2(g, log2e, mul2(t, twice(-1.f)));
+  const float2 x = both(t);
+  const Pair p = pair(rec_power(x.x), rec_power(x.y));
+  return fma2(mul2(p, twice(0.693147180559945309f)), r, p);
+}
 __device__ __forceinline__ float rec_reciprocal(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float rec_over_root(float x) { float y; asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
@@ -117,10 +128,10 @@ template <int MODE>
 __device__ __forceinline__ void rec_factors(Pair gp, Pair& a, Pair& m) {
   const float2 g = both(gp);
   if constexpr (MODE == kRecDecay) {
-    a = pair(expf(g.x), expf(g.y));
+    a = rec_exp(g.x, g.y);
     m = twice(1.f);
   } else if constexpr (MODE == kRecNormed) {
-    const float2 e = make_float2(expf(g.x), expf(g.y));
+    const float2 e = both(rec_exp(g.x, g.y));
     const bool nx = fabsf(g.x) <= 0.25f, ny = fabsf(g.y) <= 0.25f;
     const Pair minus = twice(-1.f), one = twice(1.f);
     const Pair qn = mul2(mul2(gp, minus), rec_slope(gp)), qf = fma2(pair(e.x, e.y), minus, one);   // 1 - a
@@ -130,8 +141,7 @@ __device__ __forceinline__ void rec_factors(Pair gp, Pair& a, Pair& m) {
     const float2 s = both(sp);
     m = mul2(sp, pair(s.x >= 1.17549435e-38f ? rec_over_root(s.x) : 0.f, s.y >= 1.17549435e-38f ? rec_over_root(s.y) : 0.f));
   } else {
-    const float2 e = make_float2(expf(-fabsf(g.x)), expf(-fabsf(g.y)));
-    const Pair ep = pair(e.x, e.y), one = twice(1.f);
+    const Pair ep = rec_exp(-fabsf(g.x), -fabsf(g.y)), one = twice(1.f);
     const float2 d = both(add2(ep, one));
     const Pair rp = pair(rec_reciprocal(d.x), rec_reciprocal(d.y)), sp = mul2(ep, rp), bp = fma2(sp, twice(-1.f), one);   // s: the smaller of a and 1 - a
     const float2 r = both(rp), s = both(sp), b = both(bp);
@@ -240,6 +250,23 @@ __device__ __forceinline__ void rec_request(unsigned char* smem, const T* base, 
   }
 }
 
+// The same where every row and channel exists and 16 bytes can be moved: `from` is the lane's first 16 bytes, `step` the bytes between those that it copies.
+template <class T, int ROWS>
+__device__ __forceinline__ void rec_request_whole(uint32_t to, const char* from, long long step) {
+  constexpr int BYTES = kRecChannels * (int)sizeof(T), AT_ONCE = 512 / BYTES;
+#pragma unroll
+  for (int i = 0; i < ROWS / AT_ONCE; ++i) {
+    rec_copy(to + i * AT_ONCE * BYTES, from, 16);
+    from += step;
+  }
+}
+template <class T>
+__device__ __forceinline__ long long rec_lane_bytes(long long ld, int row) {   // of a lane's first 16 bytes, from a tile's first value on
+  constexpr int LANES = kRecChannels * (int)sizeof(T) / 16;
+  const int lane = threadIdx.x & 31;
+  return (row + lane / LANES) * ld * (int)sizeof(T) + 16 * (lane % LANES);
+}
+
 __device__ __forceinline__ unsigned long long rec_peek(const unsigned long long* p) {
   unsigned long long v;
   asm volatile("ld.relaxed.gpu.global.b64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
@@ -303,73 +330,92 @@ __device__ __forceinline__ void rec_arrive(int which, int threads) { asm volatil
 // Where a block stands: a tile of an item, which is a tile (with words) or a whole sequence
 struct RecAt {
   int item;            // >= the number of items: none left
-  int seq, col;
+  int seq, c0;         // c0: the tile's first channel
   int begin, len;      // the sequence's
   int index, tiles;    // the tile, of how many
-  __device__ __forceinline__ long long tok0() const { return (long long)begin + (long long)index * kRecTile; }
-  __device__ __forceinline__ int n() const { return min(kRecTile, len - index * kRecTile); }
+  int n;               // its tokens
+  bool whole;          // all tokens and channels of a tile
+  long long tok0;
+  long long slot;      // of its words
+  long long at[5];     // where its first value lies in each tensor, in bytes
 };
-// The tile of an item, its entry of the table at hand (packed sequences)
-template <bool WORDS>
-__device__ __forceinline__ RecAt rec_decode(const RecArgs& a, int item, const RecTile& entry, bool back) {
-  RecAt t{};
-  t.item = item;
-  if (item >= a.n_segs * a.cols) return t;
-  const int r = item / a.cols;
-  t.col = item - r * a.cols;
-  if (a.table) {
-    t.begin = entry.tok0; t.len = entry.n; t.seq = entry.seq; t.index = entry.index; t.tiles = entry.tiles;
-  } else {
-    const int rank = back && WORDS ? a.n_segs - 1 - r : r;
-    t.index = WORDS ? rank / a.n_seqs : 0;   // the sequences' tiles in turn: the one in front of a tile is n_seqs (times the columns) items ahead of it
-    t.tiles = max(1, (int)(((unsigned)a.T + kRecTile - 1) / kRecTile));
-    t.seq = WORDS ? rank - t.index * a.n_seqs : rank;
-    t.begin = t.seq * a.T;
-    t.len = a.T;
-  }
-  if (!WORDS && back) t.index = t.tiles - 1;
-  return t;
-}
-__device__ __forceinline__ RecTile rec_entry(const RecArgs& a, int item, bool back) {   // of the table, for an item that may be past the last
-  if (!a.table || item >= a.n_segs * a.cols) return RecTile{};
-  const int r = item / a.cols;
-  return a.table[back ? a.n_segs - 1 - r : r];
-}
-
-// A block's tiles in order: the one that it works on, the one before (whose entry is awaited) and those that are on their way lie in a ring in shared memory, which one thread keeps ahead.
-// With words the items are drawn from the ticket, so that the tiles in front of a tile are done or in the hands of blocks that run; else they go by a fixed stride.
+// The order of a block's tiles.  The one that it works on, the one before and those that are on their way lie in a ring in shared memory, which one thread keeps ahead.  With words the items are drawn
+// from the ticket, so that the tiles in front of a tile are done or in the hands of blocks that run; else they go by a fixed stride.
 constexpr int kRecRing = 8;
-template <bool WORDS>
+template <bool WORDS, int TILE, int TENSORS, bool BACK>
 struct RecFeed {
-  int drawn;         // the item whose entry is asked for next
-  RecAt last;        // without words: the tile that was given last
-  RecTile entry;
+  const RecArgs& a;
+  long long ld[TENSORS];   // bytes
+  int width;               // bytes of a value
+  int drawn;               // the item whose entry of the table is asked for next
+  RecAt last;              // without words: the tile that was given last
+  __device__ __forceinline__ bool more() const { return !WORDS && last.item < a.n_segs * a.cols && (BACK ? last.index > 0 : last.index + 1 < last.tiles); }
+  __device__ __forceinline__ RecTile entry(int item) const {
+    if (!a.table || item >= a.n_segs * a.cols) return RecTile{};
+    const int r = item / a.cols;
+    return a.table[BACK && WORDS ? a.n_segs - 1 - r : r];
+  }
+  __device__ __forceinline__ void place() {
+    last.n = min(TILE, last.len - last.index * TILE);
+    last.whole = last.n == TILE && last.c0 + kRecChannels <= a.D;
+    last.tok0 = last.begin + (long long)last.index * TILE;
+    last.slot = rec_slot(last.begin, last.seq, TILE) + last.index;
+#pragma unroll
+    for (int k = 0; k < TENSORS; ++k) last.at[k] = last.tok0 * ld[k] + (long long)last.c0 * width;
+  }
+  __device__ __forceinline__ void decode(int item, const RecTile& e) {
+    last.item = item;
+    if (item >= a.n_segs * a.cols) return;
+    const int r = item / a.cols;
+    last.c0 = (item - r * a.cols) * kRecChannels;
+    if (a.table) {
+      last.begin = e.tok0; last.len = e.n; last.seq = e.seq; last.index = e.index; last.tiles = e.tiles;
+    } else {
+      const int rank = BACK && WORDS ? a.n_segs - 1 - r : r;
+      last.index = WORDS ? rank / a.n_seqs : 0;   // the sequences' tiles in turn: the one in front of a tile is n_seqs (times the columns) items ahead of it
+      last.tiles = max(1, (int)(((unsigned)a.T + TILE - 1) / TILE));
+      last.seq = WORDS ? rank - last.index * a.n_seqs : rank;
+      last.begin = last.seq * a.T;
+      last.len = a.T;
+    }
+    if (!WORDS) {
+      last.tiles = max(1, (int)(((unsigned)last.len + TILE - 1) / TILE));
+      last.index = BACK ? last.tiles - 1 : 0;
+    }
+    place();
+  }
+  __device__ __forceinline__ void follow() { last.index += BACK ? -1 : 1; place(); }
   // Ahead of the first tile: `n` tiles into the ring
-  __device__ __forceinline__ void begin(const RecArgs& a, RecAt* ring, int n, bool back) {
-    const int stride = gridDim.x;
+  __device__ __forceinline__ void begin(RecAt* ring, int n) {
     int item = blockIdx.x;
     for (int i = 0; i < n; ++i) {
-      if (WORDS) item = (int)atomicAdd(a.ticket, 1u);
-      if (!WORDS && i > 0 && more(last, back)) { ring[i] = last = after(last, back); continue; }
-      ring[i] = last = rec_decode<WORDS>(a, item, rec_entry(a, item, back), back);
-      item += stride;
+      if (i > 0 && more()) {
+        follow();
+      } else {
+        if (WORDS) item = (int)atomicAdd(a.ticket, 1u);
+        decode(item, entry(item));
+        item += gridDim.x;
+      }
+      ring[i] = last;
     }
     drawn = WORDS ? (int)atomicAdd(a.ticket, 1u) : item;
   }
-  static __device__ __forceinline__ bool more(const RecAt& t, bool back) { return back ? t.index > 0 : t.index + 1 < t.tiles; }
-  static __device__ __forceinline__ RecAt after(RecAt t, bool back) { t.index += back ? -1 : 1; return t; }
   // Early in a round: asks for what `give` needs
   int next_drawn, given;
-  __device__ __forceinline__ void ask(const RecArgs& a, bool back) {
+  RecTile asked;
+  __device__ __forceinline__ void ask() {
     given = drawn;
-    entry = rec_entry(a, drawn, back);
+    asked = entry(drawn);
     if (WORDS) next_drawn = (int)atomicAdd(a.ticket, 1u);
   }
-  __device__ __forceinline__ RecAt give(const RecArgs& a, bool back) {
-    if (!WORDS && last.item < a.n_segs * a.cols && more(last, back)) return last = after(last, back);
-    last = rec_decode<WORDS>(a, given, entry, back);
-    drawn = WORDS ? next_drawn : given + (int)gridDim.x;
-    return last;
+  __device__ __forceinline__ void give(RecAt* to) {
+    if (more()) {
+      follow();
+    } else {
+      decode(given, asked);
+      drawn = WORDS ? next_drawn : given + (int)gridDim.x;
+    }
+    *to = last;
   }
 };
 #endif

@@ -6,9 +6,9 @@
 namespace tri_inv {
 namespace {
 
-constexpr int kWarps = 8, kTok = kRecTile / kWarps, kStages = 3;
+constexpr int kWarps = 8, kTok = kRecCarry / kWarps, kStages = 3;
 constexpr int kThreads = 32 * kWarps + kRecChannels;   // warps of tokens, and a thread for each channel that joins them
-template <class T> constexpr int kTensor = kRecTile * kRecChannels * (int)sizeof(T);   // bytes of a tile of one tensor
+template <class T> constexpr int kTensor = kRecCarry * kRecChannels * (int)sizeof(T);   // bytes of a tile of one tensor
 
 // What a warp's tokens of a tile make of x, from what the first pass over them left: a, m
 template <int MODE> struct Held { Pair a[kTok], m[kTok]; };
@@ -42,9 +42,10 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
   __shared__ RecAt ring[kRecRing];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int items = a.n_segs * a.cols;
-  RecFeed<WORDS> feed;
+  constexpr int es = sizeof(T);
+  RecFeed<WORDS, kRecCarry, 5, true> feed{a, {a.ld_x * es, a.ld_g * es, a.ld_dy * es, a.ld_dx * es, a.ld_dg * es}, es};
   wait_for_predecessor();
-  if (tid == 32 * kWarps) feed.begin(a, ring, 4, true);
+  if (tid == 32 * kWarps) feed.begin(ring, 4);
   __syncthreads();
 
   if (warp >= kWarps) {   // a channel
@@ -52,12 +53,12 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
     const unsigned long long limit = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
     float carried = 0.f;
     for (int i = 0;; ++i) {
-      const RecAt t = ring[i & (kRecRing - 1)];
+      const RecAt& t = ring[i & (kRecRing - 1)];
       if (t.item >= items) break;
-      if (ch == 0) feed.ask(a, true);
-      const int c = t.col * kRecChannels + ch;
-      const bool in = c < a.D, first = t.index == 0, last = t.index + 1 == t.tiles;
-      const long long at = (rec_slot(t.begin, t.seq) + t.index) * a.D + c, state = (long long)t.seq * a.D + c;
+      if (ch == 0) feed.ask();
+      const int c = t.c0 + ch, behind = t.tiles - 1 - t.index;
+      const bool in = c < a.D, first = t.index == 0, last = behind == 0;
+      const long long at = t.slot * a.D + c, state = (long long)t.seq * a.D + c;
       float h = !in ? 0.f : !first ? a.carries[at - a.D] : a.h0 ? a.h0[state] : 0.f;   // the state in front of the tile
       float e = last && in && a.dh ? a.dh[state] : 0.f;
       rec_meet(kRecMaps + (i & 1), kThreads);
@@ -79,7 +80,7 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
       if (in) {
         if (WORDS && !last) {
           if (!first) rec_post(a.words + at, P, C);
-          e = rec_look_back(a.words + at + a.D, -(long long)a.D, t.tiles - 1 - t.index, limit, a.status);
+          e = rec_look_back(a.words + at + a.D, -(long long)a.D, behind, limit, a.status);
         } else if (!last) {
           e = carried;
         }
@@ -91,7 +92,7 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
         }
       }
       entry[i & 1][ch] = e;
-      if (ch == 0) ring[(i + 4) & (kRecRing - 1)] = feed.give(a, true);
+      if (ch == 0) feed.give(&ring[(i + 4) & (kRecRing - 1)]);
       rec_arrive(kRecEntry + (i & 1), kThreads);
     }
     return;
@@ -99,17 +100,29 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
 
   using Lane = RecLane<T>;
   using Raw = typename Lane::Raw;
-  constexpr int ROW = kRecChannels * (int)sizeof(T);
+  constexpr int ROW = kRecChannels * es;
   const T *X = (const T*)a.x, *G = (const T*)a.g, *DY = (const T*)a.dy;
   const int x_access = rec_access<T>(X, a.ld_x), g_access = rec_access<T>(G, a.ld_g), dy_access = rec_access<T>(DY, a.ld_dy);
-  const int dx_access = rec_access<T>(a.dx, a.ld_dx), dg_access = rec_access<T>(a.dg, a.ld_dg), plain = sizeof(T) == 4 ? kRecWide : kRecFours;   // whole lanes can be written
+  const int dx_access = rec_access<T>(a.dx, a.ld_dx), dg_access = rec_access<T>(a.dg, a.ld_dg), most = es == 4 ? kRecWide : kRecFours;
+  const bool wide = x_access == kRecWide && g_access == kRecWide && dy_access == kRecWide, plain = dx_access <= most && dg_access <= most;   // plain: whole lanes can be written
+  const char *x_from = (const char*)X + rec_lane_bytes<T>(a.ld_x, warp * kTok), *g_from = (const char*)G + rec_lane_bytes<T>(a.ld_g, warp * kTok),
+             *dy_from = (const char*)DY + rec_lane_bytes<T>(a.ld_dy, warp * kTok);
+  const uint32_t lane_to = (uint32_t)__cvta_generic_to_shared(stages) + warp * kTok * ROW + 16 * lane;
   auto request = [&](const RecAt& t, int stage) {
     if (t.item < items) {
-      const int first = warp * kTok, rows = t.n() - first, c0 = t.col * kRecChannels;
-      unsigned char* at = stages + stage * 3 * kTensor<T> + first * ROW;
-      rec_request<T, kTok>(at, X, a.ld_x, t.tok0() + first, rows, c0, a.D, x_access);
-      rec_request<T, kTok>(at + kTensor<T>, G, a.ld_g, t.tok0() + first, rows, c0, a.D, g_access);
-      rec_request<T, kTok>(at + 2 * kTensor<T>, DY, a.ld_dy, t.tok0() + first, rows, c0, a.D, dy_access);
+      if (t.whole && wide) {
+        const uint32_t to = lane_to + stage * 3 * kTensor<T>;
+        constexpr int at_once = 512 / ROW * es;
+        rec_request_whole<T, kTok>(to, x_from + t.at[0], a.ld_x * at_once);
+        rec_request_whole<T, kTok>(to + kTensor<T>, g_from + t.at[1], a.ld_g * at_once);
+        rec_request_whole<T, kTok>(to + 2 * kTensor<T>, dy_from + t.at[2], a.ld_dy * at_once);
+      } else {
+        const int first = warp * kTok;
+        unsigned char* to = stages + stage * 3 * kTensor<T> + first * ROW;
+        rec_request<T, kTok>(to, X, a.ld_x, t.tok0 + first, t.n - first, t.c0, a.D, x_access);
+        rec_request<T, kTok>(to + kTensor<T>, G, a.ld_g, t.tok0 + first, t.n - first, t.c0, a.D, g_access);
+        rec_request<T, kTok>(to + 2 * kTensor<T>, DY, a.ld_dy, t.tok0 + first, t.n - first, t.c0, a.D, dy_access);
+      }
     }
     rec_commit();
   };
@@ -122,14 +135,14 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
     const int stage_next = 3 - stage - stage_before;
     request(ring[(i + 1) & (kRecRing - 1)], stage_next);
     const bool has_now = ring[i & (kRecRing - 1)].item < items;
-    const int place = warp * kTok * ROW + 2 * lane * (int)sizeof(T);
+    const int place = warp * kTok * ROW + 2 * lane * es;
     bool now_resets = false;
     if (has_now) {
       rec_wait<1>();
       __syncwarp();
       const unsigned char* sx = stages + stage * 3 * kTensor<T> + place;
       auto read = [&](int tensor, int k) { return Lane::widen(*reinterpret_cast<const Raw*>(sx + tensor * kTensor<T> + k * ROW)); };
-      const int left = ring[i & (kRecRing - 1)].n() - warp * kTok;
+      const int left = ring[i & (kRecRing - 1)].n - warp * kTok;
       Pair P = twice(1.f), H = twice(0.f), C = twice(0.f);
 #pragma unroll
       for (int k = 0; k < kTok; ++k) {
@@ -177,32 +190,30 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
       const float4 q = *reinterpret_cast<const float4*>(&part[(i - 1) & 1][warp][2 * lane]);
       const float2 s = *reinterpret_cast<const float2*>(&side[(i - 1) & 1][warp][2 * lane]), e0 = *reinterpret_cast<const float2*>(&entry[(i - 1) & 1][2 * lane]);
       Pair h = pair(s.x, s.y), C = rec_step(pair(q.x, q.z), pair(e0.x, e0.y), pair(q.y, q.w)), w[kTok];
-      const int left = p.n() - warp * kTok, c = p.col * kRecChannels + 2 * lane;
-      T* dx_row = (T*)a.dx + (p.tok0() + warp * kTok) * a.ld_dx;
-      T* dg_row = (T*)a.dg + (p.tok0() + warp * kTok) * a.ld_dg;
       auto m_of = [&](int k) {
         if constexpr (MODE == kRecDecay) return twice(1.f);
         else return before.m[k];
       };
-      if (left >= kTok && (p.col + 1) * kRecChannels <= a.D && dx_access <= plain && dg_access <= plain && !resets) {
+      if (p.whole && plain && !resets) {
 #pragma unroll
         for (int k = 0; k < kTok; ++k) {
           const Pair x = read(0, k);
           w[k] = weight<MODE>(before.a[k], m_of(k), h, x);
           h = fma2(before.a[k], h, rec_input<MODE>(m_of(k), x));
         }
-        dx_row += (kTok - 1) * a.ld_dx + c;
-        dg_row += (kTok - 1) * a.ld_dg + c;
+        char *dx_row = (char*)a.dx + p.at[3] + (warp * kTok * a.ld_dx + 2 * lane) * es, *dg_row = (char*)a.dg + p.at[4] + (warp * kTok * a.ld_dg + 2 * lane) * es;
+        const uint32_t dx_step = (uint32_t)a.ld_dx * es, dg_step = (uint32_t)a.ld_dg * es;
 #pragma unroll
         for (int k = kTok - 1; k >= 0; --k) {
           const Pair e = add2(C, read(2, k));
-          *reinterpret_cast<Raw*>(dx_row) = Lane::pack(rec_input<MODE>(m_of(k), e));
-          *reinterpret_cast<Raw*>(dg_row) = Lane::pack(mul2(w[k], e));
+          *reinterpret_cast<Raw*>(dx_row + (unsigned long long)dx_step * k) = Lane::pack(rec_input<MODE>(m_of(k), e));
+          *reinterpret_cast<Raw*>(dg_row + (unsigned long long)dg_step * k) = Lane::pack(mul2(w[k], e));
           C = mul2(before.a[k], e);
-          dx_row -= a.ld_dx;
-          dg_row -= a.ld_dg;
         }
       } else {
+        const int left = p.n - warp * kTok, c = p.c0 + 2 * lane;
+        T* dx_row = (T*)a.dx + (p.tok0 + warp * kTok) * a.ld_dx;
+        T* dg_row = (T*)a.dg + (p.tok0 + warp * kTok) * a.ld_dg;
 #pragma unroll
         for (int k = 0; k < kTok; ++k) {
           const Pair x = read(0, k);

@@ -6,7 +6,7 @@
 namespace tri_inv {
 namespace {
 
-constexpr int kWarps = 8, kTok = kRecTile / kWarps, kStages = 3;
+constexpr int kWarps = 8, kTok = kRecTile / kWarps, kStages = 2;
 constexpr int kThreads = 32 * kWarps + kRecChannels;   // warps of tokens, and a thread for each channel that joins them
 template <class T> constexpr int kTensor = kRecTile * kRecChannels * (int)sizeof(T);   // bytes of a tile of one tensor
 
@@ -18,9 +18,10 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_kernel(const __g
   __shared__ RecAt ring[kRecRing];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int items = a.n_segs * a.cols;
-  RecFeed<WORDS> feed;
+  constexpr int es = sizeof(T);
+  RecFeed<WORDS, kRecTile, 3, false> feed{a, {a.ld_x * es, a.ld_g * es, a.ld_y * es}, es};
   wait_for_predecessor();
-  if (tid == 32 * kWarps) feed.begin(a, ring, 4, false);
+  if (tid == 32 * kWarps) feed.begin(ring, 4);
   __syncthreads();
 
   if (warp >= kWarps) {   // a channel
@@ -28,11 +29,11 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_kernel(const __g
     const unsigned long long limit = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
     float carried = 0.f;   // without words: what leaves the tile before
     for (int i = 0;; ++i) {
-      const RecAt t = ring[i & (kRecRing - 1)];
+      const RecAt& t = ring[i & (kRecRing - 1)];
       if (t.item >= items) break;
-      if (ch == 0) feed.ask(a, false);
-      const int c = t.col * kRecChannels + ch;
-      const bool in = c < a.D, first = t.index == 0, last = t.index + 1 == t.tiles;
+      if (ch == 0) feed.ask();
+      const int c = t.c0 + ch, index = t.index;
+      const bool in = c < a.D, first = index == 0, last = index + 1 == t.tiles;
       float h = first && in && a.h0 ? a.h0[(long long)t.seq * a.D + c] : 0.f;
       rec_meet(kRecMaps + (i & 1), kThreads);
       float P = 1.f, H = 0.f;
@@ -44,121 +45,124 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_kernel(const __g
         H = rec_step(q.x, H, q.y);
       }
       if (in) {
-        const long long at = (rec_slot(t.begin, t.seq) + t.index) * a.D + c;
         if (WORDS && !first) {
-          if (!last) rec_post(a.words + at, P, H);
-          h = rec_look_back(a.words + at - a.D, a.D, t.index, limit, a.status);
+          unsigned long long* word = a.words + t.slot * a.D + c;
+          if (!last) rec_post(word, P, H);
+          h = rec_look_back(word - a.D, a.D, index, limit, a.status);
         } else if (!first) {
           h = carried;
         }
         carried = rec_step(P, h, H);
-        if (last) {
-          if (a.h_out) a.h_out[(long long)t.seq * a.D + c] = carried;
-        } else {
-          if (WORDS && !(a.test_stall && t.item == 0)) rec_post(a.words + at, 0.f, carried);
-          if (a.carries) a.carries[at] = carried;
-        }
+        if (WORDS && !last && !(a.test_stall && t.item == 0)) rec_post(a.words + t.slot * a.D + c, 0.f, carried);
       }
       entry[i & 1][ch] = h;
-      if (ch == 0) ring[(i + 4) & (kRecRing - 1)] = feed.give(a, false);
+      if (ch == 0) feed.give(&ring[(i + 4) & (kRecRing - 1)]);
       rec_arrive(kRecEntry + (i & 1), kThreads);
+      if (in && last && a.h_out) a.h_out[(long long)t.seq * a.D + c] = carried;
+      if (in && a.carries) {   // those that a further token of the sequence follows
+        float* to = a.carries + (rec_slot(t.begin, t.seq, kRecCarry) + (long long)index * (kRecTile / kRecCarry)) * a.D + c;
+        const int left = t.len - index * kRecTile;
+#pragma unroll
+        for (int k = 1; k <= kRecTile / kRecCarry; ++k)
+          if (k * kRecCarry < left) {
+            float s = carried;
+            if (k * kRecCarry < kRecTile) {
+              const float2 q = part[i & 1][k * kRecCarry / kTok][ch];
+              s = rec_step(q.x, h, q.y);
+            }
+            to[(long long)(k - 1) * a.D] = s;
+          }
+      }
     }
     return;
   }
 
   using Lane = RecLane<T>;
-  constexpr int ROW = kRecChannels * (int)sizeof(T);
+  using Raw = typename Lane::Raw;
+  constexpr int ROW = kRecChannels * es;
   const T *X = (const T*)a.x, *G = (const T*)a.g;
   T* Y = (T*)a.y;
   const int x_access = rec_access<T>(X, a.ld_x), g_access = rec_access<T>(G, a.ld_g), y_access = rec_access<T>(Y, a.ld_y);
+  const bool wide = x_access == kRecWide && g_access == kRecWide, plain = y_access <= (es == 4 ? kRecWide : kRecFours);   // whole lanes can be written
+  const char *x_from = (const char*)X + rec_lane_bytes<T>(a.ld_x, warp * kTok), *g_from = (const char*)G + rec_lane_bytes<T>(a.ld_g, warp * kTok);
+  const long long x_step = a.ld_x * (512 / ROW) * es, g_step = a.ld_g * (512 / ROW) * es;
+  const uint32_t lane_to = (uint32_t)__cvta_generic_to_shared(stages) + warp * kTok * ROW + 16 * lane;   // (a warp's 512 bytes at a time follow one another)
   // A warp asks for the rows that it alone reads, so that no barrier stands between a copy and its use.
   auto request = [&](const RecAt& t, int stage) {
     if (t.item < items) {
-      const int first = warp * kTok, rows = t.n() - first;
-      unsigned char* at = stages + stage * 2 * kTensor<T> + first * ROW;
-      rec_request<T, kTok>(at, X, a.ld_x, t.tok0() + first, rows, t.col * kRecChannels, a.D, x_access);
-      rec_request<T, kTok>(at + kTensor<T>, G, a.ld_g, t.tok0() + first, rows, t.col * kRecChannels, a.D, g_access);
+      if (t.whole && wide) {
+        const uint32_t to = lane_to + stage * 2 * kTensor<T>;
+        rec_request_whole<T, kTok>(to, x_from + t.at[0], x_step);
+        rec_request_whole<T, kTok>(to + kTensor<T>, g_from + t.at[1], g_step);
+      } else {
+        const int first = warp * kTok;
+        unsigned char* to = stages + stage * 2 * kTensor<T> + first * ROW;
+        rec_request<T, kTok>(to, X, a.ld_x, t.tok0 + first, t.n - first, t.c0, a.D, x_access);
+        rec_request<T, kTok>(to + kTensor<T>, G, a.ld_g, t.tok0 + first, t.n - first, t.c0, a.D, g_access);
+      }
     }
     rec_commit();
   };
   request(ring[0], 0);
-  request(ring[1], 1);
-  // Round i: the maps of tile i, and the output of tile i - 1, whose entry the channels' threads have found out meanwhile.
-  struct Held { Pair a[kTok], u[kTok]; };
-  Held even, odd;
-  bool resets = false;   // whether some decay of the warp's tokens of tile i - 1 is zero
-  int stage = 0;
-  auto round = [&](int i, Held& now, const Held& before) -> bool {
-    request(ring[(i + 2) & (kRecRing - 1)], stage == 0 ? 2 : stage - 1);
-    const bool has_now = ring[i & (kRecRing - 1)].item < items;
-    bool now_resets = false;
-    if (has_now) {
-      rec_wait<2>();
-      __syncwarp();
-      const unsigned char* sx = stages + stage * 2 * kTensor<T> + warp * kTok * ROW + 2 * lane * (int)sizeof(T);
+  for (int i = 0;; ++i) {
+    const RecAt& t = ring[i & (kRecRing - 1)];
+    if (t.item >= items) break;
+    request(ring[(i + 1) & (kRecRing - 1)], (i + 1) & 1);
+    rec_wait<1>();
+    __syncwarp();
+    const unsigned char* sx = stages + (i & 1) * 2 * kTensor<T> + warp * kTok * ROW + 2 * lane * es;
+    Pair av[kTok], uv[kTok];
 #pragma unroll
-      for (int k = 0; k < kTok; ++k) {
-        const Pair x = Lane::widen(*reinterpret_cast<const typename Lane::Raw*>(sx + k * ROW)), g = Lane::widen(*reinterpret_cast<const typename Lane::Raw*>(sx + kTensor<T> + k * ROW));
-        Pair m;
-        rec_factors<MODE>(g, now.a[k], m);
-        now.u[k] = rec_input<MODE>(m, x);
-      }
-      const int left = ring[i & (kRecRing - 1)].n() - warp * kTok;
-      if (left < kTok) {
-#pragma unroll
-        for (int k = 0; k < kTok; ++k)
-          if (k >= left) { now.a[k] = twice(1.f); now.u[k] = twice(0.f); }
-      }
-      Pair P = now.a[0], H = now.u[0];
-#pragma unroll
-      for (int k = 1; k < kTok; ++k) {
-        P = mul2(P, now.a[k]);
-        H = fma2(now.a[k], H, now.u[k]);
-      }
-      now_resets = __any_sync(0xffffffffu, any_zero(P));
-      if (now_resets) {
-        H = twice(0.f);
-#pragma unroll
-        for (int k = 0; k < kTok; ++k) H = rec_step(now.a[k], H, now.u[k]);
-      }
-      const float2 pp = both(P), hh = both(H);
-      *reinterpret_cast<float4*>(&part[i & 1][warp][2 * lane]) = make_float4(pp.x, hh.x, pp.y, hh.y);
-      rec_arrive(kRecMaps + (i & 1), kThreads);
+    for (int k = 0; k < kTok; ++k) {
+      const Pair x = Lane::widen(*reinterpret_cast<const Raw*>(sx + k * ROW)), g = Lane::widen(*reinterpret_cast<const Raw*>(sx + kTensor<T> + k * ROW));
+      Pair m;
+      rec_factors<MODE>(g, av[k], m);
+      uv[k] = rec_input<MODE>(m, x);
     }
-    if (i > 0) {
-      rec_meet(kRecEntry + ((i - 1) & 1), kThreads);
-      if (Y) {
-        const RecAt& p = ring[(i - 1) & (kRecRing - 1)];
-        const float4 q = *reinterpret_cast<const float4*>(&part[(i - 1) & 1][warp][2 * lane]);
-        const float2 e = *reinterpret_cast<const float2*>(&entry[(i - 1) & 1][2 * lane]);
-        Pair h = rec_step(pair(q.x, q.z), pair(e.x, e.y), pair(q.y, q.w));
-        const int left = p.n() - warp * kTok, c = p.col * kRecChannels + 2 * lane;
-        T* row = Y + (p.tok0() + warp * kTok) * a.ld_y;
-        if (left >= kTok && (p.col + 1) * kRecChannels <= a.D && (sizeof(T) == 4 ? y_access == kRecWide : y_access != kRecSingle) && !resets) {
-          row += c;
+    const int left = t.n - warp * kTok;
+    if (left < kTok) {
 #pragma unroll
-          for (int k = 0; k < kTok; ++k) {
-            h = fma2(before.a[k], h, before.u[k]);
-            *reinterpret_cast<typename Lane::Raw*>(row) = Lane::pack(h);
-            row += a.ld_y;
-          }
-        } else {
+      for (int k = 0; k < kTok; ++k)
+        if (k >= left) { av[k] = twice(1.f); uv[k] = twice(0.f); }
+    }
+    Pair P = av[0], H = uv[0];
 #pragma unroll
-          for (int k = 0; k < kTok; ++k) {
-            h = rec_step(before.a[k], h, before.u[k]);
-            if (k < left) rec_store(row + k * a.ld_y, c, a.D, y_access, h);
-          }
+    for (int k = 1; k < kTok; ++k) {
+      P = mul2(P, av[k]);
+      H = fma2(av[k], H, uv[k]);
+    }
+    const bool resets = __any_sync(0xffffffffu, any_zero(P));   // some decay of the warp's tokens is zero
+    if (resets) {
+      H = twice(0.f);
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) H = rec_step(av[k], H, uv[k]);
+    }
+    const float2 pp = both(P), hh = both(H);
+    *reinterpret_cast<float4*>(&part[i & 1][warp][2 * lane]) = make_float4(pp.x, hh.x, pp.y, hh.y);
+    rec_arrive(kRecMaps + (i & 1), kThreads);
+    rec_meet(kRecEntry + (i & 1), kThreads);
+    if (Y) {
+      const float4 q = *reinterpret_cast<const float4*>(&part[i & 1][warp][2 * lane]);
+      const float2 e = *reinterpret_cast<const float2*>(&entry[i & 1][2 * lane]);
+      Pair h = rec_step(pair(q.x, q.z), pair(e.x, e.y), pair(q.y, q.w));
+      if (t.whole && plain && !resets) {
+        char* row = (char*)Y + t.at[2] + (warp * kTok * a.ld_y + 2 * lane) * es;
+        const uint32_t step = (uint32_t)a.ld_y * es;
+#pragma unroll
+        for (int k = 0; k < kTok; ++k) {
+          h = fma2(av[k], h, uv[k]);
+          *reinterpret_cast<Raw*>(row + (unsigned long long)step * k) = Lane::pack(h);
+        }
+      } else {
+        T* row = Y + (t.tok0 + warp * kTok) * a.ld_y;
+#pragma unroll
+        for (int k = 0; k < kTok; ++k) {
+          h = rec_step(av[k], h, uv[k]);
+          if (k < left) rec_store(row + k * a.ld_y, t.c0 + 2 * lane, a.D, y_access, h);
         }
       }
     }
-    resets = now_resets;
-    stage = stage == 2 ? 0 : stage + 1;
     __syncwarp();
-    return has_now;
-  };
-  for (int i = 0;; i += 2) {
-    if (!round(i, even, odd)) break;
-    if (!round(i + 1, odd, even)) break;
   }
   rec_wait<0>();
 }
@@ -170,11 +174,11 @@ struct SetupArgs {
   unsigned long long* words;
   RecTile* table;          // where these sequences' entries begin
   long long n_words;       // to clear; 0: neither words nor ticket
-  int n_seqs, by_tile;
+  int n_seqs, tile;        // tile: tokens of one; 0: an entry is a whole sequence
 };
 template <int SEQS>
 struct SeqBatch { SeqRange seq[SEQS]; };   // the longest first
-__host__ __device__ __forceinline__ int tiles_of(int n) { return n > 0 ? (int)(((unsigned)n + kRecTile - 1) / kRecTile) : 1; }
+__host__ __device__ __forceinline__ int tiles_of(int n, int tile) { return n > 0 && tile ? (int)(((unsigned)n + tile - 1) / tile) : 1; }
 // The ticket, the words, and up to 320 sequences' entries of the table, a warp per sequence.  Tiles lie in turn, every sequence's first, then every second, so that the tile in front of a tile is
 // as far ahead of it as there are sequences left.
 template <int SEQS>
@@ -182,7 +186,7 @@ __global__ void __launch_bounds__(256) rec_setup_kernel(const __grid_constant__ 
   __shared__ int tiles[SEQS];
   let_successor_start();
   if constexpr (SEQS > 1)
-    for (int q = threadIdx.x; q < b.n_seqs; q += 256) tiles[q] = tiles_of(batch.seq[q].n);
+    for (int q = threadIdx.x; q < b.n_seqs; q += 256) tiles[q] = tiles_of(batch.seq[q].n, b.tile);
   __syncthreads();
   wait_for_predecessor();
   if (b.n_words) {
@@ -198,10 +202,6 @@ __global__ void __launch_bounds__(256) rec_setup_kernel(const __grid_constant__ 
     for (int s = blockIdx.x * 8 + (threadIdx.x >> 5); s < b.n_seqs; s += gridDim.x * 8) {
       const SeqRange r = batch.seq[s];
       RecTile e{r.tok0, r.n, r.seq, 0, tiles[s]};
-      if (!b.by_tile) {
-        if (lane == 0) b.table[s] = e;
-        continue;
-      }
       for (int k = lane; k < e.tiles; k += 32) {
         long long at = s;   // among the k-th tiles: the sequences before this one are as long at least
         for (int q = 0; q < b.n_seqs; ++q) at += min(tiles[q], k);
@@ -246,8 +246,8 @@ cudaError_t launch_gated_recurrence(const RecArgs& a, int dtype, cudaStream_t st
   return dtype == TRI_INV_F32 ? launch_type<float>(a, stream) : launch_type<__nv_bfloat16>(a, stream);
 }
 
-cudaError_t launch_rec_setup(unsigned int* ticket, unsigned long long* words, long long n_words, RecTile* table, const int32_t* cu, int n_seqs, cudaStream_t stream) {
-  SetupArgs b{ticket, words, table, words ? n_words : 0, 0, words != nullptr};
+cudaError_t launch_rec_setup(unsigned int* ticket, unsigned long long* words, long long n_words, RecTile* table, int tile, const int32_t* cu, int n_seqs, cudaStream_t stream) {
+  SetupArgs b{ticket, words, table, words ? n_words : 0, 0, words ? tile : 0};
   auto grid = [&]() { return dim3((unsigned)std::max<long long>(1, std::min<long long>(std::max<long long>((b.n_seqs + 7) / 8, (b.n_words / 2 + 1023) / 1024), 592))); };
   if (!cu) return b.n_words ? launch_early(rec_setup_kernel<1>, grid(), 256, 0, stream, b, SeqBatch<1>{}) : cudaSuccess;
   SeqBatch<kSeqsPerSetup> batch;
@@ -256,7 +256,7 @@ cudaError_t launch_rec_setup(unsigned int* ticket, unsigned long long* words, lo
     b.n_seqs = std::min(kSeqsPerSetup, n_seqs - s0);
     for (int q = 0; q < b.n_seqs; ++q) {
       batch.seq[q] = SeqRange{cu[s0 + q], cu[s0 + q + 1] - cu[s0 + q], s0 + q};
-      entries += words ? tiles_of(batch.seq[q].n) : 1;
+      entries += tiles_of(batch.seq[q].n, b.tile);
     }
     std::sort(batch.seq, batch.seq + b.n_seqs, [](const SeqRange& x, const SeqRange& y) { return x.n != y.n ? x.n > y.n : x.seq < y.seq; });
     const cudaError_t e = launch_early(rec_setup_kernel<kSeqsPerSetup>, grid(), 256, 0, stream, b, batch);

@@ -11,11 +11,13 @@ namespace {
 
 size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
 
+constexpr int64_t kMostBetweenRows = 1 << 26;
+
 int check_rec(const tri_inv_rec_desc* d) {
   if (!d || d->B < 1 || d->T < 0 || d->D < 1) return TRI_INV_ERR_INVALID_ARG;
   if (d->dtype != TRI_INV_F32 && d->dtype != TRI_INV_BF16) return TRI_INV_ERR_INVALID_ARG;
   if (d->mode != TRI_INV_REC_DECAY && d->mode != TRI_INV_REC_NORMED && d->mode != TRI_INV_REC_GATE) return TRI_INV_ERR_INVALID_ARG;
-  if ((long long)d->B * d->T > 0x7fffffffLL || d->D > 0x7fffff00) return TRI_INV_ERR_INVALID_ARG;
+  if ((long long)d->B * d->T > 0x7fffffffLL || d->D > kMostBetweenRows) return TRI_INV_ERR_INVALID_ARG;
   if (d->cu_seqlens) {
     if (d->B != 1 || d->n_seqs < 0 || d->cu_seqlens[0] != 0 || d->cu_seqlens[d->n_seqs] != d->T) return TRI_INV_ERR_INVALID_ARG;
     for (int s = 0; s < d->n_seqs; ++s)
@@ -27,24 +29,30 @@ int check_rec(const tri_inv_rec_desc* d) {
 }
 int seqs_of(const tri_inv_rec_desc* d) { return d->cu_seqlens ? d->n_seqs : d->B; }
 long long tokens_of(const tri_inv_rec_desc* d) { return (long long)d->B * d->T; }
-long long slots_of(const tri_inv_rec_desc* d) { return rec_slot(tokens_of(d), seqs_of(d)) + 1; }
+long long slots_of(const tri_inv_rec_desc* d, int tile) { return rec_slot(tokens_of(d), seqs_of(d), tile) + 1; }
 Rows rows_of(const tri_inv_rec_desc* d, const void* p, int64_t ld) {
   const int es = d->dtype == TRI_INV_F32 ? 4 : 2;
   return Rows{p, tokens_of(d), (__int128)d->D * es, (__int128)ld * es};
 }
+bool strides_fit(std::initializer_list<int64_t> lds) {   // sixteen rows are counted in 32 bits of bytes
+  for (int64_t ld : lds)
+    if (ld > kMostBetweenRows) return false;
+  return true;
+}
 Span states_of(const tri_inv_rec_desc* d, const void* p) { return Span{p, (__int128)seqs_of(d) * d->D * 4}; }
-Span carries_of(const tri_inv_rec_desc* d, const void* p) { return Span{p, (__int128)slots_of(d) * d->D * 4}; }
+Span carries_of(const tri_inv_rec_desc* d, const void* p) { return Span{p, (__int128)slots_of(d, kRecCarry) * d->D * 4}; }
 
 // How a walk goes: tile by tile with words between the tiles, or whole sequences.
 struct RecPlan {
+  int tile;
   bool words;
   int n_segs, cols;
   size_t table_bytes, word_bytes;   // word_bytes: with the ticket in front
   size_t bytes() const { return table_bytes + word_bytes; }
 };
-int plan(const tri_inv_rec_desc* d, RecPlan* p) {
+int plan(const tri_inv_rec_desc* d, int tile, RecPlan* p) {
   const int n_seqs = seqs_of(d);
-  auto tiles_of = [](long long n) { return std::max(1ll, (n + kRecTile - 1) / kRecTile); };
+  auto tiles_of = [&](long long n) { return std::max(1ll, (n + tile - 1) / tile); };
   long long tiles = 0, longest = 1;
   if (d->cu_seqlens) {
     for (int s = 0; s < n_seqs; ++s) {
@@ -56,6 +64,7 @@ int plan(const tri_inv_rec_desc* d, RecPlan* p) {
     longest = tiles_of(d->T);
     tiles = longest * n_seqs;
   }
+  p->tile = tile;
   p->cols = (int)(((long long)d->D + kRecChannels - 1) / kRecChannels);
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return TRI_INV_ERR_CUDA;
@@ -64,8 +73,20 @@ int plan(const tri_inv_rec_desc* d, RecPlan* p) {
   if (segs * p->cols > 0x40000000LL) return TRI_INV_ERR_INVALID_ARG;   // items are counted in 32 bits
   p->n_segs = (int)segs;
   p->table_bytes = d->cu_seqlens ? round_up((size_t)segs * sizeof(RecTile)) : 0;
-  p->word_bytes = p->words ? 256 + round_up((size_t)slots_of(d) * d->D * 8) : 0;
+  p->word_bytes = p->words ? 256 + round_up((size_t)slots_of(d, tile) * d->D * 8) : 0;
   return TRI_INV_OK;
+}
+
+// The gradient's walk and, without carries, one in front of it that forms them
+struct BackPlan {
+  RecPlan back, front;
+  size_t carry_bytes;
+  size_t bytes() const { return carry_bytes + std::max(back.bytes(), carry_bytes ? front.bytes() : 0); }
+};
+int plan_back(const tri_inv_rec_desc* d, bool with_carries, BackPlan* p) {
+  p->carry_bytes = with_carries ? 0 : round_up((size_t)slots_of(d, kRecCarry) * d->D * 4);
+  const int e = plan(d, kRecCarry, &p->back);
+  return e ? e : plan(d, kRecTile, &p->front);
 }
 
 // The arguments that do not differ between the walks; the set-up of the workspace is enqueued
@@ -80,7 +101,7 @@ int begin_walk(RecArgs& a, const RecPlan& p, const tri_inv_rec_desc* d, void* wo
   a.table = d->cu_seqlens ? table : nullptr;
   a.ticket = p.words ? (unsigned int*)((char*)workspace + p.table_bytes) : nullptr;
   a.words = p.words ? (unsigned long long*)((char*)workspace + p.table_bytes + 256) : nullptr;
-  return launch_rec_setup(a.ticket, a.words, slots_of(d) * d->D, table, d->cu_seqlens, a.n_seqs, stream) == cudaSuccess ? TRI_INV_OK : TRI_INV_ERR_CUDA;
+  return launch_rec_setup(a.ticket, a.words, slots_of(d, p.tile) * d->D, table, p.tile, d->cu_seqlens, a.n_seqs, stream) == cudaSuccess ? TRI_INV_OK : TRI_INV_ERR_CUDA;
 }
 
 int check_heads(const tri_inv_heads_desc* d) {
@@ -106,7 +127,7 @@ int tri_inv_gated_recurrence_carries(const tri_inv_rec_desc* desc, int64_t* rows
   const int rc = check_rec(desc);
   if (rc) return rc;
   if (!rows) return TRI_INV_ERR_INVALID_ARG;
-  *rows = slots_of(desc);
+  *rows = slots_of(desc, kRecCarry);
   return TRI_INV_OK;
 }
 
@@ -115,7 +136,7 @@ int tri_inv_gated_recurrence_workspace(const tri_inv_rec_desc* desc, size_t* byt
   if (rc) return rc;
   if (!bytes) return TRI_INV_ERR_INVALID_ARG;
   RecPlan p;
-  const int e = plan(desc, &p);
+  const int e = plan(desc, kRecTile, &p);
   if (e) return e;
   *bytes = p.bytes();
   return TRI_INV_OK;
@@ -127,6 +148,7 @@ int tri_inv_gated_recurrence(const void* X, int64_t ldx, const void* G, int64_t 
   if (rc) return rc;
   const int32_t D = desc->D;
   if ((tokens_of(desc) > 0 && (!X || !G || (!Y && !h_out && !carries))) || ldx < D || ldg < D || (Y && ldy < D)) return TRI_INV_ERR_INVALID_ARG;
+  if (!strides_fit({ldx, ldg, ldy})) return TRI_INV_ERR_UNSUPPORTED;
   if (!on_type(desc->dtype, X, G, Y) || !aligned4(h0) || !aligned4(h_out) || !aligned4(carries) || !aligned16(workspace)) return TRI_INV_ERR_INVALID_ARG;
   const Rows x = rows_of(desc, X, ldx), g = rows_of(desc, G, ldg), y = rows_of(desc, Y, ldy);
   const Span s0 = states_of(desc, h0), s1 = states_of(desc, h_out), sc = carries_of(desc, carries);
@@ -134,7 +156,7 @@ int tri_inv_gated_recurrence(const void* X, int64_t ldx, const void* G, int64_t 
       meets(span_of(y), s0) || meets_any(sc, span_of(x), span_of(g), span_of(y), s0))
     return TRI_INV_ERR_INVALID_ARG;
   RecPlan p;
-  const int e = plan(desc, &p);
+  const int e = plan(desc, kRecTile, &p);
   if (e) return e;
   const Span work{workspace, (__int128)p.bytes()};
   if (workspace_bytes < p.bytes() || (p.bytes() > 0 && !workspace) || meets_any(work, span_of(x), span_of(g), span_of(y), s0, s1, sc)) return TRI_INV_ERR_INVALID_ARG;
@@ -151,7 +173,7 @@ int tri_inv_selftest_recurrence_wait_timeout(const void* X, const void* G, void*
   const int rc = check_rec(desc);
   if (rc) return rc;
   RecPlan p;
-  const int e = plan(desc, &p);
+  const int e = plan(desc, kRecTile, &p);
   if (e) return e;
   if (!p.words || desc->cu_seqlens) return TRI_INV_ERR_UNSUPPORTED;
   if (!X || !G || !Y || !on_type(desc->dtype, X, G, Y) || !wait_limit_ns || !workspace || !aligned16(workspace) || workspace_bytes < p.bytes()) return TRI_INV_ERR_INVALID_ARG;
@@ -167,9 +189,13 @@ int tri_inv_selftest_recurrence_wait_timeout(const void* X, const void* G, void*
 }
 
 int tri_inv_gated_recurrence_backward_workspace(const tri_inv_rec_desc* desc, int with_carries, size_t* bytes) {
-  const int rc = tri_inv_gated_recurrence_workspace(desc, bytes);
+  const int rc = check_rec(desc);
   if (rc) return rc;
-  if (!with_carries) *bytes += round_up((size_t)slots_of(desc) * desc->D * 4);
+  if (!bytes) return TRI_INV_ERR_INVALID_ARG;
+  BackPlan p;
+  const int e = plan_back(desc, with_carries, &p);
+  if (e) return e;
+  *bytes = p.bytes();
   return TRI_INV_OK;
 }
 
@@ -180,6 +206,7 @@ int tri_inv_gated_recurrence_backward(const void* dY, int64_t lddy, const void* 
   if (rc) return rc;
   const int32_t D = desc->D;
   if ((tokens_of(desc) > 0 && (!dY || !X || !G || !dX || !dG)) || lddy < D || ldx < D || ldg < D || lddx < D || lddg < D) return TRI_INV_ERR_INVALID_ARG;
+  if (!strides_fit({lddy, ldx, ldg, lddx, lddg})) return TRI_INV_ERR_UNSUPPORTED;
   if (!on_type(desc->dtype, dY, X, G, dX, dG) || !aligned4(h0) || !aligned4(dh) || !aligned4(carries) || !aligned4(dh0) || !aligned16(workspace)) return TRI_INV_ERR_INVALID_ARG;
   const Rows dy = rows_of(desc, dY, lddy), x = rows_of(desc, X, ldx), g = rows_of(desc, G, ldg), dx = rows_of(desc, dX, lddx), dg = rows_of(desc, dG, lddg);
   const Span s0 = states_of(desc, h0), sd = states_of(desc, dh), s1 = states_of(desc, dh0), sc = carries_of(desc, carries);
@@ -188,25 +215,26 @@ int tri_inv_gated_recurrence_backward(const void* dY, int64_t lddy, const void* 
   if (meets_any(s1, span_of(dy), span_of(x), span_of(g), span_of(dx), span_of(dg), s0, sc) || (dh0 != dh && meets(s1, sd)) || meets_any(span_of(dx), s0, sd, sc) ||
       meets_any(span_of(dg), s0, sd, sc))
     return TRI_INV_ERR_INVALID_ARG;
-  RecPlan p;
-  const int e = plan(desc, &p);
+  BackPlan p;
+  const int e = plan_back(desc, carries != nullptr, &p);
   if (e) return e;
-  const size_t need = p.bytes() + (carries ? 0 : round_up((size_t)slots_of(desc) * D * 4));
+  const size_t need = p.bytes();
   if (workspace_bytes < need || (need > 0 && !workspace) ||
       meets_any(Span{workspace, (__int128)need}, span_of(dy), span_of(x), span_of(g), span_of(dx), span_of(dg), s0, sd, s1, sc))
     return TRI_INV_ERR_INVALID_ARG;
   RecArgs a{};
   a.x = X; a.ld_x = ldx; a.g = G; a.ld_g = ldg; a.h0 = h0;
-  a.carries = carries ? (float*)carries : (float*)((char*)workspace + p.bytes());
+  a.carries = carries ? (float*)carries : (float*)workspace;
+  void* control = (char*)workspace + p.carry_bytes;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   if (!carries) {
-    const int b = begin_walk(a, p, desc, workspace, stream);
-    if (b || p.n_segs == 0) return b;
+    const int b = begin_walk(a, p.front, desc, control, stream);
+    if (b || p.front.n_segs == 0) return b;
     if (launch_gated_recurrence(a, desc->dtype, stream) != cudaSuccess) return TRI_INV_ERR_CUDA;
   }
   a.dy = dY; a.ld_dy = lddy; a.dx = dX; a.ld_dx = lddx; a.dg = dG; a.ld_dg = lddg; a.dh = dh; a.dh0 = dh0;
-  const int b = begin_walk(a, p, desc, workspace, stream);
-  if (b || p.n_segs == 0) return b;
+  const int b = begin_walk(a, p.back, desc, control, stream);
+  if (b || p.back.n_segs == 0) return b;
   return launch_gated_recurrence_backward(a, desc->dtype, stream) == cudaSuccess ? TRI_INV_OK : TRI_INV_ERR_CUDA;
 }
 
