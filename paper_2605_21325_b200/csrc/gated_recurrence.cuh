@@ -8,7 +8,7 @@
 //     e_t = dy_t + c_{t+1},   c_t = a_t e_t,   dx_t = m_t e_t (m: what multiplies x in u),   dh0 = c_0,
 //     dg_t = e_t w_t,   w_t = a_t h_{t-1} (decay),   a_t h_{t-1} - a_t^2 / m_t x_t (normed),   (h_{t-1} - x_t) a_t (1 - a_t) (gate)
 //
-// Both are walks over tiles of kRecTile (kRecCarry) tokens of kRecChannels channels.  A tile is an affine map of what enters it, (P, H): h -> P h + H,
+// Both are walks over tiles of some tokens and channels.  A tile is an affine map of what enters it, (P, H): h -> P h + H,
 // and so is a run of tiles; the tokens of a warp, the warps of a tile and the tiles of a sequence join by the same rule.
 #pragma once
 #include "common.cuh"
@@ -16,8 +16,11 @@
 namespace tri_inv {
 
 constexpr int kRecCarry = TRI_INV_REC_TILE;   // tokens from one carried state to the next
-constexpr int kRecTile = 128;                 // tokens of a tile of the forward walk; the gradient's have kRecCarry
-constexpr int kRecChannels = 64;              // channels of a tile
+constexpr int kRecWarps = 4;     // warps of tokens of a block
+constexpr int kRecGroups = 2;    // lane groups of a warp, each with tokens of its own (RecShape)
+constexpr int kRecTok = 16, kRecBackTok = 8;                                                // tokens of a lane, forwards and in the gradient
+constexpr int kRecThreads = 32 * kRecWarps + 32;                                            // and a thread for each channel that joins them
+constexpr int kRecTile = kRecWarps * kRecGroups * kRecTok, kRecBackTile = kRecWarps * kRecGroups * kRecBackTok, kRecChannels = 64 / kRecGroups;   // of a tile
 
 // An entry of the table of packed sequences: a tile, or a whole sequence (index 0)
 struct RecTile {
@@ -99,57 +102,38 @@ template <> struct RecLane<float> {
   }
 };
 
-// (1 - e^g) / -g from its series up to the seventh power: for |g| <= 1/4 the first term left out is g^7 / 8! < 2^-29
-__device__ __forceinline__ Pair rec_slope(Pair g) {
-  Pair s = twice(1.f / 5040.f);
-  s = fma2(s, g, twice(1.f / 720.f));
-  s = fma2(s, g, twice(1.f / 120.f));
-  s = fma2(s, g, twice(1.f / 24.f));
-  s = fma2(s, g, twice(1.f / 6.f));
-  s = fma2(s, g, twice(0.5f));
-  return fma2(s, g, twice(1.f));
-}
-// e^g for g in -inf .. 88 as 2^(g log2 e), the product in two parts t + r (the second changes the power by its factor 1 + r ln 2): off by the power's own error, 2^-22.5.  Results below 2^-126 are 0.
-__device__ __forceinline__ float rec_above(float g) { float y; asm("max.NaN.f32 %0, %1, 0fC3480000;" : "=f"(y) : "f"(g)); return y; }   // -200: so that t and r are finite
+// e^g as 2^(g log2 e), off by the power's own error, 2^-22.5, and by that of the rounded product, |g| 2^-24, which is what a rounding of g itself would change.  Results below 2^-126 are 0.
 __device__ __forceinline__ float rec_power(float t) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(t)); return y; }
-__device__ __forceinline__ Pair rec_exp(float gx, float gy) {
-  const Pair g = pair(rec_above(gx), rec_above(gy)), log2e = twice(1.44269504088896341f);
-  const Pair t = mul2(g, log2e), r = fma2(g, log2e, mul2(t, twice(-1.f)));
-  const float2 x = both(t);
-  const Pair p = pair(rec_power(x.x), rec_power(x.y));
-  return fma2(mul2(p, twice(0.693147180559945309f)), r, p);
+__device__ __forceinline__ Pair rec_exp(Pair g) {
+  const float2 t = both(mul2(g, twice(1.44269504088896341f)));
+  return pair(rec_power(t.x), rec_power(t.y));
 }
 __device__ __forceinline__ float rec_reciprocal(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-__device__ __forceinline__ float rec_over_root(float x) { float y; asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float rec_root(float x) { float y; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
-// a and m (what multiplies x).  Near 1, a is formed as 1 minus what it lacks, so that its error is a rounding's and has no preferred side: a state sums a's errors over as many tokens as
-// it remembers.
+// a and m (what multiplies x).  normed: 1 - a^2 = -2 sinh(g) e^g, which does not cancel, for |g| <= 1/4, where the first term left out of sinh(g) / g is g^6 / 7! < 2^-24.  gate: both from the smaller one, the larger as
+// 1 minus it, so that its error is a rounding's and has no preferred side.
 template <int MODE>
 __device__ __forceinline__ void rec_factors(Pair gp, Pair& a, Pair& m) {
   const float2 g = both(gp);
+  const Pair one = twice(1.f), minus = twice(-1.f);
   if constexpr (MODE == kRecDecay) {
-    a = rec_exp(g.x, g.y);
-    m = twice(1.f);
+    a = rec_exp(gp);
+    m = one;
   } else if constexpr (MODE == kRecNormed) {
-    const float2 e = both(rec_exp(g.x, g.y));
-    const bool nx = fabsf(g.x) <= 0.25f, ny = fabsf(g.y) <= 0.25f;
-    const Pair minus = twice(-1.f), one = twice(1.f);
-    const Pair qn = mul2(mul2(gp, minus), rec_slope(gp)), qf = fma2(pair(e.x, e.y), minus, one);   // 1 - a
-    const float2 n = both(qn), f = both(qf), an = both(fma2(qn, minus, one));
-    a = pair(nx ? an.x : e.x, ny ? an.y : e.y);
-    const Pair q = pair(nx ? n.x : f.x, ny ? n.y : f.y), sp = mul2(q, add2(a, one));   // 1 - a^2
-    const float2 s = both(sp);
-    m = mul2(sp, pair(s.x >= 1.17549435e-38f ? rec_over_root(s.x) : 0.f, s.y >= 1.17549435e-38f ? rec_over_root(s.y) : 0.f));
+    a = rec_exp(gp);
+    const Pair y = mul2(gp, gp), near = mul2(mul2(gp, a), fma2(fma2(y, twice(-1.f / 60.f), twice(-1.f / 3.f)), y, twice(-2.f))), far = fma2(mul2(a, minus), a, one);
+    const float2 n = both(near), f = both(far);   // 1 - a^2
+    m = pair(rec_root(fmaxf(fabsf(g.x) <= 0.25f ? n.x : f.x, 0.f)), rec_root(fmaxf(fabsf(g.y) <= 0.25f ? n.y : f.y, 0.f)));
   } else {
-    const Pair ep = rec_exp(-fabsf(g.x), -fabsf(g.y)), one = twice(1.f);
-    const float2 d = both(add2(ep, one));
-    const Pair rp = pair(rec_reciprocal(d.x), rec_reciprocal(d.y)), sp = mul2(ep, rp), bp = fma2(sp, twice(-1.f), one);   // s: the smaller of a and 1 - a
+    const Pair e = rec_exp(pair(-fabsf(g.x), -fabsf(g.y)));
+    const float2 d = both(add2(e, one));
+    const Pair rp = pair(rec_reciprocal(d.x), rec_reciprocal(d.y)), sp = mul2(e, rp), bp = fma2(sp, minus, one);   // s: the smaller of a and 1 - a
     const float2 r = both(rp), s = both(sp), b = both(bp);
     a = pair(g.x >= 0.f ? b.x : s.x, g.y >= 0.f ? b.y : s.y);
     m = pair(g.x >= 0.f ? s.x : r.x, g.y >= 0.f ? s.y : r.y);
   }
 }
-
 template <int MODE>
 __device__ __forceinline__ Pair rec_input(Pair m, Pair x) {   // u
   if constexpr (MODE == kRecDecay) return x;
@@ -162,6 +146,26 @@ __device__ __forceinline__ Pair rec_step(Pair a, Pair h, Pair u) {
   const float2 x = both(a), y = both(h), z = both(u);
   return pair(rec_step(x.x, y.x, z.x), rec_step(x.y, y.y, z.y));
 }
+// The maps of the lane groups of a warp join: (P, H) of a lane's group becomes that of the whole warp, (before_P, before_H) that of the groups in front of it (BACK: behind it).
+template <bool BACK>
+__device__ __forceinline__ void rec_join_groups(Pair& P, Pair& H, Pair& before_P, Pair& before_H) {
+  before_P = twice(1.f);
+  before_H = twice(0.f);
+#pragma unroll
+  for (int m = 32 / kRecGroups; m < 32; m <<= 1) {
+    const float2 p = both(P), h = both(H);
+    const Pair op = pair(__shfl_xor_sync(0xffffffffu, p.x, m), __shfl_xor_sync(0xffffffffu, p.y, m)), oh = pair(__shfl_xor_sync(0xffffffffu, h.x, m), __shfl_xor_sync(0xffffffffu, h.y, m));
+    const bool second = ((threadIdx.x & m) != 0) != BACK;   // the other half comes before this lane's
+    if (second) {
+      before_H = rec_step(before_P, oh, before_H);
+      before_P = mul2(before_P, op);
+      H = rec_step(P, oh, H);
+    } else {
+      H = rec_step(op, H, oh);
+    }
+    P = mul2(P, op);
+  }
+}
 __device__ __forceinline__ bool any_zero(Pair a) { const float2 x = both(a); return x.x == 0.f || x.y == 0.f; }
 
 // How a tensor's rows are moved: 16 bytes (everything aligned to them), 4 bytes, or value by value (bf16 at odd places)
@@ -172,6 +176,13 @@ __device__ __forceinline__ int rec_access(const void* p, long long ld) {
   return (at & 15) == 0 ? kRecWide : (at & 3) == 0 ? kRecFours : kRecSingle;
 }
 
+// Two neighbouring 16-bit values, of which those past `width` are zero
+template <class T>
+__device__ __forceinline__ uint32_t rec_half_words(const T* row, int c, int width) {
+  const uint16_t* p = reinterpret_cast<const uint16_t*>(row);
+  const uint32_t lo = c < width ? p[c] : 0u, hi = c + 1 < width ? p[c + 1] : 0u;
+  return lo | hi << 16;
+}
 // A lane's channels c, c + 1 of a row of `width`: those past the last read as zero and are not written.
 template <class T>
 __device__ __forceinline__ typename RecLane<T>::Raw rec_load(const T* row, int c, int width, int access) {
@@ -180,9 +191,7 @@ __device__ __forceinline__ typename RecLane<T>::Raw rec_load(const T* row, int c
     return make_uint2(c < width ? __float_as_uint(row[c]) : 0u, c + 1 < width ? __float_as_uint(row[c + 1]) : 0u);
   } else {
     if (access != kRecSingle && c + 1 < width) return *reinterpret_cast<const uint32_t*>(row + c);
-    const uint16_t* p = reinterpret_cast<const uint16_t*>(row);
-    const uint32_t lo = c < width ? p[c] : 0u, hi = c + 1 < width ? p[c + 1] : 0u;
-    return lo | hi << 16;
+    return rec_half_words(row, c, width);
   }
 }
 template <class T>
@@ -210,62 +219,64 @@ __device__ __forceinline__ void rec_commit() { asm volatile("cp.async.commit_gro
 template <int N>
 __device__ __forceinline__ void rec_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Asks for a warp's ROWS rows of a tile: rows row0 .. of which `rows` exist, channels c0 .. of `width`; what does not exist reads as zero.
-template <class T, int ROWS>
-__device__ __forceinline__ void rec_request(unsigned char* smem, const T* base, long long ld, long long row0, int rows, int c0, int width, int access) {
-  constexpr int BYTES = kRecChannels * (int)sizeof(T), LANES = BYTES / 16, AT_ONCE = 32 / LANES;   // of a row; lanes of 16 bytes; rows
-  static_assert(ROWS % AT_ONCE == 0, "");
-  const int lane = threadIdx.x & 31;
-  const int left = (width - c0) * (int)sizeof(T);   // bytes of a row from the tile's first channel on
-  const uint32_t to = (uint32_t)__cvta_generic_to_shared(smem);
-  if (access == kRecWide) {
-    const int r0 = lane / LANES, at = 16 * (lane % LANES), bytes = min(16, left - at);
-    const T* from = base + (row0 + r0) * ld + c0 + at / (int)sizeof(T);
-    const uint32_t there = to + r0 * BYTES + at;
-    if (rows >= ROWS && left >= BYTES) {
+// The lanes of a warp stand in kRecGroups groups, each of which has TOK tokens behind one another, two channels a lane.  In shared memory a row follows the one before, and a
+// group's rows are one row further on, so that the groups' reads meet in no bank.
+template <class T, int TOK>
+struct RecShape {
+  static constexpr int GROUPS = kRecGroups, CHANNELS = kRecChannels, ROW = CHANNELS * (int)sizeof(T), LANES = 32 / GROUPS, GROUP_BYTES = (TOK + 1) * ROW, WARP_BYTES = GROUPS * GROUP_BYTES;
+  static constexpr int WARP_TOK = GROUPS * TOK, TILE = kRecWarps * WARP_TOK, TENSOR = kRecWarps * WARP_BYTES;
+  static constexpr int AT_ONCE = 512 / ROW;   // rows of a warp's 16-byte copies
+  static_assert(TOK % AT_ONCE == 0 || AT_ONCE % TOK == 0, "");
+  // of a lane: its group, its first channel, where its values begin in a warp's rows
+  static __device__ __forceinline__ int group() { return (threadIdx.x & 31) / LANES; }
+  static __device__ __forceinline__ int channel() { return 2 * ((threadIdx.x & 31) % LANES); }
+  static __device__ __forceinline__ int place() { return group() * GROUP_BYTES + channel() * (int)sizeof(T); }
+  // bytes of a lane's first 16, from the tile's first value on, in memory and in the warp's rows
+  static __device__ __forceinline__ long long copy_from(long long ld, int row0) {
+    const int lane = threadIdx.x & 31;
+    return (row0 + lane * 16 / ROW) * ld * (int)sizeof(T) + lane * 16 % ROW;
+  }
+  static __device__ __forceinline__ uint32_t copy_to() { const int lane = threadIdx.x & 31; return 16 * lane + lane * 16 / ROW / TOK * ROW; }
+  // Asks for a warp's rows of a tile, where every row and channel exists and 16 bytes can be moved; ld in values
+  static __device__ __forceinline__ void request_whole(uint32_t warp_smem, const char* from, long long ld) {
+    const uint32_t to = warp_smem + copy_to();
 #pragma unroll
-      for (int i = 0; i < ROWS / AT_ONCE; ++i) rec_copy(there + i * AT_ONCE * BYTES, from + i * AT_ONCE * ld, 16);
-    } else {
+    for (int i = 0; i < WARP_TOK / AT_ONCE; ++i) {
+      rec_copy(to + i * 512 + i * AT_ONCE / TOK * ROW, from, 16);
+      from += ld * (AT_ONCE * (int)sizeof(T));
+    }
+  }
+  // ... where not: rows row0 .. of which `rows` exist, channels c0 .. of `width`; what does not exist reads as zero
+  static __device__ __forceinline__ void request(uint32_t warp_smem, const T* base, long long ld, long long row0, int rows, int c0, int width, int access) {
+    const int lane = threadIdx.x & 31;
+    if (access == kRecWide) {
+      const int left = (width - c0) * (int)sizeof(T), at = lane * 16 % ROW, bytes = min(16, left - at), r0 = lane * 16 / ROW;
 #pragma unroll
-      for (int i = 0; i < ROWS / AT_ONCE; ++i) {
+      for (int i = 0; i < WARP_TOK / AT_ONCE; ++i) {
         const bool in = r0 + i * AT_ONCE < rows && bytes > 0;
-        rec_copy(there + i * AT_ONCE * BYTES, in ? from + i * AT_ONCE * ld : base, in ? bytes : 0);
+        rec_copy(warp_smem + copy_to() + i * 512 + i * AT_ONCE / TOK * ROW, in ? base + (row0 + r0 + i * AT_ONCE) * ld + c0 + at / (int)sizeof(T) : base, in ? bytes : 0);
+      }
+    } else {
+      const int first = group() * TOK, c = c0 + channel();
+      const uint32_t to = warp_smem + place();
+      if (sizeof(T) == 4 || (access == kRecFours && (width - c0 >= CHANNELS || width % 2 == 0))) {
+#pragma unroll
+        for (int k = 0; k < TOK; ++k)
+#pragma unroll
+          for (int j = 0; j < (int)sizeof(T) / 2; ++j) {
+            const bool in = first + k < rows && c + j < width;
+            rec_copy4(to + k * ROW + 4 * j, in ? base + (row0 + first + k) * ld + c + j : base, in ? 4 : 0);
+          }
+      } else {
+        uint32_t raw[TOK];
+#pragma unroll
+        for (int k = 0; k < TOK; ++k) raw[k] = first + k < rows ? rec_half_words(base + (row0 + first + k) * ld, c, width) : 0u;
+#pragma unroll
+        for (int k = 0; k < TOK; ++k) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + k * ROW), "r"(raw[k]) : "memory");
       }
     }
-  } else if (access == kRecFours && (left % 4 == 0 || left >= BYTES)) {
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-      for (int i = 0; i < BYTES / 128; ++i) {
-        const int at = 128 * i + 4 * lane;
-        const bool in = r < rows && at < left;
-        rec_copy4(to + r * BYTES + at, in ? base + (row0 + r) * ld + c0 + at / (int)sizeof(T) : base, in ? 4 : 0);
-      }
-  } else {
-    typename RecLane<T>::Raw raw[ROWS];
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) raw[r] = r < rows ? rec_load(base + (row0 + r) * ld, c0 + 2 * lane, width, access) : typename RecLane<T>::Raw{};
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) *reinterpret_cast<typename RecLane<T>::Raw*>(smem + r * BYTES + 2 * lane * (int)sizeof(T)) = raw[r];
   }
-}
-
-// The same where every row and channel exists and 16 bytes can be moved: `from` is the lane's first 16 bytes, `step` the bytes between those that it copies.
-template <class T, int ROWS>
-__device__ __forceinline__ void rec_request_whole(uint32_t to, const char* from, long long step) {
-  constexpr int BYTES = kRecChannels * (int)sizeof(T), AT_ONCE = 512 / BYTES;
-#pragma unroll
-  for (int i = 0; i < ROWS / AT_ONCE; ++i) {
-    rec_copy(to + i * AT_ONCE * BYTES, from, 16);
-    from += step;
-  }
-}
-template <class T>
-__device__ __forceinline__ long long rec_lane_bytes(long long ld, int row) {   // of a lane's first 16 bytes, from a tile's first value on
-  constexpr int LANES = kRecChannels * (int)sizeof(T) / 16;
-  const int lane = threadIdx.x & 31;
-  return (row + lane / LANES) * ld * (int)sizeof(T) + 16 * (lane % LANES);
-}
+};
 
 __device__ __forceinline__ unsigned long long rec_peek(const unsigned long long* p) {
   unsigned long long v;
@@ -288,7 +299,7 @@ __device__ __forceinline__ unsigned long long rec_now() {
 // from the nearest on until one forgets what came before (P = 0; a tile that knows what leaves it says so with P = 0, the first one always does).
 // A word that is missing for the time limit raises the status word, and the NaN that is returned then goes on with this tile's own word, so that no later tile waits as long.
 __device__ __forceinline__ float rec_look_back(const unsigned long long* word, long long step, int count, unsigned long long limit, int* status) {
-  constexpr int AT_ONCE = 8;   // words that are asked for together
+  constexpr int AT_ONCE = 4;   // words that are asked for together
   constexpr unsigned long long NONE = ~0ull;
   float P = 1.f, H = 0.f;
   unsigned long long begin = 0;

@@ -6,13 +6,13 @@
 namespace tri_inv {
 namespace {
 
-constexpr int kWarps = 8, kTok = kRecCarry / kWarps, kStages = 3;
-constexpr int kThreads = 32 * kWarps + kRecChannels;   // warps of tokens, and a thread for each channel that joins them
-template <class T> constexpr int kTensor = kRecCarry * kRecChannels * (int)sizeof(T);   // bytes of a tile of one tensor
-
+constexpr int kTok = kRecBackTok, kStages = 3;
+template <int MODE> constexpr int kBlocks = MODE == kRecDecay ? 4 : 3;   // an SM's, by the registers that a lane's tokens take
 // What a warp's tokens of a tile make of x, from what the first pass over them left: a, m
-template <int MODE> struct Held { Pair a[kTok], m[kTok]; };
-template <> struct Held<kRecDecay> { Pair a[kTok]; };
+template <int MODE> struct Factors { Pair a[kTok], m[kTok]; };
+template <> struct Factors<kRecDecay> { Pair a[kTok]; };
+// and the maps of its lane groups: (fP, fH) of those in front of the lane's, (bP, bC) of those behind it
+template <int MODE> struct Held : Factors<MODE> { Pair fP, fH, bP, bC; };
 
 // w: what multiplies e in dg, from the state in front of the token
 template <int MODE>
@@ -34,22 +34,24 @@ __device__ __forceinline__ Pair none_where_zero(Pair a, Pair v) {
 }
 
 template <class T, int MODE, bool WORDS>
-__global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(const __grid_constant__ RecArgs a) {
+__global__ void __launch_bounds__(kRecThreads, kBlocks<MODE>) gated_recurrence_backward_kernel(const __grid_constant__ RecArgs a) {
+  using Shape = RecShape<T, kTok>;
+  constexpr int CH = Shape::CHANNELS, TILE = Shape::TILE, ROW = Shape::ROW;
   extern __shared__ __align__(128) unsigned char stages[];
-  __shared__ __align__(16) float2 part[2][kWarps][kRecChannels];   // (P, H) of each warp's tokens; then (P, C) of all tokens of the tile behind them
-  __shared__ __align__(8) float side[2][kWarps][kRecChannels];     // C: what each warp's tokens pass on, where nothing reaches them from behind; then the state in front of them
-  __shared__ __align__(8) float entry[2][kRecChannels];            // what reaches a tile from behind
+  __shared__ __align__(16) float2 part[2][kRecWarps][CH];   // (P, H) of each warp's tokens; then (P, C) of all tokens of the tile behind them
+  __shared__ __align__(8) float side[2][kRecWarps][CH];     // C: what each warp's tokens pass on, where nothing reaches them from behind; then the state in front of them
+  __shared__ __align__(8) float entry[2][CH];            // what reaches a tile from behind
   __shared__ RecAt ring[kRecRing];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int items = a.n_segs * a.cols;
   constexpr int es = sizeof(T);
-  RecFeed<WORDS, kRecCarry, 5, true> feed{a, {a.ld_x * es, a.ld_g * es, a.ld_dy * es, a.ld_dx * es, a.ld_dg * es}, es};
+  RecFeed<WORDS, TILE, 5, true> feed{a, {a.ld_x * es, a.ld_g * es, a.ld_dy * es, a.ld_dx * es, a.ld_dg * es}, es};
   wait_for_predecessor();
-  if (tid == 32 * kWarps) feed.begin(ring, 4);
+  if (tid == 32 * kRecWarps) feed.begin(ring, 4);
   __syncthreads();
 
-  if (warp >= kWarps) {   // a channel
-    const int ch = tid - 32 * kWarps;
+  if (warp >= kRecWarps) {   // a channel
+    const int ch = tid - 32 * kRecWarps;
     const unsigned long long limit = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
     float carried = 0.f;
     for (int i = 0;; ++i) {
@@ -59,18 +61,18 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
       const int c = t.c0 + ch, behind = t.tiles - 1 - t.index;
       const bool in = c < a.D, first = t.index == 0, last = behind == 0;
       const long long at = t.slot * a.D + c, state = (long long)t.seq * a.D + c;
-      float h = !in ? 0.f : !first ? a.carries[at - a.D] : a.h0 ? a.h0[state] : 0.f;   // the state in front of the tile
+      float h = !in ? 0.f : !first ? a.carries[(rec_slot(t.begin, t.seq, kRecCarry) + (long long)t.index * (TILE / kRecCarry) - 1) * a.D + c] : a.h0 ? a.h0[state] : 0.f;   // the state in front of the tile
       float e = last && in && a.dh ? a.dh[state] : 0.f;
-      rec_meet(kRecMaps + (i & 1), kThreads);
-      float P = 1.f, C = 0.f, kept[kWarps];
+      rec_meet(kRecMaps + (i & 1), kRecThreads);
+      float P = 1.f, C = 0.f, kept[kRecWarps];
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
+      for (int w = 0; w < kRecWarps; ++w) {
         const float2 q = part[i & 1][w][ch];
         kept[w] = h;
         h = rec_step(q.x, h, q.y);
       }
 #pragma unroll
-      for (int w = kWarps - 1; w >= 0; --w) {
+      for (int w = kRecWarps - 1; w >= 0; --w) {
         const float p = part[i & 1][w][ch].x, c_own = side[i & 1][w][ch];
         part[i & 1][w][ch] = make_float2(P, C);
         side[i & 1][w][ch] = kept[w];
@@ -93,35 +95,31 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
       }
       entry[i & 1][ch] = e;
       if (ch == 0) feed.give(&ring[(i + 4) & (kRecRing - 1)]);
-      rec_arrive(kRecEntry + (i & 1), kThreads);
+      rec_arrive(kRecEntry + (i & 1), kRecThreads);
     }
     return;
   }
 
   using Lane = RecLane<T>;
   using Raw = typename Lane::Raw;
-  constexpr int ROW = kRecChannels * es;
   const T *X = (const T*)a.x, *G = (const T*)a.g, *DY = (const T*)a.dy;
   const int x_access = rec_access<T>(X, a.ld_x), g_access = rec_access<T>(G, a.ld_g), dy_access = rec_access<T>(DY, a.ld_dy);
   const int dx_access = rec_access<T>(a.dx, a.ld_dx), dg_access = rec_access<T>(a.dg, a.ld_dg), most = es == 4 ? kRecWide : kRecFours;
   const bool wide = x_access == kRecWide && g_access == kRecWide && dy_access == kRecWide, plain = dx_access <= most && dg_access <= most;   // plain: whole lanes can be written
-  const char *x_from = (const char*)X + rec_lane_bytes<T>(a.ld_x, warp * kTok), *g_from = (const char*)G + rec_lane_bytes<T>(a.ld_g, warp * kTok),
-             *dy_from = (const char*)DY + rec_lane_bytes<T>(a.ld_dy, warp * kTok);
-  const uint32_t lane_to = (uint32_t)__cvta_generic_to_shared(stages) + warp * kTok * ROW + 16 * lane;
+  const int first = warp * Shape::WARP_TOK;
+  const char *x_from = (const char*)X + Shape::copy_from(a.ld_x, first), *g_from = (const char*)G + Shape::copy_from(a.ld_g, first), *dy_from = (const char*)DY + Shape::copy_from(a.ld_dy, first);
+  const uint32_t warp_smem = (uint32_t)__cvta_generic_to_shared(stages) + warp * Shape::WARP_BYTES;
   auto request = [&](const RecAt& t, int stage) {
     if (t.item < items) {
+      const uint32_t to = warp_smem + stage * 3 * Shape::TENSOR;
       if (t.whole && wide) {
-        const uint32_t to = lane_to + stage * 3 * kTensor<T>;
-        constexpr int at_once = 512 / ROW * es;
-        rec_request_whole<T, kTok>(to, x_from + t.at[0], a.ld_x * at_once);
-        rec_request_whole<T, kTok>(to + kTensor<T>, g_from + t.at[1], a.ld_g * at_once);
-        rec_request_whole<T, kTok>(to + 2 * kTensor<T>, dy_from + t.at[2], a.ld_dy * at_once);
+        Shape::request_whole(to, x_from + t.at[0], a.ld_x);
+        Shape::request_whole(to + Shape::TENSOR, g_from + t.at[1], a.ld_g);
+        Shape::request_whole(to + 2 * Shape::TENSOR, dy_from + t.at[2], a.ld_dy);
       } else {
-        const int first = warp * kTok;
-        unsigned char* to = stages + stage * 3 * kTensor<T> + first * ROW;
-        rec_request<T, kTok>(to, X, a.ld_x, t.tok0 + first, t.n - first, t.c0, a.D, x_access);
-        rec_request<T, kTok>(to + kTensor<T>, G, a.ld_g, t.tok0 + first, t.n - first, t.c0, a.D, g_access);
-        rec_request<T, kTok>(to + 2 * kTensor<T>, DY, a.ld_dy, t.tok0 + first, t.n - first, t.c0, a.D, dy_access);
+        Shape::request(to, X, a.ld_x, t.tok0 + first, t.n - first, t.c0, a.D, x_access);
+        Shape::request(to + Shape::TENSOR, G, a.ld_g, t.tok0 + first, t.n - first, t.c0, a.D, g_access);
+        Shape::request(to + 2 * Shape::TENSOR, DY, a.ld_dy, t.tok0 + first, t.n - first, t.c0, a.D, dy_access);
       }
     }
     rec_commit();
@@ -135,14 +133,14 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
     const int stage_next = 3 - stage - stage_before;
     request(ring[(i + 1) & (kRecRing - 1)], stage_next);
     const bool has_now = ring[i & (kRecRing - 1)].item < items;
-    const int place = warp * kTok * ROW + 2 * lane * es;
+    const int place = warp * Shape::WARP_BYTES + Shape::place();
     bool now_resets = false;
     if (has_now) {
       rec_wait<1>();
       __syncwarp();
-      const unsigned char* sx = stages + stage * 3 * kTensor<T> + place;
-      auto read = [&](int tensor, int k) { return Lane::widen(*reinterpret_cast<const Raw*>(sx + tensor * kTensor<T> + k * ROW)); };
-      const int left = ring[i & (kRecRing - 1)].n - warp * kTok;
+      const unsigned char* sx = stages + stage * 3 * Shape::TENSOR + place;
+      auto read = [&](int tensor, int k) { return Lane::widen(*reinterpret_cast<const Raw*>(sx + tensor * Shape::TENSOR + k * ROW)); };
+      const int left = ring[i & (kRecRing - 1)].n - first - Shape::group() * kTok;   // of the lane's tokens
       Pair P = twice(1.f), H = twice(0.f), C = twice(0.f);
 #pragma unroll
       for (int k = 0; k < kTok; ++k) {
@@ -150,7 +148,7 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
         rec_factors<MODE>(read(1, k), now.a[k], m);
         if constexpr (MODE != kRecDecay) now.m[k] = m;
       }
-      if (left < kTok) {
+      if (!ring[i & (kRecRing - 1)].whole) {
 #pragma unroll
         for (int k = 0; k < kTok; ++k)
           if (k >= left) {
@@ -177,19 +175,26 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
           C = none_where_zero(now.a[kTok - 1 - k], mul2(now.a[kTok - 1 - k], add2(C, read(2, kTok - 1 - k))));
         }
       }
+      Pair same = P;
+      rec_join_groups<true>(same, C, now.bP, now.bC);
+      rec_join_groups<false>(P, H, now.fP, now.fH);
       const float2 pp = both(P), hh = both(H), cc = both(C);
-      *reinterpret_cast<float4*>(&part[i & 1][warp][2 * lane]) = make_float4(pp.x, hh.x, pp.y, hh.y);
-      *reinterpret_cast<float2*>(&side[i & 1][warp][2 * lane]) = cc;
-      rec_arrive(kRecMaps + (i & 1), kThreads);
+      if (lane < Shape::LANES) {
+        *reinterpret_cast<float4*>(&part[i & 1][warp][Shape::channel()]) = make_float4(pp.x, hh.x, pp.y, hh.y);
+        *reinterpret_cast<float2*>(&side[i & 1][warp][Shape::channel()]) = cc;
+      }
+      rec_arrive(kRecMaps + (i & 1), kRecThreads);
     }
     if (i > 0) {
-      const unsigned char* sx = stages + stage_before * 3 * kTensor<T> + place;
-      auto read = [&](int tensor, int k) { return Lane::widen(*reinterpret_cast<const Raw*>(sx + tensor * kTensor<T> + k * ROW)); };
-      rec_meet(kRecEntry + ((i - 1) & 1), kThreads);
+      const unsigned char* sx = stages + stage_before * 3 * Shape::TENSOR + place;
+      auto read = [&](int tensor, int k) { return Lane::widen(*reinterpret_cast<const Raw*>(sx + tensor * Shape::TENSOR + k * ROW)); };
+      rec_meet(kRecEntry + ((i - 1) & 1), kRecThreads);
       const RecAt& p = ring[(i - 1) & (kRecRing - 1)];
-      const float4 q = *reinterpret_cast<const float4*>(&part[(i - 1) & 1][warp][2 * lane]);
-      const float2 s = *reinterpret_cast<const float2*>(&side[(i - 1) & 1][warp][2 * lane]), e0 = *reinterpret_cast<const float2*>(&entry[(i - 1) & 1][2 * lane]);
+      const float4 q = *reinterpret_cast<const float4*>(&part[(i - 1) & 1][warp][Shape::channel()]);
+      const float2 s = *reinterpret_cast<const float2*>(&side[(i - 1) & 1][warp][Shape::channel()]), e0 = *reinterpret_cast<const float2*>(&entry[(i - 1) & 1][Shape::channel()]);
       Pair h = pair(s.x, s.y), C = rec_step(pair(q.x, q.z), pair(e0.x, e0.y), pair(q.y, q.w)), w[kTok];
+      h = rec_step(before.fP, h, before.fH);
+      C = rec_step(before.bP, C, before.bC);
       auto m_of = [&](int k) {
         if constexpr (MODE == kRecDecay) return twice(1.f);
         else return before.m[k];
@@ -201,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
           w[k] = weight<MODE>(before.a[k], m_of(k), h, x);
           h = fma2(before.a[k], h, rec_input<MODE>(m_of(k), x));
         }
-        char *dx_row = (char*)a.dx + p.at[3] + (warp * kTok * a.ld_dx + 2 * lane) * es, *dg_row = (char*)a.dg + p.at[4] + (warp * kTok * a.ld_dg + 2 * lane) * es;
+        char *dx_row = (char*)a.dx + p.at[3] + ((first + Shape::group() * kTok) * a.ld_dx + Shape::channel()) * es, *dg_row = (char*)a.dg + p.at[4] + ((first + Shape::group() * kTok) * a.ld_dg + Shape::channel()) * es;
         const uint32_t dx_step = (uint32_t)a.ld_dx * es, dg_step = (uint32_t)a.ld_dg * es;
 #pragma unroll
         for (int k = kTok - 1; k >= 0; --k) {
@@ -211,9 +216,9 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_backward_kernel(
           C = mul2(before.a[k], e);
         }
       } else {
-        const int left = p.n - warp * kTok, c = p.c0 + 2 * lane;
-        T* dx_row = (T*)a.dx + (p.tok0 + warp * kTok) * a.ld_dx;
-        T* dg_row = (T*)a.dg + (p.tok0 + warp * kTok) * a.ld_dg;
+        const int at = first + Shape::group() * kTok, left = p.n - at, c = p.c0 + Shape::channel();
+        T* dx_row = (T*)a.dx + (p.tok0 + at) * a.ld_dx;
+        T* dg_row = (T*)a.dg + (p.tok0 + at) * a.ld_dg;
 #pragma unroll
         for (int k = 0; k < kTok; ++k) {
           const Pair x = read(0, k);
@@ -249,10 +254,10 @@ cudaError_t launch_one(const RecArgs& a, cudaStream_t stream) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess || (e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-  constexpr size_t smem = (size_t)kStages * 3 * kTensor<T>;
+  constexpr size_t smem = (size_t)kStages * 3 * RecShape<T, kTok>::TENSOR;
   if ((e = allow_shared<gated_recurrence_backward_kernel<T, MODE, WORDS>>(smem)) != cudaSuccess) return e;
   const long long items = (long long)a.n_segs * a.cols;
-  if ((e = launch_early(gated_recurrence_backward_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, 2ll * sms)), kThreads, smem, stream, a)) != cudaSuccess) return e;
+  if ((e = launch_early(gated_recurrence_backward_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, (long long)kBlocks<MODE> * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
   return launched();
 }
 template <class T>

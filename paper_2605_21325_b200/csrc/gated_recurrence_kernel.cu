@@ -6,26 +6,25 @@
 namespace tri_inv {
 namespace {
 
-constexpr int kWarps = 8, kTok = kRecTile / kWarps, kStages = 2;
-constexpr int kThreads = 32 * kWarps + kRecChannels;   // warps of tokens, and a thread for each channel that joins them
-template <class T> constexpr int kTensor = kRecTile * kRecChannels * (int)sizeof(T);   // bytes of a tile of one tensor
-
+constexpr int kTok = kRecTok, kBlocks = 4;   // tokens of a lane; blocks an SM
 template <class T, int MODE, bool WORDS>
-__global__ void __launch_bounds__(kThreads, 2) gated_recurrence_kernel(const __grid_constant__ RecArgs a) {
+__global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(const __grid_constant__ RecArgs a) {
+  using Shape = RecShape<T, kTok>;
+  constexpr int CH = Shape::CHANNELS, TILE = Shape::TILE, ROW = Shape::ROW;
   extern __shared__ __align__(128) unsigned char stages[];
-  __shared__ __align__(16) float2 part[2][kWarps][kRecChannels];   // (P, H) of each warp's tokens, then of all tokens of the tile before them
-  __shared__ __align__(8) float entry[2][kRecChannels];            // what enters a tile
+  __shared__ __align__(16) float2 part[2][kRecWarps][CH];   // (P, H) of each warp's tokens, then of all tokens of the tile before them
+  __shared__ __align__(8) float entry[2][CH];            // what enters a tile
   __shared__ RecAt ring[kRecRing];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int items = a.n_segs * a.cols;
   constexpr int es = sizeof(T);
-  RecFeed<WORDS, kRecTile, 3, false> feed{a, {a.ld_x * es, a.ld_g * es, a.ld_y * es}, es};
+  RecFeed<WORDS, TILE, 3, false> feed{a, {a.ld_x * es, a.ld_g * es, a.ld_y * es}, es};
   wait_for_predecessor();
-  if (tid == 32 * kWarps) feed.begin(ring, 4);
+  if (tid == 32 * kRecWarps) feed.begin(ring, 4);
   __syncthreads();
 
-  if (warp >= kWarps) {   // a channel
-    const int ch = tid - 32 * kWarps;
+  if (warp >= kRecWarps) {   // a channel
+    const int ch = tid - 32 * kRecWarps;
     const unsigned long long limit = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
     float carried = 0.f;   // without words: what leaves the tile before
     for (int i = 0;; ++i) {
@@ -35,10 +34,10 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_kernel(const __g
       const int c = t.c0 + ch, index = t.index;
       const bool in = c < a.D, first = index == 0, last = index + 1 == t.tiles;
       float h = first && in && a.h0 ? a.h0[(long long)t.seq * a.D + c] : 0.f;
-      rec_meet(kRecMaps + (i & 1), kThreads);
+      rec_meet(kRecMaps + (i & 1), kRecThreads);
       float P = 1.f, H = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
+      for (int w = 0; w < kRecWarps; ++w) {
         const float2 q = part[i & 1][w][ch];
         part[i & 1][w][ch] = make_float2(P, H);
         P *= q.x;
@@ -57,17 +56,17 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_kernel(const __g
       }
       entry[i & 1][ch] = h;
       if (ch == 0) feed.give(&ring[(i + 4) & (kRecRing - 1)]);
-      rec_arrive(kRecEntry + (i & 1), kThreads);
+      rec_arrive(kRecEntry + (i & 1), kRecThreads);
       if (in && last && a.h_out) a.h_out[(long long)t.seq * a.D + c] = carried;
       if (in && a.carries) {   // those that a further token of the sequence follows
-        float* to = a.carries + (rec_slot(t.begin, t.seq, kRecCarry) + (long long)index * (kRecTile / kRecCarry)) * a.D + c;
-        const int left = t.len - index * kRecTile;
+        float* to = a.carries + (rec_slot(t.begin, t.seq, kRecCarry) + (long long)index * (TILE / kRecCarry)) * a.D + c;
+        const int left = t.len - index * TILE;
 #pragma unroll
-        for (int k = 1; k <= kRecTile / kRecCarry; ++k)
+        for (int k = 1; k <= TILE / kRecCarry; ++k)
           if (k * kRecCarry < left) {
             float s = carried;
-            if (k * kRecCarry < kRecTile) {
-              const float2 q = part[i & 1][k * kRecCarry / kTok][ch];
+            if (k * kRecCarry < TILE) {
+              const float2 q = part[i & 1][k * kRecCarry / Shape::WARP_TOK][ch];
               s = rec_step(q.x, h, q.y);
             }
             to[(long long)(k - 1) * a.D] = s;
@@ -79,26 +78,23 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_kernel(const __g
 
   using Lane = RecLane<T>;
   using Raw = typename Lane::Raw;
-  constexpr int ROW = kRecChannels * es;
   const T *X = (const T*)a.x, *G = (const T*)a.g;
   T* Y = (T*)a.y;
   const int x_access = rec_access<T>(X, a.ld_x), g_access = rec_access<T>(G, a.ld_g), y_access = rec_access<T>(Y, a.ld_y);
   const bool wide = x_access == kRecWide && g_access == kRecWide, plain = y_access <= (es == 4 ? kRecWide : kRecFours);   // whole lanes can be written
-  const char *x_from = (const char*)X + rec_lane_bytes<T>(a.ld_x, warp * kTok), *g_from = (const char*)G + rec_lane_bytes<T>(a.ld_g, warp * kTok);
-  const long long x_step = a.ld_x * (512 / ROW) * es, g_step = a.ld_g * (512 / ROW) * es;
-  const uint32_t lane_to = (uint32_t)__cvta_generic_to_shared(stages) + warp * kTok * ROW + 16 * lane;   // (a warp's 512 bytes at a time follow one another)
+  const int first = warp * Shape::WARP_TOK;   // of the warp's tokens
+  const char *x_from = (const char*)X + Shape::copy_from(a.ld_x, first), *g_from = (const char*)G + Shape::copy_from(a.ld_g, first);
+  const uint32_t warp_smem = (uint32_t)__cvta_generic_to_shared(stages) + warp * Shape::WARP_BYTES;
   // A warp asks for the rows that it alone reads, so that no barrier stands between a copy and its use.
   auto request = [&](const RecAt& t, int stage) {
     if (t.item < items) {
+      const uint32_t to = warp_smem + stage * 2 * Shape::TENSOR;
       if (t.whole && wide) {
-        const uint32_t to = lane_to + stage * 2 * kTensor<T>;
-        rec_request_whole<T, kTok>(to, x_from + t.at[0], x_step);
-        rec_request_whole<T, kTok>(to + kTensor<T>, g_from + t.at[1], g_step);
+        Shape::request_whole(to, x_from + t.at[0], a.ld_x);
+        Shape::request_whole(to + Shape::TENSOR, g_from + t.at[1], a.ld_g);
       } else {
-        const int first = warp * kTok;
-        unsigned char* to = stages + stage * 2 * kTensor<T> + first * ROW;
-        rec_request<T, kTok>(to, X, a.ld_x, t.tok0 + first, t.n - first, t.c0, a.D, x_access);
-        rec_request<T, kTok>(to + kTensor<T>, G, a.ld_g, t.tok0 + first, t.n - first, t.c0, a.D, g_access);
+        Shape::request(to, X, a.ld_x, t.tok0 + first, t.n - first, t.c0, a.D, x_access);
+        Shape::request(to + Shape::TENSOR, G, a.ld_g, t.tok0 + first, t.n - first, t.c0, a.D, g_access);
       }
     }
     rec_commit();
@@ -110,17 +106,17 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_kernel(const __g
     request(ring[(i + 1) & (kRecRing - 1)], (i + 1) & 1);
     rec_wait<1>();
     __syncwarp();
-    const unsigned char* sx = stages + (i & 1) * 2 * kTensor<T> + warp * kTok * ROW + 2 * lane * es;
+    const unsigned char* sx = stages + (i & 1) * 2 * Shape::TENSOR + warp * Shape::WARP_BYTES + Shape::place();
     Pair av[kTok], uv[kTok];
 #pragma unroll
     for (int k = 0; k < kTok; ++k) {
-      const Pair x = Lane::widen(*reinterpret_cast<const Raw*>(sx + k * ROW)), g = Lane::widen(*reinterpret_cast<const Raw*>(sx + kTensor<T> + k * ROW));
+      const Pair x = Lane::widen(*reinterpret_cast<const Raw*>(sx + k * ROW)), g = Lane::widen(*reinterpret_cast<const Raw*>(sx + Shape::TENSOR + k * ROW));
       Pair m;
       rec_factors<MODE>(g, av[k], m);
       uv[k] = rec_input<MODE>(m, x);
     }
-    const int left = t.n - warp * kTok;
-    if (left < kTok) {
+    const int left = t.n - first - Shape::group() * kTok;   // of the lane's tokens
+    if (!t.whole) {
 #pragma unroll
       for (int k = 0; k < kTok; ++k)
         if (k >= left) { av[k] = twice(1.f); uv[k] = twice(0.f); }
@@ -137,16 +133,19 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_kernel(const __g
 #pragma unroll
       for (int k = 0; k < kTok; ++k) H = rec_step(av[k], H, uv[k]);
     }
+    Pair group_P, group_H;
+    rec_join_groups<false>(P, H, group_P, group_H);
     const float2 pp = both(P), hh = both(H);
-    *reinterpret_cast<float4*>(&part[i & 1][warp][2 * lane]) = make_float4(pp.x, hh.x, pp.y, hh.y);
-    rec_arrive(kRecMaps + (i & 1), kThreads);
-    rec_meet(kRecEntry + (i & 1), kThreads);
+    if (lane < Shape::LANES) *reinterpret_cast<float4*>(&part[i & 1][warp][Shape::channel()]) = make_float4(pp.x, hh.x, pp.y, hh.y);
+    rec_arrive(kRecMaps + (i & 1), kRecThreads);
+    rec_meet(kRecEntry + (i & 1), kRecThreads);
     if (Y) {
-      const float4 q = *reinterpret_cast<const float4*>(&part[i & 1][warp][2 * lane]);
-      const float2 e = *reinterpret_cast<const float2*>(&entry[i & 1][2 * lane]);
+      const float4 q = *reinterpret_cast<const float4*>(&part[i & 1][warp][Shape::channel()]);
+      const float2 e = *reinterpret_cast<const float2*>(&entry[i & 1][Shape::channel()]);
       Pair h = rec_step(pair(q.x, q.z), pair(e.x, e.y), pair(q.y, q.w));
+      h = rec_step(group_P, h, group_H);
       if (t.whole && plain && !resets) {
-        char* row = (char*)Y + t.at[2] + (warp * kTok * a.ld_y + 2 * lane) * es;
+        char* row = (char*)Y + t.at[2] + ((first + Shape::group() * kTok) * a.ld_y + Shape::channel()) * es;
         const uint32_t step = (uint32_t)a.ld_y * es;
 #pragma unroll
         for (int k = 0; k < kTok; ++k) {
@@ -154,11 +153,11 @@ __global__ void __launch_bounds__(kThreads, 2) gated_recurrence_kernel(const __g
           *reinterpret_cast<Raw*>(row + (unsigned long long)step * k) = Lane::pack(h);
         }
       } else {
-        T* row = Y + (t.tok0 + warp * kTok) * a.ld_y;
+        T* row = Y + (t.tok0 + first + Shape::group() * kTok) * a.ld_y;
 #pragma unroll
         for (int k = 0; k < kTok; ++k) {
           h = rec_step(av[k], h, uv[k]);
-          if (k < left) rec_store(row + k * a.ld_y, t.c0 + 2 * lane, a.D, y_access, h);
+          if (k < left) rec_store(row + k * a.ld_y, t.c0 + Shape::channel(), a.D, y_access, h);
         }
       }
     }
@@ -224,10 +223,10 @@ cudaError_t launch_one(const RecArgs& a, cudaStream_t stream) {
     if ((e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
     sms[dev] = n;
   }
-  constexpr size_t smem = (size_t)kStages * 2 * kTensor<T>;
+  constexpr size_t smem = 4 * (size_t)RecShape<T, kTok>::TENSOR;   // two tiles of two tensors
   if ((e = allow_shared<gated_recurrence_kernel<T, MODE, WORDS>>(smem)) != cudaSuccess) return e;
   const long long items = (long long)a.n_segs * a.cols;
-  if ((e = launch_early(gated_recurrence_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, 2ll * n)), kThreads, smem, stream, a)) != cudaSuccess) return e;
+  if ((e = launch_early(gated_recurrence_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, (long long)kBlocks * n)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
   return launched();
 }
 template <class T>
