@@ -18,9 +18,12 @@ namespace tri_inv {
 constexpr int kRecCarry = TRI_INV_REC_TILE;   // tokens from one carried state to the next
 constexpr int kRecWarps = 4;     // warps of tokens of a block
 constexpr int kRecGroups = 2;    // lane groups of a warp, each with tokens of its own (RecShape)
-constexpr int kRecTok = 16, kRecBackTok = 8;                                                // tokens of a lane, forwards and in the gradient
+constexpr int kRecTok = 16;                                                                 // tokens of a lane
+// ... in the gradient: sixteen where their registers hold one number a value and their three tensors leave room for four blocks an SM
+__host__ __device__ constexpr int rec_back_tok(int mode, int bytes) { return mode == TRI_INV_REC_DECAY && bytes == 2 ? 16 : 8; }
 constexpr int kRecThreads = 32 * kRecWarps + 32;                                            // and a thread for each channel that joins them
-constexpr int kRecTile = kRecWarps * kRecGroups * kRecTok, kRecBackTile = kRecWarps * kRecGroups * kRecBackTok, kRecChannels = 64 / kRecGroups;   // of a tile
+constexpr int kRecTile = kRecWarps * kRecGroups * kRecTok, kRecChannels = 64 / kRecGroups;   // of a tile
+__host__ __device__ constexpr int rec_back_tile(int mode, int bytes) { return kRecWarps * kRecGroups * rec_back_tok(mode, bytes); }
 
 // An entry of the table of packed sequences: a tile, or a whole sequence (index 0)
 struct RecTile {
@@ -146,25 +149,11 @@ __device__ __forceinline__ Pair rec_step(Pair a, Pair h, Pair u) {
   const float2 x = both(a), y = both(h), z = both(u);
   return pair(rec_step(x.x, y.x, z.x), rec_step(x.y, y.y, z.y));
 }
-// The maps of the lane groups of a warp join: (P, H) of a lane's group becomes that of the whole warp, (before_P, before_H) that of the groups in front of it (BACK: behind it).
-template <bool BACK>
-__device__ __forceinline__ void rec_join_groups(Pair& P, Pair& H, Pair& before_P, Pair& before_H) {
-  before_P = twice(1.f);
-  before_H = twice(0.f);
-#pragma unroll
-  for (int m = 32 / kRecGroups; m < 32; m <<= 1) {
-    const float2 p = both(P), h = both(H);
-    const Pair op = pair(__shfl_xor_sync(0xffffffffu, p.x, m), __shfl_xor_sync(0xffffffffu, p.y, m)), oh = pair(__shfl_xor_sync(0xffffffffu, h.x, m), __shfl_xor_sync(0xffffffffu, h.y, m));
-    const bool second = ((threadIdx.x & m) != 0) != BACK;   // the other half comes before this lane's
-    if (second) {
-      before_H = rec_step(before_P, oh, before_H);
-      before_P = mul2(before_P, op);
-      H = rec_step(P, oh, H);
-    } else {
-      H = rec_step(op, H, oh);
-    }
-    P = mul2(P, op);
-  }
+// The same of the other lane group's lane
+static_assert(kRecGroups == 2, "the lane groups of a warp join in one exchange");
+__device__ __forceinline__ Pair rec_other(Pair v) {
+  const float2 f = both(v);
+  return pair(__shfl_xor_sync(0xffffffffu, f.x, 16), __shfl_xor_sync(0xffffffffu, f.y, 16));
 }
 __device__ __forceinline__ bool any_zero(Pair a) { const float2 x = both(a); return x.x == 0.f || x.y == 0.f; }
 
@@ -333,10 +322,10 @@ __device__ __forceinline__ float rec_look_back(const unsigned long long* word, l
   }
 }
 
-// Where the warps of tokens and the threads of channels meet: the maps of a tile's warps are there, a tile's entry is there; tiles take two of each in turn
-enum : int { kRecMaps = 1, kRecEntry = 3 };
-__device__ __forceinline__ void rec_meet(int which, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(which), "r"(threads) : "memory"); }
-__device__ __forceinline__ void rec_arrive(int which, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(which), "r"(threads) : "memory"); }
+// Where warps meet: those of tokens when their maps are there; all when what enters the tile is there as well
+enum : int { kRecMaps = 1, kRecEntry = 2 };
+template <int WHICH, int THREADS>
+__device__ __forceinline__ void rec_meet() { asm volatile("bar.sync %0, %1;" ::"n"(WHICH), "n"(THREADS) : "memory"); }
 
 // Where a block stands: a tile of an item, which is a tile (with words) or a whole sequence
 struct RecAt {
@@ -396,20 +385,12 @@ struct RecFeed {
     place();
   }
   __device__ __forceinline__ void follow() { last.index += BACK ? -1 : 1; place(); }
-  // Ahead of the first tile: `n` tiles into the ring
-  __device__ __forceinline__ void begin(RecAt* ring, int n) {
-    int item = blockIdx.x;
-    for (int i = 0; i < n; ++i) {
-      if (i > 0 && more()) {
-        follow();
-      } else {
-        if (WORDS) item = (int)atomicAdd(a.ticket, 1u);
-        decode(item, entry(item));
-        item += gridDim.x;
-      }
-      ring[i] = last;
-    }
-    drawn = WORDS ? (int)atomicAdd(a.ticket, 1u) : item;
+  // The first tile
+  __device__ __forceinline__ void begin(RecAt* ring) {
+    const int item = WORDS ? (int)atomicAdd(a.ticket, 1u) : (int)blockIdx.x;
+    decode(item, entry(item));
+    ring[0] = last;
+    drawn = WORDS ? (int)atomicAdd(a.ticket, 1u) : item + (int)gridDim.x;
   }
   // Early in a round: asks for what `give` needs
   int next_drawn, given;

@@ -6,23 +6,18 @@
 namespace tri_inv {
 namespace {
 
-constexpr int kTok = kRecBackTok, kStages = 3;
-template <int MODE> constexpr int kBlocks = MODE == kRecDecay ? 4 : 3;   // an SM's, by the registers that a lane's tokens take
-// What a warp's tokens of a tile make of x, from what the first pass over them left: a, m
-template <int MODE> struct Factors { Pair a[kTok], m[kTok]; };
-template <> struct Factors<kRecDecay> { Pair a[kTok]; };
-// and the maps of its lane groups: (fP, fH) of those in front of the lane's, (bP, bC) of those behind it
-template <int MODE> struct Held : Factors<MODE> { Pair fP, fH, bP, bC; };
+// Blocks an SM: those for which the tokens of a lane find room in registers
+__host__ __device__ constexpr int blocks(int mode, int bytes) { return mode == kRecGate && bytes == 2 ? 5 : 4; }
 
-// w: what multiplies e in dg, from the state in front of the token
-template <int MODE>
+// w: what multiplies e in dg, from the state in front of the token.  SAFE: where m may be zero
+template <int MODE, bool SAFE>
 __device__ __forceinline__ Pair weight(Pair a, Pair m, Pair h, Pair x) {
   const Pair minus = twice(-1.f);
   if constexpr (MODE == kRecDecay) {
     return mul2(a, h);
   } else if constexpr (MODE == kRecNormed) {
     const float2 f = both(m);
-    const Pair over = pair(f.x > 0.f ? rec_reciprocal(f.x) : 0.f, f.y > 0.f ? rec_reciprocal(f.y) : 0.f);
+    const Pair over = SAFE ? pair(f.x > 0.f ? rec_reciprocal(f.x) : 0.f, f.y > 0.f ? rec_reciprocal(f.y) : 0.f) : pair(rec_reciprocal(f.x), rec_reciprocal(f.y));
     return mul2(a, fma2(mul2(mul2(a, over), x), minus, h));
   } else {
     return mul2(fma2(x, minus, h), mul2(a, m));
@@ -34,74 +29,60 @@ __device__ __forceinline__ Pair none_where_zero(Pair a, Pair v) {
 }
 
 template <class T, int MODE, bool WORDS>
-__global__ void __launch_bounds__(kRecThreads, kBlocks<MODE>) gated_recurrence_backward_kernel(const __grid_constant__ RecArgs a) {
+__global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_recurrence_backward_kernel(const __grid_constant__ RecArgs a) {
+  constexpr int kTok = rec_back_tok(MODE, sizeof(T));
   using Shape = RecShape<T, kTok>;
-  constexpr int CH = Shape::CHANNELS, TILE = Shape::TILE, ROW = Shape::ROW;
+  using Lane = RecLane<T>;
+  using Raw = typename Lane::Raw;
+  constexpr int CH = kRecChannels, TILE = Shape::TILE, ROW = Shape::ROW, es = sizeof(T);
   extern __shared__ __align__(128) unsigned char stages[];
-  __shared__ __align__(16) float2 part[2][kRecWarps][CH];   // (P, H) of each warp's tokens; then (P, C) of all tokens of the tile behind them
-  __shared__ __align__(8) float side[2][kRecWarps][CH];     // C: what each warp's tokens pass on, where nothing reaches them from behind; then the state in front of them
-  __shared__ __align__(8) float entry[2][CH];            // what reaches a tile from behind
+  __shared__ __align__(16) float2 part[2][kRecWarps][CH];   // (P, H) of each warp's tokens
+  __shared__ __align__(8) float back[2][kRecWarps][CH];     // C: what they pass on where nothing reaches them from behind
+  __shared__ __align__(16) float2 entry[2][CH];             // the state in front of a tile, and what reaches it from behind
   __shared__ RecAt ring[kRecRing];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int items = a.n_segs * a.cols;
-  constexpr int es = sizeof(T);
   RecFeed<WORDS, TILE, 5, true> feed{a, {a.ld_x * es, a.ld_g * es, a.ld_dy * es, a.ld_dx * es, a.ld_dg * es}, es};
   wait_for_predecessor();
-  if (tid == 32 * kRecWarps) feed.begin(ring, 4);
+  if (tid == 32 * kRecWarps) feed.begin(ring);
   __syncthreads();
 
-  if (warp >= kRecWarps) {   // a channel
-    const int ch = tid - 32 * kRecWarps;
+  if (warp == kRecWarps) {   // a lane for each channel
+    if (lane == 0)
+      for (int i = 1; i < 3; ++i) { feed.ask(); feed.give(&ring[i]); }
+    __syncthreads();
     const unsigned long long limit = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
     float carried = 0.f;
     for (int i = 0;; ++i) {
       const RecAt& t = ring[i & (kRecRing - 1)];
       if (t.item >= items) break;
-      if (ch == 0) feed.ask();
-      const int c = t.c0 + ch, behind = t.tiles - 1 - t.index;
+      if (lane == 0) feed.ask();
+      const int c = t.c0 + lane, behind = t.tiles - 1 - t.index;
       const bool in = c < a.D, first = t.index == 0, last = behind == 0;
       const long long at = t.slot * a.D + c, state = (long long)t.seq * a.D + c;
-      float h = !in ? 0.f : !first ? a.carries[(rec_slot(t.begin, t.seq, kRecCarry) + (long long)t.index * (TILE / kRecCarry) - 1) * a.D + c] : a.h0 ? a.h0[state] : 0.f;   // the state in front of the tile
-      float e = last && in && a.dh ? a.dh[state] : 0.f;
-      rec_meet(kRecMaps + (i & 1), kRecThreads);
-      float P = 1.f, C = 0.f, kept[kRecWarps];
-#pragma unroll
-      for (int w = 0; w < kRecWarps; ++w) {
-        const float2 q = part[i & 1][w][ch];
-        kept[w] = h;
-        h = rec_step(q.x, h, q.y);
-      }
-#pragma unroll
-      for (int w = kRecWarps - 1; w >= 0; --w) {
-        const float p = part[i & 1][w][ch].x, c_own = side[i & 1][w][ch];
-        part[i & 1][w][ch] = make_float2(P, C);
-        side[i & 1][w][ch] = kept[w];
-        P *= p;
-        C = rec_step(p, C, c_own);
-      }
+      float h = 0.f, e = 0.f;
       if (in) {
-        if (WORDS && !last) {
-          if (!first) rec_post(a.words + at, P, C);
-          e = rec_look_back(a.words + at + a.D, -(long long)a.D, behind, limit, a.status);
-        } else if (!last) {
-          e = carried;
-        }
-        carried = rec_step(P, e, C);
-        if (first) {
-          if (a.dh0) a.dh0[state] = carried;
-        } else if (WORDS) {
-          rec_post(a.words + at, 0.f, carried);
-        }
+        if (!first) h = a.carries[(rec_slot(t.begin, t.seq, kRecCarry) + (long long)t.index * (TILE / kRecCarry) - 1) * a.D + c];
+        else if (a.h0) h = a.h0[state];
+        if (last) e = a.dh ? a.dh[state] : 0.f;
+        else e = WORDS ? rec_look_back(a.words + at + a.D, -(long long)a.D, behind, limit, a.status) : carried;
       }
-      entry[i & 1][ch] = e;
-      if (ch == 0) feed.give(&ring[(i + 4) & (kRecRing - 1)]);
-      rec_arrive(kRecEntry + (i & 1), kRecThreads);
+      entry[i & 1][lane] = make_float2(h, e);
+      rec_meet<kRecEntry, kRecThreads>();
+      float s = e;
+#pragma unroll
+      for (int w = kRecWarps - 1; w >= 0; --w) s = rec_step(part[i & 1][w][lane].x, s, back[i & 1][w][lane]);
+      carried = s;
+      if (in) {
+        if (first) { if (a.dh0) a.dh0[state] = s; }
+        else if (WORDS) rec_post(a.words + at, 0.f, s);
+      }
+      if (lane == 0) feed.give(&ring[(i + 3) & (kRecRing - 1)]);
+      __syncwarp();
     }
     return;
   }
 
-  using Lane = RecLane<T>;
-  using Raw = typename Lane::Raw;
   const T *X = (const T*)a.x, *G = (const T*)a.g, *DY = (const T*)a.dy;
   const int x_access = rec_access<T>(X, a.ld_x), g_access = rec_access<T>(G, a.ld_g), dy_access = rec_access<T>(DY, a.ld_dy);
   const int dx_access = rec_access<T>(a.dx, a.ld_dx), dg_access = rec_access<T>(a.dg, a.ld_dg), most = es == 4 ? kRecWide : kRecFours;
@@ -125,126 +106,117 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks<MODE>) gated_recurrence_b
     rec_commit();
   };
   request(ring[0], 0);
-  // Round i: the maps of tile i, and the output of tile i - 1, whose entry the channels' threads have found out meanwhile.  A tile's rows stay for both.
-  Held<MODE> even, odd;
-  bool resets = false;
-  int stage = 0, stage_before = 2;
-  auto round = [&](int i, Held<MODE>& now, const Held<MODE>& before) -> bool {
-    const int stage_next = 3 - stage - stage_before;
-    request(ring[(i + 1) & (kRecRing - 1)], stage_next);
-    const bool has_now = ring[i & (kRecRing - 1)].item < items;
-    const int place = warp * Shape::WARP_BYTES + Shape::place();
-    bool now_resets = false;
-    if (has_now) {
-      rec_wait<1>();
-      __syncwarp();
-      const unsigned char* sx = stages + stage * 3 * Shape::TENSOR + place;
-      auto read = [&](int tensor, int k) { return Lane::widen(*reinterpret_cast<const Raw*>(sx + tensor * Shape::TENSOR + k * ROW)); };
-      const int left = ring[i & (kRecRing - 1)].n - first - Shape::group() * kTok;   // of the lane's tokens
-      Pair P = twice(1.f), H = twice(0.f), C = twice(0.f);
-#pragma unroll
-      for (int k = 0; k < kTok; ++k) {
-        Pair m;
-        rec_factors<MODE>(read(1, k), now.a[k], m);
-        if constexpr (MODE != kRecDecay) now.m[k] = m;
-      }
-      if (!ring[i & (kRecRing - 1)].whole) {
-#pragma unroll
-        for (int k = 0; k < kTok; ++k)
-          if (k >= left) {
-            now.a[k] = twice(1.f);
-            if constexpr (MODE != kRecDecay) now.m[k] = twice(0.f);
-          }
-      }
-      auto input = [&](int k) {
-        if constexpr (MODE == kRecDecay) return read(0, k);
-        else return mul2(now.m[k], read(0, k));
-      };
-#pragma unroll
-      for (int k = 0; k < kTok; ++k) {
-        P = mul2(P, now.a[k]);
-        H = fma2(now.a[k], H, input(k));
-        C = mul2(now.a[kTok - 1 - k], add2(C, read(2, kTok - 1 - k)));
-      }
-      now_resets = __any_sync(0xffffffffu, any_zero(P));
-      if (now_resets) {
-        H = C = twice(0.f);
-#pragma unroll
-        for (int k = 0; k < kTok; ++k) {
-          H = rec_step(now.a[k], H, input(k));
-          C = none_where_zero(now.a[kTok - 1 - k], mul2(now.a[kTok - 1 - k], add2(C, read(2, kTok - 1 - k))));
-        }
-      }
-      Pair same = P;
-      rec_join_groups<true>(same, C, now.bP, now.bC);
-      rec_join_groups<false>(P, H, now.fP, now.fH);
-      const float2 pp = both(P), hh = both(H), cc = both(C);
-      if (lane < Shape::LANES) {
-        *reinterpret_cast<float4*>(&part[i & 1][warp][Shape::channel()]) = make_float4(pp.x, hh.x, pp.y, hh.y);
-        *reinterpret_cast<float2*>(&side[i & 1][warp][Shape::channel()]) = cc;
-      }
-      rec_arrive(kRecMaps + (i & 1), kRecThreads);
-    }
-    if (i > 0) {
-      const unsigned char* sx = stages + stage_before * 3 * Shape::TENSOR + place;
-      auto read = [&](int tensor, int k) { return Lane::widen(*reinterpret_cast<const Raw*>(sx + tensor * Shape::TENSOR + k * ROW)); };
-      rec_meet(kRecEntry + ((i - 1) & 1), kRecThreads);
-      const RecAt& p = ring[(i - 1) & (kRecRing - 1)];
-      const float4 q = *reinterpret_cast<const float4*>(&part[(i - 1) & 1][warp][Shape::channel()]);
-      const float2 s = *reinterpret_cast<const float2*>(&side[(i - 1) & 1][warp][Shape::channel()]), e0 = *reinterpret_cast<const float2*>(&entry[(i - 1) & 1][Shape::channel()]);
-      Pair h = pair(s.x, s.y), C = rec_step(pair(q.x, q.z), pair(e0.x, e0.y), pair(q.y, q.w)), w[kTok];
-      h = rec_step(before.fP, h, before.fH);
-      C = rec_step(before.bP, C, before.bC);
-      auto m_of = [&](int k) {
-        if constexpr (MODE == kRecDecay) return twice(1.f);
-        else return before.m[k];
-      };
-      if (p.whole && plain && !resets) {
-#pragma unroll
-        for (int k = 0; k < kTok; ++k) {
-          const Pair x = read(0, k);
-          w[k] = weight<MODE>(before.a[k], m_of(k), h, x);
-          h = fma2(before.a[k], h, rec_input<MODE>(m_of(k), x));
-        }
-        char *dx_row = (char*)a.dx + p.at[3] + ((first + Shape::group() * kTok) * a.ld_dx + Shape::channel()) * es, *dg_row = (char*)a.dg + p.at[4] + ((first + Shape::group() * kTok) * a.ld_dg + Shape::channel()) * es;
-        const uint32_t dx_step = (uint32_t)a.ld_dx * es, dg_step = (uint32_t)a.ld_dg * es;
-#pragma unroll
-        for (int k = kTok - 1; k >= 0; --k) {
-          const Pair e = add2(C, read(2, k));
-          *reinterpret_cast<Raw*>(dx_row + (unsigned long long)dx_step * k) = Lane::pack(rec_input<MODE>(m_of(k), e));
-          *reinterpret_cast<Raw*>(dg_row + (unsigned long long)dg_step * k) = Lane::pack(mul2(w[k], e));
-          C = mul2(before.a[k], e);
-        }
-      } else {
-        const int at = first + Shape::group() * kTok, left = p.n - at, c = p.c0 + Shape::channel();
-        T* dx_row = (T*)a.dx + (p.tok0 + at) * a.ld_dx;
-        T* dg_row = (T*)a.dg + (p.tok0 + at) * a.ld_dg;
-#pragma unroll
-        for (int k = 0; k < kTok; ++k) {
-          const Pair x = read(0, k);
-          w[k] = none_where_zero(before.a[k], weight<MODE>(before.a[k], m_of(k), h, x));
-          h = rec_step(before.a[k], h, rec_input<MODE>(m_of(k), x));
-        }
-#pragma unroll
-        for (int k = kTok - 1; k >= 0; --k) {
-          const Pair e = add2(C, read(2, k));
-          if (k < left) {
-            rec_store(dx_row + k * a.ld_dx, c, a.D, dx_access, rec_input<MODE>(m_of(k), e));
-            rec_store(dg_row + k * a.ld_dg, c, a.D, dg_access, mul2(w[k], e));
-          }
-          C = none_where_zero(before.a[k], mul2(before.a[k], e));
-        }
-      }
-    }
-    resets = now_resets;
-    stage_before = stage;
-    stage = stage_next;
+  __syncthreads();
+  for (int i = 0;; ++i) {
+    const RecAt& t = ring[i & (kRecRing - 1)];
+    if (t.item >= items) break;
+    request(ring[(i + 1) & (kRecRing - 1)], (i + 1) & 1);
+    rec_wait<1>();
     __syncwarp();
-    return has_now;
-  };
-  for (int i = 0;; i += 2) {
-    if (!round(i, even, odd)) break;
-    if (!round(i + 1, odd, even)) break;
+    const unsigned char* sx = stages + (i & 1) * 3 * Shape::TENSOR + warp * Shape::WARP_BYTES + Shape::place();
+    auto read = [&](int tensor, int k) { return Lane::widen(*reinterpret_cast<const Raw*>(sx + tensor * Shape::TENSOR + k * ROW)); };
+    Pair av[kTok], mv[kTok];   // (mv is not used where it is 1)
+#pragma unroll
+    for (int k = 0; k < kTok; ++k) rec_factors<MODE>(read(1, k), av[k], mv[k]);
+    const int at = first + Shape::group() * kTok, left = t.n - at;   // of the lane's tokens
+    if (!t.whole) {
+#pragma unroll
+      for (int k = 0; k < kTok; ++k)
+        if (k >= left) { av[k] = twice(1.f); mv[k] = twice(0.f); }
+    }
+    Pair P = twice(1.f), H = twice(0.f), C = twice(0.f);
+#pragma unroll
+    for (int k = 0; k < kTok; ++k) {
+      P = mul2(P, av[k]);
+      H = fma2(av[k], H, rec_input<MODE>(mv[k], read(0, k)));
+      C = mul2(av[kTok - 1 - k], add2(C, read(2, kTok - 1 - k)));
+    }
+    const bool resets = __any_sync(0xffffffffu, any_zero(P));
+    bool no_input = false;   // some m is zero
+    if constexpr (MODE == kRecNormed) {
+      float2 least = both(mv[0]);
+#pragma unroll
+      for (int k = 1; k < kTok; ++k) { const float2 f = both(mv[k]); least = make_float2(fminf(least.x, f.x), fminf(least.y, f.y)); }
+      no_input = __any_sync(0xffffffffu, fminf(least.x, least.y) == 0.f);
+    }
+    if (resets) {
+      H = C = twice(0.f);
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) {
+        H = rec_step(av[k], H, rec_input<MODE>(mv[k], read(0, k)));
+        C = none_where_zero(av[kTok - 1 - k], mul2(av[kTok - 1 - k], add2(C, read(2, kTok - 1 - k))));
+      }
+    }
+    const Pair other_P = rec_other(P), other_H = rec_other(H), other_C = rec_other(C);   // the second group's tokens come behind the first one's
+    const bool second = lane >= Shape::LANES;
+    const float2 pp = both(mul2(P, other_P)), hh = both(rec_step(other_P, H, other_H)), cc = both(rec_step(P, other_C, C));
+    if (!second) {
+      *reinterpret_cast<float4*>(&part[i & 1][warp][Shape::channel()]) = make_float4(pp.x, hh.x, pp.y, hh.y);
+      *reinterpret_cast<float2*>(&back[i & 1][warp][Shape::channel()]) = cc;
+    }
+    rec_meet<kRecMaps, 32 * kRecWarps>();
+    if (WORDS && warp == 0 && t.index > 0 && t.index + 1 < t.tiles) {   // the tile's word, for those in front of it
+      float TP = 1.f, TC = 0.f;
+#pragma unroll
+      for (int w = kRecWarps - 1; w >= 0; --w) {
+        const float p = part[i & 1][w][lane].x;
+        TP *= p;
+        TC = rec_step(p, TC, back[i & 1][w][lane]);
+      }
+      if (t.c0 + lane < a.D) rec_post(a.words + t.slot * a.D + t.c0 + lane, TP, TC);
+    }
+    rec_meet<kRecEntry, kRecThreads>();
+    const float4 e0 = *reinterpret_cast<const float4*>(&entry[i & 1][Shape::channel()]);
+    Pair h = pair(e0.x, e0.z);
+    C = pair(e0.y, e0.w);
+    for (int w = 0; w < warp; ++w) {
+      const float4 q = *reinterpret_cast<const float4*>(&part[i & 1][w][Shape::channel()]);
+      h = rec_step(pair(q.x, q.z), h, pair(q.y, q.w));
+    }
+    for (int w = kRecWarps - 1; w > warp; --w) {
+      const float4 q = *reinterpret_cast<const float4*>(&part[i & 1][w][Shape::channel()]);
+      const float2 s = *reinterpret_cast<const float2*>(&back[i & 1][w][Shape::channel()]);
+      C = rec_step(pair(q.x, q.z), C, pair(s.x, s.y));
+    }
+    if (second) h = rec_step(other_P, h, other_H);
+    else C = rec_step(other_P, C, other_C);
+    Pair wv[kTok];
+    if (t.whole && plain && !resets && !no_input) {
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) {
+        const Pair x = read(0, k);
+        wv[k] = weight<MODE, false>(av[k], mv[k], h, x);
+        h = fma2(av[k], h, rec_input<MODE>(mv[k], x));
+      }
+      char *dx_row = (char*)a.dx + t.at[3] + (at * a.ld_dx + Shape::channel()) * es, *dg_row = (char*)a.dg + t.at[4] + (at * a.ld_dg + Shape::channel()) * es;
+      const uint32_t dx_step = (uint32_t)a.ld_dx * es, dg_step = (uint32_t)a.ld_dg * es;
+#pragma unroll
+      for (int k = kTok - 1; k >= 0; --k) {
+        const Pair e = add2(C, read(2, k));
+        *reinterpret_cast<Raw*>(dx_row + (unsigned long long)dx_step * k) = Lane::pack(rec_input<MODE>(mv[k], e));
+        *reinterpret_cast<Raw*>(dg_row + (unsigned long long)dg_step * k) = Lane::pack(mul2(wv[k], e));
+        C = mul2(av[k], e);
+      }
+    } else {
+      const int c = t.c0 + Shape::channel();
+      T *dx_row = (T*)a.dx + (t.tok0 + at) * a.ld_dx, *dg_row = (T*)a.dg + (t.tok0 + at) * a.ld_dg;
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) {
+        const Pair x = read(0, k);
+        wv[k] = none_where_zero(av[k], weight<MODE, true>(av[k], mv[k], h, x));
+        h = rec_step(av[k], h, rec_input<MODE>(mv[k], x));
+      }
+#pragma unroll
+      for (int k = kTok - 1; k >= 0; --k) {
+        const Pair e = add2(C, read(2, k));
+        if (k < left) {
+          rec_store(dx_row + k * a.ld_dx, c, a.D, dx_access, rec_input<MODE>(mv[k], e));
+          rec_store(dg_row + k * a.ld_dg, c, a.D, dg_access, mul2(wv[k], e));
+        }
+        C = none_where_zero(av[k], mul2(av[k], e));
+      }
+    }
+    __syncwarp();
   }
   rec_wait<0>();
 }
@@ -254,10 +226,10 @@ cudaError_t launch_one(const RecArgs& a, cudaStream_t stream) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess || (e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-  constexpr size_t smem = (size_t)kStages * 3 * RecShape<T, kTok>::TENSOR;
+  constexpr size_t smem = 6 * (size_t)RecShape<T, rec_back_tok(MODE, sizeof(T))>::TENSOR;
   if ((e = allow_shared<gated_recurrence_backward_kernel<T, MODE, WORDS>>(smem)) != cudaSuccess) return e;
   const long long items = (long long)a.n_segs * a.cols;
-  if ((e = launch_early(gated_recurrence_backward_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, (long long)kBlocks<MODE> * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
+  if ((e = launch_early(gated_recurrence_backward_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, (long long)blocks(MODE, sizeof(T)) * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
   return launched();
 }
 template <class T>

@@ -10,74 +10,61 @@ constexpr int kTok = kRecTok, kBlocks = 4;   // tokens of a lane; blocks an SM
 template <class T, int MODE, bool WORDS>
 __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(const __grid_constant__ RecArgs a) {
   using Shape = RecShape<T, kTok>;
-  constexpr int CH = Shape::CHANNELS, TILE = Shape::TILE, ROW = Shape::ROW;
+  using Lane = RecLane<T>;
+  using Raw = typename Lane::Raw;
+  constexpr int CH = kRecChannels, TILE = Shape::TILE, ROW = Shape::ROW, es = sizeof(T);
   extern __shared__ __align__(128) unsigned char stages[];
-  __shared__ __align__(16) float2 part[2][kRecWarps][CH];   // (P, H) of each warp's tokens, then of all tokens of the tile before them
-  __shared__ __align__(8) float entry[2][CH];            // what enters a tile
+  __shared__ __align__(16) float2 part[2][kRecWarps][CH];   // (P, H) of each warp's tokens
+  __shared__ __align__(8) float entry[2][CH];               // what enters a tile
   __shared__ RecAt ring[kRecRing];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int items = a.n_segs * a.cols;
-  constexpr int es = sizeof(T);
   RecFeed<WORDS, TILE, 3, false> feed{a, {a.ld_x * es, a.ld_g * es, a.ld_y * es}, es};
   wait_for_predecessor();
-  if (tid == 32 * kRecWarps) feed.begin(ring, 4);
+  if (tid == 32 * kRecWarps) feed.begin(ring);
   __syncthreads();
 
-  if (warp >= kRecWarps) {   // a channel
-    const int ch = tid - 32 * kRecWarps;
+  if (warp == kRecWarps) {   // a lane for each channel: finds out what enters a tile while the other warps read it
+    if (lane == 0)
+      for (int i = 1; i < 3; ++i) { feed.ask(); feed.give(&ring[i]); }
+    __syncthreads();
     const unsigned long long limit = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
     float carried = 0.f;   // without words: what leaves the tile before
     for (int i = 0;; ++i) {
       const RecAt& t = ring[i & (kRecRing - 1)];
       if (t.item >= items) break;
-      if (ch == 0) feed.ask();
-      const int c = t.c0 + ch, index = t.index;
+      if (lane == 0) feed.ask();
+      const int c = t.c0 + lane, index = t.index;
       const bool in = c < a.D, first = index == 0, last = index + 1 == t.tiles;
-      float h = first && in && a.h0 ? a.h0[(long long)t.seq * a.D + c] : 0.f;
-      rec_meet(kRecMaps + (i & 1), kRecThreads);
-      float P = 1.f, H = 0.f;
+      const long long at = t.slot * a.D + c;
+      float h = 0.f;
+      if (in) {
+        if (first) h = a.h0 ? a.h0[(long long)t.seq * a.D + c] : 0.f;
+        else h = WORDS ? rec_look_back(a.words + at - a.D, a.D, index, limit, a.status) : carried;
+      }
+      entry[i & 1][lane] = h;
+      rec_meet<kRecEntry, kRecThreads>();
+      float s = h;
+      float* to = in && a.carries ? a.carries + (rec_slot(t.begin, t.seq, kRecCarry) + (long long)index * (TILE / kRecCarry)) * a.D + c : nullptr;
+      const int left = t.len - index * TILE;
 #pragma unroll
       for (int w = 0; w < kRecWarps; ++w) {
-        const float2 q = part[i & 1][w][ch];
-        part[i & 1][w][ch] = make_float2(P, H);
-        P *= q.x;
-        H = rec_step(q.x, H, q.y);
+        const float2 q = part[i & 1][w][lane];
+        s = rec_step(q.x, s, q.y);
+        const int n = (w + 1) * Shape::WARP_TOK;
+        if (n % kRecCarry == 0 && to && n < left) to[(long long)(n / kRecCarry - 1) * a.D] = s;   // those that a further token of the sequence follows
       }
+      carried = s;
       if (in) {
-        if (WORDS && !first) {
-          unsigned long long* word = a.words + t.slot * a.D + c;
-          if (!last) rec_post(word, P, H);
-          h = rec_look_back(word - a.D, a.D, index, limit, a.status);
-        } else if (!first) {
-          h = carried;
-        }
-        carried = rec_step(P, h, H);
-        if (WORDS && !last && !(a.test_stall && t.item == 0)) rec_post(a.words + t.slot * a.D + c, 0.f, carried);
+        if (last) { if (a.h_out) a.h_out[(long long)t.seq * a.D + c] = s; }
+        else if (WORDS && !(a.test_stall && t.item == 0)) rec_post(a.words + at, 0.f, s);
       }
-      entry[i & 1][ch] = h;
-      if (ch == 0) feed.give(&ring[(i + 4) & (kRecRing - 1)]);
-      rec_arrive(kRecEntry + (i & 1), kRecThreads);
-      if (in && last && a.h_out) a.h_out[(long long)t.seq * a.D + c] = carried;
-      if (in && a.carries) {   // those that a further token of the sequence follows
-        float* to = a.carries + (rec_slot(t.begin, t.seq, kRecCarry) + (long long)index * (TILE / kRecCarry)) * a.D + c;
-        const int left = t.len - index * TILE;
-#pragma unroll
-        for (int k = 1; k <= TILE / kRecCarry; ++k)
-          if (k * kRecCarry < left) {
-            float s = carried;
-            if (k * kRecCarry < TILE) {
-              const float2 q = part[i & 1][k * kRecCarry / Shape::WARP_TOK][ch];
-              s = rec_step(q.x, h, q.y);
-            }
-            to[(long long)(k - 1) * a.D] = s;
-          }
-      }
+      if (lane == 0) feed.give(&ring[(i + 3) & (kRecRing - 1)]);
+      __syncwarp();
     }
     return;
   }
 
-  using Lane = RecLane<T>;
-  using Raw = typename Lane::Raw;
   const T *X = (const T*)a.x, *G = (const T*)a.g;
   T* Y = (T*)a.y;
   const int x_access = rec_access<T>(X, a.ld_x), g_access = rec_access<T>(G, a.ld_g), y_access = rec_access<T>(Y, a.ld_y);
@@ -100,6 +87,7 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
     rec_commit();
   };
   request(ring[0], 0);
+  __syncthreads();   // the next tiles are known
   for (int i = 0;; ++i) {
     const RecAt& t = ring[i & (kRecRing - 1)];
     if (t.item >= items) break;
@@ -133,17 +121,33 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
 #pragma unroll
       for (int k = 0; k < kTok; ++k) H = rec_step(av[k], H, uv[k]);
     }
-    Pair group_P, group_H;
-    rec_join_groups<false>(P, H, group_P, group_H);
-    const float2 pp = both(P), hh = both(H);
-    if (lane < Shape::LANES) *reinterpret_cast<float4*>(&part[i & 1][warp][Shape::channel()]) = make_float4(pp.x, hh.x, pp.y, hh.y);
-    rec_arrive(kRecMaps + (i & 1), kRecThreads);
-    rec_meet(kRecEntry + (i & 1), kRecThreads);
+    const Pair other_P = rec_other(P), other_H = rec_other(H);   // the second group's tokens come behind the first one's
+    const bool second = lane >= Shape::LANES;
+    const float2 pp = both(mul2(P, other_P)), hh = both(rec_step(other_P, H, other_H));
+    if (!second) *reinterpret_cast<float4*>(&part[i & 1][warp][Shape::channel()]) = make_float4(pp.x, hh.x, pp.y, hh.y);
+    rec_meet<kRecMaps, 32 * kRecWarps>();
+    if (WORDS && warp == kRecWarps - 1 && t.index > 0 && t.index + 1 < t.tiles) {   // the tile's word, for those behind it
+      float TP = 1.f, TH = 0.f;
+#pragma unroll
+      for (int w = 0; w < kRecWarps; ++w) {
+        const float2 q = part[i & 1][w][lane];
+        TP *= q.x;
+        TH = rec_step(q.x, TH, q.y);
+      }
+      if (t.c0 + lane < a.D) rec_post(a.words + t.slot * a.D + t.c0 + lane, TP, TH);
+    }
+    P = twice(1.f);
+    H = twice(0.f);
+    for (int w = 0; w < warp; ++w) {   // the tile's tokens in front of the warp's
+      const float4 q = *reinterpret_cast<const float4*>(&part[i & 1][w][Shape::channel()]);
+      H = rec_step(pair(q.x, q.z), H, pair(q.y, q.w));
+      P = mul2(P, pair(q.x, q.z));
+    }
+    rec_meet<kRecEntry, kRecThreads>();
     if (Y) {
-      const float4 q = *reinterpret_cast<const float4*>(&part[i & 1][warp][Shape::channel()]);
       const float2 e = *reinterpret_cast<const float2*>(&entry[i & 1][Shape::channel()]);
-      Pair h = rec_step(pair(q.x, q.z), pair(e.x, e.y), pair(q.y, q.w));
-      h = rec_step(group_P, h, group_H);
+      Pair h = rec_step(P, pair(e.x, e.y), H);
+      if (second) h = rec_step(other_P, h, other_H);
       if (t.whole && plain && !resets) {
         char* row = (char*)Y + t.at[2] + ((first + Shape::group() * kTok) * a.ld_y + Shape::channel()) * es;
         const uint32_t step = (uint32_t)a.ld_y * es;

@@ -85,7 +85,7 @@ struct BackPlan {
 };
 int plan_back(const tri_inv_rec_desc* d, bool with_carries, BackPlan* p) {
   p->carry_bytes = with_carries ? 0 : round_up((size_t)slots_of(d, kRecCarry) * d->D * 4);
-  const int e = plan(d, kRecBackTile, &p->back);
+  const int e = plan(d, rec_back_tile(d->mode, d->dtype == TRI_INV_F32 ? 4 : 2), &p->back);
   return e ? e : plan(d, kRecTile, &p->front);
 }
 
