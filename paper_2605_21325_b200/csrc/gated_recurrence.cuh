@@ -19,11 +19,23 @@ constexpr int kRecCarry = TRI_INV_REC_TILE;   // tokens from one carried state t
 constexpr int kRecWarps = 4;     // warps of tokens of a block
 constexpr int kRecGroups = 2;    // lane groups of a warp, each with tokens of its own (RecShape)
 constexpr int kRecTok = 16;                                                                 // tokens of a lane
-// ... in the gradient: sixteen where their registers hold one number a value and their three tensors leave room for four blocks an SM
-__host__ __device__ constexpr int rec_back_tok(int mode, int bytes) { return mode == TRI_INV_REC_DECAY && bytes == 2 ? 16 : 8; }
+// ... in the gradient: sixteen of fp32 would leave shared memory for two blocks an SM
+__host__ __device__ constexpr int rec_back_tok(int bytes) { return bytes == 2 ? 16 : 8; }
 constexpr int kRecThreads = 32 * kRecWarps + 32;                                            // and a thread for each channel that joins them
 constexpr int kRecTile = kRecWarps * kRecGroups * kRecTok, kRecChannels = 64 / kRecGroups;   // of a tile
-__host__ __device__ constexpr int rec_back_tile(int mode, int bytes) { return kRecWarps * kRecGroups * rec_back_tok(mode, bytes); }
+__host__ __device__ constexpr int rec_back_tile(int bytes) { return kRecWarps * kRecGroups * rec_back_tok(bytes); }
+
+// n / d for n < 2^30 as (n m) >> (30 + L), 2^L >= d, m = ceil(2^(30 + L) / d): what m d has above 2^(30 + L) is below d <= 2^L, and n times it below 2^(30 + L), so that the quotient's floor is exact.
+struct RecDivide {
+  uint32_t m;
+  int shift;
+};
+inline RecDivide rec_divide_by(int d) {
+  int L = 0;
+  while ((1ll << L) < d) ++L;
+  return RecDivide{(uint32_t)(((1ull << (30 + L)) + (unsigned)d - 1) / (unsigned)d), 30 + L};
+}
+__host__ __device__ __forceinline__ int rec_quotient(int n, RecDivide by) { return (int)(((unsigned long long)(unsigned)n * by.m) >> by.shift); }
 
 // An entry of the table of packed sequences: a tile, or a whole sequence (index 0)
 struct RecTile {
@@ -48,6 +60,8 @@ struct RecArgs {
   const RecTile* table;            // packed sequences: tiles (with words) or whole sequences; null: dense
   int n_segs;                      // entries of the table, or tiles (whole sequences) of the dense form
   int n_seqs, T, D, cols;          // cols: column tiles
+  RecDivide by_cols, by_seqs;
+  int items;                       // n_segs * cols
   int mode;
   int* status;
   unsigned long long wait_limit_ns;   // 0: two seconds
@@ -335,8 +349,8 @@ struct RecAt {
   int index, tiles;    // the tile, of how many
   int n;               // its tokens
   bool whole;          // all tokens and channels of a tile
-  long long tok0;
-  long long slot;      // of its words
+  int tok0;
+  int slot;            // of its words
   long long at[5];     // where its first value lies in each tensor, in bytes
 };
 // The order of a block's tiles.  The one that it works on, the one before and those that are on their way lie in a ring in shared memory, which one thread keeps ahead.  With words the items are drawn
@@ -345,34 +359,34 @@ constexpr int kRecRing = 8;
 template <bool WORDS, int TILE, int TENSORS, bool BACK>
 struct RecFeed {
   const RecArgs& a;
-  long long ld[TENSORS];   // bytes
+  int ld[TENSORS];         // bytes
   int width;               // bytes of a value
   int drawn;               // the item whose entry of the table is asked for next
   RecAt last;              // without words: the tile that was given last
-  __device__ __forceinline__ bool more() const { return !WORDS && last.item < a.n_segs * a.cols && (BACK ? last.index > 0 : last.index + 1 < last.tiles); }
+  __device__ __forceinline__ bool more() const { return !WORDS && last.item < a.items && (BACK ? last.index > 0 : last.index + 1 < last.tiles); }
   __device__ __forceinline__ RecTile entry(int item) const {
-    if (!a.table || item >= a.n_segs * a.cols) return RecTile{};
-    const int r = item / a.cols;
+    if (!a.table || item >= a.items) return RecTile{};
+    const int r = rec_quotient(item, a.by_cols);
     return a.table[BACK && WORDS ? a.n_segs - 1 - r : r];
   }
   __device__ __forceinline__ void place() {
     last.n = min(TILE, last.len - last.index * TILE);
     last.whole = last.n == TILE && last.c0 + kRecChannels <= a.D;
-    last.tok0 = last.begin + (long long)last.index * TILE;
-    last.slot = rec_slot(last.begin, last.seq, TILE) + last.index;
+    last.tok0 = last.begin + last.index * TILE;   // below 2^31
+    last.slot = last.begin / TILE + last.seq + last.index;
 #pragma unroll
-    for (int k = 0; k < TENSORS; ++k) last.at[k] = last.tok0 * ld[k] + (long long)last.c0 * width;
+    for (int k = 0; k < TENSORS; ++k) last.at[k] = (long long)last.tok0 * ld[k] + last.c0 * width;
   }
   __device__ __forceinline__ void decode(int item, const RecTile& e) {
     last.item = item;
-    if (item >= a.n_segs * a.cols) return;
-    const int r = item / a.cols;
+    if (item >= a.items) return;
+    const int r = rec_quotient(item, a.by_cols);
     last.c0 = (item - r * a.cols) * kRecChannels;
     if (a.table) {
       last.begin = e.tok0; last.len = e.n; last.seq = e.seq; last.index = e.index; last.tiles = e.tiles;
     } else {
       const int rank = BACK && WORDS ? a.n_segs - 1 - r : r;
-      last.index = WORDS ? rank / a.n_seqs : 0;   // the sequences' tiles in turn: the one in front of a tile is n_seqs (times the columns) items ahead of it
+      last.index = WORDS ? rec_quotient(rank, a.by_seqs) : 0;   // the sequences' tiles in turn: the one in front of a tile is n_seqs (times the columns) items ahead of it
       last.tiles = max(1, (int)(((unsigned)a.T + TILE - 1) / TILE));
       last.seq = WORDS ? rank - last.index * a.n_seqs : rank;
       last.begin = last.seq * a.T;

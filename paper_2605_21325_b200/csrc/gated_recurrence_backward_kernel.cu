@@ -7,7 +7,7 @@ namespace tri_inv {
 namespace {
 
 // Blocks an SM: those for which the tokens of a lane find room in registers
-__host__ __device__ constexpr int blocks(int mode, int bytes) { return mode == kRecGate && bytes == 2 ? 5 : 4; }
+__host__ __device__ constexpr int blocks(int mode, int bytes) { return mode != kRecDecay && bytes == 2 ? 3 : 4; }
 
 // w: what multiplies e in dg, from the state in front of the token.  SAFE: where m may be zero
 template <int MODE, bool SAFE>
@@ -30,7 +30,7 @@ __device__ __forceinline__ Pair none_where_zero(Pair a, Pair v) {
 
 template <class T, int MODE, bool WORDS>
 __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_recurrence_backward_kernel(const __grid_constant__ RecArgs a) {
-  constexpr int kTok = rec_back_tok(MODE, sizeof(T));
+  constexpr int kTok = rec_back_tok(sizeof(T)), kPart = MODE == kRecDecay || kTok == 8 ? kTok : kTok / 2;   // tokens that are finished at a time
   using Shape = RecShape<T, kTok>;
   using Lane = RecLane<T>;
   using Raw = typename Lane::Raw;
@@ -41,8 +41,8 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
   __shared__ __align__(16) float2 entry[2][CH];             // the state in front of a tile, and what reaches it from behind
   __shared__ RecAt ring[kRecRing];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int items = a.n_segs * a.cols;
-  RecFeed<WORDS, TILE, 5, true> feed{a, {a.ld_x * es, a.ld_g * es, a.ld_dy * es, a.ld_dx * es, a.ld_dg * es}, es};
+  const int items = a.items;
+  RecFeed<WORDS, TILE, 5, true> feed{a, {(int)(a.ld_x * es), (int)(a.ld_g * es), (int)(a.ld_dy * es), (int)(a.ld_dx * es), (int)(a.ld_dg * es)}, es};
   wait_for_predecessor();
   if (tid == 32 * kRecWarps) feed.begin(ring);
   __syncthreads();
@@ -124,9 +124,10 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
       for (int k = 0; k < kTok; ++k)
         if (k >= left) { av[k] = twice(1.f); mv[k] = twice(0.f); }
     }
-    Pair P = twice(1.f), H = twice(0.f), C = twice(0.f);
+    Pair P = twice(1.f), H = twice(0.f), C = twice(0.f), half_P, half_H;   // half: of the first half of the tokens
 #pragma unroll
     for (int k = 0; k < kTok; ++k) {
+      if (k == kTok / 2) { half_P = P; half_H = H; }
       P = mul2(P, av[k]);
       H = fma2(av[k], H, rec_input<MODE>(mv[k], read(0, k)));
       C = mul2(av[kTok - 1 - k], add2(C, read(2, kTok - 1 - k)));
@@ -143,6 +144,7 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
       H = C = twice(0.f);
 #pragma unroll
       for (int k = 0; k < kTok; ++k) {
+        if (k == kTok / 2) half_H = H;
         H = rec_step(av[k], H, rec_input<MODE>(mv[k], read(0, k)));
         C = none_where_zero(av[kTok - 1 - k], mul2(av[kTok - 1 - k], add2(C, read(2, kTok - 1 - k))));
       }
@@ -163,7 +165,7 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
         TP *= p;
         TC = rec_step(p, TC, back[i & 1][w][lane]);
       }
-      if (t.c0 + lane < a.D) rec_post(a.words + t.slot * a.D + t.c0 + lane, TP, TC);
+      if (t.c0 + lane < a.D) rec_post(a.words + (long long)t.slot * a.D + t.c0 + lane, TP, TC);
     }
     rec_meet<kRecEntry, kRecThreads>();
     const float4 e0 = *reinterpret_cast<const float4*>(&entry[i & 1][Shape::channel()]);
@@ -180,40 +182,51 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
     }
     if (second) h = rec_step(other_P, h, other_H);
     else C = rec_step(other_P, C, other_C);
-    Pair wv[kTok];
+    // The last part first: what multiplies e, in order, then e from behind
+    const Pair h_half = rec_step(half_P, h, half_H);
     if (t.whole && plain && !resets && !no_input) {
-#pragma unroll
-      for (int k = 0; k < kTok; ++k) {
-        const Pair x = read(0, k);
-        wv[k] = weight<MODE, false>(av[k], mv[k], h, x);
-        h = fma2(av[k], h, rec_input<MODE>(mv[k], x));
-      }
       char *dx_row = (char*)a.dx + t.at[3] + (at * a.ld_dx + Shape::channel()) * es, *dg_row = (char*)a.dg + t.at[4] + (at * a.ld_dg + Shape::channel()) * es;
       const uint32_t dx_step = (uint32_t)a.ld_dx * es, dg_step = (uint32_t)a.ld_dg * es;
 #pragma unroll
-      for (int k = kTok - 1; k >= 0; --k) {
-        const Pair e = add2(C, read(2, k));
-        *reinterpret_cast<Raw*>(dx_row + (unsigned long long)dx_step * k) = Lane::pack(rec_input<MODE>(mv[k], e));
-        *reinterpret_cast<Raw*>(dg_row + (unsigned long long)dg_step * k) = Lane::pack(mul2(wv[k], e));
-        C = mul2(av[k], e);
+      for (int k0 = kTok - kPart; k0 >= 0; k0 -= kPart) {
+        Pair wv[kPart], s = k0 ? h_half : h;
+#pragma unroll
+        for (int j = 0; j < kPart; ++j) {
+          const Pair x = read(0, k0 + j);
+          wv[j] = weight<MODE, false>(av[k0 + j], mv[k0 + j], s, x);
+          s = fma2(av[k0 + j], s, rec_input<MODE>(mv[k0 + j], x));
+        }
+#pragma unroll
+        for (int j = kPart - 1; j >= 0; --j) {
+          const int k = k0 + j;
+          const Pair e = add2(C, read(2, k));
+          *reinterpret_cast<Raw*>(dx_row + (unsigned long long)dx_step * k) = Lane::pack(rec_input<MODE>(mv[k], e));
+          *reinterpret_cast<Raw*>(dg_row + (unsigned long long)dg_step * k) = Lane::pack(mul2(wv[j], e));
+          C = mul2(av[k], e);
+        }
       }
     } else {
       const int c = t.c0 + Shape::channel();
-      T *dx_row = (T*)a.dx + (t.tok0 + at) * a.ld_dx, *dg_row = (T*)a.dg + (t.tok0 + at) * a.ld_dg;
+      T *dx_row = (T*)a.dx + (long long)(t.tok0 + at) * a.ld_dx, *dg_row = (T*)a.dg + (long long)(t.tok0 + at) * a.ld_dg;
 #pragma unroll
-      for (int k = 0; k < kTok; ++k) {
-        const Pair x = read(0, k);
-        wv[k] = none_where_zero(av[k], weight<MODE, true>(av[k], mv[k], h, x));
-        h = rec_step(av[k], h, rec_input<MODE>(mv[k], x));
-      }
+      for (int k0 = kTok - kPart; k0 >= 0; k0 -= kPart) {
+        Pair wv[kPart], s = k0 ? h_half : h;
 #pragma unroll
-      for (int k = kTok - 1; k >= 0; --k) {
-        const Pair e = add2(C, read(2, k));
-        if (k < left) {
-          rec_store(dx_row + k * a.ld_dx, c, a.D, dx_access, rec_input<MODE>(mv[k], e));
-          rec_store(dg_row + k * a.ld_dg, c, a.D, dg_access, mul2(wv[k], e));
+        for (int j = 0; j < kPart; ++j) {
+          const Pair x = read(0, k0 + j);
+          wv[j] = none_where_zero(av[k0 + j], weight<MODE, true>(av[k0 + j], mv[k0 + j], s, x));
+          s = rec_step(av[k0 + j], s, rec_input<MODE>(mv[k0 + j], x));
         }
-        C = none_where_zero(av[k], mul2(av[k], e));
+#pragma unroll
+        for (int j = kPart - 1; j >= 0; --j) {
+          const int k = k0 + j;
+          const Pair e = add2(C, read(2, k));
+          if (k < left) {
+            rec_store(dx_row + k * a.ld_dx, c, a.D, dx_access, rec_input<MODE>(mv[k], e));
+            rec_store(dg_row + k * a.ld_dg, c, a.D, dg_access, mul2(wv[j], e));
+          }
+          C = none_where_zero(av[k], mul2(av[k], e));
+        }
       }
     }
     __syncwarp();
@@ -226,9 +239,9 @@ cudaError_t launch_one(const RecArgs& a, cudaStream_t stream) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess || (e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-  constexpr size_t smem = 6 * (size_t)RecShape<T, rec_back_tok(MODE, sizeof(T))>::TENSOR;
+  constexpr size_t smem = 6 * (size_t)RecShape<T, rec_back_tok(sizeof(T))>::TENSOR;
   if ((e = allow_shared<gated_recurrence_backward_kernel<T, MODE, WORDS>>(smem)) != cudaSuccess) return e;
-  const long long items = (long long)a.n_segs * a.cols;
+  const long long items = a.items;
   if ((e = launch_early(gated_recurrence_backward_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, (long long)blocks(MODE, sizeof(T)) * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
   return launched();
 }

@@ -18,8 +18,8 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
   __shared__ __align__(8) float entry[2][CH];               // what enters a tile
   __shared__ RecAt ring[kRecRing];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int items = a.n_segs * a.cols;
-  RecFeed<WORDS, TILE, 3, false> feed{a, {a.ld_x * es, a.ld_g * es, a.ld_y * es}, es};
+  const int items = a.items;
+  RecFeed<WORDS, TILE, 3, false> feed{a, {(int)(a.ld_x * es), (int)(a.ld_g * es), (int)(a.ld_y * es)}, es};
   wait_for_predecessor();
   if (tid == 32 * kRecWarps) feed.begin(ring);
   __syncthreads();
@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
       if (lane == 0) feed.ask();
       const int c = t.c0 + lane, index = t.index;
       const bool in = c < a.D, first = index == 0, last = index + 1 == t.tiles;
-      const long long at = t.slot * a.D + c;
+      const long long at = (long long)t.slot * a.D + c;
       float h = 0.f;
       if (in) {
         if (first) h = a.h0 ? a.h0[(long long)t.seq * a.D + c] : 0.f;
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
         TP *= q.x;
         TH = rec_step(q.x, TH, q.y);
       }
-      if (t.c0 + lane < a.D) rec_post(a.words + t.slot * a.D + t.c0 + lane, TP, TH);
+      if (t.c0 + lane < a.D) rec_post(a.words + (long long)t.slot * a.D + t.c0 + lane, TP, TH);
     }
     P = twice(1.f);
     H = twice(0.f);
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
           *reinterpret_cast<Raw*>(row + (unsigned long long)step * k) = Lane::pack(h);
         }
       } else {
-        T* row = Y + (t.tok0 + first + Shape::group() * kTok) * a.ld_y;
+        T* row = Y + (long long)(t.tok0 + first + Shape::group() * kTok) * a.ld_y;
 #pragma unroll
         for (int k = 0; k < kTok; ++k) {
           h = rec_step(av[k], h, uv[k]);
@@ -229,7 +229,7 @@ cudaError_t launch_one(const RecArgs& a, cudaStream_t stream) {
   }
   constexpr size_t smem = 4 * (size_t)RecShape<T, kTok>::TENSOR;   // two tiles of two tensors
   if ((e = allow_shared<gated_recurrence_kernel<T, MODE, WORDS>>(smem)) != cudaSuccess) return e;
-  const long long items = (long long)a.n_segs * a.cols;
+  const long long items = a.items;
   if ((e = launch_early(gated_recurrence_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, (long long)kBlocks * n)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
   return launched();
 }

@@ -42,6 +42,12 @@ bool strides_fit(std::initializer_list<int64_t> lds) {   // sixteen rows are cou
 Span states_of(const tri_inv_rec_desc* d, const void* p) { return Span{p, (__int128)seqs_of(d) * d->D * 4}; }
 Span carries_of(const tri_inv_rec_desc* d, const void* p) { return Span{p, (__int128)slots_of(d, kRecCarry) * d->D * 4}; }
 
+// Sequences of so many tiles are walked whole, whatever the number of channels: the words cost a launch that clears them and, at each tile, the way through the L2 cache.  Longer ones go tile by tile, which
+// spreads them over the chip and lets no block be the last for long.  Measured (bf16, us, forward and gradient, tile by tile | whole): 1 x 200 tokens x 2048 channels 7.0 and 7.7 | 5.4 and 7.3; 1 x 333 x 2048 7.3 and 8.1 |
+// 6.4 and 9.0; 8 x 333 x 2048 14.6 and 21.4 | 11.2 and 21.0; 1 x 1000 x 2048 10.4 and 12.3 | 11.8 and 18.0; 1 x 4000 x 512 10.7 and 13.3 | 39 and 61; 16 x 1024 x 2048 40.5 and 73.5 | 42.6 and 77.9; 20 x 2048 x 2048
+// 88.5 and 163 | 85.6 and 170.
+constexpr int kMostWalked = 3, kMostWalkedBack = 2;
+
 // How a walk goes: tile by tile with words between the tiles, or whole sequences.
 struct RecPlan {
   int tile;
@@ -50,7 +56,7 @@ struct RecPlan {
   size_t table_bytes, word_bytes;   // word_bytes: with the ticket in front
   size_t bytes() const { return table_bytes + word_bytes; }
 };
-int plan(const tri_inv_rec_desc* d, int tile, RecPlan* p) {
+int plan(const tri_inv_rec_desc* d, int tile, int most_walked, RecPlan* p) {
   const int n_seqs = seqs_of(d);
   auto tiles_of = [&](long long n) { return std::max(1ll, (n + tile - 1) / tile); };
   long long tiles = 0, longest = 1;
@@ -66,11 +72,9 @@ int plan(const tri_inv_rec_desc* d, int tile, RecPlan* p) {
   }
   p->tile = tile;
   p->cols = (int)(((long long)d->D + kRecChannels - 1) / kRecChannels);
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return TRI_INV_ERR_CUDA;
-  p->words = longest > 1;
+  p->words = longest > most_walked;
   const long long segs = p->words ? tiles : n_seqs;
-  if (segs * p->cols > 0x40000000LL) return TRI_INV_ERR_INVALID_ARG;   // items are counted in 32 bits
+  if (segs * p->cols >= 0x3ff00000LL) return TRI_INV_ERR_INVALID_ARG;   // items are counted in 32 bits
   p->n_segs = (int)segs;
   p->table_bytes = d->cu_seqlens ? round_up((size_t)segs * sizeof(RecTile)) : 0;
   p->word_bytes = p->words ? 256 + round_up((size_t)slots_of(d, tile) * d->D * 8) : 0;
@@ -85,8 +89,8 @@ struct BackPlan {
 };
 int plan_back(const tri_inv_rec_desc* d, bool with_carries, BackPlan* p) {
   p->carry_bytes = with_carries ? 0 : round_up((size_t)slots_of(d, kRecCarry) * d->D * 4);
-  const int e = plan(d, rec_back_tile(d->mode, d->dtype == TRI_INV_F32 ? 4 : 2), &p->back);
-  return e ? e : plan(d, kRecTile, &p->front);
+  const int e = plan(d, rec_back_tile(d->dtype == TRI_INV_F32 ? 4 : 2), kMostWalkedBack, &p->back);
+  return e ? e : plan(d, kRecTile, kMostWalked, &p->front);
 }
 
 // The arguments that do not differ between the walks; the set-up of the workspace is enqueued
@@ -96,6 +100,9 @@ int begin_walk(RecArgs& a, const RecPlan& p, const tri_inv_rec_desc* d, void* wo
   if (!a.status) return TRI_INV_ERR_CUDA;
   a.n_seqs = seqs_of(d); a.T = d->T; a.D = d->D; a.cols = p.cols; a.n_segs = p.n_segs; a.mode = d->mode;
   if (p.n_segs == 0) return TRI_INV_OK;
+  a.items = p.n_segs * p.cols;
+  a.by_cols = rec_divide_by(p.cols);
+  a.by_seqs = rec_divide_by(a.n_seqs);
   if (d->T == 0) a.x = a.g = a.dy = a.status;   // no row is read, but the copies' addresses are formed
   RecTile* table = (RecTile*)workspace;
   a.table = d->cu_seqlens ? table : nullptr;
@@ -136,7 +143,7 @@ int tri_inv_gated_recurrence_workspace(const tri_inv_rec_desc* desc, size_t* byt
   if (rc) return rc;
   if (!bytes) return TRI_INV_ERR_INVALID_ARG;
   RecPlan p;
-  const int e = plan(desc, kRecTile, &p);
+  const int e = plan(desc, kRecTile, kMostWalked, &p);
   if (e) return e;
   *bytes = p.bytes();
   return TRI_INV_OK;
@@ -156,7 +163,7 @@ int tri_inv_gated_recurrence(const void* X, int64_t ldx, const void* G, int64_t 
       meets(span_of(y), s0) || meets_any(sc, span_of(x), span_of(g), span_of(y), s0))
     return TRI_INV_ERR_INVALID_ARG;
   RecPlan p;
-  const int e = plan(desc, kRecTile, &p);
+  const int e = plan(desc, kRecTile, kMostWalked, &p);
   if (e) return e;
   const Span work{workspace, (__int128)p.bytes()};
   if (workspace_bytes < p.bytes() || (p.bytes() > 0 && !workspace) || meets_any(work, span_of(x), span_of(g), span_of(y), s0, s1, sc)) return TRI_INV_ERR_INVALID_ARG;
@@ -173,7 +180,7 @@ int tri_inv_selftest_recurrence_wait_timeout(const void* X, const void* G, void*
   const int rc = check_rec(desc);
   if (rc) return rc;
   RecPlan p;
-  const int e = plan(desc, kRecTile, &p);
+  const int e = plan(desc, kRecTile, kMostWalked, &p);
   if (e) return e;
   if (!p.words || desc->cu_seqlens) return TRI_INV_ERR_UNSUPPORTED;
   if (!X || !G || !Y || !on_type(desc->dtype, X, G, Y) || !wait_limit_ns || !workspace || !aligned16(workspace) || workspace_bytes < p.bytes()) return TRI_INV_ERR_INVALID_ARG;
