@@ -13,27 +13,113 @@ namespace tri_inv {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kTable = kHeadsMaxDim / 2;   // angles of a token
 
-template <class T, int V> struct alignas(sizeof(T) * V) Vec { T v[V]; };
+// Two fp32 numbers that the arithmetic takes at a time: a pair of features
+struct Pair { unsigned long long v; };
+__device__ __forceinline__ Pair pair(float x, float y) { Pair d; asm("mov.b64 %0, {%1, %2};" : "=l"(d.v) : "f"(x), "f"(y)); return d; }
+__device__ __forceinline__ float2 both(Pair a) { float2 d; asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(a.v)); return d; }
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) { Pair d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v)); return d; }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return d; }
+__device__ __forceinline__ Pair twice(float x) { return pair(x, x); }
 
-__device__ __forceinline__ float up(float x) { return x; }
-__device__ __forceinline__ float up(__nv_bfloat16 x) { return __bfloat162float(x); }
+// V values as they lie in memory
+template <class T, int V> struct Vec;
+template <> struct Vec<__nv_bfloat16, 8> { using Raw = uint4; };
+template <> struct Vec<__nv_bfloat16, 4> { using Raw = uint2; };
+template <> struct Vec<__nv_bfloat16, 1> { using Raw = uint16_t; };
+template <> struct Vec<float, 4> { using Raw = uint4; };
+template <> struct Vec<float, 1> { using Raw = uint32_t; };
+// A lane's unit is two vectors, which hold the first and the second features of V pairs: halves of the head's turned part, or, interleaved, neighbours.  U and W are those features, in twos (one and a zero where V is 1).
+template <int V> constexpr int kTwos = V == 1 ? 1 : V / 2;
 template <class T, int V>
-__device__ __forceinline__ void load(float (&to)[V], const T* p) {
-  const Vec<T, V> raw = *reinterpret_cast<const Vec<T, V>*>(p);
+__device__ __forceinline__ float at(typename Vec<T, V>::Raw raw, int i) {
+  if constexpr (sizeof(T) == 4) {
+    return reinterpret_cast<const float*>(&raw)[i];
+  } else if constexpr (V == 1) {
+    return __uint_as_float((uint32_t)raw << 16);
+  } else {
+    const uint32_t u = reinterpret_cast<const uint32_t*>(&raw)[i / 2];
+    return __uint_as_float(i & 1 ? u & 0xffff0000u : u << 16);
+  }
+}
+template <class T, int V, bool INTER>
+__device__ __forceinline__ void widen(Pair (&U)[kTwos<V>], Pair (&W)[kTwos<V>], typename Vec<T, V>::Raw a, typename Vec<T, V>::Raw b) {
+  if constexpr (V == 1) {
+    U[0] = pair(at<T, V>(a, 0), 0.f);
+    W[0] = pair(at<T, V>(b, 0), 0.f);
+  } else if constexpr (INTER) {   // pairs 0 .. V / 2 - 1 are in a, the others in b
 #pragma unroll
-  for (int i = 0; i < V; ++i) to[i] = up(raw.v[i]);
+    for (int j = 0; j < V / 2; ++j) {
+      const auto raw = j < V / 4 ? a : b;
+      const int i = 4 * j % V;
+      U[j] = pair(at<T, V>(raw, i), at<T, V>(raw, i + 2));
+      W[j] = pair(at<T, V>(raw, i + 1), at<T, V>(raw, i + 3));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+      U[j] = pair(at<T, V>(a, 2 * j), at<T, V>(a, 2 * j + 1));
+      W[j] = pair(at<T, V>(b, 2 * j), at<T, V>(b, 2 * j + 1));
+    }
+  }
+}
+// ... and back, as values in the order of memory
+template <int V, bool INTER>
+__device__ __forceinline__ void spread(float (&a)[V], float (&b)[V], const Pair (&U)[kTwos<V>], const Pair (&W)[kTwos<V>]) {
+  if constexpr (V == 1) {
+    a[0] = both(U[0]).x;
+    b[0] = both(W[0]).x;
+  } else {
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+      const float2 u = both(U[j]), w = both(W[j]);
+      if constexpr (INTER) {
+        float* to = j < V / 4 ? a : b;
+        const int i = 4 * j % V;
+        to[i] = u.x; to[i + 1] = w.x; to[i + 2] = u.y; to[i + 3] = w.y;
+      } else {
+        a[2 * j] = u.x; a[2 * j + 1] = u.y; b[2 * j] = w.x; b[2 * j + 1] = w.y;
+      }
+    }
+  }
 }
 template <class T, int V>
 __device__ __forceinline__ void store(T* p, const float (&from)[V]) {
-  Vec<T, V> raw;
+  typename Vec<T, V>::Raw raw;
+  if constexpr (sizeof(T) == 4) {
+    float* f = reinterpret_cast<float*>(&raw);
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    if constexpr (sizeof(T) == 4) raw.v[i] = from[i];
-    else raw.v[i] = __float2bfloat16_rn(from[i]);
+    for (int i = 0; i < V; ++i) f[i] = from[i];
+  } else if constexpr (V == 1) {
+    const __nv_bfloat16 x = __float2bfloat16_rn(from[0]);
+    raw = reinterpret_cast<const uint16_t&>(x);
+  } else {
+    uint32_t* u = reinterpret_cast<uint32_t*>(&raw);
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      const __nv_bfloat162 x = __floats2bfloat162_rn(from[i], from[i + 1]);
+      u[i / 2] = reinterpret_cast<const uint32_t&>(x);
+    }
   }
-  *reinterpret_cast<Vec<T, V>*>(p) = raw;
+  *reinterpret_cast<typename Vec<T, V>::Raw*>(p) = raw;
 }
+
+// Asks for a vector of a lane's own, to a place in shared memory that only this lane reads; where it does not exist it reads as zero.  (Single 16-bit values go through a register.)
+template <class T, int V>
+__device__ __forceinline__ void request(typename Vec<T, V>::Raw* to, const T* from, const T* any, bool in) {
+  constexpr int BYTES = V * (int)sizeof(T);
+  if constexpr (BYTES == 2) {
+    *to = in ? *reinterpret_cast<const uint16_t*>(from) : (uint16_t)0;
+  } else {
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(in ? from : any), "r"(in ? 16 : 0) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(at), "l"(in ? from : any), "n"(BYTES), "r"(in ? BYTES : 0) : "memory");
+  }
+}
+
+// Steps of a warp in shared memory: of `bytes` a lane, tensor and half
+__host__ __device__ constexpr int steps(int bytes, bool back) { return bytes >= 16 ? (back ? 3 : 4) : back ? 4 : 6; }
 
 // f / 2 pi modulo 1 in units of 2^-64
 __device__ __forceinline__ unsigned long long fraction(float f) {
@@ -51,171 +137,239 @@ __device__ __forceinline__ void columns(int p, int r, bool interleaved, int& c0,
   c1 = c0 + (pairs ? r : V);
 }
 
-// Turns a lane's pairs; back: the other way
-template <int V, bool BACK>
-__device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const float2* table, int p, int r, bool interleaved) {
-  float2 cs[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) cs[i] = p * V + i < r ? table[p * V + i] : make_float2(1.f, 0.f);
-  auto one = [](float& u, float& v, float2 q) {
-    const float s = BACK ? -q.y : q.y, x = u, y = v;
-    u = x * q.x - y * s;
-    v = y * q.x + x * s;
-  };
-  if (interleaved) {
-    if constexpr (V == 1) {
-      one(a[0], b[0], cs[0]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V / 2; ++i) {
-        one(a[2 * i], a[2 * i + 1], cs[i]);
-        one(b[2 * i], b[2 * i + 1], cs[V / 2 + i]);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) one(a[i], b[i], cs[i]);
-  }
+// Turns two pairs by cs = (cos, cos', sin, sin')
+__device__ __forceinline__ void turn(Pair& u, Pair& w, float4 cs) {
+  const Pair c = pair(cs.x, cs.y), x = u;
+  u = fma2(u, c, mul2(w, pair(-cs.z, -cs.w)));
+  w = fma2(w, c, mul2(x, pair(cs.z, cs.w)));
 }
 
 struct HeadsPlan {
   int blocks[2];       // of queries and of keys
   int parts[2];        // warps that share a token's heads
 };
+// Where a warp stands: HEADS heads of a token at a time, `left` of them in all to go
+struct At {
+  long long item;
+  int left;
+  const char *x, *dy;   // of the lane's head
+};
 
-// NU: units (pairs of vectors) of a lane
-template <class T, int V, int LANES, int NU, bool BACK>
-__global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const __grid_constant__ HeadsArgs a, const __grid_constant__ HeadsPlan plan) {
-  constexpr int HEADS = 32 / LANES;   // of a warp at a time
-  __shared__ unsigned long long freq[kHeadsMaxDim / 2];
-  __shared__ float2 tables[kWarps][kHeadsMaxDim / 2];
-  __shared__ float joined[BACK ? kWarps : 1][BACK ? kHeadsMaxDim : 1];
+// NU: units of a lane.  A warp's next STEPS - 1 steps are on their way to shared memory while it works on one.
+template <class T, int V, int LANES, int NU, bool BACK, bool INTER>
+__global__ void __launch_bounds__(kThreads, BACK ? 3 : 4) qk_norm_rope_kernel(const __grid_constant__ HeadsArgs a, const __grid_constant__ HeadsPlan plan) {
+  using Raw = typename Vec<T, V>::Raw;
+  constexpr int HEADS = 32 / LANES, N = kTwos<V>, UNITS = LANES * NU, es = sizeof(T);
+  constexpr int STEPS = steps(V * es * NU, BACK), TENSORS = BACK ? 2 : 1;
+  extern __shared__ __align__(16) unsigned char dynamic[];
+  __shared__ unsigned long long freq[kTable];
+  __shared__ int places[kWarps][STEPS];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, sub = lane / LANES, t = lane % LANES;
+  float4* table = reinterpret_cast<float4*>(dynamic) + warp * kTable;   // of angles 2 j, 2 j + 1 of unit p at [j][p], so that the lanes of a head read side by side
+  Raw* ring = reinterpret_cast<Raw*>(dynamic + kWarps * kTable * sizeof(float4)) + warp * STEPS * TENSORS * NU * 2 * 32 + lane;
   const int which = (int)blockIdx.x >= plan.blocks[0], block = blockIdx.x - (which ? plan.blocks[0] : 0);
   const HeadsSide& s = a.side[which];
   const T *X = (const T*)s.x, *W = (const T*)s.w, *DY = (const T*)s.dy;
   wait_for_predecessor();
-  for (int i = tid; i < a.r; i += kThreads) freq[i] = fraction(a.inv_freq[i]);
+
+  const int parts = plan.parts[which], per = ((s.H + HEADS - 1) / HEADS + parts - 1) / parts * HEADS;   // heads of a part
+  const long long items = a.tokens * parts, stride = (long long)plan.blocks[which] * kWarps;
+  auto token_of = [&](long long item) { return parts == 1 ? item : item / parts; };
+  auto first_of = [&](long long item) { return parts == 1 ? 0 : (int)(item - item / parts * parts) * per; };
+  auto place = [&](At& p) {   // an item's first step; items without heads (a token's last part may have none) are passed over
+    for (;; p.item += stride) {
+      if (p.item >= items) return;
+      const int h = first_of(p.item);
+      p.left = min(s.H - h, per);
+      if (p.left <= 0) continue;
+      const long long token = token_of(p.item);
+      p.x = (const char*)(X + token * s.ld_x + (long long)(h + sub) * a.d);
+      if (BACK) p.dy = (const char*)(DY + token * s.ld_dy + (long long)(h + sub) * a.d);
+      return;
+    }
+  };
+  const int step_bytes = HEADS * a.d * es;
   int c0[NU], c1[NU];
-  float w0[NU][V], w1[NU][V], g0[BACK ? NU : 1][V], g1[BACK ? NU : 1][V];
+#pragma unroll
+  for (int k = 0; k < NU; ++k) columns<V>(k * LANES + t, a.r, INTER, c0[k], c1[k]);
+  // Asks for the step at p, and goes on to the next
+  auto ask = [&](At& p, int slot, bool fresh) {
+    if (p.item < items) {
+      if (fresh && lane == 0) {
+        const long long token = token_of(p.item);
+        if (a.positions) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(&places[warp][slot])), "l"(a.positions + token) : "memory");
+        else places[warp][slot] = (int)(token % a.T);
+      }
+#pragma unroll
+      for (int k = 0; k < NU; ++k) {
+        Raw* to = ring + (slot * NU + k) * TENSORS * 2 * 32;
+        const bool i0 = sub < p.left && c0[k] < a.d, i1 = sub < p.left && c1[k] < a.d;
+        request<T, V>(to, (const T*)p.x + c0[k], X, i0);
+        request<T, V>(to + 32, (const T*)p.x + c1[k], X, i1);
+        if constexpr (BACK) {
+          request<T, V>(to + 64, (const T*)p.dy + c0[k], DY, i0);
+          request<T, V>(to + 96, (const T*)p.dy + c1[k], DY, i1);
+        }
+      }
+      p.left -= HEADS;
+      p.x += step_bytes;
+      if (BACK) p.dy += step_bytes;
+      if (p.left <= 0) {
+        p.item += stride;
+        place(p);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  At ahead;
+  ahead.item = (long long)block * kWarps + warp;
+  place(ahead);
+  At now = ahead;
+  long long asked = -1;   // the item whose position has been asked for
+#pragma unroll
+  for (int i = 0; i < STEPS - 1; ++i) {
+    const long long item = ahead.item;
+    ask(ahead, i, item != asked);
+    asked = item;
+  }
+
+  for (int i = tid; i < a.r; i += kThreads) freq[i] = fraction(a.inv_freq[i]);
+  auto angle = [&](int f) { return reinterpret_cast<float*>(table) + (V == 1 ? 4 * f : f % V / 2 * UNITS * 4 + f / V * 4 + f % 2); };   // its cosine; its sine is two further on
+  for (int f = a.r + lane; f < UNITS * V; f += 32) { angle(f)[0] = 1.f; angle(f)[2] = 0.f; }   // what is not turned
+  if (V == 1)
+    for (int f = lane; f < UNITS; f += 32) { angle(f)[1] = 1.f; angle(f)[3] = 0.f; }
+  Pair wu[NU][N], ww[NU][N], gu[BACK ? NU : 1][N], gw[BACK ? NU : 1][N];
 #pragma unroll
   for (int k = 0; k < NU; ++k) {
-    columns<V>(k * LANES + t, a.r, a.interleaved, c0[k], c1[k]);
+    Raw raw[2];
+    T* v = reinterpret_cast<T*>(raw);
 #pragma unroll
-    for (int i = 0; i < V; ++i) w0[k][i] = w1[k][i] = 1.f;
-    if (W && c0[k] < a.d) load<T, V>(w0[k], W + c0[k]);
-    if (W && c1[k] < a.d) load<T, V>(w1[k], W + c1[k]);
+    for (int i = 0; i < V; ++i) {
+      v[i] = W && c0[k] < a.d ? W[c0[k] + i] : T(1.f);
+      v[V + i] = W && c1[k] < a.d ? W[c1[k] + i] : T(1.f);
+    }
+    widen<T, V, INTER>(wu[k], ww[k], raw[0], raw[1]);
     if constexpr (BACK)
 #pragma unroll
-      for (int i = 0; i < V; ++i) g0[k][i] = g1[k][i] = 0.f;
+      for (int j = 0; j < N; ++j) gu[k][j] = gw[k][j] = twice(0.f);
   }
   __syncthreads();
-  float2* table = tables[warp];
-  const int parts = plan.parts[which], per = ((s.H + HEADS - 1) / HEADS + parts - 1) / parts * HEADS;   // heads of a part
-  const long long items = a.tokens * parts;
+
   const float over_d = 1.f / (float)a.d;
-  for (long long item = (long long)block * kWarps + warp; item < items; item += (long long)plan.blocks[which] * kWarps) {
-    const long long token = item / parts;
-    const int first = (int)(item - token * parts) * per, end = min(s.H, first + per);
-    const int position = a.positions ? a.positions[token] : (int)(token % a.T);
-    const bool real = position >= 0;
-    __syncwarp();
-    for (int i = lane; i < a.r; i += 32) {
-      const int turns = (int)(((unsigned long long)(unsigned)position * freq[i]) >> 32);   // of 2^-32 of a whole one, signed
-      float sn, cs;
-      sincospif((float)turns * 4.656612873077393e-10f, &sn, &cs);   // 2^-31
-      table[i] = make_float2(cs, sn);
+  T* to = nullptr;
+  bool real = false, fresh = true;   // fresh: the step is its item's first
+  for (int slot = 0; now.item < items; slot = slot + 1 == STEPS ? 0 : slot + 1) {
+    {
+      const long long item = ahead.item;
+      ask(ahead, slot == 0 ? STEPS - 1 : slot - 1, item != asked);
+      asked = item;
     }
-    __syncwarp();
-    for (int h0 = first; h0 < end; h0 += HEADS) {
-      const int h = h0 + sub;
-      const bool in = h < end && real;
-      const T* x = X + token * s.ld_x + (long long)h * a.d;
-      float x0[NU][V], x1[NU][V], y0[NU][V], y1[NU][V];
+    asm volatile("cp.async.wait_group %0;" ::"n"(STEPS - 1) : "memory");
+    if (fresh) {
+      const long long token = token_of(now.item);
+      to = (BACK ? (T*)s.dx + token * s.ld_dx : (T*)s.y + token * s.ld_y) + (long long)(first_of(now.item) + sub) * a.d;
+      __syncwarp();
+      const int position = places[warp][slot];
+      real = position >= 0;
+      for (int f = lane; f < a.r; f += 32) {
+        const int turns = (int)(((unsigned long long)(unsigned)position * freq[f]) >> 32);   // of 2^-32 of a whole one, signed
+        float sn, cs;
+        sincospif((float)turns * 4.656612873077393e-10f, &sn, &cs);   // 2^-31
+        angle(f)[0] = cs;
+        angle(f)[2] = BACK ? -sn : sn;
+      }
+      __syncwarp();
+    }
+    Pair xu[NU][N], xw[NU][N], yu[NU][N], yw[NU][N], sum = twice(0.f), mixed = twice(0.f);
 #pragma unroll
-      for (int k = 0; k < NU; ++k) {
+    for (int k = 0; k < NU; ++k) {
+      const Raw* from = ring + (slot * NU + k) * TENSORS * 2 * 32;
+      widen<T, V, INTER>(xu[k], xw[k], from[0], from[32]);
+      if constexpr (BACK) widen<T, V, INTER>(yu[k], yw[k], from[64], from[96]);
 #pragma unroll
-        for (int i = 0; i < V; ++i) x0[k][i] = x1[k][i] = y0[k][i] = y1[k][i] = 0.f;
-        if (in && c0[k] < a.d) load<T, V>(x0[k], x + c0[k]);
-        if (in && c1[k] < a.d) load<T, V>(x1[k], x + c1[k]);
+      for (int j = 0; j < N; ++j) {
+        sum = fma2(xu[k][j], xu[k][j], fma2(xw[k][j], xw[k][j], sum));
         if constexpr (BACK) {
-          const T* dy = DY + token * s.ld_dy + (long long)h * a.d;
-          if (in && c0[k] < a.d) load<T, V>(y0[k], dy + c0[k]);
-          if (in && c1[k] < a.d) load<T, V>(y1[k], dy + c1[k]);
+          turn(yu[k][j], yw[k][j], table[j * UNITS + k * LANES + t]);
+          mixed = fma2(mul2(yu[k][j], wu[k][j]), xu[k][j], fma2(mul2(yw[k][j], ww[k][j]), xw[k][j], mixed));
         }
       }
-      float sum = 0.f, mixed = 0.f;
+    }
+    float total = both(sum).x + both(sum).y, mix = BACK ? both(mixed).x + both(mixed).y : 0.f;
 #pragma unroll
-      for (int k = 0; k < NU; ++k) {
-        if constexpr (BACK) turn<V, true>(y0[k], y1[k], table, k * LANES + t, a.r, a.interleaved);
+    for (int m = LANES / 2; m >= 1; m >>= 1) {
+      total += __shfl_xor_sync(0xffffffffu, total, m);
+      if constexpr (BACK) mix += __shfl_xor_sync(0xffffffffu, mix, m);
+    }
+    const float rstd = rsqrtf(total * over_d + a.eps);
+    const Pair rstd2 = twice(rstd), pull = twice(-rstd * rstd * rstd * (mix * over_d));
+    const bool in = sub < now.left;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          sum = fmaf(x0[k][i], x0[k][i], fmaf(x1[k][i], x1[k][i], sum));
-          if constexpr (BACK) mixed = fmaf(y0[k][i] * w0[k][i], x0[k][i], fmaf(y1[k][i] * w1[k][i], x1[k][i], mixed));
-        }
-      }
+    for (int k = 0; k < NU; ++k) {
 #pragma unroll
-      for (int m = LANES / 2; m >= 1; m >>= 1) {
-        sum += __shfl_xor_sync(0xffffffffu, sum, m);
-        if constexpr (BACK) mixed += __shfl_xor_sync(0xffffffffu, mixed, m);
-      }
-      const float rstd = real ? rsqrtf(sum * over_d + a.eps) : 0.f;
-      if constexpr (BACK) {
-        const float pull = rstd * rstd * (mixed * over_d);
-#pragma unroll
-        for (int k = 0; k < NU; ++k)
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            if (in) {
-              g0[k][i] = fmaf(y0[k][i], x0[k][i] * rstd, g0[k][i]);
-              g1[k][i] = fmaf(y1[k][i], x1[k][i] * rstd, g1[k][i]);
-            }
-            y0[k][i] = rstd * (y0[k][i] * w0[k][i] - x0[k][i] * pull);
-            y1[k][i] = rstd * (y1[k][i] * w1[k][i] - x1[k][i] * pull);
+      for (int j = 0; j < N; ++j) {
+        if constexpr (BACK) {
+          if (in && real) {
+            gu[k][j] = fma2(yu[k][j], mul2(xu[k][j], rstd2), gu[k][j]);
+            gw[k][j] = fma2(yw[k][j], mul2(xw[k][j], rstd2), gw[k][j]);
           }
-      } else {
-#pragma unroll
-        for (int k = 0; k < NU; ++k) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            y0[k][i] = x0[k][i] * (rstd * w0[k][i]);
-            y1[k][i] = x1[k][i] * (rstd * w1[k][i]);
-          }
-          turn<V, false>(y0[k], y1[k], table, k * LANES + t, a.r, a.interleaved);
+          yu[k][j] = fma2(xu[k][j], pull, mul2(mul2(yu[k][j], wu[k][j]), rstd2));
+          yw[k][j] = fma2(xw[k][j], pull, mul2(mul2(yw[k][j], ww[k][j]), rstd2));
+        } else {
+          yu[k][j] = mul2(xu[k][j], mul2(rstd2, wu[k][j]));
+          yw[k][j] = mul2(xw[k][j], mul2(rstd2, ww[k][j]));
+          turn(yu[k][j], yw[k][j], table[j * UNITS + k * LANES + t]);
         }
       }
-      if (h < end) {
-        T* y = BACK ? (T*)s.dx + token * s.ld_dx + (long long)h * a.d : (T*)s.y + token * s.ld_y + (long long)h * a.d;
+      float v0[V], v1[V];
+      spread<V, INTER>(v0, v1, yu[k], yw[k]);
+      if (!real)
 #pragma unroll
-        for (int k = 0; k < NU; ++k) {
-          if (!real)
-#pragma unroll
-            for (int i = 0; i < V; ++i) y0[k][i] = y1[k][i] = 0.f;
-          if (c0[k] < a.d) store<T, V>(y + c0[k], y0[k]);
-          if (c1[k] < a.d) store<T, V>(y + c1[k], y1[k]);
-        }
-      }
+        for (int i = 0; i < V; ++i) v0[i] = v1[i] = 0.f;
+      if (in && c0[k] < a.d) store<T, V>(to + c0[k], v0);
+      if (in && c1[k] < a.d) store<T, V>(to + c1[k], v1);
+    }
+    now.left -= HEADS;
+    to += HEADS * a.d;
+    fresh = now.left <= 0;
+    if (fresh) {
+      now.item += stride;
+      place(now);
     }
   }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
   if constexpr (BACK) {   // the block's sums for the weight: heads side by side, then the warps
+    __syncthreads();
+    float* joined = reinterpret_cast<float*>(dynamic);   // [kWarps][kHeadsMaxDim], in place of the tables
 #pragma unroll
-    for (int k = 0; k < NU; ++k)
+    for (int k = 0; k < NU; ++k) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
+      for (int j = 0; j < N; ++j) {
+        float2 u = both(gu[k][j]), w = both(gw[k][j]);
 #pragma unroll
         for (int m = LANES; m < 32; m <<= 1) {
-          g0[k][i] += __shfl_xor_sync(0xffffffffu, g0[k][i], m);
-          g1[k][i] += __shfl_xor_sync(0xffffffffu, g1[k][i], m);
+          u.x += __shfl_xor_sync(0xffffffffu, u.x, m);
+          u.y += __shfl_xor_sync(0xffffffffu, u.y, m);
+          w.x += __shfl_xor_sync(0xffffffffu, w.x, m);
+          w.y += __shfl_xor_sync(0xffffffffu, w.y, m);
         }
-        if (sub == 0 && c0[k] < a.d) joined[warp][c0[k] + i] = g0[k][i];
-        if (sub == 0 && c1[k] < a.d) joined[warp][c1[k] + i] = g1[k][i];
+        gu[k][j] = pair(u.x, u.y);
+        gw[k][j] = pair(w.x, w.y);
       }
+      float v0[V], v1[V];
+      spread<V, INTER>(v0, v1, gu[k], gw[k]);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (sub == 0 && c0[k] < a.d) joined[warp * kHeadsMaxDim + c0[k] + i] = v0[i];
+        if (sub == 0 && c1[k] < a.d) joined[warp * kHeadsMaxDim + c1[k] + i] = v1[i];
+      }
+    }
     __syncthreads();
     for (int c = tid; c < a.d; c += kThreads) {
-      float g = 0.f;
+      float sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) g += joined[w][c];
-      a.partial[(long long)blockIdx.x * a.d + c] = g;
+      for (int w = 0; w < kWarps; ++w) sum += joined[w * kHeadsMaxDim + c];
+      a.partial[(long long)blockIdx.x * a.d + c] = sum;
     }
   }
 }
@@ -259,14 +413,16 @@ HeadsPlan plan_of(const HeadsArgs& a, int heads, int sms, int most) {
   return p;
 }
 
-template <class T, int V, int LANES, int NU, bool BACK>
+template <class T, int V, int LANES, int NU, bool BACK, bool INTER>
 cudaError_t launch_one(const HeadsArgs& a, cudaStream_t stream) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess || (e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-  const HeadsPlan p = plan_of(a, 32 / LANES, sms, BACK ? std::min(kHeadsPartials, 2 * sms) : 8 * sms);
+  constexpr size_t smem = (size_t)kWarps * (kTable * sizeof(float4) + (size_t)steps(V * (int)sizeof(T) * NU, BACK) * (BACK ? 2 : 1) * NU * 2 * 32 * V * sizeof(T));
+  if ((e = allow_shared<qk_norm_rope_kernel<T, V, LANES, NU, BACK, INTER>>(smem)) != cudaSuccess) return e;
+  const HeadsPlan p = plan_of(a, 32 / LANES, sms, BACK ? std::min(kHeadsPartials - 1, 3 * sms) : 4 * sms);
   if (p.blocks[0] + p.blocks[1] > 0) {
-    if ((e = launch_early(qk_norm_rope_kernel<T, V, LANES, NU, BACK>, dim3(p.blocks[0] + p.blocks[1]), kThreads, 0, stream, a, p)) != cudaSuccess) return e;
+    if ((e = launch_early(qk_norm_rope_kernel<T, V, LANES, NU, BACK, INTER>, dim3(p.blocks[0] + p.blocks[1]), kThreads, smem, stream, a, p)) != cudaSuccess) return e;
     if ((e = launched()) != cudaSuccess) return e;
   }
   if constexpr (BACK) {
@@ -277,16 +433,17 @@ cudaError_t launch_one(const HeadsArgs& a, cudaStream_t stream) {
   return cudaSuccess;
 }
 
-template <class T, int V, bool BACK>
+template <class T, int V, bool BACK, bool INTER>
 cudaError_t launch_width(const HeadsArgs& a, cudaStream_t stream) {
-  const int first = a.interleaved ? 0 : a.r / V, rest = a.d / V - 2 * first, units = first + (rest + 1) / 2;
+  const int first = INTER ? 0 : a.r / V, rest = a.d / V - 2 * first, units = first + (rest + 1) / 2;
   if constexpr (V == 1) {
-    if (units <= 32) return launch_one<T, 1, 32, 1, BACK>(a, stream);
-    return units <= 64 ? launch_one<T, 1, 32, 2, BACK>(a, stream) : launch_one<T, 1, 32, 4, BACK>(a, stream);
+    if (units <= 32) return launch_one<T, 1, 32, 1, BACK, INTER>(a, stream);
+    return units <= 64 ? launch_one<T, 1, 32, 2, BACK, INTER>(a, stream) : launch_one<T, 1, 32, 4, BACK, INTER>(a, stream);
   } else {
-    if (units <= 4) return launch_one<T, V, 4, 1, BACK>(a, stream);
-    if (units <= 8) return launch_one<T, V, 8, 1, BACK>(a, stream);
-    return units <= 16 ? launch_one<T, V, 16, 1, BACK>(a, stream) : launch_one<T, V, 32, 1, BACK>(a, stream);
+    if (units <= 4) return launch_one<T, V, 4, 1, BACK, INTER>(a, stream);
+    if (units <= 8) return launch_one<T, V, 8, 1, BACK, INTER>(a, stream);
+    if constexpr (V == 8) return launch_one<T, V, 16, 1, BACK, INTER>(a, stream);
+    else return units <= 16 ? launch_one<T, V, 16, 1, BACK, INTER>(a, stream) : launch_one<T, V, 32, 1, BACK, INTER>(a, stream);
   }
 }
 
@@ -304,9 +461,9 @@ cudaError_t launch_type(const HeadsArgs& a, cudaStream_t stream) {
   }
   auto fits = [&](int v) { return (at & (v * sizeof(T) - 1)) == 0 && a.d % v == 0 && (a.interleaved || a.r % v == 0); };
   if constexpr (sizeof(T) == 2)
-    if (fits(8)) return launch_width<T, 8, BACK>(a, stream);
-  if (fits(4)) return launch_width<T, 4, BACK>(a, stream);
-  return launch_width<T, 1, BACK>(a, stream);
+    if (fits(8)) return a.interleaved ? launch_width<T, 8, BACK, true>(a, stream) : launch_width<T, 8, BACK, false>(a, stream);
+  if (fits(4)) return a.interleaved ? launch_width<T, 4, BACK, true>(a, stream) : launch_width<T, 4, BACK, false>(a, stream);
+  return a.interleaved ? launch_width<T, 1, BACK, true>(a, stream) : launch_width<T, 1, BACK, false>(a, stream);
 }
 
 }  // namespace

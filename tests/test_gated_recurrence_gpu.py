@@ -11,7 +11,8 @@ MODES = [oracle.DECAY, oracle.NORMED, oracle.GATE]
 NAMES = {"ids": ["decay", "normed", "gate"]}
 # (lengths, D, packed): one token, tiles' edges, odd widths, many sequences, long ones
 SHAPES = [([1], 1, False), ([1] * 3, 33, False), ([63], 64, False), ([64], 65, False), ([65] * 2, 31, False), ([128] * 3, 128, False), ([333], 200, False), ([1000] * 2, 72, False),
-          ([700] * 9, 1100, False), ([5000], 6, False), ([17, 0, 64, 65, 1, 200, 0, 129], 40, True), ([3, 300, 1], 129, True), ([0, 0], 10, True), ([1] * 400, 16, True), ([64] * 40, 257, True)]
+          ([700] * 9, 1100, False), ([5000], 6, False), ([17, 0, 64, 65, 1, 200, 0, 129], 40, True), ([3, 300, 1], 129, True), ([0, 0], 10, True), ([1] * 400, 16, True), ([64] * 40, 257, True),
+          ([1000, 5, 0, 450, 129, 640], 40, True), ([400 + i % 3 for i in range(330)], 33, True)]
 
 
 @pytest.fixture(scope="module")
