@@ -202,7 +202,7 @@ class _NoNative:
 
 
 def _operators():
-    """The extension's functions for linear attention and the RMS norm, bound to the loaded library (once)."""
+    """The extension's functions for linear attention, the norms and the gated recurrence, bound to the loaded library (once)."""
     global _native_ops
     if _native_ops is None:
         load_native()   # its warning where the extension is missing
@@ -211,6 +211,8 @@ def _operators():
             addr = lambda f: ctypes.cast(getattr(load(), "tri_inv_" + f), ctypes.c_void_p).value   # noqa: E731
             _native.bind_operators(*(addr(f) for f in ("linear_attention_workspace", "linear_attention", "linear_attention_backward_workspace", "linear_attention_backward",
                                                        "linear_attention_step", "rms_norm", "rms_norm_backward_workspace", "rms_norm_backward")))
+            _native.bind_mixers(*(addr(f) for f in ("gated_recurrence_carries", "gated_recurrence_workspace", "gated_recurrence", "gated_recurrence_backward_workspace", "gated_recurrence_backward",
+                                                    "gated_recurrence_step", "qk_norm_rope", "qk_norm_rope_backward_workspace", "qk_norm_rope_backward")))
             _native_ops = _native
         except (ImportError, AttributeError):
             _native_ops = _NoNative()
@@ -599,6 +601,10 @@ def gated_recurrence(X, G, mode=REC_DECAY, h0=None, cu_seqlens=None, out=None, w
     """The gated linear recurrence h_t = a_t h_{t-1} + u_t of every channel -> (Y, h_final or None, carries or None).  X, G, Y [B,T,D] (slices of one projection's output need no
     copy); h0, h_final [sequences,D] fp32 (``state_out`` may be h0 itself).  ``mode``: REC_DECAY a = exp(G), u = X; REC_NORMED a = exp(G), u = sqrt(1 - a^2) X;
     REC_GATE a = sigmoid(G), u = (1 - a) X.  ``want_carries``: the states that ``gated_recurrence_backward`` takes to save a walk.  ``out`` may be X or G itself."""
+    if out is None and state_out is None and stream is None:
+        made = (_native_ops or _operators()).gated_recurrence(X, G, mode, h0, cu_seqlens, bool(want_state), bool(want_carries))
+        if made is not None:
+            return _marshalled(made, "tri_inv_gated_recurrence")
     desc, keep, st = _rec_desc(X, mode, cu_seqlens)
     dt, f32 = X.dtype, torch.float32
     x, g, s0 = _rows("X", X, X.shape, dt), _rows("G", G, X.shape, dt), _optional("h0", h0, st, f32)
@@ -630,6 +636,10 @@ def gated_recurrence_backward(dY, X, G, mode=REC_DECAY, h0=None, dh=None, carrie
     states are walked again.  ``want_dh0``: by default where h0 is given.  ``out`` = (dX, dG), which may be slices of one projection's gradient."""
     if want_dh0 is None:
         want_dh0 = h0 is not None
+    if out is None and stream is None:
+        made = (_native_ops or _operators()).gated_recurrence_backward(dY, X, G, mode, h0, dh, carries, cu_seqlens, bool(want_dh0))
+        if made is not None:
+            return _marshalled(made, "tri_inv_gated_recurrence_backward")
     desc, keep, st = _rec_desc(X, mode, cu_seqlens)
     dt, f32 = X.dtype, torch.float32
     args = [*_rows("dY", dY, X.shape, dt), *_rows("X", X, X.shape, dt), *_rows("G", G, X.shape, dt), _optional("h0", h0, st, f32), _optional("dh", dh, st, f32),
@@ -647,6 +657,10 @@ def gated_recurrence_backward(dY, X, G, mode=REC_DECAY, h0=None, dh=None, carrie
 def gated_recurrence_step(X, G, h, mode=REC_DECAY, slots=None, out=None, stream=None):
     """One token for each row, on states that lie in the slots of a cache and are updated in place -> Y [B,D].  X, G [B,D], h [n_slots,D] fp32, slots [B] int32 (negative: a padded
     row, output zero) or None: row b has slot b.  Slots that do not differ, or lie past the cache, are left out and show in ``last_device_status``.  ``out`` may be X or G itself."""
+    if out is None and stream is None:
+        made = (_native_ops or _operators()).gated_recurrence_step(X, G, h, mode, slots)
+        if made is not None:
+            return _marshalled(made, "tri_inv_gated_recurrence_step")
     if X.dim() != 2 or h.dim() != 2:
         raise ValueError("X must be [B, D] and h [slots, D], got %s and %s" % (tuple(X.shape), tuple(h.shape)))
     B, D = X.shape
@@ -681,6 +695,10 @@ def qk_norm_rope(Q, K, wq, wk, inv_freq, positions=None, eps=1e-6, interleaved=F
     """The RMS norm of each query and key head, then the rotation of the pairs of its first 2 len(inv_freq) features by the angles position x inv_freq -> (Yq, Yk).  Q [...,heads,d], K [...,key
     heads,d] or None (slices of one projection's output need no copy), wq, wk [d] or None (ones), inv_freq [r] fp32 or None (no rotation), positions int32, one for each token (negative: a padded
     token, outputs zero) or None: a token's index along the dimension in front of the heads.  Pairs are (i, i + r), or (2 i, 2 i + 1) if ``interleaved``.  ``out`` = (Yq, Yk), which may be Q and K."""
+    if out is None and stream is None:
+        made = (_native_ops or _operators()).qk_norm_rope(Q, K, wq, wk, inv_freq, positions, eps, interleaved)
+        if made is not None:
+            return _marshalled(made, "tri_inv_qk_norm_rope")
     desc, small = _heads_call(Q, K, inv_freq, positions, eps, interleaved, wq, wk)
     q, k = _heads_rows("Q", Q, Q), _heads_rows("K", K, K)
     (Yq, Yk), _ = _made_for(stream, lambda: (torch.empty(Q.shape, dtype=Q.dtype, device=Q.device), None if K is None else torch.empty(K.shape, dtype=K.dtype, device=K.device))) if out is None else (out, None)
@@ -693,6 +711,10 @@ def qk_norm_rope(Q, K, wq, wk, inv_freq, positions=None, eps=1e-6, interleaved=F
 def qk_norm_rope_backward(dYq, dYk, Q, K, wq, wk, inv_freq, positions=None, eps=1e-6, interleaved=False, out=None, stream=None):
     """The gradient of ``qk_norm_rope`` -> (dQ, dK, dwq, dwk), from those of its outputs and its other arguments as they were; None for what was None.  ``out`` = (dQ, dK), which
     may be slices of one projection's gradient, or dYq and dYk, or Q and K."""
+    if out is None and stream is None:
+        made = (_native_ops or _operators()).qk_norm_rope_backward(Q, K, wq, wk, inv_freq, positions, eps, interleaved, dYq, dYk)
+        if made is not None:
+            return _marshalled(made, "tri_inv_qk_norm_rope_backward")
     desc, small = _heads_call(Q, K, inv_freq, positions, eps, interleaved, wq, wk)
     rows = [*_heads_rows("dYq", dYq, Q), *_heads_rows("dYk", dYk, K), *_heads_rows("Q", Q, Q), *_heads_rows("K", K, K)]
     need = _workspace("tri_inv_qk_norm_rope_backward_workspace", desc)

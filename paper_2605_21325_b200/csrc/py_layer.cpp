@@ -1,5 +1,5 @@
-// The marshalling of binding.gdn_forward, of the linear attention and of the RMS norm in native code: shape checks, the outputs, the workspace and the call, for the ordinary case of
-// plain contiguous CUDA tensors on the current stream.  Whatever else comes (other types, other devices, arguments that convert) makes a function return None, and the
+// The marshalling of binding.gdn_forward, of the linear attention, the RMS norm, the gated recurrence and the heads' norm with rotation in native code: shape checks, the outputs, the workspace and the call, for the ordinary case of
+// plain CUDA tensors (contiguous, or, where the function takes them, with rows at one distance) on the current stream.  Whatever else comes (other types, other devices, arguments that convert) makes a function return None, and the
 // Python body of the binding's function takes the call, with its conversions and its errors.
 //
 // A decode step is one kernel of 5.7 us; eight data pointers, a descriptor, two allocations and two calls through ctypes took 12.9 us of host time for it; a token of linear
@@ -9,6 +9,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <c10/cuda/CUDAStream.h>
 
+#include <algorithm>
 #include <climits>
 #include <vector>
 
@@ -303,11 +304,243 @@ PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- gated recurrence and the heads' norm with rotation
+
+using RecRowsFn = int (*)(const tri_inv_rec_desc*, int64_t*);
+using RecBytesFn = int (*)(const tri_inv_rec_desc*, size_t*);
+using RecFn = int (*)(const void*, int64_t, const void*, int64_t, const float*, void*, int64_t, float*, float*, void*, size_t, const tri_inv_rec_desc*, void*);
+using RecBackBytesFn = int (*)(const tri_inv_rec_desc*, int, size_t*);
+using RecBackFn = int (*)(const void*, int64_t, const void*, int64_t, const void*, int64_t, const float*, const float*, const float*, void*, int64_t, void*, int64_t, float*, void*,
+                          size_t, const tri_inv_rec_desc*, void*);
+using RecStepFn = int (*)(const void*, int64_t, const void*, int64_t, float*, const int32_t*, int32_t, void*, int64_t, const tri_inv_rec_desc*, void*);
+using HeadsFn = int (*)(const void*, int64_t, const void*, int64_t, const void*, const void*, const float*, const int32_t*, void*, int64_t, void*, int64_t, const tri_inv_heads_desc*, void*);
+using HeadsBytesFn = int (*)(const tri_inv_heads_desc*, size_t*);
+using HeadsBackFn = int (*)(const void*, int64_t, const void*, int64_t, const void*, int64_t, const void*, int64_t, const void*, const void*, const float*, const int32_t*, void*, int64_t,
+                            void*, int64_t, void*, void*, void*, size_t, const tri_inv_heads_desc*, void*);
+struct {
+  RecRowsFn rows; RecBytesFn bytes; RecFn rec; RecBackBytesFn back_bytes; RecBackFn back; RecStepFn step; HeadsFn heads; HeadsBytesFn heads_bytes; HeadsBackFn heads_back;
+} g_mixers = {};
+
+PyObject* bind_mixers(PyObject*, PyObject* args) {   // the addresses of the entry points above, in this order
+  unsigned long long f[9];
+  if (!PyArg_ParseTuple(args, "KKKKKKKKK", f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8)) return nullptr;
+  g_mixers = {(RecRowsFn)f[0], (RecBytesFn)f[1], (RecFn)f[2], (RecBackBytesFn)f[3], (RecBackFn)f[4], (RecStepFn)f[5], (HeadsFn)f[6], (HeadsBytesFn)f[7], (HeadsBackFn)f[8]};
+  Py_RETURN_NONE;
+}
+
+// A tensor on the current device whose last `inner` dimensions are contiguous and whose tokens, the dimensions before them, lie at one distance
+struct Strided {
+  void* p = nullptr;
+  int64_t ld = 0;
+  bool take(PyObject* o, at::ScalarType type, at::IntArrayRef shape, int inner) {
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.layout() != at::kStrided || t.scalar_type() != type || t.sizes() != shape || !on_current_device(t) || t.dim() < inner) return false;
+    int64_t width = 1, tokens = 1;
+    int i = (int)t.dim() - 1;
+    for (; i >= (int)t.dim() - inner; --i) {
+      if (t.size(i) != 1 && t.numel() && t.stride(i) != width) return false;
+      width *= t.size(i);
+    }
+    bool has = false;
+    for (; i >= 0; --i) {
+      if (t.size(i) == 1 || !t.numel()) continue;
+      if (!has) { ld = t.stride(i); has = true; }
+      else if (t.stride(i) != ld * tokens) return false;
+      tokens *= t.size(i);
+    }
+    if (!has) ld = std::max<int64_t>(width, 1);
+    p = t.data_ptr();
+    return true;
+  }
+};
+bool tensor(PyObject* o) { return THPVariable_CheckExact(o); }
+
+// X [B,T,D], mode, cu_seqlens: the descriptor and the shapes, or false
+struct Recurrence {
+  tri_inv_rec_desc d{};
+  std::vector<int32_t> cu;
+  std::vector<int64_t> shape, state;
+  at::ScalarType type;
+  Strided x, g;
+  bool take(PyObject* X, PyObject* G, PyObject* mode, PyObject* cu_seqlens) {
+    long m = 0;
+    if (!tensor(X) || !whole(mode, 0, INT_MAX, &m)) return false;
+    const at::Tensor& t = THPVariable_Unpack(X);
+    if (t.dim() != 3 || !stored(t, &d.dtype)) return false;
+    type = t.scalar_type();
+    shape = t.sizes().vec();
+    for (int64_t n : shape)
+      if (n > INT_MAX) return false;
+    d.B = (int32_t)shape[0]; d.T = (int32_t)shape[1]; d.D = (int32_t)shape[2]; d.mode = (int32_t)m;
+    int64_t n = shape[0];
+    if (cu_seqlens != Py_None) {
+      if (!offsets(cu_seqlens, &cu)) return false;
+      d.cu_seqlens = cu.data();
+      d.n_seqs = (int32_t)cu.size() - 1;
+      n = d.n_seqs;
+    }
+    state = {n, shape[2]};
+    return x.take(X, type, shape, 1) && g.take(G, type, shape, 1);
+  }
+  at::TensorOptions options(PyObject* X) const { return THPVariable_Unpack(X).options(); }
+};
+
+// (X, G, mode, h0, cu_seqlens, want_state, want_carries) -> (Y, h or None, carries or None), None, or the failing call's status (+ 256: the workspace query's)
+PyObject* gated_recurrence(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Recurrence x;
+  if (n != 7 || !g_mixers.rec || !x.take(a[0], a[1], a[2], a[4]) || !is(a[3], at::kFloat, x.state, true)) Py_RETURN_NONE;
+  size_t need = 0;
+  int64_t rows = 0;
+  int rc = g_mixers.bytes(&x.d, &need);
+  if (!rc && a[6] == Py_True) rc = g_mixers.rows(&x.d, &rows);
+  if (rc) return PyLong_FromLong(rc + 256);
+  const at::TensorOptions like = x.options(a[0]), f32 = like.dtype(at::kFloat);
+  at::Tensor Y = at::empty(x.shape, like), S, C, work;
+  if (a[5] == Py_True) S = at::empty(x.state, f32);
+  if (a[6] == Py_True) C = at::empty({rows, x.shape[2]}, f32);
+  if (need) work = at::empty({(int64_t)need}, like.dtype(at::kByte));
+  void *h0 = data(a[3]), *y = Y.data_ptr(), *s = S.defined() ? S.data_ptr() : nullptr, *c = C.defined() ? C.data_ptr() : nullptr, *w = need ? work.data_ptr() : nullptr, *stream = current_stream();
+  Py_BEGIN_ALLOW_THREADS
+  rc = g_mixers.rec(x.x.p, x.x.ld, x.g.p, x.g.ld, (float*)h0, y, x.shape[2], (float*)s, (float*)c, w, need, &x.d, stream);
+  Py_END_ALLOW_THREADS
+  return rc ? PyLong_FromLong(rc) : tuple_of({Y, S, C});
+  END_HANDLE_TH_ERRORS
+}
+
+// (dY, X, G, mode, h0, dh, carries, cu_seqlens, want_dh0) -> (dX, dG, dh0 or None), None, or a status as above
+PyObject* gated_recurrence_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Recurrence x;
+  Strided dy;
+  if (n != 9 || !g_mixers.back || !x.take(a[1], a[2], a[3], a[7]) || !dy.take(a[0], x.type, x.shape, 1) || !is(a[4], at::kFloat, x.state, true) || !is(a[5], at::kFloat, x.state, true))
+    Py_RETURN_NONE;
+  int64_t rows = 0;
+  size_t need = 0;
+  int rc = g_mixers.rows(&x.d, &rows);
+  if (!rc) rc = g_mixers.back_bytes(&x.d, a[6] != Py_None, &need);
+  if (rc) return PyLong_FromLong(rc + 256);
+  if (!is(a[6], at::kFloat, {rows, x.shape[2]}, true)) Py_RETURN_NONE;
+  const at::TensorOptions like = x.options(a[1]);
+  at::Tensor dX = at::empty(x.shape, like), dG = at::empty(x.shape, like), dh0, work;
+  if (a[8] == Py_True) dh0 = at::empty(x.state, like.dtype(at::kFloat));
+  if (need) work = at::empty({(int64_t)need}, like.dtype(at::kByte));
+  void *h0 = data(a[4]), *dh = data(a[5]), *c = data(a[6]), *gx = dX.data_ptr(), *gg = dG.data_ptr(), *gh = dh0.defined() ? dh0.data_ptr() : nullptr, *w = need ? work.data_ptr() : nullptr,
+       *stream = current_stream();
+  const int64_t D = x.shape[2];
+  Py_BEGIN_ALLOW_THREADS
+  rc = g_mixers.back(dy.p, dy.ld, x.x.p, x.x.ld, x.g.p, x.g.ld, (float*)h0, (float*)dh, (float*)c, gx, D, gg, D, (float*)gh, w, need, &x.d, stream);
+  Py_END_ALLOW_THREADS
+  return rc ? PyLong_FromLong(rc) : tuple_of({dX, dG, dh0});
+  END_HANDLE_TH_ERRORS
+}
+
+// (X, G, h, mode, slots) -> Y, None, or a status
+PyObject* gated_recurrence_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  long mode = 0;
+  if (n != 5 || !g_mixers.step || !tensor(a[0]) || !plain(a[2], 2) || !whole(a[3], 0, INT_MAX, &mode)) Py_RETURN_NONE;
+  const at::Tensor &X = THPVariable_Unpack(a[0]), &h = THPVariable_Unpack(a[2]);
+  tri_inv_rec_desc d{};
+  if (X.dim() != 2 || !stored(X, &d.dtype)) Py_RETURN_NONE;
+  const int64_t B = X.size(0), D = X.size(1), slots = h.size(0);
+  Strided x, g;
+  if (B < 1 || B > INT_MAX || D > INT_MAX || slots > INT_MAX || !x.take(a[0], X.scalar_type(), X.sizes(), 1) || !g.take(a[1], X.scalar_type(), X.sizes(), 1) ||
+      !is(a[2], at::kFloat, {slots, D}) || !is(a[4], at::kInt, {B}, true))
+    Py_RETURN_NONE;
+  d.B = (int32_t)B; d.T = 1; d.D = (int32_t)D; d.mode = (int32_t)mode;
+  at::Tensor Y = at::empty({B, D}, X.options());
+  const int rc = g_mixers.step(x.p, x.ld, g.p, g.ld, (float*)h.data_ptr(), (int32_t*)data(a[4]), (int32_t)slots, Y.data_ptr(), D, &d, current_stream());
+  return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(Y);
+  END_HANDLE_TH_ERRORS
+}
+
+// Q [...,H,d], K [...,H_k,d] or None, wq, wk, inv_freq, positions, eps, interleaved: the descriptor, or false
+struct Heads {
+  tri_inv_heads_desc d{};
+  std::vector<int64_t> q_shape, k_shape;
+  at::ScalarType type;
+  Strided q, k;
+  bool has_k;
+  bool take(PyObject* const* a) {
+    if (!tensor(a[0]) || !(a[1] == Py_None || tensor(a[1])) || !PyFloat_CheckExact(a[6]) || !PyBool_Check(a[7])) return false;
+    const at::Tensor& Q = THPVariable_Unpack(a[0]);
+    if (Q.dim() < 3 || !stored(Q, &d.dtype)) return false;
+    has_k = a[1] != Py_None;
+    type = Q.scalar_type();
+    q_shape = Q.sizes().vec();
+    const int dims = (int)q_shape.size();
+    for (int64_t n : q_shape)
+      if (n > INT_MAX) return false;
+    k_shape = q_shape;
+    if (has_k) {
+      const at::Tensor& K = THPVariable_Unpack(a[1]);
+      if (K.dim() != Q.dim() || K.size(dims - 2) > INT_MAX) return false;
+      k_shape[dims - 2] = K.size(dims - 2);
+    }
+    const int64_t width = q_shape[dims - 1];
+    int64_t r = 0;
+    if (a[4] != Py_None) {
+      if (!plain(a[4], 1)) return false;
+      r = THPVariable_Unpack(a[4]).size(0);
+      if (r > INT_MAX) return false;
+    }
+    std::vector<int64_t> tokens(q_shape.begin(), q_shape.end() - 2);
+    if (!q.take(a[0], type, q_shape, 2) || (has_k && !k.take(a[1], type, k_shape, 2)) || !is(a[2], type, {width}, true) || !is(a[3], type, {width}, true) || !is(a[4], at::kFloat, {r}, true) ||
+        !is(a[5], at::kInt, tokens, true) || (!has_k && a[3] != Py_None))
+      return false;
+    d.tokens = 1;
+    for (int64_t n : tokens) d.tokens *= n;
+    d.T = (int32_t)std::max<int64_t>(1, tokens.back());
+    d.H_q = (int32_t)q_shape[dims - 2]; d.H_k = has_k ? (int32_t)k_shape[dims - 2] : 0; d.d = (int32_t)width; d.r = (int32_t)r;
+    d.interleaved = a[7] == Py_True; d.eps = (float)PyFloat_AS_DOUBLE(a[6]);
+    return true;
+  }
+};
+
+// (Q, K, wq, wk, inv_freq, positions, eps, interleaved) -> (Yq, Yk or None), None, or a status
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Heads x;
+  if (n != 8 || !g_mixers.heads || !x.take(a)) Py_RETURN_NONE;
+  const at::TensorOptions like = THPVariable_Unpack(a[0]).options();
+  at::Tensor Yq = at::empty(x.q_shape, like), Yk;
+  if (x.has_k) Yk = at::empty(x.k_shape, like);
+  const int rc = g_mixers.heads(x.q.p, x.q.ld, x.k.p, x.k.ld, data(a[2]), data(a[3]), (float*)data(a[4]), (int32_t*)data(a[5]), Yq.data_ptr(), (int64_t)x.d.H_q * x.d.d,
+                                x.has_k ? Yk.data_ptr() : nullptr, (int64_t)x.d.H_k * x.d.d, &x.d, current_stream());
+  return rc ? PyLong_FromLong(rc) : tuple_of({Yq, Yk});
+  END_HANDLE_TH_ERRORS
+}
+
+// (Q, K, wq, wk, inv_freq, positions, eps, interleaved, dYq, dYk) -> (dQ, dK, dwq, dwk), None, or a status
+PyObject* qk_norm_rope_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Heads x;
+  Strided dq, dk;
+  if (n != 10 || !g_mixers.heads_back || !x.take(a) || !dq.take(a[8], x.type, x.q_shape, 2) || (x.has_k && !dk.take(a[9], x.type, x.k_shape, 2))) Py_RETURN_NONE;
+  size_t need = 0;
+  int rc = g_mixers.heads_bytes(&x.d, &need);
+  if (rc) return PyLong_FromLong(rc + 256);
+  const at::TensorOptions like = THPVariable_Unpack(a[0]).options();
+  at::Tensor dQ = at::empty(x.q_shape, like), dK, dwq, dwk, work = at::empty({(int64_t)need}, like.dtype(at::kByte));
+  if (x.has_k) dK = at::empty(x.k_shape, like);
+  if (a[2] != Py_None) dwq = at::empty({x.d.d}, like);
+  if (a[3] != Py_None) dwk = at::empty({x.d.d}, like);
+  rc = g_mixers.heads_back(dq.p, dq.ld, dk.p, dk.ld, x.q.p, x.q.ld, x.k.p, x.k.ld, data(a[2]), data(a[3]), (float*)data(a[4]), (int32_t*)data(a[5]), dQ.data_ptr(), (int64_t)x.d.H_q * x.d.d,
+                           x.has_k ? dK.data_ptr() : nullptr, (int64_t)x.d.H_k * x.d.d, dwq.defined() ? dwq.data_ptr() : nullptr, dwk.defined() ? dwk.data_ptr() : nullptr, work.data_ptr(), need,
+                           &x.d, current_stream());
+  return rc ? PyLong_FromLong(rc) : tuple_of({dQ, dK, dwq, dwk});
+  END_HANDLE_TH_ERRORS
+}
+
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"gdn_forward", (PyCFunction)(void (*)(void))gdn_forward, METH_FASTCALL, nullptr},
                          {"bind_operators", bind_operators, METH_VARARGS, nullptr},
                          FAST(linear_attention), FAST(linear_attention_backward), FAST(linear_attention_step), FAST(rms_norm), FAST(rms_norm_backward),
+                         {"bind_mixers", bind_mixers, METH_VARARGS, nullptr}, FAST(gated_recurrence), FAST(gated_recurrence_backward), FAST(gated_recurrence_step), FAST(qk_norm_rope),
+                         FAST(qk_norm_rope_backward),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods};
 

@@ -21,6 +21,7 @@ struct HeadsArgs {
   float* partial;                        // gradient: [kHeadsPartials][d]
   long long tokens;
   int T, d, r, interleaved;
+  int units;                             // pairs of vectors of a head (set by the launcher)
   float eps;
 };
 cudaError_t launch_qk_norm_rope(const HeadsArgs& a, int dtype, cudaStream_t stream);

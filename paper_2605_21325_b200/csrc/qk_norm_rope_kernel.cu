@@ -119,7 +119,7 @@ __device__ __forceinline__ void request(typename Vec<T, V>::Raw* to, const T* fr
 }
 
 // Steps of a warp in shared memory: of `bytes` a lane, tensor and half
-__host__ __device__ constexpr int steps(int bytes, bool back) { return bytes >= 16 ? (back ? 3 : 4) : back ? 4 : 6; }
+__host__ __device__ constexpr int steps(int bytes, bool back) { return bytes >= 16 || back ? 4 : 6; }
 
 // f / 2 pi modulo 1 in units of 2^-64
 __device__ __forceinline__ unsigned long long fraction(float f) {
@@ -129,12 +129,36 @@ __device__ __forceinline__ unsigned long long fraction(float f) {
   return ((unsigned long long)hi << 32) + (unsigned long long)lo;   // (x = 1 wraps to 0)
 }
 
-// The first features of the two vectors of unit p, >= d where the head has none.  Where the pairs are (i, i + r) the units of the first r / V are pairs, and the others two neighbours of the rest.
-template <int V>
-__device__ __forceinline__ void columns(int p, int r, bool interleaved, int& c0, int& c1) {
-  const bool pairs = !interleaved && p * V < r;
-  c0 = pairs ? p * V : 2 * p * V;   // (behind the pairs: 2 r + 2 (p V - r))
-  c1 = c0 + (pairs ? r : V);
+// The first features of the two vectors of unit p of `units`, >= d where the head has none.  Where the pairs are (i, i + r) the first r / V units are pairs of vectors, and the others two of the rest; interleaved a
+// vector holds its pairs and any two will do.  Vectors of neighbouring lanes lie side by side: with two neighbouring vectors to a lane each access would use half of what it fetches (32768 tokens of 40 heads, interleaved, 174 -> 125 us).
+template <int V, bool INTER>
+__device__ __forceinline__ void columns(int p, int r, int d, int units, int& c0, int& c1) {
+  if (p >= units) {
+    c0 = c1 = d;
+  } else if (INTER && V == 1) {   // a pair
+    c0 = 2 * p;
+    c1 = c0 + 1;
+  } else if (INTER) {
+    c0 = p * V;
+    c1 = c0 + units * V;
+  } else {
+    const bool pairs = p * V < r;
+    c0 = pairs ? p * V : p * V + r;
+    c1 = c0 + (pairs ? r : units * V - r);
+  }
+}
+// Where pair f's angle belongs: which unit, which of its V pairs
+template <int V, bool INTER>
+__device__ __forceinline__ void unit_of(int f, int units, int& p, int& i) {
+  if (INTER && V > 1) {
+    constexpr int HALF = V / 2 > 0 ? V / 2 : 1;
+    const int q = f / HALF;
+    p = q < units ? q : q - units;
+    i = f % HALF + (q < units ? 0 : HALF);
+  } else {
+    p = f / V;
+    i = f % V;
+  }
 }
 
 // Turns two pairs by cs = (cos, cos', sin, sin')
@@ -147,6 +171,7 @@ __device__ __forceinline__ void turn(Pair& u, Pair& w, float4 cs) {
 struct HeadsPlan {
   int blocks[2];       // of queries and of keys
   int parts[2];        // warps that share a token's heads
+  int group[2];        // tokens that share a warp, where they have few heads (parts is 1 then)
 };
 // Where a warp stands: HEADS heads of a token at a time, `left` of them in all to go
 struct At {
@@ -156,14 +181,14 @@ struct At {
 };
 
 // NU: units of a lane.  A warp's next STEPS - 1 steps are on their way to shared memory while it works on one.
-template <class T, int V, int LANES, int NU, bool BACK, bool INTER>
-__global__ void __launch_bounds__(kThreads, BACK ? 3 : 4) qk_norm_rope_kernel(const __grid_constant__ HeadsArgs a, const __grid_constant__ HeadsPlan plan) {
+template <class T, int V, int LANES, int NU, bool BACK, bool INTER, bool GROUP>
+__global__ void __launch_bounds__(kThreads, BACK ? 2 : 3) qk_norm_rope_kernel(const __grid_constant__ HeadsArgs a, const __grid_constant__ HeadsPlan plan) {
   using Raw = typename Vec<T, V>::Raw;
   constexpr int HEADS = 32 / LANES, N = kTwos<V>, UNITS = LANES * NU, es = sizeof(T);
   constexpr int STEPS = steps(V * es * NU, BACK), TENSORS = BACK ? 2 : 1;
   extern __shared__ __align__(16) unsigned char dynamic[];
   __shared__ unsigned long long freq[kTable];
-  __shared__ int places[kWarps][STEPS];
+  __shared__ int places[kWarps][STEPS][HEADS];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, sub = lane / LANES, t = lane % LANES;
   float4* table = reinterpret_cast<float4*>(dynamic) + warp * kTable;   // of angles 2 j, 2 j + 1 of unit p at [j][p], so that the lanes of a head read side by side
   Raw* ring = reinterpret_cast<Raw*>(dynamic + kWarps * kTable * sizeof(float4)) + warp * STEPS * TENSORS * NU * 2 * 32 + lane;
@@ -173,10 +198,18 @@ __global__ void __launch_bounds__(kThreads, BACK ? 3 : 4) qk_norm_rope_kernel(co
   wait_for_predecessor();
 
   const int parts = plan.parts[which], per = ((s.H + HEADS - 1) / HEADS + parts - 1) / parts * HEADS;   // heads of a part
-  const long long items = a.tokens * parts, stride = (long long)plan.blocks[which] * kWarps;
+  const int group = GROUP ? plan.group[which] : 1, mine = group > 1 ? sub / s.H : 0;   // mine: the lane's token among those of the warp
+  const long long items = group > 1 ? (a.tokens + group - 1) / group : a.tokens * parts, stride = (long long)plan.blocks[which] * kWarps;
   auto token_of = [&](long long item) { return parts == 1 ? item : item / parts; };
   auto first_of = [&](long long item) { return parts == 1 ? 0 : (int)(item - item / parts * parts) * per; };
   auto place = [&](At& p) {   // an item's first step; items without heads (a token's last part may have none) are passed over
+    if (group > 1) {   // one step, whose `left` says whether the lane has a head in it
+      const long long token = p.item * group + mine;
+      p.left = mine < group && token < a.tokens ? HEADS : sub;
+      p.x = (const char*)(X + token * s.ld_x + (long long)(sub - mine * s.H) * a.d);
+      if (BACK) p.dy = (const char*)(DY + token * s.ld_dy + (long long)(sub - mine * s.H) * a.d);
+      return;
+    }
     for (;; p.item += stride) {
       if (p.item >= items) return;
       const int h = first_of(p.item);
@@ -191,14 +224,14 @@ __global__ void __launch_bounds__(kThreads, BACK ? 3 : 4) qk_norm_rope_kernel(co
   const int step_bytes = HEADS * a.d * es;
   int c0[NU], c1[NU];
 #pragma unroll
-  for (int k = 0; k < NU; ++k) columns<V>(k * LANES + t, a.r, INTER, c0[k], c1[k]);
+  for (int k = 0; k < NU; ++k) columns<V, INTER>(k * LANES + t, a.r, a.d, a.units, c0[k], c1[k]);
   // Asks for the step at p, and goes on to the next
   auto ask = [&](At& p, int slot, bool fresh) {
     if (p.item < items) {
-      if (fresh && lane == 0) {
-        const long long token = token_of(p.item);
-        if (a.positions) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(&places[warp][slot])), "l"(a.positions + token) : "memory");
-        else places[warp][slot] = (int)(token % a.T);
+      const long long token = group > 1 ? p.item * group + lane : token_of(p.item);
+      if (fresh && lane < group && token < a.tokens) {
+        if (a.positions) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(&places[warp][slot][lane])), "l"(a.positions + token) : "memory");
+        else places[warp][slot][lane] = (int)(token % a.T);
       }
 #pragma unroll
       for (int k = 0; k < NU; ++k) {
@@ -234,10 +267,12 @@ __global__ void __launch_bounds__(kThreads, BACK ? 3 : 4) qk_norm_rope_kernel(co
   }
 
   for (int i = tid; i < a.r; i += kThreads) freq[i] = fraction(a.inv_freq[i]);
-  auto angle = [&](int f) { return reinterpret_cast<float*>(table) + (V == 1 ? 4 * f : f % V / 2 * UNITS * 4 + f / V * 4 + f % 2); };   // its cosine; its sine is two further on
-  for (int f = a.r + lane; f < UNITS * V; f += 32) { angle(f)[0] = 1.f; angle(f)[2] = 0.f; }   // what is not turned
-  if (V == 1)
-    for (int f = lane; f < UNITS; f += 32) { angle(f)[1] = 1.f; angle(f)[3] = 0.f; }
+  auto angle = [&](int f) {   // its cosine; its sine is two further on
+    int p, i;
+    unit_of<V, INTER>(f, a.units, p, i);
+    return reinterpret_cast<float*>(table) + (i / 2 * UNITS + p) * 4 + i % 2;
+  };
+  for (int i = lane; i < group * N * UNITS; i += 32) table[i] = make_float4(1.f, 1.f, 0.f, 0.f);   // what is not turned stays so
   Pair wu[NU][N], ww[NU][N], gu[BACK ? NU : 1][N], gw[BACK ? NU : 1][N];
 #pragma unroll
   for (int k = 0; k < NU; ++k) {
@@ -256,6 +291,7 @@ __global__ void __launch_bounds__(kThreads, BACK ? 3 : 4) qk_norm_rope_kernel(co
   __syncthreads();
 
   const float over_d = 1.f / (float)a.d;
+  const float4* turns_of = table + (mine < group ? mine : 0) * N * UNITS + t;   // of the lane's token
   T* to = nullptr;
   bool real = false, fresh = true;   // fresh: the step is its item's first
   for (int slot = 0; now.item < items; slot = slot + 1 == STEPS ? 0 : slot + 1) {
@@ -266,17 +302,19 @@ __global__ void __launch_bounds__(kThreads, BACK ? 3 : 4) qk_norm_rope_kernel(co
     }
     asm volatile("cp.async.wait_group %0;" ::"n"(STEPS - 1) : "memory");
     if (fresh) {
-      const long long token = token_of(now.item);
-      to = (BACK ? (T*)s.dx + token * s.ld_dx : (T*)s.y + token * s.ld_y) + (long long)(first_of(now.item) + sub) * a.d;
+      const long long token = group > 1 ? now.item * group + mine : token_of(now.item);
+      to = (BACK ? (T*)s.dx + token * s.ld_dx : (T*)s.y + token * s.ld_y) + (long long)(group > 1 ? sub - mine * s.H : first_of(now.item) + sub) * a.d;
       __syncwarp();
-      const int position = places[warp][slot];
-      real = position >= 0;
-      for (int f = lane; f < a.r; f += 32) {
-        const int turns = (int)(((unsigned long long)(unsigned)position * freq[f]) >> 32);   // of 2^-32 of a whole one, signed
-        float sn, cs;
-        sincospif((float)turns * 4.656612873077393e-10f, &sn, &cs);   // 2^-31
-        angle(f)[0] = cs;
-        angle(f)[2] = BACK ? -sn : sn;
+      real = mine < group && places[warp][slot][mine] >= 0;
+      for (int q = 0; q < group; ++q) {
+        const unsigned position = (unsigned)places[warp][slot][q];
+        for (int f = lane; f < a.r; f += 32) {
+          const int turns = (int)(((unsigned long long)position * freq[f]) >> 32);   // of 2^-32 of a whole one, signed
+          float sn, cs;
+          sincospif((float)turns * 4.656612873077393e-10f, &sn, &cs);   // 2^-31
+          angle(f)[4 * q * N * UNITS] = cs;
+          angle(f)[4 * q * N * UNITS + 2] = BACK ? -sn : sn;
+        }
       }
       __syncwarp();
     }
@@ -290,7 +328,7 @@ __global__ void __launch_bounds__(kThreads, BACK ? 3 : 4) qk_norm_rope_kernel(co
       for (int j = 0; j < N; ++j) {
         sum = fma2(xu[k][j], xu[k][j], fma2(xw[k][j], xw[k][j], sum));
         if constexpr (BACK) {
-          turn(yu[k][j], yw[k][j], table[j * UNITS + k * LANES + t]);
+          turn(yu[k][j], yw[k][j], turns_of[j * UNITS + k * LANES]);
           mixed = fma2(mul2(yu[k][j], wu[k][j]), xu[k][j], fma2(mul2(yw[k][j], ww[k][j]), xw[k][j], mixed));
         }
       }
@@ -318,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, BACK ? 3 : 4) qk_norm_rope_kernel(co
         } else {
           yu[k][j] = mul2(xu[k][j], mul2(rstd2, wu[k][j]));
           yw[k][j] = mul2(xw[k][j], mul2(rstd2, ww[k][j]));
-          turn(yu[k][j], yw[k][j], table[j * UNITS + k * LANES + t]);
+          turn(yu[k][j], yw[k][j], turns_of[j * UNITS + k * LANES]);
         }
       }
       float v0[V], v1[V];
@@ -397,32 +435,41 @@ __global__ void __launch_bounds__(1024) heads_weight_kernel(const __grid_constan
   }
 }
 
-// Blocks by the sides' shares of the heads.  Where there are fewer tokens than warps on the chip, several warps share a token's heads.
+// Blocks by the sides' shares of the work, a token's angles counted as three steps.  Where there are fewer tokens than warps on the chip, several warps share a token's heads; where a token has at most half as many
+// heads as a warp holds, a warp takes several tokens.
 HeadsPlan plan_of(const HeadsArgs& a, int heads, int sms, int most) {
   HeadsPlan p{};
-  const long long total = a.side[0].H + a.side[1].H;
-  long long want[2];
+  long long want[2], work[2];
   for (int i = 0; i < 2; ++i) {
-    const int groups = (a.side[i].H + heads - 1) / heads;
-    if (!groups) { p.parts[i] = 1; want[i] = 0; continue; }
-    const long long warps = std::max<long long>(1, (long long)sms * kWarps * 2 * a.side[i].H / total);
-    p.parts[i] = (int)std::min<long long>(groups, std::max<long long>(1, warps / std::max<long long>(1, a.tokens)));
-    want[i] = (a.tokens * p.parts[i] + kWarps - 1) / kWarps;
+    const int H = a.side[i].H, steps = (H + heads - 1) / heads;
+    p.parts[i] = p.group[i] = 1;
+    want[i] = work[i] = 0;
+    if (!H) continue;
+    if (H <= heads / 2) {
+      p.group[i] = heads / H;
+      work[i] = (1 + 3 * p.group[i]) * 12 / p.group[i];
+      want[i] = ((a.tokens + p.group[i] - 1) / p.group[i] + kWarps - 1) / kWarps;
+    } else {
+      const long long warps = (long long)sms * kWarps;
+      p.parts[i] = (int)std::min<long long>(steps, std::max<long long>(1, warps / std::max<long long>(1, a.tokens)));
+      work[i] = (steps + 3) * 12;
+      want[i] = (a.tokens * p.parts[i] + kWarps - 1) / kWarps;
+    }
   }
-  for (int i = 0; i < 2; ++i) p.blocks[i] = (int)(want[i] ? std::max<long long>(1, std::min<long long>(want[i], (long long)most * a.side[i].H / total)) : 0);
+  for (int i = 0; i < 2; ++i) p.blocks[i] = (int)(want[i] ? std::max<long long>(1, std::min<long long>(want[i], most * work[i] / (work[0] + work[1]))) : 0);
   return p;
 }
 
-template <class T, int V, int LANES, int NU, bool BACK, bool INTER>
-cudaError_t launch_one(const HeadsArgs& a, cudaStream_t stream) {
+template <class T, int V, int LANES, int NU, bool BACK, bool INTER, bool GROUP>
+cudaError_t launch_kernel(const HeadsArgs& a, cudaStream_t stream) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess || (e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
   constexpr size_t smem = (size_t)kWarps * (kTable * sizeof(float4) + (size_t)steps(V * (int)sizeof(T) * NU, BACK) * (BACK ? 2 : 1) * NU * 2 * 32 * V * sizeof(T));
-  if ((e = allow_shared<qk_norm_rope_kernel<T, V, LANES, NU, BACK, INTER>>(smem)) != cudaSuccess) return e;
-  const HeadsPlan p = plan_of(a, 32 / LANES, sms, BACK ? std::min(kHeadsPartials - 1, 3 * sms) : 4 * sms);
+  if ((e = allow_shared<qk_norm_rope_kernel<T, V, LANES, NU, BACK, INTER, GROUP>>(smem)) != cudaSuccess) return e;
+  const HeadsPlan p = plan_of(a, 32 / LANES, sms, BACK ? std::min(kHeadsPartials - 1, 2 * sms) : 3 * sms);
   if (p.blocks[0] + p.blocks[1] > 0) {
-    if ((e = launch_early(qk_norm_rope_kernel<T, V, LANES, NU, BACK, INTER>, dim3(p.blocks[0] + p.blocks[1]), kThreads, smem, stream, a, p)) != cudaSuccess) return e;
+    if ((e = launch_early(qk_norm_rope_kernel<T, V, LANES, NU, BACK, INTER, GROUP>, dim3(p.blocks[0] + p.blocks[1]), kThreads, smem, stream, a, p)) != cudaSuccess) return e;
     if ((e = launched()) != cudaSuccess) return e;
   }
   if constexpr (BACK) {
@@ -433,9 +480,18 @@ cudaError_t launch_one(const HeadsArgs& a, cudaStream_t stream) {
   return cudaSuccess;
 }
 
+template <class T, int V, int LANES, int NU, bool BACK, bool INTER>
+cudaError_t launch_one(const HeadsArgs& a, cudaStream_t stream) {
+  if constexpr (LANES < 32)
+    for (const HeadsSide& s : a.side)
+      if (s.H && s.H <= 32 / LANES / 2) return launch_kernel<T, V, LANES, NU, BACK, INTER, true>(a, stream);
+  return launch_kernel<T, V, LANES, NU, BACK, INTER, false>(a, stream);
+}
+
 template <class T, int V, bool BACK, bool INTER>
-cudaError_t launch_width(const HeadsArgs& a, cudaStream_t stream) {
+cudaError_t launch_width(HeadsArgs a, cudaStream_t stream) {
   const int first = INTER ? 0 : a.r / V, rest = a.d / V - 2 * first, units = first + (rest + 1) / 2;
+  a.units = units;
   if constexpr (V == 1) {
     if (units <= 32) return launch_one<T, 1, 32, 1, BACK, INTER>(a, stream);
     return units <= 64 ? launch_one<T, 1, 32, 2, BACK, INTER>(a, stream) : launch_one<T, 1, 32, 4, BACK, INTER>(a, stream);
