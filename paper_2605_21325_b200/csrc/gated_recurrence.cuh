@@ -70,9 +70,16 @@ struct RecArgs {
 
 cudaError_t launch_gated_recurrence(const RecArgs& a, int dtype, cudaStream_t stream);
 cudaError_t launch_gated_recurrence_backward(const RecArgs& a, int dtype, cudaStream_t stream);
-// What the walks find in their workspace: the ticket (zero), the words (all ones; null: none, the table then holds whole sequences) and the table of packed sequences
-// from the host offsets `cu` (null: dense, no table).
-cudaError_t launch_rec_setup(unsigned int* ticket, unsigned long long* words, long long n_words, RecTile* table, int tile, const int32_t* cu, int n_seqs, cudaStream_t stream);
+// What a walk finds in its workspace: the ticket (zero) and the words (all ones), null where whole sequences are walked, and the table of packed sequences, null for dense ones.
+struct RecSetup {
+  unsigned int* ticket;
+  unsigned long long* words;
+  RecTile* table;
+  long long n_words;
+  int tile;                        // tokens of an entry; 0: whole sequences
+};
+// Sets up one walk or two from the host offsets `cu` (null: dense).
+cudaError_t launch_rec_setup(const RecSetup* walks, int n_walks, const int32_t* cu, int n_seqs, cudaStream_t stream);
 
 struct RecStepArgs {
   const void *x, *g;

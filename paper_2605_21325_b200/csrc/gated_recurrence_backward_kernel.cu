@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
     if (!t.whole) {
 #pragma unroll
       for (int k = 0; k < kTok; ++k)
-        if (k >= left) { av[k] = twice(1.f); mv[k] = twice(0.f); }
+        if (k >= left) av[k] = mv[k] = twice(1.f);   // (x and dy read as zero there)
     }
     Pair P = twice(1.f), H = twice(0.f), C = twice(0.f), half_P, half_H;   // half: of the first half of the tokens
 #pragma unroll

@@ -173,43 +173,43 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
 constexpr int kSeqsPerSetup = 320;
 struct SeqRange { int32_t tok0, n, seq; };
 struct SetupArgs {
-  unsigned int* ticket;
-  unsigned long long* words;
-  RecTile* table;          // where these sequences' entries begin
-  long long n_words;       // to clear; 0: neither words nor ticket
-  int n_seqs, tile;        // tile: tokens of one; 0: an entry is a whole sequence
+  RecSetup walk[2];        // table: where these sequences' entries begin; n_words: to clear, 0 for neither words nor ticket
+  int n_walks, n_seqs;
 };
 template <int SEQS>
 struct SeqBatch { SeqRange seq[SEQS]; };   // the longest first
 __host__ __device__ __forceinline__ int tiles_of(int n, int tile) { return n > 0 && tile ? (int)(((unsigned)n + tile - 1) / tile) : 1; }
-// The ticket, the words, and up to 320 sequences' entries of the table, a warp per sequence.  Tiles lie in turn, every sequence's first, then every second, so that the tile in front of a tile is
+// The tickets, the words, and up to 320 sequences' entries of the tables, a warp per sequence.  Tiles lie in turn, every sequence's first, then every second, so that the tile in front of a tile is
 // as far ahead of it as there are sequences left.
 template <int SEQS>
 __global__ void __launch_bounds__(256) rec_setup_kernel(const __grid_constant__ SetupArgs b, const __grid_constant__ SeqBatch<SEQS> batch) {
-  __shared__ int tiles[SEQS];
+  __shared__ SeqRange seq[SEQS];
   let_successor_start();
   if constexpr (SEQS > 1)
-    for (int q = threadIdx.x; q < b.n_seqs; q += 256) tiles[q] = tiles_of(batch.seq[q].n, b.tile);
+    for (int q = threadIdx.x; q < b.n_seqs; q += 256) seq[q] = batch.seq[q];
   __syncthreads();
   wait_for_predecessor();
-  if (b.n_words) {
-    const bool one = blockIdx.x == 0 && threadIdx.x == 0;
-    if (one) *b.ticket = 0;
-    const long long pairs = b.n_words / 2, stride = (long long)gridDim.x * 256;
-    const uint4 none = make_uint4(~0u, ~0u, ~0u, ~0u);
-    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < pairs; i += stride) reinterpret_cast<uint4*>(b.words)[i] = none;
-    if (one && (b.n_words & 1)) b.words[b.n_words - 1] = ~0ull;
-  }
-  if constexpr (SEQS > 1) {
-    const int lane = threadIdx.x & 31;
-    for (int s = blockIdx.x * 8 + (threadIdx.x >> 5); s < b.n_seqs; s += gridDim.x * 8) {
-      const SeqRange r = batch.seq[s];
-      RecTile e{r.tok0, r.n, r.seq, 0, tiles[s]};
-      for (int k = lane; k < e.tiles; k += 32) {
-        long long at = s;   // among the k-th tiles: the sequences before this one are as long at least
-        for (int q = 0; q < b.n_seqs; ++q) at += min(tiles[q], k);
-        e.index = k;
-        b.table[at] = e;
+  for (int i = 0; i < b.n_walks; ++i) {
+    const RecSetup& w = b.walk[i];
+    if (w.n_words) {
+      const bool one = blockIdx.x == 0 && threadIdx.x == 0;
+      if (one) *w.ticket = 0;
+      const long long pairs = w.n_words / 2, stride = (long long)gridDim.x * 256;
+      const uint4 none = make_uint4(~0u, ~0u, ~0u, ~0u);
+      for (long long j = blockIdx.x * 256ll + threadIdx.x; j < pairs; j += stride) reinterpret_cast<uint4*>(w.words)[j] = none;
+      if (one && (w.n_words & 1)) w.words[w.n_words - 1] = ~0ull;
+    }
+    if constexpr (SEQS > 1) {
+      const int lane = threadIdx.x & 31;
+      for (int s = blockIdx.x * 8 + (threadIdx.x >> 5); s < b.n_seqs; s += gridDim.x * 8) {
+        RecTile e{seq[s].tok0, seq[s].n, seq[s].seq, 0, tiles_of(seq[s].n, w.tile)};
+        for (int k = lane; k < e.tiles; k += 32) {
+          long long at = s;   // among the k-th tiles: the sequences before this one are as long at least
+          if (k > 0)
+            for (int q = 0; q < b.n_seqs; ++q) at += min(tiles_of(seq[q].n, w.tile), k);
+          e.index = k;
+          w.table[at] = e;
+        }
       }
     }
   }
@@ -249,23 +249,28 @@ cudaError_t launch_gated_recurrence(const RecArgs& a, int dtype, cudaStream_t st
   return dtype == TRI_INV_F32 ? launch_type<float>(a, stream) : launch_type<__nv_bfloat16>(a, stream);
 }
 
-cudaError_t launch_rec_setup(unsigned int* ticket, unsigned long long* words, long long n_words, RecTile* table, int tile, const int32_t* cu, int n_seqs, cudaStream_t stream) {
-  SetupArgs b{ticket, words, table, words ? n_words : 0, 0, words ? tile : 0};
-  auto grid = [&]() { return dim3((unsigned)std::max<long long>(1, std::min<long long>(std::max<long long>((b.n_seqs + 7) / 8, (b.n_words / 2 + 1023) / 1024), 592))); };
-  if (!cu) return b.n_words ? launch_early(rec_setup_kernel<1>, grid(), 256, 0, stream, b, SeqBatch<1>{}) : cudaSuccess;
+cudaError_t launch_rec_setup(const RecSetup* walks, int n_walks, const int32_t* cu, int n_seqs, cudaStream_t stream) {
+  SetupArgs b{};
+  b.n_walks = n_walks;
+  long long words = 0;
+  for (int i = 0; i < n_walks; ++i) {
+    b.walk[i] = walks[i];
+    words += walks[i].n_words;
+  }
+  auto grid = [&]() { return dim3((unsigned)std::max<long long>(1, std::min<long long>(std::max<long long>((b.n_seqs + 7) / 8, (words / 2 + 1023) / 1024), 592))); };
+  if (!cu) return words ? launch_early(rec_setup_kernel<1>, grid(), 256, 0, stream, b, SeqBatch<1>{}) : cudaSuccess;
   SeqBatch<kSeqsPerSetup> batch;
   for (int s0 = 0; s0 < n_seqs; s0 += kSeqsPerSetup) {
-    long long entries = 0;
     b.n_seqs = std::min(kSeqsPerSetup, n_seqs - s0);
-    for (int q = 0; q < b.n_seqs; ++q) {
-      batch.seq[q] = SeqRange{cu[s0 + q], cu[s0 + q + 1] - cu[s0 + q], s0 + q};
-      entries += tiles_of(batch.seq[q].n, b.tile);
-    }
+    for (int q = 0; q < b.n_seqs; ++q) batch.seq[q] = SeqRange{cu[s0 + q], cu[s0 + q + 1] - cu[s0 + q], s0 + q};
     std::sort(batch.seq, batch.seq + b.n_seqs, [](const SeqRange& x, const SeqRange& y) { return x.n != y.n ? x.n > y.n : x.seq < y.seq; });
     const cudaError_t e = launch_early(rec_setup_kernel<kSeqsPerSetup>, grid(), 256, 0, stream, b, batch);
     if (e != cudaSuccess) return e;
-    b.table += entries;
-    b.n_words = 0;
+    words = 0;
+    for (int i = 0; i < n_walks; ++i) {
+      for (int q = 0; q < b.n_seqs; ++q) b.walk[i].table += tiles_of(batch.seq[q].n, b.walk[i].tile);
+      b.walk[i].n_words = 0;
+    }
   }
   return cudaSuccess;
 }

@@ -85,7 +85,7 @@ int plan(const tri_inv_rec_desc* d, int tile, int most_walked, RecPlan* p) {
 struct BackPlan {
   RecPlan back, front;
   size_t carry_bytes;
-  size_t bytes() const { return carry_bytes + std::max(back.bytes(), carry_bytes ? front.bytes() : 0); }
+  size_t bytes() const { return carry_bytes + (carry_bytes ? front.bytes() : 0) + back.bytes(); }
 };
 int plan_back(const tri_inv_rec_desc* d, bool with_carries, BackPlan* p) {
   p->carry_bytes = with_carries ? 0 : round_up((size_t)slots_of(d, kRecCarry) * d->D * 4);
@@ -93,22 +93,25 @@ int plan_back(const tri_inv_rec_desc* d, bool with_carries, BackPlan* p) {
   return e ? e : plan(d, kRecTile, kMostWalked, &p->front);
 }
 
-// The arguments that do not differ between the walks; the set-up of the workspace is enqueued
-int begin_walk(RecArgs& a, const RecPlan& p, const tri_inv_rec_desc* d, void* workspace, cudaStream_t stream) {
+// A walk's share of the arguments, and what is to be set up in its part of the workspace
+RecSetup place_walk(RecArgs& a, const RecPlan& p, const tri_inv_rec_desc* d, void* workspace) {
+  a.n_seqs = seqs_of(d); a.T = d->T; a.D = d->D; a.cols = p.cols; a.n_segs = p.n_segs; a.mode = d->mode;
+  a.items = p.n_segs * p.cols;
+  a.by_cols = rec_divide_by(p.cols);
+  a.by_seqs = rec_divide_by(std::max(1, a.n_seqs));
+  if (d->T == 0) a.x = a.g = a.dy = a.status;   // no row is read, but the copies' addresses are formed
+  a.table = d->cu_seqlens ? (RecTile*)workspace : nullptr;
+  a.ticket = p.words ? (unsigned int*)((char*)workspace + p.table_bytes) : nullptr;
+  a.words = p.words ? (unsigned long long*)((char*)workspace + p.table_bytes + 256) : nullptr;
+  return RecSetup{a.ticket, a.words, (RecTile*)a.table, p.words ? slots_of(d, p.tile) * d->D : 0, p.words ? p.tile : 0};
+}
+int walk_forward(RecArgs& a, const RecPlan& p, const tri_inv_rec_desc* d, void* workspace, cudaStream_t stream) {
   cudaError_t err;
   a.status = status_word_for_current_device(&err);
   if (!a.status) return TRI_INV_ERR_CUDA;
-  a.n_seqs = seqs_of(d); a.T = d->T; a.D = d->D; a.cols = p.cols; a.n_segs = p.n_segs; a.mode = d->mode;
   if (p.n_segs == 0) return TRI_INV_OK;
-  a.items = p.n_segs * p.cols;
-  a.by_cols = rec_divide_by(p.cols);
-  a.by_seqs = rec_divide_by(a.n_seqs);
-  if (d->T == 0) a.x = a.g = a.dy = a.status;   // no row is read, but the copies' addresses are formed
-  RecTile* table = (RecTile*)workspace;
-  a.table = d->cu_seqlens ? table : nullptr;
-  a.ticket = p.words ? (unsigned int*)((char*)workspace + p.table_bytes) : nullptr;
-  a.words = p.words ? (unsigned long long*)((char*)workspace + p.table_bytes + 256) : nullptr;
-  return launch_rec_setup(a.ticket, a.words, slots_of(d, p.tile) * d->D, table, p.tile, d->cu_seqlens, a.n_seqs, stream) == cudaSuccess ? TRI_INV_OK : TRI_INV_ERR_CUDA;
+  const RecSetup setup = place_walk(a, p, d, workspace);
+  return launch_rec_setup(&setup, 1, d->cu_seqlens, a.n_seqs, stream) == cudaSuccess && launch_gated_recurrence(a, d->dtype, stream) == cudaSuccess ? TRI_INV_OK : TRI_INV_ERR_CUDA;
 }
 
 int check_heads(const tri_inv_heads_desc* d) {
@@ -170,9 +173,7 @@ int tri_inv_gated_recurrence(const void* X, int64_t ldx, const void* G, int64_t 
   RecArgs a{};
   a.x = X; a.ld_x = ldx; a.g = G; a.ld_g = ldg; a.y = Y; a.ld_y = ldy;
   a.h0 = h0; a.h_out = h_out; a.carries = carries;
-  const int b = begin_walk(a, p, desc, workspace, (cudaStream_t)cuda_stream);
-  if (b || p.n_segs == 0) return b;
-  return launch_gated_recurrence(a, desc->dtype, (cudaStream_t)cuda_stream) == cudaSuccess ? TRI_INV_OK : TRI_INV_ERR_CUDA;
+  return walk_forward(a, p, desc, workspace, (cudaStream_t)cuda_stream);
 }
 
 int tri_inv_selftest_recurrence_wait_timeout(const void* X, const void* G, void* Y, void* workspace, size_t workspace_bytes, const tri_inv_rec_desc* desc,
@@ -189,9 +190,8 @@ int tri_inv_selftest_recurrence_wait_timeout(const void* X, const void* G, void*
   a.ld_x = a.ld_g = a.ld_y = desc->D;
   a.wait_limit_ns = wait_limit_ns;
   a.test_stall = 1;
-  const int b = begin_walk(a, p, desc, workspace, (cudaStream_t)cuda_stream);
+  const int b = walk_forward(a, p, desc, workspace, (cudaStream_t)cuda_stream);
   if (b) return b;
-  if (launch_gated_recurrence(a, desc->dtype, (cudaStream_t)cuda_stream) != cudaSuccess) return TRI_INV_ERR_CUDA;
   return cudaStreamSynchronize((cudaStream_t)cuda_stream) == cudaSuccess ? TRI_INV_OK : TRI_INV_ERR_CUDA;
 }
 
@@ -232,16 +232,19 @@ int tri_inv_gated_recurrence_backward(const void* dY, int64_t lddy, const void* 
   RecArgs a{};
   a.x = X; a.ld_x = ldx; a.g = G; a.ld_g = ldg; a.h0 = h0;
   a.carries = carries ? (float*)carries : (float*)workspace;
+  cudaError_t err;
+  a.status = status_word_for_current_device(&err);
+  if (!a.status) return TRI_INV_ERR_CUDA;
+  if (p.back.n_segs == 0) return TRI_INV_OK;
+  RecArgs front = a;
+  RecSetup setup[2];
   void* control = (char*)workspace + p.carry_bytes;
-  const cudaStream_t stream = (cudaStream_t)cuda_stream;
-  if (!carries) {
-    const int b = begin_walk(a, p.front, desc, control, stream);
-    if (b || p.front.n_segs == 0) return b;
-    if (launch_gated_recurrence(a, desc->dtype, stream) != cudaSuccess) return TRI_INV_ERR_CUDA;
-  }
+  if (!carries) setup[1] = place_walk(front, p.front, desc, (char*)control + p.back.bytes());
   a.dy = dY; a.ld_dy = lddy; a.dx = dX; a.ld_dx = lddx; a.dg = dG; a.ld_dg = lddg; a.dh = dh; a.dh0 = dh0;
-  const int b = begin_walk(a, p.back, desc, control, stream);
-  if (b || p.back.n_segs == 0) return b;
+  setup[0] = place_walk(a, p.back, desc, control);
+  const cudaStream_t stream = (cudaStream_t)cuda_stream;
+  if (launch_rec_setup(setup, carries ? 1 : 2, desc->cu_seqlens, a.n_seqs, stream) != cudaSuccess) return TRI_INV_ERR_CUDA;
+  if (!carries && launch_gated_recurrence(front, desc->dtype, stream) != cudaSuccess) return TRI_INV_ERR_CUDA;
   return launch_gated_recurrence_backward(a, desc->dtype, stream) == cudaSuccess ? TRI_INV_OK : TRI_INV_ERR_CUDA;
 }
 
