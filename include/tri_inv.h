@@ -398,29 +398,29 @@ int tri_inv_rms_norm_backward(const void* dY, const void* X, const void* w, cons
  *     TRI_INV_REC_DECAY    a = exp(g),             u = x
  *     TRI_INV_REC_NORMED   a = exp(g),             u = sqrt(1 - a^2) x        (0 where g >= 0)
  *     TRI_INV_REC_GATE     a = 1 / (1 + exp(-g)),  u = (1 - a) x
- * g is at most 0 in any model of the first two (-inf: the state forgets at once), but positive values are computed as given, as long as the decays' product over 64 tokens is finite.  Where a is zero
- * the state is u, whatever came before it, also where that is not finite; a state that is not finite may also be forgotten where the decays' product since is below 2^-149.
+ * g is at most 0 in any model of the first two (-inf: the state forgets at once), but positive values are computed as given, as long as the decays' product over 128 tokens is finite.  A decay below 2^-126 counts as zero.
+ * Where a is zero the state is u, whatever came before it, also where that is not finite; a state that is not finite may also be forgotten where the decays' product over some tokens since is below 2^-149.
  */
 enum { TRI_INV_REC_DECAY = 0, TRI_INV_REC_NORMED = 1, TRI_INV_REC_GATE = 2 };
 #define TRI_INV_REC_TILE 64   /* tokens from one carried state to the next */
 typedef struct tri_inv_rec_desc {
   int32_t B;        /* sequences in dense mode; must be 1 in packed mode */
   int32_t T;        /* tokens per sequence (dense) or total tokens (packed); B * T < 2^31 */
-  int32_t D;        /* channels, at least 1 */
+  int32_t D;        /* channels, 1 .. 2^26 (more: TRI_INV_ERR_UNSUPPORTED) */
   int32_t dtype;    /* storage of X, G, Y and of the gradients' tensors: TRI_INV_F32 or TRI_INV_BF16 */
   int32_t mode;     /* TRI_INV_REC_* */
   int32_t n_seqs;   /* packed: number of sequences; dense: 0 */
   const int32_t* cu_seqlens;   /* packed: HOST array of n_seqs + 1 offsets, 0 first, T last, none below the one before; dense: NULL */
 } tri_inv_rec_desc;
 /*
- *   X, G, Y: one row of D values for each token, ldx, ldg, ldy values from one token's row to the next (at least D; dense: a sequence's first row follows the last one's last), so that
+ *   X, G, Y: one row of D values for each token, ldx, ldg, ldy values from one token's row to the next (at least D, at most 2^26, else TRI_INV_ERR_UNSUPPORTED; dense: a sequence's first row follows the last one's last), so that
  *   halves of one projection's output need no copy.  Pointers aligned to their type; pointers and rows that are 16-byte aligned are the fastest.  h0, h_out [n_sequences, D] fp32, each may be NULL.
  *   carries [tri_inv_gated_recurrence_carries() rows, D] fp32 or NULL: the state behind every 64th token of a sequence, for the gradient; rows that no token stands for are left as they are.
  * Y may be X or G itself, h_out may be h0 itself; otherwise no output may overlap an input or another output: TRI_INV_ERR_INVALID_ARG.  Y NULL: only the states are wanted.
- * Everything between loads and stores is fp32.  The sums' order, and so every bit of the result, depends on the call's sizes alone, save where tiles of a long sequence meet: which
- * of the maps that join them were already joined depends on timing (a rounding of the carried state, 2^-24).
+ * Everything between loads and stores is fp32, and the order of the sums depends on the sizes alone: two calls give the same bits.
  * workspace: at least tri_inv_gated_recurrence_workspace() bytes of device memory (which may be 0: then it may be NULL), 16-byte aligned, contents arbitrary; nothing else
- * may use it until the call has run.  Nothing is allocated.  Launches: one, one more where sequences are cut, and with packed sequences one for every 320 of them.
+ * may use it until the call has run.  Nothing is allocated.  Launches: one; one more where a dense call's sequences are cut, or, packed, one for every 320
+ * sequences.
  */
 int tri_inv_gated_recurrence_carries(const tri_inv_rec_desc* desc, int64_t* rows);
 int tri_inv_gated_recurrence_workspace(const tri_inv_rec_desc* desc, size_t* bytes);
@@ -442,7 +442,7 @@ int tri_inv_selftest_recurrence_wait_timeout(const void* X, const void* G, void*
  *     dg_t = e_t a_t h_{t-1}  |  e_t (a_t h_{t-1} - a_t^2 / m_t x_t)  |  e_t (h_{t-1} - x_t) a_t (1 - a_t)
  * (normed: the second term counts as 0 where m = 0; where a = 0 all of dg is 0 and nothing reaches what came before).  The states are formed again in fp32, from h0 and from `carries` as the forward call with the same X, G, h0 and sequences left
  * them, or, where carries is NULL, from a walk of this call's own.  dX may be X or dY itself, dG may be G or dY itself, dh0 may be dh itself (dX and dG not both dY); otherwise no output may overlap anything.
- * Types, layouts, sequences and launches as there (one walk more without carries); workspace: by the query with the same desc and whether carries are given.
+ * Types, layouts, sequences and launches as there, one launch more without carries; workspace: by the query with the same desc and whether carries are given.
  */
 int tri_inv_gated_recurrence_backward_workspace(const tri_inv_rec_desc* desc, int with_carries, size_t* bytes);
 int tri_inv_gated_recurrence_backward(const void* dY, int64_t lddy, const void* X, int64_t ldx, const void* G, int64_t ldg, const float* h0, const float* dh,
@@ -607,7 +607,7 @@ int tri_inv_count_matrices(const tri_inv_desc* desc, int64_t* out);
  * status word of the current device.  *out is TRI_INV_OK, or
  * TRI_INV_ERR_DEVICE_TIMEOUT if a kernel gave up on a bounded wait (the
  * kernel then returned early and its outputs are incomplete), or
- * TRI_INV_ERR_INVALID_ARG if tri_inv_linear_attention_step met a slot that it refuses.  This call
+ * TRI_INV_ERR_INVALID_ARG if tri_inv_linear_attention_step or tri_inv_gated_recurrence_step met a slot that it refuses.  This call
  * copies 4 bytes from the device and so synchronises with it.
  */
 int tri_inv_last_device_status(int* out);

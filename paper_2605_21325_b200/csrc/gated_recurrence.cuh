@@ -305,41 +305,59 @@ __device__ __forceinline__ unsigned long long rec_now() {
   return t;
 }
 
-// What enters a tile, from the words of the `count` tiles in front of it in its sequence (words of one channel, `step` from one to the one before): their maps join
-// from the nearest on until one forgets what came before (P = 0; a tile that knows what leaves it says so with P = 0, the first one always does).
-// A word that is missing for the time limit raises the status word, and the NaN that is returned then goes on with this tile's own word, so that no later tile waits as long.
+// What enters a tile, from the words of the `count` tiles in front of it in its sequence (words of one channel, `step` from one to the one before).  The search goes back to the nearest tile that forgets what came
+// before it (P = 0; a tile that knows what leaves it says so with P = 0, the first one always does) and then applies the maps in between in order: the same sums as from tile to tile, whichever words were
+// already there.  A word that is missing for the time limit raises the status word, and the NaN that is returned then goes on with this tile's own word, so that no later tile waits as long.
 __device__ __forceinline__ float rec_look_back(const unsigned long long* word, long long step, int count, unsigned long long limit, int* status) {
   constexpr int AT_ONCE = 4;   // words that are asked for together
   constexpr unsigned long long NONE = ~0ull;
-  float P = 1.f, H = 0.f;
+  {   // mostly one of the nearest two knows
+    const unsigned long long v = rec_peek(word), u = count > 1 ? rec_peek(word - step) : NONE;
+    const float P = __uint_as_float((uint32_t)v), H = __uint_as_float((uint32_t)(v >> 32));
+    if (v != NONE && P == 0.f) return H;
+    if (v != NONE && u != NONE && (uint32_t)u << 1 == 0) return rec_step(P, __uint_as_float((uint32_t)(u >> 32)), H);
+  }
   unsigned long long begin = 0;
+  float h = 0.f;
+  bool found = false;
+  int base = 0;
   for (unsigned int polls = 1;; ++polls) {
     unsigned long long v[AT_ONCE];
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) v[i] = i < count ? rec_peek(word - i * step) : NONE;
-    int got = 0;
+    for (int i = 0; i < AT_ONCE; ++i) v[i] = base + i < count ? rec_peek(word - (base + i) * step) : NONE;
+    int from = AT_ONCE;   // the maps before this one are applied
+    if (!found) {
+      int got = 0;
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-      if (got == i && v[i] != NONE) {
-        const float p = __uint_as_float((uint32_t)v[i]), h = __uint_as_float((uint32_t)(v[i] >> 32));
-        H = fmaf(P, h, H);   // (P is not zero here)
-        if (p == 0.f) return H;
-        P *= p;
-        if (P == 0.f) return H;
-        ++got;
+      for (int i = 0; i < AT_ONCE; ++i) {
+        if (!found && got == i && v[i] != NONE) {
+          ++got;
+          if (__uint_as_float((uint32_t)v[i]) == 0.f) {
+            h = __uint_as_float((uint32_t)(v[i] >> 32));
+            found = true;
+            from = i;
+          }
+        }
+      }
+      if (!found) {
+        if (got == AT_ONCE) {
+          base += AT_ONCE;
+        } else if ((polls & 127) == 0) {
+          const unsigned long long now = rec_now();
+          if (begin == 0) begin = now;
+          else if (now - begin > limit) {
+            atomicMax(status, (int)TRI_INV_ERR_DEVICE_TIMEOUT);
+            return __uint_as_float(0x7fc00000u);
+          }
+        }
+        continue;
       }
     }
-    word -= got * step;
-    count -= got;
-    if (count <= 0) return H;
-    if (got == 0 && (polls & 127) == 0) {
-      const unsigned long long now = rec_now();
-      if (begin == 0) begin = now;
-      else if (now - begin > limit) {
-        atomicMax(status, (int)TRI_INV_ERR_DEVICE_TIMEOUT);
-        return __uint_as_float(0x7fc00000u);
-      }
-    }
+#pragma unroll
+    for (int i = AT_ONCE - 1; i >= 0; --i)
+      if (i < from) h = rec_step(__uint_as_float((uint32_t)v[i]), h, __uint_as_float((uint32_t)(v[i] >> 32)));
+    if (base == 0) return h;
+    base -= AT_ONCE;
   }
 }
 

@@ -38,6 +38,7 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
   extern __shared__ __align__(128) unsigned char stages[];
   __shared__ __align__(16) float2 part[2][kRecWarps][CH];   // (P, H) of each warp's tokens
   __shared__ __align__(8) float back[2][kRecWarps][CH];     // C: what they pass on where nothing reaches them from behind
+  __shared__ __align__(8) float2 total[2][CH];              // (P, C) of a tile
   __shared__ __align__(16) float2 entry[2][CH];             // the state in front of a tile, and what reaches it from behind
   __shared__ RecAt ring[kRecRing];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -69,9 +70,8 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
       }
       entry[i & 1][lane] = make_float2(h, e);
       rec_meet<kRecEntry, kRecThreads>();
-      float s = e;
-#pragma unroll
-      for (int w = kRecWarps - 1; w >= 0; --w) s = rec_step(part[i & 1][w][lane].x, s, back[i & 1][w][lane]);
+      const float2 map = total[i & 1][lane];
+      const float s = rec_step(map.x, e, map.y);
       carried = s;
       if (in) {
         if (first) { if (a.dh0) a.dh0[state] = s; }
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
       *reinterpret_cast<float2*>(&back[i & 1][warp][Shape::channel()]) = cc;
     }
     rec_meet<kRecMaps, 32 * kRecWarps>();
-    if (WORDS && warp == 0 && t.index > 0 && t.index + 1 < t.tiles) {   // the tile's word, for those in front of it
+    if (warp == 0) {   // the tile's map; as a word for those in front of it
       float TP = 1.f, TC = 0.f;
 #pragma unroll
       for (int w = kRecWarps - 1; w >= 0; --w) {
@@ -165,7 +165,8 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
         TP *= p;
         TC = rec_step(p, TC, back[i & 1][w][lane]);
       }
-      if (t.c0 + lane < a.D) rec_post(a.words + (long long)t.slot * a.D + t.c0 + lane, TP, TC);
+      total[i & 1][lane] = make_float2(TP, TC);
+      if (WORDS && t.index > 0 && t.index + 1 < t.tiles && t.c0 + lane < a.D) rec_post(a.words + (long long)t.slot * a.D + t.c0 + lane, TP, TC);
     }
     rec_meet<kRecEntry, kRecThreads>();
     const float4 e0 = *reinterpret_cast<const float4*>(&entry[i & 1][Shape::channel()]);

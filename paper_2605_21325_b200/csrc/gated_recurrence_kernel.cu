@@ -15,6 +15,7 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
   constexpr int CH = kRecChannels, TILE = Shape::TILE, ROW = Shape::ROW, es = sizeof(T);
   extern __shared__ __align__(128) unsigned char stages[];
   __shared__ __align__(16) float2 part[2][kRecWarps][CH];   // (P, H) of each warp's tokens
+  __shared__ __align__(8) float2 total[2][CH];              // ... of the tile
   __shared__ __align__(8) float entry[2][CH];               // what enters a tile
   __shared__ RecAt ring[kRecRing];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -44,15 +45,19 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
       }
       entry[i & 1][lane] = h;
       rec_meet<kRecEntry, kRecThreads>();
-      float s = h;
-      float* to = in && a.carries ? a.carries + (rec_slot(t.begin, t.seq, kRecCarry) + (long long)index * (TILE / kRecCarry)) * a.D + c : nullptr;
-      const int left = t.len - index * TILE;
+      const float2 map = total[i & 1][lane];
+      const float s = rec_step(map.x, h, map.y);
+      if (a.carries && in) {   // those that a further token of the sequence follows; a tile's last one by its map, as its word says
+        float* to = a.carries + (rec_slot(t.begin, t.seq, kRecCarry) + (long long)index * (TILE / kRecCarry)) * a.D + c;
+        const int left = t.len - index * TILE;
+        float m = h;
 #pragma unroll
-      for (int w = 0; w < kRecWarps; ++w) {
-        const float2 q = part[i & 1][w][lane];
-        s = rec_step(q.x, s, q.y);
-        const int n = (w + 1) * Shape::WARP_TOK;
-        if (n % kRecCarry == 0 && to && n < left) to[(long long)(n / kRecCarry - 1) * a.D] = s;   // those that a further token of the sequence follows
+        for (int n = Shape::WARP_TOK; n < TILE; n += Shape::WARP_TOK) {
+          const float2 q = part[i & 1][n / Shape::WARP_TOK - 1][lane];
+          m = rec_step(q.x, m, q.y);
+          if (n % kRecCarry == 0 && n < left) to[(long long)(n / kRecCarry - 1) * a.D] = m;
+        }
+        if (TILE < left) to[(long long)(TILE / kRecCarry - 1) * a.D] = s;
       }
       carried = s;
       if (in) {
@@ -126,7 +131,7 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
     const float2 pp = both(mul2(P, other_P)), hh = both(rec_step(other_P, H, other_H));
     if (!second) *reinterpret_cast<float4*>(&part[i & 1][warp][Shape::channel()]) = make_float4(pp.x, hh.x, pp.y, hh.y);
     rec_meet<kRecMaps, 32 * kRecWarps>();
-    if (WORDS && warp == kRecWarps - 1 && t.index > 0 && t.index + 1 < t.tiles) {   // the tile's word, for those behind it
+    if (warp == kRecWarps - 1) {   // the tile's map; as a word for those behind it
       float TP = 1.f, TH = 0.f;
 #pragma unroll
       for (int w = 0; w < kRecWarps; ++w) {
@@ -134,7 +139,8 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
         TP *= q.x;
         TH = rec_step(q.x, TH, q.y);
       }
-      if (t.c0 + lane < a.D) rec_post(a.words + (long long)t.slot * a.D + t.c0 + lane, TP, TH);
+      total[i & 1][lane] = make_float2(TP, TH);
+      if (WORDS && t.index > 0 && t.index + 1 < t.tiles && t.c0 + lane < a.D) rec_post(a.words + (long long)t.slot * a.D + t.c0 + lane, TP, TH);
     }
     P = twice(1.f);
     H = twice(0.f);

@@ -17,7 +17,7 @@ int check_rec(const tri_inv_rec_desc* d) {
   if (!d || d->B < 1 || d->T < 0 || d->D < 1) return TRI_INV_ERR_INVALID_ARG;
   if (d->dtype != TRI_INV_F32 && d->dtype != TRI_INV_BF16) return TRI_INV_ERR_INVALID_ARG;
   if (d->mode != TRI_INV_REC_DECAY && d->mode != TRI_INV_REC_NORMED && d->mode != TRI_INV_REC_GATE) return TRI_INV_ERR_INVALID_ARG;
-  if ((long long)d->B * d->T > 0x7fffffffLL || d->D > kMostBetweenRows) return TRI_INV_ERR_INVALID_ARG;
+  if ((long long)d->B * d->T > 0x7fffffffLL) return TRI_INV_ERR_INVALID_ARG;
   if (d->cu_seqlens) {
     if (d->B != 1 || d->n_seqs < 0 || d->cu_seqlens[0] != 0 || d->cu_seqlens[d->n_seqs] != d->T) return TRI_INV_ERR_INVALID_ARG;
     for (int s = 0; s < d->n_seqs; ++s)
@@ -25,7 +25,7 @@ int check_rec(const tri_inv_rec_desc* d) {
   } else if (d->n_seqs != 0) {
     return TRI_INV_ERR_INVALID_ARG;
   }
-  return TRI_INV_OK;
+  return d->D > kMostBetweenRows ? TRI_INV_ERR_UNSUPPORTED : TRI_INV_OK;
 }
 int seqs_of(const tri_inv_rec_desc* d) { return d->cu_seqlens ? d->n_seqs : d->B; }
 long long tokens_of(const tri_inv_rec_desc* d) { return (long long)d->B * d->T; }

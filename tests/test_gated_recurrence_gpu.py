@@ -294,3 +294,19 @@ def test_no_tokens(bnd):
     dX, dG, dh0 = bnd.gated_recurrence_backward(X, X, X, h0=h0, dh=dh)
     assert dX.shape == X.shape and torch.equal(dh0, dh)
     assert bool((bnd.gated_recurrence(X, X)[1] == 0).all())
+
+
+@pytest.mark.parametrize("D", [64, 700, 2048])
+def test_two_calls_give_the_same_bits(bnd, D):
+    """Whatever order the tiles of a long sequence arrive in, in a batch or alone."""
+    for mode in MODES:
+        s = make([3000] * 3, D, False, torch.bfloat16, mode)
+        call = lambda c: bnd.gated_recurrence_backward(s["dY"], s["X"], s["G"], mode=mode, h0=s["h0"], dh=s["dh"], carries=c)   # noqa: E731
+        first = bnd.gated_recurrence(s["X"], s["G"], mode=mode, h0=s["h0"], want_carries=True)
+        grads = call(first[2])
+        for _ in range(5):
+            Y, S, c = bnd.gated_recurrence(s["X"], s["G"], mode=mode, h0=s["h0"], want_carries=True)
+            assert torch.equal(Y, first[0]) and torch.equal(S, first[1])
+            assert all(torch.equal(a, b) for a, b in zip(call(c), grads)) and all(torch.equal(a, b) for a, b in zip(call(None), grads))
+        one = bnd.gated_recurrence(s["X"][1:2], s["G"][1:2], mode=mode, h0=s["h0"][1:2])
+        assert torch.equal(one[0][0], first[0][1]) and torch.equal(one[1][0], first[1][1])
