@@ -398,7 +398,7 @@ int tri_inv_rms_norm_backward(const void* dY, const void* X, const void* w, cons
  *     TRI_INV_REC_DECAY    a = exp(g),             u = x
  *     TRI_INV_REC_NORMED   a = exp(g),             u = sqrt(1 - a^2) x        (0 where g >= 0)
  *     TRI_INV_REC_GATE     a = 1 / (1 + exp(-g)),  u = (1 - a) x
- * g is at most 0 in any model of the first two (-inf: the state forgets at once), but positive values are computed as given, as long as the decays' product over 128 tokens is finite.  A decay below 2^-126 counts as zero.
+ * g is at most 0 in any model of the first two (-inf: the state forgets at once), but positive values are computed as given, as long as the decays' product over 128 tokens is finite.  A decay that fp32 holds only as a number below 2^-126 may count as zero.
  * Where a is zero the state is u, whatever came before it, also where that is not finite; a state that is not finite may also be forgotten where the decays' product over some tokens since is below 2^-149.
  */
 enum { TRI_INV_REC_DECAY = 0, TRI_INV_REC_NORMED = 1, TRI_INV_REC_GATE = 2 };

@@ -126,29 +126,34 @@ template <> struct RecLane<float> {
   }
 };
 
-// e^g as 2^(g log2 e), off by the power's own error, 2^-22.5, and by that of the rounded product, |g| 2^-24, which is what a rounding of g itself would change.  Results below 2^-126 are 0.
+// e^g as 2^(g log2 e), off by the power's own error, 2^-22.5, and by that of the rounded product, |g| 2^-24, which is what a rounding of g itself would change.  Results below 2^-126 are 0 (squared, below 2^-149).
 __device__ __forceinline__ float rec_power(float t) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(t)); return y; }
+template <int HALF = 0>   // of g / 2
 __device__ __forceinline__ Pair rec_exp(Pair g) {
-  const float2 t = both(mul2(g, twice(1.44269504088896341f)));
+  const float2 t = both(mul2(g, twice(HALF ? 0.72134752044448170f : 1.44269504088896341f)));
   return pair(rec_power(t.x), rec_power(t.y));
 }
 __device__ __forceinline__ float rec_reciprocal(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float rec_root(float x) { float y; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
-// a and m (what multiplies x).  normed: 1 - a^2 = -2 sinh(g) e^g, which does not cancel, for |g| <= 1/4, where the first term left out of sinh(g) / g is g^6 / 7! < 2^-24.  gate: both from the smaller one, the larger as
-// 1 minus it, so that its error is a rounding's and has no preferred side.
+// a and m (what multiplies x).  A state sums a's errors over as many tokens as it remembers, so near 1 they may have no preferred side: decay and normed take a = 1 - q, q = 1 - e^g = -2 sinh(g / 2) e^{g / 2}, for |g| <= 1/4 (the
+// first term left out of sinh(x) / x is x^6 / 7!, x = g / 2: 2^-30), which is off by a rounding, and e^{g / 2} squared elsewhere; gate forms the smaller one of a and 1 - a and takes it from 1.  Measured over
+// g = -0.02 .. -0.004, mean (mean of the size) of a's error in 2^-24: 0.00 (0.25); a power of two alone -0.43 (0.54), expf -0.08 (0.42).  normed: 1 - a^2 = q (1 + a), which does not cancel.
 template <int MODE>
 __device__ __forceinline__ void rec_factors(Pair gp, Pair& a, Pair& m) {
   const float2 g = both(gp);
   const Pair one = twice(1.f), minus = twice(-1.f);
-  if constexpr (MODE == kRecDecay) {
-    a = rec_exp(gp);
-    m = one;
-  } else if constexpr (MODE == kRecNormed) {
-    a = rec_exp(gp);
-    const Pair y = mul2(gp, gp), near = mul2(mul2(gp, a), fma2(fma2(y, twice(-1.f / 60.f), twice(-1.f / 3.f)), y, twice(-2.f))), far = fma2(mul2(a, minus), a, one);
-    const float2 n = both(near), f = both(far);   // 1 - a^2
-    m = pair(rec_root(fmaxf(fabsf(g.x) <= 0.25f ? n.x : f.x, 0.f)), rec_root(fmaxf(fabsf(g.y) <= 0.25f ? n.y : f.y, 0.f)));
+  if constexpr (MODE == kRecDecay || MODE == kRecNormed) {
+    const Pair e = rec_exp<1>(gp), y = mul2(gp, gp), poly = fma2(fma2(y, twice(1.f / 1920.f), twice(1.f / 24.f)), y, one), fall = mul2(mul2(gp, e), poly);   // fall: a - 1
+    const float2 near = both(add2(fall, one)), far = both(mul2(e, e));
+    const bool nx = fabsf(g.x) <= 0.25f, ny = fabsf(g.y) <= 0.25f;
+    a = pair(nx ? near.x : far.x, ny ? near.y : far.y);
+    if constexpr (MODE == kRecNormed) {
+      const float2 n = both(fma2(fall, a, fall)), f = both(fma2(a, a, minus));   // a^2 - 1
+      m = pair(rec_root(fmaxf(-(nx ? n.x : f.x), 0.f)), rec_root(fmaxf(-(ny ? n.y : f.y), 0.f)));
+    } else {
+      m = one;
+    }
   } else {
     const Pair e = rec_exp(pair(-fabsf(g.x), -fabsf(g.y)));
     const float2 d = both(add2(e, one));
@@ -358,6 +363,21 @@ __device__ __forceinline__ float rec_look_back(const unsigned long long* word, l
       if (i < from) h = rec_step(__uint_as_float((uint32_t)v[i]), h, __uint_as_float((uint32_t)(v[i] >> 32)));
     if (base == 0) return h;
     base -= AT_ONCE;
+  }
+}
+
+// Waits until the tile of this word has read what it reads: where a final state lies in the place of the one carried in, nothing else may order the tile that writes it behind the tile that reads
+// (a decay of zero in between forgets).
+__device__ __forceinline__ void rec_await(const unsigned long long* word, unsigned long long limit, int* status) {
+  unsigned long long begin = 0;
+  for (unsigned int polls = 1; rec_peek(word) == ~0ull; ++polls) {
+    if ((polls & 127) != 0) continue;
+    const unsigned long long now = rec_now();
+    if (begin == 0) begin = now;
+    else if (now - begin > limit) {
+      atomicMax(status, (int)TRI_INV_ERR_DEVICE_TIMEOUT);
+      return;
+    }
   }
 }
 

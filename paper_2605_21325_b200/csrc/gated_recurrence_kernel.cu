@@ -1,4 +1,14 @@
 // Gated linear recurrence: the forward walk, and what both walks find in their workspace.
+//
+// One pass: every value is read once, by asynchronous copies one tile ahead, and every output written once.  A block of five warps takes a tile of 128 tokens and 32 channels.  Four warps hold 32 tokens each in
+// registers (two lane groups of 16 tokens, two channels a lane), as a and u, form their maps and meet; the fifth, a lane for each channel, meanwhile looks for what enters the tile in the words of the tiles in front of it;
+// then the four write h.  Long sequences are spread over the chip that way: a tile's own map is there for the tiles behind it as soon as it has been read.
+// What bounds it: with all channels of a large batch bytes (64 x 1024 tokens x 2048 channels, gate, bf16 146 us, 0.85 of a copy's rate; fp32 0.9); on the way instructions, 19 (decay) to 27 (normed) a value, and registers:
+// a and u of 16 tokens and two channels are 64, which leaves four blocks an SM.  Long walks over few channels wait for one another (1 x 65536 x 256 44 us, 0.35).
+// Why this shape, in us (1 x 32768 x 4096 decay | 4 x 4096 x 2560 normed | 64 x 1024 x 2048 gate; 125 | 39 | 125 of memory time): 64 x 64 tiles, every warp waiting for the entry 497 | 143; channels' threads aside and the next tile read
+// meanwhile 231 | 90; 128 x 64 tiles of sixteen tokens a lane, places worked out once a tile 184 | 79 (eight tokens 30 % more instructions: the fixed cost of a warp's tile, about 200 instructions, is shared by
+// half as many values); four warps and 32 channels, which leaves four blocks whose waits overlap 164 | 60 | 167; the entry looked for ahead of the maps 151 | 52 | 140; carried states joined in order, for equal bits,
+// 159 | 53 | 146.  16 or 64 channels a tile were slower, as were three or five blocks.
 #include <algorithm>
 
 #include "gated_recurrence.cuh"
@@ -6,7 +16,7 @@
 namespace tri_inv {
 namespace {
 
-constexpr int kTok = kRecTok, kBlocks = 4;   // tokens of a lane; blocks an SM
+constexpr int kTok = kRecTok, kBlocks = 4;   // tokens of a lane; blocks an SM: 96 registers a thread
 template <class T, int MODE, bool WORDS>
 __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(const __grid_constant__ RecArgs a) {
   using Shape = RecShape<T, kTok>;
@@ -61,8 +71,12 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
       }
       carried = s;
       if (in) {
-        if (last) { if (a.h_out) a.h_out[(long long)t.seq * a.D + c] = s; }
-        else if (WORDS && !(a.test_stall && t.item == 0)) rec_post(a.words + at, 0.f, s);
+        if (last) {
+          if (a.h_out) {
+            if (WORDS && !first && a.h_out == a.h0) rec_await(a.words + at - (long long)index * a.D, limit, a.status);
+            a.h_out[(long long)t.seq * a.D + c] = s;
+          }
+        } else if (WORDS && !(a.test_stall && t.item == 0)) rec_post(a.words + at, 0.f, s);
       }
       if (lane == 0) feed.give(&ring[(i + 3) & (kRecRing - 1)]);
       __syncwarp();
@@ -223,20 +237,13 @@ __global__ void __launch_bounds__(256) rec_setup_kernel(const __grid_constant__ 
 
 template <class T, int MODE, bool WORDS>
 cudaError_t launch_one(const RecArgs& a, cudaStream_t stream) {
-  static int sms[64] = {0};
-  int dev = 0;
+  int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  int n = sms[dev];
-  if (!n) {
-    if ((e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-    sms[dev] = n;
-  }
+  if (e != cudaSuccess || (e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
   constexpr size_t smem = 4 * (size_t)RecShape<T, kTok>::TENSOR;   // two tiles of two tensors
   if ((e = allow_shared<gated_recurrence_kernel<T, MODE, WORDS>>(smem)) != cudaSuccess) return e;
   const long long items = a.items;
-  if ((e = launch_early(gated_recurrence_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, (long long)kBlocks * n)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
+  if ((e = launch_early(gated_recurrence_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, (long long)kBlocks * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
   return launched();
 }
 template <class T>

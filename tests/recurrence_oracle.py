@@ -1,8 +1,9 @@
 """The gated linear recurrence and its gradient token by token in 64 bits, with a bound on what fp32 arithmetic may be off by, carried along by the same recurrences.
 
-STEP = 12 roundings of 2^-24 a token: the decay's own error (expf 2, a quotient 4, the series, products and differences 1 each: at most 9 for the logistic form), a fused
-product and sum 1, and 2 more for the maps that join tokens, warps and tiles.  The factor of x carries as many (square root form: half of 9, and 5 for the reciprocal root and its product), its
-reciprocal twice as many.
+STEP = 12 roundings of 2^-24 a token: the decay's own error (a power of two 2.8, a reciprocal 2, products and differences 1 each: at most 9 for the logistic form), a fused
+product and sum 1, and 2 more for the maps that join tokens, warps and tiles.  The factor of x carries as many (square root form: half of 9, and 3 for the root and its product), its
+reciprocal twice as many.  The exponent's product with log2 e rounds to |g| 2^-24 of the decay: beyond |g| = 8, where that alone would pass the rest, the decay leaves less than e^-8 of the state, and the token's input
+carries the sum.
 """
 import torch
 

@@ -310,3 +310,25 @@ def test_two_calls_give_the_same_bits(bnd, D):
             assert all(torch.equal(a, b) for a, b in zip(call(c), grads)) and all(torch.equal(a, b) for a, b in zip(call(None), grads))
         one = bnd.gated_recurrence(s["X"][1:2], s["G"][1:2], mode=mode, h0=s["h0"][1:2])
         assert torch.equal(one[0][0], first[0][1]) and torch.equal(one[1][0], first[1][1])
+
+
+@pytest.mark.parametrize("mode", MODES, **NAMES)
+def test_states_in_place_across_resets(bnd, mode):
+    """The final state in the place of the initial one, its gradient in the place of the final one's: also where decays of zero let no tile of the end wait for one of the beginning."""
+    lens, D = [2000] * 3, 300
+    s = make(lens, D, False, torch.bfloat16, mode)
+    s["G"][:, 5::7] = float("-inf")
+    want = bnd.gated_recurrence(s["X"], s["G"], mode=mode, h0=s["h0"], want_carries=True)
+    ref = oracle.walk(s["X"], s["G"], mode, lens, s["h0"])
+    oracle.inside(want[0], ref["h"], ref["eh"])
+    grads = bnd.gated_recurrence_backward(s["dY"], s["X"], s["G"], mode=mode, h0=s["h0"], dh=s["dh"])
+    L, p = bnd.load(), lambda t: t.data_ptr()   # noqa: E731
+    desc, need = bnd.RecDesc(3, 2000, D, bnd.BF16, mode, 0, None), bnd._workspace("tri_inv_gated_recurrence_backward_workspace", bnd.RecDesc(3, 2000, D, bnd.BF16, mode, 0, None), 1)
+    work, dX, dG = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty_like(s["X"]), torch.empty_like(s["X"])
+    for _ in range(5):
+        h, dh = s["h0"].clone(), s["dh"].clone()
+        Y, S, _ = bnd.gated_recurrence(s["X"], s["G"], mode=mode, h0=h, state_out=h)
+        assert S is h and torch.equal(Y, want[0]) and torch.equal(h, want[1])
+        assert L.tri_inv_gated_recurrence_backward(p(s["dY"]), D, p(s["X"]), D, p(s["G"]), D, p(s["h0"]), p(dh), p(want[2]), p(dX), D, p(dG), D, p(dh), p(work), need, desc, None) == 0
+        assert torch.equal(dX, grads[0]) and torch.equal(dG, grads[1]) and torch.equal(dh, grads[2])
+    assert bnd.last_device_status() == 0
