@@ -183,12 +183,12 @@ __device__ __forceinline__ Pair rec_other(Pair v) {
 }
 __device__ __forceinline__ bool any_zero(Pair a) { const float2 x = both(a); return x.x == 0.f || x.y == 0.f; }
 
-// How a tensor's rows are moved: 16 bytes (everything aligned to them), 4 bytes, or value by value (bf16 at odd places)
-enum : int { kRecWide = 0, kRecFours = 1, kRecSingle = 2 };
+// How a tensor's rows are moved: 16, 8 or 4 bytes at a time (everything aligned to them), or by single values (bf16 at odd places)
+enum : int { kRecWide = 0, kRecEights = 1, kRecFours = 2, kRecSingle = 3 };
 template <class T>
-__device__ __forceinline__ int rec_access(const void* p, long long ld) {
+__host__ __device__ __forceinline__ int rec_access(const void* p, long long ld) {
   const unsigned long long at = reinterpret_cast<unsigned long long>(p) | (unsigned long long)ld * sizeof(T);
-  return (at & 15) == 0 ? kRecWide : (at & 3) == 0 ? kRecFours : kRecSingle;
+  return (at & 15) == 0 ? kRecWide : (at & 7) == 0 ? kRecEights : (at & 3) == 0 ? kRecFours : kRecSingle;
 }
 
 // Two neighbouring 16-bit values, of which those past `width` are zero
@@ -202,7 +202,7 @@ __device__ __forceinline__ uint32_t rec_half_words(const T* row, int c, int widt
 template <class T>
 __device__ __forceinline__ typename RecLane<T>::Raw rec_load(const T* row, int c, int width, int access) {
   if constexpr (sizeof(T) == 4) {
-    if (access == kRecWide && c + 1 < width) return *reinterpret_cast<const uint2*>(row + c);
+    if (access <= kRecEights && c + 1 < width) return *reinterpret_cast<const uint2*>(row + c);
     return make_uint2(c < width ? __float_as_uint(row[c]) : 0u, c + 1 < width ? __float_as_uint(row[c + 1]) : 0u);
   } else {
     if (access != kRecSingle && c + 1 < width) return *reinterpret_cast<const uint32_t*>(row + c);
@@ -213,7 +213,7 @@ template <class T>
 __device__ __forceinline__ void rec_store(T* row, int c, int width, int access, Pair v) {
   const typename RecLane<T>::Raw raw = RecLane<T>::pack(v);
   if constexpr (sizeof(T) == 4) {
-    if (access == kRecWide && c + 1 < width) { *reinterpret_cast<uint2*>(row + c) = raw; return; }
+    if (access <= kRecEights && c + 1 < width) { *reinterpret_cast<uint2*>(row + c) = raw; return; }
     if (c < width) row[c] = __uint_as_float(raw.x);
     if (c + 1 < width) row[c + 1] = __uint_as_float(raw.y);
   } else {
@@ -230,10 +230,23 @@ __device__ __forceinline__ void rec_copy(uint32_t to, const void* from, int byte
 __device__ __forceinline__ void rec_copy4(uint32_t to, const void* from, int bytes4) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes4) : "memory");
 }
+__device__ __forceinline__ void rec_copy8(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory"); }
 __device__ __forceinline__ void rec_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void rec_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// Where a block stands: a tile of an item, which is a tile (with words) or a whole sequence
+struct RecAt {
+  int item;            // >= the number of items: none left
+  int seq, c0;         // c0: the tile's first channel
+  int begin, len;      // the sequence's
+  int index, tiles;    // the tile, of how many
+  int n;               // its tokens
+  bool whole;          // all tokens and channels of a tile
+  int tok0;
+  int slot;            // of its words
+  long long at[5];     // where its first value lies in each tensor, in bytes
+};
 // The lanes of a warp stand in kRecGroups groups, each of which has TOK tokens behind one another, two channels a lane.  In shared memory a row follows the one before, and a
 // group's rows are one row further on, so that the groups' reads meet in no bank.
 template <class T, int TOK>
@@ -261,6 +274,66 @@ struct RecShape {
       from += ld * (AT_ONCE * (int)sizeof(T));
     }
   }
+  // ... where BYTES can be moved; at: of the tile's first value, in bytes
+  template <int BYTES>
+  static __device__ __forceinline__ void request_pieces(uint32_t warp_smem, const char* tile, long long ld_bytes, int row0) {
+    constexpr int PER_ROW = ROW / BYTES, ROWS = 32 / PER_ROW;   // lanes of a row, rows at once
+    static_assert(TOK % ROWS == 0, "");
+    const int lane = threadIdx.x & 31, r = lane / PER_ROW, off = lane % PER_ROW * BYTES;
+    const char* from = tile + (row0 + r) * ld_bytes + off;
+#pragma unroll
+    for (int i = 0; i < WARP_TOK / ROWS; ++i) {
+      const uint32_t to = warp_smem + r * ROW + off + i * ROWS * ROW + i * ROWS / TOK * ROW;
+      if constexpr (BYTES == 8) rec_copy8(to, from);
+      else rec_copy4(to, from, 4);
+      from += ROWS * ld_bytes;
+    }
+  }
+  // A whole tile of 16-bit values at odd places comes as the aligned words that hold a row: the row's sixteen and, in `rest` (a warp's, [WARP_TOK]), the one behind them.  The words of the first row's first channels and of the last
+  // row's last ones may lie half outside the tensor: those tiles do not come so.
+  static __device__ __forceinline__ bool by_words(const RecArgs& a, int tok0, int c0) {
+    const long long tokens = a.table ? a.T : (long long)a.n_seqs * a.T;
+    return sizeof(T) == 2 && (tok0 > 0 || c0 > 0) && (tok0 + TILE < tokens || c0 + CHANNELS < a.D);
+  }
+  static __device__ __forceinline__ void request_words(uint32_t warp_smem, uint32_t rest, const char* tile, long long ld_bytes, int row0) {
+    const int lane = threadIdx.x & 31, r = group(), off = lane % LANES * 4;
+    auto word = [](const char* p) { return reinterpret_cast<const char*>(reinterpret_cast<unsigned long long>(p) & ~3ull); };
+    const char* from = tile + (row0 + r * TOK) * ld_bytes;
+#pragma unroll
+    for (int k = 0; k < TOK; ++k) {
+      rec_copy4(warp_smem + place() + k * ROW, word(from) + off, 4);
+      from += ld_bytes;
+    }
+    for (int row = lane; row < WARP_TOK; row += 32) {
+      const char* p = tile + (row0 + row) * ld_bytes;   // (a row that is aligned has no word behind it to read)
+      const bool odd = reinterpret_cast<unsigned long long>(p) & 2;
+      rec_copy4(rest + 4 * row, odd ? word(p) + ROW : p, odd ? 4 : 0);
+    }
+  }
+  static __device__ __forceinline__ void settle_words(unsigned char* warp_smem, const unsigned char* rest, const char* tile, long long ld_bytes, int row0) {   // the rows as they would have come
+    const int lane = threadIdx.x & 31, r = group();
+    const uint32_t start = (uint32_t)reinterpret_cast<unsigned long long>(tile) + (uint32_t)(row0 + r * TOK) * (uint32_t)ld_bytes;
+#pragma unroll
+    for (int k = 0; k < TOK; ++k) {
+      uint32_t* at = reinterpret_cast<uint32_t*>(warp_smem + place() + k * ROW);
+      const uint32_t w = *at;
+      uint32_t next = __shfl_down_sync(0xffffffffu, w, 1);
+      if (lane % LANES == LANES - 1) next = *reinterpret_cast<const uint32_t*>(rest + 4 * (r * TOK + k));
+      if ((start + (uint32_t)k * (uint32_t)ld_bytes) & 2) *at = __funnelshift_r(w, next, 16);
+    }
+  }
+  // A tensor's rows of a whole tile however they lie
+  static __device__ __forceinline__ void request_any(uint32_t warp_smem, uint32_t rest, const RecArgs& a, const T* base, const RecAt& t, int tensor, long long ld, int row0, int access) {
+    const char* tile = (const char*)base + t.at[tensor];
+    if (access == kRecWide) request_whole(warp_smem, tile + copy_from(ld, row0), ld);
+    else if (access == kRecEights) request_pieces<8>(warp_smem, tile, ld * (int)sizeof(T), row0);
+    else if (access == kRecFours) request_pieces<4>(warp_smem, tile, ld * (int)sizeof(T), row0);
+    else if (by_words(a, t.tok0, t.c0)) request_words(warp_smem, rest, tile, ld * (int)sizeof(T), row0);
+    else request(warp_smem, base, ld, t.tok0 + row0, TILE, t.c0, a.D, access);
+  }
+  static __device__ __forceinline__ void settle_any(unsigned char* warp_smem, const unsigned char* rest, const RecArgs& a, const T* base, const RecAt& t, int tensor, long long ld, int row0, int access) {
+    if (access == kRecSingle && t.whole && by_words(a, t.tok0, t.c0)) settle_words(warp_smem, rest, (const char*)base + t.at[tensor], ld * (int)sizeof(T), row0);
+  }
   // ... where not: rows row0 .. of which `rows` exist, channels c0 .. of `width`; what does not exist reads as zero
   static __device__ __forceinline__ void request(uint32_t warp_smem, const T* base, long long ld, long long row0, int rows, int c0, int width, int access) {
     const int lane = threadIdx.x & 31;
@@ -274,7 +347,7 @@ struct RecShape {
     } else {
       const int first = group() * TOK, c = c0 + channel();
       const uint32_t to = warp_smem + place();
-      if (sizeof(T) == 4 || (access == kRecFours && (width - c0 >= CHANNELS || width % 2 == 0))) {
+      if (sizeof(T) == 4 || (access != kRecSingle && (width - c0 >= CHANNELS || width % 2 == 0))) {
 #pragma unroll
         for (int k = 0; k < TOK; ++k)
 #pragma unroll
@@ -386,18 +459,6 @@ enum : int { kRecMaps = 1, kRecEntry = 2 };
 template <int WHICH, int THREADS>
 __device__ __forceinline__ void rec_meet() { asm volatile("bar.sync %0, %1;" ::"n"(WHICH), "n"(THREADS) : "memory"); }
 
-// Where a block stands: a tile of an item, which is a tile (with words) or a whole sequence
-struct RecAt {
-  int item;            // >= the number of items: none left
-  int seq, c0;         // c0: the tile's first channel
-  int begin, len;      // the sequence's
-  int index, tiles;    // the tile, of how many
-  int n;               // its tokens
-  bool whole;          // all tokens and channels of a tile
-  int tok0;
-  int slot;            // of its words
-  long long at[5];     // where its first value lies in each tensor, in bytes
-};
 // The order of a block's tiles.  The one that it works on, the one before and those that are on their way lie in a ring in shared memory, which one thread keeps ahead.  With words the items are drawn
 // from the ticket, so that the tiles in front of a tile are done or in the hands of blocks that run; else they go by a fixed stride.
 constexpr int kRecRing = 8;

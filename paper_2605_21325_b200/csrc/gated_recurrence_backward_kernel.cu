@@ -34,7 +34,8 @@ __device__ __forceinline__ Pair none_where_zero(Pair a, Pair v) {
   return pair(x.x == 0.f ? 0.f : y.x, x.y == 0.f ? 0.f : y.y);
 }
 
-template <class T, int MODE, bool WORDS>
+// ANY: some input cannot be moved 16 bytes at a time
+template <class T, int MODE, bool WORDS, bool ANY>
 __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_recurrence_backward_kernel(const __grid_constant__ RecArgs a) {
   constexpr int kTok = rec_back_tok(sizeof(T)), kPart = MODE == kRecDecay || kTok == 8 ? kTok : kTok / 2;   // tokens that are finished at a time
   using Shape = RecShape<T, kTok>;
@@ -47,6 +48,7 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
   __shared__ __align__(8) float2 total[2][CH];              // (P, C) of a tile
   __shared__ __align__(16) float2 entry[2][CH];             // the state in front of a tile, and what reaches it from behind
   __shared__ RecAt ring[kRecRing];
+  __shared__ __align__(4) unsigned char rest[ANY ? 2 : 1][3][kRecWarps][ANY && es == 2 ? 4 * Shape::WARP_TOK : 4];   // of rows at odd places (RecShape)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int items = a.items;
   RecFeed<WORDS, TILE, 5, true> feed{a, {(int)(a.ld_x * es), (int)(a.ld_g * es), (int)(a.ld_dy * es), (int)(a.ld_dx * es), (int)(a.ld_dg * es)}, es};
@@ -94,19 +96,25 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
   }
 
   const T *X = (const T*)a.x, *G = (const T*)a.g, *DY = (const T*)a.dy;
-  const int x_access = rec_access<T>(X, a.ld_x), g_access = rec_access<T>(G, a.ld_g), dy_access = rec_access<T>(DY, a.ld_dy);
-  const int dx_access = rec_access<T>(a.dx, a.ld_dx), dg_access = rec_access<T>(a.dg, a.ld_dg), most = es == 4 ? kRecWide : kRecFours;
-  const bool wide = x_access == kRecWide && g_access == kRecWide && dy_access == kRecWide, plain = dx_access <= most && dg_access <= most;   // plain: whole lanes can be written
+  const int x_access = ANY ? rec_access<T>(X, a.ld_x) : (int)kRecWide, g_access = ANY ? rec_access<T>(G, a.ld_g) : (int)kRecWide, dy_access = ANY ? rec_access<T>(DY, a.ld_dy) : (int)kRecWide;
+  const int dx_access = rec_access<T>(a.dx, a.ld_dx), dg_access = rec_access<T>(a.dg, a.ld_dg), most = es == 4 ? kRecEights : kRecFours;
+  const bool plain = dx_access <= most && dg_access <= most;   // plain: whole lanes can be written
+  const bool odd = x_access == kRecSingle || g_access == kRecSingle || dy_access == kRecSingle;
   const int first = warp * Shape::WARP_TOK;
   const char *x_from = (const char*)X + Shape::copy_from(a.ld_x, first), *g_from = (const char*)G + Shape::copy_from(a.ld_g, first), *dy_from = (const char*)DY + Shape::copy_from(a.ld_dy, first);
   const uint32_t warp_smem = (uint32_t)__cvta_generic_to_shared(stages) + warp * Shape::WARP_BYTES;
   auto request = [&](const RecAt& t, int stage) {
     if (t.item < items) {
       const uint32_t to = warp_smem + stage * 3 * Shape::TENSOR;
-      if (t.whole && wide) {
+      if (!ANY && t.whole) {
         Shape::request_whole(to, x_from + t.at[0], a.ld_x);
         Shape::request_whole(to + Shape::TENSOR, g_from + t.at[1], a.ld_g);
         Shape::request_whole(to + 2 * Shape::TENSOR, dy_from + t.at[2], a.ld_dy);
+      } else if (ANY && t.whole) {
+        auto space = [&](int tensor) { return (uint32_t)__cvta_generic_to_shared(rest[ANY ? stage : 0][tensor][warp]); };
+        Shape::request_any(to, space(0), a, X, t, 0, a.ld_x, first, x_access);
+        Shape::request_any(to + Shape::TENSOR, space(1), a, G, t, 1, a.ld_g, first, g_access);
+        Shape::request_any(to + 2 * Shape::TENSOR, space(2), a, DY, t, 2, a.ld_dy, first, dy_access);
       } else {
         Shape::request(to, X, a.ld_x, t.tok0 + first, t.n - first, t.c0, a.D, x_access);
         Shape::request(to + Shape::TENSOR, G, a.ld_g, t.tok0 + first, t.n - first, t.c0, a.D, g_access);
@@ -123,6 +131,13 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
     request(ring[(i + 1) & (kRecRing - 1)], (i + 1) & 1);
     rec_wait<1>();
     __syncwarp();
+    if (ANY && odd) {
+      unsigned char* rows = stages + (i & 1) * 3 * Shape::TENSOR + warp * Shape::WARP_BYTES;
+      Shape::settle_any(rows, rest[ANY ? i & 1 : 0][0][warp], a, X, t, 0, a.ld_x, first, x_access);
+      Shape::settle_any(rows + Shape::TENSOR, rest[ANY ? i & 1 : 0][1][warp], a, G, t, 1, a.ld_g, first, g_access);
+      Shape::settle_any(rows + 2 * Shape::TENSOR, rest[ANY ? i & 1 : 0][2][warp], a, DY, t, 2, a.ld_dy, first, dy_access);
+      __syncwarp();
+    }
     const unsigned char* sx = stages + (i & 1) * 3 * Shape::TENSOR + warp * Shape::WARP_BYTES + Shape::place();
     auto read = [&](int tensor, int k) { return Lane::widen(*reinterpret_cast<const Raw*>(sx + tensor * Shape::TENSOR + k * ROW)); };
     Pair av[kTok], mv[kTok];   // (mv is not used where it is 1)
@@ -245,25 +260,26 @@ __global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_re
   rec_wait<0>();
 }
 
-template <class T, int MODE, bool WORDS>
+template <class T, int MODE, bool WORDS, bool ANY>
 cudaError_t launch_one(const RecArgs& a, cudaStream_t stream) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess || (e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
   constexpr size_t smem = 6 * (size_t)RecShape<T, rec_back_tok(sizeof(T))>::TENSOR;
-  if ((e = allow_shared<gated_recurrence_backward_kernel<T, MODE, WORDS>>(smem)) != cudaSuccess) return e;
+  if ((e = allow_shared<gated_recurrence_backward_kernel<T, MODE, WORDS, ANY>>(smem)) != cudaSuccess) return e;
   const long long items = a.items;
-  if ((e = launch_early(gated_recurrence_backward_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, (long long)blocks(MODE, sizeof(T)) * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
+  if ((e = launch_early(gated_recurrence_backward_kernel<T, MODE, WORDS, ANY>, dim3((unsigned)std::min<long long>(items, (long long)blocks(MODE, sizeof(T)) * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
   return launched();
+}
+template <class T, int MODE>
+cudaError_t launch_mode(const RecArgs& a, cudaStream_t stream) {
+  const bool any = rec_access<T>(a.x, a.ld_x) != kRecWide || rec_access<T>(a.g, a.ld_g) != kRecWide || rec_access<T>(a.dy, a.ld_dy) != kRecWide;
+  if (a.words) return any ? launch_one<T, MODE, true, true>(a, stream) : launch_one<T, MODE, true, false>(a, stream);
+  return any ? launch_one<T, MODE, false, true>(a, stream) : launch_one<T, MODE, false, false>(a, stream);
 }
 template <class T>
 cudaError_t launch_type(const RecArgs& a, cudaStream_t stream) {
-  const bool w = a.words != nullptr;
-  switch (a.mode) {
-    case kRecDecay: return w ? launch_one<T, kRecDecay, true>(a, stream) : launch_one<T, kRecDecay, false>(a, stream);
-    case kRecNormed: return w ? launch_one<T, kRecNormed, true>(a, stream) : launch_one<T, kRecNormed, false>(a, stream);
-    default: return w ? launch_one<T, kRecGate, true>(a, stream) : launch_one<T, kRecGate, false>(a, stream);
-  }
+  return a.mode == kRecDecay ? launch_mode<T, kRecDecay>(a, stream) : a.mode == kRecNormed ? launch_mode<T, kRecNormed>(a, stream) : launch_mode<T, kRecGate>(a, stream);
 }
 
 }  // namespace

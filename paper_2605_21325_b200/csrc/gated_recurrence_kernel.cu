@@ -17,7 +17,8 @@ namespace tri_inv {
 namespace {
 
 constexpr int kTok = kRecTok, kBlocks = 4;   // tokens of a lane; blocks an SM: 96 registers a thread
-template <class T, int MODE, bool WORDS>
+// ANY: some input cannot be moved 16 bytes at a time
+template <class T, int MODE, bool WORDS, bool ANY>
 __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(const __grid_constant__ RecArgs a) {
   using Shape = RecShape<T, kTok>;
   using Lane = RecLane<T>;
@@ -28,6 +29,7 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
   __shared__ __align__(8) float2 total[2][CH];              // ... of the tile
   __shared__ __align__(8) float entry[2][CH];               // what enters a tile
   __shared__ RecAt ring[kRecRing];
+  __shared__ __align__(4) unsigned char rest[ANY ? 2 : 1][2][kRecWarps][ANY && es == 2 ? 4 * Shape::WARP_TOK : 4];   // of rows at odd places (RecShape)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int items = a.items;
   RecFeed<WORDS, TILE, 3, false> feed{a, {(int)(a.ld_x * es), (int)(a.ld_g * es), (int)(a.ld_y * es)}, es};
@@ -86,8 +88,9 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
 
   const T *X = (const T*)a.x, *G = (const T*)a.g;
   T* Y = (T*)a.y;
-  const int x_access = rec_access<T>(X, a.ld_x), g_access = rec_access<T>(G, a.ld_g), y_access = rec_access<T>(Y, a.ld_y);
-  const bool wide = x_access == kRecWide && g_access == kRecWide, plain = y_access <= (es == 4 ? kRecWide : kRecFours);   // whole lanes can be written
+  const int x_access = ANY ? rec_access<T>(X, a.ld_x) : (int)kRecWide, g_access = ANY ? rec_access<T>(G, a.ld_g) : (int)kRecWide, y_access = rec_access<T>(Y, a.ld_y);
+  const bool plain = y_access <= (es == 4 ? kRecEights : kRecFours);   // whole lanes can be written
+  const bool odd = x_access == kRecSingle || g_access == kRecSingle;
   const int first = warp * Shape::WARP_TOK;   // of the warp's tokens
   const char *x_from = (const char*)X + Shape::copy_from(a.ld_x, first), *g_from = (const char*)G + Shape::copy_from(a.ld_g, first);
   const uint32_t warp_smem = (uint32_t)__cvta_generic_to_shared(stages) + warp * Shape::WARP_BYTES;
@@ -95,9 +98,12 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
   auto request = [&](const RecAt& t, int stage) {
     if (t.item < items) {
       const uint32_t to = warp_smem + stage * 2 * Shape::TENSOR;
-      if (t.whole && wide) {
+      if (!ANY && t.whole) {
         Shape::request_whole(to, x_from + t.at[0], a.ld_x);
         Shape::request_whole(to + Shape::TENSOR, g_from + t.at[1], a.ld_g);
+      } else if (ANY && t.whole) {
+        Shape::request_any(to, (uint32_t)__cvta_generic_to_shared(rest[ANY ? stage : 0][0][warp]), a, X, t, 0, a.ld_x, first, x_access);
+        Shape::request_any(to + Shape::TENSOR, (uint32_t)__cvta_generic_to_shared(rest[ANY ? stage : 0][1][warp]), a, G, t, 1, a.ld_g, first, g_access);
       } else {
         Shape::request(to, X, a.ld_x, t.tok0 + first, t.n - first, t.c0, a.D, x_access);
         Shape::request(to + Shape::TENSOR, G, a.ld_g, t.tok0 + first, t.n - first, t.c0, a.D, g_access);
@@ -113,6 +119,12 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
     request(ring[(i + 1) & (kRecRing - 1)], (i + 1) & 1);
     rec_wait<1>();
     __syncwarp();
+    if (ANY && odd) {
+      unsigned char* rows = stages + (i & 1) * 2 * Shape::TENSOR + warp * Shape::WARP_BYTES;
+      Shape::settle_any(rows, rest[ANY ? i & 1 : 0][0][warp], a, X, t, 0, a.ld_x, first, x_access);
+      Shape::settle_any(rows + Shape::TENSOR, rest[ANY ? i & 1 : 0][1][warp], a, G, t, 1, a.ld_g, first, g_access);
+      __syncwarp();
+    }
     const unsigned char* sx = stages + (i & 1) * 2 * Shape::TENSOR + warp * Shape::WARP_BYTES + Shape::place();
     Pair av[kTok], uv[kTok];
 #pragma unroll
@@ -176,6 +188,14 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
           h = fma2(av[k], h, uv[k]);
           *reinterpret_cast<Raw*>(row + (unsigned long long)step * k) = Lane::pack(h);
         }
+      } else if (t.whole && !resets) {   // by single values
+        T* row = Y + (long long)(t.tok0 + first + Shape::group() * kTok) * a.ld_y + t.c0 + Shape::channel();
+#pragma unroll
+        for (int k = 0; k < kTok; ++k) {
+          h = fma2(av[k], h, uv[k]);
+          rec_store(row, 0, 2, kRecSingle, h);
+          row += a.ld_y;
+        }
       } else {
         T* row = Y + (long long)(t.tok0 + first + Shape::group() * kTok) * a.ld_y;
 #pragma unroll
@@ -235,25 +255,26 @@ __global__ void __launch_bounds__(256) rec_setup_kernel(const __grid_constant__ 
   }
 }
 
-template <class T, int MODE, bool WORDS>
+template <class T, int MODE, bool WORDS, bool ANY>
 cudaError_t launch_one(const RecArgs& a, cudaStream_t stream) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess || (e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
   constexpr size_t smem = 4 * (size_t)RecShape<T, kTok>::TENSOR;   // two tiles of two tensors
-  if ((e = allow_shared<gated_recurrence_kernel<T, MODE, WORDS>>(smem)) != cudaSuccess) return e;
+  if ((e = allow_shared<gated_recurrence_kernel<T, MODE, WORDS, ANY>>(smem)) != cudaSuccess) return e;
   const long long items = a.items;
-  if ((e = launch_early(gated_recurrence_kernel<T, MODE, WORDS>, dim3((unsigned)std::min<long long>(items, (long long)kBlocks * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
+  if ((e = launch_early(gated_recurrence_kernel<T, MODE, WORDS, ANY>, dim3((unsigned)std::min<long long>(items, (long long)kBlocks * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
   return launched();
+}
+template <class T, int MODE>
+cudaError_t launch_mode(const RecArgs& a, cudaStream_t stream) {
+  const bool any = rec_access<T>(a.x, a.ld_x) != kRecWide || rec_access<T>(a.g, a.ld_g) != kRecWide;
+  if (a.words) return any ? launch_one<T, MODE, true, true>(a, stream) : launch_one<T, MODE, true, false>(a, stream);
+  return any ? launch_one<T, MODE, false, true>(a, stream) : launch_one<T, MODE, false, false>(a, stream);
 }
 template <class T>
 cudaError_t launch_type(const RecArgs& a, cudaStream_t stream) {
-  const bool w = a.words != nullptr;
-  switch (a.mode) {
-    case kRecDecay: return w ? launch_one<T, kRecDecay, true>(a, stream) : launch_one<T, kRecDecay, false>(a, stream);
-    case kRecNormed: return w ? launch_one<T, kRecNormed, true>(a, stream) : launch_one<T, kRecNormed, false>(a, stream);
-    default: return w ? launch_one<T, kRecGate, true>(a, stream) : launch_one<T, kRecGate, false>(a, stream);
-  }
+  return a.mode == kRecDecay ? launch_mode<T, kRecDecay>(a, stream) : a.mode == kRecNormed ? launch_mode<T, kRecNormed>(a, stream) : launch_mode<T, kRecGate>(a, stream);
 }
 
 }  // namespace
