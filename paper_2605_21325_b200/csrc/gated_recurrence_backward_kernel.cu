@@ -1,10 +1,10 @@
 // Gated linear recurrence: the gradient's walk, from the last tile to the first.
 //
 // As the forward walk, with what tokens pass on in the place of the state: the words join (P, C) from behind.  The states are formed again in fp32 from the one carried into the tile, so that the forward call's outputs, rounded to
-// their type, play no part, and dY, X and G are all that is read (10 bytes a value in bf16; with the outputs kept it would be 12).  x and dy stay in shared memory for the second pass; the weights w of the gated forms are
-// formed for half the tokens at a time, the second half first, from the state in its middle.
-// What bounds it: instructions, about 30 (decay) to 45 (normed) a value, at the occupancy that a and m leave: 128 registers, three blocks an SM, against 96 and four for decay.  1 x 32768 x 4096 decay 258 us, 0.81 of a copy's
-// rate; 64 x 1024 x 2048 gate 254, 0.82; 4 x 4096 x 2560 normed 93, 0.70; fp32 0.88.  Eight tokens a lane and four blocks: 290 and 98.
+// their type, play no part, and dY, X and G are all that is read (10 bytes a value in bf16; with the outputs kept it would be 12).  x and dy stay in shared memory for the second pass; the weights w are formed for eight tokens at a
+// time, the last first, from the state in front of them.
+// What bounds it: instructions, about 30 (decay) to 45 (normed) a value, at the occupancy that a and m of sixteen tokens leave: 128 registers, three blocks an SM.  bf16: 1 x 32768 x 4096 decay 256 us, 0.81 of a copy's rate;
+// 64 x 1024 x 2048 gate 260, 0.80; 4 x 4096 x 2560 normed 100, 0.65; fp32 (eight tokens, four blocks) 0.88.  Eight tokens in bf16: 290 (gate); four blocks, with what then spills, 285 (decay).
 #include <algorithm>
 
 #include "gated_recurrence.cuh"
@@ -12,8 +12,8 @@
 namespace tri_inv {
 namespace {
 
-// Blocks an SM: those for which the tokens of a lane find room in registers (decay holds no m)
-__host__ __device__ constexpr int blocks(int mode, int bytes) { return mode != kRecDecay && bytes == 2 ? 3 : 4; }
+// Blocks an SM: those for which the tokens of a lane find room in registers
+__host__ __device__ constexpr int blocks(int bytes) { return bytes == 2 ? 3 : 4; }
 
 // w: what multiplies e in dg, from the state in front of the token.  SAFE: where m may be zero
 template <int MODE, bool SAFE>
@@ -36,8 +36,8 @@ __device__ __forceinline__ Pair none_where_zero(Pair a, Pair v) {
 
 // ANY: some input cannot be moved 16 bytes at a time
 template <class T, int MODE, bool WORDS, bool ANY>
-__global__ void __launch_bounds__(kRecThreads, blocks(MODE, sizeof(T))) gated_recurrence_backward_kernel(const __grid_constant__ RecArgs a) {
-  constexpr int kTok = rec_back_tok(sizeof(T)), kPart = MODE == kRecDecay || kTok == 8 ? kTok : kTok / 2;   // tokens that are finished at a time
+__global__ void __launch_bounds__(kRecThreads, blocks(sizeof(T))) gated_recurrence_backward_kernel(const __grid_constant__ RecArgs a) {
+  constexpr int kTok = rec_back_tok(sizeof(T)), kPart = 8;   // tokens of a lane; those that are finished at a time
   using Shape = RecShape<T, kTok>;
   using Lane = RecLane<T>;
   using Raw = typename Lane::Raw;
@@ -268,7 +268,7 @@ cudaError_t launch_one(const RecArgs& a, cudaStream_t stream) {
   constexpr size_t smem = 6 * (size_t)RecShape<T, rec_back_tok(sizeof(T))>::TENSOR;
   if ((e = allow_shared<gated_recurrence_backward_kernel<T, MODE, WORDS, ANY>>(smem)) != cudaSuccess) return e;
   const long long items = a.items;
-  if ((e = launch_early(gated_recurrence_backward_kernel<T, MODE, WORDS, ANY>, dim3((unsigned)std::min<long long>(items, (long long)blocks(MODE, sizeof(T)) * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
+  if ((e = launch_early(gated_recurrence_backward_kernel<T, MODE, WORDS, ANY>, dim3((unsigned)std::min<long long>(items, (long long)blocks(sizeof(T)) * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
   return launched();
 }
 template <class T, int MODE>
