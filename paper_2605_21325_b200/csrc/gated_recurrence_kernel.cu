@@ -3,7 +3,7 @@
 // One pass: every value is read once, by asynchronous copies one tile ahead, and every output written once.  A block of five warps takes a tile of 128 tokens and 32 channels.  Four warps hold 32 tokens each in
 // registers (two lane groups of 16 tokens, two channels a lane), as a and u, form their maps and meet; the fifth, a lane for each channel, meanwhile looks for what enters the tile in the words of the tiles in front of it;
 // then the four write h.  Long sequences are spread over the chip that way: a tile's own map is there for the tiles behind it as soon as it has been read.
-// What bounds it: with all channels of a large batch bytes (64 x 1024 tokens x 2048 channels, gate, bf16 147 us, 0.85 of a copy's rate; fp32 0.9); on the way instructions, about 23 (decay) to 29 (normed) a value, and registers: a
+// What bounds it: with all channels of a large batch bytes (64 x 1024 tokens x 2048 channels, gate, bf16 147 us, 0.85 of a copy's rate; fp32 0.9); on the way instructions, 25 (decay) to 30 (normed) a value, and registers: a
 // and u of 16 tokens and two channels are 64, which leaves four blocks an SM.  Long walks over few channels wait for one another (1 x 65536 x 256 43 us, 0.37).
 // Why this shape, in us (1 x 32768 x 4096 decay | 4 x 4096 x 2560 normed | 64 x 1024 x 2048 gate; 125 | 39 | 125 of memory time): 64 x 64 tiles, every warp waiting for the entry 497 | 143; channels' threads
 // aside and the next tile read meanwhile 231 | 90; 128 x 64 tiles of sixteen tokens a lane, places worked out once a tile 184 | 79 (eight tokens 30 % more instructions: the fixed cost of a warp's tile, about
