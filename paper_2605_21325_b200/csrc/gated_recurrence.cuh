@@ -45,6 +45,8 @@ struct RecTile {
 
 // Where the words of a sequence's tiles, and its carried states, begin: sequences of any length leave no two tiles at one place.
 __host__ __device__ __forceinline__ long long rec_slot(long long tok0, int seq, int tile) { return tok0 / tile + seq; }
+// Channel c of row `row` of an array of D values a row, as the words, the carried states and the states are: a row's number times D may pass 2^31.
+__host__ __device__ __forceinline__ long long rec_at(long long row, int D, int c) { return row * D + c; }
 
 struct RecArgs {
   const void *x, *g, *dy;          // dy: gradient only

@@ -68,10 +68,10 @@ __global__ void __launch_bounds__(kRecThreads, blocks(sizeof(T))) gated_recurren
       if (lane == 0) feed.ask();
       const int c = t.c0 + lane, behind = t.tiles - 1 - t.index;
       const bool in = c < a.D, first = t.index == 0, last = behind == 0;
-      const long long at = t.slot * a.D + c, state = (long long)t.seq * a.D + c;
+      const long long at = rec_at(t.slot, a.D, c), state = rec_at(t.seq, a.D, c);
       float h = 0.f, e = 0.f;
       if (in) {
-        if (!first) h = a.carries[(rec_slot(t.begin, t.seq, kRecCarry) + (long long)t.index * (TILE / kRecCarry) - 1) * a.D + c];
+        if (!first) h = a.carries[rec_at(rec_slot(t.begin, t.seq, kRecCarry) + (long long)t.index * (TILE / kRecCarry) - 1, a.D, c)];
         else if (a.h0) h = a.h0[state];
         if (last) e = a.dh ? a.dh[state] : 0.f;
         else e = WORDS ? rec_look_back(a.words + at + a.D, -(long long)a.D, behind, limit, a.status) : carried;
@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kRecThreads, blocks(sizeof(T))) gated_recurren
         TC = rec_step(p, TC, back[i & 1][w][lane]);
       }
       total[i & 1][lane] = make_float2(TP, TC);
-      if (WORDS && t.index > 0 && t.index + 1 < t.tiles && t.c0 + lane < a.D) rec_post(a.words + (long long)t.slot * a.D + t.c0 + lane, TP, TC);
+      if (WORDS && t.index > 0 && t.index + 1 < t.tiles && t.c0 + lane < a.D) rec_post(a.words + rec_at(t.slot, a.D, t.c0 + lane), TP, TC);
     }
     rec_meet<kRecEntry, kRecThreads>();
     const float4 e0 = *reinterpret_cast<const float4*>(&entry[i & 1][Shape::channel()]);

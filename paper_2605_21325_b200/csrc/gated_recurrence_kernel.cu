@@ -50,10 +50,10 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
       if (lane == 0) feed.ask();
       const int c = t.c0 + lane, index = t.index;
       const bool in = c < a.D, first = index == 0, last = index + 1 == t.tiles;
-      const long long at = (long long)t.slot * a.D + c;
+      const long long at = rec_at(t.slot, a.D, c);
       float h = 0.f;
       if (in) {
-        if (first) h = a.h0 ? a.h0[(long long)t.seq * a.D + c] : 0.f;
+        if (first) h = a.h0 ? a.h0[rec_at(t.seq, a.D, c)] : 0.f;
         else h = WORDS ? rec_look_back(a.words + at - a.D, a.D, index, limit, a.status) : carried;
       }
       entry[i & 1][lane] = h;
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
       const float2 map = total[i & 1][lane];
       const float s = rec_step(map.x, h, map.y);
       if (a.carries && in) {   // those that a further token of the sequence follows; a tile's last one by its map, as its word says
-        float* to = a.carries + (rec_slot(t.begin, t.seq, kRecCarry) + (long long)index * (TILE / kRecCarry)) * a.D + c;
+        float* to = a.carries + rec_at(rec_slot(t.begin, t.seq, kRecCarry) + (long long)index * (TILE / kRecCarry), a.D, c);
         const int left = t.len - index * TILE;
         float m = h;
 #pragma unroll
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
         if (last) {
           if (a.h_out) {
             if (WORDS && !first && a.h_out == a.h0) rec_await(a.words + at - (long long)index * a.D, limit, a.status);
-            a.h_out[(long long)t.seq * a.D + c] = s;
+            a.h_out[rec_at(t.seq, a.D, c)] = s;
           }
         } else if (WORDS && !(a.test_stall && t.item == 0)) rec_post(a.words + at, 0.f, s);
       }
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
         TH = rec_step(q.x, TH, q.y);
       }
       total[i & 1][lane] = make_float2(TP, TH);
-      if (WORDS && t.index > 0 && t.index + 1 < t.tiles && t.c0 + lane < a.D) rec_post(a.words + (long long)t.slot * a.D + t.c0 + lane, TP, TH);
+      if (WORDS && t.index > 0 && t.index + 1 < t.tiles && t.c0 + lane < a.D) rec_post(a.words + rec_at(t.slot, a.D, t.c0 + lane), TP, TH);
     }
     P = twice(1.f);
     H = twice(0.f);
