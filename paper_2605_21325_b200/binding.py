@@ -679,6 +679,8 @@ def gated_recurrence_step(X, G, h, mode=REC_DECAY, slots=None, out=None, stream=
 def _heads_call(Q, K, inv_freq, positions, eps, interleaved, wq, wk):
     if Q.dim() < 3 or (K is not None and (K.dim() != Q.dim() or K.shape[:-2] != Q.shape[:-2] or K.shape[-1] != Q.shape[-1])):
         raise ValueError("Q and K must be [..., heads, d] of the same tokens and d, got %s and %s" % (tuple(Q.shape), None if K is None else tuple(K.shape)))
+    if K is not None and K.dtype != Q.dtype:
+        raise TypeError("K must be %s as Q is, got %s" % (Q.dtype, K.dtype))
     tokens, d = Q.shape[:-2], Q.shape[-1]
     n = tokens.numel()
     r = 0 if inv_freq is None else inv_freq.numel()

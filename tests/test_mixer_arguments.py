@@ -1,0 +1,22 @@
+"""Arguments of the gated recurrence and of the heads' norm that the binding has to turn away itself, because the C call could not see them: no GPU is needed."""
+import pytest
+import torch
+
+import __graft_entry__ as entry
+
+
+@pytest.fixture(scope="module")
+def bnd():
+    entry.build()
+    from paper_2605_21325_b200 import binding
+    return binding
+
+
+@pytest.mark.parametrize("q,k", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)], ids=["fp32-bf16", "bf16-fp32"])
+def test_queries_and_keys_of_different_types(bnd, q, k):
+    """One storage type goes with a call: keys of half as many bytes would be read past their end."""
+    Q, K, f = torch.zeros(2, 10, 4, 64, dtype=q), torch.zeros(2, 10, 2, 64, dtype=k), torch.zeros(32)
+    for call in (lambda **kw: bnd.qk_norm_rope(Q, K, None, None, f, **kw), lambda **kw: bnd.qk_norm_rope_backward(Q, K, Q, K, None, None, f, **kw)):
+        for kw in (dict(), dict(out=(Q, K))):
+            with pytest.raises(TypeError, match="K must be"):
+                call(**kw)
