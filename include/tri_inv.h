@@ -487,7 +487,7 @@ int tri_inv_qk_norm_rope(const void* Q, int64_t ldq, const void* K, int64_t ldk,
 /*
  * Its gradient, from dYq, dYk and the forward call's Q, K and weights: with v = R(-p) dy, rstd = 1 / sqrt(mean x^2 + eps) and u = v w
  *     dx = rstd (u - x rstd^2 mean(u x)),        dw = sum over tokens and heads of v x rstd
- * A padded token's dQ and dK are zero and it adds nothing to dw.  dwq, dwk [d], each may be NULL; summed in fp32 in an order that depends on the sizes and layouts alone.  dQ may be Q or dYq itself, dK may be K or dYk itself; otherwise outputs
+ * A padded token's dQ and dK are zero and it adds nothing to dw.  dwq, dwk [d], each may be NULL (zero where the side has no heads, or there are no tokens); summed in fp32 in an order that depends on the sizes and layouts alone.  dQ may be Q or dYq itself, dK may be K or dYk itself; otherwise outputs
  * overlap nothing.  workspace: at least tri_inv_qk_norm_rope_backward_workspace() bytes of device memory, 16-byte aligned.  Two launches (one without dwq and dwk), nothing is allocated.
  */
 int tri_inv_qk_norm_rope_backward_workspace(const tri_inv_heads_desc* desc, size_t* bytes);

@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, BACK ? 2 : 3) qk_norm_rope_kernel(co
   }
 }
 
-// The blocks' sums: a block takes 32 features of one weight
+// The blocks' sums: a block takes 32 features of one weight (of a side without heads there are none: zero)
 template <class T>
 __global__ void __launch_bounds__(1024) heads_weight_kernel(const __grid_constant__ HeadsArgs a, const __grid_constant__ HeadsPlan plan) {
   __shared__ float sums[32][33];
@@ -478,7 +478,7 @@ cudaError_t launch_kernel(const HeadsArgs& a, cudaStream_t stream) {
   }
   if constexpr (BACK) {
     if (!a.side[0].dw && !a.side[1].dw) return cudaSuccess;
-    if ((e = launch_early(heads_weight_kernel<T>, dim3((a.d + 31) / 32, a.side[1].H ? 2 : 1), 1024, 0, stream, a, p)) != cudaSuccess) return e;
+    if ((e = launch_early(heads_weight_kernel<T>, dim3((a.d + 31) / 32, a.side[1].dw ? 2 : 1), 1024, 0, stream, a, p)) != cudaSuccess) return e;
     return launched();
   }
   return cudaSuccess;

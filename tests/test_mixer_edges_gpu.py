@@ -1,0 +1,44 @@
+"""GPU tests of the gated recurrence and of the heads' norm at the edges of what their header allows."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16]
+
+
+@pytest.fixture(scope="module")
+def bnd():
+    import __graft_entry__ as entry
+    entry.build()
+    from paper_2605_21325_b200 import binding
+    torch.cuda.set_device(0)
+    return binding
+
+
+def normal(seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return lambda *s: torch.randn(*s, device="cuda", generator=g)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["fp32", "bf16"])
+@pytest.mark.parametrize("Hq,Hk", [(3, 0), (0, 3), (0, 0)])
+def test_weights_of_a_side_without_heads_have_zero_gradients(bnd, Hq, Hk, dtype):
+    """Sums over no heads, written all the same: whatever the memory held."""
+    n, d = normal(1), 64
+    Q, K = n(2, 5, Hq, d).to(dtype), n(2, 5, Hk, d).to(dtype)
+    w, f = torch.ones(d, device="cuda").to(dtype), torch.rand(32, device="cuda")
+    junk = [torch.full((d,), 7.0, dtype=dtype, device="cuda") for _ in range(8)]
+    del junk
+    for H, got in zip((Hq, Hk), bnd.qk_norm_rope_backward(Q, K, Q, K, w, w, f)[2:]):
+        assert bool((got != 0).any()) == (H > 0)
+    dw = [torch.full((d,), 7.0, dtype=dtype, device="cuda") for _ in range(2)]
+    desc = bnd.HeadsDesc(10, 5, Hq, Hk, d, 32, 0, bnd._dtype_code(w), 1e-6)
+    need = bnd._workspace("tri_inv_qk_norm_rope_backward_workspace", desc)
+    work, dQ, dK, p = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty_like(Q), torch.empty_like(K), lambda t: t.data_ptr()   # noqa: E731
+    ld = Hq * d, Hk * d
+    assert bnd.load().tri_inv_qk_norm_rope_backward(p(Q), ld[0], p(K), ld[1], p(Q), ld[0], p(K), ld[1], p(w), p(w), p(f), None, p(dQ), ld[0], p(dK), ld[1], *map(p, dw), p(work), need, desc,
+                                                    torch.cuda.current_stream().cuda_stream) == bnd.OK
+    for H, got in zip((Hq, Hk), dw):
+        assert bool((got == 0).all()) == (H == 0) and not bool((got == 7).all())
+
