@@ -344,7 +344,8 @@ __global__ void __launch_bounds__(kThreads, BACK ? 2 : 3) qk_norm_rope_kernel(co
       if constexpr (BACK) mix += __shfl_xor_sync(0xffffffffu, mix, m);
     }
     const float rstd = rsqrtf(total * over_d + a.eps);
-    const Pair rstd2 = twice(rstd), pull = twice(-rstd * rstd * rstd * (mix * over_d));
+    // (the mean first: rstd^3 alone is no normal number beyond heads of 1e-13 to 1e12, where dx is)
+    const Pair rstd2 = twice(rstd), pull = twice(-(mix * over_d * rstd) * rstd * rstd);
     const bool in = sub < now.left;
 #pragma unroll
     for (int k = 0; k < NU; ++k) {

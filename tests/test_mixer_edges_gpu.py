@@ -4,6 +4,8 @@ import torch
 
 pytestmark = pytest.mark.gpu
 
+ULP = 2.0 ** -24
+STORE = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
 DTYPES = [torch.float32, torch.bfloat16]
 
 
@@ -42,3 +44,19 @@ def test_weights_of_a_side_without_heads_have_zero_gradients(bnd, Hq, Hk, dtype)
     for H, got in zip((Hq, Hk), dw):
         assert bool((got == 0).all()) == (H == 0) and not bool((got == 7).all())
 
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["fp32", "bf16"])
+@pytest.mark.parametrize("d", [64, 7])
+def test_gradient_of_small_and_large_heads_without_eps(bnd, d, dtype):
+    """Heads of 1e-17 to 1e17: squares, their sum and the gradient are normal numbers of fp32, and so is all that lies between.  48 roundings, as the gradient's other tests count them."""
+    n = normal(5)
+    scale = 10.0 ** torch.tensor([-17.0, -14.0, -13.0, -9.0, 0.0, 9.0, 13.0, 15.0, 17.0], device="cuda")
+    Q, dQ = (n(1, 9, 2, d) * scale[:, None, None]).to(dtype), n(1, 9, 2, d).to(dtype)
+    w = (1 + 0.2 * n(d)).to(dtype)
+    got = bnd.qk_norm_rope_backward(dQ, None, Q, None, w, None, None, eps=0.0)[0]
+    x, u = Q.double(), dQ.double() * w.double()
+    rstd = 1 / x.square().mean(-1, keepdim=True).sqrt()
+    ref = rstd * (u - x * (rstd ** 2 * (u * x).mean(-1, keepdim=True)))
+    bound = 48 * ULP * rstd * (u.abs() + x.abs() * (rstd ** 2 * (u * x).abs().mean(-1, keepdim=True)))
+    off = (got.double() - ref).abs() / (1.01 * (bound + STORE[dtype] * ref.abs()))
+    assert bool((off <= 1).all()), off.amax((0, 2, 3))
