@@ -477,7 +477,7 @@ typedef struct tri_inv_heads_desc {
 /*
  *   Q, Yq: a row of H_q heads of d values for each token, ldq, ldyq values from one row to the next (at least H_q d); K, Yk the same with H_k (0: K, wk and Yk are not used).  wq, wk [d], each may be NULL (ones);
  *   inv_freq [r] fp32 device, finite;  positions [tokens] int32 device or NULL.  A negative position is a padded token: its outputs are zero.
- * Angles are exact to 2^-25 of a turn at any position: p inv_freq / 2 pi is taken modulo 1 in 64 bits.  The rest is fp32.  Yq may be Q itself and Yk may be K itself; otherwise outputs overlap nothing
+ * Angles are exact to 2^-25 of a turn at any position and any finite frequency: p inv_freq / 2 pi is taken modulo 1 in 64 bits.  The rest is fp32, the mean square too: with eps 0 it has to be a normal number.  Yq may be Q itself and Yk may be K itself; otherwise outputs overlap nothing
  * (rows of one buffer may lie beside each other): TRI_INV_ERR_INVALID_ARG.  Pointers aligned to their type; d, r (where pairs are not interleaved), rows and pointers in
  * whole 16-byte vectors are the fastest.  One launch, nothing is allocated.
  */

@@ -8,7 +8,7 @@
 // What bounds it: bytes (4 x 4096 tokens x 32 heads of 128, bf16 46 us, 0.90 of a copy's rate; the gradient 68 us, 0.92; fp32 0.86), at 70 % of the issue slots.  On the way, forward and gradient: loads straight to registers 68 and 122 us;
 // copies ahead, but a table whose lanes met in the banks 143 and 205; the table turned 62 and 144; two features an instruction and pointers that step 52 and 109; three and two blocks an SM instead of four and three, so that nothing spills
 // 46 and 68.  Heads whose d or pairs are not whole vectors go value by value (d = 120, 59 pairs: 0.23 and 0.17).  Eight tokens of 32 heads 3.2 us on the device.
-// Angles: p f / 2 pi only counts modulo 1, so f / 2 pi is kept as a 64-bit fraction F and p F modulo 2^64 is the exact product's fraction: a position of 2^31 is as good as one of 1.
+// Angles: p f / 2 pi only counts modulo 1, so f / 2 pi is kept as a 64-bit fraction F (of any finite f: fraction()) and p F modulo 2^64 is the exact product's fraction, off by 3 p units (2^-31 of a turn) at most: a position of 2^31 is as good as one of 1.
 #include <algorithm>
 
 #include "qk_norm_rope.cuh"
@@ -125,12 +125,20 @@ __device__ __forceinline__ void request(typename Vec<T, V>::Raw* to, const T* fr
 // Steps of a warp in shared memory: of `bytes` a lane, tensor and half
 __host__ __device__ constexpr int steps(int bytes, bool back) { return bytes >= 16 || back ? 4 : 6; }
 
-// f / 2 pi modulo 1 in units of 2^-64
+// f / 2 pi modulo 1 in units of 2^-64, off by less than three of them.  1 / 2 pi (203 bits by Machin's formula) lies in pieces of 29 bits, so that each one's product with f's 24 bits is exact in fp64, and so is what
+// it has above a whole number; the fractions are summed as integers.  Small frequencies need the first two or three pieces.
 __device__ __forceinline__ unsigned long long fraction(float f) {
-  double x = (double)f * 0.15915494309189533577;
-  x -= floor(x);
-  const double hi = floor(x * 4294967296.0), lo = (x * 4294967296.0 - hi) * 4294967296.0;
-  return ((unsigned long long)hi << 32) + (unsigned long long)lo;   // (x = 1 wraps to 0)
+  constexpr double PIECES[7] = {85445659.0, 240010261.0, 88048874.0, 524801235.0, 249589169.0, 156865476.0, 119571452.0};
+  const double x = fabs((double)f);
+  unsigned long long sum = 0;
+  double scale = 0x1p-29;
+#pragma unroll
+  for (int k = 0; k < 7; ++k, scale *= 0x1p-29) {
+    if (k > 1 && x * scale < 0x1p-93) break;   // times a piece below 2^29 it is no whole unit
+    const double y = x * (PIECES[k] * scale);
+    sum += (unsigned long long)((y - floor(y)) * 0x1p64);
+  }
+  return f < 0.f ? 0 - sum : sum;
 }
 
 // The first features of the two vectors of unit p of `units`, >= d where the head has none.  Where the pairs are (i, i + r) the first r / V units are pairs of vectors, and the others two of the rest; interleaved a

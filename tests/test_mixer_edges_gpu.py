@@ -1,4 +1,6 @@
 """GPU tests of the gated recurrence and of the heads' norm at the edges of what their header allows."""
+from fractions import Fraction
+
 import pytest
 import torch
 
@@ -60,3 +62,39 @@ def test_gradient_of_small_and_large_heads_without_eps(bnd, d, dtype):
     bound = 48 * ULP * rstd * (u.abs() + x.abs() * (rstd ** 2 * (u * x).abs().mean(-1, keepdim=True)))
     off = (got.double() - ref).abs() / (1.01 * (bound + STORE[dtype] * ref.abs()))
     assert bool((off <= 1).all()), off.amax((0, 2, 3))
+
+
+def over_two_pi(bits):
+    """floor(2^bits / 2 pi), with pi = 16 arctan(1/5) - 4 arctan(1/239) (Machin)."""
+    one, pi = 1 << (bits + 64), 0
+    for c, x in ((16, 5), (-4, 239)):
+        k, term = 0, one // x
+        while term:
+            pi += c * (term // (2 * k + 1)) * (-1) ** k
+            term //= x * x
+            k += 1
+    return (one << bits) // (2 * pi)
+
+
+@pytest.mark.parametrize("f", [1e-3, -1e-3, 0.5, 1.0, -3.0, 10.0, 1000.0, -12345.678, 1e9, 3e38])
+def test_angles_at_any_position_and_frequency(bnd, f):
+    """Angles to 2^-25 of a turn (pi roundings of 2^-24 in radians), against exact ones.  x = (1, 1) without eps: the norm's root 2, two products 2, sine and cosine 2 each of |u| + |v|, two products and a sum 3:
+    12 with the angle's."""
+    BITS = 420
+    g = torch.Generator().manual_seed(6)
+    pos = torch.cat([torch.tensor([0, 1, 2 ** 31 - 1]), torch.randint(2 ** 30, 2 ** 31 - 1, (200,), generator=g), torch.randint(0, 100000, (53,), generator=g)]).to(torch.int32)
+    freq = torch.tensor([f], dtype=torch.float32)
+    exact, by = Fraction(float(freq[0])), over_two_pi(BITS)
+    turns = [int(p) * exact * by for p in pos.tolist()]                                # in 2^-BITS of a turn
+    angle = torch.tensor([float((t / 2 ** BITS) % 1) for t in turns], dtype=torch.float64) * 2 * torch.pi
+    Q = torch.ones(1, len(pos), 1, 2, device="cuda")
+    got = bnd.qk_norm_rope(Q, None, None, None, freq.cuda(), positions=pos.cuda()[None], eps=0.0)[0][0, :, 0].double().cpu()
+    want = torch.stack([angle.cos() - angle.sin(), angle.cos() + angle.sin()], -1)
+    off = (got - want).abs() / (12 * ULP * 2)
+    assert bool((off <= 1).all()), float(off.max())
+    back = bnd.qk_norm_rope_backward(torch.ones_like(Q), None, 2 * Q + torch.tensor([1.0, -1.0], device="cuda"), None, None, None, freq.cuda(), positions=pos.cuda()[None], eps=0.0)[0]
+    # v = R(-p) (1, 1) = (c + s, c - s) at x = (3, 1): mean square 5, dx = (v - x (v . x) / 10) / sqrt 5
+    v = torch.stack([angle.cos() + angle.sin(), angle.cos() - angle.sin()], -1)
+    x = torch.tensor([3.0, 1.0], dtype=torch.float64)
+    dx = (v - x * (v @ x)[:, None] / 10) / 5 ** 0.5
+    assert float((back[0, :, 0].double().cpu() - dx).abs().max()) <= 48 * ULP * (2 + 3 * 8 / 10) / 5 ** 0.5
