@@ -136,6 +136,7 @@ __device__ __forceinline__ Pair rec_exp(Pair g) {
   return pair(rec_power(t.x), rec_power(t.y));
 }
 __device__ __forceinline__ float rec_reciprocal(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float rec_at_least_zero(float x) { float y; asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(x)); return y; }   // what is not a number stays so
 __device__ __forceinline__ float rec_root(float x) { float y; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 // a and m (what multiplies x).  A state sums a's errors over as many tokens as it remembers, so near 1 they may have no preferred side: decay and normed take a = 1 - q, q = 1 - e^g = -2 sinh(g / 2) e^{g / 2}, for |g| <= 1/4 (the
@@ -152,7 +153,7 @@ __device__ __forceinline__ void rec_factors(Pair gp, Pair& a, Pair& m) {
     a = pair(nx ? near.x : far.x, ny ? near.y : far.y);
     if constexpr (MODE == kRecNormed) {
       const float2 n = both(fma2(fall, a, fall)), f = both(fma2(a, a, minus));   // a^2 - 1
-      m = pair(rec_root(fmaxf(-(nx ? n.x : f.x), 0.f)), rec_root(fmaxf(-(ny ? n.y : f.y), 0.f)));
+      m = pair(rec_root(rec_at_least_zero(-(nx ? n.x : f.x))), rec_root(rec_at_least_zero(-(ny ? n.y : f.y))));
     } else {
       m = one;
     }

@@ -4,6 +4,8 @@ from fractions import Fraction
 import pytest
 import torch
 
+import recurrence_oracle as oracle
+
 pytestmark = pytest.mark.gpu
 
 ULP = 2.0 ** -24
@@ -98,3 +100,15 @@ def test_angles_at_any_position_and_frequency(bnd, f):
     x = torch.tensor([3.0, 1.0], dtype=torch.float64)
     dx = (v - x * (v @ x)[:, None] / 10) / 5 ** 0.5
     assert float((back[0, :, 0].double().cpu() - dx).abs().max()) <= 48 * ULP * (2 + 3 * 8 / 10) / 5 ** 0.5
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["fp32", "bf16"])
+def test_gates_that_are_not_numbers_reach_the_input_s_gradient(bnd, dtype):
+    """u = sqrt(1 - a^2) x: where a is not a number neither is dx = sqrt(1 - a^2) e, although e is."""
+    n = normal(2)
+    X, G, dY = n(1, 300, 40).to(dtype), -torch.rand(1, 300, 40, device="cuda").to(dtype), n(1, 300, 40).to(dtype)
+    for t, c in ((0, 3), (77, 4), (150, 9), (299, 39)):
+        G[0, t, c] = float("nan")
+    got = bnd.gated_recurrence_backward(dY, X, G, mode=bnd.REC_NORMED, want_dh0=True)
+    for x, (r, e) in zip(got, oracle.gradient(X, G, oracle.NORMED, [300], None, dY, None)):
+        oracle.inside(x, r, e)
