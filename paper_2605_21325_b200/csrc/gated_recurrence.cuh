@@ -178,13 +178,20 @@ __device__ __forceinline__ Pair rec_step(Pair a, Pair h, Pair u) {
   const float2 x = both(a), y = both(h), z = both(u);
   return pair(rec_step(x.x, y.x, z.x), rec_step(x.y, y.y, z.y));
 }
+// The product of two maps' decays: zero where either is, whatever the other.  A decay that is not a number (or the product of an infinite one and zero) is forgotten like any state.
+__device__ __forceinline__ float rec_product(float a, float b) { return a == 0.f || b == 0.f ? 0.f : a * b; }
+__device__ __forceinline__ Pair rec_product(Pair a, Pair b) {
+  const float2 x = both(a), y = both(b), z = both(mul2(a, b));
+  return pair(x.x == 0.f || y.x == 0.f ? 0.f : z.x, x.y == 0.f || y.y == 0.f ? 0.f : z.y);
+}
 // The same of the other lane group's lane
 static_assert(kRecGroups == 2, "the lane groups of a warp join in one exchange");
 __device__ __forceinline__ Pair rec_other(Pair v) {
   const float2 f = both(v);
   return pair(__shfl_xor_sync(0xffffffffu, f.x, 16), __shfl_xor_sync(0xffffffffu, f.y, 16));
 }
-__device__ __forceinline__ bool any_zero(Pair a) { const float2 x = both(a); return x.x == 0.f || x.y == 0.f; }
+// whether a plain product of decays may hide one that is zero: it is zero itself, or no number
+__device__ __forceinline__ bool any_zero(Pair a) { const float2 x = both(a); return !(x.x > 0.f) || !(x.y > 0.f); }
 
 // How a tensor's rows are moved: 16, 8 or 4 bytes at a time (everything aligned to them), or by single values (bf16 at odd places)
 enum : int { kRecWide = 0, kRecEights = 1, kRecFours = 2, kRecSingle = 3 };

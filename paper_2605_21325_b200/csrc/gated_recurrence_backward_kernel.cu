@@ -166,6 +166,14 @@ __global__ void __launch_bounds__(kRecThreads, blocks(sizeof(T))) gated_recurren
       no_input = __any_sync(0xffffffffu, fminf(least.x, least.y) == 0.f);
     }
     if (resets) {
+      float2 least = make_float2(1.f, 1.f);
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) {
+        const float2 f = both(av[k]);
+        least = make_float2(fminf(least.x, f.x), fminf(least.y, f.y));   // (passes over what is no number)
+        if (k == kTok / 2 - 1) half_P = none_where_zero(pair(least.x, least.y), half_P);
+      }
+      P = none_where_zero(pair(least.x, least.y), P);
       H = C = twice(0.f);
 #pragma unroll
       for (int k = 0; k < kTok; ++k) {
@@ -176,7 +184,7 @@ __global__ void __launch_bounds__(kRecThreads, blocks(sizeof(T))) gated_recurren
     }
     const Pair other_P = rec_other(P), other_H = rec_other(H), other_C = rec_other(C);   // the second group's tokens come behind the first one's
     const bool second = lane >= Shape::LANES;
-    const float2 pp = both(mul2(P, other_P)), hh = both(rec_step(other_P, H, other_H)), cc = both(rec_step(P, other_C, C));
+    const float2 pp = both(rec_product(P, other_P)), hh = both(rec_step(other_P, H, other_H)), cc = both(rec_step(P, other_C, C));
     if (!second) {
       *reinterpret_cast<float4*>(&part[i & 1][warp][Shape::channel()]) = make_float4(pp.x, hh.x, pp.y, hh.y);
       *reinterpret_cast<float2*>(&back[i & 1][warp][Shape::channel()]) = cc;
@@ -187,7 +195,7 @@ __global__ void __launch_bounds__(kRecThreads, blocks(sizeof(T))) gated_recurren
 #pragma unroll
       for (int w = kRecWarps - 1; w >= 0; --w) {
         const float p = part[i & 1][w][lane].x;
-        TP *= p;
+        TP = rec_product(TP, p);
         TC = rec_step(p, TC, back[i & 1][w][lane]);
       }
       total[i & 1][lane] = make_float2(TP, TC);

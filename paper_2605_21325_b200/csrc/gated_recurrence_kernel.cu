@@ -149,13 +149,17 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
     }
     const bool resets = __any_sync(0xffffffffu, any_zero(P));   // some decay of the warp's tokens is zero
     if (resets) {
+      P = twice(1.f);
       H = twice(0.f);
 #pragma unroll
-      for (int k = 0; k < kTok; ++k) H = rec_step(av[k], H, uv[k]);
+      for (int k = 0; k < kTok; ++k) {
+        P = rec_product(P, av[k]);
+        H = rec_step(av[k], H, uv[k]);
+      }
     }
     const Pair other_P = rec_other(P), other_H = rec_other(H);   // the second group's tokens come behind the first one's
     const bool second = lane >= Shape::LANES;
-    const float2 pp = both(mul2(P, other_P)), hh = both(rec_step(other_P, H, other_H));
+    const float2 pp = both(rec_product(P, other_P)), hh = both(rec_step(other_P, H, other_H));
     if (!second) *reinterpret_cast<float4*>(&part[i & 1][warp][Shape::channel()]) = make_float4(pp.x, hh.x, pp.y, hh.y);
     rec_meet<kRecMaps, 32 * kRecWarps>();
     if (warp == kRecWarps - 1) {   // the tile's map; as a word for those behind it
@@ -163,7 +167,7 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
 #pragma unroll
       for (int w = 0; w < kRecWarps; ++w) {
         const float2 q = part[i & 1][w][lane];
-        TP *= q.x;
+        TP = rec_product(TP, q.x);
         TH = rec_step(q.x, TH, q.y);
       }
       total[i & 1][lane] = make_float2(TP, TH);
@@ -174,7 +178,7 @@ __global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(
     for (int w = 0; w < warp; ++w) {   // the tile's tokens in front of the warp's
       const float4 q = *reinterpret_cast<const float4*>(&part[i & 1][w][Shape::channel()]);
       H = rec_step(pair(q.x, q.z), H, pair(q.y, q.w));
-      P = mul2(P, pair(q.x, q.z));
+      P = rec_product(P, pair(q.x, q.z));
     }
     rec_meet<kRecEntry, kRecThreads>();
     if (Y) {

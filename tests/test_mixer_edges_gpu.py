@@ -11,6 +11,8 @@ pytestmark = pytest.mark.gpu
 ULP = 2.0 ** -24
 STORE = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
 DTYPES = [torch.float32, torch.bfloat16]
+MODES = [oracle.DECAY, oracle.NORMED, oracle.GATE]
+NAMES = {"ids": ["decay", "normed", "gate"]}
 
 
 @pytest.fixture(scope="module")
@@ -112,3 +114,49 @@ def test_gates_that_are_not_numbers_reach_the_input_s_gradient(bnd, dtype):
     got = bnd.gated_recurrence_backward(dY, X, G, mode=bnd.REC_NORMED, want_dh0=True)
     for x, (r, e) in zip(got, oracle.gradient(X, G, oracle.NORMED, [300], None, dY, None)):
         oracle.inside(x, r, e)
+
+
+def faded(a, back=False):
+    """Where a state (or, from behind, what reaches a token) is no number because of a decay that is none, and the decays since then come to less than e^-100: below 2^-149 = e^-103 it may be forgotten."""
+    out = torch.zeros_like(a, dtype=torch.bool)
+    tainted, since = out[0].clone(), torch.zeros_like(a[0])
+    for t in reversed(range(len(a))) if back else range(len(a)):
+        if back:
+            out[t] = tainted & (since < -100)
+        bad, reset = torch.isnan(a[t]), a[t] == 0
+        tainted = (tainted | bad) & ~reset
+        since = torch.where(bad, 0.0, since + torch.where(bad | reset, 1.0, a[t]).log())
+        if not back:
+            out[t] = tainted & (since < -100)
+    return out
+
+
+@pytest.mark.parametrize("T", [300, 900])
+@pytest.mark.parametrize("mode", MODES, **NAMES)
+@pytest.mark.parametrize("dtype", DTYPES, ids=["fp32", "bf16"])
+def test_resets_forget_gates_that_are_not_numbers(bnd, dtype, mode, T):
+    """A decay of zero leaves nothing of what came before it, a decay that is not a number included, and of what comes back from behind it: in the same lane's tokens, other lanes', other warps', and tiles on."""
+    D = 70
+    n = normal(3)
+    X, G, dY, h0, dh = n(1, T, D).to(dtype), n(1, T, D), n(1, T, D).to(dtype), n(1, D), n(1, D)
+    G = (G if mode == oracle.GATE else -0.2 * G.abs()).to(dtype)
+    for before, bad, reset, c in ((3, 5, 9, 0), (2, 6, 20, 1), (10, 20, 40, 2), (20, 40, 100, 3), (60, 100, 140, 4), (100, 130, 290, 5), (298, 0, 299, 6)):
+        G[0, bad, c::7] = float("nan")
+        G[0, [before, reset], c::7] = float("-inf")
+    if T > 300:
+        G[0, 200, 2::7] = float("nan")
+        G[0, 850, 2::7] = float("-inf")
+    Y, S, carries = bnd.gated_recurrence(X, G, mode=mode, h0=h0, want_carries=True)
+    f = oracle.walk(X, G, mode, [T], h0)
+    a = oracle.factors(G[0], mode)[0]
+    h_faded, e_faded = faded(a), faded(a, back=True)
+    before = torch.cat([torch.zeros_like(h_faded[:1]), h_faded[:-1]])
+    oracle.inside(torch.where(h_faded, f["h"].to(dtype), Y[0]), f["h"], f["eh"])
+    oracle.inside(S, f["state"], f["estate"])
+    assert bool(torch.isfinite(S).all()) and bool(torch.isnan(Y).any())
+    ref = oracle.gradient(X, G, mode, [T], h0, dY, dh)
+    for c in (carries, None):
+        for x, (r, e), either in zip(bnd.gated_recurrence_backward(dY, X, G, mode=mode, h0=h0, dh=dh, carries=c, want_dh0=True), ref, (e_faded, e_faded | before, torch.zeros(1, D, dtype=torch.bool, device="cuda"))):
+            oracle.inside(torch.where(either, r.to(x.dtype), x.view(r.shape)), r, e)
+        assert not bool(torch.isnan(ref[2][0]).view(-1, 7)[:, :6].any())
+    assert bnd.last_device_status() == 0
