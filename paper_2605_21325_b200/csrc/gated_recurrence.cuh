@@ -464,10 +464,11 @@ __device__ __forceinline__ void rec_await(const unsigned long long* word, unsign
   }
 }
 
-// Where warps meet: those of tokens when their maps are there; all when what enters the tile is there as well
+// Where warps meet: those of tokens when their maps are there; all when what enters the tile is there as well.  The barrier is the form that a warp's lanes have to reach together, and they may come from words that
+// each waited for by itself, or from stores of half of them.
 enum : int { kRecMaps = 1, kRecEntry = 2 };
 template <int WHICH, int THREADS>
-__device__ __forceinline__ void rec_meet() { asm volatile("bar.sync %0, %1;" ::"n"(WHICH), "n"(THREADS) : "memory"); }
+__device__ __forceinline__ void rec_meet() { __syncwarp(); asm volatile("bar.sync %0, %1;" ::"n"(WHICH), "n"(THREADS) : "memory"); }
 
 // The order of a block's tiles.  The one that it works on, the one before and those that are on their way lie in a ring in shared memory, which one thread keeps ahead.  With words the items are drawn
 // from the ticket, so that the tiles in front of a tile are done or in the hands of blocks that run; else they go by a fixed stride.

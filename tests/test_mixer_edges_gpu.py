@@ -160,3 +160,19 @@ def test_resets_forget_gates_that_are_not_numbers(bnd, dtype, mode, T):
             oracle.inside(torch.where(either, r.to(x.dtype), x.view(r.shape)), r, e)
         assert not bool(torch.isnan(ref[2][0]).view(-1, 7)[:, :6].any())
     assert bnd.last_device_status() == 0
+
+
+@pytest.mark.parametrize("D", [1, 33, 45])
+def test_channels_that_fill_part_of_a_warp(bnd, D):
+    """Long walks of channels that leave lanes without one, whose lanes wait for words for different times: right, and the same bits each time."""
+    mode, T = oracle.GATE, 4000
+    n = normal(4)
+    X, G, dY, h0, dh = n(2, T, D).bfloat16(), (n(2, T, D) + 3).bfloat16(), n(2, T, D).bfloat16(), n(2, D), n(2, D)
+    call = lambda: bnd.gated_recurrence(X, G, mode=mode, h0=h0)[:2] + bnd.gated_recurrence_backward(dY, X, G, mode=mode, h0=h0, dh=dh)   # noqa: E731
+    first = call()
+    f = oracle.walk(X, G, mode, [T] * 2, h0)
+    for x, (r, e) in zip(first, ((f["h"], f["eh"]), (f["state"], f["estate"]), *oracle.gradient(X, G, mode, [T] * 2, h0, dY, dh))):
+        oracle.inside(x, r, e)
+    for _ in range(10):
+        assert all(torch.equal(x, y) for x, y in zip(call(), first))
+    assert bnd.last_device_status() == 0
