@@ -25,6 +25,9 @@ constexpr int kRecThreads = 32 * kRecWarps + 32;                                
 constexpr int kRecTile = kRecWarps * kRecGroups * kRecTok, kRecChannels = 64 / kRecGroups;   // of a tile
 __host__ __device__ constexpr int rec_back_tile(int bytes) { return kRecWarps * kRecGroups * rec_back_tok(bytes); }
 
+// Whether so many blocks of a walk are resident on an SM together: of its 228 KB of shared memory a block takes 1 KB besides its own.
+__host__ __device__ constexpr bool rec_fit(int blocks, size_t dynamic_bytes, size_t static_bytes) { return blocks * (dynamic_bytes + static_bytes + 1024) <= 228 * 1024; }
+
 // n / d for n < 2^30 as (n m) >> (30 + L), 2^L >= d, m = ceil(2^(30 + L) / d): what m d has above 2^(30 + L) is below d <= 2^L, and n times it below 2^(30 + L), so that the quotient's floor is exact.
 struct RecDivide {
   uint32_t m;

@@ -4,7 +4,7 @@
 // their type, play no part, and dY, X and G are all that is read (10 bytes a value in bf16; with the outputs kept it would be 12).  x and dy stay in shared memory for the second pass; the weights w are formed for eight tokens at a
 // time, the last first, from the state in front of them.
 // What bounds it: instructions, 49 a value in the normed form, at the occupancy that a and m of sixteen tokens leave: 128 registers, three blocks an SM.  bf16: 1 x 32768 x 4096 decay 256 us, 0.81 of a copy's rate;
-// 64 x 1024 x 2048 gate 260, 0.80; 4 x 4096 x 2560 normed 100, 0.65; fp32 (eight tokens, four blocks) 0.88.  Eight tokens in bf16: 290 (gate); four blocks, with what then spills, 285 (decay).
+// 64 x 1024 x 2048 gate 260, 0.80; 4 x 4096 x 2560 normed 100, 0.65; fp32 (eight tokens, three blocks, which is what shared memory holds) 0.88.  Eight tokens in bf16: 290 (gate); four blocks, with what then spills, 285 (decay).
 #include <algorithm>
 
 #include "gated_recurrence.cuh"
@@ -12,8 +12,8 @@
 namespace tri_inv {
 namespace {
 
-// Blocks an SM: those for which the tokens of a lane find room in registers
-__host__ __device__ constexpr int blocks(int bytes) { return bytes == 2 ? 3 : 4; }
+// Blocks an SM: in bf16 128 registers a thread, in fp32 what shared memory holds
+constexpr int kBlocks = 3;
 
 // w: what multiplies e in dg, from the state in front of the token.  SAFE: where m may be zero
 template <int MODE, bool SAFE>
@@ -36,7 +36,7 @@ __device__ __forceinline__ Pair none_where_zero(Pair a, Pair v) {
 
 // ANY: some input cannot be moved 16 bytes at a time
 template <class T, int MODE, bool WORDS, bool ANY>
-__global__ void __launch_bounds__(kRecThreads, blocks(sizeof(T))) gated_recurrence_backward_kernel(const __grid_constant__ RecArgs a) {
+__global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_backward_kernel(const __grid_constant__ RecArgs a) {
   constexpr int kTok = rec_back_tok(sizeof(T)), kPart = 8;   // tokens of a lane; those that are finished at a time
   using Shape = RecShape<T, kTok>;
   using Lane = RecLane<T>;
@@ -274,9 +274,10 @@ cudaError_t launch_one(const RecArgs& a, cudaStream_t stream) {
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess || (e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
   constexpr size_t smem = 6 * (size_t)RecShape<T, rec_back_tok(sizeof(T))>::TENSOR;
+  static_assert(rec_fit(kBlocks, smem, 8 * 1024), "a grid of blocks that are not all resident");
   if ((e = allow_shared<gated_recurrence_backward_kernel<T, MODE, WORDS, ANY>>(smem)) != cudaSuccess) return e;
   const long long items = a.items;
-  if ((e = launch_early(gated_recurrence_backward_kernel<T, MODE, WORDS, ANY>, dim3((unsigned)std::min<long long>(items, (long long)blocks(sizeof(T)) * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
+  if ((e = launch_early(gated_recurrence_backward_kernel<T, MODE, WORDS, ANY>, dim3((unsigned)std::min<long long>(items, (long long)kBlocks * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
   return launched();
 }
 template <class T, int MODE>

@@ -4,10 +4,10 @@
 // registers (two lane groups of 16 tokens, two channels a lane), as a and u, form their maps and meet; the fifth, a lane for each channel, meanwhile looks for what enters the tile in the words of the tiles in front of it;
 // then the four write h.  Long sequences are spread over the chip that way: a tile's own map is there for the tiles behind it as soon as it has been read.
 // What bounds it: with all channels of a large batch bytes (64 x 1024 tokens x 2048 channels, gate, bf16 147 us, 0.85 of a copy's rate; fp32 0.9); on the way instructions, 25 (decay) to 30 (normed) a value, and registers: a
-// and u of 16 tokens and two channels are 64, which leaves four blocks an SM.  Long walks over few channels wait for one another (1 x 65536 x 256 43 us, 0.37).
+// and u of 16 tokens and two channels are 64, which leaves four blocks an SM (fp32 three, by shared memory: a grid of four, whose last blocks start when others end, took 27.4 us instead of 21.2 for 37 x 100 tokens x 2048, gate).  Long walks over few channels wait for one another (1 x 65536 x 256 43 us, 0.37).
 // Why this shape, in us (1 x 32768 x 4096 decay | 4 x 4096 x 2560 normed | 64 x 1024 x 2048 gate; 125 | 39 | 125 of memory time): 64 x 64 tiles, every warp waiting for the entry 497 | 143; channels' threads
 // aside and the next tile read meanwhile 231 | 90; 128 x 64 tiles of sixteen tokens a lane, places worked out once a tile 184 | 79 (eight tokens 30 % more instructions: the fixed cost of a warp's tile, about
-// 200 instructions, is shared by half as many values); four warps and 32 channels, which leaves four blocks whose waits overlap 164 | 60 | 167; the entry looked for ahead of the maps 151 | 52 | 140; carried states
+// 200 instructions, is shared by half as many values); four warps and 32 channels, which leaves (in bf16) four blocks whose waits overlap 164 | 60 | 167; the entry looked for ahead of the maps 151 | 52 | 140; carried states
 // joined in order, for equal bits, 159 | 53 | 146; decays near 1 without bias 168 | 57 | 147.  16 or 64 channels a tile were slower, as were three or five blocks.
 // Rows at odd places (4 x 2048 x 2047 gate, bf16 59 us; 25 with 2048) come as the aligned words that hold them, put in order in shared memory; by single loads 102.
 #include <algorithm>
@@ -17,10 +17,12 @@
 namespace tri_inv {
 namespace {
 
-constexpr int kTok = kRecTok, kBlocks = 4;   // tokens of a lane; blocks an SM: 96 registers a thread
+constexpr int kTok = kRecTok;   // tokens of a lane
+// Blocks an SM: four leave 96 registers a thread; fp32 has shared memory for three
+__host__ __device__ constexpr int blocks(int bytes) { return bytes == 2 ? 4 : 3; }
 // ANY: some input cannot be moved 16 bytes at a time
 template <class T, int MODE, bool WORDS, bool ANY>
-__global__ void __launch_bounds__(kRecThreads, kBlocks) gated_recurrence_kernel(const __grid_constant__ RecArgs a) {
+__global__ void __launch_bounds__(kRecThreads, blocks(sizeof(T))) gated_recurrence_kernel(const __grid_constant__ RecArgs a) {
   using Shape = RecShape<T, kTok>;
   using Lane = RecLane<T>;
   using Raw = typename Lane::Raw;
@@ -266,9 +268,10 @@ cudaError_t launch_one(const RecArgs& a, cudaStream_t stream) {
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess || (e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
   constexpr size_t smem = 4 * (size_t)RecShape<T, kTok>::TENSOR;   // two tiles of two tensors
+  static_assert(rec_fit(blocks(sizeof(T)), smem, 6 * 1024), "a grid of blocks that are not all resident");
   if ((e = allow_shared<gated_recurrence_kernel<T, MODE, WORDS, ANY>>(smem)) != cudaSuccess) return e;
   const long long items = a.items;
-  if ((e = launch_early(gated_recurrence_kernel<T, MODE, WORDS, ANY>, dim3((unsigned)std::min<long long>(items, (long long)kBlocks * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
+  if ((e = launch_early(gated_recurrence_kernel<T, MODE, WORDS, ANY>, dim3((unsigned)std::min<long long>(items, (long long)blocks(sizeof(T)) * sms)), kRecThreads, smem, stream, a)) != cudaSuccess) return e;
   return launched();
 }
 template <class T, int MODE>
