@@ -45,8 +45,10 @@ Span carries_of(const tri_inv_rec_desc* d, const void* p) { return Span{p, (__in
 // Sequences of so many tiles are walked whole, whatever the number of channels: the words cost a launch that clears them and, at each tile, the way through the L2 cache.  Longer ones go tile by tile, which
 // spreads them over the chip and lets no block be the last for long.  Measured (bf16, us, forward and gradient, tile by tile | whole): 1 x 200 tokens x 2048 channels 7.0 and 7.7 | 5.4 and 7.3; 1 x 333 x 2048 7.3 and 8.1 |
 // 6.4 and 9.0; 8 x 333 x 2048 14.6 and 21.4 | 11.2 and 21.0; 1 x 1000 x 2048 10.4 and 12.3 | 11.8 and 18.0; 1 x 4000 x 512 10.7 and 13.3 | 39 and 61; 16 x 1024 x 2048 40.5 and 73.5 | 42.6 and 77.9; 20 x 2048 x 2048
-// 88.5 and 163 | 85.6 and 170.
-constexpr int kMostWalked = 3, kMostWalkedBack = 2;
+// 88.5 and 163 | 85.6 and 170.  The gradient at three tiles: bf16 (128 tokens a tile) 1 x 333 x 2048 7.7 | 9.7 and 64 x 333 x 2048 120 | 127, against 8 x 333 x 2048 22.4 | 21.4; fp32 (64 tokens) 1 x 180 x 2048 6.7 | 6.3,
+// 8 x 180 x 2048 14.9 | 14.2, 64 x 180 x 2048 86 | 81, 200 x 180 x 256 36.4 | 34.5; at four, fp32, 1 x 250 x 2048 7.0 | 7.6, 64 x 250 x 2048 115 | 124, 1 x 250 x 333 7.7 | 12.7, against 16 x 250 x 512 12.5 | 10.0.
+constexpr int kMostWalked = 3;
+constexpr int most_walked_back(int dtype) { return dtype == TRI_INV_F32 ? 3 : 2; }
 
 // How a walk goes: tile by tile with words between the tiles, or whole sequences.
 struct RecPlan {
@@ -89,7 +91,7 @@ struct BackPlan {
 };
 int plan_back(const tri_inv_rec_desc* d, bool with_carries, BackPlan* p) {
   p->carry_bytes = with_carries ? 0 : round_up((size_t)slots_of(d, kRecCarry) * d->D * 4);
-  const int e = plan(d, rec_back_tile(d->dtype == TRI_INV_F32 ? 4 : 2), kMostWalkedBack, &p->back);
+  const int e = plan(d, rec_back_tile(d->dtype == TRI_INV_F32 ? 4 : 2), most_walked_back(d->dtype), &p->back);
   return e ? e : plan(d, kRecTile, kMostWalked, &p->front);
 }
 
