@@ -250,12 +250,26 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError("K/V must be float32 or bfloat16, got %s" % t.dtype)
 
 
+def _offsets(cu_seqlens):
+    """The sequences' offsets as the C calls take them.  What 32 bits do not hold is refused, not wrapped to other sequences."""
+    given = np.asarray(cu_seqlens)
+    if given.ndim != 1:
+        raise ValueError("cu_seqlens must have one dimension, got shape %s" % (given.shape,))
+    if given.dtype == np.int32:
+        return np.ascontiguousarray(given)
+    with np.errstate(invalid="ignore"):
+        keep = np.ascontiguousarray(given, dtype=np.int32)
+    if not np.array_equal(keep, given):
+        raise ValueError("cu_seqlens must be whole numbers of 32 bits")
+    return keep
+
+
 def make_desc(B, T, H, d_k, d_v, C, kv_dtype, cu_seqlens=None):
     """Returns (Desc, keepalive).  ``cu_seqlens`` is a host int array of n_seqs+1 offsets or None."""
     keep = None
     ptr, n_seqs = None, 0
     if cu_seqlens is not None:
-        keep = np.ascontiguousarray(np.asarray(cu_seqlens), dtype=np.int32)
+        keep = _offsets(cu_seqlens)
         ptr, n_seqs = keep.ctypes.data, len(keep) - 1
     return Desc(B, T, H, d_k, d_v, C, kv_dtype, n_seqs, ptr), keep
 
@@ -581,7 +595,7 @@ def _rec_desc(X, mode, cu_seqlens):
         raise ValueError("X must be [B, T, D], got %s" % (tuple(X.shape),))
     keep, ptr, n_seqs = None, None, 0
     if cu_seqlens is not None:
-        keep = np.ascontiguousarray(np.asarray(cu_seqlens), dtype=np.int32)
+        keep = _offsets(cu_seqlens)
         ptr, n_seqs = keep.ctypes.data, len(keep) - 1
     B, T, D = X.shape
     return RecDesc(B, T, D, _dtype_code(X), int(mode), n_seqs, ptr), keep, (B if keep is None else n_seqs, D)

@@ -1,4 +1,5 @@
 """Arguments of the gated recurrence and of the heads' norm that the binding has to turn away itself, because the C call could not see them: no GPU is needed."""
+import numpy as np
 import pytest
 import torch
 
@@ -20,3 +21,15 @@ def test_queries_and_keys_of_different_types(bnd, q, k):
         for kw in (dict(), dict(out=(Q, K))):
             with pytest.raises(TypeError, match="K must be"):
                 call(**kw)
+
+
+def test_offsets_that_32_bits_do_not_hold(bnd):
+    """They wrapped: 2^32 + 100 was a sequence of 100 tokens."""
+    X = torch.zeros(1, 300, 40)
+    for bad in ([0, 2 ** 32 + 100, 300], np.array([0, 2 ** 32 + 100, 300]), (0, -2 ** 32 + 100, 300), [0, 100.5, 300], [0, float("nan"), 300], [[0, 300]], torch.tensor([0, 2 ** 40, 300])):
+        for call in (lambda: bnd.gated_recurrence_carries(X, bad), lambda: bnd.make_desc(1, 300, 2, 64, 64, 64, bnd.F32, cu_seqlens=bad)):
+            with pytest.raises(ValueError, match="cu_seqlens"):
+                call()
+    want = bnd.gated_recurrence_carries(X, [0, 100, 300])
+    for good in ((0, 100, 300), np.array([0, 100, 300]), torch.tensor([0, 100, 300]), np.array([0, 100, 300], np.uint64), np.array([0.0, 100.0, 300.0])):
+        assert bnd.gated_recurrence_carries(X, good) == want
