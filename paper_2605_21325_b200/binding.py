@@ -637,9 +637,10 @@ def gated_recurrence(X, G, mode=REC_DECAY, h0=None, cu_seqlens=None, out=None, w
 def selftest_recurrence_wait_timeout(X, G, wait_limit_ns, out, mode=REC_DECAY):
     """tri_inv_selftest_recurrence_wait_timeout: the recurrence with short wait limits and the first tile of the first channels never announced.  ``out`` = Y."""
     desc, keep, _ = _rec_desc(X, mode, None)
+    args = [_operand(n, t, X.shape, X.dtype) for n, t in (("X", X), ("G", G), ("out", out))]
     need = _workspace("tri_inv_gated_recurrence_workspace", desc)
     work = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
-    rc = load().tri_inv_selftest_recurrence_wait_timeout(_p(X), _p(G), _p(out), _p(work), need, desc, ctypes.c_uint64(int(wait_limit_ns)), _stream(None))
+    rc = load().tri_inv_selftest_recurrence_wait_timeout(*args, _p(work), need, desc, ctypes.c_uint64(int(wait_limit_ns)), _stream(None))
     if rc != OK:
         raise TriInvError("tri_inv_selftest_recurrence_wait_timeout", rc)
     return out
