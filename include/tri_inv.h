@@ -399,7 +399,7 @@ int tri_inv_rms_norm_backward(const void* dY, const void* X, const void* w, cons
  *     TRI_INV_REC_NORMED   a = exp(g),             u = sqrt(1 - a^2) x        (0 where g >= 0)
  *     TRI_INV_REC_GATE     a = 1 / (1 + exp(-g)),  u = (1 - a) x
  * g is at most 0 in any model of the first two (-inf: the state forgets at once), but positive values are computed as given, as long as the decays' product over 128 tokens is finite.  A decay that fp32 holds only as a number below 2^-126 may count as zero.
- * Where a is zero the state is u, whatever came before it, also where that is not finite; a state that is not finite may also be forgotten where the decays' product over some tokens since is below 2^-149.
+ * Where a is zero the state is u, whatever came before it, also states that are not finite and decays that are not numbers; a state that is not finite may also be forgotten where the decays' product over some tokens since is below 2^-149.
  */
 enum { TRI_INV_REC_DECAY = 0, TRI_INV_REC_NORMED = 1, TRI_INV_REC_GATE = 2 };
 #define TRI_INV_REC_TILE 64   /* tokens from one carried state to the next */
@@ -428,8 +428,8 @@ int tri_inv_gated_recurrence(const void* X, int64_t ldx, const void* G, int64_t 
                              void* workspace, size_t workspace_bytes, const tri_inv_rec_desc* desc, void* cuda_stream);
 
 /*
- * Self-test of the give-up path: the call (dense, sequences cut, zero initial state) with every wait limited to wait_limit_ns, and the first tile of the first channels of sequence 0 never
- * announced.  The tile behind it raises TRI_INV_ERR_DEVICE_TIMEOUT in the status word and goes on with NaN: what follows the first 64 tokens there is undefined, all other output as usual.
+ * Self-test of the give-up path: the call (dense, sequences cut, zero initial state) with every wait limited to wait_limit_ns, and the first tile (128 tokens) of the first 32 channels of sequence 0 never
+ * announced.  The tile behind it raises TRI_INV_ERR_DEVICE_TIMEOUT in the status word and goes on with NaN: what those channels hold behind the first 128 tokens is undefined, all other output as usual.
  * Synchronises the stream.  TRI_INV_ERR_UNSUPPORTED where the call cuts no sequence.
  */
 int tri_inv_selftest_recurrence_wait_timeout(const void* X, const void* G, void* Y, void* workspace, size_t workspace_bytes, const tri_inv_rec_desc* desc,

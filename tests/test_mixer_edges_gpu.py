@@ -176,3 +176,29 @@ def test_channels_that_fill_part_of_a_warp(bnd, D):
     for _ in range(10):
         assert all(torch.equal(x, y) for x, y in zip(call(), first))
     assert bnd.last_device_status() == 0
+
+
+def test_the_self_test_checks_its_tensors(bnd):
+    """Refused on the host: the call has one type and one shape."""
+    X = torch.zeros(1, 400, 40, device="cuda")
+    for G, out in ((X.bfloat16(), X), (X, X.bfloat16())):
+        with pytest.raises(TypeError, match="must be"):
+            bnd.selftest_recurrence_wait_timeout(X, G, 1000, out)
+    for G, out in ((X[:, :200], X), (X, X[:, :200]), (X.cpu(), X)):
+        with pytest.raises(ValueError, match="must"):
+            bnd.selftest_recurrence_wait_timeout(X, G, 1000, out)
+    assert bnd.last_device_status() == 0
+
+
+def test_a_wait_that_runs_out_leaves_the_other_tiles_alone(bnd):
+    """The first tile of the first 32 channels is never announced: its own 128 tokens and all other channels are as usual, and what its channels hold behind it says so, as long as no product of decays could forget it."""
+    n = normal(7)
+    X, G = n(1, 400, 100).bfloat16(), (-0.5 * torch.rand(1, 400, 100, device="cuda")).bfloat16()
+    Y = torch.zeros_like(X)
+    bnd.selftest_recurrence_wait_timeout(X, G, 2_000_000, Y)
+    assert bnd.last_device_status() == bnd.ERR_DEVICE_TIMEOUT
+    f = oracle.walk(X, G, oracle.DECAY, [400], None)
+    oracle.inside(Y[0, :128, :32], f["h"][:128, :32], f["eh"][:128, :32])
+    oracle.inside(Y[0, :, 32:], f["h"][:, 32:], f["eh"][:, 32:])
+    kept = G[0, 128:, :32].double().cumsum(0) > -80                                   # e^-80 is a normal number
+    assert bool(torch.isnan(Y[0, 128:, :32])[kept].all()) and int(kept.sum()) > 5000
