@@ -250,6 +250,12 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError("K/V must be float32 or bfloat16, got %s" % t.dtype)
 
 
+def _counted(*sizes):
+    """The C calls count these in 32 bits, to which ctypes would wrap others."""
+    if max(sizes) > 0x7fffffff or min(sizes) < -0x80000000:
+        raise ValueError("sizes must be whole numbers of 32 bits, got %s" % (sizes,))
+
+
 def _offsets(cu_seqlens):
     """The sequences' offsets as the C calls take them.  What 32 bits do not hold is refused, not wrapped to other sequences."""
     given = np.asarray(cu_seqlens)
@@ -266,6 +272,7 @@ def _offsets(cu_seqlens):
 
 def make_desc(B, T, H, d_k, d_v, C, kv_dtype, cu_seqlens=None):
     """Returns (Desc, keepalive).  ``cu_seqlens`` is a host int array of n_seqs+1 offsets or None."""
+    _counted(B, T, H, d_k, d_v, C)
     keep = None
     ptr, n_seqs = None, 0
     if cu_seqlens is not None:
@@ -508,6 +515,7 @@ def linear_attention_step(Q, K, V, log_decay, S, scale=1.0, slots=None, out=None
         raise ValueError("Q and V must be [B, H, d] and S [slots, H, d_k, d_v], got %s, %s and %s" % (tuple(Q.shape), tuple(V.shape), tuple(S.shape)))
     B, H, d_k = Q.shape
     d_v, dt, f32 = V.shape[2], Q.dtype, torch.float32
+    _counted(S.shape[0])
     O = _made_for(stream, lambda: (torch.empty_like(V),))[0][0] if out is None else out
     if B == 0:
         return O
@@ -530,6 +538,7 @@ def rms_norm(X, w, eps=1e-6, residual=None, out_dtype=None, group=128, out=None,
         if made is not None:
             return _marshalled(made, "tri_inv_rms_norm")
     n, dt = X.shape[-1], X.dtype
+    _counted(n)
     code = _dtype_code(X)
     coded = out_dtype is not None and out_dtype != dt
     if coded and out_dtype != torch.float8_e4m3fn:
@@ -554,6 +563,7 @@ def rms_norm_backward(dY, X, w, eps=1e-6, dH=None, stream=None):
         if made is not None:
             return _marshalled(made, "tri_inv_rms_norm_backward")
     n, dt = X.shape[-1], X.dtype
+    _counted(n)
     code = _dtype_code(X)
     rows = X.numel() // n if n else 0
     need = _workspace("tri_inv_rms_norm_backward_workspace", rows, n)
@@ -598,6 +608,7 @@ def _rec_desc(X, mode, cu_seqlens):
         keep = _offsets(cu_seqlens)
         ptr, n_seqs = keep.ctypes.data, len(keep) - 1
     B, T, D = X.shape
+    _counted(B, T, D, int(mode))
     return RecDesc(B, T, D, _dtype_code(X), int(mode), n_seqs, ptr), keep, (B if keep is None else n_seqs, D)
 
 
@@ -679,6 +690,7 @@ def gated_recurrence_step(X, G, h, mode=REC_DECAY, slots=None, out=None, stream=
     if X.dim() != 2 or h.dim() != 2:
         raise ValueError("X must be [B, D] and h [slots, D], got %s and %s" % (tuple(X.shape), tuple(h.shape)))
     B, D = X.shape
+    _counted(B, D, h.shape[0], int(mode))
     dt = X.dtype
     Y = _made_for(stream, lambda: (torch.empty((B, D), dtype=dt, device=X.device),))[0][0] if out is None else out
     if B == 0:
@@ -699,6 +711,7 @@ def _heads_call(Q, K, inv_freq, positions, eps, interleaved, wq, wk):
     tokens, d = Q.shape[:-2], Q.shape[-1]
     n = tokens.numel()
     r = 0 if inv_freq is None else inv_freq.numel()
+    _counted(n, d, r, Q.shape[-2], 0 if K is None else K.shape[-2])
     desc = HeadsDesc(n, max(1, tokens[-1]), Q.shape[-2], 0 if K is None else K.shape[-2], d, r, int(bool(interleaved)), _dtype_code(Q), float(eps))
     return desc, [_optional("wq", wq, (d,), Q.dtype), None if K is None else _optional("wk", wk, (d,), Q.dtype), _optional("inv_freq", inv_freq, (r,), torch.float32),
                   _optional("positions", positions, tokens, torch.int32)]

@@ -33,3 +33,20 @@ def test_offsets_that_32_bits_do_not_hold(bnd):
     want = bnd.gated_recurrence_carries(X, [0, 100, 300])
     for good in ((0, 100, 300), np.array([0, 100, 300]), torch.tensor([0, 100, 300]), np.array([0, 100, 300], np.uint64), np.array([0.0, 100.0, 300.0])):
         assert bnd.gated_recurrence_carries(X, good) == want
+
+
+def test_sizes_that_32_bits_do_not_hold(bnd):
+    """They wrapped: 2^32 + 100 tokens were 100, and the others' outputs as the memory was."""
+    n, f32 = 2 ** 32 + 100, torch.float32
+    e = lambda *s, dtype=f32: torch.empty(*s, dtype=dtype, device="meta")   # noqa: E731
+    X, w = e(1, n, 1), e(1)
+    long, few = e(n, 1), e(4, 1)
+    calls = [lambda: bnd.gated_recurrence_carries(X), lambda: bnd.gated_recurrence(X, X), lambda: bnd.gated_recurrence(e(1, 5, n), e(1, 5, n)), lambda: bnd.gated_recurrence(e(1, 5, 1), e(1, 5, 1), mode=1 << 32),
+             lambda: bnd.gated_recurrence_backward(X, X, X), lambda: bnd.gated_recurrence_step(long, long, few), lambda: bnd.gated_recurrence_step(few, few, long),
+             lambda: bnd.qk_norm_rope(e(5, n, 1), None, None, None, None), lambda: bnd.qk_norm_rope(e(5, 1, 1), e(5, n, 1), None, None, None), lambda: bnd.qk_norm_rope(e(5, 1, n), None, None, None, None),
+             lambda: bnd.qk_norm_rope_backward(e(n, 1, 1), None, e(n, 1, 1), None, None, None, None), lambda: bnd.qk_norm_rope(e(5, 1, 1), None, None, None, e(n)),
+             lambda: bnd.make_desc(1, n, 2, 64, 64, 64, bnd.F32), lambda: bnd.linear_attention_step(e(4, 1, 1), e(4, 1, 1), e(4, 1, 1), w, e(n, 1, 1, 1)),
+             lambda: bnd.rms_norm(e(1, n), e(n)), lambda: bnd.rms_norm_backward(e(1, n), e(1, n), e(n))]
+    for call in calls:
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
