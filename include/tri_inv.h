@@ -417,7 +417,7 @@ typedef struct tri_inv_rec_desc {
  *   halves of one projection's output need no copy.  Pointers aligned to their type; pointers and rows that are 16-byte aligned are the fastest.  h0, h_out [n_sequences, D] fp32, each may be NULL.
  *   carries [tri_inv_gated_recurrence_carries() rows, D] fp32 or NULL: the state behind every 64th token of a sequence, for the gradient; rows that no token stands for are left as they are.
  * Y may be X or G itself, h_out may be h0 itself; otherwise no output may overlap an input or another output: TRI_INV_ERR_INVALID_ARG.  Y NULL: only the states are wanted.
- * Everything between loads and stores is fp32, and the order of the sums depends on the sizes alone: two calls give the same bits.
+ * Everything between loads and stores is fp32, and the order of the sums depends on the sizes alone: two calls of the same layout give the same bits (the gradient's last bits may differ where outputs are aligned otherwise).
  * workspace: at least tri_inv_gated_recurrence_workspace() bytes of device memory (which may be 0: then it may be NULL), 16-byte aligned, contents arbitrary; nothing else
  * may use it until the call has run.  Nothing is allocated.  Launches: one; one more where a dense call's sequences are cut, or, packed, one for every 320
  * sequences.
