@@ -3,8 +3,10 @@
 // As the forward walk, with what tokens pass on in the place of the state: the words join (P, C) from behind.  The states are formed again in fp32 from the one carried into the tile, so that the forward call's outputs, rounded to
 // their type, play no part, and dY, X and G are all that is read (10 bytes a value in bf16; with the outputs kept it would be 12).  x and dy stay in shared memory for the second pass; the weights w are formed for eight tokens at a
 // time, the last first, from the state in front of them.
-// What bounds it: instructions, 49 a value in the normed form, at the occupancy that a and m of sixteen tokens leave: 128 registers, three blocks an SM.  bf16: 1 x 32768 x 4096 decay 256 us, 0.81 of a copy's rate;
-// 64 x 1024 x 2048 gate 260, 0.80; 4 x 4096 x 2560 normed 100, 0.65; fp32 (eight tokens, three blocks, which is what shared memory holds) 0.88.  Eight tokens in bf16: 290 (gate); four blocks, with what then spills, 285 (decay).
+// What bounds it: no unit is full.  49 instructions a value (normed) take 0.56 of the issue slots at the occupancy that a and m of sixteen tokens leave, 128 registers and three blocks an SM, where the normed and gate forms spill 116
+// to 168 bytes a thread; the largest stalls are the barrier, instructions that wait for one another, and shared and local memory.  bf16: 1 x 32768 x 4096 decay 257 us, 0.81 of a copy's rate; 64 x 1024 x 2048 gate 261, 0.80;
+// 4 x 4096 x 2560 normed 101, 0.65; fp32 (eight tokens, three blocks, which is what shared memory holds) 0.88 to 0.91.  Eight tokens in bf16: 290 (gate); four blocks, which spill more, 285 (decay).
+// Rows at odd places: 4 x 2048 x 2047 gate, bf16 132 us (42 with 2048).
 #include <algorithm>
 
 #include "gated_recurrence.cuh"

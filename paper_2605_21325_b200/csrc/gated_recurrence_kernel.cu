@@ -3,12 +3,14 @@
 // One pass: every value is read once, by asynchronous copies one tile ahead, and every output written once.  A block of five warps takes a tile of 128 tokens and 32 channels.  Four warps hold 32 tokens each in
 // registers (two lane groups of 16 tokens, two channels a lane), as a and u, form their maps and meet; the fifth, a lane for each channel, meanwhile looks for what enters the tile in the words of the tiles in front of it;
 // then the four write h.  Long sequences are spread over the chip that way: a tile's own map is there for the tiles behind it as soon as it has been read.
-// What bounds it: with all channels of a large batch bytes (64 x 1024 tokens x 2048 channels, gate, bf16 147 us, 0.85 of a copy's rate; fp32 0.9); on the way instructions, 25 (decay) to 30 (normed) a value, and registers: a
-// and u of 16 tokens and two channels are 64, which leaves four blocks an SM (fp32 three, by shared memory: a grid of four, whose last blocks start when others end, took 27.4 us instead of 21.2 for 37 x 100 tokens x 2048, gate).  Long walks over few channels wait for one another (1 x 65536 x 256 43 us, 0.37).
+// What bounds it: with all channels of a large batch bytes (64 x 1024 tokens x 2048 channels, gate, bf16 148 us, 0.84 of a copy's rate; fp32 263, 0.95).  Otherwise (1 x 32768 x 4096 decay 170, 0.74; 4 x 4096 x 2560 normed
+// 58, 0.67) neither bytes nor instructions fill: 26 (decay) to 31 (normed) instructions a value take 0.55 to 0.62 of the issue slots, and the largest stall, 2.4 to 3.4 cycles an issued instruction, is the barrier where the warps
+// of tokens wait for what enters their tile, with the next one read already.  a and u of 16 tokens and two channels are 64 registers, which leaves four blocks an SM (fp32 three, by shared memory: a grid of four, whose
+// last blocks start when others end, took 27.4 us instead of 21.2 for 37 x 100 tokens x 2048, gate).  Long walks over few channels wait for one another (1 x 65536 x 256 43 us, 0.37; 1 x 16384 x 1024 normed 40, 0.39).
 // Why this shape, in us (1 x 32768 x 4096 decay | 4 x 4096 x 2560 normed | 64 x 1024 x 2048 gate; 125 | 39 | 125 of memory time): 64 x 64 tiles, every warp waiting for the entry 497 | 143; channels' threads
 // aside and the next tile read meanwhile 231 | 90; 128 x 64 tiles of sixteen tokens a lane, places worked out once a tile 184 | 79 (eight tokens 30 % more instructions: the fixed cost of a warp's tile, about
 // 200 instructions, is shared by half as many values); four warps and 32 channels, which leaves (in bf16) four blocks whose waits overlap 164 | 60 | 167; the entry looked for ahead of the maps 151 | 52 | 140; carried states
-// joined in order, for equal bits, 159 | 53 | 146; decays near 1 without bias 168 | 57 | 147.  16 or 64 channels a tile were slower, as were three or five blocks.
+// joined in order, for equal bits, 159 | 53 | 146; decays near 1 without bias 168 | 57 | 147; decays that are not numbers forgotten as states are 170 | 58 | 148.  16 or 64 channels a tile were slower, as were three or five blocks.
 // Rows at odd places (4 x 2048 x 2047 gate, bf16 59 us; 25 with 2048) come as the aligned words that hold them, put in order in shared memory; by single loads 102.
 #include <algorithm>
 

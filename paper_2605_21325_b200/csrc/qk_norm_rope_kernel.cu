@@ -5,9 +5,11 @@
 // A head is held by LANES lanes, a lane has the two halves of its pairs (two vectors of V values), so that the rotation stays in registers and the mean takes log2 LANES exchanges; a warp
 // holds 32 / LANES heads of one token at a time and goes through the token's heads with one table of sines and cosines.
 // A warp's next three steps are on their way to shared memory, each lane's vectors to a place of its own, so that nothing waits at a barrier and no register holds what is not there yet.
-// What bounds it: bytes (4 x 4096 tokens x 32 heads of 128, bf16 46 us, 0.90 of a copy's rate; the gradient 68 us, 0.92; fp32 0.86), at 70 % of the issue slots.  On the way, forward and gradient: loads straight to registers 68 and 122 us;
+// What bounds it: bytes (4 x 4096 tokens x 32 heads of 128, bf16 46 us, 0.90 of a copy's rate; the gradient 67 us, 0.93; fp32 0.86), at 69 and 63 % of the issue slots; d = 64 0.82 and 0.74, d = 256 0.79 and 0.70.
+// On the way, forward and gradient: loads straight to registers 68 and 122 us;
 // copies ahead, but a table whose lanes met in the banks 143 and 205; the table turned 62 and 144; two features an instruction and pointers that step 52 and 109; three and two blocks an SM instead of four and three, so that nothing spills
-// 46 and 68.  Heads whose d or pairs are not whole vectors go value by value (d = 120, 59 pairs: 0.23 and 0.17).  Eight tokens of 32 heads 3.2 us on the device.
+// 46 and 68.  Heads whose d or pairs are not whole 16-byte vectors go by four values (d = 96, 20 pairs: 0.44 and 0.39)
+// or by single ones (d = 120, 59 pairs: 0.22 and 0.17): the pairs' distance sets the width of the loads too.  One query and one key head a token: 0.29 and 0.34, each side works out the token's angles.  Eight tokens of 32 heads 3.2 us on the device.
 // Angles: p f / 2 pi only counts modulo 1, so f / 2 pi is kept as a 64-bit fraction F (of any finite f: fraction()) and p F modulo 2^64 is the exact product's fraction, off by 3 p units (2^-31 of a turn) at most: a position of 2^31 is as good as one of 1.
 #include <algorithm>
 
