@@ -400,6 +400,7 @@ int tri_inv_rms_norm_backward(const void* dY, const void* X, const void* w, cons
  *     TRI_INV_REC_GATE     a = 1 / (1 + exp(-g)),  u = (1 - a) x
  * g is at most 0 in any model of the first two (-inf: the state forgets at once), but positive values are computed as given, as long as the decays' product over 128 tokens is finite.  A decay that fp32 holds only as a number below 2^-126 may count as zero.
  * Where a is zero the state is u, whatever came before it, also states that are not finite and decays that are not numbers; a state that is not finite may also be forgotten where the decays' product over some tokens since is below 2^-149.
+ * That product, over up to 128 tokens, is an fp32 number: below 2^-126 it keeps fewer bits of the state before it, below 2^-149 none.
  */
 enum { TRI_INV_REC_DECAY = 0, TRI_INV_REC_NORMED = 1, TRI_INV_REC_GATE = 2 };
 #define TRI_INV_REC_TILE 64   /* tokens from one carried state to the next */
@@ -440,7 +441,7 @@ int tri_inv_selftest_recurrence_wait_timeout(const void* X, const void* G, void*
  * (c behind the last token: dh) and m the factor of x in u:
  *     e_t = dy_t + c_{t+1},    c_t = a_t e_t,    dx_t = m_t e_t,    dh0 = c_1,
  *     dg_t = e_t a_t h_{t-1}  |  e_t (a_t h_{t-1} - a_t^2 / m_t x_t)  |  e_t (h_{t-1} - x_t) a_t (1 - a_t)
- * (normed: the second term counts as 0 where m = 0; where a = 0 all of dg is 0 and nothing reaches what came before).  The states are formed again in fp32, from h0 and from `carries` as the forward call with the same X, G, h0 and sequences left
+ * (normed: the second term counts as 0 where m = 0, which it is where 1 - a^2 is below 2^-126; where a = 0 all of dg is 0 and nothing reaches what came before).  The states are formed again in fp32, from h0 and from `carries` as the forward call with the same X, G, h0 and sequences left
  * them, or, where carries is NULL, from a walk of this call's own.  dX may be X or dY itself, dG may be G or dY itself, dh0 may be dh itself (dX and dG not both dY); otherwise no output may overlap anything.
  * Types, layouts, sequences and launches as there, one launch more without carries; workspace: by the query with the same desc and whether carries are given.
  */
